@@ -1,0 +1,574 @@
+// Causal softmax attention of packed prompts with grouped heads, on tcgen05 tensor cores.
+//
+// The query heads that share a key/value head are rows of one matrix: row r of a tile is head r % group of token r / group, so a tile
+// of 128 rows holds 128 / group tokens (rounded down; the rows left over are not stored).  K and V are then read once for the whole
+// group, a short prompt still fills its rows, and the rows of a tile end within 128 / group keys of one another: little of the diagonal
+// is computed for nothing.  A work unit is kWg consecutive tiles of one key/value head; a softmax warpgroup (one thread per row)
+// works on each.  The key loop walks 80 keys a step up to the last key that the tile's last row sees.
+//
+//   warp 0       TMA producer of K and V tiles (ring)
+//   warps 1..    UMMA issuers, one per warpgroup: S = Q K^T (128 x 80) into TMEM, O += P V (128 x head_dim) in TMEM; they also load
+//                the warpgroup's Q tile (refilled as soon as its last scores are complete)
+//   warps 4..    softmax warpgroups: three at head_dim 64 (P takes S's own columns, dead once the row is in registers), two at
+//                head_dim 128 (P in columns of its own: the next scores are issued as soon as the row has been read)
+//
+// The pipeline is that of attention_rr.cuh, whose figures gave the split: what counts is the number of tiles in flight, and tensor
+// memory holds 3 x (80 + 64) or 2 x (80 + 40 + 128) columns.  At head_dim 128 a step of a tile costs the tensor pipe 640 cycles and
+// the special-function unit 640, so neither can wait for the other.
+//
+// The reference maximum only moves when the row maximum grows by more than 2^8 in the exponent; then the thread rescales
+// its O row in TMEM.  Scores, sums and O are fp32; P is rounded to the data type (bf16 or fp16: what the matrix product takes), and the
+// output once at the end.  A row's arithmetic depends on its own sequence alone, not on the unit, the packing or the SMs.
+//
+// Masked keys: their scores are replaced by -inf (P exactly 0), whatever K held.  0 x Inf is not 0, so value rows behind the
+// sequence's end are cleared in shared memory, and a row whose O is not finite although its sum is (a value row that later rows of the tile
+// see, this one does not, holds Inf or NaN) is computed again by plain fp32 loops over the keys it sees.
+#pragma once
+#include "attention_rr.cuh"
+#include "kv_cache.cuh"
+#include "ptx.cuh"
+
+namespace eas {
+
+constexpr int kPromptMaxSeqs = 128;      // sequences of one launch (kernel parameters)
+
+struct PromptParams {
+  CUtensorMap map_q;      // [tokens, heads, HD], box {64, group, 128 / group}, 128-byte swizzle
+  CUtensorMap map_k, map_v;   // [HD / 64 halves x heads, tokens, 64], box {64, 80, HD / 64}
+  const uint16_t *q, *k, *v;
+  uint16_t* out;
+  long long ld_q, ld_k, ld_v, ld_out;
+  int group, n_kv, tile_tokens;
+  float scale_log2;       // scale * log2(e)
+  int n_seqs, total_units;
+  int q0[kPromptMaxSeqs], k0[kPromptMaxSeqs], len_q[kPromptMaxSeqs], len_k[kPromptMaxSeqs];
+  int unit_prefix[kPromptMaxSeqs + 1];
+  uint32_t* status;
+  int early_launch;
+};
+
+template <int HD>
+struct PromptCfg {
+  static constexpr bool kOwnP = HD == 128;
+  static constexpr int kKeys = 80;
+  static constexpr int kWg = kOwnP ? 2 : 3;
+  static constexpr int kHalves = HD / 64;
+  static constexpr int kStages = kOwnP ? 4 : 8;
+  static constexpr int kRegsLight = kOwnP ? 112 : 80, kRegsSoftmax = kOwnP ? 192 : 144, kRegsLaunch = kOwnP ? 168 : 128;
+  static constexpr int kThreads = 128 * (1 + kWg);
+  static constexpr int kQHalf = 128 * 128;                 // 128 rows x 64 elements
+  static constexpr int kQBytes = kQHalf * kHalves;
+  static constexpr int kAtomBytes = kKeys * 128;           // 80 keys x 64 elements
+  static constexpr int kTileBytes = kAtomBytes * kHalves;
+  static constexpr int kStageBytes = 2 * kTileBytes;
+  static constexpr int kKvOff = kWg * kQBytes;
+  static constexpr int kBarOff = kKvOff + kStages * kStageBytes;
+  static constexpr int kBytes = kBarOff + 512 + 1024;      // barriers + alignment slack
+  // TMEM columns of warpgroup w
+  static constexpr int kSCol0 = kOwnP ? kWg * HD : 0, kSStride = kOwnP ? kKeys + kKeys / 2 : kKeys + HD;
+  static constexpr int kOCol0 = kOwnP ? 0 : kKeys, kOStride = kOwnP ? HD : kKeys + HD;
+  static constexpr int kPOff = kOwnP ? kKeys : 0;          // from S
+  static_assert(kBytes <= 232448, "exceeds the shared memory of an SM");
+  static_assert(kBytes > 116224, "a second CTA must not fit beside this one");
+  static_assert(kQBytes % 1024 == 0 && kAtomBytes % 1024 == 0, "tiles start on swizzle-atom boundaries");
+  static_assert(kSCol0 + (kWg - 1) * kSStride + kKeys + (kOwnP ? kKeys / 2 : HD) <= 512, "tensor memory columns");
+  // an issuer holds stage g while it waits for the first stage of the next unit, which is at most this many steps on: the tiles of a unit
+  // end at most 128 (kWg - 1) keys apart
+  static_assert((128 * (kWg - 1) + kKeys - 1) / kKeys + 1 < kStages, "the ring holds the steps between two tiles' ends");
+  static_assert(128 * kRegsLight + 128 * kWg * kRegsSoftmax <= kThreads * kRegsLaunch, "setmaxnreg budget exceeds the CTA's register allocation");
+  static_assert(kThreads * kRegsLaunch <= 65536, "registers");
+};
+
+struct PromptUnit {
+  int q0, k0, len_q, len_k, ahead, head, tile0, n_q, n_max;   // ahead: keys in front of the first query
+};
+template <int HD>
+__device__ __forceinline__ int prompt_steps(const PromptParams& p, const PromptUnit& u, int w) {      // key steps of the unit's tile w
+  const int seen = min((u.tile0 + w + 1) * p.tile_tokens, u.len_q) + u.ahead;
+  return (max(min(seen, u.len_k), 0) + PromptCfg<HD>::kKeys - 1) / PromptCfg<HD>::kKeys;
+}
+// units of a sequence from its last tiles (the costliest) to its first, the heads side by side
+template <int HD>
+__device__ __forceinline__ PromptUnit prompt_decode(const PromptParams& p, int unit, int& cursor) {
+  constexpr int NWG = PromptCfg<HD>::kWg;
+  int lo = cursor;
+  while (lo + 1 < p.n_seqs && p.unit_prefix[lo + 1] <= unit) ++lo;
+  cursor = lo;
+  PromptUnit u;
+  u.q0 = p.q0[lo];
+  u.k0 = p.k0[lo];
+  u.len_q = p.len_q[lo];
+  u.len_k = p.len_k[lo];
+  u.ahead = u.len_k - u.len_q;
+  const int tiles = (u.len_q + p.tile_tokens - 1) / p.tile_tokens, per_head = (tiles + NWG - 1) / NWG;
+  const int k = unit - p.unit_prefix[lo], back = k / p.n_kv;
+  u.head = k - back * p.n_kv;
+  u.tile0 = (per_head - 1 - back) * NWG;
+  u.n_q = min(NWG, tiles - u.tile0);
+  u.n_max = prompt_steps<HD>(p, u, u.n_q - 1);
+  return u;
+}
+
+__host__ __device__ constexpr uint32_t make_idesc_16(bool fp16, int m, int n, int a_mn, int b_mn) {
+  return make_idesc_bf16(m, n, a_mn, b_mn) & ~(fp16 ? (1u << 7) | (1u << 10) : 0u);      // A and B are both fp16 or both bf16
+}
+template <bool FP16>
+__device__ __forceinline__ uint32_t pack_16x2(float lo, float hi) {
+  if constexpr (FP16) return Pair16<__half>::pack(lo, hi);
+  else return pack_bf16x2(lo, hi);
+}
+
+// One output row again, by a whole warp (lane i: HD / 32 dims): out = sum over the keys that the row sees.  Only elements that are not
+// finite although every value that the row sees is are replaced.
+template <int HD, bool FP16>
+__device__ __noinline__ void prompt_repair(const PromptParams& p, int q_row, int q_head, int kv_head, int k0, int limit, float m, float l) {
+  constexpr int N = HD / 32;
+  const int lane = threadIdx.x & 31;
+  uint16_t* dst = p.out + q_row * p.ld_out + q_head * HD + lane * N;
+  const uint16_t* vp = p.v + k0 * p.ld_v + kv_head * HD + lane * N;
+  const uint16_t* kp = p.k + k0 * p.ld_k + kv_head * HD + lane * N;
+  float q[N], acc[N];
+  uint32_t bad = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    q[i] = load16(p.q[q_row * p.ld_q + q_head * HD + lane * N + i], FP16);
+    acc[i] = 0.f;
+    if (!isfinite(load16(dst[i], FP16))) bad |= 1u << i;
+  }
+  for (int j = 0; j < limit && __any_sync(0xffffffffu, bad != 0u); j += 8)
+    for (int e = j; e < min(j + 8, limit); ++e)
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (!isfinite(load16(vp[e * p.ld_v + i], FP16))) bad &= ~(1u << i);
+  if (!__any_sync(0xffffffffu, bad != 0u)) return;
+#pragma unroll 4
+  for (int j = 0; j < limit; ++j) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) s = fmaf(q[i], load16(kp[j * p.ld_k + i], FP16), s);
+#pragma unroll
+    for (int d = 16; d > 0; d /= 2) s += __shfl_xor_sync(0xffffffffu, s, d);
+    const float w = fast_ex2((s - m) * p.scale_log2);
+#pragma unroll
+    for (int i = 0; i < N; ++i) acc[i] = fmaf(w, load16(vp[j * p.ld_v + i], FP16), acc[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (bad & (1u << i)) dst[i] = static_cast<uint16_t>(pack_16x2<FP16>(acc[i] / l, 0.f));
+}
+
+template <int HD, bool FP16>
+__global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_kernel(const __grid_constant__ PromptParams p) {
+  using L = PromptCfg<HD>;
+  constexpr int NST = L::kStages, NWG = L::kWg, KEYS = L::kKeys;
+  constexpr bool OWN_P = L::kOwnP;
+  extern __shared__ uint8_t smem_raw_prompt[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw_prompt) + 1023) & ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBarOff);
+  uint64_t* q_full = bars;                 // [NWG]
+  uint64_t* s_full = q_full + NWG;         // [NWG] scores of a step complete (and everything issued before them)
+  uint64_t* p_ready = s_full + NWG;        // [NWG] P stored, O rescaled if it had to be
+  uint64_t* s_free = p_ready + NWG;        // [NWG] own P: the warpgroup has read the scores out of tensor memory
+  uint64_t* pv_done = s_free + NWG;        // [NWG] own P: P V of a step complete
+  uint64_t* k_full = pv_done + NWG;        // [NST]
+  uint64_t* v_full = k_full + NST;         // [NST]
+  uint64_t* kv_empty = v_full + NST;       // [NST] every issuer hands every stage back
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(kv_empty + NST);
+  volatile uint32_t* abort_flag = tmem_slot + 1;
+  static_assert((5 * NWG + 3 * NST) * 8 + 8 <= 512, "barrier area");
+
+  const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < NWG; ++i) { mbar_init(&q_full[i], 1); mbar_init(&s_full[i], 1); mbar_init(&p_ready[i], 4); mbar_init(&s_free[i], 4); mbar_init(&pv_done[i], 1); }
+    for (int i = 0; i < NST; ++i) { mbar_init(&k_full[i], 1); mbar_init(&v_full[i], 1); mbar_init(&kv_empty[i], NWG); }
+    *abort_flag = 0;
+    mbar_fence_init();
+    tma_prefetch_desc(&p.map_q);
+    tma_prefetch_desc(&p.map_k);
+    tma_prefetch_desc(&p.map_v);
+  }
+  if (warp == 1) {
+    tmem_alloc(tmem_slot, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = *tmem_slot;
+  if (p.early_launch) pdl_launch_dependents();
+  pdl_wait();
+
+  auto q_tile = [&](int w) { return smem + w * L::kQBytes; };
+  auto k_tile = [&](uint32_t s) { return smem + L::kKvOff + s * L::kStageBytes; };
+  auto v_tile = [&](uint32_t s) { return smem + L::kKvOff + s * L::kStageBytes + L::kTileBytes; };
+
+  if (warp == 0) {
+    // ------------------------------------------------------------------ K / V producer
+    setmaxnreg_dec<L::kRegsLight>();
+    if (lane == 0) {
+      uint32_t g = 0, round = 0;
+      bool ok = true;
+      int cursor = 0;
+      for (int unit = attn_unit_at(0); unit < p.total_units && ok; unit = attn_unit_at(++round)) {
+        const PromptUnit u = prompt_decode<HD>(p, unit, cursor);
+        for (int j = 0; j < u.n_max; ++j, ++g) {
+          const uint32_t s = g % NST;
+          if (!mbar_wait(&kv_empty[s], ((g / NST) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+          const int y = u.k0 + j * KEYS, z = u.head * L::kHalves;
+          mbar_expect_tx(&k_full[s], L::kTileBytes);
+          tma_load_3d(k_tile(s), &p.map_k, &k_full[s], 0, y, z);
+          mbar_expect_tx(&v_full[s], L::kTileBytes);
+          tma_load_3d(v_tile(s), &p.map_v, &v_full[s], 0, y, z);
+        }
+      }
+      // the last hand-backs of the stages: asynchronous arrivals, in before the CTA's shared memory passes to another one
+      for (uint32_t e = g; e < g + NST && ok; ++e) ok = mbar_wait(&kv_empty[e % NST], ((e / NST) & 1u) ^ 1u, abort_flag);
+      if (!ok) {
+        const long long t0 = clock64();
+        while (clock64() - t0 < 4000000) {}     // let loads in flight land before the CTA retires
+      }
+    }
+  } else if (warp <= NWG) {
+    // ------------------------------------------------------------------ UMMA issuers, one warp per warpgroup
+    // The whole warp walks the steps and one elected lane issues.  A step: P V of this step and the scores of the next one (the next
+    // unit's first, behind the last).  Every issuer sees every K/V stage of the CTA land, in order, also those past its own tile's end
+    // (which it hands back with a plain arrival), so that it never mistakes a barrier's phase for an earlier one.
+    setmaxnreg_dec<L::kRegsLight>();
+    const int w = warp - 1;
+    constexpr uint32_t idesc_s = make_idesc_16(FP16, 128, KEYS, 0, 0);     // S = Q K^T, both K-major
+    constexpr uint32_t idesc_o = make_idesc_16(FP16, 128, HD, 0, 1);       // O += P V, V is MN-major
+    const uint32_t tm_s = tmem_base + L::kSCol0 + w * L::kSStride, tm_p = tm_s + L::kPOff, tm_o = tmem_base + L::kOCol0 + w * L::kOStride;
+    uint32_t n_q = 0, n_s = 0, n_p = 0;          // Q tiles waited for, s_full phases committed, p_ready phases waited for
+    bool started = false;                        // the first scores of this unit's tile are issued already
+    bool owed = false;                           // the warpgroup still has to say that it has seen a bare commit
+    uint32_t base = 0, round = 0;                // base: ring position of the unit's first K/V tile
+    bool ok = true;
+    int cursor = 0;
+    PromptUnit un{};
+    int un_steps = 0;                            // key steps of this issuer's tile in the next unit (0: none)
+    auto look = [&](int unit) {
+      un_steps = 0;
+      if (unit < p.total_units) {
+        un = prompt_decode<HD>(p, unit, cursor);
+        if (w < un.n_q) un_steps = prompt_steps<HD>(p, un, w);
+      }
+    };
+    look(attn_unit_at(0));
+
+    auto load_q = [&](const PromptUnit& u) {
+      if (elect_one()) {
+        const int tok = u.q0 + (u.tile0 + w) * p.tile_tokens;
+        mbar_expect_tx(&q_full[w], static_cast<uint32_t>(p.tile_tokens * p.group * 128 * L::kHalves));
+#pragma unroll
+        for (int h = 0; h < L::kHalves; ++h) tma_load_3d(q_tile(w) + h * L::kQHalf, &p.map_q, &q_full[w], h * 64, u.head * p.group, tok);
+      }
+      __syncwarp();
+    };
+    auto q_landed = [&]() -> bool {
+      if (!warp_mbar_wait(&q_full[w], n_q & 1u, abort_flag)) return false;
+      ++n_q;
+      return true;
+    };
+    auto k_landed = [&](uint32_t g) -> bool { return warp_mbar_wait(&k_full[g % NST], (g / NST) & 1u, abort_flag); };
+    auto hand_back = [&](uint32_t from, uint32_t to) -> bool {   // stages past this tile's end
+      for (uint32_t g = from; g < to; ++g) {
+        if (!k_landed(g)) return false;
+        if (elect_one()) mbar_arrive(&kv_empty[g % NST]);
+        __syncwarp();
+      }
+      return true;
+    };
+    // Only the first `rows` value rows at ring position g belong to the sequence: clears the others.  Every issuer does so before
+    // its own P V; later ones store the zeros that are there already.
+    auto clear_behind = [&](uint32_t g, int rows) {
+#pragma unroll
+      for (int h = 0; h < L::kHalves; ++h) {
+        uint8_t* v = v_tile(g % NST) + h * L::kAtomBytes;
+#pragma unroll 4
+        for (int c = rows * 8 + lane; c < KEYS * 8; c += 32)      // 16-byte chunks, 8 a row
+          *reinterpret_cast<uint4*>(v + c * 16) = make_uint4(0u, 0u, 0u, 0u);
+      }
+      fence_proxy_async_smem();                                // generic-proxy stores -> visible to the tensor core's operand reads
+      __syncwarp();
+    };
+    // by the elected lane: scores of the current tile (the last one waited for) against the K tile at ring position g
+    auto mma_s = [&](uint32_t g) {
+      const uint64_t ad = make_smem_desc(smem_u32(q_tile(w)), 16, 1024, kSwizzle128B);
+      const uint64_t bd = make_smem_desc(smem_u32(k_tile(g % NST)), 16, 1024, kSwizzle128B);
+#pragma unroll
+      for (int h = 0; h < L::kHalves; ++h)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          umma_bf16_ss(tm_s, ad + h * (L::kQHalf >> 4) + 2 * k, bd + h * (L::kAtomBytes >> 4) + 2 * k, idesc_s, h != 0 || k != 0);
+      umma_commit(&s_full[w]);
+    };
+
+    for (int unit = attn_unit_at(0); unit < p.total_units && ok; unit = attn_unit_at(++round)) {
+      const PromptUnit u = un;
+      const int n_steps = un_steps;
+      look(attn_unit_at(round + 1));
+      const uint32_t next_base = base + static_cast<uint32_t>(u.n_max);
+      if (n_steps == 0) {
+        ok = hand_back(base, next_base);
+        base = next_base;
+        started = false;
+        continue;
+      }
+      const bool chain = un_steps > 0;                // the next unit's first scores follow this unit's last ones
+      if (!started) {
+        if (owed) {                              // the warpgroup has seen the bare commit, so s_full may be used again
+          if (!warp_mbar_wait(&p_ready[w], n_p & 1u, abort_flag)) { ok = false; break; }
+          ++n_p;
+        }
+        load_q(u);
+        if (!q_landed() || !k_landed(base)) { ok = false; break; }
+        if (OWN_P && n_s > 0 && !warp_mbar_wait(&s_free[w], (n_s - 1u) & 1u, abort_flag)) { ok = false; break; }
+        tc_fence_after_sync();
+        if (elect_one()) mma_s(base);
+        __syncwarp();
+        ++n_s;
+      }
+      for (int j = 0; j < n_steps; ++j) {
+        const bool last = j + 1 == n_steps;
+        const bool more = !last || chain;
+        const uint32_t g = base + static_cast<uint32_t>(j), gn = last ? next_base : g + 1;      // gn: the K tile of the scores to come
+        if (last && chain) {                     // the Q tile is free when the last scores are complete
+          if (!warp_mbar_wait(&s_full[w], (n_s - 1u) & 1u, abort_flag)) { ok = false; break; }
+          load_q(un);
+        }
+        if (last && !hand_back(g + 1, next_base)) { ok = false; break; }
+        const int rows = u.len_k - j * KEYS;     // key rows of this step that belong to the sequence
+        if (!OWN_P && !warp_mbar_wait(&v_full[g % NST], (g / NST) & 1u, abort_flag)) { ok = false; break; }
+        if (!OWN_P && rows < KEYS) clear_behind(g, rows);
+        if (more && !k_landed(gn)) { ok = false; break; }
+        if (last && chain && !q_landed()) { ok = false; break; }
+        if (OWN_P && more) {
+          if (!warp_mbar_wait(&s_free[w], (n_s - 1u) & 1u, abort_flag)) { ok = false; break; }
+          tc_fence_after_sync();
+          if (elect_one()) mma_s(gn);
+          __syncwarp();
+          ++n_s;
+        }
+        if (OWN_P && !warp_mbar_wait(&v_full[g % NST], (g / NST) & 1u, abort_flag)) { ok = false; break; }
+        if (OWN_P && rows < KEYS) clear_behind(g, rows);
+        if (!warp_mbar_wait(&p_ready[w], n_p & 1u, abort_flag)) { ok = false; break; }
+        ++n_p;
+        tc_fence_after_sync();
+        const uint64_t bd = make_smem_desc(smem_u32(v_tile(g % NST)), L::kAtomBytes, 1024, kSwizzle128B);
+        if (elect_one()) {
+#pragma unroll
+          for (int ks = 0; ks < KEYS / 16; ++ks)                 // 16 keys: 8 columns of P, 2 KB of V
+            umma_bf16_ts(tm_o, tm_p + ks * 8, bd + ks * (2048 >> 4), idesc_o, (j != 0 || ks != 0) ? 1u : 0u);
+          if (OWN_P) umma_commit(&pv_done[w]);
+          else if (more) mma_s(gn);
+          else umma_commit(&s_full[w]);                          // bare: tells the warpgroup that its O is final
+          umma_commit(&kv_empty[g % NST]);
+        }
+        __syncwarp();
+        if (!OWN_P) ++n_s;
+      }
+      started = chain;
+      owed = !OWN_P && !chain;
+      base = next_base;
+    }
+  } else if (warp < 4) {
+    setmaxnreg_dec<L::kRegsLight>();
+  } else {
+    // ------------------------------------------------------------------ softmax warpgroups
+    setmaxnreg_inc<L::kRegsSoftmax>();
+    const int w = (warp - 4) >> 2;
+    const int quarter = warp & 3;                  // TMEM lane quarter of this warp
+    const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
+    const uint32_t s_addr = lane_addr + L::kSCol0 + w * L::kSStride, p_addr = s_addr + L::kPOff, o_addr = lane_addr + L::kOCol0 + w * L::kOStride;
+    const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2);
+    const int row = quarter * 32 + lane, row_tok = row / p.group, row_head = row - row_tok * p.group;   // token of the tile, head of the group
+    uint32_t n = 0;                                // s_full phases waited for (own P: steps done)
+    bool ok = true;
+    // the finished tile whose output is still in tensor memory
+    bool pend = false;
+    int pend_q = -1, pend_head = 0, pend_k0 = 0, pend_limit = 0;   // query row (-1: not stored), key/value head, first key row, keys seen
+    float pend_l = 1.f, pend_m = 0.f;
+    auto flush_output = [&]() {
+      const float inv = pend_limit > 0 ? 1.0f / pend_l : 0.f;
+      uint4* dst = reinterpret_cast<uint4*>(p.out + static_cast<long long>(max(pend_q, 0)) * p.ld_out + (pend_head * p.group + row_head) * HD);
+      bool wrong = false;
+#pragma unroll 1
+      for (int c = 0; c < HD / 16; ++c) {
+        uint32_t o[16];
+        __syncwarp();
+        tmem_ld_32x16(o_addr + c * 16, o);
+        tmem_ld_wait_16<0>(o);
+        uint32_t pkd[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          // (Inf x 0 = NaN too: one test for both)
+          wrong = wrong || !(__uint_as_float(o[2 * i]) * 0.f + __uint_as_float(o[2 * i + 1]) * 0.f == 0.f);
+          pkd[i] = pend_limit > 0 ? pack_16x2<FP16>(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv) : 0u;
+        }
+        if (pend_q >= 0) {
+          dst[2 * c] = make_uint4(pkd[0], pkd[1], pkd[2], pkd[3]);
+          dst[2 * c + 1] = make_uint4(pkd[4], pkd[5], pkd[6], pkd[7]);
+        }
+      }
+      uint32_t todo = __ballot_sync(0xffffffffu, wrong && pend_q >= 0 && pend_limit > 0 && pend_l * 0.f == 0.f);
+      while (__builtin_expect(todo != 0u, 0)) {
+        const int src = __ffs(todo) - 1;
+        todo &= todo - 1u;
+        __syncwarp();
+        prompt_repair<HD, FP16>(p, __shfl_sync(0xffffffffu, pend_q, src), __shfl_sync(0xffffffffu, pend_head * p.group + row_head, src), pend_head,
+                                pend_k0, __shfl_sync(0xffffffffu, pend_limit, src), __shfl_sync(0xffffffffu, pend_m, src),
+                                __shfl_sync(0xffffffffu, pend_l, src));
+      }
+      __syncwarp();
+      pend = false;
+    };
+
+    int cursor = 0;
+    uint32_t round = 0;
+    for (int unit = attn_unit_at(0); unit < p.total_units && ok; unit = attn_unit_at(++round)) {
+      const PromptUnit u = prompt_decode<HD>(p, unit, cursor);
+      const int n_steps = w < u.n_q ? prompt_steps<HD>(p, u, w) : 0;
+      const int tok = (u.tile0 + w) * p.tile_tokens + row_tok;
+      const bool stored = w < u.n_q && row_tok < p.tile_tokens && tok < u.len_q;
+      if (n_steps == 0) {                           // no tile in this unit, or one that sees no key
+        if (pend) {
+          if (!warp_mbar_wait(OWN_P ? &pv_done[w] : &s_full[w], (OWN_P ? n - 1u : n) & 1u, abort_flag)) { ok = false; break; }
+          tc_fence_after_sync();
+          flush_output();
+          if (!OWN_P) {
+            ++n;
+            tc_fence_before_sync();
+            __syncwarp();
+            mbar_arrive_if(&p_ready[w], lane == 0);        // the issuer may use s_full[w] again
+          }
+        }
+        if (stored) {
+          uint4* dst = reinterpret_cast<uint4*>(p.out + (static_cast<long long>(u.q0) + tok) * p.ld_out + (u.head * p.group + row_head) * HD);
+          for (int c = 0; c < HD / 8; ++c) dst[c] = make_uint4(0u, 0u, 0u, 0u);
+        }
+        continue;
+      }
+      // keys that this row sees; rows that are not stored see all (what they compute does not matter, and masking would cost every step)
+      const int limit = stored ? max(tok + 1 + u.ahead, 0) : 0x7fffffff;
+      float m_used = 0.f;
+      uint64_t l2[2] = {0, 0};                      // row sum, two packed accumulators
+      int left = limit;                             // of them from this step on
+#pragma unroll 1
+      for (int j = 0; j < n_steps; ++j, left -= KEYS) {
+        if (!warp_mbar_wait(&s_full[w], n & 1u, abort_flag)) { ok = false; break; }
+        ++n;
+        tc_fence_after_sync();
+        if (!OWN_P && __builtin_expect(pend, 0)) flush_output();       // the previous tile's P V is complete
+        uint32_t s[KEYS];
+        tmem_ld_32x32_at<0>(s_addr, s);
+        tmem_ld_32x32_at<32>(s_addr, s);
+        tmem_ld_32x16_at<64>(s_addr, s);
+        tmem_ld_wait_16<0>(s); tmem_ld_tie_16<16>(s); tmem_ld_tie_16<32>(s); tmem_ld_tie_16<48>(s); tmem_ld_tie_16<64>(s);
+        if (OWN_P) {
+          tc_fence_before_sync();
+          __syncwarp();
+          mbar_arrive_if(&s_free[w], lane == 0);
+        }
+        if (__builtin_expect(left < KEYS, 0)) {              // keys that the row does not see
+#pragma unroll
+          for (int i = 0; i < KEYS; ++i) if (i >= left) s[i] = 0xff800000u;   // -inf
+        }
+        float mx;
+        {
+          float c0 = -INFINITY, c1 = -INFINITY, c2 = -INFINITY, c3 = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < KEYS; i += 8) {
+            c0 = fmax3(c0, __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
+            c1 = fmax3(c1, __uint_as_float(s[i + 2]), __uint_as_float(s[i + 3]));
+            c2 = fmax3(c2, __uint_as_float(s[i + 4]), __uint_as_float(s[i + 5]));
+            c3 = fmax3(c3, __uint_as_float(s[i + 6]), __uint_as_float(s[i + 7]));
+          }
+          mx = fmax3(fmaxf(c0, c1), c2, c3);
+        }
+        // the reference maximum moves only when the row maximum grew by more than the threshold (the first step: always).  A row that
+        // sees nothing keeps 0: its exponentials are those of -inf.
+        const float m_old = m_used;
+        const bool moved = (j == 0 && mx != -INFINITY) || (mx - m_used) * p.scale_log2 > kRescaleThreshold;
+        m_used = moved ? mx : m_used;
+        const uint32_t rescale = __ballot_sync(0xffffffffu, moved && j != 0);
+        const float mb = m_used * p.scale_log2;
+        const uint64_t nmb2 = pack2(-mb, -mb);
+        const uint64_t l_old[2] = {l2[0], l2[1]};
+        l2[0] = l2[1] = 0;
+        const uint32_t pv_ok = OWN_P ? mbar_try_wait(&pv_done[w], n & 1u) : 1u;      // the previous step's, tested ahead
+        uint32_t pk[KEYS / 2];
+#pragma unroll
+        for (int i = 0; i < KEYS / 2; ++i) {
+          const uint64_t t = ffma2(pack2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), scale2, nmb2);
+          float p0, p1;
+          unpack2(t, p0, p1);
+          p0 = fast_ex2(p0);
+          p1 = fast_ex2(p1);
+          l2[i & 1] = fadd2(l2[i & 1], pack2(p0, p1));
+          pk[i] = pack_16x2<FP16>(p0, p1);
+        }
+        if (OWN_P) {
+          // P goes where the previous step's was, and O may change: that step's P V has to be complete
+          if (n > 1u && !warp_mbar_wait_tested(pv_ok, &pv_done[w], n & 1u, abort_flag)) { ok = false; break; }
+          tc_fence_after_sync();
+          if (__builtin_expect(pend, 0)) flush_output();
+        }
+        if (__builtin_expect(rescale != 0u, 0)) {
+          const float corr = moved ? fast_ex2((m_old - m_used) * p.scale_log2) : 1.0f;
+          const uint64_t corr2 = pack2(corr, corr);
+          l2[0] = fadd2(fmul2(l_old[0], corr2), l2[0]);
+          l2[1] = fadd2(fmul2(l_old[1], corr2), l2[1]);
+#pragma unroll 1
+          for (int c = 0; c < HD / 8; ++c) {
+            uint32_t o[8];
+            asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3]), "=r"(o[4]), "=r"(o[5]), "=r"(o[6]), "=r"(o[7]) : "r"(o_addr + c * 8) : "memory");
+            asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(o[0]), "+r"(o[1]), "+r"(o[2]), "+r"(o[3]), "+r"(o[4]), "+r"(o[5]), "+r"(o[6]), "+r"(o[7])::"memory");
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * corr);
+            tmem_st_32x8_from(o_addr + c * 8, o);
+          }
+        } else {
+          l2[0] = fadd2(l_old[0], l2[0]);
+          l2[1] = fadd2(l_old[1], l2[1]);
+        }
+        // P row: two elements per column of this thread's lane
+        __syncwarp();
+        tmem_st_32x32_from(p_addr, pk);
+        tmem_st_32x8_from(p_addr + 32, pk + 32);
+        tmem_st_wait();
+        tc_fence_before_sync();
+        __syncwarp();
+        mbar_arrive_if(&p_ready[w], lane == 0);
+      }
+      if (!ok) break;
+      pend = true;
+      float a0, a1, a2, a3;
+      unpack2(l2[0], a0, a1);
+      unpack2(l2[1], a2, a3);
+      pend_l = (a0 + a1) + (a2 + a3);
+      pend_m = m_used;
+      pend_q = stored ? u.q0 + tok : -1;
+      pend_head = u.head;
+      pend_k0 = u.k0;
+      pend_limit = stored ? limit : 0;
+    }
+    if (ok && pend) {
+      if (warp_mbar_wait(OWN_P ? &pv_done[w] : &s_full[w], (OWN_P ? n - 1u : n) & 1u, abort_flag)) {
+        tc_fence_after_sync();
+        flush_output();
+      }
+    }
+  }
+
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem_base, 512);
+  }
+  if (threadIdx.x == 0 && *abort_flag) atomicCAS(p.status, DEV_OK, DEV_ERR_WAIT_TIMEOUT);
+}
+
+}  // namespace eas

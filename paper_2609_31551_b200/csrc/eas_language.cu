@@ -1,0 +1,331 @@
+// C ABI of the language-model operators (include/eas_language.h): checks, tensor maps, launches.
+#include "../../include/eas_language.h"
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <vector>
+
+#include "attention_cache.cuh"
+#include "attention_prompt.cuh"
+#include "host.cuh"
+#include "kv_cache.cuh"
+
+using namespace eas;
+
+static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+static constexpr double kLog2e = 1.4426950408889634;
+
+// ------------------------------------------------------------------------------------ prompts
+// [tokens, heads * HD] with token distance ld, seen as {HD, heads, tokens}: one box holds a tile's rows, the heads of a token side by side
+static eas_status prompt_q_map(CUtensorMap* m, const void* q, int heads, int hd, int64_t tokens, int64_t ld, int group, int tile_tokens) {
+  const uint64_t dims[3] = {static_cast<uint64_t>(hd), static_cast<uint64_t>(heads), static_cast<uint64_t>(tokens)};
+  const uint64_t strides[2] = {static_cast<uint64_t>(hd) * 2, static_cast<uint64_t>(ld) * 2};
+  const uint32_t box[3] = {64, static_cast<uint32_t>(group), static_cast<uint32_t>(tile_tokens)};
+  return make_tmap(m, q, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+// the same seen as {64, tokens, heads * HD / 64}: one box holds 80 keys of a head, its 64-column halves one behind the other
+static eas_status prompt_kv_map(CUtensorMap* m, const void* k, int heads, int hd, int64_t tokens, int64_t ld, int keys) {
+  const uint64_t dims[3] = {64, static_cast<uint64_t>(tokens), static_cast<uint64_t>(heads) * hd / 64};
+  const uint64_t strides[2] = {static_cast<uint64_t>(ld) * 2, 128};
+  const uint32_t box[3] = {64, static_cast<uint32_t>(keys), static_cast<uint32_t>(hd / 64)};
+  return make_tmap(m, k, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+template <int HD, bool FP16>
+static eas_status launch_prompt(PromptParams& pp, int budget, cudaStream_t stream) {
+  using L = PromptCfg<HD>;
+  static OncePerDevice once;
+  if (once.first()) {
+    CUDA_TRY(cudaFuncSetAttribute(prompt_attention_kernel<HD, FP16>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes));
+    once.settled();
+  }
+  return launch_kernel(prompt_attention_kernel<HD, FP16>, std::min(budget, pp.total_units), L::kThreads, L::kBytes, stream, pp);
+}
+
+static eas_status prompt_attention(const eas_prompt_inputs* in, int32_t sm_budget, void* stream, uint32_t* status_dev) {
+  if (in == nullptr) return fail(EAS_ERR_INVALID_ARG, "inputs are null");
+  const int H = in->n_heads, G = in->n_kv_heads, hd = in->head_dim, n = in->n_seqs;
+  if (n < 0) return fail(EAS_ERR_INVALID_ARG, "n_seqs %d", n);
+  if (in->cu_q == nullptr || in->cu_k == nullptr || status_dev == nullptr) return fail(EAS_ERR_INVALID_ARG, "a required pointer is null");
+  if (in->dtype != EAS_DTYPE_BF16 && in->dtype != EAS_DTYPE_FP16) return fail(EAS_ERR_UNSUPPORTED, "dtype %d", in->dtype);
+  if (hd != 64 && hd != 128) return fail(EAS_ERR_UNSUPPORTED, "head_dim %d (supported: 64, 128)", hd);
+  if (H <= 0 || G <= 0 || H % G != 0) return fail(EAS_ERR_INVALID_ARG, "%d query heads for %d key/value heads", H, G);
+  if (H / G > 128) return fail(EAS_ERR_UNSUPPORTED, "%d query heads per key/value head (at most 128)", H / G);
+  if (!(in->scale > 0.0f) || !std::isfinite(in->scale)) return fail(EAS_ERR_INVALID_ARG, "scale must be positive and finite");
+  if (in->cu_q[0] < 0 || in->cu_k[0] < 0) return fail(EAS_ERR_INVALID_ARG, "cu_q and cu_k start at 0 or above");
+  for (int i = 0; i < n; ++i)
+    if (in->cu_q[i + 1] < in->cu_q[i] || in->cu_k[i + 1] < in->cu_k[i])
+      return fail(EAS_ERR_INVALID_ARG, "cu_q or cu_k decreases at sequence %d", i);
+  const int64_t Tq = in->cu_q[n], Tk = in->cu_k[n], wq = static_cast<int64_t>(H) * hd, wk = static_cast<int64_t>(G) * hd;
+  if (Tq > in->cu_q[0]) {
+    if (in->q == nullptr || in->out == nullptr || (Tk > 0 && (in->k == nullptr || in->v == nullptr)))
+      return fail(EAS_ERR_INVALID_ARG, "a required pointer is null");
+    if (!aligned16(in->q) || !aligned16(in->out) || (Tk > 0 && (!aligned16(in->k) || !aligned16(in->v))))
+      return fail(EAS_ERR_INVALID_ARG, "q, k, v and out must be 16-byte aligned");
+    if (in->ld_q < wq || in->ld_out < wq || in->ld_q % 8 != 0 || in->ld_out % 8 != 0 ||
+        (Tk > 0 && (in->ld_k < wk || in->ld_v < wk || in->ld_k % 8 != 0 || in->ld_v % 8 != 0)))
+      return fail(EAS_ERR_INVALID_ARG, "token distances must be multiples of 8 that hold a token's heads");
+  }
+  int budget = 0;
+  EAS_TRY(resolve_budget(sm_budget, &budget));
+  if (Tq == in->cu_q[0]) return EAS_OK;                          // no query
+
+  PromptParams pp{};
+  pp.group = H / G; pp.n_kv = G; pp.tile_tokens = 128 / pp.group;
+  EAS_TRY(prompt_q_map(&pp.map_q, in->q, H, hd, Tq, in->ld_q, pp.group, pp.tile_tokens));
+  if (Tk > 0) {
+    EAS_TRY(prompt_kv_map(&pp.map_k, in->k, G, hd, Tk, in->ld_k, PromptCfg<64>::kKeys));
+    EAS_TRY(prompt_kv_map(&pp.map_v, in->v, G, hd, Tk, in->ld_v, PromptCfg<64>::kKeys));
+  } else {                                                       // (no key at all: no tile is ever loaded)
+    pp.map_k = pp.map_v = pp.map_q;
+  }
+  static_assert(PromptCfg<64>::kKeys == PromptCfg<128>::kKeys, "one box for both");
+  pp.q = static_cast<const uint16_t*>(in->q); pp.k = static_cast<const uint16_t*>(in->k); pp.v = static_cast<const uint16_t*>(in->v);
+  pp.out = static_cast<uint16_t*>(in->out);
+  pp.ld_q = in->ld_q; pp.ld_k = in->ld_k; pp.ld_v = in->ld_v; pp.ld_out = in->ld_out;
+  pp.scale_log2 = static_cast<float>(in->scale * kLog2e);
+  pp.status = status_dev;
+  const int wg = hd == 64 ? PromptCfg<64>::kWg : PromptCfg<128>::kWg;
+  std::vector<int> order;                                        // longest first (stable): the tail of the static deal is short work
+  for (int i = 0; i < n; ++i)
+    if (in->cu_q[i + 1] > in->cu_q[i]) order.push_back(i);
+  std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return in->cu_k[a + 1] - in->cu_k[a] > in->cu_k[b + 1] - in->cu_k[b]; });
+  const int rows = static_cast<int>(order.size());
+  for (int first = 0; first < rows; first += kPromptMaxSeqs) {
+    pp.n_seqs = std::min(kPromptMaxSeqs, rows - first);
+    int64_t units = 0;
+    for (int j = 0; j < pp.n_seqs; ++j) {
+      const int i = order[first + j];
+      pp.q0[j] = in->cu_q[i]; pp.len_q[j] = in->cu_q[i + 1] - in->cu_q[i];
+      pp.k0[j] = in->cu_k[i]; pp.len_k[j] = in->cu_k[i + 1] - in->cu_k[i];
+      pp.unit_prefix[j] = static_cast<int>(units);
+      const int64_t tiles = (static_cast<int64_t>(pp.len_q[j]) + pp.tile_tokens - 1) / pp.tile_tokens;
+      units += (tiles + wg - 1) / wg * G;
+      if (units > (1 << 30)) return fail(EAS_ERR_UNSUPPORTED, "too many query rows for one call");
+    }
+    pp.unit_prefix[pp.n_seqs] = pp.total_units = static_cast<int>(units);
+    const bool h = in->dtype == EAS_DTYPE_FP16;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    EAS_TRY(hd == 64 ? (h ? launch_prompt<64, true>(pp, budget, st) : launch_prompt<64, false>(pp, budget, st))
+                     : (h ? launch_prompt<128, true>(pp, budget, st) : launch_prompt<128, false>(pp, budget, st)));
+  }
+  return EAS_OK;
+}
+
+// ------------------------------------------------------------------------------------ cache
+struct eas_cache {
+  eas_cache_desc d;
+  int device = 0, sm_count = 0, bs_log2 = 0;
+  CUtensorMap map_k, map_v;
+};
+
+// the cache as rows of head_dim bytes: a box is part of one head of one block
+static eas_status cache_map(CUtensorMap* m, const int8_t* base, const eas_cache_desc& d) {
+  PFN_cuTensorMapEncodeTiled_v12000 fn = get_encode_fn();
+  if (fn == nullptr) return fail(EAS_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+  const cuuint64_t gdim[2] = {static_cast<cuuint64_t>(d.head_dim), static_cast<cuuint64_t>(d.n_blocks) * d.n_kv_heads * d.block_size};
+  const cuuint64_t gstr[1] = {static_cast<cuuint64_t>(d.head_dim)};
+  const cuuint32_t box[2] = {static_cast<cuuint32_t>(d.head_dim), static_cast<cuuint32_t>(std::min(d.block_size, 4096 / d.head_dim))};
+  const cuuint32_t es[2] = {1, 1};
+  CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(base), gdim, gstr, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  d.head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(EAS_ERR_CUDA, "cuTensorMapEncodeTiled (cache) failed with code %d", static_cast<int>(r));
+  return EAS_OK;
+}
+
+static eas_status cache_create(const eas_cache_desc* d, eas_cache** out) {
+  if (out == nullptr) return fail(EAS_ERR_INVALID_ARG, "out is null");
+  *out = nullptr;
+  if (d == nullptr || d->k == nullptr || d->v == nullptr || d->k_scale == nullptr || d->v_scale == nullptr)
+    return fail(EAS_ERR_INVALID_ARG, "a required pointer is null");
+  if (d->head_dim != 64 && d->head_dim != 128) return fail(EAS_ERR_UNSUPPORTED, "head_dim %d (supported: 64, 128)", d->head_dim);
+  if (d->block_size != 16 && d->block_size != 32 && d->block_size != 64 && d->block_size != 128)
+    return fail(EAS_ERR_UNSUPPORTED, "block_size %d (supported: 16, 32, 64, 128)", d->block_size);
+  if (d->n_blocks <= 0 || d->n_kv_heads <= 0) return fail(EAS_ERR_INVALID_ARG, "non-positive cache size");
+  if (static_cast<int64_t>(d->n_blocks) * d->n_kv_heads > 0x7fffffffLL / d->block_size)
+    return fail(EAS_ERR_UNSUPPORTED, "more than 2^31 - 1 rows of tokens and heads");
+  if (!aligned16(d->k) || !aligned16(d->v)) return fail(EAS_ERR_INVALID_ARG, "k and v must be 16-byte aligned");
+  eas_cache c{};
+  c.d = *d;
+  EAS_TRY(device_check(&c.sm_count, &c.device));
+  for (c.bs_log2 = 4; (1 << c.bs_log2) < d->block_size; ++c.bs_log2) {}
+  EAS_TRY(cache_map(&c.map_k, d->k, *d));
+  EAS_TRY(cache_map(&c.map_v, d->v, *d));
+  *out = new (std::nothrow) eas_cache(c);
+  return *out != nullptr ? EAS_OK : fail(EAS_ERR_INVALID_ARG, "out of host memory");
+}
+
+static eas_status check_cache_call(const eas_cache* c, const eas_cache_seqs* s, bool rows, int32_t dtype, const uint32_t* status_dev, int32_t sm_budget,
+                                   int* budget) {
+  if (c == nullptr || s == nullptr || status_dev == nullptr) return fail(EAS_ERR_INVALID_ARG, "a required pointer is null");
+  if (dtype != EAS_DTYPE_BF16 && dtype != EAS_DTYPE_FP16) return fail(EAS_ERR_UNSUPPORTED, "dtype %d", dtype);
+  if (s->n_seqs < 0 || s->max_blocks < 0) return fail(EAS_ERR_INVALID_ARG, "n_seqs %d, max_blocks %d", s->n_seqs, s->max_blocks);
+  if (s->n_seqs > 0) {
+    if ((s->max_blocks > 0 && s->block_table == nullptr) || (rows ? s->cu_seqlens == nullptr || s->start == nullptr : s->seq_lens == nullptr))
+      return fail(EAS_ERR_INVALID_ARG, "a required pointer is null");
+    if (s->ld_table < s->max_blocks) return fail(EAS_ERR_INVALID_ARG, "ld_table %lld below max_blocks", static_cast<long long>(s->ld_table));
+  }
+  EAS_TRY(resolve_budget(sm_budget, budget));
+  int dev = -1;
+  CUDA_TRY(cudaGetDevice(&dev));
+  if (dev != c->device) return fail(EAS_ERR_INVALID_ARG, "the cache was created on device %d but device %d is current", c->device, dev);
+  return EAS_OK;
+}
+
+static CacheView view_of(const eas_cache* c) {
+  return CacheView{c->d.k, c->d.v, c->d.k_scale, c->d.v_scale, c->d.n_blocks, c->d.n_kv_heads, c->bs_log2};
+}
+
+template <int HD, typename T>
+static eas_status launch_rows(bool store, const CacheRowsParams& p, int budget, bool all, cudaStream_t stream) {
+  // one CTA an SM: on a share of the SMs the shared-memory request keeps a second one out; on all of them it is not needed, and L1 is larger
+  static OncePerDevice once;
+  if (once.first()) {
+    CUDA_TRY(cudaFuncSetAttribute(cache_store_kernel<HD, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kOnePerSmSmem));
+    CUDA_TRY(cudaFuncSetAttribute(cache_load_kernel<HD, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kOnePerSmSmem));
+    once.settled();
+  }
+  // few units: fewer warps a CTA, so that every SM has some
+  int warps = 32;
+  while (warps > 4 && static_cast<long long>(warps / 2) * budget >= p.units) warps /= 2;
+  const int grid = static_cast<int>(std::min<long long>(budget, (p.units + warps - 1) / warps));
+  return launch_kernel(store ? cache_store_kernel<HD, T> : cache_load_kernel<HD, T>, grid, warps * 32, all ? 0 : kOnePerSmSmem, stream, p);
+}
+
+static eas_status cache_rows(bool store, const eas_cache* c, const eas_cache_seqs* s, void* k, int64_t ld_k, void* v, int64_t ld_v, int32_t n_rows,
+                             int32_t dtype, int32_t sm_budget, void* stream, uint32_t* status_dev) {
+  int budget = 0;
+  EAS_TRY(check_cache_call(c, s, true, dtype, status_dev, sm_budget, &budget));
+  if (n_rows < 0) return fail(EAS_ERR_INVALID_ARG, "n_rows %d", n_rows);
+  if (n_rows == 0 || s->n_seqs == 0) return EAS_OK;
+  if (k == nullptr || v == nullptr) return fail(EAS_ERR_INVALID_ARG, "a required pointer is null");
+  const int64_t w = static_cast<int64_t>(c->d.n_kv_heads) * c->d.head_dim;
+  if (!aligned16(k) || !aligned16(v)) return fail(EAS_ERR_INVALID_ARG, "k and v must be 16-byte aligned");
+  if (ld_k < w || ld_v < w || ld_k % 8 != 0 || ld_v % 8 != 0)
+    return fail(EAS_ERR_INVALID_ARG, "token distances must be multiples of 8 that hold a token's heads");
+  CacheRowsParams p{};
+  p.c = view_of(c);
+  p.s = CacheSeqs{s->block_table, s->cu_seqlens, s->start, s->ld_table, s->n_seqs, s->max_blocks};
+  p.k = k; p.v = v; p.ld_k = ld_k; p.ld_v = ld_v; p.n_rows = n_rows;
+  const int64_t pairs = (n_rows >> c->bs_log2) + 2LL * s->n_seqs;
+  if (pairs * c->d.n_kv_heads > 0x7fffffffLL) return fail(EAS_ERR_UNSUPPORTED, "too many rows for one call");
+  p.units = pairs * c->d.n_kv_heads * 2;
+  p.status = status_dev;
+  const bool all = budget == c->sm_count, h = dtype == EAS_DTYPE_FP16;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (c->d.head_dim == 64) return h ? launch_rows<64, __half>(store, p, budget, all, st) : launch_rows<64, bf16>(store, p, budget, all, st);
+  return h ? launch_rows<128, __half>(store, p, budget, all, st) : launch_rows<128, bf16>(store, p, budget, all, st);
+}
+
+// pieces of the line of tiles: a function of the device, not of sm_budget (the sums' order depends on them)
+static int attention_rows(int group) { return group <= 8 ? 8 : 16; }
+static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+static size_t attention_workspace(const eas_cache* c, int32_t n_seqs, int32_t n_heads, size_t* ml_off, size_t* o_off) {
+  const size_t rows = static_cast<size_t>(2) * c->sm_count * attention_rows(n_heads / c->d.n_kv_heads);
+  *ml_off = up256((static_cast<size_t>(std::min(n_seqs, kCacheMaxSeqs)) + 2) * 4);
+  *o_off = *ml_off + up256(rows * 8);
+  return *o_off + rows * c->d.head_dim * 4;
+}
+
+template <int HD, int NT>
+static eas_status launch_attention(CacheAttnParams& p, int budget, bool all, cudaStream_t stream) {
+  using L = CacheAttnCfg<HD, NT>;
+  static OncePerDevice once;
+  if (once.first()) {
+    CUDA_TRY(cudaFuncSetAttribute(cache_attention_kernel<HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes));
+    CUDA_TRY(cudaFuncSetAttribute(cache_join_kernel<HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kOnePerSmSmem));
+    once.settled();
+  }
+  EAS_TRY(launch_kernel(cache_attention_kernel<HD, NT>, std::min(budget, p.n_pieces), kCacheThreads, L::kBytes, stream, p));
+  const int64_t heads = static_cast<int64_t>(p.n_seqs) * p.c.n_kv * p.group;
+  return launch_kernel(cache_join_kernel<HD, NT>, static_cast<int>(std::min<int64_t>(budget, (heads + 7) / 8)), 256, all ? 0 : kOnePerSmSmem, stream, p);
+}
+
+static eas_status cache_attention(const eas_cache* c, const eas_cache_seqs* s, const void* q, int64_t ld_q, void* out, int64_t ld_out, int32_t n_heads,
+                                  int32_t dtype, float scale, void* workspace, size_t workspace_bytes, int32_t sm_budget, void* stream,
+                                  uint32_t* status_dev) {
+  int budget = 0;
+  EAS_TRY(check_cache_call(c, s, false, dtype, status_dev, sm_budget, &budget));
+  const int G = c->d.n_kv_heads, hd = c->d.head_dim;
+  if (n_heads <= 0 || n_heads % G != 0) return fail(EAS_ERR_INVALID_ARG, "%d query heads for %d key/value heads", n_heads, G);
+  if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(EAS_ERR_INVALID_ARG, "scale must be positive and finite");
+  if (s->n_seqs == 0) return EAS_OK;
+  if (q == nullptr || out == nullptr || workspace == nullptr) return fail(EAS_ERR_INVALID_ARG, "a required pointer is null");
+  if (!aligned16(q) || !aligned16(out)) return fail(EAS_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
+  const int64_t w = static_cast<int64_t>(n_heads) * hd;
+  if (ld_q < w || ld_out < w || ld_q % 8 != 0 || ld_out % 8 != 0)
+    return fail(EAS_ERR_INVALID_ARG, "token distances must be multiples of 8 that hold a token's heads");
+  size_t ml_off = 0, o_off = 0;
+  const size_t need = attention_workspace(c, s->n_seqs, n_heads, &ml_off, &o_off);
+  if (workspace_bytes < need) return fail(EAS_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, need);
+  if ((reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return fail(EAS_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
+  CacheAttnParams p{};
+  p.map_k = c->map_k; p.map_v = c->map_v;
+  p.c = view_of(c);
+  p.group = n_heads / G;
+  const int rows = attention_rows(p.group), tile = 4096 / hd;
+  p.row_blocks = (p.group + rows - 1) / rows;
+  const int64_t places = static_cast<int64_t>(s->max_blocks) * c->d.block_size, tiles = (places + tile - 1) / tile;
+  if (places > 0x7fffffffLL || tiles * G * p.row_blocks > 0x7fffffffLL / std::min(s->n_seqs, kCacheMaxSeqs))
+    return fail(EAS_ERR_UNSUPPORTED, "max_blocks %d is too large for %d sequences", s->max_blocks, s->n_seqs);
+  p.ld_table = s->ld_table; p.max_blocks = s->max_blocks;
+  p.ld_q = ld_q; p.ld_out = ld_out; p.fp16 = dtype == EAS_DTYPE_FP16;
+  p.n_pieces = c->sm_count;
+  p.min_tiles = kCacheWarps;
+  p.scale_log2 = static_cast<float>(scale * kLog2e);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  p.head_ws = reinterpret_cast<int*>(ws); p.ml_ws = reinterpret_cast<float*>(ws + ml_off); p.o_ws = reinterpret_cast<float*>(ws + o_off);
+  p.status = status_dev;
+  const bool all = budget == c->sm_count;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  for (int first = 0; first < s->n_seqs; first += kCacheMaxSeqs) {
+    p.n_seqs = std::min(kCacheMaxSeqs, s->n_seqs - first);
+    p.table = s->block_table + first * s->ld_table;
+    p.seq_lens = s->seq_lens + first;
+    p.q = static_cast<const uint16_t*>(q) + first * ld_q;
+    p.out = static_cast<uint16_t*>(out) + first * ld_out;
+    EAS_TRY(hd == 64 ? (rows == 8 ? launch_attention<64, 1>(p, budget, all, st) : launch_attention<64, 2>(p, budget, all, st))
+                     : (rows == 8 ? launch_attention<128, 1>(p, budget, all, st) : launch_attention<128, 2>(p, budget, all, st)));
+  }
+  return EAS_OK;
+}
+
+// ------------------------------------------------------------------------------------ entry points (no exception passes them)
+extern "C" eas_status eas_prompt_attention(const eas_prompt_inputs* in, int32_t sm_budget, void* stream, uint32_t* status_dev) {
+  try {
+    return prompt_attention(in, sm_budget, stream, status_dev);
+  } catch (const std::bad_alloc&) {
+    return fail(EAS_ERR_INVALID_ARG, "out of host memory");
+  }
+}
+
+extern "C" eas_status eas_cache_create(const eas_cache_desc* desc, eas_cache** out) { return cache_create(desc, out); }
+
+extern "C" void eas_cache_destroy(eas_cache* cache) { delete cache; }
+
+extern "C" eas_status eas_cache_store(const eas_cache* cache, const eas_cache_seqs* seqs, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                                      int32_t n_rows, int32_t dtype, int32_t sm_budget, void* stream, uint32_t* status_dev) {
+  return cache_rows(true, cache, seqs, const_cast<void*>(k), ld_k, const_cast<void*>(v), ld_v, n_rows, dtype, sm_budget, stream, status_dev);
+}
+
+extern "C" eas_status eas_cache_load(const eas_cache* cache, const eas_cache_seqs* seqs, void* k, int64_t ld_k, void* v, int64_t ld_v, int32_t n_rows,
+                                     int32_t dtype, int32_t sm_budget, void* stream, uint32_t* status_dev) {
+  return cache_rows(false, cache, seqs, k, ld_k, v, ld_v, n_rows, dtype, sm_budget, stream, status_dev);
+}
+
+extern "C" size_t eas_cache_attention_workspace_bytes(const eas_cache* cache, int32_t n_seqs, int32_t n_heads) {
+  if (cache == nullptr || n_seqs < 0 || n_heads <= 0 || n_heads % cache->d.n_kv_heads != 0) {
+    fail(EAS_ERR_INVALID_ARG, "bad arguments");
+    return 0;
+  }
+  size_t ml_off = 0, o_off = 0;
+  return attention_workspace(cache, n_seqs, n_heads, &ml_off, &o_off);
+}
+
+extern "C" eas_status eas_cache_attention(const eas_cache* cache, const eas_cache_seqs* seqs, const void* q, int64_t ld_q, void* out, int64_t ld_out,
+                                          int32_t n_heads, int32_t dtype, float scale, void* workspace, size_t workspace_bytes, int32_t sm_budget,
+                                          void* stream, uint32_t* status_dev) {
+  return cache_attention(cache, seqs, q, ld_q, out, ld_out, n_heads, dtype, scale, workspace, workspace_bytes, sm_budget, stream, status_dev);
+}

@@ -1,0 +1,233 @@
+// The 8-bit paged key/value cache: rows in, rows out.
+//
+// A block holds block_size tokens of every head, [head][token][head_dim] bytes, with one fp32 scale for each head of it (keys and
+// values apart): value = number * scale.  A scale for a whole block of a head costs 4 bytes in block_size * head_dim, and the
+// numbers of a block can enter an integer-valued matrix product as they are, the scale coming in once per product.
+#pragma once
+#include <cuda_fp16.h>
+
+#include "ptx.cuh"
+
+namespace eas {
+
+enum : uint32_t { DEV_ERR_CACHE_RANGE = 3 };     // a block number or a place outside the cache
+constexpr float kCacheMinScale = 7.888609052210118e-31f;   // 2^-100: blocks of zeros, and no division by a subnormal scale
+
+struct CacheView {
+  int8_t *k, *v;
+  float *k_scale, *v_scale;
+  int n_blocks, n_kv, bs_log2;
+};
+struct CacheSeqs {
+  const int32_t *table, *cu, *start;
+  long long ld_table;
+  int n_seqs, max_blocks;
+};
+
+__device__ __forceinline__ void raise_status(uint32_t* status, uint32_t code) { atomicCAS(status, DEV_OK, code); }
+
+template <typename T> struct Pair16;
+template <> struct Pair16<bf16> {
+  static __device__ __forceinline__ float lo(uint32_t w) { return bf16_lo(w); }
+  static __device__ __forceinline__ float hi(uint32_t w) { return bf16_hi(w); }
+  static __device__ __forceinline__ uint32_t pack(float a, float b) { return pack_bf16x2(a, b); }
+};
+template <> struct Pair16<__half> {
+  static __device__ __forceinline__ float lo(uint32_t w) { return __half2float(__ushort_as_half(static_cast<unsigned short>(w & 0xFFFFu))); }
+  static __device__ __forceinline__ float hi(uint32_t w) { return __half2float(__ushort_as_half(static_cast<unsigned short>(w >> 16))); }
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+};
+__device__ __forceinline__ float load16(uint16_t x, bool fp16) {
+  return fp16 ? __half2float(__ushort_as_half(x)) : __uint_as_float(static_cast<uint32_t>(x) << 16);
+}
+
+// ------------------------------------------------------------------------------------------------ store, load
+// Both walk (sequence, block) pairs.  How many blocks a sequence touches is only known on the device, so a pair has a number that the
+// host can bound: sequence s owns the numbers from floor(cu[s] / bs) + 2 s on.  A run of n tokens touches at most
+// floor(n / bs) + 2 blocks and floor(a / bs) + floor(n / bs) <= floor((a + n) / bs), so the ranges never overlap, and
+// all numbers are below floor(n_rows / bs) + 2 n_seqs.
+struct CacheRowsParams {
+  CacheView c;
+  CacheSeqs s;
+  void *k, *v;            // [n_rows][n_kv * head_dim] (store: read, load: written)
+  long long ld_k, ld_v;
+  int n_rows;
+  long long units;        // pair numbers x heads x {keys, values}
+  uint32_t* status;
+  int early_launch;
+};
+
+struct CacheRun {         // the part of a sequence's rows that lies in one block
+  int block;              // -1: none
+  int lo, hi;             // places in the block
+  int row;                // row of place lo
+};
+__device__ __forceinline__ CacheRun cache_run(const CacheRowsParams& p, int pair, bool report) {
+  CacheRun r;
+  r.block = -1;
+  auto cu = [&](int i) { return min(max(__ldg(p.s.cu + i), 0), p.n_rows); };
+  int lo = 0, hi = p.s.n_seqs - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if ((cu(mid) >> p.c.bs_log2) + 2 * mid <= pair) lo = mid; else hi = mid - 1;
+  }
+  const int c0 = cu(lo), len = cu(lo + 1) - c0, j = pair - ((c0 >> p.c.bs_log2) + 2 * lo);
+  if (len <= 0 || j < 0) return r;
+  const long long at = __ldg(p.s.start + lo), end = at + len;
+  if (at < 0) {
+    if (report && j == 0) raise_status(p.status, DEV_ERR_CACHE_RANGE);
+    return r;
+  }
+  const long long b = (at >> p.c.bs_log2) + j, b0 = b << p.c.bs_log2;
+  if (b0 >= end) return r;
+  int block = -1;
+  if (b < p.s.max_blocks) block = __ldg(p.s.table + lo * p.s.ld_table + b);
+  if (block < 0 || block >= p.c.n_blocks) {
+    if (report) raise_status(p.status, DEV_ERR_CACHE_RANGE);
+    return r;
+  }
+  r.block = block;
+  r.lo = static_cast<int>(max(at - b0, 0LL));
+  r.hi = static_cast<int>(min(end - b0, 1LL << p.c.bs_log2));
+  r.row = c0 + static_cast<int>(b0 + r.lo - at);
+  return r;
+}
+
+// The nearest integer to x / s (ties to even) in the low byte.  x * inv is off by a few 2^-24 relative, so its floor k is right or one
+// off where x / s lies next to an integer, and in both cases the answer is k or k + 1; which, says the sign of
+// x - (k + 1/2) s, and one fma gives that sign exactly (k + 1/2 has 8 bits; the difference, if not 0, is far above the subnormals for s >= 2^-100).
+__device__ __forceinline__ uint32_t quantise(float x, float s, float inv) {
+  const float k = floorf(x * inv);
+  const float d = fmaf(-(k + 0.5f), s, x);
+  const uint32_t kb = __float_as_uint(k + 12582912.0f);          // 1.5 * 2^23: k in the low bits, two's complement
+  return kb + ((d > 0.0f || (d == 0.0f && (kb & 1u))) ? 1u : 0u);
+}
+// The same for a number that is in the block already: number * old / s.  The product has too many bits for one fma, so what comes
+// within 2^-10 of a tie is decided in fp64 (31 by 24 bits: the rounded quotient is a tie exactly where the true one is).
+__device__ __forceinline__ uint32_t requantise(int q, float old, float s, float ratio) {
+  const float r = static_cast<float>(q) * ratio;
+  float n = rintf(r);
+  if (fabsf(fabsf(r - n) - 0.5f) < 0.0009765625f) n = static_cast<float>(rint(static_cast<double>(q) * old / s));
+  return __float_as_uint(n + 12582912.0f);
+}
+
+// One warp per (sequence, block, head, keys or values): the largest magnitude of the new rows, the scale, the numbers.  Memory-bound: 2 bytes
+// read and 1 written per value.  The rows are read twice, the second time from L1 or L2 (a block of 64 tokens is 16 KB; kept in
+// registers it would be 128 a lane).
+template <int HD, typename T>
+__global__ void __launch_bounds__(1024, 1) cache_store_kernel(const __grid_constant__ CacheRowsParams p) {
+  if (p.early_launch) pdl_launch_dependents();
+  pdl_wait();
+  const int lane = threadIdx.x & 31;
+  constexpr int kChunks = HD / 8, kRows = 32 / kChunks;          // lanes per row (8 values each), rows per step of the warp
+  const int chunk = lane % kChunks, sub = lane / kChunks;
+  const long long warps = static_cast<long long>(gridDim.x) * (blockDim.x >> 5);
+  for (long long u = static_cast<long long>(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5); u < p.units; u += warps) {
+    const bool values = u & 1;
+    const int pair_head = static_cast<int>(u >> 1), head = pair_head % p.c.n_kv;
+    const CacheRun r = cache_run(p, pair_head / p.c.n_kv, lane == 0 && head == 0 && !values);
+    if (r.block < 0) continue;
+    const long long ld = values ? p.ld_v : p.ld_k;
+    const T* src = static_cast<const T*>(values ? p.v : p.k) + static_cast<long long>(r.row) * ld + head * HD + chunk * 8;
+    const long long at = static_cast<long long>(r.block) * p.c.n_kv + head;
+    float* scale = (values ? p.c.v_scale : p.c.k_scale) + at;
+    int8_t* dst = (values ? p.c.v : p.c.k) + ((at << p.c.bs_log2) * HD);
+    const int n = r.hi - r.lo;
+    // magnitudes compare as integers, with Inf above every number and NaN above Inf
+    uint32_t m2 = 0;
+#pragma unroll 8
+    for (int t = sub; t < n; t += kRows) {
+      const uint4 x = *reinterpret_cast<const uint4*>(src + t * ld);
+      m2 = __vmaxu2(m2, __vmaxu2(__vmaxu2(x.x & 0x7FFF7FFFu, x.y & 0x7FFF7FFFu), __vmaxu2(x.z & 0x7FFF7FFFu, x.w & 0x7FFF7FFFu)));
+    }
+    const uint32_t m = __reduce_max_sync(0xffffffffu, max(m2 & 0xFFFFu, m2 >> 16));
+    float s = __fdiv_rn(Pair16<T>::lo(m), 127.0f);
+    if (s < kCacheMinScale) s = kCacheMinScale;
+    if (r.lo > 0) {
+      const float old = *scale;
+      if (!(s <= old) && old == old) {                           // the scale grows (or stops being a number)
+        const float ratio = __fdiv_rn(old, s);
+        constexpr int kLanes = HD / 16;
+        for (int t = lane / kLanes; t < r.lo; t += 32 / kLanes) {
+          uint4* w = reinterpret_cast<uint4*>(dst + t * HD + (lane % kLanes) * 16);
+          const uint4 x = *w;
+          uint32_t xw[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t y = 0;
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+              y |= (requantise(static_cast<int8_t>(xw[i] >> (8 * b)), old, s, ratio) & 0xFFu) << (8 * b);
+            xw[i] = y;
+          }
+          *w = make_uint4(xw[0], xw[1], xw[2], xw[3]);
+        }
+      } else {
+        s = old;
+      }
+    }
+    const float inv = __fdiv_rn(1.0f, s);
+    int8_t* out = dst + r.lo * HD + chunk * 8;
+#pragma unroll 4
+    for (int t = sub; t < n; t += kRows) {
+      const uint4 x = *reinterpret_cast<const uint4*>(src + t * ld);
+      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+      uint32_t q[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        q[2 * i] = quantise(Pair16<T>::lo(w[i]), s, inv);
+        q[2 * i + 1] = quantise(Pair16<T>::hi(w[i]), s, inv);
+      }
+      uint2 y;
+      y.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+      y.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
+      *reinterpret_cast<uint2*>(out + t * HD) = y;
+    }
+    __syncwarp();
+    if (lane == 0) *scale = s;
+  }
+}
+
+// four bytes of x (two's complement) as floats, exact: 2^23 + 128 + number as the bit pattern 0x4B0000xx, less 2^23 + 128
+__device__ __forceinline__ void bytes_to_floats(uint32_t x, float (&f)[4]) {
+  x ^= 0x80808080u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(__byte_perm(x, 0x4B000000u, 0x7440 | i)) - 8388736.0f;
+}
+
+// One warp per (sequence, block, head, keys or values).  Memory-bound: 1 byte read and 2 written per value.
+template <int HD, typename T>
+__global__ void __launch_bounds__(1024, 1) cache_load_kernel(const __grid_constant__ CacheRowsParams p) {
+  if (p.early_launch) pdl_launch_dependents();
+  pdl_wait();
+  const int lane = threadIdx.x & 31;
+  constexpr int kChunks = HD / 8, kRows = 32 / kChunks;
+  const int chunk = lane % kChunks, sub = lane / kChunks;
+  const long long warps = static_cast<long long>(gridDim.x) * (blockDim.x >> 5);
+  for (long long u = static_cast<long long>(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5); u < p.units; u += warps) {
+    const bool values = u & 1;
+    const int pair_head = static_cast<int>(u >> 1), head = pair_head % p.c.n_kv;
+    const CacheRun r = cache_run(p, pair_head / p.c.n_kv, lane == 0 && head == 0 && !values);
+    if (r.block < 0) continue;
+    const long long ld = values ? p.ld_v : p.ld_k;
+    T* dst = static_cast<T*>(values ? p.v : p.k) + static_cast<long long>(r.row) * ld + head * HD + chunk * 8;
+    const long long at = static_cast<long long>(r.block) * p.c.n_kv + head;
+    const float s = *((values ? p.c.v_scale : p.c.k_scale) + at);
+    const int8_t* src = (values ? p.c.v : p.c.k) + ((at << p.c.bs_log2) * HD) + r.lo * HD + chunk * 8;
+    const int n = r.hi - r.lo;
+#pragma unroll 8
+    for (int t = sub; t < n; t += kRows) {
+      const uint2 x = *reinterpret_cast<const uint2*>(src + t * HD);
+      float f[4], g[4];
+      bytes_to_floats(x.x, f);
+      bytes_to_floats(x.y, g);
+      *reinterpret_cast<uint4*>(dst + t * ld) = make_uint4(Pair16<T>::pack(f[0] * s, f[1] * s), Pair16<T>::pack(f[2] * s, f[3] * s),
+                                                           Pair16<T>::pack(g[0] * s, g[1] * s), Pair16<T>::pack(g[2] * s, g[3] * s));
+    }
+  }
+}
+
+}  // namespace eas
