@@ -84,7 +84,7 @@ enum { EAS_DEVICE_CACHE_RANGE = 3 }; /* value of the status word, beside 1 (a bo
  *   number = nearest integer to value / scale, ties to even
  * "In the block already" are the tokens at places below start[s] of the same block; where the scale grows their numbers are
  * rounded again (number * old scale / scale).  Places behind the last one written keep whatever they hold.  A value that is
- * not finite makes the scale of its block and head Inf or NaN, and what is read from there NaN.
+ * not finite makes the scale of its block and head NaN, and with it all that is read from there, until the block is written from its first place again.
  * n_rows: rows of k and v that exist (a bound on cu_seqlens).  Deterministic: no atomics. */
 eas_status eas_cache_store(const eas_cache* cache, const eas_cache_seqs* seqs, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
                            int32_t n_rows, int32_t dtype, int32_t sm_budget, void* stream, uint32_t* status_dev);

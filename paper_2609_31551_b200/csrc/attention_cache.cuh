@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(kCacheThreads, 1) cache_attention_kernel(const
   } else {
     // ------------------------------------------------------------------ consumers
     const int qg = lane >> 2, qt = lane & 3;
-    uint32_t g = 0;                                    // tiles of this CTA so far: tile g is warp g % 8's, in stage g % NST
+    uint32_t g = 0;                                    // tiles of this CTA so far: tile g lies in stage g % NST
     for (long long piece = blockIdx.x; piece * quota < total; piece += gridDim.x) {
       const int first = static_cast<int>(piece) * quota, end = min(first + quota, total);
       for (int pos = first; pos < end;) {
@@ -268,7 +268,8 @@ __global__ void __launch_bounds__(kCacheThreads, 1) cache_attention_kernel(const
         const int row = in_seq / n_tiles, tile0 = in_seq - row * n_tiles, n = min(n_tiles - tile0, end - pos);
         const int kvh = row / p.row_blocks, head0 = (row - kvh * p.row_blocks) * ROWS;      // first query head, within the group
         const int n_rows = min(ROWS, p.group - head0);
-        const uint32_t k0 = (static_cast<uint32_t>(warp) - g) & (kCacheWarps - 1);          // this warp's first tile
+        // this warp's first tile: they go round from the piece's first, so that a sum's order does not depend on what the CTA did before
+        const uint32_t k0 = static_cast<uint32_t>(warp - (pos - first)) & (kCacheWarps - 1);
         float m_ref[NT][2], l[NT][2], o[HD / 16][NT][4];
 #pragma unroll
         for (int j = 0; j < NT; ++j) {

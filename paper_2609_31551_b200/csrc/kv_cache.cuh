@@ -146,6 +146,7 @@ __global__ void __launch_bounds__(1024, 1) cache_store_kernel(const __grid_const
     const uint32_t m = __reduce_max_sync(0xffffffffu, max(m2 & 0xFFFFu, m2 >> 16));
     float s = __fdiv_rn(Pair16<T>::lo(m), 127.0f);
     if (s < kCacheMinScale) s = kCacheMinScale;
+    if (!(s * 0.0f == 0.0f)) s = __uint_as_float(0x7FFFFFFFu);     // Inf or NaN among the values: the block and head reads as NaN
     if (r.lo > 0) {
       const float old = *scale;
       if (!(s <= old) && old == old) {                           // the scale grows (or stops being a number)
