@@ -2,9 +2,10 @@
 // key/value head are the columns of one matrix product.
 //
 // What bounds it is the cache: 2 head_dim bytes a token and key/value head, read once.  So everything serves the stream of tiles:
-//   warp 8      producer: 8 lanes a step, each finds the sequence, head and block of its tile and brings keys and values by TMA
-//               into a ring of 8 KB stages (some 130-160 KB in flight on every SM)
-//   warps 0..7  take the tiles in turn.  The products are transposed, S^T = K Q^T and O^T += V^T P^T, so that the tokens of a
+//   4 producer warps, 4 lanes each: a lane finds the sequence, head and block of its tile and brings keys and values by TMA
+//               into a ring of 8 KB stages; a tile's chain (block number, then its bytes and scales) is two trips to memory,
+//               and with four warps 16 of them are under way
+//   8 or 12 consumer warps take the tiles in turn.  The products are transposed, S^T = K Q^T and O^T += V^T P^T, so that the tokens of a
 //               tile fill the 16 rows of mma.sync.m16n8k16 and up to 8 query heads its columns: with single tokens there are 1 to
 //               16 rows of queries, of which the 128-row tiles of tcgen05 would leave nearly all empty, and the bytes go
 //               from shared memory to registers anyway, to become fp16.
@@ -45,28 +46,34 @@ struct CacheAttnParams {
 };
 
 constexpr int kCacheMaxSeqs = 1024;      // sequences of one launch (the prefix sums lie in shared memory)
-constexpr int kCacheWarps = 8;
-constexpr int kCacheThreads = 32 * (kCacheWarps + 1);
-constexpr int kCacheStep = 8;            // tiles that the producer brings at once
+constexpr int kCacheProducers = 4;       // producer warps
+constexpr int kCacheStep = 4;            // tiles that a producer brings at once
 
 template <int HD, int NT>
 struct CacheAttnCfg {
   static constexpr int kTile = 4096 / HD;                      // tokens of a stage
   static constexpr int kMt = kTile / 16;                       // matrix tiles of 16 tokens
+  static constexpr int kWarps = NT == 1 ? 12 : 8;              // consumers: their registers decide
+  static constexpr int kThreads = 32 * (kWarps + kCacheProducers);
+  static constexpr int kRegsProducer = 40, kRegsConsumer = NT == 1 ? 152 : 224, kRegsLaunch = NT == 1 ? 128 : 168;
   static constexpr int kStages = NT == 1 ? 20 : 16;
   static constexpr int kRows = 8 * NT;
   static constexpr int kOPitch = HD + 4;                       // floats: the fragments' float2 stores then cover all banks
   static constexpr int kRingBytes = kStages * 8192;
   static constexpr int kOOff = kRingBytes;
-  static constexpr int kMlOff = kOOff + kCacheWarps * kRows * kOPitch * 4;
-  static constexpr int kMetaOff = kMlOff + kCacheWarps * kRows * 8;            // [stage][kMt] {key scale, log2 and reciprocal of the value scale, tokens}
+  static constexpr int kMlOff = kOOff + kWarps * kRows * kOPitch * 4;
+  static constexpr int kMetaOff = kMlOff + kWarps * kRows * 8;            // [stage][kMt] {key scale, log2 and reciprocal of the value scale, tokens}
   static constexpr int kPrefixOff = kMetaOff + kStages * kMt * 16;
   static constexpr int kLenOff = kPrefixOff + (kCacheMaxSeqs + 4) * 4;
   static constexpr int kBarOff = kLenOff + kCacheMaxSeqs * 4;
-  static constexpr int kBytes = kBarOff + 2 * kStages * 8 + 64 + 1024;         // barriers, words, alignment slack
+  static constexpr int kBytes = kBarOff + 2 * kStages * 8 + (16 + kStages + 4) * 4 + 1024;         // barriers, words, alignment slack
   static_assert(kBytes <= 232448, "exceeds the shared memory of an SM");
   static_assert(kBytes > 116224, "a second CTA must not fit beside this one");
-  static_assert(kStages >= 2 * kCacheStep, "a step of the producer never waits for a tile of its own step");
+  static_assert(kStages >= kCacheProducers * kCacheStep, "no step waits for a tile of its own or of one under way beside it");
+  static_assert(32 * (kWarps * kRegsConsumer + kCacheProducers * kRegsProducer) <= kThreads * kRegsLaunch && kThreads * kRegsLaunch <= 65536,
+                "setmaxnreg budget exceeds the CTA's register allocation");
+  static_assert(kWarps % 4 == 0 && kCacheProducers % 4 == 0, "setmaxnreg acts on warpgroups");
+  static_assert(32 * kWarps >= 256 && kWarps <= 12, "the scan of the lengths takes 256 threads");
 };
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -100,10 +107,27 @@ __device__ __forceinline__ float fast_lg2(float x) {
   return y;
 }
 
+// Waits (bounded) until *word, in shared memory, is `value`.
+__device__ __forceinline__ bool word_wait(const volatile int* word, int value, volatile uint32_t* abort_flag) {
+  if (*word == value) return true;
+  const long long t0 = clock64();
+  uint32_t it = 0;
+  while (*word != value) {
+    if ((++it & 63u) == 0u) {
+      if (*abort_flag) return false;
+      if (clock64() - t0 > kWaitCycleLimit) {
+        *abort_flag = 1u;
+        return false;
+      }
+    }
+  }
+  return true;
+}
+
 template <int HD, int NT>
-__global__ void __launch_bounds__(kCacheThreads, 1) cache_attention_kernel(const __grid_constant__ CacheAttnParams p) {
+__global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_attention_kernel(const __grid_constant__ CacheAttnParams p) {
   using L = CacheAttnCfg<HD, NT>;
-  constexpr int TILE = L::kTile, MT = L::kMt, NST = L::kStages, ROWS = L::kRows, PITCH = L::kOPitch;
+  constexpr int TILE = L::kTile, MT = L::kMt, NST = L::kStages, ROWS = L::kRows, PITCH = L::kOPitch, WARPS = L::kWarps;
   extern __shared__ uint8_t smem_raw_cache[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw_cache) + 1023) & ~uintptr_t(1023));
   float* sm_o = reinterpret_cast<float*>(smem + L::kOOff);
@@ -113,12 +137,16 @@ __global__ void __launch_bounds__(kCacheThreads, 1) cache_attention_kernel(const
   int* sm_len = reinterpret_cast<int*>(smem + L::kLenOff);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBarOff);
   uint64_t* empty = full + NST;
-  int* sm_sum = reinterpret_cast<int*>(empty + NST);                     // [9] sums of the scan's warps
-  volatile uint32_t* abort_flag = reinterpret_cast<uint32_t*>(sm_sum + 12);
+  int* sm_sum = reinterpret_cast<int*>(empty + NST);                     // [16] sums of the scan's warps
+  // The tile that a stage was last given to.  Neighbouring uses of a stage belong to different warps, on both sides, and a barrier's parity
+  // tells only neighbouring phases apart; so whoever waits for a stage's barrier first waits until the tile before (producers) or the tile
+  // itself (consumers) has been issued: the barrier is then in the phase that is waited for, or just past it.
+  volatile int* sm_tile = sm_sum + 16;                                   // [NST]
+  volatile uint32_t* abort_flag = reinterpret_cast<uint32_t*>(sm_sum + 16 + NST);
   const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < NST; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
+    for (int i = 0; i < NST; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); sm_tile[i] = i - NST; }
     *abort_flag = 0;
     mbar_fence_init();
     tma_prefetch_desc(&p.map_k);
@@ -184,15 +212,17 @@ __global__ void __launch_bounds__(kCacheThreads, 1) cache_attention_kernel(const
     return lo;
   };
 
-  if (warp == kCacheWarps) {
-    // ------------------------------------------------------------------ producer
+  if (warp >= WARPS) {
+    // ------------------------------------------------------------------ producers: each takes every fourth step
+    setmaxnreg_dec<L::kRegsProducer>();
+    const int me = warp - WARPS;
     const int box_log2 = min(p.c.bs_log2, TILE == 32 ? 5 : 6), boxes = TILE >> box_log2;
     uint32_t g = 0;
     bool ok = true;
     for (long long piece = blockIdx.x; ok && piece * quota < total; piece += gridDim.x) {
       const int first = static_cast<int>(piece) * quota, end = min(first + quota, total);
-      for (int pos = first; pos < end; pos += kCacheStep) {
-        const uint32_t it = g + lane;
+      for (int pos = first + me * kCacheStep; pos < end; pos += kCacheProducers * kCacheStep) {
+        const uint32_t it = g + static_cast<uint32_t>(pos - first + lane);
         if (lane < kCacheStep && pos + lane < end) {
           const int at = pos + lane, s = find(at);
           const int n_tiles = sm_prefix[s + 1] - sm_prefix[s], in_seq = at - sm_prefix[s] * R;
@@ -211,7 +241,7 @@ __global__ void __launch_bounds__(kCacheThreads, 1) cache_attention_kernel(const
           }
           if (!good) raise_status(p.status, DEV_ERR_CACHE_RANGE);
           const int st = it % NST;
-          if (!mbar_wait(&empty[st], ((it / NST) & 1u) ^ 1u, abort_flag)) {
+          if (!word_wait(&sm_tile[st], static_cast<int>(it) - NST, abort_flag) || !mbar_wait(&empty[st], ((it / NST) & 1u) ^ 1u, abort_flag)) {
             ok = false;
           } else {
             uint8_t* kd = smem + st * 8192;
@@ -244,13 +274,14 @@ __global__ void __launch_bounds__(kCacheThreads, 1) cache_attention_kernel(const
               }
               sm_meta[st * MT + m] = meta;
             }
+            sm_tile[st] = static_cast<int>(it);
             mbar_expect_tx(&full[st], bytes);
           }
         }
-        g += static_cast<uint32_t>(min(kCacheStep, end - pos));
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
       }
+      g += static_cast<uint32_t>(end - first);
     }
     if (!ok) {
       const long long t0 = clock64();
@@ -258,6 +289,7 @@ __global__ void __launch_bounds__(kCacheThreads, 1) cache_attention_kernel(const
     }
   } else {
     // ------------------------------------------------------------------ consumers
+    setmaxnreg_inc<L::kRegsConsumer>();
     const int qg = lane >> 2, qt = lane & 3;
     uint32_t g = 0;                                    // tiles of this CTA so far: tile g lies in stage g % NST
     for (long long piece = blockIdx.x; piece * quota < total; piece += gridDim.x) {
@@ -269,7 +301,7 @@ __global__ void __launch_bounds__(kCacheThreads, 1) cache_attention_kernel(const
         const int kvh = row / p.row_blocks, head0 = (row - kvh * p.row_blocks) * ROWS;      // first query head, within the group
         const int n_rows = min(ROWS, p.group - head0);
         // this warp's first tile: they go round from the piece's first, so that a sum's order does not depend on what the CTA did before
-        const uint32_t k0 = static_cast<uint32_t>(warp - (pos - first)) & (kCacheWarps - 1);
+        const uint32_t k0 = static_cast<uint32_t>(warp + WARPS - (pos - first) % WARPS) % WARPS;
         float m_ref[NT][2], l[NT][2], o[HD / 16][NT][4];
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
@@ -315,10 +347,11 @@ __global__ void __launch_bounds__(kCacheThreads, 1) cache_attention_kernel(const
             c_row[j][0] = __shfl_sync(0xffffffffu, c, 8 * qt);
             c_row[j][1] = __shfl_sync(0xffffffffu, c, 8 * qt + 4);
           }
-          for (uint32_t k = k0; k < static_cast<uint32_t>(n); k += kCacheWarps) {
+          for (uint32_t k = k0; k < static_cast<uint32_t>(n); k += WARPS) {
             const uint32_t it = g + k;
             const int st = it % NST;
-            if (!warp_mbar_wait(&full[st], (it / NST) & 1u, abort_flag)) break;
+            if (!__all_sync(0xffffffffu, word_wait(&sm_tile[st], static_cast<int>(it), abort_flag)) ||
+                !warp_mbar_wait(&full[st], (it / NST) & 1u, abort_flag)) break;
             const uint32_t kb = smem_u32(smem) + st * 8192, vb = kb + 4096;
             // scores: token rows qg and qg + 8 of each 16, columns 2 qt and 2 qt + 1
             float sc[MT][NT][4];
@@ -431,8 +464,8 @@ __global__ void __launch_bounds__(kCacheThreads, 1) cache_attention_kernel(const
             if (lane == 0) mbar_arrive(&empty[st]);
           }
         }
-        // ---------------- the warps' parts of this (sequence, head): put together by all 256 threads, in the order of the warps
-        asm volatile("bar.sync 1, 256;" ::: "memory");           // the parts of the one before have been read
+        // ---------------- the warps' parts of this (sequence, head): put together by all of them, in the order of the warps
+        asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory");           // the parts of the one before have been read
         float* part = sm_o + warp * ROWS * PITCH;
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
@@ -452,18 +485,18 @@ __global__ void __launch_bounds__(kCacheThreads, 1) cache_attention_kernel(const
             }
           }
         }
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-        constexpr int kQuads = HD / 4, kPass = 256 / kQuads;     // 4 dims a thread
+        asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory");
+        constexpr int kQuads = HD / 4, kPass = 32 * WARPS / kQuads;     // 4 dims a thread
         const int d0 = (threadIdx.x % kQuads) * 4, og = d0 / (HD / 8), oi = (d0 % (HD / 8)) / 2;
         const bool whole = n == n_tiles;
         const long long slot = 2 * piece + (pos == first ? 0 : 1);
         for (int r = threadIdx.x / kQuads; r < n_rows; r += kPass) {
           float mr = -INFINITY;
 #pragma unroll
-          for (int w = 0; w < kCacheWarps; ++w) mr = fmaxf(mr, sm_ml[w * ROWS + r].x);
+          for (int w = 0; w < WARPS; ++w) mr = fmaxf(mr, sm_ml[w * ROWS + r].x);
           float lr = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int w = 0; w < kCacheWarps; ++w) {
+          for (int w = 0; w < WARPS; ++w) {
             const float2 ml = sm_ml[w * ROWS + r];
             if (ml.x == -INFINITY && ml.y == ml.y) continue;       // no token of this warp counts (its O may never have been written)
             const float f = fast_ex2(ml.x - mr);

@@ -238,7 +238,7 @@ static eas_status launch_attention(CacheAttnParams& p, int budget, bool all, cud
     CUDA_TRY(cudaFuncSetAttribute(cache_join_kernel<HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kOnePerSmSmem));
     once.settled();
   }
-  EAS_TRY(launch_kernel(cache_attention_kernel<HD, NT>, std::min(budget, p.n_pieces), kCacheThreads, L::kBytes, stream, p));
+  EAS_TRY(launch_kernel(cache_attention_kernel<HD, NT>, std::min(budget, p.n_pieces), L::kThreads, L::kBytes, stream, p));
   const int64_t heads = static_cast<int64_t>(p.n_seqs) * p.c.n_kv * p.group;
   return launch_kernel(cache_join_kernel<HD, NT>, static_cast<int>(std::min<int64_t>(budget, (heads + 7) / 8)), 256, all ? 0 : kOnePerSmSmem, stream, p);
 }
@@ -273,7 +273,7 @@ static eas_status cache_attention(const eas_cache* c, const eas_cache_seqs* s, c
   p.ld_table = s->ld_table; p.max_blocks = s->max_blocks;
   p.ld_q = ld_q; p.ld_out = ld_out; p.fp16 = dtype == EAS_DTYPE_FP16;
   p.n_pieces = c->sm_count;
-  p.min_tiles = kCacheWarps;
+  p.min_tiles = 8;
   p.scale_log2 = static_cast<float>(scale * kLog2e);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   p.head_ws = reinterpret_cast<int*>(ws); p.ml_ws = reinterpret_cast<float*>(ws + ml_off); p.o_ws = reinterpret_cast<float*>(ws + o_off);

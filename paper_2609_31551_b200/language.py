@@ -18,14 +18,13 @@ LANGUAGE_SYMBOLS = [
 ]
 STATUS_CACHE_RANGE = 3          # EAS_DEVICE_CACHE_RANGE
 _DTYPES = {torch.bfloat16: 0, torch.float16: 1}
-_I32P = C.POINTER(C.c_int32)
 
 
 class PromptInputs(C.Structure):
     _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("out", C.c_void_p),
                 ("ld_q", C.c_int64), ("ld_k", C.c_int64), ("ld_v", C.c_int64), ("ld_out", C.c_int64),
                 ("dtype", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
-                ("scale", C.c_float), ("n_seqs", C.c_int32), ("cu_q", _I32P), ("cu_k", _I32P)]
+                ("scale", C.c_float), ("n_seqs", C.c_int32), ("cu_q", C.c_void_p), ("cu_k", C.c_void_p)]
 
 
 class CacheDesc(C.Structure):
@@ -70,31 +69,44 @@ def _need(ok, text):
         raise B.EasError(1, text)
 
 
-def _rows(t, name, heads=None, head_dim=None, dtype=None, device=None):
+# (Texts are put together only where a check fails: these run before every launch.)
+def _rows(t, name, heads, head_dim, dtype, index):
     """Checks a [tokens, heads, head_dim] tensor whose tokens' heads are contiguous; returns the distance of two tokens."""
-    _need(t.dim() == 3, f"{name} must be [tokens, heads, head_dim]")
-    _need(dtype is None or t.dtype == dtype, f"{name} is {t.dtype}, expected {dtype}")
-    _need(device is None or t.device == device, f"{name} is on {t.device}, expected {device}")
-    _need((heads is None or t.shape[1] == heads) and (head_dim is None or t.shape[2] == head_dim), f"{name} has shape {tuple(t.shape)}")
-    _need(t.stride(2) == 1 and (t.shape[1] == 1 or t.stride(1) == t.shape[2]), f"{name}: the heads of a token must be contiguous")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[1] != heads or shape[2] != head_dim:
+        raise B.EasError(1, f"{name} has shape {tuple(shape)}, expected [tokens, {heads}, {head_dim}]")
+    if t.dtype != dtype or t.get_device() != index:
+        raise B.EasError(1, f"{name} is {t.dtype} on {t.device}, expected {dtype} on GPU {index}")
+    if stride[2] != 1 or (stride[1] != head_dim and heads != 1):
+        raise B.EasError(1, f"{name}: the heads of a token must be contiguous")
+    return stride[0] if shape[0] > 1 else heads * head_dim
 
 
-def _ints(t, name, shape, device):
-    _need(t.dtype == torch.int32 and t.device == device and t.is_contiguous() and tuple(t.shape) == shape,
-          f"{name} must be a contiguous int32 tensor of shape {shape} on {device}")
+def _ints(t, name, n, index):
+    if t.dtype != torch.int32 or t.get_device() != index or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise B.EasError(1, f"{name} must be a contiguous int32 tensor [{n}] on GPU {index}, not {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
+def _elsewhere(index, stream):
+    """True if a call has to run inside _on: another device is current than the tensors', or a stream is asked for."""
+    return stream is not None or torch._C._cuda_getDevice() != index
+
+
 @contextlib.contextmanager
-def _on(device, stream):
-    """The tensors' device is current inside, and allocations belong to the call's stream."""
-    with torch.cuda.device(device):
-        if stream is None or stream == torch.cuda.current_stream(device):
-            yield torch.cuda.current_stream(device).cuda_stream
-        else:
-            with torch.cuda.stream(stream):
-                yield stream.cuda_stream
+def _on(index, stream):
+    """The tensors' device is current inside, and so is the call's stream: allocations belong to it."""
+    if stream is not None and stream.device.index != index:
+        raise B.EasError(1, f"the stream is on {stream.device}, the tensors on GPU {index}")
+    with torch.cuda.device(index), torch.cuda.stream(stream):
+        yield
+
+
+def _host_ints(x, name):
+    x = np.ascontiguousarray(x, dtype=np.int32)
+    if x.ndim != 1 or x.size < 1:
+        raise B.EasError(1, f"{name} must be a list of at least one offset")
+    return x, x.__array_interface__["data"][0]
 
 
 def prompt_attention(q, k, v, cu_seqlens_host, cu_seqlens_k_host=None, scale=None, out=None, sm_budget=0, stream=None, status=None):
@@ -102,25 +114,31 @@ def prompt_attention(q, k, v, cu_seqlens_host, cu_seqlens_k_host=None, scale=Non
     cu_seqlens_host (int32 [n + 1]) gives the queries of each sequence, cu_seqlens_k_host its keys (default: the same; a sequence's
     queries are the last tokens among its keys).  scale: 1 / sqrt(head_dim).  Returns (out, device status word); `out` and
     `status` (device int32, zeroed by the caller) can be passed in so that a call allocates nothing."""
-    _need(q.is_cuda and q.dtype in _DTYPES, f"q must be a bf16 or fp16 tensor on a GPU, not {q.dtype} on {q.device}")
-    H, hd = q.shape[-2], q.shape[-1]
-    ld_q = _rows(q, "q")
-    ld_k = _rows(k, "k", head_dim=hd, dtype=q.dtype, device=q.device)
-    ld_v = _rows(v, "v", heads=k.shape[1], head_dim=hd, dtype=q.dtype, device=q.device)
-    cu_q = np.ascontiguousarray(cu_seqlens_host, dtype=np.int32)
-    cu_k = cu_q if cu_seqlens_k_host is None else np.ascontiguousarray(cu_seqlens_k_host, dtype=np.int32)
-    _need(cu_q.ndim == 1 and cu_q.size >= 1 and cu_k.shape == cu_q.shape, "cu_seqlens must be two lists of the same length")
-    _need(cu_q[-1] <= q.shape[0] and cu_k[-1] <= k.shape[0] and k.shape[0] == v.shape[0], "cu_seqlens reach past the rows of q, k or v")
-    with _on(q.device, stream) as s:
-        if out is None:
-            out = torch.empty((q.shape[0], H, hd), dtype=q.dtype, device=q.device)
-        ld_out = _rows(out, "out", heads=H, head_dim=hd, dtype=q.dtype, device=q.device)
-        _need(out.shape[0] >= cu_q[-1], "out has fewer rows than q")
-        if status is None:
-            status = torch.zeros(4, dtype=torch.int32, device=q.device)
-        pin = PromptInputs(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), ld_q, ld_k, ld_v, ld_out, _DTYPES[q.dtype], H, k.shape[1], hd,
-                           hd ** -0.5 if scale is None else scale, cu_q.size - 1, cu_q.ctypes.data_as(_I32P), cu_k.ctypes.data_as(_I32P))
-        B._check(lib().eas_prompt_attention(C.byref(pin), sm_budget, s, status.data_ptr()))
+    dtype, index = q.dtype, q.get_device()
+    if index < 0 or dtype not in _DTYPES or q.dim() != 3 or k.dim() != 3:
+        raise B.EasError(1, f"q and k must be bf16 or fp16 tensors [tokens, heads, head_dim] on a GPU, q is {dtype} {tuple(q.shape)} on {q.device}")
+    if _elsewhere(index, stream):
+        with _on(index, stream):
+            return prompt_attention(q, k, v, cu_seqlens_host, cu_seqlens_k_host, scale, out, sm_budget, None, status)
+    T, H, hd = q.shape
+    Tk, G, _ = k.shape
+    ld_q, ld_k, ld_v = _rows(q, "q", H, hd, dtype, index), _rows(k, "k", G, hd, dtype, index), _rows(v, "v", G, hd, dtype, index)
+    cu_q, at_q = _host_ints(cu_seqlens_host, "cu_seqlens")
+    cu_k, at_k = (cu_q, at_q) if cu_seqlens_k_host is None else _host_ints(cu_seqlens_k_host, "cu_seqlens_k")
+    if cu_k.size != cu_q.size or cu_q[-1] > T or cu_k[-1] > Tk or Tk != v.shape[0]:
+        raise B.EasError(1, "cu_seqlens are two lists of the same length that end within the rows of q, and of k and v")
+    if out is None:
+        out = torch.empty((T, H, hd), dtype=dtype, device=q.device)
+    ld_out = _rows(out, "out", H, hd, dtype, index)
+    if out.shape[0] < cu_q[-1]:
+        raise B.EasError(1, "out has fewer rows than cu_seqlens name")
+    if status is None:
+        status = torch.zeros(4, dtype=torch.int32, device=q.device)
+    pin = PromptInputs(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), ld_q, ld_k, ld_v, ld_out, _DTYPES[dtype], H, G, hd,
+                       hd ** -0.5 if scale is None else scale, cu_q.size - 1, at_q, at_k)
+    rc = lib().eas_prompt_attention(C.byref(pin), sm_budget, torch._C._cuda_getCurrentRawStream(index), status.data_ptr())
+    if rc:
+        B._check(rc)
     return out, status
 
 
@@ -142,6 +160,7 @@ class KvCache:
                        torch.zeros(shape[:2], device=device), torch.zeros(shape[:2], device=device))
         self.k, self.v, self.k_scale, self.v_scale = tensors
         self.device = self.k.device
+        self._index = self.k.get_device()
         for t, name, dt, s in ((self.k, "k", torch.int8, shape), (self.v, "v", torch.int8, shape), (self.k_scale, "k_scale", torch.float32, shape[:2]),
                                (self.v_scale, "v_scale", torch.float32, shape[:2])):
             _need(t.is_cuda and t.device == self.device and t.dtype == dt and tuple(t.shape) == s and t.is_contiguous(),
@@ -149,6 +168,7 @@ class KvCache:
         self.n_blocks, self.block_size, self.n_kv_heads, self.head_dim = n_blocks, block_size, n_kv_heads, head_dim
         with torch.cuda.device(self.device):
             self._status = torch.zeros(4, dtype=torch.int32, device=self.device)
+            self._status_at = self._status.data_ptr()
             desc = CacheDesc(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(), n_blocks, block_size, n_kv_heads, head_dim)
             h = C.c_void_p()
             B._check(self.lib.eas_cache_create(C.byref(desc), C.byref(h)))
@@ -167,36 +187,47 @@ class KvCache:
             pass
 
     def _seqs(self, block_table, n):
-        _need(self.handle is not None, "the cache is closed")
-        _need(block_table.dim() == 2 and block_table.dtype == torch.int32 and block_table.device == self.device and block_table.shape[0] == n
-              and (block_table.stride(1) == 1 or block_table.shape[1] <= 1), f"block_table must be an int32 tensor [{n}, max_blocks] on {self.device}")
-        return CacheSeqs(n, block_table.data_ptr(), block_table.shape[1], block_table.stride(0) if n > 1 else block_table.shape[1], None, None, None)
+        shape = block_table.shape
+        if self.handle is None:
+            raise B.EasError(1, "the cache is closed")
+        if (len(shape) != 2 or shape[0] != n or block_table.dtype != torch.int32 or block_table.get_device() != self._index
+                or (shape[1] > 1 and block_table.stride(1) != 1)):
+            raise B.EasError(1, f"block_table must be an int32 tensor [{n}, max_blocks] on {self.device}")
+        return CacheSeqs(n, block_table.data_ptr(), shape[1], block_table.stride(0) if n > 1 else shape[1], None, None, None)
 
-    def _move(self, call, k, v, cu_seqlens, start, block_table, sm_budget, s):
-        n = start.shape[0]
+    def _move(self, call, k, v, cu_seqlens, start, block_table, sm_budget):
+        n, index, dtype = start.shape[0], self._index, k.dtype
         seqs = self._seqs(block_table, n)
-        seqs.cu_seqlens = _ints(cu_seqlens, "cu_seqlens", (n + 1,), self.device)
-        seqs.start = _ints(start, "start", (n,), self.device)
-        ld_k = _rows(k, "k", self.n_kv_heads, self.head_dim, device=self.device)
-        ld_v = _rows(v, "v", self.n_kv_heads, self.head_dim, dtype=k.dtype, device=self.device)
-        _need(k.dtype in _DTYPES and k.shape[0] == v.shape[0], "k and v must be bf16 or fp16, with as many rows")
-        B._check(call(self.handle, C.byref(seqs), k.data_ptr(), ld_k, v.data_ptr(), ld_v, k.shape[0], _DTYPES[k.dtype], sm_budget, s,
-                      self._status.data_ptr()))
+        seqs.cu_seqlens = _ints(cu_seqlens, "cu_seqlens", n + 1, index)
+        seqs.start = _ints(start, "start", n, index)
+        rows = k.shape[0]
+        if dtype not in _DTYPES or rows != v.shape[0]:
+            raise B.EasError(1, "k and v must be bf16 or fp16, with as many rows")
+        ld_k, ld_v = _rows(k, "k", self.n_kv_heads, self.head_dim, dtype, index), _rows(v, "v", self.n_kv_heads, self.head_dim, dtype, index)
+        rc = call(self.handle, C.byref(seqs), k.data_ptr(), ld_k, v.data_ptr(), ld_v, rows, _DTYPES[dtype], sm_budget,
+                  torch._C._cuda_getCurrentRawStream(index), self._status_at)
+        if rc:
+            B._check(rc)
 
     def store(self, k, v, cu_seqlens, start, block_table, sm_budget=0, stream=None):
         """eas_cache_store: rows cu_seqlens[s] .. cu_seqlens[s + 1] - 1 of k and v ([rows, n_kv_heads, head_dim]) go to places start[s], ... of
         sequence s.  cu_seqlens (int32 [n + 1]), start (int32 [n]) and block_table are on the device.  A prompt starts at 0; a
         decoding step writes one row per sequence, cu_seqlens = 0, 1, 2, ..., start = the lengths so far."""
-        with _on(self.device, stream) as s:
-            self._move(self.lib.eas_cache_store, k, v, cu_seqlens, start, block_table, sm_budget, s)
+        if _elsewhere(self._index, stream):
+            with _on(self._index, stream):
+                return self.store(k, v, cu_seqlens, start, block_table, sm_budget)
+        self._move(self.lib.eas_cache_store, k, v, cu_seqlens, start, block_table, sm_budget)
 
     def load(self, cu_seqlens, start, block_table, n_rows, dtype=torch.bfloat16, out=None, sm_budget=0, stream=None):
         """eas_cache_load: the values of the same places -> (k, v), [n_rows, n_kv_heads, head_dim].  Rows that cu_seqlens does not name are
         left as they were (`out`, a pair of tensors) or are not set."""
-        with _on(self.device, stream) as s:
-            if out is None:
-                out = tuple(torch.empty((n_rows, self.n_kv_heads, self.head_dim), dtype=dtype, device=self.device) for _ in range(2))
-            self._move(self.lib.eas_cache_load, out[0], out[1], cu_seqlens, start, block_table, sm_budget, s)
+        if _elsewhere(self._index, stream):
+            with _on(self._index, stream):
+                return self.load(cu_seqlens, start, block_table, n_rows, dtype, out, sm_budget)
+        if out is None:
+            shape = (n_rows, self.n_kv_heads, self.head_dim)
+            out = torch.empty(shape, dtype=dtype, device=self.device), torch.empty(shape, dtype=dtype, device=self.device)
+        self._move(self.lib.eas_cache_load, out[0], out[1], cu_seqlens, start, block_table, sm_budget)
         return out
 
     def attention_workspace_bytes(self, n_seqs, n_heads):
@@ -206,24 +237,32 @@ class KvCache:
         """eas_cache_attention: q [n_seqs, n_heads, head_dim], one token a sequence, attends to places 0 .. seq_lens[s] - 1 (the token's own key
         and value among them, stored before).  workspace: a uint8 tensor of attention_workspace_bytes(), on a 256-byte boundary;
         calls that may run at the same time need one each (default: allocated by the call)."""
-        n = q.shape[0]
-        _need(q.dtype in _DTYPES, f"q is {q.dtype}")
-        ld_q = _rows(q, "q", head_dim=self.head_dim, device=self.device)
+        index, dtype = self._index, q.dtype
+        if _elsewhere(index, stream):
+            with _on(index, stream):
+                return self.attention(q, seq_lens, block_table, scale, out, workspace, sm_budget)
+        if q.dim() != 3 or dtype not in _DTYPES:
+            raise B.EasError(1, f"q must be bf16 or fp16 [n_seqs, n_heads, head_dim], not {dtype} {tuple(q.shape)}")
+        n, H, hd = q.shape
+        ld_q = _rows(q, "q", H, self.head_dim, dtype, index)
         seqs = self._seqs(block_table, n)
-        seqs.seq_lens = _ints(seq_lens, "seq_lens", (n,), self.device)
-        H = q.shape[1]
-        with _on(self.device, stream) as s:
-            if out is None:
-                out = torch.empty((n, H, self.head_dim), dtype=q.dtype, device=self.device)
-            ld_out = _rows(out, "out", H, self.head_dim, dtype=q.dtype, device=self.device)
-            _need(out.shape[0] >= n, "out has fewer rows than q")
-            if workspace is None:
-                need = self.attention_workspace_bytes(n, H)
-                workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
-            _need(workspace.is_cuda and workspace.device == self.device and workspace.is_contiguous(), "workspace must be a tensor on the cache's GPU")
-            B._check(self.lib.eas_cache_attention(self.handle, C.byref(seqs), q.data_ptr(), ld_q, out.data_ptr(), ld_out, H, _DTYPES[q.dtype],
-                                                  self.head_dim ** -0.5 if scale is None else scale, workspace.data_ptr(),
-                                                  workspace.numel() * workspace.element_size(), sm_budget, s, self._status.data_ptr()))
+        seqs.seq_lens = _ints(seq_lens, "seq_lens", n, index)
+        if out is None:
+            out = torch.empty((n, H, hd), dtype=dtype, device=self.device)
+            ld_out = H * hd
+        else:
+            ld_out = _rows(out, "out", H, hd, dtype, index)
+            if out.shape[0] < n:
+                raise B.EasError(1, "out has fewer rows than q")
+        if workspace is None:
+            workspace = torch.empty(self.attention_workspace_bytes(n, H), dtype=torch.uint8, device=self.device)
+        elif workspace.get_device() != index or not workspace.is_contiguous():
+            raise B.EasError(1, "workspace must be a contiguous tensor on the cache's GPU")
+        rc = self.lib.eas_cache_attention(self.handle, C.byref(seqs), q.data_ptr(), ld_q, out.data_ptr(), ld_out, H, _DTYPES[dtype],
+                                          hd ** -0.5 if scale is None else scale, workspace.data_ptr(), workspace.nbytes, sm_budget,
+                                          torch._C._cuda_getCurrentRawStream(index), self._status_at)
+        if rc:
+            B._check(rc)
         return out
 
     def check(self, stream=None):

@@ -86,7 +86,10 @@ def _inputs(lang, **over):
     a = dict(q=1 << 20, k=1 << 21, v=1 << 22, out=1 << 23, ld_q=512, ld_k=128, ld_v=128, ld_out=512, dtype=0, n_heads=4, n_kv_heads=1,
              head_dim=128, scale=0.1, n_seqs=2, cu_q=cu, cu_k=cu)
     a.update(over)
-    return lang.PromptInputs(*[a[f] for f, _ in lang.PromptInputs._fields_])
+    at = {f: C.addressof(a[f]) if a[f] is not None else None for f in ("cu_q", "cu_k")}
+    pin = lang.PromptInputs(*[at.get(f, a[f]) for f, _ in lang.PromptInputs._fields_])
+    pin.keep = a
+    return pin
 
 
 @pytest.mark.parametrize("over,status", [
