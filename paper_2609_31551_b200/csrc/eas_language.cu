@@ -223,8 +223,10 @@ static eas_status cache_rows(bool store, const eas_cache* c, const eas_cache_seq
 static int attention_rows(int group) { return group <= 8 ? 8 : 16; }
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 static size_t attention_workspace(const eas_cache* c, int32_t n_seqs, int32_t n_heads, size_t* ml_off, size_t* o_off) {
-  const size_t rows = static_cast<size_t>(2) * c->sm_count * attention_rows(n_heads / c->d.n_kv_heads);
-  *ml_off = up256((static_cast<size_t>(std::min(n_seqs, kCacheMaxSeqs)) + 2) * 4);
+  const int r = attention_rows(n_heads / c->d.n_kv_heads);
+  const int warps = r == 8 ? CacheAttnCfg<128, 1>::kWarps : CacheAttnCfg<128, 2>::kWarps;
+  const size_t rows = static_cast<size_t>(2) * c->sm_count * warps * r;
+  *ml_off = up256((static_cast<size_t>(std::min(n_seqs, kCacheMaxSeqs)) + 1) * 4);
   *o_off = *ml_off + up256(rows * 8);
   return *o_off + rows * c->d.head_dim * 4;
 }
@@ -238,7 +240,7 @@ static eas_status launch_attention(CacheAttnParams& p, int budget, bool all, cud
     CUDA_TRY(cudaFuncSetAttribute(cache_join_kernel<HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kOnePerSmSmem));
     once.settled();
   }
-  EAS_TRY(launch_kernel(cache_attention_kernel<HD, NT>, std::min(budget, p.n_pieces), L::kThreads, L::kBytes, stream, p));
+  EAS_TRY(launch_kernel(cache_attention_kernel<HD, NT>, std::min(budget, p.n_ctas), L::kThreads, L::kBytes, stream, p));
   const int64_t heads = static_cast<int64_t>(p.n_seqs) * p.c.n_kv * p.group;
   return launch_kernel(cache_join_kernel<HD, NT>, static_cast<int>(std::min<int64_t>(budget, (heads + 7) / 8)), 256, all ? 0 : kOnePerSmSmem, stream, p);
 }
@@ -267,13 +269,12 @@ static eas_status cache_attention(const eas_cache* c, const eas_cache_seqs* s, c
   p.group = n_heads / G;
   const int rows = attention_rows(p.group), tile = 4096 / hd;
   p.row_blocks = (p.group + rows - 1) / rows;
-  const int64_t places = static_cast<int64_t>(s->max_blocks) * c->d.block_size, tiles = (places + tile - 1) / tile;
+  const int64_t places = static_cast<int64_t>(s->max_blocks) * c->d.block_size, tiles = (places + tile - 1) / tile + kRowCost;
   if (places > 0x7fffffffLL || tiles * G * p.row_blocks > 0x7fffffffLL / std::min(s->n_seqs, kCacheMaxSeqs))
     return fail(EAS_ERR_UNSUPPORTED, "max_blocks %d is too large for %d sequences", s->max_blocks, s->n_seqs);
   p.ld_table = s->ld_table; p.max_blocks = s->max_blocks;
   p.ld_q = ld_q; p.ld_out = ld_out; p.fp16 = dtype == EAS_DTYPE_FP16;
-  p.n_pieces = c->sm_count;
-  p.min_tiles = 8;
+  p.n_ctas = c->sm_count;
   p.scale_log2 = static_cast<float>(scale * kLog2e);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   p.head_ws = reinterpret_cast<int*>(ws); p.ml_ws = reinterpret_cast<float*>(ws + ml_off); p.o_ws = reinterpret_cast<float*>(ws + o_off);
