@@ -16,7 +16,8 @@
 // The tiles of all sequences and heads form one line, cut into as many equal pieces as the device has warps (a function of the device, not of
 // sm_budget: the cut, and with it every sum, is the same on a share of the SMs).  Beginning a row of tiles (queries in, output out) costs
 // about as much as kRowCost tiles, so a row counts as that many more.  Lengths are read on the device: each CTA sums them up itself.  A piece
-// that holds a whole row writes its output; what is cut leaves (m, l, O) in the workspace, and cache_join_kernel puts it together, in order.
+// that holds a whole row writes its output.  What is cut leaves (m, l, O): the warps of a CTA, whose pieces are neighbours, put together what
+// they hold of one row that goes on behind them, and cache_join_kernel the CTAs' parts and the row's end, all in the order of the pieces.
 #pragma once
 #include "kv_cache.cuh"
 #include "ptx.cuh"
@@ -36,7 +37,6 @@ struct CacheAttnParams {
   int group, row_blocks;       // query heads per key/value head; blocks of 8 NT of them
   int n_ctas;                  // CTAs of the whole device: the line has kWarps pieces for each
   float scale_log2;            // scale * log2(e)
-  int* head_ws;                // [n_seqs + 1] cost of a row of tiles of the sequences before
   float* ml_ws;                // [2 pieces][8 NT rows][2]
   float* o_ws;                 // [2 pieces][8 NT rows][HD]
   uint32_t* status;
@@ -59,7 +59,7 @@ struct CacheAttnCfg {
   static constexpr int kBytes = kBarOff + kWarps * kDepth * 8 + 64 + 1024;     // barriers, words, alignment slack
   static_assert(kBytes <= 232448, "exceeds the shared memory of an SM");
   static_assert(kBytes > 116224, "a second CTA must not fit beside this one");
-  static_assert(kThreads >= 256 && kWarps <= 15, "the scan of the lengths takes 256 threads");
+  static_assert(kThreads >= 256 && kWarps <= 12, "the scan of the lengths takes 256 threads");
 };
 
 // The line of tiles: pieces, and the rows of tiles along it.  A row's tiles lie at its end, behind its kRowCost.
@@ -103,6 +103,45 @@ __device__ __forceinline__ float fast_lg2(float x) {
   return y;
 }
 
+// Prefix sums over the sequences of what a row of tiles costs, by a whole CTA of 256 or more threads (4 sequences a thread): prefix[0 .. n_seqs].
+template <int TILE>
+__device__ __forceinline__ void cache_prefix(const CacheAttnParams& p, int* prefix, int* lens, int* sums, bool report) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int t[4], sum = 0;
+  if (threadIdx.x < 256) {
+    const long long most = static_cast<long long>(p.max_blocks) << p.c.bs_log2;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int s = threadIdx.x * 4 + i;
+      int n = s < p.n_seqs ? max(__ldg(p.seq_lens + s), 0) : 0;
+      if (n > most) {
+        n = static_cast<int>(most);
+        if (report) raise_status(p.status, DEV_ERR_CACHE_RANGE);
+      }
+      if (lens != nullptr && s < p.n_seqs) lens[s] = n;
+      t[i] = sum;
+      sum += n > 0 ? (n + TILE - 1) / TILE + kRowCost : 0;
+    }
+  }
+  int incl = sum;
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const int o = __shfl_up_sync(0xffffffffu, incl, d);
+    if (lane >= d) incl += o;
+  }
+  if (lane == 31) sums[warp] = incl;
+  __syncthreads();
+  if (threadIdx.x < 256) {
+    int base = incl - sum;
+    for (int w = 0; w < warp; ++w) base += sums[w];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (threadIdx.x * 4 + i <= p.n_seqs) prefix[threadIdx.x * 4 + i] = base + t[i];
+    if (threadIdx.x == 255 && p.n_seqs == kCacheMaxSeqs) prefix[kCacheMaxSeqs] = base + sum;
+  }
+  __syncthreads();
+}
+
 template <int HD, int NT>
 __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_attention_kernel(const __grid_constant__ CacheAttnParams p) {
   using L = CacheAttnCfg<HD, NT>;
@@ -112,8 +151,8 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
   int* sm_prefix = reinterpret_cast<int*>(smem + L::kPrefixOff);         // cost of a row of tiles, summed over the sequences before
   int* sm_len = reinterpret_cast<int*>(smem + L::kLenOff);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBarOff);       // [warp][stage] tile landed
-  int* sm_sum = reinterpret_cast<int*>(bars + WARPS * DEPTH);            // [15] sums of the scan's warps
-  volatile uint32_t* abort_flag = reinterpret_cast<uint32_t*>(sm_sum + 15);
+  int* sm_sum = reinterpret_cast<int*>(bars + WARPS * DEPTH);            // [12] sums of the scan's warps; the rows that go on behind the warps
+  volatile uint32_t* abort_flag = reinterpret_cast<uint32_t*>(sm_sum + 12);
   const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
@@ -123,51 +162,9 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
     tma_prefetch_desc(&p.map_k);
     tma_prefetch_desc(&p.map_v);
   }
-  if (p.early_launch) pdl_launch_dependents();
   pdl_wait();
-
-  // lengths, and the prefix sums of what their rows of tiles cost: 4 sequences a thread of the first 256
-  {
-    int t[4], sum = 0;
-    if (threadIdx.x < 256) {
-      const long long most = static_cast<long long>(p.max_blocks) << p.c.bs_log2;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int s = threadIdx.x * 4 + i;
-        int n = s < p.n_seqs ? max(__ldg(p.seq_lens + s), 0) : 0;
-        if (n > most) {
-          n = static_cast<int>(most);
-          if (blockIdx.x == 0) raise_status(p.status, DEV_ERR_CACHE_RANGE);
-        }
-        if (s < p.n_seqs) sm_len[s] = n;
-        t[i] = sum;
-        sum += n > 0 ? (n + TILE - 1) / TILE + kRowCost : 0;
-      }
-    }
-    int incl = sum;
-#pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-      const int o = __shfl_up_sync(0xffffffffu, incl, d);
-      if (lane >= d) incl += o;
-    }
-    if (lane == 31) sm_sum[warp] = incl;
-    __syncthreads();
-    if (threadIdx.x < 256) {
-      int base = incl - sum;
-      for (int w = 0; w < warp; ++w) base += sm_sum[w];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int s = threadIdx.x * 4 + i;
-        if (s <= p.n_seqs) sm_prefix[s] = base + t[i];
-        if (s <= p.n_seqs && blockIdx.x == 0) p.head_ws[s] = base + t[i];
-      }
-      if (threadIdx.x == 255 && p.n_seqs == kCacheMaxSeqs) {
-        sm_prefix[kCacheMaxSeqs] = base + sum;
-        if (blockIdx.x == 0) p.head_ws[kCacheMaxSeqs] = base + sum;
-      }
-    }
-    __syncthreads();
-  }
+  if (p.early_launch) pdl_launch_dependents();     // behind the wait: the joining kernel reads the lengths ahead of its own
+  cache_prefix<TILE>(p, sm_prefix, sm_len, sm_sum, blockIdx.x == 0);
   const int R = p.c.n_kv * p.row_blocks;                         // rows of tiles a sequence has
   const CacheLine line(sm_prefix[p.n_seqs], R, p.n_ctas * WARPS);
   const int qg = lane >> 2, qt = lane & 3;
@@ -177,15 +174,15 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
   uint32_t issued = 0, done = 0;                                 // tiles of this warp so far: tile i lies in stage i % DEPTH
   bool ok = true;
 
-  for (int cta = blockIdx.x; cta < p.n_ctas && ok; cta += gridDim.x) {
+  for (int cta = blockIdx.x; cta < p.n_ctas && cta * WARPS < line.pieces; cta += gridDim.x) {
     const int piece = cta * WARPS + warp;
-    if (piece >= line.pieces) break;
-    const int begin = line.begin(piece), end = line.begin(piece + 1);
+    const int begin = line.begin(min(piece, line.pieces)), end = line.begin(min(piece + 1, line.pieces));
+    int open_row = -1;                                           // the row that goes on behind this piece
     // the row of tiles at the piece's beginning, and how many tiles the piece has
     int s0 = 0;
     {
       int hi = p.n_seqs - 1;
-      const int x = begin / R;
+      const int x = min(begin, line.total - 1) / R;
       while (s0 < hi) {                                          // the last sequence that begins at or before x (those without tiles are passed over)
         const int mid = (s0 + hi + 1) >> 1;
         if (sm_prefix[mid] <= x) s0 = mid; else hi = mid - 1;
@@ -472,11 +469,14 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
           next_id = load_id(iw);
         }
       }
-      if (!ok) break;
+      if (!ok) break;      // (the CTA's barriers below are still met)
 
-      // the row's part of this piece: lane (qg, qt) has dims qg * (HD / 8) .. of queries 2 qt and 2 qt + 1
-      const bool whole = first == 0 && last == row_tiles;
-      const long long slot = 2LL * piece + (first == 0 ? 1 : 0);
+      // the row's part of this piece: lane (qg, qt) has dims qg * (HD / 8) .. of queries 2 qt and 2 qt + 1.  The whole row goes out; a row's end
+      // into the workspace; a row that goes on is the last thing this piece has: into the warp's ring, for the CTA.
+      const bool ends = last == row_tiles, whole = ends && first == 0;
+      float* part = ends ? p.o_ws + 2LL * piece * ROWS * HD : reinterpret_cast<float*>(ring);
+      float* part_ml = ends ? p.ml_ws + 4LL * piece * ROWS : reinterpret_cast<float*>(ring) + ROWS * HD;
+      if (!ends) open_row = s * R + cw.row;
 #pragma unroll
       for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -499,16 +499,45 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
               *reinterpret_cast<uint4*>(dst + 2 * i) = make_uint4(y[0], y[1], y[2], y[3]);
             }
           } else {
-            float* dst = p.o_ws + (slot * ROWS + r) * HD + qg * (HD / 8);
+            float* dst = part + r * HD + qg * (HD / 8);
 #pragma unroll
             for (int i = 0; i < HD / 16; i += 2)
               *reinterpret_cast<float4*>(dst + 2 * i) = make_float4(o[i][j][b], o[i][j][b + 2], o[i + 1][j][b], o[i + 1][j][b + 2]);
-            if (qg == 0) *reinterpret_cast<float2*>(p.ml_ws + (slot * ROWS + r) * 2) = make_float2(m_ref[j][b], x);
+            if (qg == 0) *reinterpret_cast<float2*>(part_ml + r * 2) = make_float2(m_ref[j][b], x);
           }
         }
       cw.tile = last;
       enter(cw);
     }
+
+    // rows that go on behind their pieces: neighbouring warps of one row put theirs together, into the second slot of the first of them
+    if (lane == 0) sm_sum[warp] = open_row;
+    __syncthreads();
+    for (int w0 = 0, w1; w0 < WARPS; w0 = w1) {
+      const int row = sm_sum[w0];
+      for (w1 = w0 + 1; w1 < WARPS && sm_sum[w1] == row && row >= 0; ++w1) {}
+      if (row < 0) continue;
+      for (int e = threadIdx.x; e < ROWS * HD / 4; e += L::kThreads) {
+        const int r = e / (HD / 4);
+        auto ml_of = [&](int w) { return *reinterpret_cast<const float2*>(reinterpret_cast<const float*>(smem + w * DEPTH * 8192) + ROWS * HD + r * 2); };
+        float m = -INFINITY, l = 0.f;
+        for (int w = w0; w < w1; ++w) m = fmaxf(m, ml_of(w).x);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int w = w0; w < w1; ++w) {
+          const float2 ml = ml_of(w);
+          const float f = ml.x == -INFINITY && ml.y == ml.y ? 0.f : fast_ex2(ml.x - m);
+          const float4 x = reinterpret_cast<const float4*>(smem + w * DEPTH * 8192)[e];
+          l = fmaf(ml.y, f, l);
+          acc.x = fmaf(x.x, f, acc.x); acc.y = fmaf(x.y, f, acc.y);
+          acc.z = fmaf(x.z, f, acc.z); acc.w = fmaf(x.w, f, acc.w);
+        }
+        const long long slot = 2LL * (cta * WARPS + w0) + 1;
+        reinterpret_cast<float4*>(p.o_ws + slot * ROWS * HD)[e] = acc;
+        if (e % (HD / 4) == 0) *reinterpret_cast<float2*>(p.ml_ws + (slot * ROWS + r) * 2) = make_float2(m, l);
+      }
+    }
+    __syncthreads();
+    fence_proxy_async_smem();                                    // the rings held plain stores: before the next loads into them
   }
   if (!ok) {
     const long long t0 = clock64();
@@ -517,30 +546,44 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
   }
 }
 
-// What the pieces' ends cut, put together: one warp per (sequence, query head), the pieces in order.  Rows that one piece held are
+// What the CTAs' and pieces' ends cut, put together: one warp per (sequence, query head), the parts in order.  Rows that one piece held are
 // there already; sequences without tokens get zeros.
 template <int HD, int NT>
 __global__ void __launch_bounds__(256) cache_join_kernel(const __grid_constant__ CacheAttnParams p) {
-  constexpr int ROWS = 8 * NT, N = HD / 32;
-  if (p.early_launch) pdl_launch_dependents();
-  pdl_wait();
+  constexpr int ROWS = 8 * NT, N = HD / 32, WARPS = CacheAttnCfg<HD, NT>::kWarps;
+  __shared__ int prefix[kCacheMaxSeqs + 1], sums[8];
+  // On the whole device this kernel starts beside the one before it, which has let it go behind its own wait: the lengths are final
+  if (!p.early_launch) pdl_wait();
+  cache_prefix<CacheAttnCfg<HD, NT>::kTile>(p, prefix, nullptr, sums, false);
   const int lane = threadIdx.x & 31, heads = p.c.n_kv * p.group, R = p.c.n_kv * p.row_blocks;
-  const CacheLine line(p.head_ws[p.n_seqs], R, p.n_ctas * CacheAttnCfg<HD, NT>::kWarps);
+  const CacheLine line(prefix[p.n_seqs], R, p.n_ctas * WARPS);
+  bool waited = false;
   for (int u = blockIdx.x * 8 + (threadIdx.x >> 5); u < p.n_seqs * heads; u += gridDim.x * 8) {
     const int s = u / heads, h = u - s * heads, kvh = h / p.group, in_group = h - kvh * p.group;
     const int row = kvh * p.row_blocks + in_group / ROWS, r = in_group % ROWS;
-    const int before = p.head_ws[s], cost = p.head_ws[s + 1] - before;
+    const int before = prefix[s], cost = prefix[s + 1] - before;
+    int w0 = 0, w1 = 0;                                            // the row's first and last piece
+    if (cost > 0) {
+      const int a = before * R + row * cost;
+      w0 = line.piece_of(a + kRowCost);
+      w1 = line.piece_of(a + cost - 1);
+      if (w0 == w1) continue;
+    }
+    if (!waited) {
+      pdl_wait();
+      waited = true;
+    }
     float acc[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) acc[i] = 0.f;
     if (cost > 0) {
-      const int a = before * R + row * cost, w0 = line.piece_of(a + kRowCost), w1 = line.piece_of(a + cost - 1);
-      if (w0 == w1) continue;
-      auto slot = [&](int w) { return (2LL * w + (w == w0 ? 1 : 0)) * ROWS + r; };
-      // 32 pieces at a time: their references and sums, one a lane, then their O, 8 in flight
+      // parts: one for each CTA that the row goes on behind, then the row's end in piece w1
+      const int c0 = w0 / WARPS, parts = (w1 - 1) / WARPS - c0 + 2;
+      auto slot = [&](int i) { return (i + 1 == parts ? 2LL * w1 : 2LL * max(w0, (c0 + i) * WARPS) + 1) * ROWS + r; };
+      // 32 at a time: their references and sums, one a lane, then their O, 8 in flight
       float m = -INFINITY, l = 0.f;
-      for (int base = w0; base <= w1; base += 32) {
-        const int n = min(32, w1 - base + 1);
+      for (int base = 0; base < parts; base += 32) {
+        const int n = min(32, parts - base);
         float2 ml = make_float2(-INFINITY, 0.f);
         if (lane < n) ml = *reinterpret_cast<const float2*>(p.ml_ws + slot(base + lane) * 2);
         float top = fmaxf(m, ml.x);
@@ -559,7 +602,7 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const __grid_constant__
           float o[8][N];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float* src = p.o_ws + slot(min(base + k + e, w1)) * HD + lane * N;
+            const float* src = p.o_ws + slot(min(base + k + e, parts - 1)) * HD + lane * N;
 #pragma unroll
             for (int i = 0; i < N; ++i) o[e][i] = src[i];
           }
@@ -580,6 +623,8 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const __grid_constant__
     for (int i = 0; i < N; i += 2)
       *reinterpret_cast<uint32_t*>(dst + i) = p.fp16 ? Pair16<__half>::pack(acc[i], acc[i + 1]) : Pair16<bf16>::pack(acc[i], acc[i + 1]);
   }
+  if (!waited) pdl_wait();                                         // (whoever follows relies on every CTA having waited)
+  if (p.early_launch) pdl_launch_dependents();
 }
 
 }  // namespace eas

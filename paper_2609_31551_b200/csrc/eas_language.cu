@@ -222,12 +222,11 @@ static eas_status cache_rows(bool store, const eas_cache* c, const eas_cache_seq
 // pieces of the line of tiles: a function of the device, not of sm_budget (the sums' order depends on them)
 static int attention_rows(int group) { return group <= 8 ? 8 : 16; }
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
-static size_t attention_workspace(const eas_cache* c, int32_t n_seqs, int32_t n_heads, size_t* ml_off, size_t* o_off) {
+static size_t attention_workspace(const eas_cache* c, int32_t n_heads, size_t* o_off) {
   const int r = attention_rows(n_heads / c->d.n_kv_heads);
   const int warps = r == 8 ? CacheAttnCfg<128, 1>::kWarps : CacheAttnCfg<128, 2>::kWarps;
   const size_t rows = static_cast<size_t>(2) * c->sm_count * warps * r;
-  *ml_off = up256((static_cast<size_t>(std::min(n_seqs, kCacheMaxSeqs)) + 1) * 4);
-  *o_off = *ml_off + up256(rows * 8);
+  *o_off = up256(rows * 8);
   return *o_off + rows * c->d.head_dim * 4;
 }
 
@@ -259,8 +258,8 @@ static eas_status cache_attention(const eas_cache* c, const eas_cache_seqs* s, c
   const int64_t w = static_cast<int64_t>(n_heads) * hd;
   if (ld_q < w || ld_out < w || ld_q % 8 != 0 || ld_out % 8 != 0)
     return fail(EAS_ERR_INVALID_ARG, "token distances must be multiples of 8 that hold a token's heads");
-  size_t ml_off = 0, o_off = 0;
-  const size_t need = attention_workspace(c, s->n_seqs, n_heads, &ml_off, &o_off);
+  size_t o_off = 0;
+  const size_t need = attention_workspace(c, n_heads, &o_off);
   if (workspace_bytes < need) return fail(EAS_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, need);
   if ((reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return fail(EAS_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
   CacheAttnParams p{};
@@ -277,7 +276,7 @@ static eas_status cache_attention(const eas_cache* c, const eas_cache_seqs* s, c
   p.n_ctas = c->sm_count;
   p.scale_log2 = static_cast<float>(scale * kLog2e);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  p.head_ws = reinterpret_cast<int*>(ws); p.ml_ws = reinterpret_cast<float*>(ws + ml_off); p.o_ws = reinterpret_cast<float*>(ws + o_off);
+  p.ml_ws = reinterpret_cast<float*>(ws); p.o_ws = reinterpret_cast<float*>(ws + o_off);
   p.status = status_dev;
   const bool all = budget == c->sm_count;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -321,8 +320,8 @@ extern "C" size_t eas_cache_attention_workspace_bytes(const eas_cache* cache, in
     fail(EAS_ERR_INVALID_ARG, "bad arguments");
     return 0;
   }
-  size_t ml_off = 0, o_off = 0;
-  return attention_workspace(cache, n_seqs, n_heads, &ml_off, &o_off);
+  size_t o_off = 0;
+  return attention_workspace(cache, n_heads, &o_off);
 }
 
 extern "C" eas_status eas_cache_attention(const eas_cache* cache, const eas_cache_seqs* seqs, const void* q, int64_t ld_q, void* out, int64_t ld_out,
