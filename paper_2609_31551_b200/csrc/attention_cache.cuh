@@ -25,7 +25,7 @@
 namespace eas {
 
 struct CacheAttnParams {
-  CUtensorMap map_k, map_v;    // bytes [blocks * heads * block_size, HD], box of min(block_size, tile) rows, swizzled
+  CUtensorMap map_k, map_v;    // bytes [blocks * heads * block_size, HD], box of min(block_size, 32) rows, swizzled
   CacheView c;
   const int32_t *table, *seq_lens;
   long long ld_table;
@@ -48,18 +48,19 @@ constexpr int kRowCost = 1;
 
 template <int HD, int NT>
 struct CacheAttnCfg {
-  static constexpr int kTile = 4096 / HD;                      // tokens of a stage
+  static constexpr int kTile = HD == 64 && NT == 1 ? 32 : 4096 / HD;           // tokens of a stage
+  static constexpr int kHalfBytes = kTile * HD, kStageBytes = 2 * kHalfBytes;  // keys, then values
   static constexpr int kMt = kTile / 16;                       // matrix tiles of 16 tokens
-  static constexpr int kWarps = NT == 1 ? 12 : 8, kDepth = NT == 1 ? 2 : 3;    // registers decide
+  static constexpr int kWarps = NT == 1 ? (HD == 64 ? 16 : 12) : 8, kDepth = NT == 1 && HD == 128 ? 2 : 3;    // registers decide
   static constexpr int kThreads = 32 * kWarps;
   static constexpr int kRows = 8 * NT;
-  static constexpr int kPrefixOff = kWarps * kDepth * 8192;
+  static constexpr int kPrefixOff = kWarps * kDepth * kStageBytes;
   static constexpr int kLenOff = kPrefixOff + (kCacheMaxSeqs + 4) * 4;
   static constexpr int kBarOff = kLenOff + kCacheMaxSeqs * 4;
-  static constexpr int kBytes = kBarOff + kWarps * kDepth * 8 + 64 + 1024;     // barriers, words, alignment slack
+  static constexpr int kBytes = kBarOff + kWarps * kDepth * 8 + 80 + 1024;     // barriers, words, alignment slack
   static_assert(kBytes <= 232448, "exceeds the shared memory of an SM");
   static_assert(kBytes > 116224, "a second CTA must not fit beside this one");
-  static_assert(kThreads >= 256 && kWarps <= 12, "the scan of the lengths takes 256 threads");
+  static_assert(kThreads >= 256 && kWarps <= 16, "the scan of the lengths takes 256 threads");
 };
 
 // The line of tiles: pieces, and the rows of tiles along it.  A row's tiles lie at its end, behind its kRowCost.
@@ -151,8 +152,8 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
   int* sm_prefix = reinterpret_cast<int*>(smem + L::kPrefixOff);         // cost of a row of tiles, summed over the sequences before
   int* sm_len = reinterpret_cast<int*>(smem + L::kLenOff);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBarOff);       // [warp][stage] tile landed
-  int* sm_sum = reinterpret_cast<int*>(bars + WARPS * DEPTH);            // [12] sums of the scan's warps; the rows that go on behind the warps
-  volatile uint32_t* abort_flag = reinterpret_cast<uint32_t*>(sm_sum + 12);
+  int* sm_sum = reinterpret_cast<int*>(bars + WARPS * DEPTH);            // [16] sums of the scan's warps; the rows that go on behind the warps
+  volatile uint32_t* abort_flag = reinterpret_cast<uint32_t*>(sm_sum + 16);
   const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
@@ -168,8 +169,8 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
   const int R = p.c.n_kv * p.row_blocks;                         // rows of tiles a sequence has
   const CacheLine line(sm_prefix[p.n_seqs], R, p.n_ctas * WARPS);
   const int qg = lane >> 2, qt = lane & 3;
-  const int box_log2 = min(p.c.bs_log2, TILE == 32 ? 5 : 6);
-  uint8_t* const ring = smem + warp * DEPTH * 8192;
+  const int box_log2 = min(p.c.bs_log2, 5);
+  uint8_t* const ring = smem + warp * DEPTH * L::kStageBytes;
   uint64_t* const full = bars + warp * DEPTH;
   uint32_t issued = 0, done = 0;                                 // tiles of this warp so far: tile i lies in stage i % DEPTH
   bool ok = true;
@@ -191,6 +192,13 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
     // A walk along the line's rows from the piece's beginning.  One walker issues loads, DEPTH tiles ahead of the one that computes.
     struct Walk {
       int s, row, tile, n_tiles, left;      // sequence, row, next tile, tiles of the row; positions of the piece from the row's end on
+      int kvh, len;                         // the row's key/value head, the sequence's length
+      const int32_t* ids;                   // and its line of the block table
+    };
+    auto at_row = [&](Walk& w) {
+      w.kvh = p.row_blocks == 1 ? w.row : w.row / p.row_blocks;
+      w.len = sm_len[w.s];
+      w.ids = p.table + w.s * p.ld_table;
     };
     auto enter = [&](Walk& w) {             // at a row's first tile (or past it, at the piece's beginning)
       while (w.n_tiles <= w.tile && w.left > 0) {                // behind the row's last tile: the next row
@@ -203,6 +211,7 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
         w.n_tiles = min(cost, w.left) - kRowCost;                // tiles of it that belong to this piece
         w.left -= cost;
         w.tile = 0;
+        at_row(w);
       }
     };
     Walk iw;
@@ -213,6 +222,7 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
       iw.tile = max(at - kRowCost, 0);
       iw.n_tiles = min(cost, at + end - begin) - kRowCost;
       iw.left = end - begin - (cost - at);
+      at_row(iw);
       enter(iw);
     }
     Walk cw = iw;
@@ -222,9 +232,9 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
     auto load_id = [&](const Walk& w) {
       int id = -1;
       const int tok = w.tile * TILE + lane * 16;
-      if (lane < MT && more(w) && tok < sm_len[w.s]) {
-        id = __ldg(p.table + w.s * p.ld_table + (tok >> p.c.bs_log2));
-        if (id < 0 || id >= p.c.n_blocks) {
+      if (lane < MT && more(w) && tok < w.len) {
+        id = __ldg(w.ids + (tok >> p.c.bs_log2));
+        if (static_cast<uint32_t>(id) >= static_cast<uint32_t>(p.c.n_blocks)) {
           raise_status(p.status, DEV_ERR_CACHE_RANGE);
           id = -1;
         }
@@ -238,10 +248,10 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
       if (lane == 0) mbar_expect_tx(&full[st], boxes * (2u * HD << box_log2));
       __syncwarp();
       if (box) {
-        const int kvh = w.row / p.row_blocks, tok = w.tile * TILE + lane * 16;
-        const int y = ((id * p.c.n_kv + kvh) << p.c.bs_log2) + (tok & ((1 << p.c.bs_log2) - 1));
-        tma_load_2d(ring + st * 8192 + lane * 16 * HD, &p.map_k, &full[st], 0, y);
-        tma_load_2d(ring + st * 8192 + 4096 + lane * 16 * HD, &p.map_v, &full[st], 0, y);
+        const int tok = w.tile * TILE + lane * 16;
+        const int y = ((id * p.c.n_kv + w.kvh) << p.c.bs_log2) + (tok & ((1 << p.c.bs_log2) - 1));
+        tma_load_2d(ring + st * L::kStageBytes + lane * 16 * HD, &p.map_k, &full[st], 0, y);
+        tma_load_2d(ring + st * L::kStageBytes + L::kHalfBytes + lane * 16 * HD, &p.map_v, &full[st], 0, y);
       }
       __syncwarp();
       ++issued;
@@ -249,7 +259,7 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
     auto load_scales = [&](const Walk& w, int id) {
       float2 sc = make_float2(0.f, 0.f);
       if (id >= 0) {
-        const long long at = static_cast<long long>(id) * p.c.n_kv + w.row / p.row_blocks;
+        const long long at = static_cast<long long>(id) * p.c.n_kv + w.kvh;
         sc = make_float2(__ldg(p.c.k_scale + at), __ldg(p.c.v_scale + at));
       }
       return sc;
@@ -277,9 +287,9 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
     }
 
     while (more(cw) && ok) {
-      const int s = cw.s, kvh = cw.row / p.row_blocks, head0 = (cw.row - kvh * p.row_blocks) * ROWS;      // head0: within the group
+      const int s = cw.s, kvh = cw.kvh, head0 = (cw.row - kvh * p.row_blocks) * ROWS;      // head0: within the group
       const int n_rows = min(ROWS, p.group - head0);
-      const int first = cw.tile, last = cw.n_tiles, row_tiles = sm_prefix[s + 1] - sm_prefix[s] - kRowCost, len = sm_len[s];
+      const int first = cw.tile, last = cw.n_tiles, row_tiles = sm_prefix[s + 1] - sm_prefix[s] - kRowCost, len = cw.len;
       float m_ref[NT][2], l[NT][2], o[HD / 16][NT][4];
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
@@ -330,7 +340,7 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
         const uint32_t st = done % DEPTH;
         if (!warp_mbar_wait(&full[st], (done / DEPTH) & 1u, abort_flag)) { ok = false; break; }
         ++done;
-        const uint32_t kb = smem_u32(ring) + st * 8192, vb = kb + 4096;
+        const uint32_t kb = smem_u32(ring) + st * L::kStageBytes, vb = kb + L::kHalfBytes;
         // scores: token rows qg and qg + 8 of each 16, columns 2 qt and 2 qt + 1
         float sc[MT][NT][4];
 #pragma unroll
@@ -413,12 +423,17 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
               }
             }
         }
+        float ref[NT][2];                                        // (no token counted yet: 2^-inf = 0, against any reference)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) ref[j][b] = fmaxf(m_ref[j][b], -3.0e38f);
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
           uint32_t pf[NT][2];
 #pragma unroll
           for (int j = 0; j < NT; ++j) {
-            const float r0 = m_ref[j][0] == -INFINITY ? 0.f : m_ref[j][0], r1 = m_ref[j][1] == -INFINITY ? 0.f : m_ref[j][1];
+            const float r0 = ref[j][0], r1 = ref[j][1];
             const float w0 = fast_ex2(sc[m][j][0] - r0), w1 = fast_ex2(sc[m][j][1] - r1);
             const float w2 = fast_ex2(sc[m][j][2] - r0), w3 = fast_ex2(sc[m][j][3] - r1);
             l[j][0] = fmaf(w0 + w2, v_inv[m], l[j][0]);
@@ -519,14 +534,14 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
       if (row < 0) continue;
       for (int e = threadIdx.x; e < ROWS * HD / 4; e += L::kThreads) {
         const int r = e / (HD / 4);
-        auto ml_of = [&](int w) { return *reinterpret_cast<const float2*>(reinterpret_cast<const float*>(smem + w * DEPTH * 8192) + ROWS * HD + r * 2); };
+        auto ml_of = [&](int w) { return *reinterpret_cast<const float2*>(reinterpret_cast<const float*>(smem + w * DEPTH * L::kStageBytes) + ROWS * HD + r * 2); };
         float m = -INFINITY, l = 0.f;
         for (int w = w0; w < w1; ++w) m = fmaxf(m, ml_of(w).x);
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int w = w0; w < w1; ++w) {
           const float2 ml = ml_of(w);
           const float f = ml.x == -INFINITY && ml.y == ml.y ? 0.f : fast_ex2(ml.x - m);
-          const float4 x = reinterpret_cast<const float4*>(smem + w * DEPTH * 8192)[e];
+          const float4 x = reinterpret_cast<const float4*>(smem + w * DEPTH * L::kStageBytes)[e];
           l = fmaf(ml.y, f, l);
           acc.x = fmaf(x.x, f, acc.x); acc.y = fmaf(x.y, f, acc.y);
           acc.z = fmaf(x.z, f, acc.z); acc.w = fmaf(x.w, f, acc.w);

@@ -126,7 +126,7 @@ static eas_status cache_map(CUtensorMap* m, const int8_t* base, const eas_cache_
   if (fn == nullptr) return fail(EAS_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
   const cuuint64_t gdim[2] = {static_cast<cuuint64_t>(d.head_dim), static_cast<cuuint64_t>(d.n_blocks) * d.n_kv_heads * d.block_size};
   const cuuint64_t gstr[1] = {static_cast<cuuint64_t>(d.head_dim)};
-  const cuuint32_t box[2] = {static_cast<cuuint32_t>(d.head_dim), static_cast<cuuint32_t>(std::min(d.block_size, 4096 / d.head_dim))};
+  const cuuint32_t box[2] = {static_cast<cuuint32_t>(d.head_dim), static_cast<cuuint32_t>(std::min(d.block_size, 32))};
   const cuuint32_t es[2] = {1, 1};
   CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(base), gdim, gstr, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   d.head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -224,7 +224,7 @@ static int attention_rows(int group) { return group <= 8 ? 8 : 16; }
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 static size_t attention_workspace(const eas_cache* c, int32_t n_heads, size_t* o_off) {
   const int r = attention_rows(n_heads / c->d.n_kv_heads);
-  const int warps = r == 8 ? CacheAttnCfg<128, 1>::kWarps : CacheAttnCfg<128, 2>::kWarps;
+  const int warps = r != 8 ? CacheAttnCfg<64, 2>::kWarps : c->d.head_dim == 64 ? CacheAttnCfg<64, 1>::kWarps : CacheAttnCfg<128, 1>::kWarps;
   const size_t rows = static_cast<size_t>(2) * c->sm_count * warps * r;
   *o_off = up256(rows * 8);
   return *o_off + rows * c->d.head_dim * 4;
@@ -266,7 +266,7 @@ static eas_status cache_attention(const eas_cache* c, const eas_cache_seqs* s, c
   p.map_k = c->map_k; p.map_v = c->map_v;
   p.c = view_of(c);
   p.group = n_heads / G;
-  const int rows = attention_rows(p.group), tile = 4096 / hd;
+  const int rows = attention_rows(p.group), tile = 32;      // (no variant's tile is smaller)
   p.row_blocks = (p.group + rows - 1) / rows;
   const int64_t places = static_cast<int64_t>(s->max_blocks) * c->d.block_size, tiles = (places + tile - 1) / tile + kRowCost;
   if (places > 0x7fffffffLL || tiles * G * p.row_blocks > 0x7fffffffLL / std::min(s->n_seqs, kCacheMaxSeqs))
