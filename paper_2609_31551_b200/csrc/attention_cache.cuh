@@ -48,10 +48,10 @@ constexpr int kRowCost = 1;
 
 template <int HD, int NT>
 struct CacheAttnCfg {
-  static constexpr int kTile = HD == 64 && NT == 1 ? 32 : 4096 / HD;           // tokens of a stage
+  static constexpr int kTile = 4096 / HD;           // tokens of a stage
   static constexpr int kHalfBytes = kTile * HD, kStageBytes = 2 * kHalfBytes;  // keys, then values
   static constexpr int kMt = kTile / 16;                       // matrix tiles of 16 tokens
-  static constexpr int kWarps = NT == 1 ? (HD == 64 ? 16 : 12) : 8, kDepth = NT == 1 && HD == 128 ? 2 : 3;    // registers decide
+  static constexpr int kWarps = NT == 1 ? 12 : 8, kDepth = NT == 1 ? 2 : 3;    // registers decide
   static constexpr int kThreads = 32 * kWarps;
   static constexpr int kRows = 8 * NT;
   static constexpr int kPrefixOff = kWarps * kDepth * kStageBytes;
@@ -241,20 +241,42 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
       }
       return id;
     };
+    // The whole warp walks; one elected lane issues, with operands that are the same in all lanes (a TMA operation takes them from uniform
+    // registers: lanes with operands of their own would go one after the other).  Returns which 16-token parts have a block.
     auto issue = [&](const Walk& w, int id) {
-      const uint32_t st = issued % DEPTH;
-      const bool box = id >= 0 && ((lane * 16) & ((1 << box_log2) - 1)) == 0;
-      const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, box));
-      if (lane == 0) mbar_expect_tx(&full[st], boxes * (2u * HD << box_log2));
-      __syncwarp();
-      if (box) {
-        const int tok = w.tile * TILE + lane * 16;
-        const int y = ((id * p.c.n_kv + w.kvh) << p.c.bs_log2) + (tok & ((1 << p.c.bs_log2) - 1));
-        tma_load_2d(ring + st * L::kStageBytes + lane * 16 * HD, &p.map_k, &full[st], 0, y);
-        tma_load_2d(ring + st * L::kStageBytes + L::kHalfBytes + lane * 16 * HD, &p.map_v, &full[st], 0, y);
+      const uint32_t st = issued % DEPTH, have = __ballot_sync(0xffffffffu, id >= 0);
+      const int at = w.tile * TILE & ((1 << p.c.bs_log2) - 1);     // place of the tile's first token in its block (blocks of 16 begin at every part)
+      if (box_log2 == 5) {
+        int y[MT / 2];
+#pragma unroll
+        for (int b = 0; b < MT / 2; ++b)
+          y[b] = ((__shfl_sync(0xffffffffu, id, 2 * b) * p.c.n_kv + w.kvh) << p.c.bs_log2) + ((at + 32 * b) & ((1 << p.c.bs_log2) - 1));
+        if (elect_one()) {
+          mbar_expect_tx(&full[st], __popc(have & 0x55555555u) * (2u * HD * 32u));
+#pragma unroll
+          for (int b = 0; b < MT / 2; ++b)
+            if (have & (1u << (2 * b))) {
+              tma_load_2d(ring + st * L::kStageBytes + b * 32 * HD, &p.map_k, &full[st], 0, y[b]);
+              tma_load_2d(ring + st * L::kStageBytes + L::kHalfBytes + b * 32 * HD, &p.map_v, &full[st], 0, y[b]);
+            }
+        }
+      } else {
+        int y[MT];
+#pragma unroll
+        for (int b = 0; b < MT; ++b) y[b] = (__shfl_sync(0xffffffffu, id, b) * p.c.n_kv + w.kvh) << 4;
+        if (elect_one()) {
+          mbar_expect_tx(&full[st], __popc(have) * (2u * HD * 16u));
+#pragma unroll
+          for (int b = 0; b < MT; ++b)
+            if (have & (1u << b)) {
+              tma_load_2d(ring + st * L::kStageBytes + b * 16 * HD, &p.map_k, &full[st], 0, y[b]);
+              tma_load_2d(ring + st * L::kStageBytes + L::kHalfBytes + b * 16 * HD, &p.map_v, &full[st], 0, y[b]);
+            }
+        }
       }
       __syncwarp();
       ++issued;
+      return have;
     };
     auto load_scales = [&](const Walk& w, int id) {
       float2 sc = make_float2(0.f, 0.f);
@@ -278,9 +300,8 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
       scales[d] = make_float2(0.f, 0.f);
       some[d] = 0;
       if (more(iw)) {
-        issue(iw, next_id);
+        some[d] = issue(iw, next_id);
         scales[d] = load_scales(iw, next_id);
-        some[d] = __ballot_sync(0xffffffffu, next_id >= 0);
         advance(iw);
         next_id = load_id(iw);
       }
@@ -477,9 +498,8 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
           some[d] = some[d + 1];
         }
         if (more(iw)) {
-          issue(iw, next_id);
+          some[DEPTH - 1] = issue(iw, next_id);
           scales[DEPTH - 1] = load_scales(iw, next_id);
-          some[DEPTH - 1] = __ballot_sync(0xffffffffu, next_id >= 0);
           advance(iw);
           next_id = load_id(iw);
         }

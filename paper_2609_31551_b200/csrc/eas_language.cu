@@ -224,7 +224,7 @@ static int attention_rows(int group) { return group <= 8 ? 8 : 16; }
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 static size_t attention_workspace(const eas_cache* c, int32_t n_heads, size_t* o_off) {
   const int r = attention_rows(n_heads / c->d.n_kv_heads);
-  const int warps = r != 8 ? CacheAttnCfg<64, 2>::kWarps : c->d.head_dim == 64 ? CacheAttnCfg<64, 1>::kWarps : CacheAttnCfg<128, 1>::kWarps;
+  const int warps = r == 8 ? CacheAttnCfg<128, 1>::kWarps : CacheAttnCfg<128, 2>::kWarps;
   const size_t rows = static_cast<size_t>(2) * c->sm_count * warps * r;
   *o_off = up256(rows * 8);
   return *o_off + rows * c->d.head_dim * 4;
