@@ -178,20 +178,37 @@ static CacheView view_of(const eas_cache* c) {
   return CacheView{c->d.k, c->d.v, c->d.k_scale, c->d.v_scale, c->d.n_blocks, c->d.n_kv_heads, c->bs_log2};
 }
 
-template <int HD, typename T>
-static eas_status launch_rows(bool store, const CacheRowsParams& p, int budget, bool all, cudaStream_t stream) {
-  // one CTA an SM: on a share of the SMs the shared-memory request keeps a second one out; on all of them it is not needed, and L1 is larger
+// One CTA an SM: on a share of the SMs the shared-memory request keeps a second one out; on all of them it is not needed, and L1 is larger.
+template <int HD, int GT, typename T>
+static eas_status launch_store(const CacheRowsParams& p, int budget, bool all, cudaStream_t stream) {
   static OncePerDevice once;
   if (once.first()) {
-    CUDA_TRY(cudaFuncSetAttribute(cache_store_kernel<HD, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kOnePerSmSmem));
+    CUDA_TRY(cudaFuncSetAttribute(cache_store_kernel<HD, GT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kOnePerSmSmem));
+    once.settled();
+  }
+  int groups = 1024 / GT;                                        // few units: fewer groups of threads a CTA, so that every SM has some
+  while (groups > 1 && static_cast<long long>(groups / 2) * budget >= p.units) groups /= 2;
+  const int grid = static_cast<int>(std::min<long long>(budget, (p.units + groups - 1) / groups));
+  return launch_kernel(cache_store_kernel<HD, GT, T>, grid, groups * GT, all ? 0 : kOnePerSmSmem, stream, p);
+}
+template <int HD, typename T>
+static eas_status launch_rows(bool store, const CacheRowsParams& p, int budget, bool all, cudaStream_t stream) {
+  if (store) {
+    switch (HD << p.c.bs_log2) {                                 // values of a block and head: 64 a thread
+      case 16384: return launch_store<HD, 256, T>(p, budget, all, stream);
+      case 8192: return launch_store<HD, 128, T>(p, budget, all, stream);
+      case 4096: return launch_store<HD, 64, T>(p, budget, all, stream);
+      default: return launch_store<HD, 32, T>(p, budget, all, stream);
+    }
+  }
+  static OncePerDevice once;
+  if (once.first()) {
     CUDA_TRY(cudaFuncSetAttribute(cache_load_kernel<HD, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kOnePerSmSmem));
     once.settled();
   }
-  // few units: fewer warps a CTA, so that every SM has some
   int warps = 32;
-  while (warps > 4 && static_cast<long long>(warps / 2) * budget >= p.units) warps /= 2;
-  const int grid = static_cast<int>(std::min<long long>(budget, (p.units + warps - 1) / warps));
-  return launch_kernel(store ? cache_store_kernel<HD, T> : cache_load_kernel<HD, T>, grid, warps * 32, all ? 0 : kOnePerSmSmem, stream, p);
+  while (warps > 4 && warps / 2 * budget >= p.n_rows) warps /= 2;
+  return launch_kernel(cache_load_kernel<HD, T>, std::min(budget, (p.n_rows + warps - 1) / warps), warps * 32, all ? 0 : kOnePerSmSmem, stream, p);
 }
 
 static eas_status cache_rows(bool store, const eas_cache* c, const eas_cache_seqs* s, void* k, int64_t ld_k, void* v, int64_t ld_v, int32_t n_rows,
