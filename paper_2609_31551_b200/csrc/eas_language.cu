@@ -186,7 +186,7 @@ static eas_status launch_store(const CacheRowsParams& p, int budget, bool all, c
     CUDA_TRY(cudaFuncSetAttribute(cache_store_kernel<HD, GT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kOnePerSmSmem));
     once.settled();
   }
-  int groups = 1024 / GT;                                        // few units: fewer groups of threads a CTA, so that every SM has some
+  int groups = 512 / GT;                                         // few units: fewer groups of threads a CTA, so that every SM has some
   while (groups > 1 && static_cast<long long>(groups / 2) * budget >= p.units) groups /= 2;
   const int grid = static_cast<int>(std::min<long long>(budget, (p.units + groups - 1) / groups));
   return launch_kernel(cache_store_kernel<HD, GT, T>, grid, groups * GT, all ? 0 : kOnePerSmSmem, stream, p);
@@ -206,7 +206,7 @@ static eas_status launch_rows(bool store, const CacheRowsParams& p, int budget, 
     CUDA_TRY(cudaFuncSetAttribute(cache_load_kernel<HD, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kOnePerSmSmem));
     once.settled();
   }
-  int warps = 32;
+  int warps = 16;
   while (warps > 4 && warps / 2 * budget >= p.n_rows) warps /= 2;
   return launch_kernel(cache_load_kernel<HD, T>, std::min(budget, (p.n_rows + warps - 1) / warps), warps * 32, all ? 0 : kOnePerSmSmem, stream, p);
 }

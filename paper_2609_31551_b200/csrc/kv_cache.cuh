@@ -105,6 +105,35 @@ __device__ __forceinline__ uint32_t quantise(float x, float s, float inv) {
   const uint32_t kb = __float_as_uint(k + 12582912.0f);          // 1.5 * 2^23: k in the low bits, two's complement
   return kb + ((d > 0.0f || (d == 0.0f && (kb & 1u))) ? 1u : 0u);
 }
+// Eight values (four words of two) to eight numbers.  The rounded product is the answer wherever it is not within 2^-15 of a tie (it is off by
+// less than 127 * 2^-22); only then the exact test above decides.
+template <typename T>
+__device__ __forceinline__ uint2 quantise8(const uint4& x, float s, float inv) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  const uint64_t inv2 = pack2(inv, inv), magic = pack2(12582912.0f, 12582912.0f), less = pack2(-12582912.0f, -12582912.0f), minus = pack2(-1.0f, -1.0f);
+  uint32_t q[8];
+  float off = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint64_t r = fmul2(pack2(Pair16<T>::lo(w[i]), Pair16<T>::hi(w[i])), inv2);
+    const uint64_t t = fadd2(r, magic);                          // the nearest integer in the low bits
+    float a, b, d0, d1;
+    unpack2(t, a, b);
+    unpack2(ffma2(fadd2(t, less), minus, r), d0, d1);
+    off = fmax3(off, fabsf(d0), fabsf(d1));
+    q[2 * i] = __float_as_uint(a);
+    q[2 * i + 1] = __float_as_uint(b);
+  }
+  if (__builtin_expect(off > 0.5f - 3.0517578125e-05f, 0)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      q[2 * i] = quantise(Pair16<T>::lo(w[i]), s, inv);
+      q[2 * i + 1] = quantise(Pair16<T>::hi(w[i]), s, inv);
+    }
+  }
+  return make_uint2(__byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410),
+                    __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410));
+}
 // The same for a number that is in the block already: number * old / s.  The product has too many bits for one fma, so what comes
 // within 2^-10 of a tie is decided in fp64 (31 by 24 bits: the rounded quotient is a tie exactly where the true one is).
 __device__ __forceinline__ uint32_t requantise(int q, float old, float s, float ratio) {
@@ -116,10 +145,10 @@ __device__ __forceinline__ uint32_t requantise(int q, float old, float s, float 
 
 // GT threads per (sequence, block, head, keys or values): the largest magnitude of the new rows, the scale, the numbers.  Memory-bound: 2 bytes
 // read and 1 written per value.  A thread holds all of its values, at most 8 loads of 16 bytes (GT = block_size * head_dim / 64): they are all
-// in flight at once, 128 KB an SM, and are read once.  (One warp per block, reading the rows twice in four trips each: 24 us instead of 11 for 6227
+// in flight at once, 64 KB an SM, and are read once.  (One warp per block, reading the rows twice in four trips each: 24 us instead of 9 for 6227
 // tokens of 8 heads of 128, blocks of 64.)
 template <int HD, int GT, typename T>
-__global__ void __launch_bounds__(1024, 1) cache_store_kernel(const __grid_constant__ CacheRowsParams p) {
+__global__ void __launch_bounds__(512, 1) cache_store_kernel(const __grid_constant__ CacheRowsParams p) {
   __shared__ uint32_t group_max[32];
   if (p.early_launch) pdl_launch_dependents();
   pdl_wait();
@@ -189,95 +218,114 @@ __global__ void __launch_bounds__(1024, 1) cache_store_kernel(const __grid_const
     int8_t* out = dst + (r.lo + sub) * HD + chunk * 8;
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-      if (sub + i * kRows < n) {
-        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-        uint32_t q[8];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          q[2 * e] = quantise(Pair16<T>::lo(w[e]), s, inv);
-          q[2 * e + 1] = quantise(Pair16<T>::hi(w[e]), s, inv);
-        }
-        uint2 y;
-        y.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
-        y.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
-        *reinterpret_cast<uint2*>(out + i * kRows * HD) = y;
-      }
+      if (sub + i * kRows < n) *reinterpret_cast<uint2*>(out + i * kRows * HD) = quantise8<T>(x[i], s, inv);
     }
     if (tid == 0) *scale = s;
   }
 }
 
-// four bytes of x (two's complement) as floats, exact: 2^23 + 128 + number as the bit pattern 0x4B0000xx, less 2^23 + 128
-__device__ __forceinline__ void bytes_to_floats(uint32_t x, float (&f)[4]) {
+// Four numbers (bytes of x, two's complement) times the scale, rounded to the data type.  0x4B000000 | (byte ^ 0x80) is 2^23 + 128 + number as
+// fp32, so the number is exact and the product the one fp32 rounding of number * scale.
+template <typename T>
+__device__ __forceinline__ uint2 dequantise4(uint32_t x, uint64_t scale2) {
   x ^= 0x80808080u;
+  const uint64_t less = pack2(-8388736.0f, -8388736.0f);
+  float f[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(__byte_perm(x, 0x4B000000u, 0x7440 | i)) - 8388736.0f;
+  for (int i = 0; i < 4; i += 2) {
+    const uint64_t raw = pack2(__uint_as_float(__byte_perm(x, 0x4B000000u, 0x7440 | i)), __uint_as_float(__byte_perm(x, 0x4B000000u, 0x7441 | i)));
+    unpack2(fmul2(fadd2(raw, less), scale2), f[i], f[i + 1]);
+  }
+  return make_uint2(Pair16<T>::pack(f[0], f[1]), Pair16<T>::pack(f[2], f[3]));
 }
 
-// One warp per row of k and of v, in stretches of neighbouring rows.  Memory-bound: 1 byte read and 2 written per value.  A lane has 8 loads of 8
-// values in flight, of whichever heads; rows are written whole.  (One warp per block and head: 43 us instead of 24 for 19993 tokens of 8 heads of 128.)
+// A warp takes a stretch of neighbouring rows of k and of v, and of it the runs that lie in one block each.  Memory-bound: 1 byte read and 2
+// written per value; rows are written whole, and two rows of keys and values are in flight (16 loads of 8 values a lane).  (One warp per
+// block and head: 43 us instead of 23 for 19993 tokens of 8 heads of 128.)
 template <int HD, typename T>
-__global__ void __launch_bounds__(1024, 1) cache_load_kernel(const __grid_constant__ CacheRowsParams p) {
+__global__ void __launch_bounds__(512, 1) cache_load_kernel(const __grid_constant__ CacheRowsParams p) {
   if (p.early_launch) pdl_launch_dependents();
   pdl_wait();
-  constexpr int kChunks = HD / 8, kBatch = 8;
-  const int lane = threadIdx.x & 31, row_chunks = p.c.n_kv * kChunks;    // 8 values each; keys, then values
+  constexpr int kChunks = HD / 8, kBatch = 4;                    // 8 values each; 128 chunks of a row at a time
+  const int lane = threadIdx.x & 31, row_chunks = p.c.n_kv * kChunks;
   const int warps = gridDim.x * (blockDim.x >> 5), me = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
   auto cu = [&](int i) { return min(max(__ldg(p.s.cu + i), 0), p.n_rows); };
-  int row = static_cast<int>(static_cast<long long>(p.n_rows) * me / warps);
+  const int begin = static_cast<int>(static_cast<long long>(p.n_rows) * me / warps);
   const int end = static_cast<int>(static_cast<long long>(p.n_rows) * (me + 1) / warps);
-  if (row >= end) return;
+  if (begin >= end) return;
   int s = 0, hi = p.s.n_seqs - 1;
-  while (s < hi) {                                               // the last sequence that begins at or before the row
+  while (s < hi) {                                               // the last sequence that begins at or before the first row
     const int mid = (s + hi + 1) >> 1;
-    if (cu(mid) <= row) s = mid; else hi = mid - 1;
+    if (cu(mid) <= begin) s = mid; else hi = mid - 1;
   }
-  int first = cu(s), next = cu(s + 1);
-  long long start = __ldg(p.s.start + s);
-  for (; row < end; ++row) {
-    while (row >= next && s + 1 < p.s.n_seqs) {
-      ++s;
-      first = next;
-      next = cu(s + 1);
-      start = __ldg(p.s.start + s);
+  for (int row = begin; row < end;) {
+    while (row >= cu(s + 1) && s + 1 < p.s.n_seqs) ++s;
+    const int first = cu(s), next = min(cu(s + 1), end);
+    if (row < first || row >= next) {                            // a row of no sequence
+      ++row;
+      continue;
     }
-    if (row < first || row >= next) continue;                    // a row of no sequence
-    const long long at = start + (row - first), b = at >> p.c.bs_log2;
+    const long long at = __ldg(p.s.start + s) + static_cast<long long>(row - first), b = at >> p.c.bs_log2;
+    const int place = static_cast<int>(at) & ((1 << p.c.bs_log2) - 1), n = min(next - row, (1 << p.c.bs_log2) - place);
     int block = -1;
     if (at >= 0 && b < p.s.max_blocks) block = __ldg(p.s.table + s * p.s.ld_table + b);
     if (block < 0 || block >= p.c.n_blocks) {
       if (lane == 0) raise_status(p.status, DEV_ERR_CACHE_RANGE);
+      row += n;
       continue;
     }
-    const int place = static_cast<int>(at) & ((1 << p.c.bs_log2) - 1);
     const long long block0 = static_cast<long long>(block) * p.c.n_kv;
-    for (int base = lane; base < 2 * row_chunks; base += 32 * kBatch) {
-      uint2 x[kBatch];
-      float sc[kBatch];
+    for (int base = lane; base < row_chunks; base += 32 * kBatch) {
+      const int8_t *k[kBatch], *v[kBatch];
+      uint64_t ks[kBatch], vs[kBatch];
+      bool there[kBatch];
 #pragma unroll
       for (int i = 0; i < kBatch; ++i) {
-        const int c = base + 32 * i;
-        if (c < 2 * row_chunks) {
-          const bool values = c >= row_chunks;
-          const int cc = values ? c - row_chunks : c, head = cc / kChunks;
-          x[i] = *reinterpret_cast<const uint2*>((values ? p.c.v : p.c.k) + (((block0 + head) << p.c.bs_log2) + place) * HD + (cc % kChunks) * 8);
-          sc[i] = (values ? p.c.v_scale : p.c.k_scale)[block0 + head];
-        }
+        const int c = base + 32 * i, head = c / kChunks;
+        there[i] = c < row_chunks;
+        const long long from = (((block0 + head) << p.c.bs_log2) + place) * HD + c % kChunks * 8;
+        k[i] = p.c.k + from;
+        v[i] = p.c.v + from;
+        const float x = there[i] ? p.c.k_scale[block0 + head] : 0.f, y = there[i] ? p.c.v_scale[block0 + head] : 0.f;
+        ks[i] = pack2(x, x);
+        vs[i] = pack2(y, y);
       }
+      T *to_k = static_cast<T*>(p.k) + row * p.ld_k + base * 8, *to_v = static_cast<T*>(p.v) + row * p.ld_v + base * 8;
+      auto fetch = [&](int t, uint2 (&x)[2 * kBatch]) {
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        const int c = base + 32 * i;
-        if (c < 2 * row_chunks) {
-          const bool values = c >= row_chunks;
-          T* dst = static_cast<T*>(values ? p.v : p.k) + row * (values ? p.ld_v : p.ld_k) + (values ? c - row_chunks : c) * 8;
-          float f[4], g[4];
-          bytes_to_floats(x[i].x, f);
-          bytes_to_floats(x[i].y, g);
-          *reinterpret_cast<uint4*>(dst) = make_uint4(Pair16<T>::pack(f[0] * sc[i], f[1] * sc[i]), Pair16<T>::pack(f[2] * sc[i], f[3] * sc[i]),
-                                                      Pair16<T>::pack(g[0] * sc[i], g[1] * sc[i]), Pair16<T>::pack(g[2] * sc[i], g[3] * sc[i]));
-        }
+        for (int i = 0; i < kBatch; ++i)
+          if (there[i]) {
+            x[i] = *reinterpret_cast<const uint2*>(k[i] + t * HD);
+            x[kBatch + i] = *reinterpret_cast<const uint2*>(v[i] + t * HD);
+          }
+      };
+      auto put = [&](const uint2 (&x)[2 * kBatch]) {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+          if (there[i]) {
+            const uint2 a = dequantise4<T>(x[i].x, ks[i]), b2 = dequantise4<T>(x[i].y, ks[i]);
+            *reinterpret_cast<uint4*>(to_k + i * 256) = make_uint4(a.x, a.y, b2.x, b2.y);
+            const uint2 c = dequantise4<T>(x[kBatch + i].x, vs[i]), d = dequantise4<T>(x[kBatch + i].y, vs[i]);
+            *reinterpret_cast<uint4*>(to_v + i * 256) = make_uint4(c.x, c.y, d.x, d.y);
+          }
+        to_k += p.ld_k;
+        to_v += p.ld_v;
+      };
+      uint2 x[2 * kBatch], y[2 * kBatch];
+      int t = 0;
+#pragma unroll 1
+      for (; t + 1 < n; t += 2) {
+        fetch(t, x);
+        fetch(t + 1, y);
+        put(x);
+        put(y);
+      }
+      if (t < n) {
+        fetch(t, x);
+        put(x);
       }
     }
+    row += n;
   }
 }
 
