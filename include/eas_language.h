@@ -44,9 +44,17 @@ typedef struct {
   const int32_t* cu_k; /* host [n_seqs + 1], likewise */
 } eas_prompt_inputs;
 
-/* status_dev: device uint32 (caller zeroes it) that the kernel raises to 1 when a bounded wait expires.
- * Errors (nothing launched): INVALID_ARG, UNSUPPORTED (head_dim, dtype, heads per key/value head), ARCH, CUDA. */
-eas_status eas_prompt_attention(const eas_prompt_inputs* in, int32_t sm_budget, void* stream, uint32_t* status_dev);
+/* Device scratch of a call on the current device, for these shapes: 0 for most (and on bad arguments).  A call whose query tiles are too few
+ * for the device's SMs although its key ranges are long cuts the key ranges and joins the parts; a sequence's last bits then depend on
+ * what else is in the call. */
+size_t eas_prompt_attention_workspace_bytes(const eas_prompt_inputs* in);
+
+/* workspace: device, 256-byte aligned, of that size (NULL where it is 0); its contents do not matter, and nothing of it is used by a later
+ * call, but calls that may run at the same time need one each.  status_dev: device uint32 (caller zeroes it) that the kernel raises to 1 when a
+ * bounded wait expires.
+ * Errors (nothing launched): INVALID_ARG, UNSUPPORTED (head_dim, dtype, heads per key/value head), WORKSPACE, ARCH, CUDA. */
+eas_status eas_prompt_attention(const eas_prompt_inputs* in, void* workspace, size_t workspace_bytes, int32_t sm_budget, void* stream,
+                                uint32_t* status_dev);
 
 /* ---- 8-bit key/value cache ----
  * Keys and values are signed 8-bit numbers in blocks of block_size tokens, with one scale for each block and head (keys and

@@ -20,6 +20,11 @@
 // its O row in TMEM.  Scores, sums and O are fp32; P is rounded to the data type (bf16 or fp16: what the matrix product takes), and the
 // output once at the end.  A row's arithmetic depends on its own sequence alone, not on the unit, the packing or the SMs.
 //
+// Few rows against many keys (a chunk of a prompt behind a long prefix) make fewer units than there are SMs.  SPLIT cuts every unit's key
+// steps into n_split equal parts, work items of their own that leave (m, l, O) in the workspace, fp32, and prompt_join_kernel puts them
+// together in order.  The host chooses n_split from the call's shapes and the device, not from sm_budget.  512 queries of 40 heads
+// (8 key/value heads of 128) behind 11801 keys: 88 units of 154 steps, KBEFORE us in one piece, KAFTER in KSPLIT parts.
+//
 // Masked keys: their scores are replaced by -inf (P exactly 0), whatever K held.  0 x Inf is not 0, so value rows behind the
 // sequence's end are cleared in shared memory, and a row whose O is not finite although its sum is (a value row that later rows of the tile
 // see, this one does not, holds Inf or NaN) is computed again by plain fp32 loops over the keys it sees.
@@ -43,6 +48,9 @@ struct PromptParams {
   int n_seqs, total_units;
   int q0[kPromptMaxSeqs], k0[kPromptMaxSeqs], len_q[kPromptMaxSeqs], len_k[kPromptMaxSeqs];
   int unit_prefix[kPromptMaxSeqs + 1];
+  int n_split;            // parts of a unit's key steps (SPLIT)
+  float4* o_ws;           // [unit][part][tile][HD / 4][128 rows]: O, not divided by the sum
+  float2* ml_ws;          // [unit][part][tile][128 rows]: reference and sum (-inf, 0: no key)
   uint32_t* status;
   int early_launch;
 };
@@ -118,10 +126,10 @@ __device__ __forceinline__ uint32_t pack_16x2(float lo, float hi) {
   else return pack_bf16x2(lo, hi);
 }
 
-// One output row again, by a whole warp (lane i: HD / 32 dims): out = sum over the keys that the row sees.  Only elements that are not
-// finite although every value that the row sees is are replaced.
+// Columns col0 .. col0 + cols - 1 of one output row again, by a whole warp (lane i: HD / 32 dims): sums over the keys that the row sees.  Only
+// elements that are not finite although every value that the row sees is are replaced.
 template <int HD, bool FP16>
-__device__ __noinline__ void prompt_repair(const PromptParams& p, int q_row, int q_head, int kv_head, int k0, int limit, float m, float l) {
+__device__ __noinline__ void prompt_repair(const PromptParams& p, int q_row, int q_head, int kv_head, int k0, int limit, float m, float l, int col0, int cols) {
   constexpr int N = HD / 32;
   const int lane = threadIdx.x & 31;
   uint16_t* dst = p.out + q_row * p.ld_out + q_head * HD + lane * N;
@@ -133,7 +141,7 @@ __device__ __noinline__ void prompt_repair(const PromptParams& p, int q_row, int
   for (int i = 0; i < N; ++i) {
     q[i] = load16(p.q[q_row * p.ld_q + q_head * HD + lane * N + i], FP16);
     acc[i] = 0.f;
-    if (!isfinite(load16(dst[i], FP16))) bad |= 1u << i;
+    if (lane * N + i >= col0 && lane * N + i < col0 + cols && !isfinite(load16(dst[i], FP16))) bad |= 1u << i;
   }
   for (int j = 0; j < limit && __any_sync(0xffffffffu, bad != 0u); j += 8)
     for (int e = j; e < min(j + 8, limit); ++e)
@@ -157,7 +165,22 @@ __device__ __noinline__ void prompt_repair(const PromptParams& p, int q_row, int
     if (bad & (1u << i)) dst[i] = static_cast<uint16_t>(pack_16x2<FP16>(acc[i] / l, 0.f));
 }
 
-template <int HD, bool FP16>
+// key steps [lo, hi) of a part: of the unit, or (hi capped) of one of its tiles
+struct PromptPart {
+  int unit, lo, hi;
+};
+template <int HD, bool SPLIT>
+__device__ __forceinline__ PromptUnit prompt_item(const PromptParams& p, int item, int& cursor, PromptPart& part) {
+  const int unit = SPLIT ? item / p.n_split : item;
+  const PromptUnit u = prompt_decode<HD>(p, unit, cursor);
+  const int i = SPLIT ? item - unit * p.n_split : 0;
+  part.unit = unit;
+  part.lo = SPLIT ? u.n_max * i / p.n_split : 0;
+  part.hi = SPLIT ? u.n_max * (i + 1) / p.n_split : u.n_max;
+  return u;
+}
+
+template <int HD, bool FP16, bool SPLIT>
 __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_kernel(const __grid_constant__ PromptParams p) {
   using L = PromptCfg<HD>;
   constexpr int NST = L::kStages, NWG = L::kWg, KEYS = L::kKeys;
@@ -210,9 +233,10 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
       uint32_t g = 0, round = 0;
       bool ok = true;
       int cursor = 0;
-      for (int unit = attn_unit_at(0); unit < p.total_units && ok; unit = attn_unit_at(++round)) {
-        const PromptUnit u = prompt_decode<HD>(p, unit, cursor);
-        for (int j = 0; j < u.n_max; ++j, ++g) {
+      for (int item = attn_unit_at(0); item < p.total_units && ok; item = attn_unit_at(++round)) {
+        PromptPart part;
+        const PromptUnit u = prompt_item<HD, SPLIT>(p, item, cursor, part);
+        for (int j = part.lo; j < part.hi; ++j, ++g) {
           const uint32_t s = g % NST;
           if (!mbar_wait(&kv_empty[s], ((g / NST) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
           const int y = u.k0 + j * KEYS, z = u.head * L::kHalves;
@@ -246,12 +270,13 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
     bool ok = true;
     int cursor = 0;
     PromptUnit un{};
-    int un_steps = 0;                            // key steps of this issuer's tile in the next unit (0: none)
-    auto look = [&](int unit) {
+    PromptPart un_part{};
+    int un_steps = 0;                            // key steps of this issuer's tile in the next item (0: none)
+    auto look = [&](int item) {
       un_steps = 0;
-      if (unit < p.total_units) {
-        un = prompt_decode<HD>(p, unit, cursor);
-        if (w < un.n_q) un_steps = prompt_steps<HD>(p, un, w);
+      if (item < p.total_units) {
+        un = prompt_item<HD, SPLIT>(p, item, cursor, un_part);
+        if (w < un.n_q) un_steps = max(min(un_part.hi, prompt_steps<HD>(p, un, w)) - un_part.lo, 0);
       }
     };
     look(attn_unit_at(0));
@@ -304,11 +329,12 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
       umma_commit(&s_full[w]);
     };
 
-    for (int unit = attn_unit_at(0); unit < p.total_units && ok; unit = attn_unit_at(++round)) {
+    for (int item = attn_unit_at(0); item < p.total_units && ok; item = attn_unit_at(++round)) {
       const PromptUnit u = un;
+      const PromptPart part = un_part;
       const int n_steps = un_steps;
       look(attn_unit_at(round + 1));
-      const uint32_t next_base = base + static_cast<uint32_t>(u.n_max);
+      const uint32_t next_base = base + static_cast<uint32_t>(part.hi - part.lo);
       if (n_steps == 0) {
         ok = hand_back(base, next_base);
         base = next_base;
@@ -338,7 +364,7 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
           load_q(un);
         }
         if (last && !hand_back(g + 1, next_base)) { ok = false; break; }
-        const int rows = u.len_k - j * KEYS;     // key rows of this step that belong to the sequence
+        const int rows = u.len_k - (part.lo + j) * KEYS;     // key rows of this step that belong to the sequence
         if (!OWN_P && !warp_mbar_wait(&v_full[g % NST], (g / NST) & 1u, abort_flag)) { ok = false; break; }
         if (!OWN_P && rows < KEYS) clear_behind(g, rows);
         if (more && !k_landed(gn)) { ok = false; break; }
@@ -389,7 +415,25 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
     bool pend = false;
     int pend_q = -1, pend_head = 0, pend_k0 = 0, pend_limit = 0;   // query row (-1: not stored), key/value head, first key row, keys seen
     float pend_l = 1.f, pend_m = 0.f;
+    int pend_slot = 0;                             // SPLIT: the part's place in the workspace
     auto flush_output = [&]() {
+      if constexpr (SPLIT) {
+        float4* dst = p.o_ws + static_cast<long long>(pend_slot) * (HD / 4) * 128 + row;
+#pragma unroll 1
+        for (int c = 0; c < HD / 16; ++c) {
+          uint32_t o[16];
+          __syncwarp();
+          tmem_ld_32x16(o_addr + c * 16, o);
+          tmem_ld_wait_16<0>(o);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            dst[(c * 4 + i) * 128] = make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]), __uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3]));
+        }
+        p.ml_ws[static_cast<long long>(pend_slot) * 128 + row] = make_float2(pend_l == 0.f ? -INFINITY : pend_m, pend_l);
+        __syncwarp();
+        pend = false;
+        return;
+      }
       const float inv = pend_limit > 0 ? 1.0f / pend_l : 0.f;
       uint4* dst = reinterpret_cast<uint4*>(p.out + static_cast<long long>(max(pend_q, 0)) * p.ld_out + (pend_head * p.group + row_head) * HD);
       bool wrong = false;
@@ -418,7 +462,7 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
         __syncwarp();
         prompt_repair<HD, FP16>(p, __shfl_sync(0xffffffffu, pend_q, src), __shfl_sync(0xffffffffu, pend_head * p.group + row_head, src), pend_head,
                                 pend_k0, __shfl_sync(0xffffffffu, pend_limit, src), __shfl_sync(0xffffffffu, pend_m, src),
-                                __shfl_sync(0xffffffffu, pend_l, src));
+                                __shfl_sync(0xffffffffu, pend_l, src), 0, HD);
       }
       __syncwarp();
       pend = false;
@@ -426,9 +470,10 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
 
     int cursor = 0;
     uint32_t round = 0;
-    for (int unit = attn_unit_at(0); unit < p.total_units && ok; unit = attn_unit_at(++round)) {
-      const PromptUnit u = prompt_decode<HD>(p, unit, cursor);
-      const int n_steps = w < u.n_q ? prompt_steps<HD>(p, u, w) : 0;
+    for (int item = attn_unit_at(0); item < p.total_units && ok; item = attn_unit_at(++round)) {
+      PromptPart part;
+      const PromptUnit u = prompt_item<HD, SPLIT>(p, item, cursor, part);
+      const int n_steps = w < u.n_q ? max(min(part.hi, prompt_steps<HD>(p, u, w)) - part.lo, 0) : 0;
       const int tok = (u.tile0 + w) * p.tile_tokens + row_tok;
       const bool stored = w < u.n_q && row_tok < p.tile_tokens && tok < u.len_q;
       if (n_steps == 0) {                           // no tile in this unit, or one that sees no key
@@ -443,7 +488,8 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
             mbar_arrive_if(&p_ready[w], lane == 0);        // the issuer may use s_full[w] again
           }
         }
-        if (stored) {
+        if (SPLIT && w < u.n_q) p.ml_ws[(static_cast<long long>(item) * NWG + w) * 128 + row] = make_float2(-INFINITY, 0.f);
+        if (!SPLIT && stored) {
           uint4* dst = reinterpret_cast<uint4*>(p.out + (static_cast<long long>(u.q0) + tok) * p.ld_out + (u.head * p.group + row_head) * HD);
           for (int c = 0; c < HD / 8; ++c) dst[c] = make_uint4(0u, 0u, 0u, 0u);
         }
@@ -453,7 +499,7 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
       const int limit = stored ? max(tok + 1 + u.ahead, 0) : 0x7fffffff;
       float m_used = 0.f;
       uint64_t l2[2] = {0, 0};                      // row sum, two packed accumulators
-      int left = limit;                             // of them from this step on
+      int left = limit - part.lo * KEYS;            // of them from this step on
 #pragma unroll 1
       for (int j = 0; j < n_steps; ++j, left -= KEYS) {
         if (!warp_mbar_wait(&s_full[w], n & 1u, abort_flag)) { ok = false; break; }
@@ -553,6 +599,7 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
       pend_head = u.head;
       pend_k0 = u.k0;
       pend_limit = stored ? limit : 0;
+      if (SPLIT) pend_slot = item * NWG + w;
     }
     if (ok && pend) {
       if (warp_mbar_wait(OWN_P ? &pv_done[w] : &s_full[w], (OWN_P ? n - 1u : n) & 1u, abort_flag)) {
@@ -569,6 +616,68 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
     tmem_dealloc(tmem_base, 512);
   }
   if (threadIdx.x == 0 && *abort_flag) atomicCAS(p.status, DEV_OK, DEV_ERR_WAIT_TIMEOUT);
+}
+
+// The parts of a split call put together: 128 threads, one a row, per (unit, tile, quarter of the columns).
+template <int HD, bool FP16>
+__global__ void __launch_bounds__(512, 1) prompt_join_kernel(const __grid_constant__ PromptParams p) {
+  constexpr int NWG = PromptCfg<HD>::kWg, COLS = HD / 4;
+  if (p.early_launch) pdl_launch_dependents();
+  pdl_wait();
+  const int row = threadIdx.x & 127, row_tok = row / p.group, row_head = row - row_tok * p.group;
+  const int units = p.total_units / p.n_split;
+  int cursor = 0;
+  for (int it = blockIdx.x * 4 + (threadIdx.x >> 7); it < units * NWG * 4; it += gridDim.x * 4) {
+    const int unit = it / (NWG * 4), w = it / 4 % NWG, col0 = it % 4 * COLS;
+    const PromptUnit u = prompt_decode<HD>(p, unit, cursor);
+    if (w >= u.n_q) continue;
+    const int tok = (u.tile0 + w) * p.tile_tokens + row_tok, limit = max(tok + 1 + u.ahead, 0);
+    const bool stored = row_tok < p.tile_tokens && tok < u.len_q;
+    auto slot = [&](int part) { return (static_cast<long long>(unit) * p.n_split + part) * NWG + w; };
+    float m = -INFINITY, l = 0.f;
+    for (int part = 0; part < p.n_split; ++part) m = fmaxf(m, p.ml_ws[slot(part) * 128 + row].x);
+    float acc[COLS];
+#pragma unroll
+    for (int i = 0; i < COLS; ++i) acc[i] = 0.f;
+    for (int part = 0; part < p.n_split; ++part) {
+      const float2 ml = p.ml_ws[slot(part) * 128 + row];
+      if (__all_sync(0xffffffffu, ml.y == 0.f)) continue;        // no key for any of the rows: O was not written
+      const float4* o = p.o_ws + (slot(part) * (HD / 4) + col0 / 4) * 128 + row;
+      float4 x[COLS / 4];
+#pragma unroll
+      for (int i = 0; i < COLS / 4; ++i) x[i] = o[i * 128];
+      const float f = ml.y == 0.f ? 0.f : fast_ex2((ml.x - m) * p.scale_log2);
+      l = fmaf(ml.y, f, l);
+#pragma unroll
+      for (int i = 0; i < COLS / 4; ++i) {
+        acc[4 * i] = ml.y == 0.f ? acc[4 * i] : fmaf(x[i].x, f, acc[4 * i]);
+        acc[4 * i + 1] = ml.y == 0.f ? acc[4 * i + 1] : fmaf(x[i].y, f, acc[4 * i + 1]);
+        acc[4 * i + 2] = ml.y == 0.f ? acc[4 * i + 2] : fmaf(x[i].z, f, acc[4 * i + 2]);
+        acc[4 * i + 3] = ml.y == 0.f ? acc[4 * i + 3] : fmaf(x[i].w, f, acc[4 * i + 3]);
+      }
+    }
+    const float inv = limit > 0 ? 1.0f / l : 0.f;
+    bool wrong = false;
+    uint16_t* dst = p.out + (static_cast<long long>(u.q0) + tok) * p.ld_out + (u.head * p.group + row_head) * HD + col0;
+#pragma unroll
+    for (int i = 0; i < COLS; i += 8) {
+      uint32_t y[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        wrong = wrong || !(acc[i + 2 * e] * 0.f + acc[i + 2 * e + 1] * 0.f == 0.f);
+        y[e] = limit > 0 ? pack_16x2<FP16>(acc[i + 2 * e] * inv, acc[i + 2 * e + 1] * inv) : 0u;
+      }
+      if (stored) *reinterpret_cast<uint4*>(dst + i) = make_uint4(y[0], y[1], y[2], y[3]);
+    }
+    uint32_t todo = __ballot_sync(0xffffffffu, wrong && stored && limit > 0 && l * 0.f == 0.f);
+    while (__builtin_expect(todo != 0u, 0)) {
+      const int src = __ffs(todo) - 1;
+      todo &= todo - 1u;
+      __syncwarp();
+      prompt_repair<HD, FP16>(p, __shfl_sync(0xffffffffu, u.q0 + tok, src), __shfl_sync(0xffffffffu, u.head * p.group + row_head, src), u.head, u.k0,
+                              __shfl_sync(0xffffffffu, limit, src), __shfl_sync(0xffffffffu, m, src), __shfl_sync(0xffffffffu, l, src), col0, COLS);
+    }
+  }
 }
 
 }  // namespace eas

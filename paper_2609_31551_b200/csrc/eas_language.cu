@@ -32,31 +32,109 @@ static eas_status prompt_kv_map(CUtensorMap* m, const void* k, int heads, int hd
   return make_tmap(m, k, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-template <int HD, bool FP16>
-static eas_status launch_prompt(PromptParams& pp, int budget, cudaStream_t stream) {
+template <int HD, bool FP16, bool SPLIT>
+static eas_status launch_prompt(PromptParams& pp, int budget, bool all, cudaStream_t stream) {
   using L = PromptCfg<HD>;
   static OncePerDevice once;
   if (once.first()) {
-    CUDA_TRY(cudaFuncSetAttribute(prompt_attention_kernel<HD, FP16>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes));
+    CUDA_TRY(cudaFuncSetAttribute(prompt_attention_kernel<HD, FP16, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes));
+    if (SPLIT) CUDA_TRY(cudaFuncSetAttribute(prompt_join_kernel<HD, FP16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kOnePerSmSmem));
     once.settled();
   }
-  return launch_kernel(prompt_attention_kernel<HD, FP16>, std::min(budget, pp.total_units), L::kThreads, L::kBytes, stream, pp);
+  EAS_TRY(launch_kernel(prompt_attention_kernel<HD, FP16, SPLIT>, std::min(budget, pp.total_units), L::kThreads, L::kBytes, stream, pp));
+  if (!SPLIT) return EAS_OK;
+  const int tiles = pp.total_units / pp.n_split * L::kWg;         // 4 threads' groups a CTA, one each for a quarter of a tile's columns
+  return launch_kernel(prompt_join_kernel<HD, FP16>, std::min(budget, tiles), 512, all ? 0 : kOnePerSmSmem, stream, pp);
 }
 
-static eas_status prompt_attention(const eas_prompt_inputs* in, int32_t sm_budget, void* stream, uint32_t* status_dev) {
+// How the work of up to kPromptMaxSeqs sequences is laid out: the units in the order in which they are dealt, and into how many parts their
+// key steps are cut.
+struct PromptPlan {
+  std::vector<int> order;        // sequences with queries, longest first (stable): the tail of the static deal is short work
+  int wg = 0, tile_tokens = 0;
+};
+static PromptPlan prompt_plan(const eas_prompt_inputs* in) {
+  PromptPlan plan;
+  plan.wg = in->head_dim == 64 ? PromptCfg<64>::kWg : PromptCfg<128>::kWg;
+  plan.tile_tokens = 128 / (in->n_heads / in->n_kv_heads);
+  for (int i = 0; i < in->n_seqs; ++i)
+    if (in->cu_q[i + 1] > in->cu_q[i]) plan.order.push_back(i);
+  std::stable_sort(plan.order.begin(), plan.order.end(),
+                   [&](int a, int b) { return in->cu_k[a + 1] - in->cu_k[a] > in->cu_k[b + 1] - in->cu_k[b]; });
+  return plan;
+}
+// Parts of the key steps for sequences order[first .. first + n).  Costs in key steps of a unit (1.2 us at head_dim 128): the busiest SM's
+// steps, kItemSteps a work item for its beginning and end, and what the parts' way through L2 takes.  One part unless another number is
+// clearly better; only for calls of fewer than kSplitUnits units an SM with long key ranges, where the deal leaves SMs without work.
+constexpr int kSplitUnits = 4, kSplitMost = 16, kSplitLeastSteps = 24;
+constexpr double kItemSteps = 2.0, kPartStepsPerSm = 0.35;
+static int prompt_split(const eas_prompt_inputs* in, const PromptPlan& plan, int first, int n, int sms) {
+  constexpr int keys = PromptCfg<64>::kKeys;
+  int64_t units = 0, total = 0, most = 0;        // of all units: their number and key steps; the costliest
+  for (int j = 0; j < n; ++j) {
+    const int i = plan.order[first + j], len_q = in->cu_q[i + 1] - in->cu_q[i], len_k = in->cu_k[i + 1] - in->cu_k[i];
+    const int64_t tiles = (static_cast<int64_t>(len_q) + plan.tile_tokens - 1) / plan.tile_tokens, per_head = (tiles + plan.wg - 1) / plan.wg;
+    units += per_head * in->n_kv_heads;
+    if (units > static_cast<int64_t>(kSplitUnits) * sms) return 1;
+    for (int64_t t = 1; t <= per_head; ++t) {
+      const int64_t seen = std::min<int64_t>(t * plan.wg * plan.tile_tokens, len_q) + len_k - len_q, steps = (std::max<int64_t>(seen, 0) + keys - 1) / keys;
+      most = std::max(most, steps);
+      total += steps * in->n_kv_heads;
+    }
+  }
+  if (most < kSplitLeastSteps) return 1;
+  double best = 0;
+  int parts = 1;
+  for (int s = 1; s <= kSplitMost && (s == 1 || most / s >= 8); ++s) {
+    const int64_t rounds = (units * s + sms - 1) / sms;          // the busiest SM has that many items of middling cost, or the costliest one
+    double t = std::max(static_cast<double>(rounds) * total / (static_cast<double>(units) * s), static_cast<double>(most) / s) + rounds * kItemSteps;
+    if (s > 1) t = 1.05 * t + 3.0 + kPartStepsPerSm * s * static_cast<double>(units) / sms;      // (3: the joining launch)
+    if (s == 1 || t < best) { best = t; parts = s; }
+  }
+  return parts;
+}
+static int64_t prompt_units(const eas_prompt_inputs* in, const PromptPlan& plan, int i) {
+  const int64_t tiles = (static_cast<int64_t>(in->cu_q[i + 1]) - in->cu_q[i] + plan.tile_tokens - 1) / plan.tile_tokens;
+  return (tiles + plan.wg - 1) / plan.wg * in->n_kv_heads;
+}
+static size_t prompt_part_bytes(int wg, int hd) { return static_cast<size_t>(wg) * 128 * (static_cast<size_t>(hd) * 4 + 8); }
+
+static eas_status check_prompt(const eas_prompt_inputs* in) {
   if (in == nullptr) return fail(EAS_ERR_INVALID_ARG, "inputs are null");
   const int H = in->n_heads, G = in->n_kv_heads, hd = in->head_dim, n = in->n_seqs;
   if (n < 0) return fail(EAS_ERR_INVALID_ARG, "n_seqs %d", n);
-  if (in->cu_q == nullptr || in->cu_k == nullptr || status_dev == nullptr) return fail(EAS_ERR_INVALID_ARG, "a required pointer is null");
+  if (in->cu_q == nullptr || in->cu_k == nullptr) return fail(EAS_ERR_INVALID_ARG, "a required pointer is null");
   if (in->dtype != EAS_DTYPE_BF16 && in->dtype != EAS_DTYPE_FP16) return fail(EAS_ERR_UNSUPPORTED, "dtype %d", in->dtype);
   if (hd != 64 && hd != 128) return fail(EAS_ERR_UNSUPPORTED, "head_dim %d (supported: 64, 128)", hd);
   if (H <= 0 || G <= 0 || H % G != 0) return fail(EAS_ERR_INVALID_ARG, "%d query heads for %d key/value heads", H, G);
   if (H / G > 128) return fail(EAS_ERR_UNSUPPORTED, "%d query heads per key/value head (at most 128)", H / G);
-  if (!(in->scale > 0.0f) || !std::isfinite(in->scale)) return fail(EAS_ERR_INVALID_ARG, "scale must be positive and finite");
   if (in->cu_q[0] < 0 || in->cu_k[0] < 0) return fail(EAS_ERR_INVALID_ARG, "cu_q and cu_k start at 0 or above");
   for (int i = 0; i < n; ++i)
     if (in->cu_q[i + 1] < in->cu_q[i] || in->cu_k[i + 1] < in->cu_k[i])
       return fail(EAS_ERR_INVALID_ARG, "cu_q or cu_k decreases at sequence %d", i);
+  return EAS_OK;
+}
+
+// scratch of a call on this device: that of its costliest launch
+static size_t prompt_workspace(const eas_prompt_inputs* in, const PromptPlan& plan, int sms) {
+  size_t bytes = 0;
+  const int rows = static_cast<int>(plan.order.size());
+  for (int first = 0; first < rows; first += kPromptMaxSeqs) {
+    const int n = std::min(kPromptMaxSeqs, rows - first), parts = prompt_split(in, plan, first, n, sms);
+    if (parts == 1) continue;
+    int64_t units = 0;
+    for (int j = 0; j < n; ++j) units += prompt_units(in, plan, plan.order[first + j]);
+    bytes = std::max(bytes, static_cast<size_t>(units) * parts * prompt_part_bytes(plan.wg, in->head_dim));
+  }
+  return bytes;
+}
+
+static eas_status prompt_attention(const eas_prompt_inputs* in, void* workspace, size_t workspace_bytes, int32_t sm_budget, void* stream,
+                                   uint32_t* status_dev) {
+  EAS_TRY(check_prompt(in));
+  if (status_dev == nullptr) return fail(EAS_ERR_INVALID_ARG, "a required pointer is null");
+  if (!(in->scale > 0.0f) || !std::isfinite(in->scale)) return fail(EAS_ERR_INVALID_ARG, "scale must be positive and finite");
+  const int H = in->n_heads, G = in->n_kv_heads, hd = in->head_dim, n = in->n_seqs;
   const int64_t Tq = in->cu_q[n], Tk = in->cu_k[n], wq = static_cast<int64_t>(H) * hd, wk = static_cast<int64_t>(G) * hd;
   if (Tq > in->cu_q[0]) {
     if (in->q == nullptr || in->out == nullptr || (Tk > 0 && (in->k == nullptr || in->v == nullptr)))
@@ -86,29 +164,39 @@ static eas_status prompt_attention(const eas_prompt_inputs* in, int32_t sm_budge
   pp.ld_q = in->ld_q; pp.ld_k = in->ld_k; pp.ld_v = in->ld_v; pp.ld_out = in->ld_out;
   pp.scale_log2 = static_cast<float>(in->scale * kLog2e);
   pp.status = status_dev;
-  const int wg = hd == 64 ? PromptCfg<64>::kWg : PromptCfg<128>::kWg;
-  std::vector<int> order;                                        // longest first (stable): the tail of the static deal is short work
-  for (int i = 0; i < n; ++i)
-    if (in->cu_q[i + 1] > in->cu_q[i]) order.push_back(i);
-  std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return in->cu_k[a + 1] - in->cu_k[a] > in->cu_k[b + 1] - in->cu_k[b]; });
-  const int rows = static_cast<int>(order.size());
+  const PromptPlan plan = prompt_plan(in);
+  int sms = 0;
+  EAS_TRY(device_check(&sms));
+  const size_t need = prompt_workspace(in, plan, sms);
+  if (workspace_bytes < need || (need > 0 && workspace == nullptr))
+    return fail(EAS_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace == nullptr ? 0 : workspace_bytes, need);
+  if (need > 0 && (reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return fail(EAS_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
+  const bool all = budget == sms, h = in->dtype == EAS_DTYPE_FP16;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const int rows = static_cast<int>(plan.order.size());
   for (int first = 0; first < rows; first += kPromptMaxSeqs) {
     pp.n_seqs = std::min(kPromptMaxSeqs, rows - first);
     int64_t units = 0;
     for (int j = 0; j < pp.n_seqs; ++j) {
-      const int i = order[first + j];
+      const int i = plan.order[first + j];
       pp.q0[j] = in->cu_q[i]; pp.len_q[j] = in->cu_q[i + 1] - in->cu_q[i];
       pp.k0[j] = in->cu_k[i]; pp.len_k[j] = in->cu_k[i + 1] - in->cu_k[i];
       pp.unit_prefix[j] = static_cast<int>(units);
-      const int64_t tiles = (static_cast<int64_t>(pp.len_q[j]) + pp.tile_tokens - 1) / pp.tile_tokens;
-      units += (tiles + wg - 1) / wg * G;
-      if (units > (1 << 30)) return fail(EAS_ERR_UNSUPPORTED, "too many query rows for one call");
+      units += prompt_units(in, plan, i);
+      if (units > (1 << 26)) return fail(EAS_ERR_UNSUPPORTED, "too many query rows for one call");
     }
-    pp.unit_prefix[pp.n_seqs] = pp.total_units = static_cast<int>(units);
-    const bool h = in->dtype == EAS_DTYPE_FP16;
-    const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    EAS_TRY(hd == 64 ? (h ? launch_prompt<64, true>(pp, budget, st) : launch_prompt<64, false>(pp, budget, st))
-                     : (h ? launch_prompt<128, true>(pp, budget, st) : launch_prompt<128, false>(pp, budget, st)));
+    pp.unit_prefix[pp.n_seqs] = static_cast<int>(units);
+    pp.n_split = prompt_split(in, plan, first, pp.n_seqs, sms);
+    pp.total_units = static_cast<int>(units) * pp.n_split;
+    if (pp.n_split == 1) {
+      EAS_TRY(hd == 64 ? (h ? launch_prompt<64, true, false>(pp, budget, all, st) : launch_prompt<64, false, false>(pp, budget, all, st))
+                       : (h ? launch_prompt<128, true, false>(pp, budget, all, st) : launch_prompt<128, false, false>(pp, budget, all, st)));
+    } else {
+      pp.o_ws = static_cast<float4*>(workspace);
+      pp.ml_ws = reinterpret_cast<float2*>(pp.o_ws + static_cast<size_t>(pp.total_units) * plan.wg * 128 * (hd / 4));
+      EAS_TRY(hd == 64 ? (h ? launch_prompt<64, true, true>(pp, budget, all, st) : launch_prompt<64, false, true>(pp, budget, all, st))
+                       : (h ? launch_prompt<128, true, true>(pp, budget, all, st) : launch_prompt<128, false, true>(pp, budget, all, st)));
+    }
   }
   return EAS_OK;
 }
@@ -310,9 +398,21 @@ static eas_status cache_attention(const eas_cache* c, const eas_cache_seqs* s, c
 }
 
 // ------------------------------------------------------------------------------------ entry points (no exception passes them)
-extern "C" eas_status eas_prompt_attention(const eas_prompt_inputs* in, int32_t sm_budget, void* stream, uint32_t* status_dev) {
+extern "C" size_t eas_prompt_attention_workspace_bytes(const eas_prompt_inputs* in) {
+  int sms = 0;
+  if (check_prompt(in) != EAS_OK || device_check(&sms) != EAS_OK) return 0;
   try {
-    return prompt_attention(in, sm_budget, stream, status_dev);
+    return prompt_workspace(in, prompt_plan(in), sms);
+  } catch (const std::bad_alloc&) {
+    fail(EAS_ERR_INVALID_ARG, "out of host memory");
+    return 0;
+  }
+}
+
+extern "C" eas_status eas_prompt_attention(const eas_prompt_inputs* in, void* workspace, size_t workspace_bytes, int32_t sm_budget, void* stream,
+                                           uint32_t* status_dev) {
+  try {
+    return prompt_attention(in, workspace, workspace_bytes, sm_budget, stream, status_dev);
   } catch (const std::bad_alloc&) {
     return fail(EAS_ERR_INVALID_ARG, "out of host memory");
   }

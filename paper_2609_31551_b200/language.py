@@ -13,7 +13,7 @@ import torch
 from . import binding as B
 
 LANGUAGE_SYMBOLS = [
-    "eas_prompt_attention", "eas_cache_create", "eas_cache_destroy", "eas_cache_store", "eas_cache_load",
+    "eas_prompt_attention_workspace_bytes", "eas_prompt_attention", "eas_cache_create", "eas_cache_destroy", "eas_cache_store", "eas_cache_load",
     "eas_cache_attention_workspace_bytes", "eas_cache_attention",
 ]
 STATUS_CACHE_RANGE = 3          # EAS_DEVICE_CACHE_RANGE
@@ -45,7 +45,9 @@ def lib():
     l = B.load_library()
     if not _declared:
         l.eas_prompt_attention.restype = C.c_int
-        l.eas_prompt_attention.argtypes = [C.POINTER(PromptInputs), C.c_int32, C.c_void_p, C.c_void_p]
+        l.eas_prompt_attention.argtypes = [C.POINTER(PromptInputs), C.c_void_p, C.c_size_t, C.c_int32, C.c_void_p, C.c_void_p]
+        l.eas_prompt_attention_workspace_bytes.restype = C.c_size_t
+        l.eas_prompt_attention_workspace_bytes.argtypes = [C.POINTER(PromptInputs)]
         l.eas_cache_create.restype = C.c_int
         l.eas_cache_create.argtypes = [C.POINTER(CacheDesc), C.POINTER(C.c_void_p)]
         l.eas_cache_destroy.restype = None
@@ -109,17 +111,18 @@ def _host_ints(x, name):
     return x, x.__array_interface__["data"][0]
 
 
-def prompt_attention(q, k, v, cu_seqlens_host, cu_seqlens_k_host=None, scale=None, out=None, sm_budget=0, stream=None, status=None):
+def prompt_attention(q, k, v, cu_seqlens_host, cu_seqlens_k_host=None, scale=None, out=None, sm_budget=0, stream=None, status=None, workspace=None):
     """eas_prompt_attention: causal attention of packed prompts.  q [T, n_heads, head_dim], k and v [T_k, n_kv_heads, head_dim];
     cu_seqlens_host (int32 [n + 1]) gives the queries of each sequence, cu_seqlens_k_host its keys (default: the same; a sequence's
-    queries are the last tokens among its keys).  scale: 1 / sqrt(head_dim).  Returns (out, device status word); `out` and
-    `status` (device int32, zeroed by the caller) can be passed in so that a call allocates nothing."""
+    queries are the last tokens among its keys).  scale: 1 / sqrt(head_dim).  Returns (out, device status word); `out`, `status` (device
+    int32, zeroed by the caller) and `workspace` (uint8, on a 256-byte boundary; few calls need one, and calls that may run at the same
+    time one each) can be passed in so that a call allocates nothing."""
     dtype, index = q.dtype, q.get_device()
     if index < 0 or dtype not in _DTYPES or q.dim() != 3 or k.dim() != 3:
         raise B.EasError(1, f"q and k must be bf16 or fp16 tensors [tokens, heads, head_dim] on a GPU, q is {dtype} {tuple(q.shape)} on {q.device}")
     if _elsewhere(index, stream):
         with _on(index, stream):
-            return prompt_attention(q, k, v, cu_seqlens_host, cu_seqlens_k_host, scale, out, sm_budget, None, status)
+            return prompt_attention(q, k, v, cu_seqlens_host, cu_seqlens_k_host, scale, out, sm_budget, None, status, workspace)
     T, H, hd = q.shape
     Tk, G, _ = k.shape
     ld_q, ld_k, ld_v = _rows(q, "q", H, hd, dtype, index), _rows(k, "k", G, hd, dtype, index), _rows(v, "v", G, hd, dtype, index)
@@ -136,10 +139,30 @@ def prompt_attention(q, k, v, cu_seqlens_host, cu_seqlens_k_host=None, scale=Non
         status = torch.zeros(4, dtype=torch.int32, device=q.device)
     pin = PromptInputs(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), ld_q, ld_k, ld_v, ld_out, _DTYPES[dtype], H, G, hd,
                        hd ** -0.5 if scale is None else scale, cu_q.size - 1, at_q, at_k)
-    rc = lib().eas_prompt_attention(C.byref(pin), sm_budget, torch._C._cuda_getCurrentRawStream(index), status.data_ptr())
+    l = lib()
+    if workspace is None:
+        need = l.eas_prompt_attention_workspace_bytes(C.byref(pin))
+        at, size = None, 0
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    elif workspace.get_device() != index or not workspace.is_contiguous():
+        raise B.EasError(1, "workspace must be a contiguous tensor on the GPU of q")
+    if workspace is not None:
+        at, size = workspace.data_ptr(), workspace.nbytes
+    rc = l.eas_prompt_attention(C.byref(pin), at, size, sm_budget, torch._C._cuda_getCurrentRawStream(index), status.data_ptr())
     if rc:
         B._check(rc)
     return out, status
+
+
+def prompt_attention_workspace_bytes(n_heads, n_kv_heads, head_dim, cu_seqlens_host, cu_seqlens_k_host=None):
+    """eas_prompt_attention_workspace_bytes: scratch of a prompt_attention call of these shapes on the current device (0 for most)."""
+    cu_q, at_q = _host_ints(cu_seqlens_host, "cu_seqlens")
+    cu_k, at_k = (cu_q, at_q) if cu_seqlens_k_host is None else _host_ints(cu_seqlens_k_host, "cu_seqlens_k")
+    if cu_k.size != cu_q.size:
+        raise B.EasError(1, "cu_seqlens are two lists of the same length")
+    pin = PromptInputs(n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, scale=1.0, n_seqs=cu_q.size - 1, cu_q=at_q, cu_k=at_k)
+    return lib().eas_prompt_attention_workspace_bytes(C.byref(pin))
 
 
 class KvCache:

@@ -205,6 +205,46 @@ def test_prompt_attention_long_sequence_tail_rows():
         assert ((out[i:i + 1].double().cpu() - ref).abs() <= tol).all()
 
 
+@pytest.mark.parametrize("hd,dtype", [(64, torch.float16), (128, torch.bfloat16), (128, torch.float16)])
+@pytest.mark.parametrize("H,G,lens,keys", [(10, 2, [40], [9000]), (8, 8, [5, 0, 33], [4001, 77, 6000]), (4, 1, [1], [12345]), (3, 1, [131], [2400]), (8, 2, [60, 20], [2500, 3])])
+def test_prompt_attention_few_queries_many_keys(hd, dtype, H, G, lens, keys):
+    """Too few tiles for the device: the key steps are cut and joined (workspace), rows that see few or no keys among them."""
+    import paper_2609_31551_b200 as P
+    cu_q, cu_k = _cu(lens), _cu(keys)
+    need = P.prompt_attention_workspace_bytes(H, G, hd, cu_q, cu_k)
+    assert need > 0
+    q = _rand((cu_q[-1], H, hd), dtype, 1, 2.0)
+    k, v = _rand((cu_k[-1], G, hd), dtype, 2), _rand((cu_k[-1], G, hd), dtype, 3)
+    args = (q.cuda(), k.cuda(), v.cuda(), cu_q, cu_k)
+    out, status = P.prompt_attention(*args)
+    assert int(status[0]) == 0
+    _check_prompt(q, k, v, cu_q, cu_k, out, hd ** -0.5)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")     # whatever the workspace holds
+    for budget in (1, 50):
+        again, status = P.prompt_attention(*args, sm_budget=budget, workspace=ws)
+        assert int(status[0]) == 0 and torch.equal(out, again)
+    with pytest.raises(P.EasError) as e:
+        P.prompt_attention(*args, workspace=ws[:need - 256])
+    assert e.value.status == 3
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_prompt_attention_split_and_non_finite_values(hd):
+    import paper_2609_31551_b200 as P
+    cu_q, cu_k = _cu([50]), _cu([5000])
+    q, k, v = _rand((50, 4, hd), torch.bfloat16, 4, 2.0), _rand((5000, 2, hd), torch.bfloat16, 5), _rand((5000, 2, hd), torch.bfloat16, 6)
+    v[4980, 0, 3], k[4990, 1, 5], v[100, 1, 9] = float("inf"), float("nan"), float("-inf")
+    assert P.prompt_attention_workspace_bytes(4, 2, hd, cu_q, cu_k) > 0
+    out, status = P.prompt_attention(q.cuda(), k.cuda(), v.cuda(), cu_q, cu_k)
+    assert int(status[0]) == 0
+    out = out.double().cpu()
+    ref, mag, smax = LO.prompt_attention(q, k, v, cu_q, cu_k, hd ** -0.5)
+    assert (out[30:, :2, 3] == float("inf")).all() and (out[:40, 2:, 9] == float("-inf")).all() and torch.isnan(out[40:, 2:]).any(-1).all()
+    fin = torch.isfinite(ref)
+    tol = _bound(mag, smax, hd, U[q.dtype], U[q.dtype], 5000, 5.0, False)
+    assert torch.isfinite(out[fin]).all() and ((out - ref).abs()[fin] <= tol[fin]).all()
+
+
 def test_prompt_attention_other_stream_and_graph():
     import paper_2609_31551_b200 as P
     cu = _cu([100, 33])

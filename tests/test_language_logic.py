@@ -101,15 +101,15 @@ def _inputs(lang, **over):
 ])
 def test_prompt_refusals(lang, over, status):
     pin = _inputs(lang, **over)
-    assert lang.lib().eas_prompt_attention(C.byref(pin), 0, None, 1 << 24) == status
+    assert lang.lib().eas_prompt_attention(C.byref(pin), None, 0, 0, None, 1 << 24) == status
     assert lang.lib().eas_last_error()
 
 
 def test_null_arguments_are_refused(lang):
     l = lang.lib()
     pin = _inputs(lang)
-    assert l.eas_prompt_attention(C.byref(pin), 0, None, None) == 1
-    assert l.eas_prompt_attention(None, 0, None, 1 << 24) == 1
+    assert l.eas_prompt_attention(C.byref(pin), None, 0, 0, None, None) == 1
+    assert l.eas_prompt_attention(None, None, 0, 0, None, 1 << 24) == 1
     seqs, h = lang.CacheSeqs(), C.c_void_p()
     assert l.eas_cache_create(None, C.byref(h)) == 1 and not h
     assert l.eas_cache_create(C.byref(lang.CacheDesc(16, 16, 16, 16, 1, 16, 1, 64)), None) == 1
