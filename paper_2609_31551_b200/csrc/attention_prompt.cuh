@@ -36,6 +36,18 @@
 namespace eas {
 
 constexpr int kPromptMaxSeqs = 128;      // sequences of one launch (kernel parameters)
+constexpr int kPromptListed = 2048;      // units that the list of a launch holds
+
+// k / d for 0 <= k < 2^24 and d <= 256 by one multiplication (by ceil(2^32 / d): off by less than k d / 2^32 < 1 / d), else by division
+struct Divider {
+  uint32_t mul;           // 0: divide
+  int d;
+#ifdef __CUDACC__
+  __device__ __forceinline__ int operator()(int k) const {
+    return d == 1 ? k : mul != 0u ? static_cast<int>(__umulhi(static_cast<uint32_t>(k), mul)) : k / d;
+  }
+#endif
+};
 
 struct PromptParams {
   CUtensorMap map_q;      // [tokens, heads, HD], box {64, group, 128 / group}, 128-byte swizzle
@@ -47,7 +59,13 @@ struct PromptParams {
   float scale_log2;       // scale * log2(e)
   int n_seqs, total_units;
   int q0[kPromptMaxSeqs], k0[kPromptMaxSeqs], len_q[kPromptMaxSeqs], len_k[kPromptMaxSeqs];
+  int tiles[kPromptMaxSeqs], per_head[kPromptMaxSeqs];     // of a sequence and key/value head: row tiles, units
   int unit_prefix[kPromptMaxSeqs + 1];
+  Divider by_kv, by_split;
+  // Few rounds of units of different cost: the deal follows this list, costliest first (sequence << 24 | unit of the sequence), instead of
+  // the sequences one after the other (8 prompts of 1 to 1563 tokens, 580 units: 14 to 39 key steps an SM without it)
+  int listed;
+  uint32_t list[kPromptListed];
   int n_split;            // parts of a unit's key steps (SPLIT)
   float4* o_ws;           // [unit][part][tile][HD / 4][128 rows]: O, not divided by the sum
   float2* ml_ws;          // [unit][part][tile][128 rows]: reference and sum (-inf, 0: no key)
@@ -99,20 +117,27 @@ __device__ __forceinline__ int prompt_steps(const PromptParams& p, const PromptU
 template <int HD>
 __device__ __forceinline__ PromptUnit prompt_decode(const PromptParams& p, int unit, int& cursor) {
   constexpr int NWG = PromptCfg<HD>::kWg;
-  int lo = cursor;
-  while (lo + 1 < p.n_seqs && p.unit_prefix[lo + 1] <= unit) ++lo;
-  cursor = lo;
+  int lo = cursor, k;
+  if (p.listed) {
+    const uint32_t e = p.list[unit];
+    lo = static_cast<int>(e >> 24);
+    k = static_cast<int>(e & 0xFFFFFFu);
+  } else {
+    while (lo + 1 < p.n_seqs && p.unit_prefix[lo + 1] <= unit) ++lo;
+    k = unit - p.unit_prefix[lo];
+    cursor = lo;
+  }
   PromptUnit u;
   u.q0 = p.q0[lo];
   u.k0 = p.k0[lo];
   u.len_q = p.len_q[lo];
   u.len_k = p.len_k[lo];
   u.ahead = u.len_k - u.len_q;
-  const int tiles = (u.len_q + p.tile_tokens - 1) / p.tile_tokens, per_head = (tiles + NWG - 1) / NWG;
-  const int k = unit - p.unit_prefix[lo], back = k / p.n_kv;
+  const int back = p.by_kv(k);
   u.head = k - back * p.n_kv;
-  u.tile0 = (per_head - 1 - back) * NWG;
-  u.n_q = min(NWG, tiles - u.tile0);
+  const int from = p.tiles[lo] - (back + 1) * NWG;        // a remainder of tiles is the cheapest unit, not the costliest
+  u.tile0 = max(from, 0);
+  u.n_q = NWG + min(from, 0);
   u.n_max = prompt_steps<HD>(p, u, u.n_q - 1);
   return u;
 }
@@ -124,6 +149,11 @@ template <bool FP16>
 __device__ __forceinline__ uint32_t pack_16x2(float lo, float hi) {
   if constexpr (FP16) return Pair16<__half>::pack(lo, hi);
   else return pack_bf16x2(lo, hi);
+}
+
+__device__ __forceinline__ void store_32bytes(void* dst, const uint32_t (&v)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
 
 // Columns col0 .. col0 + cols - 1 of one output row again, by a whole warp (lane i: HD / 32 dims): sums over the keys that the row sees.  Only
@@ -171,12 +201,12 @@ struct PromptPart {
 };
 template <int HD, bool SPLIT>
 __device__ __forceinline__ PromptUnit prompt_item(const PromptParams& p, int item, int& cursor, PromptPart& part) {
-  const int unit = SPLIT ? item / p.n_split : item;
+  const int unit = SPLIT ? p.by_split(item) : item;
   const PromptUnit u = prompt_decode<HD>(p, unit, cursor);
   const int i = SPLIT ? item - unit * p.n_split : 0;
   part.unit = unit;
-  part.lo = SPLIT ? u.n_max * i / p.n_split : 0;
-  part.hi = SPLIT ? u.n_max * (i + 1) / p.n_split : u.n_max;
+  part.lo = SPLIT ? p.by_split(u.n_max * i) : 0;
+  part.hi = SPLIT ? p.by_split(u.n_max * (i + 1)) : u.n_max;
   return u;
 }
 
@@ -416,18 +446,23 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
     int pend_q = -1, pend_head = 0, pend_k0 = 0, pend_limit = 0;   // query row (-1: not stored), key/value head, first key row, keys seen
     float pend_l = 1.f, pend_m = 0.f;
     int pend_slot = 0;                             // SPLIT: the part's place in the workspace
+    // 64 columns of O at a time: the trip to tensor memory is what a flush waits for (16 at a time: 1.6 us of a tile's beginning)
+    auto load_64 = [&](uint32_t addr, uint32_t (&o)[64]) {
+      __syncwarp();
+      tmem_ld_32x32_at<0>(addr, o);
+      tmem_ld_32x32_at<32>(addr, o);
+      tmem_ld_wait_16<0>(o); tmem_ld_tie_16<16>(o); tmem_ld_tie_16<32>(o); tmem_ld_tie_16<48>(o);
+    };
     auto flush_output = [&]() {
       if constexpr (SPLIT) {
         float4* dst = p.o_ws + static_cast<long long>(pend_slot) * (HD / 4) * 128 + row;
 #pragma unroll 1
-        for (int c = 0; c < HD / 16; ++c) {
-          uint32_t o[16];
-          __syncwarp();
-          tmem_ld_32x16(o_addr + c * 16, o);
-          tmem_ld_wait_16<0>(o);
+        for (int c = 0; c < HD; c += 64) {
+          uint32_t o[64];
+          load_64(o_addr + c, o);
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            dst[(c * 4 + i) * 128] = make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]), __uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3]));
+          for (int i = 0; i < 16; ++i)
+            dst[(c / 4 + i) * 128] = make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]), __uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3]));
         }
         p.ml_ws[static_cast<long long>(pend_slot) * 128 + row] = make_float2(pend_l == 0.f ? -INFINITY : pend_m, pend_l);
         __syncwarp();
@@ -438,21 +473,20 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
       uint4* dst = reinterpret_cast<uint4*>(p.out + static_cast<long long>(max(pend_q, 0)) * p.ld_out + (pend_head * p.group + row_head) * HD);
       bool wrong = false;
 #pragma unroll 1
-      for (int c = 0; c < HD / 16; ++c) {
-        uint32_t o[16];
-        __syncwarp();
-        tmem_ld_32x16(o_addr + c * 16, o);
-        tmem_ld_wait_16<0>(o);
-        uint32_t pkd[8];
+      for (int c = 0; c < HD; c += 64) {
+        uint32_t o[64];
+        load_64(o_addr + c, o);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          // (Inf x 0 = NaN too: one test for both)
-          wrong = wrong || !(__uint_as_float(o[2 * i]) * 0.f + __uint_as_float(o[2 * i + 1]) * 0.f == 0.f);
-          pkd[i] = pend_limit > 0 ? pack_16x2<FP16>(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv) : 0u;
-        }
-        if (pend_q >= 0) {
-          dst[2 * c] = make_uint4(pkd[0], pkd[1], pkd[2], pkd[3]);
-          dst[2 * c + 1] = make_uint4(pkd[4], pkd[5], pkd[6], pkd[7]);
+        for (int j = 0; j < 4; ++j) {
+          uint32_t pkd[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float lo = __uint_as_float(o[16 * j + 2 * i]), hi = __uint_as_float(o[16 * j + 2 * i + 1]);
+            wrong = wrong || !(lo * 0.f + hi * 0.f == 0.f);      // (Inf x 0 = NaN too: one test for both)
+            pkd[i] = pend_limit > 0 ? pack_16x2<FP16>(lo * inv, hi * inv) : 0u;
+          }
+          // 32 bytes, a whole sector: a warp's store touches 32 rows, and it is the rows that the store unit counts
+          if (pend_q >= 0) store_32bytes(dst + c / 8 + 2 * j, pkd);
         }
       }
       uint32_t todo = __ballot_sync(0xffffffffu, wrong && pend_q >= 0 && pend_limit > 0 && pend_l * 0.f == 0.f);

@@ -76,8 +76,8 @@ static int prompt_split(const eas_prompt_inputs* in, const PromptPlan& plan, int
     const int64_t tiles = (static_cast<int64_t>(len_q) + plan.tile_tokens - 1) / plan.tile_tokens, per_head = (tiles + plan.wg - 1) / plan.wg;
     units += per_head * in->n_kv_heads;
     if (units > static_cast<int64_t>(kSplitUnits) * sms) return 1;
-    for (int64_t t = 1; t <= per_head; ++t) {
-      const int64_t seen = std::min<int64_t>(t * plan.wg * plan.tile_tokens, len_q) + len_k - len_q, steps = (std::max<int64_t>(seen, 0) + keys - 1) / keys;
+    for (int64_t t = tiles; t > 0; t -= plan.wg) {
+      const int64_t seen = std::min<int64_t>(t * plan.tile_tokens, len_q) + len_k - len_q, steps = (std::max<int64_t>(seen, 0) + keys - 1) / keys;
       most = std::max(most, steps);
       total += steps * in->n_kv_heads;
     }
@@ -92,6 +92,32 @@ static int prompt_split(const eas_prompt_inputs* in, const PromptPlan& plan, int
     if (s == 1 || t < best) { best = t; parts = s; }
   }
   return parts;
+}
+// The units of a launch by cost, costliest first (a counting sort over their key steps): they are dealt to the SMs in rounds
+static void prompt_list(PromptParams& pp, int wg) {
+  constexpr int keys = PromptCfg<64>::kKeys;
+  std::vector<int> count;
+  auto steps = [&](int s, int back) {
+    const int seen = std::min((pp.tiles[s] - back * wg) * pp.tile_tokens, pp.len_q[s]) + pp.len_k[s] - pp.len_q[s];
+    return (std::max(seen, 0) + keys - 1) / keys;
+  };
+  for (int s = 0; s < pp.n_seqs; ++s)
+    for (int b = 0; b < pp.per_head[s]; ++b) {
+      const size_t c = static_cast<size_t>(steps(s, b));
+      if (count.size() <= c) count.resize(c + 1, 0);
+      count[c] += pp.n_kv;
+    }
+  int at = 0;
+  for (size_t c = count.size(); c-- > 0;) { const int n = count[c]; count[c] = at; at += n; }
+  for (int s = 0; s < pp.n_seqs; ++s)
+    for (int b = 0; b < pp.per_head[s]; ++b) {
+      int& to = count[static_cast<size_t>(steps(s, b))];
+      for (int h = 0; h < pp.n_kv; ++h) pp.list[to++] = static_cast<uint32_t>(s) << 24 | static_cast<uint32_t>(b * pp.n_kv + h);
+    }
+  pp.listed = 1;
+}
+static Divider divider(int d) {
+  return Divider{d >= 2 && d <= 256 ? static_cast<uint32_t>(((1ull << 32) + d - 1) / d) : 0u, d};
 }
 static int64_t prompt_units(const eas_prompt_inputs* in, const PromptPlan& plan, int i) {
   const int64_t tiles = (static_cast<int64_t>(in->cu_q[i + 1]) - in->cu_q[i] + plan.tile_tokens - 1) / plan.tile_tokens;
@@ -149,7 +175,8 @@ static eas_status prompt_attention(const eas_prompt_inputs* in, void* workspace,
   EAS_TRY(resolve_budget(sm_budget, &budget));
   if (Tq == in->cu_q[0]) return EAS_OK;                          // no query
 
-  PromptParams pp{};
+  PromptParams pp;                                               // (the list behind it is not cleared)
+  pp.listed = 0; pp.o_ws = nullptr; pp.ml_ws = nullptr;
   pp.group = H / G; pp.n_kv = G; pp.tile_tokens = 128 / pp.group;
   EAS_TRY(prompt_q_map(&pp.map_q, in->q, H, hd, Tq, in->ld_q, pp.group, pp.tile_tokens));
   if (Tk > 0) {
@@ -182,12 +209,17 @@ static eas_status prompt_attention(const eas_prompt_inputs* in, void* workspace,
       pp.q0[j] = in->cu_q[i]; pp.len_q[j] = in->cu_q[i + 1] - in->cu_q[i];
       pp.k0[j] = in->cu_k[i]; pp.len_k[j] = in->cu_k[i + 1] - in->cu_k[i];
       pp.unit_prefix[j] = static_cast<int>(units);
+      pp.tiles[j] = (pp.len_q[j] - 1) / pp.tile_tokens + 1;
+      pp.per_head[j] = (pp.tiles[j] - 1) / plan.wg + 1;
       units += prompt_units(in, plan, i);
-      if (units > (1 << 26)) return fail(EAS_ERR_UNSUPPORTED, "too many query rows for one call");
+      if (units > (1 << 24)) return fail(EAS_ERR_UNSUPPORTED, "too many query rows for one call");
     }
     pp.unit_prefix[pp.n_seqs] = static_cast<int>(units);
     pp.n_split = prompt_split(in, plan, first, pp.n_seqs, sms);
     pp.total_units = static_cast<int>(units) * pp.n_split;
+    pp.by_kv = divider(G); pp.by_split = divider(pp.n_split);
+    pp.listed = 0;
+    if (units <= kPromptListed && units > budget && pp.n_seqs > 1) prompt_list(pp, plan.wg);
     if (pp.n_split == 1) {
       EAS_TRY(hd == 64 ? (h ? launch_prompt<64, true, false>(pp, budget, all, st) : launch_prompt<64, false, false>(pp, budget, all, st))
                        : (h ? launch_prompt<128, true, false>(pp, budget, all, st) : launch_prompt<128, false, false>(pp, budget, all, st)));
