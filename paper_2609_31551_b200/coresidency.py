@@ -11,6 +11,10 @@ SMs, and the neighbour's own slow-down.
 
     python -m paper_2609_31551_b200.coresidency --config c1 --micro-batch 8
 
+`--neighbour` chooses what else a language model's workers would run there: `prompt`, the causal attention of a prefill batch (compute-bound
+like the matrix products, with bursts of K and V from L2), or `token`, the attention of a decoding step over 8-bit caches (bound by HBM, which no
+partition of the SMs divides).
+
 The neighbour's kernels never wait for the encoder's or the reverse: they are independent launches on two streams."""
 from __future__ import annotations
 import argparse
@@ -47,6 +51,54 @@ class PrefillNeighbour:
             B.kernel_gemm(self.a, self.w, self.bias, sm_budget=sm_budget, stream=self.stream, out=self.out, status=self.status)
 
 
+class PromptNeighbour:
+    """Prefill attention: a batch of prompts (32 query heads, 8 key/value heads of 128), causal, packed."""
+
+    def __init__(self, lens=(4096, 2048, 1024, 1024)):
+        from . import language as L
+        self._call = L.prompt_attention
+        g = torch.Generator(device="cuda").manual_seed(7)
+        self.cu = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+        qkv = torch.randn(int(self.cu[-1]), 48, 128, device="cuda", generator=g).bfloat16()
+        self.q, self.k, self.v = qkv[:, :32], qkv[:, 32:40], qkv[:, 40:]
+        self.out = torch.empty_like(self.q, memory_format=torch.contiguous_format)
+        self.status = torch.zeros(4, dtype=torch.int32, device="cuda")
+        self.flops = sum(2.0 * n * (n + 1) for n in lens) * 32 * 128
+        self.stream = torch.cuda.Stream()
+
+    def enqueue(self, count: int, sm_budget: int):
+        for _ in range(count):
+            self._call(self.q, self.k, self.v, self.cu, out=self.out, status=self.status, sm_budget=sm_budget, stream=self.stream)
+
+
+class TokenNeighbour:
+    """Decode attention: one token of each of `n` sequences (32 query heads, 8 key/value heads of 128) over its 8-bit cache."""
+
+    def __init__(self, n: int = 64, tokens: int = 4096, block: int = 64):
+        from . import language as L
+        blocks = tokens // block
+        self.cache = L.KvCache(n * blocks, block, 8, 128)
+        self.cache.k.random_(-127, 128)
+        self.cache.v.random_(-127, 128)
+        self.cache.k_scale.fill_(0.03)
+        self.cache.v_scale.fill_(0.03)
+        self.q = torch.randn(n, 32, 128, device="cuda").bfloat16()
+        self.out = torch.empty_like(self.q)
+        self.lens = torch.full((n,), tokens, dtype=torch.int32, device="cuda")
+        self.table = torch.randperm(n * blocks, device="cuda").to(torch.int32).view(n, blocks)
+        self.workspace = torch.empty(self.cache.attention_workspace_bytes(n, 32), dtype=torch.uint8, device="cuda")
+        self.flops = 4.0 * 32 * 128 * n * tokens
+        self.stream = torch.cuda.Stream()
+        torch.cuda.synchronize()
+
+    def enqueue(self, count: int, sm_budget: int):
+        for _ in range(count):
+            self.cache.attention(self.q, self.lens, self.table, out=self.out, workspace=self.workspace, sm_budget=sm_budget, stream=self.stream)
+
+
+NEIGHBOURS = {"gemm": PrefillNeighbour, "prompt": PromptNeighbour, "token": TokenNeighbour}
+
+
 def _encode_ms(enc, batch, sm_budget, reps, stream):
     data, shapes, offsets, cu, cu_dev, out, ws = batch
     e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
@@ -59,12 +111,13 @@ def _encode_ms(enc, batch, sm_budget, reps, stream):
 
 
 def measure(config: str, micro_batch: int, levels=(0.3, 0.5, 0.7), reps: int = 5, neighbour_shape=(4096, 8192, 8192),
-            partition: str = "grid"):
+            partition: str = "grid", neighbour: str = "gemm"):
     """-> list of dicts, one per SM level: encode latency alone / beside the neighbour, and the neighbour's rate.
 
     partition = "grid": both sides bound their SM use by their grid sizes (`sm_budget`) on ordinary streams.
     partition = "green": eas_sm_partition splits the SMs into two driver-enforced sets (green contexts) and each side
-    runs on its set's stream; the level is rounded up to the driver's granularity."""
+    runs on its set's stream; the level is rounded up to the driver's granularity.
+    neighbour: one of NEIGHBOURS; neighbour_shape is the matrix product's."""
     cfg = S.get_config(config)
     enc = B.Encoder(cfg, B.weights_to_device(S.make_weights(cfg)))
     shapes = S.draw_item_shapes(cfg, micro_batch, 3000 + micro_batch)
@@ -76,7 +129,7 @@ def measure(config: str, micro_batch: int, levels=(0.3, 0.5, 0.7), reps: int = 5
     ws = torch.empty(enc.workspace_bytes(int(cu[-1]), len(shapes)) + 1024, dtype=torch.uint8, device="cuda")
     batch = (data, shapes, offsets, cu, cu_dev, out, ws)
     sm_total = torch.cuda.get_device_properties(0).multi_processor_count
-    nb = PrefillNeighbour(*neighbour_shape)
+    nb = PrefillNeighbour(*neighbour_shape) if neighbour == "gemm" else NEIGHBOURS[neighbour]()
     enc_stream = torch.cuda.Stream()
     torch.cuda.synchronize()
 
@@ -127,7 +180,7 @@ def measure(config: str, micro_batch: int, levels=(0.3, 0.5, 0.7), reps: int = 5
         if part is not None:
             enc_stream, nb.stream = plain_streams
             part.close()
-        rows.append({"partition": partition, "sm_encode": n_enc, "sm_neighbour": n_nb, "encode_ms_exclusive": exclusive, "encode_ms_alone": alone,
+        rows.append({"partition": partition, "neighbour": neighbour, "sm_encode": n_enc, "sm_neighbour": n_nb, "encode_ms_exclusive": exclusive, "encode_ms_alone": alone,
                      "encode_ms_beside_neighbour": beside, "inflation": beside / alone,
                      "vs_exclusive": beside / exclusive,
                      "neighbour_tflops_alone": nb.flops / (nb_ms * 1e-3) / 1e12,
@@ -141,8 +194,9 @@ def main():
     ap.add_argument("--micro-batch", type=int, default=8)
     ap.add_argument("--levels", default="0.3,0.5,0.7")
     ap.add_argument("--partition", default="grid", choices=("grid", "green"))
+    ap.add_argument("--neighbour", default="gemm", choices=tuple(NEIGHBOURS))
     a = ap.parse_args()
-    for r in measure(a.config, a.micro_batch, tuple(float(x) for x in a.levels.split(",")), partition=a.partition):
+    for r in measure(a.config, a.micro_batch, tuple(float(x) for x in a.levels.split(",")), partition=a.partition, neighbour=a.neighbour):
         print(json.dumps(r))
 
 

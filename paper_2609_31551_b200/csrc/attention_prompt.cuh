@@ -23,7 +23,7 @@
 // Few rows against many keys (a chunk of a prompt behind a long prefix) make fewer units than there are SMs.  SPLIT cuts every unit's key
 // steps into n_split equal parts, work items of their own that leave (m, l, O) in the workspace, fp32, and prompt_join_kernel puts them
 // together in order.  The host chooses n_split from the call's shapes and the device, not from sm_budget.  512 queries of 40 heads
-// (8 key/value heads of 128) behind 11801 keys: 88 units of 154 steps, KBEFORE us in one piece, KAFTER in KSPLIT parts.
+// (8 key/value heads of 128) behind 11801 keys: 88 units of 154 steps, 210 us in one piece, 134 to 160 (from box to box) in 5 parts.
 //
 // Masked keys: their scores are replaced by -inf (P exactly 0), whatever K held.  0 x Inf is not 0, so value rows behind the
 // sequence's end are cleared in shared memory, and a row whose O is not finite although its sum is (a value row that later rows of the tile

@@ -613,3 +613,23 @@ def test_prompts_then_tokens(hd, dtype, bs):
         now = [n + 1 for n in now]
         _check_tokens(cache, nums, scs, q, now, table)
     assert torch.equal(cache.k.cpu(), nums[0]) and torch.equal(cache.v_scale.cpu(), scs[1])
+
+
+# ------------------------------------------------------------------------------------------------ the commands that call them
+@pytest.mark.parametrize("neighbour", ["prompt", "token"])
+def test_coresidency_with_a_language_model_neighbour(neighbour):
+    from paper_2609_31551_b200 import coresidency
+    rows = coresidency.measure("c0", 2, levels=(0.5,), reps=2, neighbour=neighbour)
+    assert len(rows) == 1 and rows[0]["neighbour"] == neighbour
+    assert rows[0]["encode_ms_beside_neighbour"] > 0 and rows[0]["neighbour_tflops_beside_encoder"] > 0
+
+
+@pytest.mark.parametrize("argv", [["prompt", "--lens", "300x2,17", "--before", "40"], ["token", "--lens", "500x3,1", "--block", "16", "--sm-budget", "20"],
+                                  ["store", "--lens", "300x2,17", "--fp16"], ["load", "--lens", "300x2,17", "--head-dim", "64"]])
+def test_kernel_bench_runs(argv, monkeypatch, capsys):
+    import json
+    from paper_2609_31551_b200 import kernel_bench
+    monkeypatch.setattr("sys.argv", ["kernel_bench"] + argv + ["--iters", "2", "--warmup", "1"])
+    kernel_bench.main()
+    line = json.loads(capsys.readouterr().out)
+    assert line["kernel"] == argv[0] and line["ms"] > 0 and line.get("tflops", line.get("gbs")) > 0
