@@ -34,7 +34,7 @@ typedef struct {
   const void* q;       /* device [cu_q[n_seqs], n_heads * head_dim], distance ld_q */
   const void* k;       /* device [cu_k[n_seqs], n_kv_heads * head_dim], distance ld_k */
   const void* v;       /* the same, distance ld_v */
-  void* out;           /* device, as q, distance ld_out; rows behind cu_q[n_seqs] and in front of cu_q[0] are left alone */
+  void* out;           /* device, as q, distance ld_out, overlaps none of them; rows behind cu_q[n_seqs] and in front of cu_q[0] are left alone */
   int64_t ld_q, ld_k, ld_v, ld_out;
   int32_t dtype;       /* EAS_DTYPE_* */
   int32_t n_heads, n_kv_heads, head_dim; /* at most 128 query heads per key/value head */

@@ -38,7 +38,7 @@ namespace eas {
 constexpr int kPromptMaxSeqs = 128;      // sequences of one launch (kernel parameters)
 constexpr int kPromptListed = 2048;      // units that the list of a launch holds
 
-// k / d for 0 <= k < 2^24 and d <= 256 by one multiplication (by ceil(2^32 / d): off by less than k d / 2^32 < 1 / d), else by division
+// k / d for 0 <= k < 2^24 and d <= 256 by one multiplication (by ceil(2^32 / d): off by less than k / 2^32 < 1 / d), else by division
 struct Divider {
   uint32_t mul;           // 0: divide
   int d;
@@ -55,6 +55,7 @@ struct PromptParams {
   const uint16_t *q, *k, *v;
   uint16_t* out;
   long long ld_q, ld_k, ld_v, ld_out;
+  int out_wide;           // output rows begin on 32-byte boundaries (else on 16-byte ones)
   int group, n_kv, tile_tokens;
   float scale_log2;       // scale * log2(e)
   int n_seqs, total_units;
@@ -486,7 +487,12 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
             pkd[i] = pend_limit > 0 ? pack_16x2<FP16>(lo * inv, hi * inv) : 0u;
           }
           // 32 bytes, a whole sector: a warp's store touches 32 rows, and it is the rows that the store unit counts
-          if (pend_q >= 0) store_32bytes(dst + c / 8 + 2 * j, pkd);
+          if (pend_q >= 0 && p.out_wide) {
+            store_32bytes(dst + c / 8 + 2 * j, pkd);
+          } else if (pend_q >= 0) {
+            dst[c / 8 + 2 * j] = make_uint4(pkd[0], pkd[1], pkd[2], pkd[3]);
+            dst[c / 8 + 2 * j + 1] = make_uint4(pkd[4], pkd[5], pkd[6], pkd[7]);
+          }
         }
       }
       uint32_t todo = __ballot_sync(0xffffffffu, wrong && pend_q >= 0 && pend_limit > 0 && pend_l * 0.f == 0.f);

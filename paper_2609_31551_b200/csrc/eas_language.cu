@@ -189,6 +189,7 @@ static eas_status prompt_attention(const eas_prompt_inputs* in, void* workspace,
   pp.q = static_cast<const uint16_t*>(in->q); pp.k = static_cast<const uint16_t*>(in->k); pp.v = static_cast<const uint16_t*>(in->v);
   pp.out = static_cast<uint16_t*>(in->out);
   pp.ld_q = in->ld_q; pp.ld_k = in->ld_k; pp.ld_v = in->ld_v; pp.ld_out = in->ld_out;
+  pp.out_wide = (reinterpret_cast<uintptr_t>(in->out) & 31) == 0 && in->ld_out % 16 == 0;
   pp.scale_log2 = static_cast<float>(in->scale * kLog2e);
   pp.status = status_dev;
   const PromptPlan plan = prompt_plan(in);

@@ -131,12 +131,14 @@ def prompt_attention(q, k, v, cu_seqlens_host, cu_seqlens_k_host=None, scale=Non
     if cu_k.size != cu_q.size or cu_q[-1] > T or cu_k[-1] > Tk or Tk != v.shape[0]:
         raise B.EasError(1, "cu_seqlens are two lists of the same length that end within the rows of q, and of k and v")
     if out is None:
-        out = torch.empty((T, H, hd), dtype=dtype, device=q.device)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     ld_out = _rows(out, "out", H, hd, dtype, index)
     if out.shape[0] < cu_q[-1]:
         raise B.EasError(1, "out has fewer rows than cu_seqlens name")
     if status is None:
         status = torch.zeros(4, dtype=torch.int32, device=q.device)
+    elif status.dtype != torch.int32 or status.get_device() != index or status.numel() < 1:
+        raise B.EasError(1, "status must be an int32 tensor on the GPU of q")
     pin = PromptInputs(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), ld_q, ld_k, ld_v, ld_out, _DTYPES[dtype], H, G, hd,
                        hd ** -0.5 if scale is None else scale, cu_q.size - 1, at_q, at_k)
     l = lib()
@@ -144,7 +146,7 @@ def prompt_attention(q, k, v, cu_seqlens_host, cu_seqlens_k_host=None, scale=Non
         need = l.eas_prompt_attention_workspace_bytes(C.byref(pin))
         at, size = None, 0
         if need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            workspace = q.new_empty(need, dtype=torch.uint8)
     elif workspace.get_device() != index or not workspace.is_contiguous():
         raise B.EasError(1, "workspace must be a contiguous tensor on the GPU of q")
     if workspace is not None:
@@ -271,14 +273,14 @@ class KvCache:
         seqs = self._seqs(block_table, n)
         seqs.seq_lens = _ints(seq_lens, "seq_lens", n, index)
         if out is None:
-            out = torch.empty((n, H, hd), dtype=dtype, device=self.device)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
             ld_out = H * hd
         else:
             ld_out = _rows(out, "out", H, hd, dtype, index)
             if out.shape[0] < n:
                 raise B.EasError(1, "out has fewer rows than q")
         if workspace is None:
-            workspace = torch.empty(self.attention_workspace_bytes(n, H), dtype=torch.uint8, device=self.device)
+            workspace = q.new_empty(self.attention_workspace_bytes(n, H), dtype=torch.uint8)
         elif workspace.get_device() != index or not workspace.is_contiguous():
             raise B.EasError(1, "workspace must be a contiguous tensor on the cache's GPU")
         rc = self.lib.eas_cache_attention(self.handle, C.byref(seqs), q.data_ptr(), ld_q, out.data_ptr(), ld_out, H, _DTYPES[dtype],

@@ -106,6 +106,23 @@ def test_prompt_attention_reads_views_and_leaves_other_rows_alone(hd):
 
 
 @pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("offset,gap", [(8, 0), (0, 8), (8, 8), (24, 40), (16, 16)])
+@pytest.mark.parametrize("lens,keys", [([150, 3], None), ([40], [9000])])
+def test_prompt_attention_output_rows_on_any_16_byte_boundary(hd, offset, gap, lens, keys):
+    import paper_2609_31551_b200 as P
+    H, G = 10, 2
+    cu_q, cu_k = _cu(lens), _cu(keys or lens)
+    T = int(cu_q[-1])
+    q, k, v = _rand((T, H, hd), torch.float16, 70, 2.0), _rand((cu_k[-1], G, hd), torch.float16, 71), _rand((cu_k[-1], G, hd), torch.float16, 72)
+    want = P.prompt_attention(q.cuda(), k.cuda(), v.cuda(), cu_q, cu_k)[0]
+    flat = torch.full((offset + T * (H * hd + gap),), 5.0, dtype=torch.float16, device="cuda")
+    buf = flat[offset:].view(T, H * hd + gap)
+    out, status = P.prompt_attention(q.cuda(), k.cuda(), v.cuda(), cu_q, cu_k, out=buf[:, :H * hd].view(T, H, hd))
+    assert int(status[0]) == 0 and torch.equal(out, want)
+    assert (flat[:offset] == 5.0).all() and (buf[:, H * hd:] == 5.0).all()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("H,G", [(2, 2), (8, 1)])
 @pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
 @pytest.mark.parametrize("where", ["behind in the sequence", "first key of the next sequence"])
@@ -281,6 +298,10 @@ def test_prompt_attention_refusals():
     with pytest.raises(P.EasError) as e:
         P.prompt_attention(y, y, y, [0, 8])
     assert e.value.status == 2
+    for status in (torch.zeros(4, dtype=torch.int32), torch.zeros(4, device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda")):
+        with pytest.raises(P.EasError) as e:
+            P.prompt_attention(x, x, x, [0, 8], status=status)
+        assert e.value.status == 1
     out, _ = P.prompt_attention(x[:0], x[:0], x[:0], [0])               # no sequence, no row: nothing to do
     assert out.shape == (0, 2, 64)
 
