@@ -636,6 +636,64 @@ def test_prompts_then_tokens(hd, dtype, bs):
     assert torch.equal(cache.k.cpu(), nums[0]) and torch.equal(cache.v_scale.cpu(), scs[1])
 
 
+def test_offsets_past_32_bits():
+    """Blocks whose bytes lie past 2^32, and token rows past 2^31 elements: the same bits as the same data near the start."""
+    import paper_2609_31551_b200 as P
+    H, G, hd, bs, n = 8, 8, 128, 128, 400
+    far = 2 ** 32 // (G * bs * hd) + 1                                  # the first block behind 2^32 bytes
+    cu, zero = _dev([0, n]), _dev([0])
+    k, v, q = _rand((n, G, hd), torch.bfloat16, 400).cuda(), _rand((n, G, hd), torch.bfloat16, 401).cuda(), _rand((n, H, hd), torch.bfloat16, 402, 2.0).cuda()
+    near, big = P.KvCache(4, bs, G, hd), P.KvCache(far + 4, bs, G, hd)
+    wide = torch.empty(n * 2 ** 23, dtype=torch.bfloat16, device="cuda")     # rows 2^23 elements apart: row 256 begins at 2^31
+
+    def spread(x, at):
+        y = wide[at:].as_strided(x.shape, (2 ** 23, x.shape[2], 1))
+        y.copy_(x)
+        return y
+    kw, vw, qw = spread(k, 0), spread(v, 4096), spread(q, 8192)
+    ow = wide[16384:].as_strided(q.shape, (2 ** 23, hd, 1))
+    want, got = P.prompt_attention(q, k, v, [0, n]), P.prompt_attention(qw, kw, vw, [0, n], out=ow)
+    assert int(want[1][0]) == 0 and int(got[1][0]) == 0 and torch.equal(want[0], got[0])
+    table = _dev([[1, 3, 0, 2]])
+    near.store(k, v, cu, zero, table)
+    big.store(kw, vw, cu, zero, table + far)
+    want, got = near.load(cu, zero, table, n), big.load(cu, zero, table + far, n, out=(kw, vw))
+    assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1]) and float(want[0].abs().max()) > 1
+    lens, tables = _dev([n - i for i in range(n)]), table.expand(n, 4).contiguous()
+    a, b = near.attention(q, lens, tables), big.attention(qw, lens, tables + far, out=ow)
+    near.check(), big.check()
+    assert torch.equal(a, b) and float(a.abs().max()) > 0.01
+
+
+def test_calls_on_two_streams_at_once():
+    """Calls that share the cache and its status word but no workspace, on shares of the SMs and on all of them."""
+    import paper_2609_31551_b200 as P
+    H, G, hd, bs, lens = 16, 4, 128, 32, [3000, 50, 900]
+    rng = np.random.Generator(np.random.PCG64(41))
+    n_blocks = sum((n + bs - 1) // bs for n in lens)
+    table = _table(rng, lens, bs, n_blocks).cuda()
+    numbers, scales = _filled(n_blocks, G, bs, hd, 410)
+    c = _cache(numbers, scales)
+    q1, lens_d = _rand((3, H, hd), torch.bfloat16, 411).cuda(), _dev(lens)
+    cu_q, cu_k = [0, 60, 61], [0, 4000, 4100]
+    q = _rand((61, H, hd), torch.bfloat16, 412).cuda()
+    k, v = _rand((4100, G, hd), torch.bfloat16, 413).cuda(), _rand((4100, G, hd), torch.bfloat16, 414).cuda()
+    assert P.prompt_attention_workspace_bytes(H, G, hd, cu_q, cu_k) > 0
+    tok, (pro, status) = c.attention(q1, lens_d, table), P.prompt_attention(q, k, v, cu_q, cu_k)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    seen = []
+    for i in range(40):
+        st, budget = streams[i % 2], (0, 60)[i // 20]
+        seen.append((tok, c.attention(q1, lens_d, table, stream=st, sm_budget=budget)))
+        out, s = P.prompt_attention(q, k, v, cu_q, cu_k, stream=streams[1 - i % 2], sm_budget=budget)
+        seen.append((pro, out))
+        seen.append((status, s))
+    torch.cuda.synchronize()
+    c.check()
+    assert int(status[0]) == 0 and all(torch.equal(a, b) for a, b in seen)
+
+
 # ------------------------------------------------------------------------------------------------ the commands that call them
 @pytest.mark.parametrize("neighbour", ["prompt", "token"])
 def test_coresidency_with_a_language_model_neighbour(neighbour):
