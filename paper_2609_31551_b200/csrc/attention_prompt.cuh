@@ -49,7 +49,7 @@ struct Divider {
 #endif
 };
 
-struct PromptParams {
+struct PromptCommon {
   CUtensorMap map_q;      // [tokens, heads, HD], box {64, group, 128 / group}, 128-byte swizzle
   CUtensorMap map_k, map_v;   // [HD / 64 halves x heads, tokens, 64], box {64, 80, HD / 64}
   const uint16_t *q, *k, *v;
@@ -59,20 +59,28 @@ struct PromptParams {
   int group, n_kv, tile_tokens;
   float scale_log2;       // scale * log2(e)
   int n_seqs, total_units;
-  int q0[kPromptMaxSeqs], k0[kPromptMaxSeqs], len_q[kPromptMaxSeqs], len_k[kPromptMaxSeqs];
-  int tiles[kPromptMaxSeqs], per_head[kPromptMaxSeqs];     // of a sequence and key/value head: row tiles, units
-  int unit_prefix[kPromptMaxSeqs + 1];
   Divider by_kv, by_split;
   // Few rounds of units of different cost: the deal follows this list, costliest first (sequence << 24 | unit of the sequence), instead of
   // the sequences one after the other (8 prompts of 1 to 1563 tokens, 580 units: 14 to 39 key steps an SM without it)
   int listed;
-  uint32_t list[kPromptListed];
   int n_split;            // parts of a unit's key steps (SPLIT)
   float4* o_ws;           // [unit][part][tile][HD / 4][128 rows]: O, not divided by the sum
   float2* ml_ws;          // [unit][part][tile][128 rows]: reference and sum (-inf, 0: no key)
   uint32_t* status;
   int early_launch;
 };
+// The kernels' parameters: with room for a few sequences dealt one after the other, or for many and a list of their units.  (12 KB of parameters
+// instead of 1 cost the host 1.3 us a launch.)
+template <int SEQS, int LISTED>
+struct PromptParamsOf : PromptCommon {
+  int q0[SEQS], k0[SEQS], len_q[SEQS], len_k[SEQS];
+  int tiles[SEQS], per_head[SEQS];     // of a sequence and key/value head: row tiles, units
+  int unit_prefix[SEQS + 1];
+  uint32_t list[LISTED];
+};
+constexpr int kPromptFewSeqs = 8;
+using PromptParams = PromptParamsOf<kPromptMaxSeqs, kPromptListed>;
+using PromptParamsFew = PromptParamsOf<kPromptFewSeqs, 1>;
 
 template <int HD>
 struct PromptCfg {
@@ -110,16 +118,16 @@ struct PromptUnit {
   int q0, k0, len_q, len_k, ahead, head, tile0, n_q, n_max;   // ahead: keys in front of the first query
 };
 template <int HD>
-__device__ __forceinline__ int prompt_steps(const PromptParams& p, const PromptUnit& u, int w) {      // key steps of the unit's tile w
+__device__ __forceinline__ int prompt_steps(const PromptCommon& p, const PromptUnit& u, int w) {      // key steps of the unit's tile w
   const int seen = min((u.tile0 + w + 1) * p.tile_tokens, u.len_q) + u.ahead;
   return (max(min(seen, u.len_k), 0) + PromptCfg<HD>::kKeys - 1) / PromptCfg<HD>::kKeys;
 }
 // units of a sequence from its last tiles (the costliest) to its first, the heads side by side
-template <int HD>
-__device__ __forceinline__ PromptUnit prompt_decode(const PromptParams& p, int unit, int& cursor) {
+template <int HD, typename Params>
+__device__ __forceinline__ PromptUnit prompt_decode(const Params& p, int unit, int& cursor) {
   constexpr int NWG = PromptCfg<HD>::kWg;
   int lo = cursor, k;
-  if (p.listed) {
+  if (sizeof(p.list) > 4 && p.listed) {
     const uint32_t e = p.list[unit];
     lo = static_cast<int>(e >> 24);
     k = static_cast<int>(e & 0xFFFFFFu);
@@ -160,7 +168,7 @@ __device__ __forceinline__ void store_32bytes(void* dst, const uint32_t (&v)[8])
 // Columns col0 .. col0 + cols - 1 of one output row again, by a whole warp (lane i: HD / 32 dims): sums over the keys that the row sees.  Only
 // elements that are not finite although every value that the row sees is are replaced.
 template <int HD, bool FP16>
-__device__ __noinline__ void prompt_repair(const PromptParams& p, int q_row, int q_head, int kv_head, int k0, int limit, float m, float l, int col0, int cols) {
+__device__ __noinline__ void prompt_repair(const PromptCommon& p, int q_row, int q_head, int kv_head, int k0, int limit, float m, float l, int col0, int cols) {
   constexpr int N = HD / 32;
   const int lane = threadIdx.x & 31;
   uint16_t* dst = p.out + q_row * p.ld_out + q_head * HD + lane * N;
@@ -200,8 +208,8 @@ __device__ __noinline__ void prompt_repair(const PromptParams& p, int q_row, int
 struct PromptPart {
   int unit, lo, hi;
 };
-template <int HD, bool SPLIT>
-__device__ __forceinline__ PromptUnit prompt_item(const PromptParams& p, int item, int& cursor, PromptPart& part) {
+template <int HD, bool SPLIT, typename Params>
+__device__ __forceinline__ PromptUnit prompt_item(const Params& p, int item, int& cursor, PromptPart& part) {
   const int unit = SPLIT ? p.by_split(item) : item;
   const PromptUnit u = prompt_decode<HD>(p, unit, cursor);
   const int i = SPLIT ? item - unit * p.n_split : 0;
@@ -211,8 +219,8 @@ __device__ __forceinline__ PromptUnit prompt_item(const PromptParams& p, int ite
   return u;
 }
 
-template <int HD, bool FP16, bool SPLIT>
-__global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_kernel(const __grid_constant__ PromptParams p) {
+template <int HD, bool FP16, bool SPLIT, typename Params>
+__global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_kernel(const __grid_constant__ Params p) {
   using L = PromptCfg<HD>;
   constexpr int NST = L::kStages, NWG = L::kWg, KEYS = L::kKeys;
   constexpr bool OWN_P = L::kOwnP;
@@ -659,8 +667,8 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
 }
 
 // The parts of a split call put together: 128 threads, one a row, per (unit, tile, quarter of the columns).
-template <int HD, bool FP16>
-__global__ void __launch_bounds__(512, 1) prompt_join_kernel(const __grid_constant__ PromptParams p) {
+template <int HD, bool FP16, typename Params>
+__global__ void __launch_bounds__(512, 1) prompt_join_kernel(const __grid_constant__ Params p) {
   constexpr int NWG = PromptCfg<HD>::kWg, COLS = HD / 4;
   if (p.early_launch) pdl_launch_dependents();
   pdl_wait();

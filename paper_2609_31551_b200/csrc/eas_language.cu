@@ -32,19 +32,36 @@ static eas_status prompt_kv_map(CUtensorMap* m, const void* k, int heads, int hd
   return make_tmap(m, k, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-template <int HD, bool FP16, bool SPLIT>
-static eas_status launch_prompt(PromptParams& pp, int budget, bool all, cudaStream_t stream) {
+template <int HD, bool FP16, bool SPLIT, typename Params>
+static eas_status launch_prompt(const Params& pp, int budget, bool all, cudaStream_t stream) {
   using L = PromptCfg<HD>;
   static OncePerDevice once;
   if (once.first()) {
-    CUDA_TRY(cudaFuncSetAttribute(prompt_attention_kernel<HD, FP16, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes));
-    if (SPLIT) CUDA_TRY(cudaFuncSetAttribute(prompt_join_kernel<HD, FP16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kOnePerSmSmem));
+    CUDA_TRY(cudaFuncSetAttribute(prompt_attention_kernel<HD, FP16, SPLIT, Params>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes));
+    if (SPLIT) CUDA_TRY(cudaFuncSetAttribute(prompt_join_kernel<HD, FP16, Params>, cudaFuncAttributeMaxDynamicSharedMemorySize, kOnePerSmSmem));
     once.settled();
   }
-  EAS_TRY(launch_kernel(prompt_attention_kernel<HD, FP16, SPLIT>, std::min(budget, pp.total_units), L::kThreads, L::kBytes, stream, pp));
+  EAS_TRY(launch_kernel(prompt_attention_kernel<HD, FP16, SPLIT, Params>, std::min(budget, pp.total_units), L::kThreads, L::kBytes, stream, pp));
   if (!SPLIT) return EAS_OK;
   const int tiles = pp.total_units / pp.n_split * L::kWg;         // 4 threads' groups a CTA, one each for a quarter of a tile's columns
-  return launch_kernel(prompt_join_kernel<HD, FP16>, std::min(budget, tiles), 512, all ? 0 : kOnePerSmSmem, stream, pp);
+  return launch_kernel(prompt_join_kernel<HD, FP16, Params>, std::min(budget, tiles), 512, all ? 0 : kOnePerSmSmem, stream, pp);
+}
+template <typename Params>
+static eas_status launch_prompt(const Params& pp, int hd, bool fp16, int budget, bool all, cudaStream_t st) {
+  if (pp.n_split == 1) {
+    if (hd == 64) return fp16 ? launch_prompt<64, true, false>(pp, budget, all, st) : launch_prompt<64, false, false>(pp, budget, all, st);
+    return fp16 ? launch_prompt<128, true, false>(pp, budget, all, st) : launch_prompt<128, false, false>(pp, budget, all, st);
+  }
+  if (hd == 64) return fp16 ? launch_prompt<64, true, true>(pp, budget, all, st) : launch_prompt<64, false, true>(pp, budget, all, st);
+  return fp16 ? launch_prompt<128, true, true>(pp, budget, all, st) : launch_prompt<128, false, true>(pp, budget, all, st);
+}
+static PromptParamsFew few_of(const PromptParams& pp) {
+  PromptParamsFew f;
+  static_cast<PromptCommon&>(f) = pp;
+  const int n = pp.n_seqs;
+  std::copy_n(pp.q0, n, f.q0); std::copy_n(pp.k0, n, f.k0); std::copy_n(pp.len_q, n, f.len_q); std::copy_n(pp.len_k, n, f.len_k);
+  std::copy_n(pp.tiles, n, f.tiles); std::copy_n(pp.per_head, n, f.per_head); std::copy_n(pp.unit_prefix, n + 1, f.unit_prefix);
+  return f;
 }
 
 // How the work of up to kPromptMaxSeqs sequences is laid out: the units in the order in which they are dealt, and into how many parts their
@@ -221,15 +238,11 @@ static eas_status prompt_attention(const eas_prompt_inputs* in, void* workspace,
     pp.by_kv = divider(G); pp.by_split = divider(pp.n_split);
     pp.listed = 0;
     if (units <= kPromptListed && units > budget && pp.n_seqs > 1) prompt_list(pp, plan.wg);
-    if (pp.n_split == 1) {
-      EAS_TRY(hd == 64 ? (h ? launch_prompt<64, true, false>(pp, budget, all, st) : launch_prompt<64, false, false>(pp, budget, all, st))
-                       : (h ? launch_prompt<128, true, false>(pp, budget, all, st) : launch_prompt<128, false, false>(pp, budget, all, st)));
-    } else {
+    if (pp.n_split > 1) {
       pp.o_ws = static_cast<float4*>(workspace);
       pp.ml_ws = reinterpret_cast<float2*>(pp.o_ws + static_cast<size_t>(pp.total_units) * plan.wg * 128 * (hd / 4));
-      EAS_TRY(hd == 64 ? (h ? launch_prompt<64, true, true>(pp, budget, all, st) : launch_prompt<64, false, true>(pp, budget, all, st))
-                       : (h ? launch_prompt<128, true, true>(pp, budget, all, st) : launch_prompt<128, false, true>(pp, budget, all, st)));
     }
+    EAS_TRY(pp.listed || pp.n_seqs > kPromptFewSeqs ? launch_prompt(pp, hd, h, budget, all, st) : launch_prompt(few_of(pp), hd, h, budget, all, st));
   }
   return EAS_OK;
 }
