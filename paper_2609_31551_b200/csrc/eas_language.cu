@@ -391,8 +391,9 @@ static eas_status launch_attention(CacheAttnParams& p, int budget, bool all, cud
     once.settled();
   }
   EAS_TRY(launch_kernel(cache_attention_kernel<HD, NT>, std::min(budget, p.n_ctas), L::kThreads, L::kBytes, stream, p));
+  constexpr int kJoinWarps = kCacheJoinThreads / 32;
   const int64_t heads = static_cast<int64_t>(p.n_seqs) * p.c.n_kv * p.group;
-  return launch_kernel(cache_join_kernel<HD, NT>, static_cast<int>(std::min<int64_t>(budget, (heads + 7) / 8)), 256, all ? 0 : kOnePerSmSmem, stream, p);
+  return launch_kernel(cache_join_kernel<HD, NT>, static_cast<int>(std::min<int64_t>(budget, (heads + kJoinWarps - 1) / kJoinWarps)), kCacheJoinThreads, all ? 0 : kOnePerSmSmem, stream, p);
 }
 
 static eas_status cache_attention(const eas_cache* c, const eas_cache_seqs* s, const void* q, int64_t ld_q, void* out, int64_t ld_out, int32_t n_heads,
