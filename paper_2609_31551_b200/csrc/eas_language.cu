@@ -43,8 +43,8 @@ static eas_status launch_prompt(const Params& pp, int budget, bool all, cudaStre
   }
   EAS_TRY(launch_kernel(prompt_attention_kernel<HD, FP16, SPLIT, Params>, std::min(budget, pp.total_units), L::kThreads, L::kBytes, stream, pp));
   if (!SPLIT) return EAS_OK;
-  const int tiles = pp.total_units / pp.n_split * L::kWg;         // 4 threads' groups a CTA, one each for a quarter of a tile's columns
-  return launch_kernel(prompt_join_kernel<HD, FP16, Params>, std::min(budget, tiles), 512, all ? 0 : kOnePerSmSmem, stream, pp);
+  const int64_t items = static_cast<int64_t>(pp.total_units / pp.n_split) * L::kWg * (HD / 8);      // 4 a CTA
+  return launch_kernel(prompt_join_kernel<HD, FP16, Params>, static_cast<int>(std::min<int64_t>(budget, (items + 3) / 4)), 512, all ? 0 : kOnePerSmSmem, stream, pp);
 }
 template <typename Params>
 static eas_status launch_prompt(const Params& pp, int hd, bool fp16, int budget, bool all, cudaStream_t st) {
