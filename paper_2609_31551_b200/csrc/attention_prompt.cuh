@@ -20,10 +20,11 @@
 // its O row in TMEM.  Scores, sums and O are fp32; P is rounded to the data type (bf16 or fp16: what the matrix product takes), and the
 // output once at the end.  A row's arithmetic depends on its own sequence alone, not on the unit, the packing or the SMs.
 //
-// Few rows against many keys (a chunk of a prompt behind a long prefix) make fewer units than there are SMs.  SPLIT cuts every unit's key
-// steps into n_split equal parts, work items of their own that leave (m, l, O) in the workspace, fp32, and prompt_join_kernel puts them
-// together in order.  The host chooses n_split from the call's shapes and the device, not from sm_budget.  512 queries of 40 heads
-// (8 key/value heads of 128) behind 11801 keys: 88 units of 154 steps, 210 us in one piece, 131 in 5 parts.
+// Few rows against many keys (a chunk of a prompt behind a long prefix) make fewer units than there are SMs.  SPLIT lays the key steps of all
+// units end to end and cuts the line into one equal piece per SM: a piece is a few work items (the end of a unit, whole units, the beginning of
+// one), each of which leaves (m, l, O) in the workspace, fp32, and prompt_join_kernel puts a unit's items together in order.  The cut
+// follows from the call's shapes and the device, not from sm_budget.  512 queries of 40 heads (8 key/value heads of 128) behind 11801 keys, 88 units
+// of 154 steps: 167 us whole, 114 as 235 items (in 5 equal parts each, 440 items, 124 to 157: what they leave then fills L2).
 //
 // Masked keys: their scores are replaced by -inf (P exactly 0), whatever K held.  0 x Inf is not 0, so value rows behind the
 // sequence's end are cleared in shared memory, and a row whose O is not finite although its sum is (a value row that later rows of the tile
@@ -37,6 +38,9 @@ namespace eas {
 
 constexpr int kPromptMaxSeqs = 128;      // sequences of one launch (kernel parameters)
 constexpr int kPromptListed = 2048;      // units that the list of a launch holds
+
+constexpr int kPromptPieces = 192;       // SPLIT: pieces of the line of steps, at most,
+constexpr int kPromptSplitUnits = 768;   // and units
 
 // k / d for 0 <= k < 2^24 and d <= 256 by one multiplication (by ceil(2^32 / d): off by less than k / 2^32 < 1 / d), else by division
 struct Divider {
@@ -59,28 +63,39 @@ struct PromptCommon {
   int group, n_kv, tile_tokens;
   float scale_log2;       // scale * log2(e)
   int n_seqs, total_units;
-  Divider by_kv, by_split;
-  // Few rounds of units of different cost: the deal follows this list, costliest first (sequence << 24 | unit of the sequence), instead of
-  // the sequences one after the other (8 prompts of 1 to 1563 tokens, 580 units: 14 to 39 key steps an SM without it)
-  int listed;
-  int n_split;            // parts of a unit's key steps (SPLIT)
-  float4* o_ws;           // [unit][part][tile][HD / 4][128 rows]: O, not divided by the sum
-  float2* ml_ws;          // [unit][part][tile][128 rows]: reference and sum (-inf, 0: no key)
+  Divider by_kv;
+  float4* o_ws;           // SPLIT: [item][tile][HD / 4][128 rows]: O, not divided by the sum
+  float2* ml_ws;          // [item][tile][128 rows]: reference and sum (-inf, 0: no key)
   uint32_t* status;
   int early_launch;
 };
-// The kernels' parameters: with room for a few sequences dealt one after the other, or for many and a list of their units.  (12 KB of parameters
-// instead of 1 cost the host 1.3 us a launch.)
-template <int SEQS, int LISTED>
-struct PromptParamsOf : PromptCommon {
+// The kernels' parameters, in three sizes (12 KB of them instead of 1 cost the host 1.3 us a launch).
+template <int SEQS>
+struct PromptSeqs : PromptCommon {
   int q0[SEQS], k0[SEQS], len_q[SEQS], len_k[SEQS];
   int tiles[SEQS], per_head[SEQS];     // of a sequence and key/value head: row tiles, units
   int unit_prefix[SEQS + 1];
-  uint32_t list[LISTED];
 };
-constexpr int kPromptFewSeqs = 8;
-using PromptParams = PromptParamsOf<kPromptMaxSeqs, kPromptListed>;
-using PromptParamsFew = PromptParamsOf<kPromptFewSeqs, 1>;
+struct PromptParamsFew : PromptSeqs<8> {                          // a few sequences, dealt one after the other
+  static constexpr int kSeqs = 8;
+  static constexpr bool kListed = false, kSplit = false;
+};
+struct PromptParams : PromptSeqs<kPromptMaxSeqs> {
+  static constexpr int kSeqs = kPromptMaxSeqs;
+  static constexpr bool kListed = true, kSplit = false;
+  // Few rounds of units of different cost: the deal follows this list, costliest first (sequence << 24 | unit of the sequence), instead of
+  // the sequences one after the other (8 prompts of 1 to 1563 tokens, 580 units: 14 to 39 key steps an SM without it)
+  int listed;
+  uint32_t list[kPromptListed];
+};
+struct PromptParamsSplit : PromptSeqs<kPromptMaxSeqs> {           // total_units: items
+  static constexpr int kSeqs = kPromptMaxSeqs;
+  static constexpr bool kListed = false, kSplit = true;
+  int n_pieces, n_units;
+  uint16_t piece_item[kPromptPieces + 1], unit_item[kPromptSplitUnits + 1];     // first items
+  uint16_t item_unit[kPromptSplitUnits + kPromptPieces];
+  int item_lo[kPromptSplitUnits + kPromptPieces];                 // first key step; the last one is in front of the unit's next item's first
+};
 
 template <int HD>
 struct PromptCfg {
@@ -127,11 +142,16 @@ template <int HD, typename Params>
 __device__ __forceinline__ PromptUnit prompt_decode(const Params& p, int unit, int& cursor) {
   constexpr int NWG = PromptCfg<HD>::kWg;
   int lo = cursor, k;
-  if (sizeof(p.list) > 4 && p.listed) {
-    const uint32_t e = p.list[unit];
-    lo = static_cast<int>(e >> 24);
-    k = static_cast<int>(e & 0xFFFFFFu);
-  } else {
+  bool listed = false;
+  if constexpr (Params::kListed) {
+    if (p.listed) {
+      const uint32_t e = p.list[unit];
+      lo = static_cast<int>(e >> 24);
+      k = static_cast<int>(e & 0xFFFFFFu);
+      listed = true;
+    }
+  }
+  if (!listed) {
     while (lo + 1 < p.n_seqs && p.unit_prefix[lo + 1] <= unit) ++lo;
     k = unit - p.unit_prefix[lo];
     cursor = lo;
@@ -212,26 +232,59 @@ __device__ __noinline__ void prompt_repair(const PromptCommon& p, int q_row, int
     if (bad & (1u << i)) dst[i] = static_cast<uint16_t>(pack_16x2<FP16>(acc[i] / l, 0.f));
 }
 
-// key steps [lo, hi) of a part: of the unit, or (hi capped) of one of its tiles
+// key steps [lo, hi) of an item: of the unit, or (hi capped) of one of its tiles
 struct PromptPart {
-  int unit, lo, hi;
+  int lo, hi;
 };
-template <int HD, bool SPLIT, typename Params>
+template <int HD, typename Params>
 __device__ __forceinline__ PromptUnit prompt_item(const Params& p, int item, int& cursor, PromptPart& part) {
-  const int unit = SPLIT ? p.by_split(item) : item;
-  const PromptUnit u = prompt_decode<HD>(p, unit, cursor);
-  const int i = SPLIT ? item - unit * p.n_split : 0;
-  part.unit = unit;
-  part.lo = SPLIT ? p.by_split(u.n_max * i) : 0;
-  part.hi = SPLIT ? p.by_split(u.n_max * (i + 1)) : u.n_max;
-  return u;
+  if constexpr (Params::kSplit) {
+    const int unit = p.item_unit[item];
+    const PromptUnit u = prompt_decode<HD>(p, unit, cursor);
+    part.lo = p.item_lo[item];
+    part.hi = item + 1 < p.unit_item[unit + 1] ? p.item_lo[item + 1] : u.n_max;
+    return u;
+  } else {
+    const PromptUnit u = prompt_decode<HD>(p, item, cursor);
+    part.lo = 0;
+    part.hi = u.n_max;
+    return u;
+  }
 }
+// The items of a CTA in order
+template <typename Params>
+struct PromptDeal {
+  const Params& p;
+  int item, end, piece;
+  uint32_t round;
+  __device__ __forceinline__ explicit PromptDeal(const Params& params) : p(params), item(0), end(0), piece(blockIdx.x), round(0) {
+    if constexpr (Params::kSplit) enter();
+    else item = attn_unit_at(0);
+  }
+  __device__ __forceinline__ void enter() {
+    if constexpr (Params::kSplit) {
+      item = piece < p.n_pieces ? p.piece_item[piece] : p.total_units;
+      end = piece < p.n_pieces ? p.piece_item[piece + 1] : 0;
+    }
+  }
+  __device__ __forceinline__ bool more() const { return item < p.total_units; }
+  __device__ __forceinline__ void next() {
+    if constexpr (Params::kSplit) {
+      if (++item == end) {
+        piece += gridDim.x;
+        enter();
+      }
+    } else {
+      item = attn_unit_at(++round);
+    }
+  }
+};
 
-template <int HD, bool FP16, bool SPLIT, typename Params>
+template <int HD, bool FP16, typename Params>
 __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_kernel(const __grid_constant__ Params p) {
   using L = PromptCfg<HD>;
   constexpr int NST = L::kStages, NWG = L::kWg, KEYS = L::kKeys;
-  constexpr bool OWN_P = L::kOwnP;
+  constexpr bool OWN_P = L::kOwnP, SPLIT = Params::kSplit;
   extern __shared__ uint8_t smem_raw_prompt[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw_prompt) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBarOff);
@@ -277,12 +330,12 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
     // ------------------------------------------------------------------ K / V producer
     setmaxnreg_dec<L::kRegsLight>();
     if (lane == 0) {
-      uint32_t g = 0, round = 0;
+      uint32_t g = 0;
       bool ok = true;
       int cursor = 0;
-      for (int item = attn_unit_at(0); item < p.total_units && ok; item = attn_unit_at(++round)) {
+      for (PromptDeal<Params> deal(p); deal.more() && ok; deal.next()) {
         PromptPart part;
-        const PromptUnit u = prompt_item<HD, SPLIT>(p, item, cursor, part);
+        const PromptUnit u = prompt_item<HD>(p, deal.item, cursor, part);
         for (int j = part.lo; j < part.hi; ++j, ++g) {
           const uint32_t s = g % NST;
           if (!mbar_wait(&kv_empty[s], ((g / NST) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
@@ -313,20 +366,21 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
     uint32_t n_q = 0, n_s = 0, n_p = 0;          // Q tiles waited for, s_full phases committed, p_ready phases waited for
     bool started = false;                        // the first scores of this unit's tile are issued already
     bool owed = false;                           // the warpgroup still has to say that it has seen a bare commit
-    uint32_t base = 0, round = 0;                // base: ring position of the unit's first K/V tile
+    uint32_t base = 0;                           // ring position of the unit's first K/V tile
     bool ok = true;
     int cursor = 0;
     PromptUnit un{};
     PromptPart un_part{};
     int un_steps = 0;                            // key steps of this issuer's tile in the next item (0: none)
-    auto look = [&](int item) {
+    PromptDeal<Params> deal(p);                  // at the next item
+    auto look = [&]() {
       un_steps = 0;
-      if (item < p.total_units) {
-        un = prompt_item<HD, SPLIT>(p, item, cursor, un_part);
+      if (deal.more()) {
+        un = prompt_item<HD>(p, deal.item, cursor, un_part);
         if (w < un.n_q) un_steps = max(min(un_part.hi, prompt_steps<HD>(p, un, w)) - un_part.lo, 0);
       }
     };
-    look(attn_unit_at(0));
+    look();
 
     auto load_q = [&](const PromptUnit& u) {
       if (elect_one()) {
@@ -376,11 +430,12 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
       umma_commit(&s_full[w]);
     };
 
-    for (int item = attn_unit_at(0); item < p.total_units && ok; item = attn_unit_at(++round)) {
+    while (deal.more() && ok) {
       const PromptUnit u = un;
       const PromptPart part = un_part;
       const int n_steps = un_steps;
-      look(attn_unit_at(round + 1));
+      deal.next();
+      look();
       const uint32_t next_base = base + static_cast<uint32_t>(part.hi - part.lo);
       if (n_steps == 0) {
         ok = hand_back(base, next_base);
@@ -471,17 +526,19 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
       tmem_ld_wait_16<0>(o); tmem_ld_tie_16<16>(o); tmem_ld_tie_16<32>(o); tmem_ld_tie_16<48>(o);
     };
     auto flush_output = [&]() {
-      if constexpr (SPLIT) {
+      if constexpr (SPLIT) {                       // (rows that are not stored leave nothing)
         float4* dst = p.o_ws + static_cast<long long>(pend_slot) * (HD / 4) * 128 + row;
 #pragma unroll 1
         for (int c = 0; c < HD; c += 64) {
           uint32_t o[64];
           load_64(o_addr + c, o);
+          if (pend_q >= 0) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            dst[(c / 4 + i) * 128] = make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]), __uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3]));
+            for (int i = 0; i < 16; ++i)
+              dst[(c / 4 + i) * 128] = make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]), __uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3]));
+          }
         }
-        p.ml_ws[static_cast<long long>(pend_slot) * 128 + row] = make_float2(pend_l == 0.f ? -INFINITY : pend_m, pend_l);
+        if (pend_q >= 0) p.ml_ws[static_cast<long long>(pend_slot) * 128 + row] = make_float2(pend_l == 0.f ? -INFINITY : pend_m, pend_l);
         __syncwarp();
         pend = false;
         return;
@@ -525,10 +582,9 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
     };
 
     int cursor = 0;
-    uint32_t round = 0;
-    for (int item = attn_unit_at(0); item < p.total_units && ok; item = attn_unit_at(++round)) {
+    for (PromptDeal<Params> deal(p); deal.more() && ok; deal.next()) {
       PromptPart part;
-      const PromptUnit u = prompt_item<HD, SPLIT>(p, item, cursor, part);
+      const PromptUnit u = prompt_item<HD>(p, deal.item, cursor, part);
       const int n_steps = w < u.n_q ? max(min(part.hi, prompt_steps<HD>(p, u, w)) - part.lo, 0) : 0;
       const int tok = (u.tile0 + w) * p.tile_tokens + row_tok;
       const bool stored = w < u.n_q && row_tok < p.tile_tokens && tok < u.len_q;
@@ -544,7 +600,7 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
             mbar_arrive_if(&p_ready[w], lane == 0);        // the issuer may use s_full[w] again
           }
         }
-        if (SPLIT && w < u.n_q) p.ml_ws[(static_cast<long long>(item) * NWG + w) * 128 + row] = make_float2(-INFINITY, 0.f);
+        if (SPLIT && stored) p.ml_ws[(static_cast<long long>(deal.item) * NWG + w) * 128 + row] = make_float2(-INFINITY, 0.f);
         if (!SPLIT && stored) {
           uint4* dst = reinterpret_cast<uint4*>(p.out + (static_cast<long long>(u.q0) + tok) * p.ld_out + (u.head * p.group + row_head) * HD);
           for (int c = 0; c < HD / 8; ++c) dst[c] = make_uint4(0u, 0u, 0u, 0u);
@@ -655,7 +711,7 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
       pend_head = u.head;
       pend_k0 = u.k0;
       pend_limit = stored ? limit : 0;
-      if (SPLIT) pend_slot = item * NWG + w;
+      if (SPLIT) pend_slot = deal.item * NWG + w;
     }
     if (ok && pend) {
       if (warp_mbar_wait(OWN_P ? &pv_done[w] : &s_full[w], (OWN_P ? n - 1u : n) & 1u, abort_flag)) {
@@ -674,18 +730,16 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
   if (threadIdx.x == 0 && *abort_flag) atomicCAS(p.status, DEV_OK, DEV_ERR_WAIT_TIMEOUT);
 }
 
-// The parts of a split call put together, in order: 128 threads, one a row, per (unit, tile, 8 columns); a thread has the loads of 8 parts in flight,
-// 80 KB an SM with 5 parts.  (A quarter of the columns each and one part after the other: 134 us instead of 131 for the chunk above, 35 instead of 28 for 128
-// tokens of 32 heads behind 8000.)
-template <int HD, bool FP16, typename Params>
-__global__ void __launch_bounds__(512, 1) prompt_join_kernel(const __grid_constant__ Params p) {
+// The items of a unit put together, in order: 128 threads, one a row, per (unit, tile, 8 columns); a thread has the loads of 8 items in flight.
+// (A quarter of the columns each and one item after the other: 128 tokens of 32 heads behind 8000 in 12 parts 35 us instead of 28.)
+template <int HD, bool FP16>
+__global__ void __launch_bounds__(512, 1) prompt_join_kernel(const __grid_constant__ PromptParamsSplit p) {
   constexpr int NWG = PromptCfg<HD>::kWg, COLS = 8, CHUNKS = HD / COLS, BATCH = 8;
   if (p.early_launch) pdl_launch_dependents();
   pdl_wait();
   const int row = threadIdx.x & 127, row_tok = row / p.group, row_head = row - row_tok * p.group;
-  const int units = p.total_units / p.n_split;
   int cursor = 0;
-  for (int it = blockIdx.x * 4 + (threadIdx.x >> 7); it < units * NWG * CHUNKS; it += gridDim.x * 4) {
+  for (int it = blockIdx.x * 4 + (threadIdx.x >> 7); it < p.n_units * NWG * CHUNKS; it += gridDim.x * 4) {
     const int unit = it / (NWG * CHUNKS), w = it / CHUNKS % NWG, col0 = it % CHUNKS * COLS;
     const PromptUnit u = prompt_decode<HD>(p, unit, cursor);
     if (w >= u.n_q) continue;
@@ -694,17 +748,18 @@ __global__ void __launch_bounds__(512, 1) prompt_join_kernel(const __grid_consta
     float m = -INFINITY, l = 0.f, acc[COLS];
 #pragma unroll
     for (int i = 0; i < COLS; ++i) acc[i] = 0.f;
-    for (int base = 0; base < p.n_split; base += BATCH) {
+    const int first = p.unit_item[unit], items = stored ? p.unit_item[unit + 1] - first : 0;      // (0 too where no row sees a key)
+    for (int base = 0; base < items; base += BATCH) {
       float ml[BATCH][2], x[BATCH][COLS];
 #pragma unroll
       for (int e = 0; e < BATCH; ++e) {
         ml[e][0] = -INFINITY;
         ml[e][1] = 0.f;
-        if (base + e < p.n_split) {
-          const long long slot = (static_cast<long long>(unit) * p.n_split + base + e) * NWG + w;
+        if (base + e < items) {
+          const long long slot = static_cast<long long>(first + base + e) * NWG + w;
           const float4* o = p.o_ws + (slot * (HD / 4) + col0 / 4) * 128 + row;
           load_ordered(p.ml_ws + slot * 128 + row, ml[e][0], ml[e][1]);
-          load_ordered(o, x[e][0], x[e][1], x[e][2], x[e][3]);         // (not written where the part has no key for any row of the tile: not used then)
+          load_ordered(o, x[e][0], x[e][1], x[e][2], x[e][3]);         // (not written where the item has no key for any row of the tile: not used then)
           load_ordered(o + 128, x[e][4], x[e][5], x[e][6], x[e][7]);
         }
       }

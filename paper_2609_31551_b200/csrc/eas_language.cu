@@ -32,29 +32,30 @@ static eas_status prompt_kv_map(CUtensorMap* m, const void* k, int heads, int hd
   return make_tmap(m, k, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-template <int HD, bool FP16, bool SPLIT, typename Params>
+template <int HD, bool FP16, typename Params>
 static eas_status launch_prompt(const Params& pp, int budget, bool all, cudaStream_t stream) {
   using L = PromptCfg<HD>;
   static OncePerDevice once;
   if (once.first()) {
-    CUDA_TRY(cudaFuncSetAttribute(prompt_attention_kernel<HD, FP16, SPLIT, Params>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes));
-    if (SPLIT) CUDA_TRY(cudaFuncSetAttribute(prompt_join_kernel<HD, FP16, Params>, cudaFuncAttributeMaxDynamicSharedMemorySize, kOnePerSmSmem));
+    CUDA_TRY(cudaFuncSetAttribute(prompt_attention_kernel<HD, FP16, Params>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes));
+    if constexpr (Params::kSplit) CUDA_TRY(cudaFuncSetAttribute(prompt_join_kernel<HD, FP16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kOnePerSmSmem));
     once.settled();
   }
-  EAS_TRY(launch_kernel(prompt_attention_kernel<HD, FP16, SPLIT, Params>, std::min(budget, pp.total_units), L::kThreads, L::kBytes, stream, pp));
-  if (!SPLIT) return EAS_OK;
-  const int64_t items = static_cast<int64_t>(pp.total_units / pp.n_split) * L::kWg * (HD / 8);      // 4 a CTA
-  return launch_kernel(prompt_join_kernel<HD, FP16, Params>, static_cast<int>(std::min<int64_t>(budget, (items + 3) / 4)), 512, all ? 0 : kOnePerSmSmem, stream, pp);
+  int grid = pp.total_units;
+  if constexpr (Params::kSplit) grid = pp.n_pieces;
+  EAS_TRY(launch_kernel(prompt_attention_kernel<HD, FP16, Params>, std::min(budget, grid), L::kThreads, L::kBytes, stream, pp));
+  if constexpr (Params::kSplit) {
+    const int64_t items = static_cast<int64_t>(pp.n_units) * L::kWg * (HD / 8);      // 4 a CTA
+    return launch_kernel(prompt_join_kernel<HD, FP16>, static_cast<int>(std::min<int64_t>(budget, (items + 3) / 4)), 512, all ? 0 : kOnePerSmSmem, stream, pp);
+  }
+  return EAS_OK;
 }
 template <typename Params>
 static eas_status launch_prompt(const Params& pp, int hd, bool fp16, int budget, bool all, cudaStream_t st) {
-  if (pp.n_split == 1) {
-    if (hd == 64) return fp16 ? launch_prompt<64, true, false>(pp, budget, all, st) : launch_prompt<64, false, false>(pp, budget, all, st);
-    return fp16 ? launch_prompt<128, true, false>(pp, budget, all, st) : launch_prompt<128, false, false>(pp, budget, all, st);
-  }
-  if (hd == 64) return fp16 ? launch_prompt<64, true, true>(pp, budget, all, st) : launch_prompt<64, false, true>(pp, budget, all, st);
-  return fp16 ? launch_prompt<128, true, true>(pp, budget, all, st) : launch_prompt<128, false, true>(pp, budget, all, st);
+  if (hd == 64) return fp16 ? launch_prompt<64, true>(pp, budget, all, st) : launch_prompt<64, false>(pp, budget, all, st);
+  return fp16 ? launch_prompt<128, true>(pp, budget, all, st) : launch_prompt<128, false>(pp, budget, all, st);
 }
+
 static PromptParamsFew few_of(const PromptParams& pp) {
   PromptParamsFew f;
   static_cast<PromptCommon&>(f) = pp;
@@ -64,8 +65,7 @@ static PromptParamsFew few_of(const PromptParams& pp) {
   return f;
 }
 
-// How the work of up to kPromptMaxSeqs sequences is laid out: the units in the order in which they are dealt, and into how many parts their
-// key steps are cut.
+// How the work of a call is laid out: the sequences in the order in which their units are dealt.
 struct PromptPlan {
   std::vector<int> order;        // sequences with queries, longest first (stable): the tail of the static deal is short work
   int wg = 0, tile_tokens = 0;
@@ -80,44 +80,77 @@ static PromptPlan prompt_plan(const eas_prompt_inputs* in) {
                    [&](int a, int b) { return in->cu_k[a + 1] - in->cu_k[a] > in->cu_k[b + 1] - in->cu_k[b]; });
   return plan;
 }
-// Parts of the key steps for sequences order[first .. first + n).  Costs in key steps of a unit (1.2 us at head_dim 128): the busiest SM's
-// steps, kItemSteps a work item for its beginning and end, and what the parts' way through L2 takes.  One part unless another number is
-// clearly better; only for calls of fewer than kSplitUnits units an SM with long key ranges, where the deal leaves SMs without work.
-constexpr int kSplitUnits = 4, kSplitMost = 16, kSplitLeastSteps = 24;
-constexpr double kItemSteps = 2.0, kPartStepsPerSm = 0.35;
-static int prompt_split(const eas_prompt_inputs* in, const PromptPlan& plan, int first, int n, int sms) {
+// key steps of a unit whose last tile is the sequence's tile number `tiles` (counted from 1)
+static int64_t prompt_unit_steps(int64_t len_q, int64_t len_k, int64_t tiles, int tile_tokens) {
   constexpr int keys = PromptCfg<64>::kKeys;
-  int64_t units = 0, total = 0, most = 0;        // of all units: their number and key steps; the costliest
+  const int64_t seen = std::min(tiles * tile_tokens, len_q) + len_k - len_q;
+  return (std::max<int64_t>(seen, 0) + keys - 1) / keys;
+}
+// Into how many pieces the line of key steps of sequences order[first .. first + n) is cut (0: it is not, units are dealt whole), and the number of
+// items.  Costs in key steps of a unit (1.2 us at head_dim 128), fitted to calls on both sides: the busiest SM's steps, kUnitSteps a whole unit and
+// kItemSteps an item for its beginning and end and its way through L2, kJoinSteps for the joining launch.  Only for calls of at most kSplitUnits units
+// an SM with long key ranges, where the deal leaves SMs without work.
+constexpr int kSplitUnits = 4, kSplitLeastSteps = 24, kPieceLeastSteps = 8;
+constexpr double kUnitSteps = 2.0, kItemSteps = 5.0, kJoinSteps = 6.0;
+struct PromptCut {
+  int pieces = 0, items = 0, units = 0;
+  int64_t steps = 0;
+};
+static PromptCut prompt_cut(const eas_prompt_inputs* in, const PromptPlan& plan, int first, int n, int sms) {
+  PromptCut cut;
+  int64_t units = 0, empty = 0, total = 0, most = 0;       // of all units: their number, those without steps, key steps; the costliest
+  const int64_t most_units = std::min<int64_t>(static_cast<int64_t>(kSplitUnits) * sms, kPromptSplitUnits);
   for (int j = 0; j < n; ++j) {
     const int i = plan.order[first + j], len_q = in->cu_q[i + 1] - in->cu_q[i], len_k = in->cu_k[i + 1] - in->cu_k[i];
     const int64_t tiles = (static_cast<int64_t>(len_q) + plan.tile_tokens - 1) / plan.tile_tokens, per_head = (tiles + plan.wg - 1) / plan.wg;
     units += per_head * in->n_kv_heads;
-    if (units > static_cast<int64_t>(kSplitUnits) * sms) return 1;
+    if (units > most_units) return cut;
     for (int64_t t = tiles; t > 0; t -= plan.wg) {
-      const int64_t seen = std::min<int64_t>(t * plan.tile_tokens, len_q) + len_k - len_q, steps = (std::max<int64_t>(seen, 0) + keys - 1) / keys;
+      const int64_t steps = prompt_unit_steps(len_q, len_k, t, plan.tile_tokens);
       most = std::max(most, steps);
       total += steps * in->n_kv_heads;
+      empty += steps == 0 ? in->n_kv_heads : 0;
     }
   }
-  if (most < kSplitLeastSteps) return 1;
-  double best = 0;
-  int parts = 1;
-  for (int s = 1; s <= kSplitMost && (s == 1 || most / s >= 8); ++s) {
-    const int64_t rounds = (units * s + sms - 1) / sms;          // the busiest SM has that many items of middling cost, or the costliest one
-    double t = std::max(static_cast<double>(rounds) * total / (static_cast<double>(units) * s), static_cast<double>(most) / s) + rounds * kItemSteps;
-    if (s > 1) t = 1.05 * t + 3.0 + kPartStepsPerSm * s * static_cast<double>(units) / sms;      // (3: the joining launch)
-    if (s == 1 || t < best) { best = t; parts = s; }
-  }
-  return parts;
+  if (most < kSplitLeastSteps) return cut;
+  const int64_t rounds = (units + sms - 1) / sms;          // whole units: the busiest SM has that many of middling cost, or the costliest one
+  const double whole = std::max(static_cast<double>(rounds) * total / units, static_cast<double>(most)) + rounds * kUnitSteps;
+  const int64_t pieces = std::min<int64_t>({sms, kPromptPieces, total / kPieceLeastSteps}), items = units - empty + pieces - 1;
+  const double in_pieces = 1.05 * (static_cast<double>(total) / pieces + ((units + pieces - 1) / pieces + 1) * kItemSteps) + kJoinSteps;
+  if (in_pieces >= whole) return cut;
+  cut.pieces = static_cast<int>(pieces);
+  cut.items = static_cast<int>(items);                     // (at most: a piece may end where a unit does)
+  cut.units = static_cast<int>(units);
+  cut.steps = total;
+  return cut;
+}
+// The items of a cut launch
+static void prompt_items(PromptParamsSplit& pp, const PromptCut& cut, int wg) {
+  int unit = 0, item = 0, piece = 0;
+  int64_t at = 0;                                          // on the line
+  for (int s = 0; s < pp.n_seqs; ++s)
+    for (int b = 0; b < pp.per_head[s]; ++b) {
+      const int64_t steps = prompt_unit_steps(pp.len_q[s], pp.len_k[s], pp.tiles[s] - static_cast<int64_t>(b) * wg, pp.tile_tokens);
+      for (int h = 0; h < pp.n_kv; ++h, ++unit) {
+        pp.unit_item[unit] = static_cast<uint16_t>(item);
+        for (int64_t lo = 0; lo < steps;) {
+          if (at + lo == cut.steps * piece / cut.pieces) pp.piece_item[piece++] = static_cast<uint16_t>(item);
+          pp.item_unit[item] = static_cast<uint16_t>(unit);
+          pp.item_lo[item++] = static_cast<int>(lo);
+          lo = std::min(steps, cut.steps * piece / cut.pieces - at);
+        }
+        at += steps;
+      }
+    }
+  pp.unit_item[unit] = pp.piece_item[piece] = static_cast<uint16_t>(item);
+  pp.n_units = unit;
+  pp.n_pieces = piece;
+  pp.total_units = item;
 }
 // The units of a launch by cost, costliest first (a counting sort over their key steps): they are dealt to the SMs in rounds
 static void prompt_list(PromptParams& pp, int wg) {
-  constexpr int keys = PromptCfg<64>::kKeys;
   std::vector<int> count;
-  auto steps = [&](int s, int back) {
-    const int seen = std::min((pp.tiles[s] - back * wg) * pp.tile_tokens, pp.len_q[s]) + pp.len_k[s] - pp.len_q[s];
-    return (std::max(seen, 0) + keys - 1) / keys;
-  };
+  auto steps = [&](int s, int back) { return prompt_unit_steps(pp.len_q[s], pp.len_k[s], pp.tiles[s] - static_cast<int64_t>(back) * wg, pp.tile_tokens); };
   for (int s = 0; s < pp.n_seqs; ++s)
     for (int b = 0; b < pp.per_head[s]; ++b) {
       const size_t c = static_cast<size_t>(steps(s, b));
@@ -163,11 +196,8 @@ static size_t prompt_workspace(const eas_prompt_inputs* in, const PromptPlan& pl
   size_t bytes = 0;
   const int rows = static_cast<int>(plan.order.size());
   for (int first = 0; first < rows; first += kPromptMaxSeqs) {
-    const int n = std::min(kPromptMaxSeqs, rows - first), parts = prompt_split(in, plan, first, n, sms);
-    if (parts == 1) continue;
-    int64_t units = 0;
-    for (int j = 0; j < n; ++j) units += prompt_units(in, plan, plan.order[first + j]);
-    bytes = std::max(bytes, static_cast<size_t>(units) * parts * prompt_part_bytes(plan.wg, in->head_dim));
+    const PromptCut cut = prompt_cut(in, plan, first, std::min(kPromptMaxSeqs, rows - first), sms);
+    bytes = std::max(bytes, static_cast<size_t>(cut.items) * prompt_part_bytes(plan.wg, in->head_dim));
   }
   return bytes;
 }
@@ -233,16 +263,21 @@ static eas_status prompt_attention(const eas_prompt_inputs* in, void* workspace,
       if (units > (1 << 24)) return fail(EAS_ERR_UNSUPPORTED, "too many query rows for one call");
     }
     pp.unit_prefix[pp.n_seqs] = static_cast<int>(units);
-    pp.n_split = prompt_split(in, plan, first, pp.n_seqs, sms);
-    pp.total_units = static_cast<int>(units) * pp.n_split;
-    pp.by_kv = divider(G); pp.by_split = divider(pp.n_split);
+    pp.total_units = static_cast<int>(units);
+    pp.by_kv = divider(G);
+    const PromptCut cut = prompt_cut(in, plan, first, pp.n_seqs, sms);
+    if (cut.pieces > 0) {
+      PromptParamsSplit split;
+      static_cast<PromptSeqs<kPromptMaxSeqs>&>(split) = pp;
+      prompt_items(split, cut, plan.wg);
+      split.o_ws = static_cast<float4*>(workspace);
+      split.ml_ws = reinterpret_cast<float2*>(split.o_ws + static_cast<size_t>(split.total_units) * plan.wg * 128 * (hd / 4));
+      EAS_TRY(launch_prompt(split, hd, h, budget, all, st));
+      continue;
+    }
     pp.listed = 0;
     if (units <= kPromptListed && units > budget && pp.n_seqs > 1) prompt_list(pp, plan.wg);
-    if (pp.n_split > 1) {
-      pp.o_ws = static_cast<float4*>(workspace);
-      pp.ml_ws = reinterpret_cast<float2*>(pp.o_ws + static_cast<size_t>(pp.total_units) * plan.wg * 128 * (hd / 4));
-    }
-    EAS_TRY(pp.listed || pp.n_seqs > kPromptFewSeqs ? launch_prompt(pp, hd, h, budget, all, st) : launch_prompt(few_of(pp), hd, h, budget, all, st));
+    EAS_TRY(pp.listed || pp.n_seqs > PromptParamsFew::kSeqs ? launch_prompt(pp, hd, h, budget, all, st) : launch_prompt(few_of(pp), hd, h, budget, all, st));
   }
   return EAS_OK;
 }

@@ -245,6 +245,28 @@ def test_prompt_attention_few_queries_many_keys(hd, dtype, H, G, lens, keys):
     assert e.value.status == 3
 
 
+@pytest.mark.parametrize("hd,H,G,seed", [(64, 8, 2, 1), (128, 8, 2, 2), (128, 5, 5, 3), (64, 24, 3, 4), (128, 4, 1, 5)])
+def test_prompt_attention_cut_lines_of_many_units(hd, H, G, seed):
+    """Units of very different lengths, some without keys, so that a piece of the line holds ends, whole units and beginnings."""
+    import paper_2609_31551_b200 as P
+    rng = np.random.Generator(np.random.PCG64(seed))
+    n = int(rng.integers(3, 30))
+    lens = [int(x) for x in rng.choice([0, 1, 2, 7, 40, 130], n)]
+    keys = [int(x) for x in rng.integers(1, 600, n)]
+    keys[1], keys[2], lens[1], lens[2] = 9000, 0, 33, 5
+    cu_q, cu_k = _cu(lens), _cu(keys)
+    assert P.prompt_attention_workspace_bytes(H, G, hd, cu_q, cu_k) > 0
+    q = _rand((cu_q[-1], H, hd), torch.bfloat16, 75, 2.0)
+    k, v = _rand((cu_k[-1], G, hd), torch.bfloat16, 76), _rand((cu_k[-1], G, hd), torch.bfloat16, 77)
+    args = (q.cuda(), k.cuda(), v.cuda(), cu_q, cu_k)
+    out, status = P.prompt_attention(*args)
+    assert int(status[0]) == 0
+    _check_prompt(q, k, v, cu_q, cu_k, out, hd ** -0.5)
+    for budget in (1, 20, 147):
+        again, status = P.prompt_attention(*args, sm_budget=budget)
+        assert int(status[0]) == 0 and torch.equal(out, again)
+
+
 @pytest.mark.parametrize("hd", [64, 128])
 def test_prompt_attention_split_and_non_finite_values(hd):
     import paper_2609_31551_b200 as P
