@@ -33,6 +33,12 @@ import eas_synth as S  # noqa: E402
 from . import binding as B  # noqa: E402
 
 
+def _check_word(status):
+    word = int(status[0])
+    if word:
+        raise RuntimeError(f"the neighbour's kernels raised status {word}")
+
+
 class PrefillNeighbour:
     """A stream of out = A W^T products (M x N x K, bf16) on `sm_budget` SMs of its own stream."""
 
@@ -49,6 +55,9 @@ class PrefillNeighbour:
     def enqueue(self, count: int, sm_budget: int):
         for _ in range(count):
             B.kernel_gemm(self.a, self.w, self.bias, sm_budget=sm_budget, stream=self.stream, out=self.out, status=self.status)
+
+    def check(self):
+        _check_word(self.status)
 
 
 class PromptNeighbour:
@@ -69,6 +78,9 @@ class PromptNeighbour:
     def enqueue(self, count: int, sm_budget: int):
         for _ in range(count):
             self._call(self.q, self.k, self.v, self.cu, out=self.out, status=self.status, sm_budget=sm_budget, stream=self.stream)
+
+    def check(self):
+        _check_word(self.status)
 
 
 class TokenNeighbour:
@@ -94,6 +106,9 @@ class TokenNeighbour:
     def enqueue(self, count: int, sm_budget: int):
         for _ in range(count):
             self.cache.attention(self.q, self.lens, self.table, out=self.out, workspace=self.workspace, sm_budget=sm_budget, stream=self.stream)
+
+    def check(self):
+        self.cache.check()
 
 
 NEIGHBOURS = {"gemm": PrefillNeighbour, "prompt": PromptNeighbour, "token": TokenNeighbour}
@@ -175,6 +190,7 @@ def measure(config: str, micro_batch: int, levels=(0.3, 0.5, 0.7), reps: int = 5
         e0, e1 = _encode_ms(enc, batch, n_enc, reps, enc_stream)
         torch.cuda.synchronize()
         enc.status(enc_stream)
+        nb.check()
         beside = e0.elapsed_time(e1) / reps
         nb_beside = n0.elapsed_time(n1) / count
         if part is not None:
