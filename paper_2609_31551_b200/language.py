@@ -234,12 +234,11 @@ class KvCache:
             raise B.EasError(1, f"block_table must be an int32 tensor [{n}, max_blocks] on {self.device}")
         return _pack_seqs(n, block_table.data_ptr(), shape[1], block_table.stride(0) if n > 1 else shape[1], cu_seqlens, start, seq_lens)
 
-    def _move(self, call, k, v, cu_seqlens, start, block_table, sm_budget):
+    def _move(self, call, k, v, rows, cu_seqlens, start, block_table, sm_budget):
         n, index, dtype = start.shape[0], self._index, k.dtype
         seqs = self._seqs(block_table, n, _ints(cu_seqlens, "cu_seqlens", n + 1, index), _ints(start, "start", n, index), 0)
-        rows = k.shape[0]
-        if dtype not in _DTYPES or rows != v.shape[0]:
-            raise B.EasError(1, "k and v must be bf16 or fp16, with as many rows")
+        if dtype not in _DTYPES or k.shape[0] != v.shape[0] or k.shape[0] < rows:
+            raise B.EasError(1, "k and v must be bf16 or fp16, with as many rows, and at least the rows of the call")
         ld_k, ld_v = _rows(k, "k", self.n_kv_heads, self.head_dim, dtype, index), _rows(v, "v", self.n_kv_heads, self.head_dim, dtype, index)
         rc = call(self.handle, seqs, k.data_ptr(), ld_k, v.data_ptr(), ld_v, rows, _DTYPES[dtype], sm_budget,
                   torch._C._cuda_getCurrentRawStream(index), self._status_at)
@@ -253,18 +252,18 @@ class KvCache:
         if _elsewhere(self._index, stream):
             with _on(self._index, stream):
                 return self.store(k, v, cu_seqlens, start, block_table, sm_budget)
-        self._move(self.lib.eas_cache_store, k, v, cu_seqlens, start, block_table, sm_budget)
+        self._move(self.lib.eas_cache_store, k, v, k.shape[0], cu_seqlens, start, block_table, sm_budget)
 
     def load(self, cu_seqlens, start, block_table, n_rows, dtype=torch.bfloat16, out=None, sm_budget=0, stream=None):
         """eas_cache_load: the values of the same places -> (k, v), [n_rows, n_kv_heads, head_dim].  Rows that cu_seqlens does not name are
-        left as they were (`out`, a pair of tensors) or are not set."""
+        left as they were (`out`, a pair of tensors of at least n_rows rows, whose type counts) or are not set."""
         if _elsewhere(self._index, stream):
             with _on(self._index, stream):
                 return self.load(cu_seqlens, start, block_table, n_rows, dtype, out, sm_budget)
         if out is None:
             shape = (n_rows, self.n_kv_heads, self.head_dim)
             out = self.k.new_empty(shape, dtype=dtype), self.k.new_empty(shape, dtype=dtype)
-        self._move(self.lib.eas_cache_load, out[0], out[1], cu_seqlens, start, block_table, sm_budget)
+        self._move(self.lib.eas_cache_load, out[0], out[1], n_rows, cu_seqlens, start, block_table, sm_budget)
         return out
 
     def attention_workspace_bytes(self, n_seqs, n_heads):

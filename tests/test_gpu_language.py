@@ -465,6 +465,22 @@ def test_cache_store_ignores_rows_past_the_tensor():
     assert torch.equal(c.k[:3], want[:3]) and torch.equal(c.k[3, 0, 5:], want[3, 0, 5:])
 
 
+def test_cache_load_writes_no_row_behind_n_rows():
+    numbers, scales = _filled(3, 2, 16, 64, 52)
+    c = _cache(numbers, scales)
+    k, v = (torch.full((12, 2, 64), 5.0, dtype=torch.float16, device="cuda") for _ in range(2))
+    cu, start, table = _dev([0, 40]), _dev([0]), _dev([[2, 0, 1]])      # 40 rows announced, 9 asked for, 12 there
+    got = c.load(cu, start, table, 9, out=(k, v))
+    c.check()
+    assert got[0] is k and (k[9:] == 5.0).all() and (v[9:] == 5.0).all()
+    want = c.load(cu, start, table, 40, dtype=torch.float16)
+    assert torch.equal(k[:9], want[0][:9]) and torch.equal(v[:9], want[1][:9])
+    import paper_2609_31551_b200 as P
+    with pytest.raises(P.EasError) as e:
+        c.load(cu, start, table, 13, out=(k, v))
+    assert e.value.status == 1
+
+
 # ------------------------------------------------------------------------------------------------ single tokens
 def _check_tokens(c, numbers, scales, q, lens, table, scale=None, **kw):
     hd, bs = q.shape[2], numbers[0].shape[2]
