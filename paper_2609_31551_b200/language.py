@@ -96,7 +96,7 @@ def _rows(t, name, heads, head_dim, dtype, index):
 
 
 def _ints(t, name, n, index):
-    if t.dtype != torch.int32 or t.get_device() != index or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+    if t.dtype != torch.int32 or t.get_device() != index or t.shape != (n,) or not t.is_contiguous():
         raise B.EasError(1, f"{name} must be a contiguous int32 tensor [{n}] on GPU {index}, not {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
@@ -234,12 +234,18 @@ class KvCache:
             raise B.EasError(1, f"block_table must be an int32 tensor [{n}, max_blocks] on {self.device}")
         return _pack_seqs(n, block_table.data_ptr(), shape[1], block_table.stride(0) if n > 1 else shape[1], cu_seqlens, start, seq_lens)
 
-    def _move(self, call, k, v, rows, cu_seqlens, start, block_table, sm_budget):
+    def _move(self, call, k, v, rows, cu_seqlens, start, block_table, sm_budget, new=False):
+        """new: k and v are the call's own, made for it."""
         n, index, dtype = start.shape[0], self._index, k.dtype
         seqs = self._seqs(block_table, n, _ints(cu_seqlens, "cu_seqlens", n + 1, index), _ints(start, "start", n, index), 0)
-        if dtype not in _DTYPES or k.shape[0] != v.shape[0] or k.shape[0] < rows:
-            raise B.EasError(1, "k and v must be bf16 or fp16, with as many rows, and at least the rows of the call")
-        ld_k, ld_v = _rows(k, "k", self.n_kv_heads, self.head_dim, dtype, index), _rows(v, "v", self.n_kv_heads, self.head_dim, dtype, index)
+        if dtype not in _DTYPES:
+            raise B.EasError(1, f"k and v must be bf16 or fp16, not {dtype}")
+        if new:
+            ld_k = ld_v = self.n_kv_heads * self.head_dim
+        else:
+            if k.shape[0] != v.shape[0] or k.shape[0] < rows:
+                raise B.EasError(1, "k and v must have as many rows, and at least the rows of the call")
+            ld_k, ld_v = _rows(k, "k", self.n_kv_heads, self.head_dim, dtype, index), _rows(v, "v", self.n_kv_heads, self.head_dim, dtype, index)
         rc = call(self.handle, seqs, k.data_ptr(), ld_k, v.data_ptr(), ld_v, rows, _DTYPES[dtype], sm_budget,
                   torch._C._cuda_getCurrentRawStream(index), self._status_at)
         if rc:
@@ -260,10 +266,11 @@ class KvCache:
         if _elsewhere(self._index, stream):
             with _on(self._index, stream):
                 return self.load(cu_seqlens, start, block_table, n_rows, dtype, out, sm_budget)
-        if out is None:
+        new = out is None
+        if new:
             shape = (n_rows, self.n_kv_heads, self.head_dim)
             out = self.k.new_empty(shape, dtype=dtype), self.k.new_empty(shape, dtype=dtype)
-        self._move(self.lib.eas_cache_load, out[0], out[1], n_rows, cu_seqlens, start, block_table, sm_budget)
+        self._move(self.lib.eas_cache_load, out[0], out[1], n_rows, cu_seqlens, start, block_table, sm_budget, new)
         return out
 
     def attention_workspace_bytes(self, n_seqs, n_heads):
