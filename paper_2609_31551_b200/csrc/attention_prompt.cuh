@@ -39,6 +39,7 @@ namespace eas {
 constexpr int kPromptMaxSeqs = 128;      // sequences of one launch (kernel parameters)
 constexpr int kPromptListed = 2048;      // units that the list of a launch holds
 
+constexpr uint32_t kPromptNoUnit = 0xFFFFFFFFu;   // an entry of the list without work
 constexpr int kPromptPieces = 192;       // SPLIT: pieces of the line of steps, at most,
 constexpr int kPromptSplitUnits = 768;   // and units
 
@@ -83,8 +84,8 @@ struct PromptParamsFew : PromptSeqs<8> {                          // a few seque
 struct PromptParams : PromptSeqs<kPromptMaxSeqs> {
   static constexpr int kSeqs = kPromptMaxSeqs;
   static constexpr bool kListed = true, kSplit = false;
-  // Few rounds of units of different cost: the deal follows this list, costliest first (sequence << 24 | unit of the sequence), instead of
-  // the sequences one after the other (8 prompts of 1 to 1563 tokens, 580 units: 14 to 39 key steps an SM without it)
+  // Few rounds of units of different cost: the deal follows this list (sequence << 24 | unit of the sequence), which gives the costliest unit to
+  // the CTA with the least to do, instead of the sequences one after the other (8 prompts of 1 to 1563 tokens, 608 units: 14 to 39 key steps an SM)
   int listed;
   uint32_t list[kPromptListed];
 };
@@ -146,6 +147,7 @@ __device__ __forceinline__ PromptUnit prompt_decode(const Params& p, int unit, i
   if constexpr (Params::kListed) {
     if (p.listed) {
       const uint32_t e = p.list[unit];
+      if (e == kPromptNoUnit) return PromptUnit{};
       lo = static_cast<int>(e >> 24);
       k = static_cast<int>(e & 0xFFFFFFu);
       listed = true;

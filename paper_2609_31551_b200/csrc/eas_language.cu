@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cmath>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "attention_cache.cuh"
@@ -147,23 +148,55 @@ static void prompt_items(PromptParamsSplit& pp, const PromptCut& cut, int wg) {
   pp.n_pieces = piece;
   pp.total_units = item;
 }
-// The units of a launch by cost, costliest first (a counting sort over their key steps): they are dealt to the SMs in rounds
-static void prompt_list(PromptParams& pp, int wg) {
+// The units of a launch by cost, costliest first (a counting sort over their key steps), each to the CTA of `grid` with the least to do so far.  The
+// CTAs' loads are small whole numbers, so those with the same load form a list, and the least load only grows.  (Dealt in rounds of alternating
+// direction instead, costliest first: 8 prompts of 1 to 1563 tokens of head_dim 128 53 instead of 49 us, 10 of 3 to 1000 29 instead of 25.5, of head_dim 64 22.9
+// instead of 24.0.  The host takes 5 ns a unit for it.)
+static void prompt_list(PromptParams& pp, int wg, int grid) {
   std::vector<int> count;
-  auto steps = [&](int s, int back) { return prompt_unit_steps(pp.len_q[s], pp.len_k[s], pp.tiles[s] - static_cast<int64_t>(back) * wg, pp.tile_tokens); };
+  auto steps = [&](int s, int back) {
+    return static_cast<size_t>(prompt_unit_steps(pp.len_q[s], pp.len_k[s], pp.tiles[s] - static_cast<int64_t>(back) * wg, pp.tile_tokens));
+  };
   for (int s = 0; s < pp.n_seqs; ++s)
     for (int b = 0; b < pp.per_head[s]; ++b) {
-      const size_t c = static_cast<size_t>(steps(s, b));
+      const size_t c = steps(s, b);
       if (count.size() <= c) count.resize(c + 1, 0);
       count[c] += pp.n_kv;
     }
+  const size_t most = count.size() - 1 + static_cast<size_t>(kUnitSteps);
+  int64_t load = 0;
   int at = 0;
-  for (size_t c = count.size(); c-- > 0;) { const int n = count[c]; count[c] = at; at += n; }
+  for (size_t c = count.size(); c-- > 0;) {
+    const int n = count[c];
+    load += static_cast<int64_t>(n) * (c + static_cast<size_t>(kUnitSteps));
+    count[c] = at;
+    at += n;
+  }
+  std::vector<std::pair<uint32_t, int>> sorted(pp.total_units);   // (unit, cost)
   for (int s = 0; s < pp.n_seqs; ++s)
     for (int b = 0; b < pp.per_head[s]; ++b) {
-      int& to = count[static_cast<size_t>(steps(s, b))];
-      for (int h = 0; h < pp.n_kv; ++h) pp.list[to++] = static_cast<uint32_t>(s) << 24 | static_cast<uint32_t>(b * pp.n_kv + h);
+      const size_t c = steps(s, b);
+      for (int h = 0; h < pp.n_kv; ++h)
+        sorted[count[c]++] = {static_cast<uint32_t>(s) << 24 | static_cast<uint32_t>(b * pp.n_kv + h), static_cast<int>(c) + static_cast<int>(kUnitSteps)};
     }
+  std::vector<int> with(load / grid + most + 1, -1), next(grid), held(grid, 0);      // the first CTA with a load, the next with the same, a CTA's units
+  for (int j = grid; j-- > 0;) { next[j] = with[0]; with[0] = j; }
+  int rounds = 0;
+  size_t least = 0;
+  auto place = [&](int r, int j) { return r * grid + (r & 1 ? grid - 1 - j : j); };  // (attn_unit_at)
+  for (const auto& [unit, cost] : sorted) {
+    while (with[least] < 0) ++least;
+    const int j = with[least], r = held[j]++;
+    with[least] = next[j];
+    next[j] = with[least + cost];
+    with[least + cost] = j;
+    if ((r + 1) * grid > kPromptListed) return;                  // (dealt without a list)
+    rounds = std::max(rounds, r + 1);
+    pp.list[place(r, j)] = unit;
+  }
+  for (int j = 0; j < grid; ++j)
+    for (int r = held[j]; r < rounds; ++r) pp.list[place(r, j)] = kPromptNoUnit;
+  pp.total_units = rounds * grid;
   pp.listed = 1;
 }
 static Divider divider(int d) {
@@ -276,7 +309,7 @@ static eas_status prompt_attention(const eas_prompt_inputs* in, void* workspace,
       continue;
     }
     pp.listed = 0;
-    if (units <= kPromptListed && units > budget && pp.n_seqs > 1) prompt_list(pp, plan.wg);
+    if (units <= kPromptListed && units > budget && pp.n_seqs > 1) prompt_list(pp, plan.wg, budget);
     EAS_TRY(pp.listed || pp.n_seqs > PromptParamsFew::kSeqs ? launch_prompt(pp, hd, h, budget, all, st) : launch_prompt(few_of(pp), hd, h, budget, all, st));
   }
   return EAS_OK;
