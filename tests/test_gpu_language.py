@@ -209,6 +209,23 @@ def test_prompt_attention_of_many_short_sequences():
     _check_prompt(q, k, v, cu, cu, out, 0.125)
 
 
+@pytest.mark.parametrize("lens,G", [([2500] + [1] * 110, 16), ([700, 30, 1, 250, 90] * 5, 8), ([129] * 60 + [1000], 5)])
+def test_prompt_attention_units_of_unequal_cost(lens, G):
+    """Lists with empty entries, and (the first) more rounds than a list holds."""
+    import paper_2609_31551_b200 as P
+    rng = np.random.Generator(np.random.PCG64(12))
+    lens = [lens[i] for i in rng.permutation(len(lens))]
+    cu = _cu(lens)
+    q, k, v = (_rand((cu[-1], G, 64), torch.float16, 90 + i, 1.5) for i in range(3))
+    args = (q.cuda(), k.cuda(), v.cuda(), cu)
+    out, status = P.prompt_attention(*args)
+    assert int(status[0]) == 0
+    _check_prompt(q, k, v, cu, cu, out, 0.125)
+    for budget in (5, 100):
+        again, status = P.prompt_attention(*args, sm_budget=budget)
+        assert int(status[0]) == 0 and torch.equal(out, again)
+
+
 def test_prompt_attention_long_sequence_tail_rows():
     """20 011 keys (some 250 steps a tile): the last rows and some others against the oracle."""
     import paper_2609_31551_b200 as P
