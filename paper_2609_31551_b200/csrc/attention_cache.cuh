@@ -10,8 +10,10 @@
 // The numbers -127 .. 127 are exact in fp16: 0x6400 | (byte ^ 0x80) is 1152 + number, less 1152 (two bytes by one and-xor and one
 // subtraction).  Queries enter as fp16 scaled by a power of two per row (bf16 has fewer bits than fp16: nothing is lost but what is
 // below 2^-24 of the row's largest).  A block's key scale multiplies its scores in fp32.  Its value scale v is an exponent: with
-// t = score + log2 v and w = 2^(t - m),  out = sum w number / sum w / v,  so w <= 2^8 fits fp16 whatever the scales are (w is
-// rounded to its 11 bits), and the sums are fp32.
+// t = score + log2 v and w = 2^(t - m),  out = sum w number / sum w / v,  and w fits fp16 whatever the scales are: m is kept 2^7 below the largest
+// t and moves when one comes more than 2^15 above it, so the row's largest w is between 2^7 and 2^15 (fp16 ends at 65504).  w is rounded to 11 bits, and below
+// 2^-14 to multiples of 2^-24, which are 2^-31 of the largest or less; the sums are fp32, that of w / v from w before its rounding.  (With m at the largest t
+// itself, multiples of 2^-24 of it: 20000 tokens of 3.5 2^-24 each behind one that holds the rest were off by a seventh.)
 //
 // The tiles of all sequences and heads form one line, cut into as many equal pieces as the device has warps (a function of the device, not of
 // sm_budget: the cut, and with it every sum, is the same on a share of the SMs).  Beginning a row of tiles (queries in, output out) costs
@@ -49,6 +51,8 @@ struct CacheAttnParams {
 
 constexpr int kCacheMaxSeqs = 1024;      // sequences of one launch (the prefix sums lie in shared memory)
 constexpr int kRowCost = 1;
+constexpr float kRefBelow = 7.0f, kRefMoves = 15.0f;      // the reference lies that far below the largest score, and moves when one is that far above it
+constexpr float kWeightDown = 0.0078125f;  // 2^-kRefBelow: takes it out of w / v, so that blocks of value scale 2^-100 do not overflow their sum, and of O in the end
 constexpr int kCacheJoinThreads = 512;      // (256: 1536 rows of heads are two rounds of the device, 48 ragged caches 24 instead of 19 us)
 
 template <int HD, int NT>
@@ -391,9 +395,9 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
             }
           }
         }
-        // the tile's scales (lane m has those of its tokens 16 m ..): v as log2 v and 1 / v
+        // the tile's scales (lane m has those of its tokens 16 m ..): v as log2 v and 2^-kRefBelow / v
         const float vs = scales[0].y < kCacheMinScale ? kCacheMinScale : scales[0].y;      // (a NaN stays)
-        const float lane_lg = fast_lg2(vs), lane_inv = fast_ex2(-lane_lg);
+        const float lane_lg = fast_lg2(vs), lane_inv = fast_ex2(-lane_lg) * kWeightDown;
         float v_inv[MT];
         bool higher = false;
         float mx[NT][2];
@@ -427,15 +431,15 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
             mx[j][1] = fmax3(mx[j][1], sc[m][j][1], sc[m][j][3]);
           }
         }
-        // the reference moves only when a score is more than 2^8 above it (the first tile: always)
+        // (the first tile: always)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) higher = higher || mx[j][0] > m_ref[j][0] + 8.0f || mx[j][1] > m_ref[j][1] + 8.0f;
+        for (int j = 0; j < NT; ++j) higher = higher || mx[j][0] > m_ref[j][0] + kRefMoves || mx[j][1] > m_ref[j][1] + kRefMoves;
         if (__any_sync(0xffffffffu, higher)) {
 #pragma unroll
           for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
-              float x = fmaxf(mx[j][b], m_ref[j][b]);
+              float x = fmaxf(mx[j][b] - kRefBelow, m_ref[j][b]);
               x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
               x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
               x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
@@ -528,7 +532,7 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
           const int r = j * 8 + 2 * qt + b;
           if (r >= n_rows) continue;
           if (whole) {
-            const float inv = x == 0.f ? 0.f : 1.0f / x;
+            const float inv = x == 0.f ? 0.f : kWeightDown / x;
             uint16_t* dst = p.out + s * p.ld_out + static_cast<long long>(kvh * p.group + head0 + r) * HD + qg * (HD / 8);
 #pragma unroll
             for (int i = 0; i < HD / 16; i += 4) {
@@ -663,7 +667,7 @@ __global__ void __launch_bounds__(kCacheJoinThreads, 1) cache_join_kernel(const 
           }
         }
       }
-      const float inv = l == 0.f ? 0.f : 1.0f / l;
+      const float inv = l == 0.f ? 0.f : kWeightDown / l;
 #pragma unroll
       for (int i = 0; i < N; ++i) acc[i] *= inv;
     }

@@ -1,0 +1,115 @@
+"""The language-model operators where sums, references and infinities go wrong, against the fp64 oracle.
+
+Bounds.  u_p, u are the largest relative errors of one rounding to the type of the probabilities and of the output (2^-8 bf16, 2^-11 fp16), A the
+attention over |v|, smax the largest sum |q k| scale of a row.  An output element is off by at most
+  u_p A + u |out| + 2 (head_dim + 8) 2^-23 smax A + 2^-17 A
+(probabilities, output, scores, exponentials and sums).  fp16 weights are kept 2^7 above the reference, so that the row's largest is at least 2^7;
+below 2^-14 they are rounded to multiples of 2^-24, each off by at most 2^-25.  Prompts: the sum of the weights is at least 2^7, so together that is
+  n 2^-25 / 2^7 max |v| = n 2^-32 max |v|.
+Tokens: a weight is 2^(score + log2 scale of the value's block), the numbers are at most 127, and the sum of weight / value scale is at least 2^7 / (value scale
+v* of the token whose weight is the largest): n 2^-32 127 v*.  fp16 outputs below 2^-14 are off by at most 2^-25."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import language_oracle as LO
+
+pytestmark = pytest.mark.gpu
+U = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+DTYPES = [torch.bfloat16, torch.float16]
+
+
+def _rand(shape, dtype, seed, scale=1.0):
+    gen = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=gen) * scale).to(dtype)
+
+
+def _dev(x):
+    return torch.as_tensor(np.asarray(x), dtype=torch.int32).cuda()
+
+
+# ------------------------------------------------------------------------------------------------ single tokens
+def _cache(numbers, scales):
+    import paper_2609_31551_b200 as P
+    n, G, bs, hd = numbers[0].shape
+    return P.KvCache(n, bs, G, hd, tensors=(numbers[0].cuda(), numbers[1].cuda(), scales[0].cuda(), scales[1].cuda()))
+
+
+def _filled(n_blocks, G, bs, hd, seed):
+    gen = torch.Generator().manual_seed(seed)
+    numbers = [torch.randint(-127, 128, (n_blocks, G, bs, hd), generator=gen, dtype=torch.int8) for _ in range(2)]
+    scales = [torch.rand(n_blocks, G, generator=gen) * 0.03 + 0.005 for _ in range(2)]
+    return numbers, scales
+
+
+def _token_bound(numbers, scales, q, lens, table):
+    """The definition and each row's own bound: n, value scale and magnitude of what this row reads."""
+    H, G, hd, bs = q.shape[1], numbers[0].shape[1], q.shape[2], numbers[0].shape[2]
+    scale = hd ** -0.5
+    ref, mag, smax = LO.cache_attention(q, numbers[0], numbers[1], scales[0], scales[1], lens, table, scale)
+    top = torch.zeros(q.shape[:2], dtype=torch.float64)              # value scale of the token of the largest weight
+    for s, n in enumerate(lens):
+        if n <= 0:
+            continue
+        k = LO.cache_values(numbers[0], scales[0], table[s], n)
+        vs = scales[1][table[s, torch.arange(n) // bs].long()].double().clamp_min(2.0 ** -100)       # [n, G]
+        for h in range(H):
+            g = h * G // H
+            t = (k[:, g] @ q[s, h].double()) * scale * 1.4426950408889634 + vs[:, g].log2()
+            top[s, h] = vs[t.argmax(), g]
+    u = U[q.dtype]
+    n_tok = torch.tensor([max(n, 0) for n in lens], dtype=torch.float64)
+    tol = mag * (2.0 ** -11 + u * 1.01 + 2 * (hd + 8) * 2.0 ** -23 * smax[..., None] + 2.0 ** -17)
+    return ref, tol + (1.1 * 2.0 ** -32 * 127 * n_tok[:, None] * top)[..., None] + (2.0 ** -25 if q.dtype == torch.float16 else 0.0)
+
+
+def _check_tokens(numbers, scales, q, lens, table, c=None):
+    c = c or _cache(numbers, scales)
+    out = c.attention(q.cuda(), _dev(lens), table.cuda())
+    c.check()
+    ref, tol = _token_bound(numbers, scales, q, lens, table)
+    err = (out.double().cpu() - ref).abs()
+    assert (err <= tol).all(), float((err / tol.clamp_min(1e-300)).max())
+    return out
+
+
+@pytest.mark.parametrize("hd,group", [(64, 1), (128, 4), (128, 12)])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("w24", [40.5, 3.5])
+@pytest.mark.parametrize("unequal", [False, True])
+def test_token_one_place_in_front_of_many_equal_ones(hd, group, dtype, w24, unequal):
+    """One place holds most of the weight and next to no value, 20000 others a weight of w24 2^-24 of it each; value scales equal, or of several sizes.
+    More rows than the device has warps (every sequence reads the same blocks), so that most are one warp's from end to end."""
+    bs, n, n_seqs, G = 128, 20000, 128, 16
+    H, blocks = G * group, (n + bs - 1) // bs
+    gen = torch.Generator().manual_seed(12)
+    numbers = [torch.zeros(blocks, G, bs, hd, dtype=torch.int8), torch.randint(90, 128, (blocks, G, bs, hd), generator=gen, dtype=torch.int8)]
+    scales = [torch.full((blocks, G), 0.01), torch.full((blocks, G), 0.01)]
+    if unequal:
+        scales[1][5::3] = 0.16
+    numbers[0][0, :, 0], numbers[1][0, :, 0] = 127, 1
+    scales[0][0] = float(np.log(2.0 ** 24 / w24) / (127 * hd ** 0.5))
+    table = torch.arange(blocks, dtype=torch.int32).repeat(n_seqs, 1)
+    c = _cache(numbers, scales)
+    got = c.attention(torch.ones(n_seqs, H, hd).to(dtype).cuda(), _dev([n] * n_seqs), table.cuda()).double().cpu()
+    c.check()
+    ref, tol = _token_bound(numbers, scales, torch.ones(1, H, hd).to(dtype)[:, ::group], [n], table)
+    err = (got - ref.repeat_interleave(group, 1)).abs()
+    assert (err <= tol.repeat_interleave(group, 1)).all(), float((err / tol.repeat_interleave(group, 1)).max())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_token_value_scales_of_all_sizes_row_by_row(dtype):
+    """Blocks whose value scales lie many powers of ten apart: each row within what its own blocks allow."""
+    bs, hd, G, H = 16, 128, 2, 6
+    numbers, scales = _filled(16, G, bs, hd, 13)
+    exps = torch.tensor([-12.0, 0.0, -3.0, -30.0, 1.0, -6.0, -1.0, -20.0, 0.0, -2.0, -9.0, -4.0, 0.5, -0.5, -8.0, -5.0])
+    if dtype == torch.float16:
+        exps = exps.clamp_min(-6.0)
+    scales[1] = (10.0 ** exps)[:, None].float().repeat(1, G)
+    table = torch.tensor([[3, 14, 0, 7, 9, 1, 11, 5, 2, 10], [4, 6, 8, 12, 13, 15, 0, 0, 0, 0]], dtype=torch.int32)
+    q = _rand((2, H, hd), dtype, 14)
+    q[0, 0] *= 1e-3
+    q[0, 1] *= 60.0
+    q[1, 2] = 0.0
+    _check_tokens(numbers, scales, q, [160, 83], table)
