@@ -18,7 +18,9 @@
 //
 // The reference maximum only moves when the row maximum grows by more than 2^8 in the exponent; then the thread rescales
 // its O row in TMEM.  Scores, sums and O are fp32; P is rounded to the data type (bf16 or fp16: what the matrix product takes), and the
-// output once at the end.  A row's arithmetic depends on its own sequence alone, not on the unit, the packing or the SMs.
+// output once at the end.  In fp16 P is 2^7 times what the reference gives (at most 2^15; fp16 ends at 65504), in the sum too: weights
+// below 2^-21 of the reference instead of 2^-14 lose bits (20000 keys of 6.5 2^-24 each behind one that holds the rest were off by 7.7 %).
+// A row's arithmetic depends on its own sequence alone, not on the unit, the packing or the SMs.
 //
 // Few rows against many keys (a chunk of a prompt behind a long prefix) make fewer units than there are SMs.  SPLIT lays the key steps of all
 // units end to end and cuts the line into one equal piece per SM: a piece is a few work items (the end of a unit, whole units, the beginning of
@@ -38,6 +40,9 @@ namespace eas {
 
 constexpr int kPromptMaxSeqs = 128;      // sequences of one launch (kernel parameters)
 constexpr int kPromptListed = 2048;      // units that the list of a launch holds
+
+template <bool FP16>
+constexpr float kPromptRaise = FP16 ? 7.0f : 0.0f;       // log2 of what P and its sum are times what the reference gives
 
 constexpr uint32_t kPromptNoUnit = 0xFFFFFFFFu;   // an entry of the list without work
 constexpr int kPromptPieces = 192;       // SPLIT: pieces of the line of steps, at most,
@@ -225,7 +230,7 @@ __device__ __noinline__ void prompt_repair(const PromptCommon& p, int q_row, int
     for (int i = 0; i < N; ++i) s = fmaf(q[i], load16(kp[j * p.ld_k + i], FP16), s);
 #pragma unroll
     for (int d = 16; d > 0; d /= 2) s += __shfl_xor_sync(0xffffffffu, s, d);
-    const float w = fast_ex2((s - m) * p.scale_log2);
+    const float w = fast_ex2((s - m) * p.scale_log2 + kPromptRaise<FP16>);
 #pragma unroll
     for (int i = 0; i < N; ++i) acc[i] = fmaf(w, load16(vp[j * p.ld_v + i], FP16), acc[i]);
   }
@@ -652,7 +657,7 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
         const bool moved = (j == 0 && mx != -INFINITY) || (mx - m_used) * p.scale_log2 > kRescaleThreshold;
         m_used = moved ? mx : m_used;
         const uint32_t rescale = __ballot_sync(0xffffffffu, moved && j != 0);
-        const float mb = m_used * p.scale_log2;
+        const float mb = m_used * p.scale_log2 - kPromptRaise<FP16>;
         const uint64_t nmb2 = pack2(-mb, -mb);
         const uint64_t l_old[2] = {l2[0], l2[1]};
         l2[0] = l2[1] = 0;

@@ -28,6 +28,45 @@ def _dev(x):
     return torch.as_tensor(np.asarray(x), dtype=torch.int32).cuda()
 
 
+def _prompt(q, k, v, cu_q, cu_k, **kw):
+    import paper_2609_31551_b200 as P
+    out, status = P.prompt_attention(q.cuda(), k.cuda(), v.cuda(), cu_q, cu_k, **kw)
+    assert int(status[0]) == 0
+    return out.cpu()
+
+
+def _is_cut(q, k, cu_q, cu_k):
+    import paper_2609_31551_b200 as P
+    return P.prompt_attention_workspace_bytes(q.shape[1], k.shape[1], q.shape[2], cu_q, cu_k) > 0
+
+
+def _prompt_tol(q, mag, smax, n, vmax):
+    hd, u = q.shape[2], U[q.dtype]
+    tol = mag * (u + u * 1.01 + 2 * (hd + 8) * 2.0 ** -23 * smax[..., None] + 2.0 ** -17)
+    return tol + (1.1 * n * 2.0 ** -32 * vmax + 2.0 ** -25 if q.dtype == torch.float16 else 0.0)
+
+
+# ------------------------------------------------------------------------------------------------ prompts: references
+@pytest.mark.parametrize("w24", [75.5, 6.5])
+@pytest.mark.parametrize("hd,H,G,T,rows,cut", [(128, 8, 2, 20011, 20011, False), (64, 48, 6, 16009, 16009, False), (128, 4, 1, 24000, 3, True)])
+def test_prompt_one_key_in_front_of_many_equal_ones_fp16(w24, hd, H, G, T, rows, cut):
+    """The first key holds most of the weight and next to no value; what comes out is what thousands of keys with weights of w24 2^-24 have."""
+    q = torch.ones(rows, H, hd).half()
+    k, v = torch.zeros(T, G, hd).half(), (_rand((T, G, hd), torch.float32, 11).abs() * 0.2 + 0.8).half()
+    k[0] = float(np.log(2.0 ** 24 / w24) / hd ** 0.5)
+    v[0] = 2.0 ** -14
+    cu_q, cu_k = [0, rows], [0, T]
+    assert _is_cut(q, k, cu_q, cu_k) == cut
+    got = _prompt(q, k, v, cu_q, cu_k).double()
+    for i in (0, 1, 77, T // 2, T - 2, T - 1):
+        if i < T - rows:
+            continue
+        r = i - (T - rows)
+        ref, mag, smax = LO.prompt_attention(q[r:r + 1], k[:i + 1], v[:i + 1], [0, 1], [0, i + 1], hd ** -0.5)
+        err, tol = (got[r:r + 1] - ref).abs(), _prompt_tol(q, mag, smax, i + 1, 2.0)
+        assert (err <= tol).all(), (i, float((err / tol).max()))
+
+
 # ------------------------------------------------------------------------------------------------ single tokens
 def _cache(numbers, scales):
     import paper_2609_31551_b200 as P
