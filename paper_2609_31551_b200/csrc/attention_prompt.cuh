@@ -616,7 +616,7 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
       }
       // keys that this row sees; rows that are not stored see all (what they compute does not matter, and masking would cost every step)
       const int limit = stored ? max(tok + 1 + u.ahead, 0) : 0x7fffffff;
-      float m_used = 0.f;
+      float m_used = -INFINITY;                     // no reference yet
       uint64_t l2[2] = {0, 0};                      // row sum, two packed accumulators
       int left = limit - part.lo * KEYS;            // of them from this step on
 #pragma unroll 1
@@ -651,13 +651,13 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
           }
           mx = fmax3(fmaxf(c0, c1), c2, c3);
         }
-        // the reference maximum moves only when the row maximum grew by more than the threshold (the first step: always).  A row that
-        // sees nothing keeps 0: its exponentials are those of -inf.
+        // the reference maximum moves when the row maximum grew by more than the threshold, and to the row's first score above -inf.  Without
+        // one the exponentials are those of -inf against 0.
         const float m_old = m_used;
-        const bool moved = (j == 0 && mx != -INFINITY) || (mx - m_used) * p.scale_log2 > kRescaleThreshold;
+        const bool moved = (mx - m_used) * p.scale_log2 > kRescaleThreshold;       // (-inf against -inf: NaN, no)
         m_used = moved ? mx : m_used;
         const uint32_t rescale = __ballot_sync(0xffffffffu, moved && j != 0);
-        const float mb = m_used * p.scale_log2 - kPromptRaise<FP16>;
+        const float mb = m_used == -INFINITY ? 0.f : m_used * p.scale_log2 - kPromptRaise<FP16>;
         const uint64_t nmb2 = pack2(-mb, -mb);
         const uint64_t l_old[2] = {l2[0], l2[1]};
         l2[0] = l2[1] = 0;
@@ -680,7 +680,7 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
           if (__builtin_expect(pend, 0)) flush_output();
         }
         if (__builtin_expect(rescale != 0u, 0)) {
-          const float corr = moved ? fast_ex2((m_old - m_used) * p.scale_log2) : 1.0f;
+          const float corr = moved ? fast_ex2((m_old - m_used) * p.scale_log2) : 1.0f;      // (from no reference: 0)
           const uint64_t corr2 = pack2(corr, corr);
           l2[0] = fadd2(fmul2(l_old[0], corr2), l2[0]);
           l2[1] = fadd2(fmul2(l_old[1], corr2), l2[1]);

@@ -17,6 +17,7 @@ from oracle import language_oracle as LO
 pytestmark = pytest.mark.gpu
 U = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
 DTYPES = [torch.bfloat16, torch.float16]
+INF, NAN = float("inf"), float("nan")
 
 
 def _rand(shape, dtype, seed, scale=1.0):
@@ -46,7 +47,41 @@ def _prompt_tol(q, mag, smax, n, vmax):
     return tol + (1.1 * n * 2.0 ** -32 * vmax + 2.0 ** -25 if q.dtype == torch.float16 else 0.0)
 
 
+def _same_where_not_finite(got, ref):
+    assert torch.equal(torch.isnan(got), torch.isnan(ref))
+    assert torch.equal(got == INF, ref == INF) and torch.equal(got == -INF, ref == -INF)
+
+
+def _check(got, q, k, v, cu_q, cu_k):
+    """All of a call's rows: the same infinities and NaN as the definition, the rest within the bound (of the finite values)."""
+    hd = q.shape[2]
+    ref, _, smax = LO.prompt_attention(q, k, v, cu_q, cu_k, hd ** -0.5)
+    tame = torch.nan_to_num(v.double(), nan=0.0, posinf=0.0, neginf=0.0)
+    mag = LO.prompt_attention(q, k, tame, cu_q, cu_k, hd ** -0.5)[1]
+    got = got.double()
+    _same_where_not_finite(got, ref)
+    fin = torch.isfinite(ref)
+    tol = _prompt_tol(q, mag, torch.nan_to_num(smax, nan=0.0, posinf=0.0), int(max(np.diff(cu_k))), float(tame.abs().max()))
+    err = (got - ref).abs()
+    assert (err[fin] <= tol[fin]).all(), float((err / tol)[fin].max())
+
+
 # ------------------------------------------------------------------------------------------------ prompts: references
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("later", [-200.0, -40.0, 3.0])
+@pytest.mark.parametrize("lead,n,ahead,cut", [(1, 200, 0, False), (80, 200, 0, False), (165, 240, 0, False), (8960, 100, 8960, True)])
+def test_prompt_first_keys_score_minus_infinity(hd, dtype, later, lead, n, ahead, cut):
+    """Keys that score -Inf do not count, however many of them come first and however small the later scores are."""
+    cu_q, cu_k = [0, n], [0, ahead + n]
+    q = torch.ones(n, 4, hd).to(dtype)
+    k = (_rand((ahead + n, 2, hd), torch.float32, 9, 0.2) + later / hd ** 0.5).to(dtype)
+    k[:lead, :, 1] = -INF
+    v = _rand((ahead + n, 2, hd), dtype, 10)
+    assert _is_cut(q, k, cu_q, cu_k) == cut
+    _check(_prompt(q, k, v, cu_q, cu_k), q, k, v, cu_q, cu_k)
+
+
 @pytest.mark.parametrize("w24", [75.5, 6.5])
 @pytest.mark.parametrize("hd,H,G,T,rows,cut", [(128, 8, 2, 20011, 20011, False), (64, 48, 6, 16009, 16009, False), (128, 4, 1, 24000, 3, True)])
 def test_prompt_one_key_in_front_of_many_equal_ones_fp16(w24, hd, H, G, T, rows, cut):
