@@ -29,8 +29,8 @@
 // of 154 steps: 167 us whole, 114 as 235 items (in 5 equal parts each, 440 items, 124 to 157: what they leave then fills L2).
 //
 // Masked keys: their scores are replaced by -inf (P exactly 0), whatever K held.  0 x Inf is not 0, so value rows behind the
-// sequence's end are cleared in shared memory, and a row whose O is not finite although its sum is (a value row that later rows of the tile
-// see, this one does not, holds Inf or NaN) is computed again by plain fp32 loops over the keys it sees.
+// sequence's end are cleared in shared memory, and elements of O that are not finite although the row's sum is (a value row that later rows of the tile
+// see, this one does not, holds Inf or NaN; or one that it sees does) are computed again by plain fp32 loops over the keys that the row sees.
 #pragma once
 #include "attention_rr.cuh"
 #include "kv_cache.cuh"
@@ -200,8 +200,9 @@ __device__ __forceinline__ void load_ordered(const float2* src, float& a, float&
   asm volatile("ld.global.v2.f32 {%0, %1}, [%2];" : "=f"(a), "=f"(b) : "l"(src) : "memory");
 }
 
-// Columns col0 .. col0 + cols - 1 of one output row again, by a whole warp (lane i: HD / 32 dims): sums over the keys that the row sees.  Only
-// elements that are not finite although every value that the row sees is are replaced.
+// Elements of columns col0 .. col0 + cols - 1 of one output row that are not finite again, by a whole warp (lane i: HD / 32 dims): from the keys that the
+// row sees alone.  A NaN among an element's values, or infinities of both signs, make it NaN; else it is the sum, to which an infinite value of a key
+// with a score above -Inf contributes itself, however small its weight is (in fp32 that may be 0, and 0 x Inf NaN).
 template <int HD, bool FP16>
 __device__ __noinline__ void prompt_repair(const PromptCommon& p, int q_row, int q_head, int kv_head, int k0, int limit, float m, float l, int col0, int cols) {
   constexpr int N = HD / 32;
@@ -210,18 +211,28 @@ __device__ __noinline__ void prompt_repair(const PromptCommon& p, int q_row, int
   const uint16_t* vp = p.v + k0 * p.ld_v + kv_head * HD + lane * N;
   const uint16_t* kp = p.k + k0 * p.ld_k + kv_head * HD + lane * N;
   float q[N], acc[N];
-  uint32_t bad = 0;
+  uint32_t bad = 0, up = 0, down = 0, nan = 0;       // bit i: element i is not finite; its values hold Inf, -Inf, NaN
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     q[i] = load16(p.q[q_row * p.ld_q + q_head * HD + lane * N + i], FP16);
     acc[i] = 0.f;
     if (lane * N + i >= col0 && lane * N + i < col0 + cols && !isfinite(load16(dst[i], FP16))) bad |= 1u << i;
   }
-  for (int j = 0; j < limit && __any_sync(0xffffffffu, bad != 0u); j += 8)
+  for (int j = 0; j < limit && __any_sync(0xffffffffu, (bad & ~nan) != 0u); j += 8) {
     for (int e = j; e < min(j + 8, limit); ++e)
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (!isfinite(load16(vp[e * p.ld_v + i], FP16))) bad &= ~(1u << i);
+      for (int i = 0; i < N; ++i) {
+        const float x = load16(vp[e * p.ld_v + i], FP16);
+        up |= (x == INFINITY ? 1u : 0u) << i;
+        down |= (x == -INFINITY ? 1u : 0u) << i;
+        nan |= (x != x ? 1u : 0u) << i;
+      }
+    nan |= up & down;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (bad & nan & (1u << i)) dst[i] = 0x7FFFu;                 // (NaN in both types)
+  bad &= ~nan;
   if (!__any_sync(0xffffffffu, bad != 0u)) return;
 #pragma unroll 4
   for (int j = 0; j < limit; ++j) {
@@ -232,7 +243,10 @@ __device__ __noinline__ void prompt_repair(const PromptCommon& p, int q_row, int
     for (int d = 16; d > 0; d /= 2) s += __shfl_xor_sync(0xffffffffu, s, d);
     const float w = fast_ex2((s - m) * p.scale_log2 + kPromptRaise<FP16>);
 #pragma unroll
-    for (int i = 0; i < N; ++i) acc[i] = fmaf(w, load16(vp[j * p.ld_v + i], FP16), acc[i]);
+    for (int i = 0; i < N; ++i) {
+      const float x = load16(vp[j * p.ld_v + i], FP16);
+      acc[i] = isfinite(x) ? fmaf(w, x, acc[i]) : s > -INFINITY ? acc[i] + x : __uint_as_float(0x7FFFFFFFu);
+    }
   }
 #pragma unroll
   for (int i = 0; i < N; ++i)

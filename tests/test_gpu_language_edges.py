@@ -66,6 +66,43 @@ def _check(got, q, k, v, cu_q, cu_k):
     assert (err[fin] <= tol[fin]).all(), float((err / tol)[fin].max())
 
 
+CHUNK = [(0, False), (9000, True)]       # keys in front of the chunk; with many the key steps are cut
+
+
+# ------------------------------------------------------------------------------------------------ prompts: seen and hidden values
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("ahead,cut", CHUNK)
+def test_prompt_seen_infinities_beside_hidden_values(hd, dtype, ahead, cut):
+    """In one tile: a row sees an infinity of its own while later rows' values hold NaN or the opposite infinity in the same column."""
+    cu_q, cu_k = [0, 200], [0, ahead + 200]
+    q, k, v = _rand((200, 4, hd), dtype, 1, 2.0), _rand((ahead + 200, 2, hd), dtype, 2), _rand((ahead + 200, 2, hd), dtype, 3)
+    t = v[ahead:]
+    t[120, 0, 3], t[140, 0, 3] = INF, NAN
+    t[110, 0, 5], t[150, 0, 5] = INF, -INF
+    t[100, 0, 7], t[130, 0, 7] = -INF, INF
+    t[125, 0, 9], t[131, 1, hd - 1], t[132, 1, hd - 1] = NAN, -INF, NAN
+    assert _is_cut(q, k, cu_q, cu_k) == cut
+    got = _prompt(q, k, v, cu_q, cu_k)
+    _check(got, q, k, v, cu_q, cu_k)
+    assert torch.equal(got.isnan(), _prompt(q, k, v, cu_q, cu_k, sm_budget=3).isnan())
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("ahead,cut", CHUNK)
+def test_prompt_infinite_value_of_a_key_that_hardly_counts(hd, dtype, ahead, cut):
+    """A weight below the smallest fp32 number times Inf is Inf; the weight of a key that scores -Inf is 0, and 0 x Inf NaN."""
+    cu_q, cu_k = [0, 150], [0, ahead + 150]
+    q = torch.full((150, 4, hd), 4.0).to(dtype)
+    k, v = _rand((ahead + 150, 2, hd), dtype, 4, 0.25), _rand((ahead + 150, 2, hd), dtype, 5)
+    at = ahead + 90
+    k[at, 0], v[at, 0, 2] = -0.8 * hd ** 0.5, INF                     # score about -3.2 hd = -205 or -410
+    k[at + 3, 1, 0], v[at + 3, 1, 4] = -INF, INF
+    assert _is_cut(q, k, cu_q, cu_k) == cut
+    _check(_prompt(q, k, v, cu_q, cu_k), q, k, v, cu_q, cu_k)
+
+
 # ------------------------------------------------------------------------------------------------ prompts: references
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("dtype", DTYPES)
