@@ -30,7 +30,7 @@
 //
 // Masked keys: their scores are replaced by -inf (P exactly 0), whatever K held.  0 x Inf is not 0, so value rows behind the
 // sequence's end are cleared in shared memory, and elements of O that are not finite although the row's sum is (a value row that later rows of the tile
-// see, this one does not, holds Inf or NaN; or one that it sees does) are computed again by plain fp32 loops over the keys that the row sees.
+// see, this one does not, holds Inf or NaN; or one that it sees does; or the sum passes the fp32 range) are computed again by plain fp32 loops over the keys that the row sees.
 #pragma once
 #include "attention_rr.cuh"
 #include "kv_cache.cuh"
@@ -202,7 +202,8 @@ __device__ __forceinline__ void load_ordered(const float2* src, float& a, float&
 
 // Elements of columns col0 .. col0 + cols - 1 of one output row that are not finite again, by a whole warp (lane i: HD / 32 dims): from the keys that the
 // row sees alone.  A NaN among an element's values, or infinities of both signs, make it NaN; else it is the sum, to which an infinite value of a key
-// with a score above -Inf contributes itself, however small its weight is (in fp32 that may be 0, and 0 x Inf NaN).
+// with a score above -Inf contributes itself, however small its weight is (in fp32 that may be 0, and 0 x Inf NaN).  The weights are divided by
+// their sum first: values near the largest number pass the fp32 range otherwise (which brings their rows here).
 template <int HD, bool FP16>
 __device__ __noinline__ void prompt_repair(const PromptCommon& p, int q_row, int q_head, int kv_head, int k0, int limit, float m, float l, int col0, int cols) {
   constexpr int N = HD / 32;
@@ -241,7 +242,7 @@ __device__ __noinline__ void prompt_repair(const PromptCommon& p, int q_row, int
     for (int i = 0; i < N; ++i) s = fmaf(q[i], load16(kp[j * p.ld_k + i], FP16), s);
 #pragma unroll
     for (int d = 16; d > 0; d /= 2) s += __shfl_xor_sync(0xffffffffu, s, d);
-    const float w = fast_ex2((s - m) * p.scale_log2 + kPromptRaise<FP16>);
+    const float w = fast_ex2((s - m) * p.scale_log2 + kPromptRaise<FP16>) / l;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float x = load16(vp[j * p.ld_v + i], FP16);
@@ -250,7 +251,7 @@ __device__ __noinline__ void prompt_repair(const PromptCommon& p, int q_row, int
   }
 #pragma unroll
   for (int i = 0; i < N; ++i)
-    if (bad & (1u << i)) dst[i] = static_cast<uint16_t>(pack_16x2<FP16>(acc[i] / l, 0.f));
+    if (bad & (1u << i)) dst[i] = static_cast<uint16_t>(pack_16x2<FP16>(acc[i], 0.f));
 }
 
 // key steps [lo, hi) of an item: of the unit, or (hi capped) of one of its tiles

@@ -103,6 +103,20 @@ def test_prompt_infinite_value_of_a_key_that_hardly_counts(hd, dtype, ahead, cut
     _check(_prompt(q, k, v, cu_q, cu_k), q, k, v, cu_q, cu_k)
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("ahead,cut", CHUNK)
+def test_prompt_values_near_the_largest_number(hd, ahead, cut):
+    """The weighted sum of the values passes the fp32 range although their mean does not."""
+    cu_q, cu_k = [0, 150], [0, ahead + 150]
+    q, k = _rand((150, 4, hd), torch.bfloat16, 6, 0.5), _rand((ahead + 150, 2, hd), torch.bfloat16, 7)
+    v = (_rand((ahead + 150, 2, hd), torch.float32, 8).sign() * 0.2 + 0.7).mul(3.3e38).bfloat16()
+    v[:, 1] = 3.0e38
+    assert _is_cut(q, k, cu_q, cu_k) == cut
+    got = _prompt(q, k, v, cu_q, cu_k)
+    assert torch.isfinite(got).all()
+    _check(got, q, k, v, cu_q, cu_k)
+
+
 # ------------------------------------------------------------------------------------------------ prompts: references
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("dtype", DTYPES)
