@@ -203,30 +203,41 @@ __device__ __forceinline__ void load_ordered(const float2* src, float& a, float&
 // Elements of columns col0 .. col0 + cols - 1 of one output row that are not finite again, by a whole warp (lane i: HD / 32 dims): from the keys that the
 // row sees alone.  A NaN among an element's values, or infinities of both signs, make it NaN; else it is the sum, to which an infinite value of a key
 // with a score above -Inf contributes itself, however small its weight is (in fp32 that may be 0, and 0 x Inf NaN).  The weights are divided by
-// their sum first: values near the largest number pass the fp32 range otherwise (which brings their rows here).
+// their sum first: values near the largest number pass the fp32 range otherwise (which brings their rows here).  No score that the row sees is NaN.
 template <int HD, bool FP16>
-__device__ __noinline__ void prompt_repair(const PromptCommon& p, int q_row, int q_head, int kv_head, int k0, int limit, float m, float l, int col0, int cols) {
+__device__ __noinline__ void prompt_repair(const PromptCommon& p, int q_row, int q_head, int kv_head, int k0, int limit, int col0, int cols) {
   constexpr int N = HD / 32;
   const int lane = threadIdx.x & 31;
   uint16_t* dst = p.out + q_row * p.ld_out + q_head * HD + lane * N;
   const uint16_t* vp = p.v + k0 * p.ld_v + kv_head * HD + lane * N;
-  const uint16_t* kp = p.k + k0 * p.ld_k + kv_head * HD + lane * N;
-  float q[N], acc[N];
+  const uint16_t* kp = p.k + k0 * p.ld_k + kv_head * HD;
+  const uint4* qp = reinterpret_cast<const uint4*>(p.q + q_row * p.ld_q + q_head * HD);
+  auto values = [&](int j, uint32_t (&x)[N / 2]) {   // a lane's dimensions of value row j, two a word
+    if constexpr (N == 4) {
+      const uint2 y = *reinterpret_cast<const uint2*>(vp + j * p.ld_v);
+      x[0] = y.x;
+      x[1] = y.y;
+    } else {
+      x[0] = *reinterpret_cast<const uint32_t*>(vp + j * p.ld_v);
+    }
+  };
+  auto element = [](const uint32_t (&x)[N / 2], int i) { return load16(static_cast<uint16_t>(i & 1 ? x[i / 2] >> 16 : x[i / 2] & 0xFFFFu), FP16); };
   uint32_t bad = 0, up = 0, down = 0, nan = 0;       // bit i: element i is not finite; its values hold Inf, -Inf, NaN
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    q[i] = load16(p.q[q_row * p.ld_q + q_head * HD + lane * N + i], FP16);
-    acc[i] = 0.f;
+  for (int i = 0; i < N; ++i)
     if (lane * N + i >= col0 && lane * N + i < col0 + cols && !isfinite(load16(dst[i], FP16))) bad |= 1u << i;
-  }
-  for (int j = 0; j < limit && __any_sync(0xffffffffu, (bad & ~nan) != 0u); j += 8) {
-    for (int e = j; e < min(j + 8, limit); ++e)
+  for (int j = 0; j < limit && __any_sync(0xffffffffu, (bad & ~nan) != 0u); j += 16) {
+    uint32_t x[16][N / 2];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) values(min(j + e, limit - 1), x[e]);
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const float x = load16(vp[e * p.ld_v + i], FP16);
-        up |= (x == INFINITY ? 1u : 0u) << i;
-        down |= (x == -INFINITY ? 1u : 0u) << i;
-        nan |= (x != x ? 1u : 0u) << i;
+        const float y = element(x[e], i);
+        up |= (y == INFINITY ? 1u : 0u) << i;
+        down |= (y == -INFINITY ? 1u : 0u) << i;
+        nan |= (y != y ? 1u : 0u) << i;
       }
     nan |= up & down;
   }
@@ -235,18 +246,57 @@ __device__ __noinline__ void prompt_repair(const PromptCommon& p, int q_row, int
     if (bad & nan & (1u << i)) dst[i] = 0x7FFFu;                 // (NaN in both types)
   bad &= ~nan;
   if (!__any_sync(0xffffffffu, bad != 0u)) return;
-#pragma unroll 4
-  for (int j = 0; j < limit; ++j) {
+  // 32 keys at a time, one a lane: scores, their maximum and the sum of the weights; then the weighted values, one dimension a lane
+  auto score = [&](int j) {
+    if (j >= limit) return -INFINITY;
+    const uint4* k4 = reinterpret_cast<const uint4*>(kp + j * p.ld_k);
     float s = 0.f;
+#pragma unroll 4
+    for (int c = 0; c < HD / 8; ++c) {
+      const uint4 a = k4[c], b = qp[c];
+      const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-    for (int i = 0; i < N; ++i) s = fmaf(q[i], load16(kp[j * p.ld_k + i], FP16), s);
+      for (int i = 0; i < 4; ++i) {
+        s = fmaf(load16(aw[i] & 0xFFFFu, FP16), load16(bw[i] & 0xFFFFu, FP16), s);
+        s = fmaf(load16(aw[i] >> 16, FP16), load16(bw[i] >> 16, FP16), s);
+      }
+    }
+    return s;
+  };
+  float m = -INFINITY, l = 0.f;
+  for (int j = lane; j < limit; j += 32) {
+    const float s = score(j), top = fmaxf(m, s);
+    if (top > -INFINITY) l = fmaf(l, fast_ex2((m - top) * p.scale_log2), fast_ex2((s - top) * p.scale_log2));
+    m = top;
+  }
+  __syncwarp();
+  float top = m;
 #pragma unroll
-    for (int d = 16; d > 0; d /= 2) s += __shfl_xor_sync(0xffffffffu, s, d);
-    const float w = fast_ex2((s - m) * p.scale_log2 + kPromptRaise<FP16>) / l;
+  for (int d = 16; d > 0; d /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+  l = m == -INFINITY ? 0.f : l * fast_ex2((m - top) * p.scale_log2);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float x = load16(vp[j * p.ld_v + i], FP16);
-      acc[i] = isfinite(x) ? fmaf(w, x, acc[i]) : s > -INFINITY ? acc[i] + x : __uint_as_float(0x7FFFFFFFu);
+  for (int d = 16; d > 0; d /= 2) l += __shfl_xor_sync(0xffffffffu, l, d);
+  float acc[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) acc[i] = 0.f;
+  for (int j = 0; j < limit; j += 32) {
+    const float s = score(j + lane), w = fast_ex2((s - top) * p.scale_log2) / l;
+    __syncwarp();
+    for (int e = 0; e < 32; e += 8) {
+      uint32_t x[8][N / 2];
+#pragma unroll
+      for (int f = 0; f < 8; ++f) values(min(j + e + f, limit - 1), x[f]);
+#pragma unroll
+      for (int f = 0; f < 8; ++f) {
+        const float wf = __shfl_sync(0xffffffffu, w, e + f), sf = __shfl_sync(0xffffffffu, s, e + f);
+        if (j + e + f < limit) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            const float y = element(x[f], i);
+            acc[i] = isfinite(y) ? fmaf(wf, y, acc[i]) : sf > -INFINITY ? acc[i] + y : __uint_as_float(0x7FFFFFFFu);
+          }
+        }
+      }
     }
   }
 #pragma unroll
@@ -301,6 +351,48 @@ struct PromptDeal {
     }
   }
 };
+
+// The second look at rows whose output holds the mark, behind a warp's last unit: a row takes as long as its keys are many, and inside the
+// pipeline the issuer's and the producer's waits, which end after a second, would run meanwhile.  The warp's units once more, 32 rows at a time.
+constexpr uint32_t kPromptMark = 0x7FFEu;          // a NaN (in both types) that no conversion gives
+template <bool FP16>
+__device__ __forceinline__ uint32_t prompt_mark(uint32_t two) {
+  constexpr uint32_t E = FP16 ? 0x7C00u : 0x7F80u;
+  if ((two & E) == E) two = (two & 0xFFFF0000u) | kPromptMark;
+  if ((two >> 16 & E) == E) two = (two & 0xFFFFu) | kPromptMark << 16;
+  return two;
+}
+__device__ __forceinline__ bool prompt_marked(uint32_t two) { return (two & 0xFFFFu) == kPromptMark || two >> 16 == kPromptMark; }
+template <int HD, bool FP16>
+__device__ __forceinline__ void prompt_repair_rows(const PromptCommon& p, bool marked, int q_row, int head, const PromptUnit& u, int limit, int col0, int cols) {
+  uint32_t todo = __ballot_sync(0xffffffffu, marked);
+  while (todo != 0u) {
+    const int src = __ffs(todo) - 1;
+    todo &= todo - 1u;
+    __syncwarp();
+    prompt_repair<HD, FP16>(p, __shfl_sync(0xffffffffu, q_row, src), __shfl_sync(0xffffffffu, head, src), u.head, u.k0, __shfl_sync(0xffffffffu, limit, src),
+                            col0, cols);
+  }
+  __syncwarp();
+}
+template <int HD, bool FP16, typename Params>
+__device__ __noinline__ void prompt_settle(const Params& p, int w, int row_tok, int row_head) {
+  int cursor = 0;
+  for (PromptDeal<Params> deal(p); deal.more(); deal.next()) {
+    PromptPart part;
+    const PromptUnit u = prompt_item<HD>(p, deal.item, cursor, part);
+    const int tok = (u.tile0 + w) * p.tile_tokens + row_tok, q_row = u.q0 + tok, head = u.head * p.group + row_head, limit = tok + 1 + u.ahead;
+    bool marked = false;
+    if (w < u.n_q && row_tok < p.tile_tokens && tok < u.len_q && limit > 0) {
+      const uint4* src = reinterpret_cast<const uint4*>(p.out + q_row * p.ld_out + head * HD);
+      for (int c = 0; c < HD / 8; ++c) {
+        const uint4 x = src[c];
+        marked = marked || prompt_marked(x.x) || prompt_marked(x.y) || prompt_marked(x.z) || prompt_marked(x.w);
+      }
+    }
+    prompt_repair_rows<HD, FP16>(p, marked, q_row, head, u, limit, 0, HD);
+  }
+}
 
 template <int HD, bool FP16, typename Params>
 __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_kernel(const __grid_constant__ Params p) {
@@ -540,6 +632,7 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
     int pend_q = -1, pend_head = 0, pend_k0 = 0, pend_limit = 0;   // query row (-1: not stored), key/value head, first key row, keys seen
     float pend_l = 1.f, pend_m = 0.f;
     int pend_slot = 0;                             // SPLIT: the part's place in the workspace
+    bool marks = false;                            // a row of this warp holds marks
     // 64 columns of O at a time: the trip to tensor memory is what a flush waits for (16 at a time: 1.6 us of a tile's beginning)
     auto load_64 = [&](uint32_t addr, uint32_t (&o)[64]) {
       __syncwarp();
@@ -590,15 +683,15 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
           }
         }
       }
-      uint32_t todo = __ballot_sync(0xffffffffu, wrong && pend_q >= 0 && pend_limit > 0 && pend_l * 0.f == 0.f);
-      while (__builtin_expect(todo != 0u, 0)) {
-        const int src = __ffs(todo) - 1;
-        todo &= todo - 1u;
-        __syncwarp();
-        prompt_repair<HD, FP16>(p, __shfl_sync(0xffffffffu, pend_q, src), __shfl_sync(0xffffffffu, pend_head * p.group + row_head, src), pend_head,
-                                pend_k0, __shfl_sync(0xffffffffu, pend_limit, src), __shfl_sync(0xffffffffu, pend_m, src),
-                                __shfl_sync(0xffffffffu, pend_l, src), 0, HD);
+      wrong = wrong && pend_q >= 0 && pend_limit > 0 && pend_l * 0.f == 0.f;
+      if (__builtin_expect(wrong, 0)) {            // (this thread's own stores: visible to it)
+#pragma unroll 1
+        for (int c = 0; c < HD / 8; ++c) {
+          const uint4 x = dst[c];
+          dst[c] = make_uint4(prompt_mark<FP16>(x.x), prompt_mark<FP16>(x.y), prompt_mark<FP16>(x.z), prompt_mark<FP16>(x.w));
+        }
       }
+      marks = marks || __any_sync(0xffffffffu, wrong);
       __syncwarp();
       pend = false;
     };
@@ -739,7 +832,12 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
       if (warp_mbar_wait(OWN_P ? &pv_done[w] : &s_full[w], (OWN_P ? n - 1u : n) & 1u, abort_flag)) {
         tc_fence_after_sync();
         flush_output();
+      } else {
+        ok = false;
       }
+    }
+    if constexpr (!SPLIT) {
+      if (__builtin_expect(marks && ok, 0)) prompt_settle<HD, FP16>(p, w, row_tok, row_head);
     }
   }
 
@@ -752,15 +850,36 @@ __global__ void __launch_bounds__(PromptCfg<HD>::kThreads, 1) prompt_attention_k
   if (threadIdx.x == 0 && *abort_flag) atomicCAS(p.status, DEV_OK, DEV_ERR_WAIT_TIMEOUT);
 }
 
+// The second look behind the joining kernel's last piece of work: there what the calls keep in registers would cost every row.
+constexpr int kPromptJoinCols = 8;
+template <int HD, bool FP16>
+__device__ __noinline__ void prompt_settle_joined(const PromptParamsSplit& p) {
+  constexpr int NWG = PromptCfg<HD>::kWg, CHUNKS = HD / kPromptJoinCols;
+  const int row = threadIdx.x & 127, row_tok = row / p.group, row_head = row - row_tok * p.group;
+  int cursor = 0;
+  for (int it = blockIdx.x * 4 + (threadIdx.x >> 7); it < p.n_units * NWG * CHUNKS; it += gridDim.x * 4) {
+    const int unit = it / (NWG * CHUNKS), w = it / CHUNKS % NWG, col0 = it % CHUNKS * kPromptJoinCols;
+    const PromptUnit u = prompt_decode<HD>(p, unit, cursor);
+    const int tok = (u.tile0 + w) * p.tile_tokens + row_tok, q_row = u.q0 + tok, head = u.head * p.group + row_head, limit = tok + 1 + u.ahead;
+    bool marked = false;
+    if (w < u.n_q && row_tok < p.tile_tokens && tok < u.len_q && limit > 0) {
+      const uint4 x = *reinterpret_cast<const uint4*>(p.out + q_row * p.ld_out + head * HD + col0);
+      marked = prompt_marked(x.x) || prompt_marked(x.y) || prompt_marked(x.z) || prompt_marked(x.w);
+    }
+    prompt_repair_rows<HD, FP16>(p, marked, q_row, head, u, limit, col0, kPromptJoinCols);
+  }
+}
+
 // The items of a unit put together, in order: 128 threads, one a row, per (unit, tile, 8 columns); a thread has the loads of 8 items in flight.
 // (A quarter of the columns each and one item after the other: 128 tokens of 32 heads behind 8000 in 12 parts 35 us instead of 28.)
 template <int HD, bool FP16>
 __global__ void __launch_bounds__(512, 1) prompt_join_kernel(const __grid_constant__ PromptParamsSplit p) {
-  constexpr int NWG = PromptCfg<HD>::kWg, COLS = 8, CHUNKS = HD / COLS, BATCH = 8;
+  constexpr int NWG = PromptCfg<HD>::kWg, COLS = kPromptJoinCols, CHUNKS = HD / COLS, BATCH = 8;
   if (p.early_launch) pdl_launch_dependents();
   pdl_wait();
   const int row = threadIdx.x & 127, row_tok = row / p.group, row_head = row - row_tok * p.group;
   int cursor = 0;
+  bool marks = false;
   for (int it = blockIdx.x * 4 + (threadIdx.x >> 7); it < p.n_units * NWG * CHUNKS; it += gridDim.x * 4) {
     const int unit = it / (NWG * CHUNKS), w = it / CHUNKS % NWG, col0 = it % CHUNKS * COLS;
     const PromptUnit u = prompt_decode<HD>(p, unit, cursor);
@@ -815,15 +934,14 @@ __global__ void __launch_bounds__(512, 1) prompt_join_kernel(const __grid_consta
       }
       if (stored) *reinterpret_cast<uint4*>(dst + i) = make_uint4(y[0], y[1], y[2], y[3]);
     }
-    uint32_t todo = __ballot_sync(0xffffffffu, wrong && stored && limit > 0 && l * 0.f == 0.f);
-    while (__builtin_expect(todo != 0u, 0)) {
-      const int src = __ffs(todo) - 1;
-      todo &= todo - 1u;
-      __syncwarp();
-      prompt_repair<HD, FP16>(p, __shfl_sync(0xffffffffu, u.q0 + tok, src), __shfl_sync(0xffffffffu, u.head * p.group + row_head, src), u.head, u.k0,
-                              __shfl_sync(0xffffffffu, limit, src), __shfl_sync(0xffffffffu, m, src), __shfl_sync(0xffffffffu, l, src), col0, COLS);
+    wrong = wrong && stored && limit > 0 && l * 0.f == 0.f;
+    if (__builtin_expect(wrong, 0)) {
+      uint4* x = reinterpret_cast<uint4*>(dst);
+      *x = make_uint4(prompt_mark<FP16>(x->x), prompt_mark<FP16>(x->y), prompt_mark<FP16>(x->z), prompt_mark<FP16>(x->w));
     }
+    marks = marks || __any_sync(0xffffffffu, wrong);
   }
+  if (__builtin_expect(marks, 0)) prompt_settle_joined<HD, FP16>(p);
 }
 
 }  // namespace eas

@@ -117,6 +117,41 @@ def test_prompt_values_near_the_largest_number(hd, ahead, cut):
     _check(got, q, k, v, cu_q, cu_k)
 
 
+@pytest.mark.parametrize("hd,dtype", [(64, torch.bfloat16), (128, torch.float16)])
+@pytest.mark.parametrize("lens", [[300, 40, 513, 1, 130], [90, 5, 260, 33, 1, 130, 77, 128, 129, 200, 64, 3]])
+def test_prompt_second_looks_in_many_units(hd, dtype, lens):
+    """Hidden NaN and infinities in every sequence and head; a CTA has one unit or many, dealt in order or by a list."""
+    cu = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    q, k, v = _rand((cu[-1], 6, hd), dtype, 20, 2.0), _rand((cu[-1], 2, hd), dtype, 21), _rand((cu[-1], 2, hd), dtype, 22)
+    for i, n in enumerate(lens):
+        for g in range(2):
+            v[cu[i] + n - 1, g, (3 * i + g) % hd] = (NAN, INF, -INF)[i % 3]
+            v[cu[i] + n // 2, g, (5 * i + 7 * g) % hd] = (INF, NAN)[(i + g) % 2]
+            k[cu[i] + n - 1, g, 1] = (1.0, NAN, INF)[i % 3]
+    got = _prompt(q, k, v, cu, cu)
+    _check(got, q, k, v, cu, cu)
+    for budget in (1, 5, 60):
+        again = _prompt(q, k, v, cu, cu, sm_budget=budget)
+        assert torch.equal(got.isnan(), again.isnan()) and torch.equal(got[~got.isnan()], again[~got.isnan()])
+
+
+def test_prompt_second_looks_that_take_longer_than_a_wait():
+    """The rows of the last tile hide a NaN from one another, and each has 600000 keys: a warp's second looks take longer than a wait
+    of the pipeline may, and its CTA has other units to do."""
+    T, hd = 600_000, 64
+    q, k, v = (_rand((T, 1, hd), torch.bfloat16, 23 + i) for i in range(3))
+    v[T - 1, 0, 5], v[T - 40, 0, 6] = NAN, INF
+    got = _prompt(q, k, v, [0, T], [0, T])
+    assert torch.isnan(got[T - 1, 0, 5]) and (got[T - 40:, 0, 6] == INF).all()
+    got[T - 1, 0, 5] = got[T - 40:, 0, 6] = 0.0
+    assert torch.isfinite(got).all()
+    for i in (T - 2, T - 41, T - 100, T - 200_000, T // 3):
+        ref, mag, smax = LO.prompt_attention(q[i:i + 1], k[:i + 1], v[:i + 1], [0, 1], [0, i + 1], hd ** -0.5)
+        err, tol = (got[i:i + 1].double() - ref).abs(), _prompt_tol(q, mag, smax, i + 1, 0.0)
+        fin = torch.isfinite(ref)
+        assert (err[fin] <= tol[fin]).all()
+
+
 # ------------------------------------------------------------------------------------------------ prompts: references
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("dtype", DTYPES)
