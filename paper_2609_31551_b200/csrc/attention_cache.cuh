@@ -360,7 +360,8 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
           qf[i][j][0] = Pair16<__half>::pack(x[4 * i] * down, x[4 * i + 2] * down);
           qf[i][j][1] = Pair16<__half>::pack(x[4 * i + 1] * down, x[4 * i + 3] * down);
         }
-        const float c = p.scale_log2 * up;                   // of column qg; this lane's scores are columns 2 qt and 2 qt + 1
+        // an infinite element makes every score Inf, -Inf or NaN, and the softmax of them NaN (of -Inf alone too: without this they would count as masked)
+        const float c = mx == INFINITY ? __uint_as_float(0x7FFFFFFFu) : p.scale_log2 * up;      // of column qg; this lane's scores are columns 2 qt and 2 qt + 1
         c_row[j][0] = __shfl_sync(0xffffffffu, c, 8 * qt);
         c_row[j][1] = __shfl_sync(0xffffffffu, c, 8 * qt + 4);
       }

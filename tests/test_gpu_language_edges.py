@@ -273,3 +273,30 @@ def test_token_value_scales_of_all_sizes_row_by_row(dtype):
     q[0, 1] *= 60.0
     q[1, 2] = 0.0
     _check_tokens(numbers, scales, q, [160, 83], table)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("H,G", [(2, 1), (12, 1)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_token_queries_that_are_not_finite(hd, H, G, dtype):
+    """Every score of such a row is Inf, -Inf or NaN, and so its softmax NaN; rows beside it and sequences without tokens do not notice."""
+    bs, lens = 16, [600, 0, 30, 2100]
+    need = [(n + bs - 1) // bs for n in lens]
+    numbers, scales = _filled(sum(need), G, bs, hd, 15)
+    numbers[0][..., 3] = numbers[0][..., 3].abs().clamp_min(1)            # a dimension in which all keys are positive
+    table = torch.zeros(len(lens), max(need), dtype=torch.int32)
+    for i, n in enumerate(need):
+        table[i, :n] = torch.arange(sum(need[:i]), sum(need[:i + 1]))
+    q = _rand((4, H, hd), dtype, 16, 2.0)
+    c = _cache(numbers, scales)
+    want = _check_tokens(numbers, scales, q, lens, table, c)
+    for at, bad in ((0, INF), (0, NAN), (3, -INF), (3, INF)):
+        for s in range(4):
+            p = q.clone()
+            p[s, 1, at] = bad
+            out = c.attention(p.cuda(), _dev(lens), table.cuda())
+            c.check()
+            ref = want.clone()
+            if lens[s]:
+                ref[s, 1] = NAN
+            assert torch.equal(out.isnan(), ref.isnan()) and torch.equal(out[~out.isnan()], ref[~out.isnan()])
