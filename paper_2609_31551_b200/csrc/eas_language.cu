@@ -224,15 +224,24 @@ static eas_status check_prompt(const eas_prompt_inputs* in) {
   return EAS_OK;
 }
 
-// scratch of a call on this device: that of its costliest launch
-static size_t prompt_workspace(const eas_prompt_inputs* in, const PromptPlan& plan, int sms) {
+// the cuts of a call's launches on this device, and its scratch: that of its costliest launch
+static size_t prompt_cuts(const eas_prompt_inputs* in, const PromptPlan& plan, int sms, std::vector<PromptCut>* cuts) {
   size_t bytes = 0;
   const int rows = static_cast<int>(plan.order.size());
   for (int first = 0; first < rows; first += kPromptMaxSeqs) {
-    const PromptCut cut = prompt_cut(in, plan, first, std::min(kPromptMaxSeqs, rows - first), sms);
-    bytes = std::max(bytes, static_cast<size_t>(cut.items) * prompt_part_bytes(plan.wg, in->head_dim));
+    cuts->push_back(prompt_cut(in, plan, first, std::min(kPromptMaxSeqs, rows - first), sms));
+    bytes = std::max(bytes, static_cast<size_t>(cuts->back().items) * prompt_part_bytes(plan.wg, in->head_dim));
   }
   return bytes;
+}
+// every launch of a call, before the first one
+static eas_status check_prompt_units(const eas_prompt_inputs* in, const PromptPlan& plan) {
+  int64_t units = 0;
+  for (size_t j = 0; j < plan.order.size(); ++j) {
+    units = (j % kPromptMaxSeqs == 0 ? 0 : units) + prompt_units(in, plan, plan.order[j]);
+    if (units > (1 << 24)) return fail(EAS_ERR_UNSUPPORTED, "too many query rows for one call");
+  }
+  return EAS_OK;
 }
 
 static eas_status prompt_attention(const eas_prompt_inputs* in, void* workspace, size_t workspace_bytes, int32_t sm_budget, void* stream,
@@ -251,6 +260,8 @@ static eas_status prompt_attention(const eas_prompt_inputs* in, void* workspace,
         (Tk > 0 && (in->ld_k < wk || in->ld_v < wk || in->ld_k % 8 != 0 || in->ld_v % 8 != 0)))
       return fail(EAS_ERR_INVALID_ARG, "token distances must be multiples of 8 that hold a token's heads");
   }
+  const PromptPlan plan = prompt_plan(in);
+  EAS_TRY(check_prompt_units(in, plan));
   int budget = 0;
   EAS_TRY(resolve_budget(sm_budget, &budget));
   if (Tq == in->cu_q[0]) return EAS_OK;                          // no query
@@ -272,10 +283,9 @@ static eas_status prompt_attention(const eas_prompt_inputs* in, void* workspace,
   pp.out_wide = (reinterpret_cast<uintptr_t>(in->out) & 31) == 0 && in->ld_out % 16 == 0;
   pp.scale_log2 = static_cast<float>(in->scale * kLog2e);
   pp.status = status_dev;
-  const PromptPlan plan = prompt_plan(in);
-  int sms = 0;
-  EAS_TRY(device_check(&sms));
-  const size_t need = prompt_workspace(in, plan, sms);
+  const int sms = g_device_sms;
+  std::vector<PromptCut> cuts;
+  const size_t need = prompt_cuts(in, plan, sms, &cuts);
   if (workspace_bytes < need || (need > 0 && workspace == nullptr))
     return fail(EAS_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace == nullptr ? 0 : workspace_bytes, need);
   if (need > 0 && (reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return fail(EAS_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
@@ -293,12 +303,11 @@ static eas_status prompt_attention(const eas_prompt_inputs* in, void* workspace,
       pp.tiles[j] = (pp.len_q[j] - 1) / pp.tile_tokens + 1;
       pp.per_head[j] = (pp.tiles[j] - 1) / plan.wg + 1;
       units += prompt_units(in, plan, i);
-      if (units > (1 << 24)) return fail(EAS_ERR_UNSUPPORTED, "too many query rows for one call");
     }
     pp.unit_prefix[pp.n_seqs] = static_cast<int>(units);
     pp.total_units = static_cast<int>(units);
     pp.by_kv = divider(G);
-    const PromptCut cut = prompt_cut(in, plan, first, pp.n_seqs, sms);
+    const PromptCut& cut = cuts[first / kPromptMaxSeqs];
     if (cut.pieces > 0) {
       PromptParamsSplit split;
       static_cast<PromptSeqs<kPromptMaxSeqs>&>(split) = pp;
@@ -517,7 +526,8 @@ extern "C" size_t eas_prompt_attention_workspace_bytes(const eas_prompt_inputs* 
   int sms = 0;
   if (check_prompt(in) != EAS_OK || device_check(&sms) != EAS_OK) return 0;
   try {
-    return prompt_workspace(in, prompt_plan(in), sms);
+    std::vector<PromptCut> cuts;
+    return prompt_cuts(in, prompt_plan(in), sms, &cuts);
   } catch (const std::bad_alloc&) {
     fail(EAS_ERR_INVALID_ARG, "out of host memory");
     return 0;

@@ -1,0 +1,25 @@
+"""CPU-only checks of the language-model operators' host side: refusals and rules that need no GPU."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+
+@pytest.fixture(scope="module")
+def lang():
+    from paper_2609_31551_b200.build import build_library
+    build_library()
+    from paper_2609_31551_b200 import language
+    language.lib()
+    return language
+
+
+@pytest.mark.parametrize("place", [0, 60, 129])
+def test_too_many_query_rows_are_refused_before_any_launch(lang, place):
+    """130 sequences take two launches, the ones with the most keys first; the one with too many rows has the fewest."""
+    lens_q, lens_k = [1] * 130, [9] * 130
+    lens_q[place], lens_k[place] = (1 << 25) + 2, 1
+    cu_q, cu_k = (np.concatenate([[0], np.cumsum(x)]).astype(np.int32) for x in (lens_q, lens_k))
+    pin = lang.PromptInputs(1 << 20, 1 << 21, 1 << 22, 1 << 23, 128 * 128, 128, 128, 128 * 128, 0, 128, 1, 128, 0.1, 130, cu_q.ctypes.data, cu_k.ctypes.data)
+    assert lang.lib().eas_prompt_attention(C.byref(pin), None, 0, 0, None, 1 << 24) == 2
+    assert b"too many query rows" in lang.lib().eas_last_error()
