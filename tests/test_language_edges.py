@@ -23,3 +23,18 @@ def test_too_many_query_rows_are_refused_before_any_launch(lang, place):
     pin = lang.PromptInputs(1 << 20, 1 << 21, 1 << 22, 1 << 23, 128 * 128, 128, 128, 128 * 128, 0, 128, 1, 128, 0.1, 130, cu_q.ctypes.data, cu_k.ctypes.data)
     assert lang.lib().eas_prompt_attention(C.byref(pin), None, 0, 0, None, 1 << 24) == 2
     assert b"too many query rows" in lang.lib().eas_last_error()
+
+
+@pytest.mark.parametrize("bad", [[0, 4.7], [0, 2 ** 31], np.array([0, 2 ** 32 + 5]), np.array([0, 2 ** 32 + 5], dtype=np.uint64), [0, float("nan")], [[0], [1, 2]], [0, None], []])
+def test_offsets_that_are_no_32_bit_numbers_are_refused(lang, bad):
+    import paper_2609_31551_b200 as P
+    for pair in ((bad, None), ([0, 5], bad)):
+        with pytest.raises(P.EasError) as e:
+            P.prompt_attention_workspace_bytes(4, 2, 64, *pair)
+        assert e.value.status == 1
+
+
+@pytest.mark.parametrize("good", [[0, 5], (0, 5), [0.0, 5.0], np.array([0, 5]), np.array([0, 9, 5], dtype=np.uint8)[::2]])
+def test_offsets_of_other_types_are_taken(lang, good):
+    x, at = lang._host_ints(good, "cu")
+    assert x.dtype == np.int32 and x.tolist() == [0, 5] and at == x.ctypes.data
