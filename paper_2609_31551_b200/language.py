@@ -242,6 +242,8 @@ class KvCache:
 
     def _move(self, call, k, v, rows, cu_seqlens, start, block_table, sm_budget, new=False):
         """new: k and v are the call's own, made for it."""
+        if len(start.shape) != 1:
+            raise B.EasError(1, "start must be a list of one place a sequence")
         n, index, dtype = start.shape[0], self._index, k.dtype
         seqs = self._seqs(block_table, n, _ints(cu_seqlens, "cu_seqlens", n + 1, index), _ints(start, "start", n, index), 0)
         if dtype not in _DTYPES:
@@ -273,6 +275,8 @@ class KvCache:
             with _on(self._index, stream):
                 return self.load(cu_seqlens, start, block_table, n_rows, dtype, out, sm_budget)
         new = out is None
+        if n_rows < 0:
+            raise B.EasError(1, f"n_rows {n_rows}")
         if new:
             shape = (n_rows, self.n_kv_heads, self.head_dim)
             out = self.k.new_empty(shape, dtype=dtype), self.k.new_empty(shape, dtype=dtype)

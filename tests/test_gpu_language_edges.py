@@ -300,3 +300,15 @@ def test_token_queries_that_are_not_finite(hd, H, G, dtype):
             if lens[s]:
                 ref[s, 1] = NAN
             assert torch.equal(out.isnan(), ref.isnan()) and torch.equal(out[~out.isnan()], ref[~out.isnan()])
+
+
+def test_row_counts_and_starts_that_make_no_sense_are_refused():
+    import paper_2609_31551_b200 as P
+    c = P.KvCache(4, 16, 2, 64)
+    x, t, cu, one = torch.zeros(3, 2, 64, dtype=torch.bfloat16, device="cuda"), _dev([[0, 1]]), _dev([0, 3]), _dev([5])
+    for call in (lambda: c.load(cu, one, t, -1), lambda: c.load(cu, one, t, -1, out=(x, x.clone())), lambda: c.load(cu, _dev(5), t, 3), lambda: c.store(x, x, cu, _dev(5), t),
+                 lambda: P.prompt_attention(x, x, x, [0, 2.5]), lambda: P.prompt_attention(x, x, x, np.array([0, 2 ** 32 + 3]))):
+        with pytest.raises(P.EasError) as e:
+            call()
+        assert e.value.status == 1
+    c.check()
