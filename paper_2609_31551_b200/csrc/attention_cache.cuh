@@ -123,7 +123,7 @@ __device__ __forceinline__ void cache_prefix(const CacheAttnParams& p, int* pref
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int s = threadIdx.x * 4 + i;
-      int n = s < p.n_seqs ? max(__ldg(p.seq_lens + s), 0) : 0;
+      int n = s < p.n_seqs ? max(p.seq_lens[s], 0) : 0;
       if (n > most) {
         n = static_cast<int>(most);
         if (report) raise_status(p.status, DEV_ERR_CACHE_RANGE);
@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
       int id = -1;
       const int tok = w.tile * TILE + lane * 16;
       if (lane < MT && more(w) && tok < w.len) {
-        id = __ldg(w.ids + (tok >> p.c.bs_log2));
+        id = w.ids[tok >> p.c.bs_log2];
         if (static_cast<uint32_t>(id) >= static_cast<uint32_t>(p.c.n_blocks)) {
           raise_status(p.status, DEV_ERR_CACHE_RANGE);
           id = -1;
@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
       float2 sc = make_float2(0.f, 0.f);
       if (id >= 0) {
         const long long at = static_cast<long long>(id) * p.c.n_kv + w.kvh;
-        sc = make_float2(__ldg(p.c.k_scale + at), __ldg(p.c.v_scale + at));
+        sc = make_float2(p.c.k_scale[at], p.c.v_scale[at]);
       }
       return sc;
     };

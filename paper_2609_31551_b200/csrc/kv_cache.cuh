@@ -13,6 +13,8 @@ namespace eas {
 enum : uint32_t { DEV_ERR_CACHE_RANGE = 3 };     // a block number or a place outside the cache
 constexpr float kCacheMinScale = 7.888609052210118e-31f;   // 2^-100: blocks of zeros, and no division by a subnormal scale
 
+// Tables, lengths, starts and scales are read by ordinary loads: an earlier kernel may still be writing them when this one starts, and a load of the
+// read-only path promises that nobody does while the kernel runs, so that nothing keeps it behind the wait for that kernel.
 struct CacheView {
   int8_t *k, *v;
   float *k_scale, *v_scale;
@@ -68,7 +70,7 @@ struct CacheRun {         // the part of a sequence's rows that lies in one bloc
 __device__ __forceinline__ CacheRun cache_run(const CacheRowsParams& p, int pair, bool report) {
   CacheRun r;
   r.block = -1;
-  auto cu = [&](int i) { return min(max(__ldg(p.s.cu + i), 0), p.n_rows); };
+  auto cu = [&](int i) { return min(max(p.s.cu[i], 0), p.n_rows); };
   int lo = 0, hi = p.s.n_seqs - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -76,7 +78,7 @@ __device__ __forceinline__ CacheRun cache_run(const CacheRowsParams& p, int pair
   }
   const int c0 = cu(lo), len = cu(lo + 1) - c0, j = pair - ((c0 >> p.c.bs_log2) + 2 * lo);
   if (len <= 0 || j < 0) return r;
-  const long long at = __ldg(p.s.start + lo), end = at + len;
+  const long long at = p.s.start[lo], end = at + len;
   if (at < 0) {
     if (report && j == 0) raise_status(p.status, DEV_ERR_CACHE_RANGE);
     return r;
@@ -84,7 +86,7 @@ __device__ __forceinline__ CacheRun cache_run(const CacheRowsParams& p, int pair
   const long long b = (at >> p.c.bs_log2) + j, b0 = b << p.c.bs_log2;
   if (b0 >= end) return r;
   int block = -1;
-  if (b < p.s.max_blocks) block = __ldg(p.s.table + lo * p.s.ld_table + b);
+  if (b < p.s.max_blocks) block = p.s.table[lo * p.s.ld_table + b];
   if (block < 0 || block >= p.c.n_blocks) {
     if (report) raise_status(p.status, DEV_ERR_CACHE_RANGE);
     return r;
@@ -249,7 +251,7 @@ __global__ void __launch_bounds__(512, 1) cache_load_kernel(const __grid_constan
   constexpr int kChunks = HD / 8, kBatch = 4;                    // 8 values each; 128 chunks of a row at a time
   const int lane = threadIdx.x & 31, row_chunks = p.c.n_kv * kChunks;
   const int warps = gridDim.x * (blockDim.x >> 5), me = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-  auto cu = [&](int i) { return min(max(__ldg(p.s.cu + i), 0), p.n_rows); };
+  auto cu = [&](int i) { return min(max(p.s.cu[i], 0), p.n_rows); };
   const int begin = static_cast<int>(static_cast<long long>(p.n_rows) * me / warps);
   const int end = static_cast<int>(static_cast<long long>(p.n_rows) * (me + 1) / warps);
   if (begin >= end) return;
@@ -265,10 +267,10 @@ __global__ void __launch_bounds__(512, 1) cache_load_kernel(const __grid_constan
       ++row;
       continue;
     }
-    const long long at = __ldg(p.s.start + s) + static_cast<long long>(row - first), b = at >> p.c.bs_log2;
+    const long long at = p.s.start[s] + static_cast<long long>(row - first), b = at >> p.c.bs_log2;
     const int place = static_cast<int>(at) & ((1 << p.c.bs_log2) - 1), n = min(next - row, (1 << p.c.bs_log2) - place);
     int block = -1;
-    if (at >= 0 && b < p.s.max_blocks) block = __ldg(p.s.table + s * p.s.ld_table + b);
+    if (at >= 0 && b < p.s.max_blocks) block = p.s.table[s * p.s.ld_table + b];
     if (block < 0 || block >= p.c.n_blocks) {
       if (lane == 0) raise_status(p.status, DEV_ERR_CACHE_RANGE);
       row += n;

@@ -312,3 +312,28 @@ def test_row_counts_and_starts_that_make_no_sense_are_refused():
             call()
         assert e.value.status == 1
     c.check()
+
+
+def test_token_and_store_calls_follow_one_another_without_a_pause():
+    """Each store grows the scale of a block that the attention behind it reads, and nothing waits between them on the host."""
+    import paper_2609_31551_b200 as P
+    G, H, hd, bs, n, steps = 16, 32, 128, 16, 40, 64
+    blocks = (steps + bs - 1) // bs
+    table = torch.arange(n * blocks, dtype=torch.int32).view(n, blocks).cuda()
+    rows = [(_rand((n, G, hd), torch.bfloat16, 500 + t, 1.0 + t).cuda(), _rand((n, G, hd), torch.bfloat16, 700 + t, 1.0 + t).cuda()) for t in range(steps)]
+    q, cu = _rand((n, H, hd), torch.bfloat16, 24).cuda(), _dev(np.arange(n + 1))
+    at, lens = [_dev([t] * n) for t in range(steps)], [_dev([t + 1] * n) for t in range(steps)]
+    seen = []
+    for paused in (True, False):
+        c = P.KvCache(n * blocks, bs, G, hd)
+        outs = []
+        for t in range(steps):
+            c.store(rows[t][0], rows[t][1], cu, at[t], table)
+            if paused:
+                torch.cuda.synchronize()
+            outs.append(c.attention(q, lens[t], table))
+            if paused:
+                torch.cuda.synchronize()
+        c.check()
+        seen.append(torch.stack(outs))
+    assert torch.equal(seen[0], seen[1])

@@ -38,3 +38,13 @@ def test_offsets_that_are_no_32_bit_numbers_are_refused(lang, bad):
 def test_offsets_of_other_types_are_taken(lang, good):
     x, at = lang._host_ints(good, "cu")
     assert x.dtype == np.int32 and x.tolist() == [0, 5] and at == x.ctypes.data
+
+
+@pytest.mark.parametrize("name", ["kv_cache.cuh", "attention_cache.cuh", "attention_prompt.cuh"])
+def test_kernels_read_what_earlier_kernels_write_by_ordered_loads(name):
+    """A kernel may start before the one in front of it has ended; only loads that are not of the read-only path stay behind its wait."""
+    import os
+    import re
+    import paper_2609_31551_b200 as P
+    src = re.sub(r"//.*", "", open(os.path.join(os.path.dirname(P.__file__), "csrc", name)).read())
+    assert not re.search(r"__ldg\b|ld\.global\.nc|__restrict__", src)
