@@ -1,5 +1,9 @@
 """CPU-only checks of the language-model operators' host side: refusals and rules that need no GPU."""
 import ctypes as C
+import os
+import re
+import shutil
+import time
 
 import numpy as np
 import pytest
@@ -43,8 +47,32 @@ def test_offsets_of_other_types_are_taken(lang, good):
 @pytest.mark.parametrize("name", ["kv_cache.cuh", "attention_cache.cuh", "attention_prompt.cuh"])
 def test_kernels_read_what_earlier_kernels_write_by_ordered_loads(name):
     """A kernel may start before the one in front of it has ended; only loads that are not of the read-only path stay behind its wait."""
-    import os
-    import re
     import paper_2609_31551_b200 as P
     src = re.sub(r"//.*", "", open(os.path.join(os.path.dirname(P.__file__), "csrc", name)).read())
     assert not re.search(r"__ldg\b|ld\.global\.nc|__restrict__", src)
+
+
+def test_objects_are_made_again_when_the_flags_change(tmp_path, monkeypatch):
+    from paper_2609_31551_b200 import build
+    (tmp_path / "csrc").mkdir()
+    (tmp_path / "include").mkdir()
+    (tmp_path / "csrc" / "one.cpp").write_text('extern "C" int answer() { return ANSWER; }\n')
+    (tmp_path / "csrc" / "two.cpp").write_text('extern "C" int two() { return 2; }\n')
+    monkeypatch.setattr(build, "HERE", str(tmp_path / "csrc"))
+    monkeypatch.setattr(build, "CSRC", str(tmp_path / "csrc"))
+    monkeypatch.setattr(build, "SOURCES", ["one.cpp", "two.cpp"])
+    ran, run = [], build._run
+    monkeypatch.setattr(build, "_run", lambda cmd: ran.append(cmd) or run(cmd))
+    (tmp_path / "lib").mkdir()
+    monkeypatch.setattr(build, "LIB_PATH", str(tmp_path / "lib" / "lib.so"))
+    for i, (answer, compiled) in enumerate(((41, 2), (41, 0), (42, 2), (42, 0))):
+        monkeypatch.setattr(build, "NVCC_FLAGS", ["-O1", "-std=c++17", "-Xcompiler", "-fPIC", f"-DANSWER={answer}"])
+        ran.clear()
+        path = build.build_library()
+        assert sum("-c" in cmd for cmd in ran) == compiled
+        assert C.CDLL(shutil.copy(path, tmp_path / f"copy{i}.so")).answer() == answer      # (a copy: a library that is loaded is not loaded again)
+    (tmp_path / "csrc" / "two.cpp").write_text('extern "C" int two() { return 3; }\n')
+    os.utime(tmp_path / "csrc" / "two.cpp", (time.time() + 5, time.time() + 5))
+    ran.clear()
+    build.build_library()
+    assert sum("-c" in cmd for cmd in ran) == 1
