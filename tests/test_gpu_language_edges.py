@@ -302,6 +302,23 @@ def test_token_queries_that_are_not_finite(hd, H, G, dtype):
             assert torch.equal(out.isnan(), ref.isnan()) and torch.equal(out[~out.isnan()], ref[~out.isnan()])
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("H,G", [(32, 1), (64, 1), (71, 1), (66, 2), (16, 1)])
+def test_token_many_heads_a_group(hd, dtype, H, G):
+    bs, lens = 32, [700, 1, 0, 4100]
+    need = [(n + bs - 1) // bs for n in lens]
+    numbers, scales = _filled(sum(need) + 1, G, bs, hd, 17)
+    perm = torch.randperm(sum(need) + 1, generator=torch.Generator().manual_seed(18)).to(torch.int32)
+    table = torch.full((len(lens), max(need)), 10 ** 6, dtype=torch.int32)
+    for i, n in enumerate(need):
+        table[i, :n] = perm[sum(need[:i]):sum(need[:i + 1])]
+    q = _rand((len(lens), H, hd), dtype, 19, 2.0)
+    c = _cache(numbers, scales)
+    out = _check_tokens(numbers, scales, q, lens, table, c)
+    assert torch.equal(out, c.attention(q.cuda(), _dev(lens), table.cuda(), sm_budget=41))
+
+
 def test_row_counts_and_starts_that_make_no_sense_are_refused():
     import paper_2609_31551_b200 as P
     c = P.KvCache(4, 16, 2, 64)
