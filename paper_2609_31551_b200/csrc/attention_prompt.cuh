@@ -200,56 +200,74 @@ __device__ __forceinline__ void load_ordered(const float2* src, float& a, float&
   asm volatile("ld.global.v2.f32 {%0, %1}, [%2];" : "=f"(a), "=f"(b) : "l"(src) : "memory");
 }
 
-// Elements of columns col0 .. col0 + cols - 1 of one output row that are not finite again, by a whole warp (lane i: HD / 32 dims): from the keys that the
-// row sees alone.  A NaN among an element's values, or infinities of both signs, make it NaN; else it is the sum, to which an infinite value of a key
-// with a score above -Inf contributes itself, however small its weight is (in fp32 that may be 0, and 0 x Inf NaN).  The weights are divided by
-// their sum first: values near the largest number pass the fp32 range otherwise (which brings their rows here).  No score that the row sees is NaN.
+// The second look at output elements that are not finite although their row's scores are numbers: from the keys that the row sees alone.  A NaN among an
+// element's values, or infinities of both signs, make it NaN; an infinite value makes it that infinity, however small the weight (in fp32 it may be
+// 0, and 0 x Inf NaN); else it is the sum.  A warp looks: lane i has HD / 32 dimensions of the row.
 template <int HD, bool FP16>
-__device__ __noinline__ void prompt_repair(const PromptCommon& p, int q_row, int q_head, int kv_head, int k0, int limit, int col0, int cols) {
-  constexpr int N = HD / 32;
-  const int lane = threadIdx.x & 31;
-  uint16_t* dst = p.out + q_row * p.ld_out + q_head * HD + lane * N;
-  const uint16_t* vp = p.v + k0 * p.ld_v + kv_head * HD + lane * N;
-  const uint16_t* kp = p.k + k0 * p.ld_k + kv_head * HD;
-  const uint4* qp = reinterpret_cast<const uint4*>(p.q + q_row * p.ld_q + q_head * HD);
-  auto values = [&](int j, uint32_t (&x)[N / 2]) {   // a lane's dimensions of value row j, two a word
+struct PromptLook {
+  static constexpr int N = HD / 32;
+  const uint16_t *kp, *vp;         // first key's row of the head; the lane's dimensions of the first value row
+  long long ld_k, ld_v;
+  __device__ __forceinline__ PromptLook(const PromptCommon& p, int kv_head, int k0)
+      : kp(p.k + k0 * p.ld_k + kv_head * HD), vp(p.v + k0 * p.ld_v + kv_head * HD + (threadIdx.x & 31) * N), ld_k(p.ld_k), ld_v(p.ld_v) {}
+  __device__ __forceinline__ void values(int j, uint32_t (&x)[N / 2]) const {      // two a word
     if constexpr (N == 4) {
-      const uint2 y = *reinterpret_cast<const uint2*>(vp + j * p.ld_v);
+      const uint2 y = *reinterpret_cast<const uint2*>(vp + j * ld_v);
       x[0] = y.x;
       x[1] = y.y;
     } else {
-      x[0] = *reinterpret_cast<const uint32_t*>(vp + j * p.ld_v);
+      x[0] = *reinterpret_cast<const uint32_t*>(vp + j * ld_v);
     }
-  };
-  auto element = [](const uint32_t (&x)[N / 2], int i) { return load16(static_cast<uint16_t>(i & 1 ? x[i / 2] >> 16 : x[i / 2] & 0xFFFFu), FP16); };
-  uint32_t bad = 0, up = 0, down = 0, nan = 0;       // bit i: element i is not finite; its values hold Inf, -Inf, NaN
+  }
+  static __device__ __forceinline__ float element(const uint32_t (&x)[N / 2], int i) {
+    return load16(static_cast<uint16_t>(i & 1 ? x[i / 2] >> 16 : x[i / 2] & 0xFFFFu), FP16);
+  }
+};
+// What the value rows of some keys hold, bit i for dimension i of the lane.  odd: a key with an infinite value has elements that are not finite itself, so
+// that its score may be -Inf and its weight 0 in earnest (the same in all lanes).
+struct PromptFound {
+  uint32_t up = 0, down = 0, nan = 0;      // Inf, -Inf, NaN (or infinities of both signs)
+  bool odd = false;
+};
+template <int HD, bool FP16>
+__device__ __noinline__ PromptFound prompt_scan(const PromptLook<HD, FP16> look, int from, int to, uint32_t cared, PromptFound f) {
+  constexpr int N = HD / 32;
+  for (int j = from; j < to && __any_sync(0xffffffffu, (cared & ~f.nan) != 0u); j += 16) {
+    uint32_t x[16][N / 2], up = 0, down = 0;
 #pragma unroll
-  for (int i = 0; i < N; ++i)
-    if (lane * N + i >= col0 && lane * N + i < col0 + cols && !isfinite(load16(dst[i], FP16))) bad |= 1u << i;
-  for (int j = 0; j < limit && __any_sync(0xffffffffu, (bad & ~nan) != 0u); j += 16) {
-    uint32_t x[16][N / 2];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) values(min(j + e, limit - 1), x[e]);
+    for (int e = 0; e < 16; ++e) look.values(min(j + e, to - 1), x[e]);
 #pragma unroll
     for (int e = 0; e < 16; ++e)
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const float y = element(x[e], i);
+        const float y = look.element(x[e], i);
         up |= (y == INFINITY ? 1u : 0u) << i;
         down |= (y == -INFINITY ? 1u : 0u) << i;
-        nan |= (y != y ? 1u : 0u) << i;
+        f.nan |= (y != y ? 1u : 0u) << i;
       }
-    nan |= up & down;
-  }
+    f.up |= up;
+    f.down |= down;
+    f.nan |= f.up & f.down;
+    if (!f.odd && __any_sync(0xffffffffu, ((up | down) & cared & ~f.nan) != 0u)) {
+      bool odd = false;
+      for (int e = j; e < min(j + 16, to); ++e)                  // (all keys of the batch: Inf is rare)
 #pragma unroll
-  for (int i = 0; i < N; ++i)
-    if (bad & nan & (1u << i)) dst[i] = 0x7FFFu;                 // (NaN in both types)
-  bad &= ~nan;
-  if (!__any_sync(0xffffffffu, bad != 0u)) return;
-  // 32 keys at a time, one a lane: scores, their maximum and the sum of the weights; then the weighted values, one dimension a lane
+        for (int i = 0; i < N; ++i) odd = odd || !isfinite(load16(look.kp[e * look.ld_k + (threadIdx.x & 31) * N + i], FP16));
+      f.odd = __any_sync(0xffffffffu, odd);
+    }
+  }
+  return f;
+}
+// The sums of one row's elements `bad`: weights divided by their sum before they meet values, since values near the largest number pass the fp32 range
+// otherwise (which brings their rows here).  An infinite value counts as itself where its key's score is above -Inf.
+template <int HD, bool FP16>
+__device__ __noinline__ void prompt_sums(const PromptCommon& p, const PromptLook<HD, FP16> look, const uint4* qp, uint16_t* dst, int limit, uint32_t bad) {
+  constexpr int N = HD / 32;
+  const int lane = threadIdx.x & 31;
+  // 32 keys at a time, one a lane: scores, their maximum and the sum of the weights; then the weighted values
   auto score = [&](int j) {
     if (j >= limit) return -INFINITY;
-    const uint4* k4 = reinterpret_cast<const uint4*>(kp + j * p.ld_k);
+    const uint4* k4 = reinterpret_cast<const uint4*>(look.kp + j * look.ld_k);
     float s = 0.f;
 #pragma unroll 4
     for (int c = 0; c < HD / 8; ++c) {
@@ -285,14 +303,14 @@ __device__ __noinline__ void prompt_repair(const PromptCommon& p, int q_row, int
     for (int e = 0; e < 32; e += 8) {
       uint32_t x[8][N / 2];
 #pragma unroll
-      for (int f = 0; f < 8; ++f) values(min(j + e + f, limit - 1), x[f]);
+      for (int f = 0; f < 8; ++f) look.values(min(j + e + f, limit - 1), x[f]);
 #pragma unroll
       for (int f = 0; f < 8; ++f) {
         const float wf = __shfl_sync(0xffffffffu, w, e + f), sf = __shfl_sync(0xffffffffu, s, e + f);
         if (j + e + f < limit) {
 #pragma unroll
           for (int i = 0; i < N; ++i) {
-            const float y = element(x[f], i);
+            const float y = look.element(x[f], i);
             acc[i] = isfinite(y) ? fmaf(wf, y, acc[i]) : sf > -INFINITY ? acc[i] + y : __uint_as_float(0x7FFFFFFFu);
           }
         }
@@ -302,6 +320,46 @@ __device__ __noinline__ void prompt_repair(const PromptCommon& p, int q_row, int
 #pragma unroll
   for (int i = 0; i < N; ++i)
     if (bad & (1u << i)) dst[i] = static_cast<uint16_t>(pack_16x2<FP16>(acc[i], 0.f));
+}
+// Columns col0 .. col0 + cols - 1 of up to 32 rows of one head, a lane's own (q_row, head, limit) where `marked`: the values that all of them see are
+// looked through once, those that follow for each row.
+template <int HD, bool FP16>
+__device__ __forceinline__ void prompt_repair_rows(const PromptCommon& p, bool marked, int q_row, int head, int kv_head, int k0, int limit, int col0, int cols) {
+  constexpr int N = HD / 32;
+  const uint32_t rows = __ballot_sync(0xffffffffu, marked);
+  if (rows == 0u) return;
+  const int lane = threadIdx.x & 31, common = __reduce_min_sync(0xffffffffu, marked ? limit : 0x7fffffff);
+  const PromptLook<HD, FP16> look(p, kv_head, k0);
+  auto row_of = [&](int src) {
+    return p.out + __shfl_sync(0xffffffffu, q_row, src) * p.ld_out + __shfl_sync(0xffffffffu, head, src) * HD + lane * N;
+  };
+  auto bad_of = [&](const uint16_t* dst) {
+    uint32_t bad = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (lane * N + i >= col0 && lane * N + i < col0 + cols && !isfinite(load16(dst[i], FP16))) bad |= 1u << i;
+    return bad;
+  };
+  uint32_t cared = 0;
+  for (uint32_t todo = rows; todo != 0u; todo &= todo - 1u) cared |= bad_of(row_of(__ffs(todo) - 1));
+  const PromptFound shared = prompt_scan<HD, FP16>(look, 0, common, cared, PromptFound{});
+  for (uint32_t todo = rows; todo != 0u; todo &= todo - 1u) {
+    const int src = __ffs(todo) - 1, seen = __shfl_sync(0xffffffffu, limit, src);
+    uint16_t* dst = row_of(src);
+    uint32_t bad = bad_of(dst);
+    const PromptFound f = prompt_scan<HD, FP16>(look, common, seen, bad, shared);
+    constexpr uint16_t kInf = FP16 ? 0x7C00 : 0x7F80, kNan = 0x7FFF;
+    const uint32_t settled = bad & (f.nan | (f.odd ? 0u : f.up | f.down));
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (settled & (1u << i)) dst[i] = f.nan & (1u << i) ? kNan : f.up & (1u << i) ? kInf : static_cast<uint16_t>(kInf | 0x8000);
+    bad &= ~settled;
+    if (__any_sync(0xffffffffu, bad != 0u)) {
+      const uint4* qp = reinterpret_cast<const uint4*>(p.q + __shfl_sync(0xffffffffu, q_row, src) * p.ld_q + __shfl_sync(0xffffffffu, head, src) * HD);
+      prompt_sums<HD, FP16>(p, look, qp, dst, seen, bad);
+    }
+    __syncwarp();
+  }
 }
 
 // key steps [lo, hi) of an item: of the unit, or (hi capped) of one of its tiles
@@ -363,18 +421,6 @@ __device__ __forceinline__ uint32_t prompt_mark(uint32_t two) {
   return two;
 }
 __device__ __forceinline__ bool prompt_marked(uint32_t two) { return (two & 0xFFFFu) == kPromptMark || two >> 16 == kPromptMark; }
-template <int HD, bool FP16>
-__device__ __forceinline__ void prompt_repair_rows(const PromptCommon& p, bool marked, int q_row, int head, const PromptUnit& u, int limit, int col0, int cols) {
-  uint32_t todo = __ballot_sync(0xffffffffu, marked);
-  while (todo != 0u) {
-    const int src = __ffs(todo) - 1;
-    todo &= todo - 1u;
-    __syncwarp();
-    prompt_repair<HD, FP16>(p, __shfl_sync(0xffffffffu, q_row, src), __shfl_sync(0xffffffffu, head, src), u.head, u.k0, __shfl_sync(0xffffffffu, limit, src),
-                            col0, cols);
-  }
-  __syncwarp();
-}
 template <int HD, bool FP16, typename Params>
 __device__ __noinline__ void prompt_settle(const Params& p, int w, int row_tok, int row_head) {
   int cursor = 0;
@@ -390,7 +436,7 @@ __device__ __noinline__ void prompt_settle(const Params& p, int w, int row_tok, 
         marked = marked || prompt_marked(x.x) || prompt_marked(x.y) || prompt_marked(x.z) || prompt_marked(x.w);
       }
     }
-    prompt_repair_rows<HD, FP16>(p, marked, q_row, head, u, limit, 0, HD);
+    prompt_repair_rows<HD, FP16>(p, marked, q_row, head, u.head, u.k0, limit, 0, HD);
   }
 }
 
@@ -866,7 +912,7 @@ __device__ __noinline__ void prompt_settle_joined(const PromptParamsSplit& p) {
       const uint4 x = *reinterpret_cast<const uint4*>(p.out + q_row * p.ld_out + head * HD + col0);
       marked = prompt_marked(x.x) || prompt_marked(x.y) || prompt_marked(x.z) || prompt_marked(x.w);
     }
-    prompt_repair_rows<HD, FP16>(p, marked, q_row, head, u, limit, col0, kPromptJoinCols);
+    prompt_repair_rows<HD, FP16>(p, marked, q_row, head, u.head, u.k0, limit, col0, kPromptJoinCols);
   }
 }
 

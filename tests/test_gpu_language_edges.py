@@ -354,3 +354,74 @@ def test_token_and_store_calls_follow_one_another_without_a_pause():
         c.check()
         seen.append(torch.stack(outs))
     assert torch.equal(seen[0], seen[1])
+
+
+# ------------------------------------------------------------------------------------------------ calls at the end of what is allowed
+@pytest.mark.parametrize("hd", [64, 128])
+def test_prompt_without_any_key_gives_zeros(hd):
+    import paper_2609_31551_b200 as P
+    q = _rand((40, 4, hd), torch.bfloat16, 25)
+    k = torch.zeros(0, 2, hd, dtype=torch.bfloat16)
+    out = torch.full((40, 4, hd), 7.0, dtype=torch.bfloat16, device="cuda")
+    got, status = P.prompt_attention(q.cuda(), k.cuda(), k.cuda(), [1, 30, 39], [0, 0, 0], out=out)
+    assert int(status[0]) == 0 and not got[1:39].any() and (got[0] == 7).all() and (got[39] == 7).all()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_prompt_of_two_launches_that_are_both_cut(hd):
+    """More sequences than a launch holds: both launches leave their parts in one workspace."""
+    import paper_2609_31551_b200 as P
+    lens, keys = [1 + i % 3 for i in range(140)], [3500 - 7 * i for i in range(140)]
+    keys[77] = 40000
+    cu_q, cu_k = (np.concatenate([[0], np.cumsum(x)]).astype(np.int32) for x in (lens, keys))
+    q = _rand((cu_q[-1], 2, hd), torch.float16, 26, 2.0)
+    k, v = _rand((cu_k[-1], 1, hd), torch.float16, 27), _rand((cu_k[-1], 1, hd), torch.float16, 28)
+    order = sorted(range(140), key=lambda i: -keys[i])
+    for part in (order[:128], order[128:]):
+        assert P.prompt_attention_workspace_bytes(2, 1, hd, *(np.concatenate([[0], np.cumsum([x[i] for i in part])]) for x in (lens, keys))) > 0
+    _check(_prompt(q, k, v, cu_q, cu_k), q, k, v, cu_q, cu_k)
+
+
+def test_cache_calls_about_nothing():
+    import paper_2609_31551_b200 as P
+    numbers, scales = _filled(3, 2, 16, 64, 29)
+    c = _cache(numbers, scales)
+    x, q = torch.zeros(0, 2, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(0, 4, 64, dtype=torch.bfloat16, device="cuda")
+    none, table = torch.zeros(0, dtype=torch.int32, device="cuda"), torch.zeros(0, 5, dtype=torch.int32, device="cuda")
+    c.store(x, x, _dev([0]), none, table)
+    assert c.load(_dev([0]), none, table, 0)[0].shape == (0, 2, 64) and c.attention(q, none, table).shape == (0, 4, 64)
+    no_blocks = torch.zeros(2, 0, dtype=torch.int32, device="cuda")
+    q = _rand((2, 4, 64), torch.bfloat16, 30).cuda()
+    assert not c.attention(q, _dev([0, 0]), no_blocks).any()
+    c.store(x, x, _dev([0, 0, 0]), _dev([0, 5]), no_blocks)
+    c.check()
+    assert not c.attention(q, _dev([0, 3]), no_blocks).any()
+    with pytest.raises(P.EasError) as e:
+        c.check()
+    assert e.value.status == 7
+    assert torch.equal(c.k.cpu(), numbers[0]) and torch.equal(c.v_scale.cpu(), scales[1])
+
+
+def test_cut_prompt_captured_and_replayed():
+    import paper_2609_31551_b200 as P
+    cu_q, cu_k = [0, 60, 61], [0, 4000, 4100]
+    q, k, v = _rand((61, 16, 128), torch.bfloat16, 31).cuda(), _rand((4100, 4, 128), torch.bfloat16, 32).cuda(), _rand((4100, 4, 128), torch.bfloat16, 33).cuda()
+    ws = torch.empty(P.prompt_attention_workspace_bytes(16, 4, 128, cu_q, cu_k), dtype=torch.uint8, device="cuda")
+    P.prompt_attention(q, k, v, cu_q, cu_k)
+    torch.cuda.synchronize()
+    graphs = []
+    for space in (ws, ws, None):                                        # two on one workspace, one with its own
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out, status = P.prompt_attention(q, k, v, cu_q, cu_k, workspace=space)
+        graphs.append((g, out, status))
+    for i in range(3):
+        q.copy_(q.flip(1))
+        v.copy_(v.flip(0))
+        want = P.prompt_attention(q, k, v, cu_q, cu_k)[0]
+        ws.fill_(0xFF)
+        for g, out, status in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for g, out, status in graphs:
+            assert torch.equal(out, want) and int(status[0]) == 0
