@@ -29,7 +29,9 @@ enum { EAS_DTYPE_BF16 = 0, EAS_DTYPE_FP16 = 1 };
  * keys: query i sees keys 0 .. i + (keys - queries).  (cu_k = cu_q: whole prompts.  More keys than queries: a chunk of a
  * prompt behind a prefix.  Fewer: the first queries see nothing; their output rows are 0.)
  *   out = softmax(scale * q k^T) v,  fp32 inside; probabilities are rounded to the data type before they meet v.
- * A row reads nothing it does not see: Inf or NaN in keys and values behind it, or in other sequences, does not reach it. */
+ * A row reads nothing it does not see: Inf or NaN in keys and values behind it, or in other sequences, does not reach it.  What it does see counts
+ * as in the formula: a key that scores -Inf has weight 0, a score of Inf or NaN, or -Inf alone, makes the row NaN, and an infinite value its element
+ * (NaN with one of the other sign, with NaN, or where its key has weight 0).  Rows with such elements are looked at a second time, slowly. */
 typedef struct {
   const void* q;       /* device [cu_q[n_seqs], n_heads * head_dim], distance ld_q */
   const void* k;       /* device [cu_k[n_seqs], n_kv_heads * head_dim], distance ld_k */
@@ -52,7 +54,7 @@ size_t eas_prompt_attention_workspace_bytes(const eas_prompt_inputs* in);
 /* workspace: device, 256-byte aligned, of that size (NULL where it is 0); its contents do not matter, and nothing of it is used by a later
  * call, but calls that may run at the same time need one each.  status_dev: device uint32 (caller zeroes it) that the kernel raises to 1 when a
  * bounded wait expires.
- * Errors (nothing launched): INVALID_ARG, UNSUPPORTED (head_dim, dtype, heads per key/value head), WORKSPACE, ARCH, CUDA. */
+ * Errors (nothing launched): INVALID_ARG, UNSUPPORTED (head_dim, dtype, heads per key/value head, more than 2^24 units of query rows), WORKSPACE, ARCH, CUDA. */
 eas_status eas_prompt_attention(const eas_prompt_inputs* in, void* workspace, size_t workspace_bytes, int32_t sm_budget, void* stream,
                                 uint32_t* status_dev);
 
@@ -103,7 +105,8 @@ eas_status eas_cache_load(const eas_cache* cache, const eas_cache_seqs* seqs, vo
                           int32_t n_rows, int32_t dtype, int32_t sm_budget, void* stream, uint32_t* status_dev);
 
 /* out[s] = softmax(scale * q[s] k^T) v over places 0 .. seq_lens[s] - 1 of sequence s: one token per sequence.  A sequence
- * of length 0 (or less) gets 0.  workspace: device scratch of eas_cache_attention_workspace_bytes() (0 on bad arguments), 256-byte
+ * of length 0 (or less) gets 0, a query with Inf or NaN in it NaN.  Inside, the query is fp16 times a power of two (elements below 2^-24 of its
+ * largest are lost) and the weights are rounded to fp16, 2^-32 of the largest at the finest; sums are fp32.  workspace: device scratch of eas_cache_attention_workspace_bytes() (0 on bad arguments), 256-byte
  * aligned; its contents do not matter and nothing of it is used by a later call, but calls that may run at the same time need one each. */
 size_t eas_cache_attention_workspace_bytes(const eas_cache* cache, int32_t n_seqs, int32_t n_heads);
 eas_status eas_cache_attention(const eas_cache* cache, const eas_cache_seqs* seqs, const void* q, int64_t ld_q, void* out, int64_t ld_out,

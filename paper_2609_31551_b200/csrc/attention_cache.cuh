@@ -21,9 +21,12 @@
 // that holds a whole row writes its output.  What is cut leaves (m, l, O): the warps of a CTA, whose pieces are neighbours, put together what
 // they hold of one row that goes on behind them, and cache_join_kernel the CTAs' parts and the row's end, all in the order of the pieces.
 //
-// Measured, without the joining launch: 8 caches of 24000 to 65536 tokens (64 heads, 8 of keys and values, of 128) 108 us, 93 % of the copy rate;
-// 48 of up to 8192 (32 and 8 heads of 128) 17, of them 9 for the bytes and the rest the chain from the lengths to the first tile; 128 of 500 to 3500
-// (16 heads of 64, one query head each) 88, 70 %: 900 instructions a tile of 64 tokens, three warps a scheduler.  The join adds 2 us.
+// More than 16 query heads a key/value head are rows of tiles of their own, so the cache is read once for every 16 of them, from L2 where it fits:
+// 8 caches of 16384 tokens with 2 key/value heads of 128 take 20 us for 8 query heads each, 24 for 12 or 16, 36 for 32, 60 for 64.
+//
+// Measured, back to back in a graph, both launches: 8 caches of 24000 to 65536 tokens (64 heads, 8 of keys and values, of 128) 109 us, 93 % of the copy rate (113
+// to 121 among other calls); 48 of up to 8192 (32 and 8 heads of 128) 19.5, of them 9 for the bytes and the rest the chain from the lengths to the first
+// tile; 128 of 500 to 3500 (16 heads of 64, one query head each) 90, 69 %: 900 instructions a tile of 64 tokens, three warps a scheduler.  The join is 2 us of it.
 #pragma once
 #include "kv_cache.cuh"
 #include "ptx.cuh"
@@ -351,7 +354,8 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
         for (int i = 0; i < HD / 4; ++i) mx = fmaxf(mx, fabsf(x[i]));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-        // the largest of the row to [1, 4): exponent e with 2^e <= mx (126 at most, so that 2^-e is a normal number)
+        // the largest of the row to [1, 2): exponent e with 2^e <= mx (-126 to 126, so that 2^e and 2^-e are normal numbers: a subnormal row stays below 1,
+        // one from 2^127 on below 4)
         const int e = mx > 0.f ? min(max(static_cast<int>(__float_as_uint(mx) >> 23) - 127, -126), 126) : 0;
         const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
         const float up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);

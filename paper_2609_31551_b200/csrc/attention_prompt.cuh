@@ -14,23 +14,25 @@
 //
 // The pipeline is that of attention_rr.cuh, whose figures gave the split: what counts is the number of tiles in flight, and tensor
 // memory holds 3 x (80 + 64) or 2 x (80 + 40 + 128) columns.  At head_dim 128 a step of a tile costs the tensor pipe 640 cycles and
-// the special-function unit 640, so neither can wait for the other.
+// the special-function unit 640, and takes some 1150 with two tiles in flight (1.17 us for both; each pipe 46 % busy): what bounds short runs is a
+// tile's chain from scores to P to O, and long ones the power cap.  At head_dim 64 a step of three tiles costs the unit 1920 cycles and the tensor pipe 960.
+// 16411 tokens (32 and 8 heads of 128) 1670-1710 us, 76-78 % of the rate of a library product in short runs; 8192 tokens of 16 and 4 heads of 64 205 us, 40 %.
 //
 // The reference maximum only moves when the row maximum grows by more than 2^8 in the exponent; then the thread rescales
 // its O row in TMEM.  Scores, sums and O are fp32; P is rounded to the data type (bf16 or fp16: what the matrix product takes), and the
 // output once at the end.  In fp16 P is 2^7 times what the reference gives (at most 2^15; fp16 ends at 65504), in the sum too: weights
 // below 2^-21 of the reference instead of 2^-14 lose bits (20000 keys of 6.5 2^-24 each behind one that holds the rest were off by 7.7 %).
-// A row's arithmetic depends on its own sequence alone, not on the unit, the packing or the SMs.
-//
-// Few rows against many keys (a chunk of a prompt behind a long prefix) make fewer units than there are SMs.  SPLIT lays the key steps of all
+// A row's arithmetic depends on its own sequence alone, not on the unit, the packing or the SMs, unless the call is cut:
+// few rows against many keys (a chunk of a prompt behind a long prefix) make fewer units than there are SMs.  SPLIT lays the key steps of all
 // units end to end and cuts the line into one equal piece per SM: a piece is a few work items (the end of a unit, whole units, the beginning of
-// one), each of which leaves (m, l, O) in the workspace, fp32, and prompt_join_kernel puts a unit's items together in order.  The cut
-// follows from the call's shapes and the device, not from sm_budget.  512 queries of 40 heads (8 key/value heads of 128) behind 11801 keys, 88 units
+// one), each of which leaves (m, l, O) in the workspace, fp32, and prompt_join_kernel puts a unit's items together in order.  The cut, and with it a
+// row's last bits, follow from the call's shapes and the device, not from sm_budget.  512 queries of 40 heads (8 key/value heads of 128) behind 11801 keys, 88 units
 // of 154 steps: 167 us whole, 114 as 235 items (in 5 equal parts each, 440 items, 124 to 157: what they leave then fills L2).
 //
 // Masked keys: their scores are replaced by -inf (P exactly 0), whatever K held.  0 x Inf is not 0, so value rows behind the
 // sequence's end are cleared in shared memory, and elements of O that are not finite although the row's sum is (a value row that later rows of the tile
-// see, this one does not, holds Inf or NaN; or one that it sees does; or the sum passes the fp32 range) are computed again by plain fp32 loops over the keys that the row sees.
+// see, this one does not, holds Inf or NaN; or one that it sees does; or the sum passes the fp32 range) are looked at again, from the values that the row
+// sees alone (prompt_settle).  8192 tokens with an infinity at token 100 then take 2 to 7 ms instead of 0.3, at token 7000 33 to 48.
 #pragma once
 #include "attention_rr.cuh"
 #include "kv_cache.cuh"

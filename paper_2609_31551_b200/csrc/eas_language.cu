@@ -88,7 +88,7 @@ static int64_t prompt_unit_steps(int64_t len_q, int64_t len_k, int64_t tiles, in
   return (std::max<int64_t>(seen, 0) + keys - 1) / keys;
 }
 // Into how many pieces the line of key steps of sequences order[first .. first + n) is cut (0: it is not, units are dealt whole), and the number of
-// items.  Costs in key steps of a unit (1.2 us at head_dim 128), fitted to calls on both sides: the busiest SM's steps, kUnitSteps a whole unit and
+// items.  Costs in key steps of a unit (1.2 us), fitted to calls of head_dim 128 on both sides: the busiest SM's steps, kUnitSteps a whole unit and
 // kItemSteps an item for its beginning and end and its way through L2, kJoinSteps for the joining launch.  Only for calls of at most kSplitUnits units
 // an SM with long key ranges, where the deal leaves SMs without work.
 constexpr int kSplitUnits = 4, kSplitLeastSteps = 24, kPieceLeastSteps = 8;
@@ -150,8 +150,9 @@ static void prompt_items(PromptParamsSplit& pp, const PromptCut& cut, int wg) {
 }
 // The units of a launch by cost, costliest first (a counting sort over their key steps), each to the CTA of `grid` with the least to do so far.  The
 // CTAs' loads are small whole numbers, so those with the same load form a list, and the least load only grows.  (Dealt in rounds of alternating
-// direction instead, costliest first: 8 prompts of 1 to 1563 tokens of head_dim 128 53 instead of 49 us, 10 of 3 to 1000 29 instead of 25.5, of head_dim 64 22.9
-// instead of 24.0.  The host takes 5 ns a unit for it.)
+// direction instead, costliest first: 8 prompts of 1 to 1563 tokens of head_dim 128 53 instead of 49 us, 10 of 3 to 1000 29 instead of 25.5.  Of head_dim 64,
+// 13 mixes: 1.5 to 25 % more in nine of them, the 8 prompts 42.7 instead of 36.4, one of 1500 beside thirty of 20 33.7 instead of 31.2; 1 % less in four, the 10
+// prompts 23.1 instead of 23.4.  The host takes 9 ns a unit for the list, 4 in rounds: 280 units 2.5 us instead of 1.0, which calls that wait for the host pay.)
 static void prompt_list(PromptParams& pp, int wg, int grid) {
   std::vector<int> count;
   auto steps = [&](int s, int back) {
