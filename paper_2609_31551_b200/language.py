@@ -115,15 +115,23 @@ def _on(index, stream):
         yield
 
 
+def _whole(x, name):
+    if x.dtype.kind != "f" or not (np.isfinite(x) & (x == np.floor(x)) & (np.abs(x) < 2 ** 53)).all():
+        raise B.EasError(1, f"{name} must be whole numbers of 32 bits")
+    return x.astype(np.int64)
+
+
 def _host_ints(x, name):
     if type(x) is not np.ndarray or x.dtype != np.int32 or not x.flags.c_contiguous:
         try:
-            x = np.asarray(x)
+            given = np.asarray(x)
         except (TypeError, ValueError, RuntimeError) as e:
             raise B.EasError(1, f"{name}: {e}") from None
-        if x.dtype.kind not in "biuf" or (x.size and not (-2 ** 31 <= x.min() <= x.max() < 2 ** 31 and (x == np.floor(x)).all())):
-            raise B.EasError(1, f"{name} must be whole numbers of 32 bits")          # (a conversion would cut them off)
-        x = np.ascontiguousarray(x, dtype=np.int32)
+        if given.dtype.kind not in "biu":
+            given = _whole(given, name)
+        x = np.ascontiguousarray(given, dtype=np.int32)
+        if np.count_nonzero(x != given):
+            raise B.EasError(1, f"{name} must be whole numbers of 32 bits")          # (the conversion cut them off)
     if x.ndim != 1 or x.size < 1:
         raise B.EasError(1, f"{name} must be a list of at least one offset")
     return x, x.__array_interface__["data"][0]

@@ -29,7 +29,7 @@ def test_too_many_query_rows_are_refused_before_any_launch(lang, place):
     assert b"too many query rows" in lang.lib().eas_last_error()
 
 
-@pytest.mark.parametrize("bad", [[0, 4.7], [0, 2 ** 31], np.array([0, 2 ** 32 + 5]), np.array([0, 2 ** 32 + 5], dtype=np.uint64), [0, float("nan")], [[0], [1, 2]], [0, None], []])
+@pytest.mark.parametrize("bad", [[0, 4.7], [0, 2 ** 31], np.array([0, 2 ** 32 + 5]), np.array([0, 2 ** 32 + 5], dtype=np.uint64), [0, float("nan")], [0, 1e30], ["0", "5"], [[0], [1, 2]], [0, None], []])
 def test_offsets_that_are_no_32_bit_numbers_are_refused(lang, bad):
     import paper_2609_31551_b200 as P
     for pair in ((bad, None), ([0, 5], bad)):
