@@ -275,6 +275,21 @@ def test_token_value_scales_of_all_sizes_row_by_row(dtype):
     _check_tokens(numbers, scales, q, [160, 83], table)
 
 
+@pytest.mark.parametrize("hd,H,G", [(64, 4, 4), (128, 8, 1), (128, 12, 1)])
+@pytest.mark.parametrize("scale", [2.6e36, 2.0 ** -100])
+def test_token_value_scales_at_the_ends_of_their_range(hd, H, G, scale):
+    """Values of up to 3.3e38, and the smallest scale that a store leaves."""
+    bs, lens = 32, [5000, 17, 0, 9000]
+    need = [(n + bs - 1) // bs for n in lens]
+    numbers, scales = _filled(sum(need), G, bs, hd, 34)
+    scales[1].fill_(scale)
+    table = torch.zeros(len(lens), max(need), dtype=torch.int32)
+    for i, n in enumerate(need):
+        table[i, :n] = torch.arange(sum(need[:i]), sum(need[:i + 1]))
+    out = _check_tokens(numbers, scales, _rand((len(lens), H, hd), torch.bfloat16, 35, 2.0), lens, table)
+    assert float(out.abs().max()) > scale
+
+
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("H,G", [(2, 1), (12, 1)])
 @pytest.mark.parametrize("dtype", DTYPES)
