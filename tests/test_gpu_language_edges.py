@@ -440,3 +440,39 @@ def test_cut_prompt_captured_and_replayed():
         torch.cuda.synchronize()
         for g, out, status in graphs:
             assert torch.equal(out, want) and int(status[0]) == 0
+
+
+def test_decoding_steps_captured_once_and_replayed():
+    """A step of a server in one graph: rows stored at the lengths, the lengths raised, attention over them, and the rows read back."""
+    import paper_2609_31551_b200 as P
+    G, H, hd, bs, n, steps = 4, 16, 64, 16, 5, 40
+    blocks = (steps + 30 + bs - 1) // bs
+    table = torch.randperm(n * blocks, generator=torch.Generator().manual_seed(36)).to(torch.int32).view(n, blocks).cuda()
+    first = _dev([0, 3, 16, 29, 30])
+    cu, cu_all = _dev(np.arange(n + 1)), _dev([0, 20, 20, 20, 20, 20])
+    rows = [[_rand((n, h, hd), torch.float16, 800 + 3 * t + i, 1.0 + 0.1 * t).cuda() for i, h in enumerate((H, G, G))] for t in range(steps)]
+    caches = [P.KvCache(n * blocks, bs, G, hd) for _ in range(2)]
+
+    def step(c, q, k, v, lens):
+        c.store(k, v, cu, lens, table)
+        lens.add_(1)
+        out = c.attention(q, lens, table)
+        return out, *c.load(cu_all, first.new_zeros(n), table, 20, dtype=torch.float16)
+    lens, want = first.clone(), []
+    for t in range(steps):
+        want.append([x.clone() for x in step(caches[0], *rows[t], lens)])
+    caches[0].check()
+    held, live = [x.clone() for x in rows[0]], first.clone()
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        outs = step(caches[1], *held, live)
+    live.copy_(first)
+    for t in range(steps):
+        for x, y in zip(held, rows[t]):
+            x.copy_(y)
+        g.replay()
+        for x, y in zip(outs, want[t]):
+            assert torch.equal(x, y)
+    caches[1].check()
+    assert torch.equal(caches[0].k, caches[1].k) and torch.equal(caches[0].v_scale, caches[1].v_scale) and torch.equal(live, lens)
