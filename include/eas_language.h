@@ -4,7 +4,7 @@
  * The paper co-locates the Encode stage with the prefill (and decode) workers of its language model (Section 3.4: the
  * encoder gets a share of the SMs, the neighbour the rest).  These are the attention operators of those
  * neighbours: causal attention of packed prompts, an 8-bit paged key/value cache that prompts and single tokens are written
- * to, and the attention of single tokens over it.  They follow the conventions of eas_encoder.h: caller-owned memory, an
+ * to, the attention of single tokens and of several new tokens a sequence over it, and rotary positions, alone and on the way into the cache.  They follow the conventions of eas_encoder.h: caller-owned memory, an
  * eas_status and eas_last_error(), work enqueued on `stream`, at most `sm_budget` SMs (0 = all), the same bytes for any
  * sm_budget.  All pointers are on the device that is current at the call.
  *
@@ -112,6 +112,61 @@ size_t eas_cache_attention_workspace_bytes(const eas_cache* cache, int32_t n_seq
 eas_status eas_cache_attention(const eas_cache* cache, const eas_cache_seqs* seqs, const void* q, int64_t ld_q, void* out, int64_t ld_out,
                                int32_t n_heads, int32_t dtype, float scale, void* workspace, size_t workspace_bytes,
                                int32_t sm_budget, void* stream, uint32_t* status_dev);
+
+/* ---- attention of several new tokens a sequence over the cache ----
+ * Rows cu_seqlens[s] .. cu_seqlens[s+1] - 1 of q are the LAST tokens among places 0 .. seq_lens[s] - 1 of sequence s (their keys and values stored before): the
+ * next chunk of a prompt, a draft to be verified, single tokens between them.  Row i of n sees places 0 .. i + seq_lens[s] - n; a row that sees nothing (a sequence
+ * shorter than its chunk, or of length 0 or less) gets 0, and rows that cu_seqlens does not name are left alone.  out = softmax(scale * q k^T) v with the types of
+ * eas_cache_attention.  Of `seqs` it takes cu_seqlens and seq_lens; they are read when the call's work runs.
+ * n_rows: rows of q that exist (a bound on cu_seqlens).  max_new: the most new tokens that a sequence has (n_rows does, too; a smaller number chooses
+ * kernels for few rows): a sequence with more is not computed and raises the status word to EAS_DEVICE_CACHE_RANGE.
+ * workspace: device scratch of eas_cache_chunk_workspace_bytes() (0 on bad arguments), 256-byte aligned; its contents do not matter and nothing of it is used
+ * by a later call, but calls that may run at the same time need one each. */
+size_t eas_cache_chunk_workspace_bytes(const eas_cache* cache, int32_t n_seqs, int32_t n_rows, int32_t max_new, int32_t n_heads);
+eas_status eas_cache_chunk_attention(const eas_cache* cache, const eas_cache_seqs* seqs, const void* q, int64_t ld_q, void* out, int64_t ld_out,
+                                     int32_t n_rows, int32_t max_new, int32_t n_heads, int32_t dtype, float scale, void* workspace, size_t workspace_bytes,
+                                     int32_t sm_budget, void* stream, uint32_t* status_dev);
+
+/* ---- rotary positions with several axes ----
+ * The first rotary_dim dimensions of a head are pairs; pair i turns by angle = position * inv_freq[i], the token's position along axis[i]:
+ *   a' = scale (a cos angle - b sin angle),  b' = scale (b cos angle + a sin angle);  the other dimensions stay as they are.
+ * One axis for text; time, height and width for the embeddings of images and clips.  Angles are exact to 2^-32 turns for every 32-bit position; the arithmetic is fp32. */
+enum { EAS_ROTARY_HALVES = 0,      /* pair i: dimensions i and i + rotary_dim / 2 */
+       EAS_ROTARY_NEIGHBOURS = 1   /* dimensions 2 i and 2 i + 1 */ };
+typedef struct {
+  int32_t head_dim;       /* 64 or 128 */
+  int32_t rotary_dim;     /* a multiple of 16, at most head_dim */
+  int32_t pairing;        /* EAS_ROTARY_* */
+  int32_t n_axes;         /* 1 .. 4 */
+  const double* inv_freq; /* host [rotary_dim / 2], radians a position, finite */
+  const int32_t* axis;    /* host [rotary_dim / 2], 0 .. n_axes - 1 (NULL: all 0) */
+  float scale;            /* > 0, finite; 1 as a rule */
+} eas_rotary_desc;
+
+typedef struct eas_rotary eas_rotary; /* opaque: the frequencies; host memory only, good for any device */
+eas_status eas_rotary_create(const eas_rotary_desc* desc, eas_rotary** out);
+void eas_rotary_destroy(eas_rotary* rotary);
+
+typedef struct {
+  const void* q;          /* device [n_rows, n_heads * head_dim], distance ld_q; NULL with n_heads 0 */
+  const void* k;          /* device [n_rows, n_kv_heads * head_dim], distance ld_k; NULL with n_kv_heads 0 */
+  void* out_q;            /* as q, as k: the same address and distance (in place), or memory that overlaps no input */
+  void* out_k;
+  int64_t ld_q, ld_k, ld_out_q, ld_out_k;
+  const int32_t* positions; /* device [n_axes][n_rows], distance ld_positions */
+  int64_t ld_positions;
+  int32_t n_rows, n_heads, n_kv_heads, dtype;
+  int32_t inverse;        /* 1: by -angle, which takes the rotation back; times scale, the gradient's way through it */
+} eas_rotary_inputs;
+
+/* out = rotated q and k, rounded once to the data type.  Errors (nothing launched): INVALID_ARG, UNSUPPORTED, ARCH, CUDA. */
+eas_status eas_rotary_apply(const eas_rotary* rotary, const eas_rotary_inputs* in, int32_t sm_budget, void* stream);
+
+/* eas_cache_store of the rotated keys and the values, and the rotated queries to out_q (n_heads 0: none), in one launch.  The keys are rotated in fp32 and
+ * rounded once, to their number in the cache.  in: k [n_rows, n_kv_heads of the cache], out_k NULL, inverse 0; positions NULL: a token's place in its sequence,
+ * along every axis.  Queries of rows that cu_seqlens does not name are left alone; those whose key has no place in the cache are written all the same. */
+eas_status eas_cache_append(const eas_cache* cache, const eas_cache_seqs* seqs, const eas_rotary* rotary, const eas_rotary_inputs* in, const void* v, int64_t ld_v,
+                            int32_t sm_budget, void* stream, uint32_t* status_dev);
 
 #ifdef __cplusplus
 }

@@ -80,3 +80,39 @@ def cache_attention(q, k_numbers, v_numbers, k_scales, v_scales, seq_lens, table
         for h in range(H):
             out[s, h], mag[s, h], smax[s, h] = attend(q[s, h], k[:, h * G // H], v[:, h * G // H], scale)
     return out, mag, smax
+
+
+def chunk_attention(q, k_numbers, v_numbers, k_scales, v_scales, cu, seq_lens, table, scale):
+    """q [rows, H, hd]: rows cu[s] .. cu[s + 1] - 1 are the last tokens among the first seq_lens[s] of sequence s.  -> out, attention over |v| and the
+    largest absolute score sum, as prompt_attention; rows of no sequence are NaN."""
+    H, G = q.shape[1], k_numbers.shape[1]
+    q = q.to(F64)
+    out, mag = torch.full_like(q, float("nan")), torch.full_like(q, float("nan"))
+    smax = torch.zeros(q.shape[:2], dtype=F64)
+    for s in range(len(cu) - 1):
+        a, b, n = int(cu[s]), int(cu[s + 1]), max(int(seq_lens[s]), 0)
+        k, v = cache_values(k_numbers, k_scales, table[s], n), cache_values(v_numbers, v_scales, table[s], n)
+        seen = torch.arange(b - a) + 1 + n - (b - a)
+        hidden = torch.arange(n)[None] >= seen[:, None]
+        for h in range(H):
+            g = h * G // H
+            x = (q[a:b, h] @ k[:, g].T * scale).masked_fill(hidden, -float("inf"))
+            p = torch.where((seen > 0)[:, None], torch.softmax(x, dim=1), 0.0) if n else x
+            out[a:b, h], mag[a:b, h] = p @ v[:, g], p @ v[:, g].abs()
+            if n and b > a:
+                smax[a:b, h] = (q[a:b, h].abs() @ k[:, g].abs().T).amax(1) * scale
+    return out, mag, smax
+
+
+def rotate(x, positions, axis, inv_freq, neighbours=False, scale=1.0, inverse=False):
+    """x [rows, heads, hd], positions [n_axes][rows], axis and inv_freq [pairs] -> fp64.  Angles in extended precision: a position of 2^31 times a
+    frequency has bits that fp64 drops."""
+    y = x.to(F64).numpy().copy()
+    n = len(inv_freq)
+    for i in range(n):
+        a, b = (2 * i, 2 * i + 1) if neighbours else (i, i + n)
+        angle = np.asarray(positions[axis[i]]).astype(np.longdouble) * np.longdouble(inv_freq[i]) * (-1 if inverse else 1)
+        c, s = (scale * f(angle).astype(np.float64)[:, None] for f in (np.cos, np.sin))
+        u, w = x[:, :, a].to(F64).numpy(), x[:, :, b].to(F64).numpy()
+        y[:, :, a], y[:, :, b] = u * c - w * s, w * c + u * s
+    return torch.from_numpy(y)

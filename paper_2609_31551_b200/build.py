@@ -7,7 +7,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libeas_encoder.so")
-SOURCES = ["eas_encoder.cu", "eas_language.cu", "serving_host.cpp"]
+SOURCES = ["eas_encoder.cu", "eas_language.cu", "eas_rotary.cu", "eas_chunk.cu", "serving_host.cpp"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-Xcompiler", "-fPIC"]
 
 

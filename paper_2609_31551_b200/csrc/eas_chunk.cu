@@ -1,0 +1,57 @@
+// C ABI of the attention of several new tokens a sequence over the cache (include/eas_language.h): checks and launches.
+#include <algorithm>
+#include <cmath>
+
+#include "attention_chunk.cuh"
+#include "cache_handle.cuh"
+
+using namespace eas;
+
+static size_t chunk_workspace(const eas_cache* c, int32_t n_seqs, int32_t n_rows, int32_t max_new, int32_t n_heads) { return 256; }
+
+static eas_status chunk_attention(const eas_cache* c, const eas_cache_seqs* s, const void* q, int64_t ld_q, void* out, int64_t ld_out, int32_t n_rows,
+                                  int32_t max_new, int32_t n_heads, int32_t dtype, float scale, void* workspace, size_t workspace_bytes, int32_t sm_budget,
+                                  void* stream, uint32_t* status_dev) {
+  int budget = 0;
+  EAS_TRY(check_cache_call(c, s, false, dtype, status_dev, sm_budget, &budget));
+  const int G = c->d.n_kv_heads, hd = c->d.head_dim;
+  if (s->n_seqs > 0 && s->cu_seqlens == nullptr) return fail(EAS_ERR_INVALID_ARG, "a required pointer is null");
+  if (n_heads <= 0 || n_heads % G != 0) return fail(EAS_ERR_INVALID_ARG, "%d query heads for %d key/value heads", n_heads, G);
+  if (n_rows < 0 || max_new < 0) return fail(EAS_ERR_INVALID_ARG, "n_rows %d, max_new %d", n_rows, max_new);
+  if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(EAS_ERR_INVALID_ARG, "scale must be positive and finite");
+  if (s->n_seqs == 0 || n_rows == 0) return EAS_OK;
+  if (q == nullptr || out == nullptr || workspace == nullptr) return fail(EAS_ERR_INVALID_ARG, "a required pointer is null");
+  if (!aligned16(q) || !aligned16(out)) return fail(EAS_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
+  const int64_t w = static_cast<int64_t>(n_heads) * hd;
+  if (ld_q < w || ld_out < w || ld_q % 8 != 0 || ld_out % 8 != 0)
+    return fail(EAS_ERR_INVALID_ARG, "token distances must be multiples of 8 that hold a token's heads");
+  const size_t need = chunk_workspace(c, s->n_seqs, n_rows, max_new, n_heads);
+  if (workspace_bytes < need) return fail(EAS_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, need);
+  if ((reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return fail(EAS_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
+  if (static_cast<int64_t>(s->max_blocks) * c->d.block_size > 0x7fffffffLL) return fail(EAS_ERR_UNSUPPORTED, "max_blocks %d is too large", s->max_blocks);
+  ChunkParams p{};
+  p.c = view_of(c);
+  p.table = s->block_table; p.cu = s->cu_seqlens; p.seq_lens = s->seq_lens;
+  p.ld_table = s->ld_table; p.n_seqs = s->n_seqs; p.max_blocks = s->max_blocks; p.n_rows = n_rows; p.max_new = max_new;
+  p.q = static_cast<const uint16_t*>(q); p.out = static_cast<uint16_t*>(out);
+  p.ld_q = ld_q; p.ld_out = ld_out; p.fp16 = dtype == EAS_DTYPE_FP16; p.group = n_heads / G;
+  p.scale_log2 = static_cast<float>(scale * kLog2e);
+  p.status = status_dev;
+  const int grid = static_cast<int>(std::min<int64_t>(static_cast<int64_t>(n_rows) * n_heads, budget == c->sm_count ? 8 * budget : budget));
+  return hd == 64 ? launch_kernel(chunk_simple_kernel<64>, grid, 128, 0, static_cast<cudaStream_t>(stream), p)
+                  : launch_kernel(chunk_simple_kernel<128>, grid, 128, 0, static_cast<cudaStream_t>(stream), p);
+}
+
+extern "C" size_t eas_cache_chunk_workspace_bytes(const eas_cache* cache, int32_t n_seqs, int32_t n_rows, int32_t max_new, int32_t n_heads) {
+  if (cache == nullptr || n_seqs < 0 || n_rows < 0 || max_new < 0 || n_heads <= 0 || n_heads % cache->d.n_kv_heads != 0) {
+    fail(EAS_ERR_INVALID_ARG, "bad arguments");
+    return 0;
+  }
+  return chunk_workspace(cache, n_seqs, n_rows, max_new, n_heads);
+}
+
+extern "C" eas_status eas_cache_chunk_attention(const eas_cache* cache, const eas_cache_seqs* seqs, const void* q, int64_t ld_q, void* out, int64_t ld_out,
+                                                int32_t n_rows, int32_t max_new, int32_t n_heads, int32_t dtype, float scale, void* workspace,
+                                                size_t workspace_bytes, int32_t sm_budget, void* stream, uint32_t* status_dev) {
+  return chunk_attention(cache, seqs, q, ld_q, out, ld_out, n_rows, max_new, n_heads, dtype, scale, workspace, workspace_bytes, sm_budget, stream, status_dev);
+}

@@ -66,36 +66,43 @@ struct CacheRun {         // the part of a sequence's rows that lies in one bloc
   int block;              // -1: none
   int lo, hi;             // places in the block
   int row;                // row of place lo
+  int place;              // place lo in the sequence
 };
-__device__ __forceinline__ CacheRun cache_run(const CacheRowsParams& p, int pair, bool report) {
+// pair number `pair`, of sequence seq
+__device__ __forceinline__ CacheRun cache_run_of(const CacheView& c, const CacheSeqs& sq, int seq, int n_rows, int pair, uint32_t* status, bool report) {
   CacheRun r;
   r.block = -1;
+  auto cu = [&](int i) { return min(max(sq.cu[i], 0), n_rows); };
+  const int c0 = cu(seq), len = cu(seq + 1) - c0, j = pair - ((c0 >> c.bs_log2) + 2 * seq);
+  if (len <= 0 || j < 0) return r;
+  const long long at = sq.start[seq], end = at + len;
+  if (at < 0) {
+    if (report && j == 0) raise_status(status, DEV_ERR_CACHE_RANGE);
+    return r;
+  }
+  const long long b = (at >> c.bs_log2) + j, b0 = b << c.bs_log2;
+  if (b0 >= end) return r;
+  int block = -1;
+  if (b < sq.max_blocks) block = sq.table[seq * sq.ld_table + b];
+  if (block < 0 || block >= c.n_blocks) {
+    if (report) raise_status(status, DEV_ERR_CACHE_RANGE);
+    return r;
+  }
+  r.block = block;
+  r.lo = static_cast<int>(max(at - b0, 0LL));
+  r.hi = static_cast<int>(min(end - b0, 1LL << c.bs_log2));
+  r.row = c0 + static_cast<int>(b0 + r.lo - at);
+  r.place = static_cast<int>(b0 + r.lo);
+  return r;
+}
+__device__ __forceinline__ CacheRun cache_run(const CacheRowsParams& p, int pair, bool report) {
   auto cu = [&](int i) { return min(max(p.s.cu[i], 0), p.n_rows); };
   int lo = 0, hi = p.s.n_seqs - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if ((cu(mid) >> p.c.bs_log2) + 2 * mid <= pair) lo = mid; else hi = mid - 1;
   }
-  const int c0 = cu(lo), len = cu(lo + 1) - c0, j = pair - ((c0 >> p.c.bs_log2) + 2 * lo);
-  if (len <= 0 || j < 0) return r;
-  const long long at = p.s.start[lo], end = at + len;
-  if (at < 0) {
-    if (report && j == 0) raise_status(p.status, DEV_ERR_CACHE_RANGE);
-    return r;
-  }
-  const long long b = (at >> p.c.bs_log2) + j, b0 = b << p.c.bs_log2;
-  if (b0 >= end) return r;
-  int block = -1;
-  if (b < p.s.max_blocks) block = p.s.table[lo * p.s.ld_table + b];
-  if (block < 0 || block >= p.c.n_blocks) {
-    if (report) raise_status(p.status, DEV_ERR_CACHE_RANGE);
-    return r;
-  }
-  r.block = block;
-  r.lo = static_cast<int>(max(at - b0, 0LL));
-  r.hi = static_cast<int>(min(end - b0, 1LL << p.c.bs_log2));
-  r.row = c0 + static_cast<int>(b0 + r.lo - at);
-  return r;
+  return cache_run_of(p.c, p.s, lo, p.n_rows, pair, p.status, report);
 }
 
 // The nearest integer to x / s (ties to even) in the low byte.  x * inv is off by a few 2^-24 relative, so its floor k is right or one
@@ -145,6 +152,38 @@ __device__ __forceinline__ uint32_t requantise(int q, float old, float s, float 
   return __float_as_uint(n + 12582912.0f);
 }
 
+// The scale of a block and head whose new values are at most `largest` in magnitude, the lo tokens that it has already having the scale `old`; where it
+// grows, GT threads round those again.  (NaN: Inf or NaN among the values, the block and head reads as NaN.)
+template <int HD, int GT>
+__device__ __forceinline__ float cache_block_scale(float largest, float old, int lo, int8_t* dst, int tid) {
+  float s = __fdiv_rn(largest, 127.0f);
+  if (s < kCacheMinScale) s = kCacheMinScale;
+  if (!(s * 0.0f == 0.0f)) s = __uint_as_float(0x7FFFFFFFu);
+  if (lo > 0) {
+    if (!(s <= old) && old == old) {                             // the scale grows (or stops being a number)
+      const float ratio = __fdiv_rn(old, s);
+      constexpr int kLanes = HD / 16;
+      for (int t = tid / kLanes; t < lo; t += GT / kLanes) {
+        uint4* w = reinterpret_cast<uint4*>(dst + t * HD + (tid % kLanes) * 16);
+        const uint4 y = *w;
+        uint32_t yw[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t z = 0;
+#pragma unroll
+          for (int b = 0; b < 4; ++b)
+            z |= (requantise(static_cast<int8_t>(yw[i] >> (8 * b)), old, s, ratio) & 0xFFu) << (8 * b);
+          yw[i] = z;
+        }
+        *w = make_uint4(yw[0], yw[1], yw[2], yw[3]);
+      }
+    } else {
+      s = old;
+    }
+  }
+  return s;
+}
+
 // GT threads per (sequence, block, head, keys or values): the largest magnitude of the new rows, the scale, the numbers.  Memory-bound: 2 bytes
 // read and 1 written per value.  A thread holds all of its values, at most 8 loads of 16 bytes (GT = block_size * head_dim / 64): they are all
 // in flight at once, 64 KB an SM, and are read once.  6227 tokens of 8 heads of 128 into blocks of 64 take 12 us, 16384 32 (half the copy rate: a group
@@ -191,31 +230,7 @@ __global__ void __launch_bounds__(512, 1) cache_store_kernel(const __grid_consta
     } else {
       __syncwarp();
     }
-    float s = __fdiv_rn(Pair16<T>::lo(m), 127.0f);
-    if (s < kCacheMinScale) s = kCacheMinScale;
-    if (!(s * 0.0f == 0.0f)) s = __uint_as_float(0x7FFFFFFFu);     // Inf or NaN among the values: the block and head reads as NaN
-    if (r.lo > 0) {
-      if (!(s <= old) && old == old) {                           // the scale grows (or stops being a number)
-        const float ratio = __fdiv_rn(old, s);
-        constexpr int kLanes = HD / 16;
-        for (int t = tid / kLanes; t < r.lo; t += GT / kLanes) {
-          uint4* w = reinterpret_cast<uint4*>(dst + t * HD + (tid % kLanes) * 16);
-          const uint4 y = *w;
-          uint32_t yw[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t z = 0;
-#pragma unroll
-            for (int b = 0; b < 4; ++b)
-              z |= (requantise(static_cast<int8_t>(yw[i] >> (8 * b)), old, s, ratio) & 0xFFu) << (8 * b);
-            yw[i] = z;
-          }
-          *w = make_uint4(yw[0], yw[1], yw[2], yw[3]);
-        }
-      } else {
-        s = old;
-      }
-    }
+    const float s = cache_block_scale<HD, GT>(Pair16<T>::lo(m), old, r.lo, dst, tid);
     const float inv = __fdiv_rn(1.0f, s);
     int8_t* out = dst + (r.lo + sub) * HD + chunk * 8;
 #pragma unroll

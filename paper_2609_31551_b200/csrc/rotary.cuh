@@ -1,0 +1,326 @@
+// Rotary positions with several axes, alone and on the way into the 8-bit cache.
+//
+// Pair i of a head (two dimensions a, b of the first rotary_dim) turns by angle = positions[axis i][token] * inv_freq[i]:
+//   a' = scale (a cos - b sin),  b' = scale (b cos + a sin)
+// fp32 loses the angles of far positions (a position of 700000 is known to 0.03 rad), fp64 costs 64 times as much.  So angles are whole numbers: with
+// F = round(inv_freq / 2 pi * 2^64), position * F mod 2^64 is the angle in turns of 2^-64, exactly but for the rounding of F, which a position below 2^31
+// makes 2^-34 turns.  The upper 32 bits, as a signed fraction of a half turn, go to sincospif.
+#pragma once
+#include "kv_cache.cuh"
+#include "ptx.cuh"
+
+namespace eas {
+
+constexpr int kRotaryMaxPairs = 64, kRotaryMaxAxes = 4;
+
+struct RotaryTable {                      // (kernel parameter)
+  uint32_t f_lo[kRotaryMaxPairs], f_hi[kRotaryMaxPairs];
+  uint8_t axis[kRotaryMaxPairs];
+  int pairs, neighbours;
+  float scale;
+};
+
+// cosine and sine of a pair's angle at a position, times the scale (the sine's is negative where the rotation is taken back)
+__device__ __forceinline__ float2 rotary_turn(uint32_t f_lo, uint32_t f_hi, int position, float scale, float sin_scale) {
+  const uint32_t p = static_cast<uint32_t>(position);
+  const uint32_t turn = p * f_hi + __umulhi(p, f_lo) - (position < 0 ? f_lo : 0u);      // bits 32 .. 63 of position * F
+  float s, c;
+  sincospif(static_cast<float>(static_cast<int32_t>(turn)) * 4.656612873077393e-10f, &s, &c);     // 2^-31
+  return make_float2(c * scale, s * sin_scale);
+}
+
+struct RotaryRows {
+  const void *q, *k;
+  void *out_q, *out_k;
+  long long ld_q, ld_k, ld_out_q, ld_out_k;
+  const int32_t* positions;
+  long long ld_positions;
+  int n_rows, n_heads, n_kv;
+  int inverse;
+  int in_place;                           // outputs lie where the inputs do: what is not rotated stays
+};
+
+// 16 dimensions of a head, as two words of 8: with halves, item c < pairs / 8 is the first halves 8 c .. of the pairs and the second ones; everything else
+// is 16 dimensions side by side.
+__device__ __forceinline__ int2 rotary_at(int c, int pairs, int neighbours) {
+  return !neighbours && 8 * c < pairs ? make_int2(8 * c, pairs + 8 * c) : make_int2(16 * c, 16 * c + 8);
+}
+// the 16 values of a rotated item, turned by its 8 pairs' cosines and sines (8 float2 from shared memory)
+template <typename T>
+__device__ __forceinline__ void rotary_turn_16(const uint4& lo, const uint4& hi, const float4* cs, int neighbours, float (&y)[16]) {
+  const uint32_t a[4] = {lo.x, lo.y, lo.z, lo.w}, b[4] = {hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {           // two pairs
+    const float4 t = cs[i];
+    if (neighbours) {
+      const uint32_t w0 = i < 2 ? a[2 * i] : b[2 * i - 4], w1 = i < 2 ? a[2 * i + 1] : b[2 * i - 3];
+      const float x0 = Pair16<T>::lo(w0), x1 = Pair16<T>::hi(w0), x2 = Pair16<T>::lo(w1), x3 = Pair16<T>::hi(w1);
+      y[4 * i] = x0 * t.x - x1 * t.y;
+      y[4 * i + 1] = x1 * t.x + x0 * t.y;
+      y[4 * i + 2] = x2 * t.z - x3 * t.w;
+      y[4 * i + 3] = x3 * t.z + x2 * t.w;
+    } else {
+      const float x0 = Pair16<T>::lo(a[i]), x1 = Pair16<T>::lo(b[i]), x2 = Pair16<T>::hi(a[i]), x3 = Pair16<T>::hi(b[i]);
+      y[2 * i] = x0 * t.x - x1 * t.y;
+      y[8 + 2 * i] = x1 * t.x + x0 * t.y;
+      y[2 * i + 1] = x2 * t.z - x3 * t.w;
+      y[9 + 2 * i] = x3 * t.z + x2 * t.w;
+    }
+  }
+}
+
+// One token's heads [head0, head1) of queries and keys side by side (keys behind the queries), by a warp.  cs: the warp's 64 cosines and sines.
+template <int HD, typename T>
+__device__ __forceinline__ void rotary_row(const RotaryTable& t, const RotaryRows& r, int row, int head0, int head1, const int (&position)[2], float2* cs) {
+  constexpr int ITEMS = HD / 16, LANES = 32 / ITEMS, BATCH = 4;          // items a head, heads a warp takes at once, loads in flight
+  const int lane = threadIdx.x & 31, item = lane % ITEMS, sub = lane / ITEMS;
+  const bool turned = 8 * item < t.pairs;
+  const int2 at = rotary_at(item, t.pairs, t.neighbours);
+  auto from = [&](int h) {
+    return h < r.n_heads ? static_cast<const T*>(r.q) + row * r.ld_q + h * HD : static_cast<const T*>(r.k) + row * r.ld_k + (h - r.n_heads) * HD;
+  };
+  auto to = [&](int h) {
+    return h < r.n_heads ? static_cast<T*>(r.out_q) + row * r.ld_out_q + h * HD : static_cast<T*>(r.out_k) + row * r.ld_out_k + (h - r.n_heads) * HD;
+  };
+  bool first = true;
+  for (int h0 = head0; h0 < head1; h0 += LANES * BATCH) {
+    uint4 lo[BATCH], hi[BATCH];
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      const int h = h0 + i * LANES + sub;
+      lo[i] = hi[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (h < head1 && (turned || !r.in_place)) {
+        const T* src = from(h);
+        lo[i] = *reinterpret_cast<const uint4*>(src + at.x);
+        hi[i] = *reinterpret_cast<const uint4*>(src + at.y);
+      }
+    }
+    if (first) {
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int pair = lane + 32 * i;
+        if (pair < t.pairs) cs[pair] = rotary_turn(t.f_lo[pair], t.f_hi[pair], position[i], t.scale, r.inverse ? -t.scale : t.scale);
+      }
+      __syncwarp();
+      first = false;
+    }
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      const int h = h0 + i * LANES + sub;
+      if (h >= head1 || (!turned && r.in_place)) continue;
+      T* dst = to(h);
+      if (turned) {
+        float y[16];
+        rotary_turn_16<T>(lo[i], hi[i], reinterpret_cast<const float4*>(cs) + item * 4, t.neighbours, y);
+        lo[i] = make_uint4(Pair16<T>::pack(y[0], y[1]), Pair16<T>::pack(y[2], y[3]), Pair16<T>::pack(y[4], y[5]), Pair16<T>::pack(y[6], y[7]));
+        hi[i] = make_uint4(Pair16<T>::pack(y[8], y[9]), Pair16<T>::pack(y[10], y[11]), Pair16<T>::pack(y[12], y[13]), Pair16<T>::pack(y[14], y[15]));
+      }
+      *reinterpret_cast<uint4*>(dst + at.x) = lo[i];
+      *reinterpret_cast<uint4*>(dst + at.y) = hi[i];
+    }
+  }
+}
+
+struct RotaryParams {
+  RotaryTable t;
+  RotaryRows r;
+  uint32_t parts;                         // a token's heads in `parts` pieces of part_heads
+  int part_heads;
+  int early_launch;
+};
+
+constexpr int kRotaryThreads = 512;
+
+template <int HD, typename T>
+__global__ void __launch_bounds__(kRotaryThreads, 1) rotary_kernel(const __grid_constant__ RotaryParams p) {
+  __shared__ float2 table[kRotaryThreads / 32][kRotaryMaxPairs];
+  if (p.early_launch) pdl_launch_dependents();
+  pdl_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t units = static_cast<uint32_t>(p.r.n_rows) * p.parts, step = gridDim.x * (blockDim.x >> 5);      // (below 2^31)
+  const int heads = p.r.n_heads + p.r.n_kv;
+  auto position_of = [&](uint32_t u, int (&position)[2]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      position[i] = u < units && lane + 32 * i < p.t.pairs ? p.r.positions[p.t.axis[lane + 32 * i] * p.r.ld_positions + u / p.parts] : 0;
+  };
+  int position[2];
+  uint32_t u = blockIdx.x * (blockDim.x >> 5) + warp;
+  position_of(u, position);
+  for (; u < units; u += step) {
+    int next[2];
+    position_of(u + step, next);
+    const int row = static_cast<int>(u / p.parts), head0 = static_cast<int>(u - row * p.parts) * p.part_heads;
+    rotary_row<HD, T>(p.t, p.r, row, head0, min(head0 + p.part_heads, heads), position, table[warp]);
+    position[0] = next[0];
+    position[1] = next[1];
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ append
+struct AppendParams {
+  CacheView c;
+  CacheSeqs s;
+  RotaryTable t;
+  RotaryRows r;                           // n_kv: 0 (the keys' rotated form goes to the cache only); positions null: a token's place in its sequence
+  const void* v;
+  long long ld_v;
+  int pairs;                              // numbers of (sequence, block) pairs (see cache_run)
+  int head_parts, part_heads;             // key/value heads of a pair in pieces
+  uint32_t q_parts;                       // query heads of a token in pieces
+  int q_part_heads;
+  uint32_t* status;
+  int early_launch;
+};
+
+constexpr int kAppendThreads = 256;
+
+// The last of the sequences 0 .. n - 1 whose key, which grows with the sequence, is at or below x (0 if none is): a whole warp looks at 32 of them at a time.
+template <typename Key>
+__device__ __forceinline__ int last_sequence(int n, int x, Key key) {
+  int lo = 0, hi = n - 1;
+  const int lane = threadIdx.x & 31;
+  while (lo < hi) {
+    const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step;
+    const int passed = __popc(__ballot_sync(0xffffffffu, at <= hi && key(at) <= x));
+    lo += passed * step;
+    hi = min(hi, lo + step - 1);
+  }
+  return lo;
+}
+
+// Eight fp32 values to eight numbers, as quantise8 does it
+__device__ __forceinline__ uint2 quantise8_fp32(const float* y, float s, float inv) {
+  uint32_t q[8];
+  float off = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float r = y[i] * inv, t = r + 12582912.0f;
+    off = fmaxf(off, fabsf(r - (t - 12582912.0f)));
+    q[i] = __float_as_uint(t);
+  }
+  if (__builtin_expect(off > 0.5f - 3.0517578125e-05f, 0)) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = quantise(y[i], s, inv);
+  }
+  return make_uint2(__byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410),
+                    __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410));
+}
+
+// An item is the run of one sequence's new rows that lies in one block, and some of its key/value heads: the cosines and sines of the run's rows go to
+// shared memory once, then GT threads take a head's keys or values, as in cache_store_kernel (a thread has 4 rows of 16 dimensions, rotated in
+// fp32 and rounded once, to the number).  Behind those the queries: a warp takes a token's heads, or some of them.
+template <int HD, int GT, typename T>
+__global__ void __launch_bounds__(kAppendThreads, 2) cache_append_kernel(const __grid_constant__ AppendParams p) {
+  extern __shared__ __align__(16) float2 append_turns[];
+  __shared__ uint32_t group_max[32];
+  if (p.early_launch) pdl_launch_dependents();
+  pdl_wait();
+  constexpr int ITEMS = HD / 16, ROWS = GT / ITEMS, STEPS = 4, GROUPS = kAppendThreads / GT;
+  const int tid = threadIdx.x % GT, group = threadIdx.x / GT, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int item = tid % ITEMS, sub = tid / ITEMS;
+  auto cu = [&](int i) { return min(max(p.s.cu[i], 0), p.r.n_rows); };
+  const int pair_items = p.pairs * p.head_parts;
+  const uint32_t q_units = static_cast<uint32_t>(p.r.n_heads > 0 ? p.r.n_rows : 0) * p.q_parts;
+  const uint32_t items = pair_items + (q_units + kAppendThreads / 32 - 1) / (kAppendThreads / 32);
+  for (uint32_t it = blockIdx.x; it < items; it += gridDim.x) {
+    if (it >= static_cast<uint32_t>(pair_items)) {
+      const uint32_t u = (it - pair_items) * (kAppendThreads / 32) + warp;
+      __syncthreads();                                             // (the table in shared memory is no longer read)
+      if (u >= q_units) continue;
+      const int row = static_cast<int>(u / p.q_parts), head0 = static_cast<int>(u - row * p.q_parts) * p.q_part_heads;
+      if (row < cu(0) || row >= cu(p.s.n_seqs)) continue;
+      int position[2] = {0, 0};
+      if (p.r.positions == nullptr) {
+        const int s = last_sequence(p.s.n_seqs, row, cu);
+        position[0] = position[1] = p.s.start[s] + (row - cu(s));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (lane + 32 * i < p.t.pairs) position[i] = p.r.positions[p.t.axis[lane + 32 * i] * p.r.ld_positions + row];
+      }
+      rotary_row<HD, T>(p.t, p.r, row, head0, min(head0 + p.q_part_heads, p.r.n_heads), position, append_turns + warp * kRotaryMaxPairs);
+      continue;
+    }
+    const int pair = static_cast<int>(it) / p.head_parts, part = static_cast<int>(it) - pair * p.head_parts;
+    const CacheRun r = cache_run_of(p.c, p.s, last_sequence(p.s.n_seqs, pair, [&](int i) { return (cu(i) >> p.c.bs_log2) + 2 * i; }), p.r.n_rows, pair, p.status,
+                                    threadIdx.x == 0 && part == 0);
+    if (r.block < 0) continue;
+    const int n = r.hi - r.lo, units = 2 * min(p.part_heads, p.c.n_kv - part * p.part_heads);
+    uint4 x[2 * STEPS];
+    auto fetch = [&](int u) {                                      // the rows of unit u: keys (even) or values (odd) of a head
+      const bool values = u & 1;
+      const int head = part * p.part_heads + (u >> 1);
+      const long long ld = values ? p.ld_v : p.r.ld_k;
+      const T* src = static_cast<const T*>(values ? p.v : p.r.k) + static_cast<long long>(r.row + sub) * ld + head * HD;
+      const int2 at = values ? make_int2(16 * item, 16 * item + 8) : rotary_at(item, p.t.pairs, p.t.neighbours);
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) {
+        x[2 * i] = x[2 * i + 1] = make_uint4(0u, 0u, 0u, 0u);
+        if (u < units && sub + i * ROWS < n) {
+          x[2 * i] = *reinterpret_cast<const uint4*>(src + i * ROWS * ld + at.x);
+          x[2 * i + 1] = *reinterpret_cast<const uint4*>(src + i * ROWS * ld + at.y);
+        }
+      }
+    };
+    fetch(group);
+    __syncthreads();                                               // (the last item's table is no longer read)
+    for (int e = threadIdx.x; e < n * p.t.pairs; e += kAppendThreads) {
+      const int j = e / p.t.pairs, i = e - j * p.t.pairs;
+      const int position = p.r.positions == nullptr ? r.place + j : p.r.positions[p.t.axis[i] * p.r.ld_positions + r.row + j];
+      append_turns[e] = rotary_turn(p.t.f_lo[i], p.t.f_hi[i], position, p.t.scale, p.t.scale);
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int u = group; u < units; u += GROUPS) {
+      const bool values = u & 1, turned = !values && 8 * item < p.t.pairs;
+      const long long at = static_cast<long long>(r.block) * p.c.n_kv + part * p.part_heads + (u >> 1);
+      float* scale = (values ? p.c.v_scale : p.c.k_scale) + at;
+      int8_t* dst = (values ? p.c.v : p.c.k) + ((at << p.c.bs_log2) * HD);
+      const float old = r.lo > 0 ? *scale : 0.0f;
+      float y[STEPS][16];
+      uint32_t m = 0;                                              // magnitudes compare as integers, with Inf above every number and NaN above Inf
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) {
+        if (turned && sub + i * ROWS < n) {
+          rotary_turn_16<T>(x[2 * i], x[2 * i + 1], reinterpret_cast<const float4*>(append_turns + (sub + i * ROWS) * p.t.pairs) + item * 4, p.t.neighbours, y[i]);
+        } else {
+          const uint32_t w[8] = {x[2 * i].x, x[2 * i].y, x[2 * i].z, x[2 * i].w, x[2 * i + 1].x, x[2 * i + 1].y, x[2 * i + 1].z, x[2 * i + 1].w};
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            y[i][2 * e] = Pair16<T>::lo(w[e]);
+            y[i][2 * e + 1] = Pair16<T>::hi(w[e]);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) m = max(m, __float_as_uint(y[i][e]) & 0x7FFFFFFFu);
+      }
+      fetch(u + GROUPS);
+      m = __reduce_max_sync(0xffffffffu, m);
+      if constexpr (GT > 32) {
+        if (lane == 0) group_max[warp] = m;
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(GT) : "memory");
+        m = group_max[(group * GT >> 5) + (lane & (GT / 32 - 1))];
+        m = __reduce_max_sync(0xffffffffu, m);
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(GT) : "memory");      // read by all (and the old scale, before it is overwritten)
+      } else {
+        __syncwarp();
+      }
+      const float s = cache_block_scale<HD, GT>(__uint_as_float(m), old, r.lo, dst, tid);
+      const float inv = __fdiv_rn(1.0f, s);
+      const int2 to = values ? make_int2(16 * item, 16 * item + 8) : rotary_at(item, p.t.pairs, p.t.neighbours);
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) {
+        if (sub + i * ROWS < n) {
+          int8_t* out = dst + (r.lo + sub + i * ROWS) * HD;
+          *reinterpret_cast<uint2*>(out + to.x) = quantise8_fp32(y[i], s, inv);
+          *reinterpret_cast<uint2*>(out + to.y) = quantise8_fp32(y[i] + 8, s, inv);
+        }
+      }
+      if (tid == 0) *scale = s;
+    }
+  }
+}
+
+}  // namespace eas

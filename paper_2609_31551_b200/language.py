@@ -15,7 +15,8 @@ from . import binding as B
 
 LANGUAGE_SYMBOLS = [
     "eas_prompt_attention_workspace_bytes", "eas_prompt_attention", "eas_cache_create", "eas_cache_destroy", "eas_cache_store", "eas_cache_load",
-    "eas_cache_attention_workspace_bytes", "eas_cache_attention",
+    "eas_cache_attention_workspace_bytes", "eas_cache_attention", "eas_cache_chunk_workspace_bytes", "eas_cache_chunk_attention",
+    "eas_rotary_create", "eas_rotary_destroy", "eas_rotary_apply", "eas_cache_append",
 ]
 STATUS_CACHE_RANGE = 3          # EAS_DEVICE_CACHE_RANGE
 _DTYPES = {torch.bfloat16: 0, torch.float16: 1}
@@ -38,9 +39,22 @@ class CacheSeqs(C.Structure):
                 ("cu_seqlens", C.c_void_p), ("start", C.c_void_p), ("seq_lens", C.c_void_p)]
 
 
+class RotaryDesc(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rotary_dim", C.c_int32), ("pairing", C.c_int32), ("n_axes", C.c_int32), ("inv_freq", C.c_void_p),
+                ("axis", C.c_void_p), ("scale", C.c_float)]
+
+
+class RotaryInputs(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("out_q", C.c_void_p), ("out_k", C.c_void_p),
+                ("ld_q", C.c_int64), ("ld_k", C.c_int64), ("ld_out_q", C.c_int64), ("ld_out_k", C.c_int64),
+                ("positions", C.c_void_p), ("ld_positions", C.c_int64),
+                ("n_rows", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("dtype", C.c_int32), ("inverse", C.c_int32)]
+
+
 # The records of a call as bytes: making a ctypes structure takes 2.5 us (a prompt's) and 0.9, packing it 0.6 and 0.3
 _prompt_record = struct.Struct("4P4q4ifi2P").pack
 _pack_seqs = struct.Struct("iPiq3P").pack
+_pack_rotary = struct.Struct("4P4qPq5i4x").pack
 _declared = False
 
 
@@ -66,6 +80,19 @@ def lib():
         l.eas_cache_attention.restype = C.c_int
         l.eas_cache_attention.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_int32,
                                           C.c_float, C.c_void_p, C.c_size_t, C.c_int32, C.c_void_p, C.c_void_p]
+        l.eas_cache_chunk_workspace_bytes.restype = C.c_size_t
+        l.eas_cache_chunk_workspace_bytes.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32]
+        l.eas_cache_chunk_attention.restype = C.c_int
+        l.eas_cache_chunk_attention.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_int32,
+                                                C.c_int32, C.c_float, C.c_void_p, C.c_size_t, C.c_int32, C.c_void_p, C.c_void_p]
+        l.eas_rotary_create.restype = C.c_int
+        l.eas_rotary_create.argtypes = [C.POINTER(RotaryDesc), C.POINTER(C.c_void_p)]
+        l.eas_rotary_destroy.restype = None
+        l.eas_rotary_destroy.argtypes = [C.c_void_p]
+        l.eas_rotary_apply.restype = C.c_int
+        l.eas_rotary_apply.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]
+        l.eas_cache_append.restype = C.c_int
+        l.eas_cache_append.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p]
         _declared = True
     return l
 
@@ -195,6 +222,102 @@ def prompt_attention_workspace_bytes(n_heads, n_kv_heads, head_dim, cu_seqlens_h
     return lib().eas_prompt_attention_workspace_bytes(pin)
 
 
+class Rotary:
+    """Rotary positions with one or several axes (eas_rotary_*).
+
+    The first rotary_dim dimensions of a head (default: all; a multiple of 16) are pairs, dimension i and i + rotary_dim / 2, or 2 i and 2 i + 1 with
+    neighbours=True.  Pair i turns by position * inv_freq[i], inv_freq being base ** (-2 i / rotary_dim) unless given (fp64, for scaled frequencies); scale
+    multiplies cosines and sines.  sections: how many of the pairs, one section behind the other, turn with the first axis (time), the second
+    (height), the third (width), ...; or axes: the axis of each pair.  Default: one axis.  A Rotary belongs to no device."""
+
+    def __init__(self, head_dim, rotary_dim=None, base=10000.0, sections=None, axes=None, inv_freq=None, neighbours=False, scale=1.0):
+        self.handle = None
+        self.lib = lib()
+        self.head_dim, self.rotary_dim = head_dim, head_dim if rotary_dim is None else rotary_dim
+        pairs = max(self.rotary_dim // 2, 0)
+        try:
+            if inv_freq is None:
+                inv_freq = float(base) ** (-np.arange(pairs, dtype=np.float64) / max(pairs, 1))
+            freq = np.ascontiguousarray(inv_freq, dtype=np.float64)
+            if sections is not None:
+                _need(axes is None, "sections or axes, not both")
+                counts = [int(n) for n in sections]
+                _need(counts and min(counts) >= 0 and sum(counts) == pairs, f"sections {counts} must name {pairs} pairs")
+                axes = np.repeat(np.arange(len(counts)), counts)
+                self.n_axes = len(counts)
+            else:
+                self.n_axes = 1 if axes is None else int(max(axes)) + 1
+            axis = np.zeros(pairs, dtype=np.int32) if axes is None else np.ascontiguousarray(axes, dtype=np.int32)
+            desc = RotaryDesc(head_dim, self.rotary_dim, 1 if neighbours else 0, self.n_axes, freq.ctypes.data, axis.ctypes.data, scale)
+        except (TypeError, ValueError, OverflowError, ZeroDivisionError) as e:
+            raise B.EasError(1, f"rotary positions: {e}") from None
+        _need(freq.shape == (pairs,) and axis.shape == (pairs,), f"inv_freq and axes must be lists of {pairs}")
+        h = C.c_void_p()
+        B._check(self.lib.eas_rotary_create(C.byref(desc), C.byref(h)))
+        self.handle = h
+
+    def close(self):
+        if getattr(self, "handle", None):
+            self.lib.eas_rotary_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _positions(self, positions, rows, index):
+        """-> address, distance of two axes."""
+        shape = positions.shape
+        if (positions.dtype != torch.int32 or positions.get_device() != index or shape[-1:] != (rows,) or positions.stride(-1) != 1 and rows > 1
+                or (shape[:-1] != (self.n_axes,) and not (self.n_axes == 1 and len(shape) == 1))):
+            raise B.EasError(1, f"positions must be int32 [{self.n_axes}, {rows}] on GPU {index}, not {positions.dtype} {tuple(shape)} on {positions.device}")
+        return positions.data_ptr(), positions.stride(0) if self.n_axes > 1 else rows
+
+    def apply(self, q, k, positions, out=None, inverse=False, sm_budget=0, stream=None):
+        """eas_rotary_apply: q [T, n_heads, head_dim] and k [T, n_kv_heads, head_dim] (or None) at positions (int32 [n_axes, T], or [T] with one axis, on
+        the device) -> rotated (q, k).  out: a pair of tensors for them, (q, k) themselves to rotate in place.  inverse takes a rotation back; a
+        gradient goes through apply by inverse=True."""
+        dtype, index = q.dtype, q.get_device()
+        if self.handle is None:
+            raise B.EasError(1, "the rotary positions are closed")
+        if index < 0 or dtype not in _DTYPES or q.dim() != 3 or (k is not None and k.dim() != 3):
+            raise B.EasError(1, f"q and k must be bf16 or fp16 tensors [tokens, heads, head_dim] on a GPU, q is {dtype} {tuple(q.shape)} on {q.device}")
+        if _elsewhere(index, stream):
+            with _on(index, stream):
+                return self.apply(q, k, positions, out, inverse, sm_budget)
+        T, H, hd = q.shape
+        ld_q = _rows(q, "q", H, self.head_dim, dtype, index)
+        G, ld_k, at_k, at_out_k, ld_out_k, out_k = 0, 0, None, None, 0, None
+        if out is None:
+            out_q = torch.empty_like(q, memory_format=torch.contiguous_format)
+            ld_out_q = H * hd
+        else:
+            out_q, out_k = out
+            ld_out_q = _rows(out_q, "out of q", H, hd, dtype, index)
+        if k is not None:
+            G = k.shape[1]
+            ld_k = _rows(k, "k", G, hd, dtype, index)
+            if out is None:
+                out_k = torch.empty_like(k, memory_format=torch.contiguous_format)
+                ld_out_k = G * hd
+            else:
+                ld_out_k = _rows(out_k, "out of k", G, hd, dtype, index)
+            at_k, at_out_k = k.data_ptr(), out_k.data_ptr()
+            if k.shape[0] != T or out_k.shape[0] != T:
+                raise B.EasError(1, "k and its output must have as many tokens as q")
+        if out_q.shape[0] != T:
+            raise B.EasError(1, "the output of q must have as many tokens as q")
+        at, ld_pos = self._positions(positions, T, index)
+        rec = _pack_rotary(q.data_ptr(), at_k or 0, out_q.data_ptr(), at_out_k or 0, ld_q, ld_k, ld_out_q, ld_out_k, at, ld_pos, T, H, G, _DTYPES[dtype],
+                           1 if inverse else 0)
+        rc = self.lib.eas_rotary_apply(self.handle, rec, sm_budget, torch._C._cuda_getCurrentRawStream(index))
+        if rc:
+            B._check(rc)
+        return out_q, out_k
+
+
 class KvCache:
     """An 8-bit paged key/value cache (eas_cache_*): n_blocks blocks of block_size tokens.
 
@@ -276,6 +399,46 @@ class KvCache:
                 return self.store(k, v, cu_seqlens, start, block_table, sm_budget)
         self._move(self.lib.eas_cache_store, k, v, k.shape[0], cu_seqlens, start, block_table, sm_budget)
 
+    def append(self, q, k, v, cu_seqlens, start, block_table, rotary, positions=None, out=None, sm_budget=0, stream=None):
+        """eas_cache_append: store() of the keys rotated by `rotary` and the values, and the queries rotated: one launch.  q [rows, n_heads, head_dim] or None, k and v
+        [rows, n_kv_heads, head_dim]; cu_seqlens, start and block_table as for store().  positions: int32 [n_axes, rows] (or [rows] with one axis);
+        default: a token's place in its sequence.  Returns the rotated queries: in `out` if given (q itself to rotate it in place), where rows that
+        cu_seqlens does not name stay as they were."""
+        index, dtype = self._index, k.dtype
+        if _elsewhere(index, stream):
+            with _on(index, stream):
+                return self.append(q, k, v, cu_seqlens, start, block_table, rotary, positions, out, sm_budget)
+        if rotary.handle is None:
+            raise B.EasError(1, "the rotary positions are closed")
+        if dtype not in _DTYPES or len(start.shape) != 1:
+            raise B.EasError(1, f"k and v must be bf16 or fp16, not {dtype}; start a list of one place a sequence")
+        n, rows, G, hd = start.shape[0], k.shape[0], self.n_kv_heads, self.head_dim
+        seqs = self._seqs(block_table, n, _ints(cu_seqlens, "cu_seqlens", n + 1, index), _ints(start, "start", n, index), 0)
+        ld_k, ld_v = _rows(k, "k", G, hd, dtype, index), _rows(v, "v", G, hd, dtype, index)
+        H, at_q, at_out, ld_q, ld_out = 0, 0, 0, 0, 0
+        if q is not None:
+            if q.dim() != 3:
+                raise B.EasError(1, f"q must be [rows, n_heads, head_dim], not {tuple(q.shape)}")
+            H = q.shape[1]
+            ld_q = _rows(q, "q", H, hd, dtype, index)
+            if out is None:
+                out = torch.empty_like(q, memory_format=torch.contiguous_format)
+                ld_out = H * hd
+            else:
+                ld_out = _rows(out, "out", H, hd, dtype, index)
+            at_q, at_out = q.data_ptr(), out.data_ptr()
+            if q.shape[0] != rows or out.shape[0] != rows:
+                raise B.EasError(1, "q and its output must have as many rows as k")
+        if v.shape[0] != rows:
+            raise B.EasError(1, "k and v must have as many rows")
+        at_pos, ld_pos = (0, 0) if positions is None else rotary._positions(positions, rows, index)
+        rec = _pack_rotary(at_q, k.data_ptr(), at_out, 0, ld_q, ld_k, ld_out, 0, at_pos, ld_pos, rows, H, G, _DTYPES[dtype], 0)
+        rc = self.lib.eas_cache_append(self.handle, seqs, rotary.handle, rec, v.data_ptr(), ld_v, sm_budget, torch._C._cuda_getCurrentRawStream(index),
+                                       self._status_at)
+        if rc:
+            B._check(rc)
+        return out
+
     def load(self, cu_seqlens, start, block_table, n_rows, dtype=torch.bfloat16, out=None, sm_budget=0, stream=None):
         """eas_cache_load: the values of the same places -> (k, v), [n_rows, n_kv_heads, head_dim].  Rows that cu_seqlens does not name are
         left as they were (`out`, a pair of tensors of at least n_rows rows, whose type counts) or are not set."""
@@ -325,6 +488,49 @@ class KvCache:
         rc = self.lib.eas_cache_attention(self.handle, seqs, q.data_ptr(), ld_q, out.data_ptr(), ld_out, H, _DTYPES[dtype],
                                           hd ** -0.5 if scale is None else scale, workspace.data_ptr(), size, sm_budget,
                                           torch._C._cuda_getCurrentRawStream(index), self._status_at)
+        if rc:
+            B._check(rc)
+        return out
+
+    def chunk_workspace_bytes(self, n_seqs, n_rows, max_new, n_heads):
+        """eas_cache_chunk_workspace_bytes: scratch of a chunk_attention call."""
+        return self.lib.eas_cache_chunk_workspace_bytes(self.handle, n_seqs, n_rows, max_new, n_heads)
+
+    def chunk_attention(self, q, cu_seqlens, seq_lens, block_table, max_new=None, scale=None, out=None, workspace=None, sm_budget=0, stream=None):
+        """eas_cache_chunk_attention: rows cu_seqlens[s] .. cu_seqlens[s + 1] - 1 of q [rows, n_heads, head_dim] are the last tokens among places
+        0 .. seq_lens[s] - 1 of sequence s (stored before); each sees the places up to its own.  max_new: the most new tokens of a sequence, which
+        chooses the kernel (default: any number); a captured call can be replayed for other cu_seqlens and seq_lens within it.  Rows that cu_seqlens does not name are
+        left as they were (`out`) or are not set.  workspace: a uint8 tensor of chunk_workspace_bytes(), on a 256-byte boundary; calls that
+        may run at the same time need one each (default: allocated by the call)."""
+        index, dtype = self._index, q.dtype
+        if _elsewhere(index, stream):
+            with _on(index, stream):
+                return self.chunk_attention(q, cu_seqlens, seq_lens, block_table, max_new, scale, out, workspace, sm_budget)
+        if q.dim() != 3 or dtype not in _DTYPES or len(seq_lens.shape) != 1:
+            raise B.EasError(1, f"q must be bf16 or fp16 [rows, n_heads, head_dim], not {dtype} {tuple(q.shape)}; seq_lens a list of one length a sequence")
+        rows, H, hd = q.shape
+        n = seq_lens.shape[0]
+        ld_q = _rows(q, "q", H, self.head_dim, dtype, index)
+        seqs = self._seqs(block_table, n, _ints(cu_seqlens, "cu_seqlens", n + 1, index), 0, _ints(seq_lens, "seq_lens", n, index))
+        if max_new is None:
+            max_new = rows
+        if out is None:
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            ld_out = H * hd
+        else:
+            ld_out = _rows(out, "out", H, hd, dtype, index)
+            if out.shape[0] < rows:
+                raise B.EasError(1, "out has fewer rows than q")
+        if workspace is None:
+            size = self.chunk_workspace_bytes(n, rows, max_new, H)
+            workspace = q.new_empty(size, dtype=torch.uint8)
+        elif workspace.get_device() != index or not workspace.is_contiguous():
+            raise B.EasError(1, "workspace must be a contiguous tensor on the cache's GPU")
+        else:
+            size = workspace.nbytes
+        rc = self.lib.eas_cache_chunk_attention(self.handle, seqs, q.data_ptr(), ld_q, out.data_ptr(), ld_out, rows, max_new, H, _DTYPES[dtype],
+                                                hd ** -0.5 if scale is None else scale, workspace.data_ptr(), size, sm_budget,
+                                                torch._C._cuda_getCurrentRawStream(index), self._status_at)
         if rc:
             B._check(rc)
         return out
