@@ -1,9 +1,36 @@
-// Attention of several new tokens a sequence over the 8-bit cache: out = softmax(scale q K^T) V, the new tokens being the last of their sequence.
+// Attention of several new tokens a sequence over the 8-bit cache, on tcgen05 tensor cores: out = softmax(scale q K^T) V, the new tokens being the
+// last of their sequence.
+//
+// The query heads that share a key/value head are rows of one matrix, 128 / group tokens a tile of 128 rows, as in attention_prompt.cuh; the numbers of the
+// cache enter as they are, exact in fp16, as in attention_cache.cuh: queries are fp16 times a power of two per row, a block's key scale multiplies its scores in
+// fp32, its value scale v is an exponent: with t = score + log2 v and w = 2^(t - m),  out = sum w number / sum w / v, m being kept 2^7 to 2^15 below the largest t.
+//
+//   warp 3        walks the line of units (below) and tells the others the items of the CTA, through a ring
+//   warp 0        bytes of K and V, 16 tokens a bulk copy (they are contiguous), into a ring of 8-bit tiles; the scales of a step
+//   warps 1, 2    UMMA issuers, one per softmax warpgroup
+//   warps 4 ..    converters: a tile of queries, then of K and V, from bytes to fp16 in the tensor core's layout.  (0x6400 | (byte ^ 0x80)) - 1152: one logic operation and
+//                 one subtraction for the bytes 0 and 2 of a word, a shift more for 1 and 3; so four dimensions lie in the order 0, 2, 1, 3, in the queries and the output too
+//   warps 8 ..    two softmax warpgroups, one thread a row
+//
+// A step is 80 keys.  A unit of two tiles of one key/value head (shared) brings each K and V tile to both warpgroups; a unit of one tile gives its steps to the
+// warpgroups in turn (alternate), which put their results together at its end: O lies in tensor memory, where the lanes of both can read it.  So two steps are in
+// flight whether there are many rows (bound by the pipes) or few (bound by the bytes).
+//
+// The units of all sequences and heads form a line, in tokens seen times tiles, cut into one equal piece an SM (a function of the shapes and the device, not of sm_budget).  A
+// piece is the end of a unit, whole units, the beginning of one; cut units leave (m, l, O) in the workspace, and chunk_join_kernel puts them together in order.
+// Lengths are read on the device: each CTA sums them up itself.
 #pragma once
+#include "attention_cache.cuh"
 #include "kv_cache.cuh"
 #include "ptx.cuh"
 
 namespace eas {
+
+constexpr int kChunkMaxSeqs = 512;       // sequences of one launch (the prefix sums lie in shared memory)
+constexpr int kChunkKeys = 80, kChunkParts = kChunkKeys / 16;
+constexpr int kChunkUnitCost = 160;      // of a unit's beginning and end, in tokens of one tile
+constexpr int kChunkLeastCost = 320;     // of a piece
+constexpr int kChunkItems = 4;           // items that the roles may be apart
 
 struct ChunkParams {
   CacheView c;
@@ -13,83 +40,934 @@ struct ChunkParams {
   const uint16_t* q;
   uint16_t* out;
   long long ld_q, ld_out;
-  int fp16, group;
+  int fp16, group, tile_tokens;
+  int n_ctas;                  // SMs of the device: pieces of the line, at most
+  int ws_rows;                 // rows of a tile that the workspace holds
   float scale_log2;
+  float4* o_ws;                // [2 pieces][2 tiles][HD / 4][ws_rows]: O, not divided by the sum
+  float2* ml_ws;               // [2 pieces][2 tiles][ws_rows]: reference and sum (-inf, 0: no key)
   uint32_t* status;
   int early_launch;
 };
 
-// The simplest form: 128 threads per (row, query head), 128 tokens at a time: a thread has a token's score, then a dimension's sum.
 template <int HD>
-__global__ void __launch_bounds__(128) chunk_simple_kernel(const __grid_constant__ ChunkParams p) {
-  __shared__ float q[HD], w[128], vs[128];
-  __shared__ int ids[128];
+struct ChunkCfg {
+  static constexpr int kHalves = HD / 64;
+  static constexpr int kRawTiles = HD == 128 ? 6 : 12, kKTiles = HD == 128 ? 2 : 3, kVTiles = HD == 128 ? 2 : 3;
+  static constexpr int kThreads = 512;
+  static constexpr int kRegsLight = 64, kRegsConvert = 80, kRegsSoftmax = 184, kRegsLaunch = 128;
+  static constexpr int kQHalf = 128 * 128, kQBytes = kQHalf * kHalves;                 // 128 rows x 64 elements
+  static constexpr int kAtomBytes = kChunkKeys * 128, kTileBytes = kAtomBytes * kHalves;   // 80 keys x 64 elements
+  static constexpr int kRawBytes = kChunkKeys * HD;
+  static constexpr int kKOff = 2 * kQBytes, kVOff = kKOff + kKTiles * kTileBytes, kRawOff = kVOff + kVTiles * kTileBytes;
+  static constexpr int kPrefixOff = kRawOff + kRawTiles * kRawBytes;
+  static constexpr int kScaleSlots = 16;
+  static constexpr int kScaleOff = kPrefixOff + (kChunkMaxSeqs + 2) * 8;               // [slot][16]: key scales, log2 of value scales, their inverses
+  static constexpr int kRowOff = kScaleOff + kScaleSlots * 64;                         // [2][128] factors of the rows' scores
+  static constexpr int kMlOff = kRowOff + 2 * 128 * 4;                                 // [2][128] reference and sum of a warpgroup's rows
+  static constexpr int kItemOff = kMlOff + 2 * 128 * 8;
+  static constexpr int kBarOff = kItemOff + kChunkItems * 64;
+  static constexpr int kBars = 2 * kRawTiles + 2 * kKTiles + 2 * kVTiles + kScaleSlots + 2 + 2 + 4 * 2 + 2 + 2 * kChunkItems;
+  static constexpr int kBytes = kBarOff + kBars * 8 + 160 + 1024;                      // words, alignment slack
+  static constexpr int kSCol0 = 2 * HD, kSStride = kChunkKeys + kChunkKeys / 2;        // tensor memory: O of both, then scores and P of each
+  static_assert(kBytes <= 232448, "exceeds the shared memory of an SM");
+  static_assert(kBytes > 116224, "a second CTA must not fit beside this one");
+  static_assert(kQBytes % 1024 == 0 && kAtomBytes % 1024 == 0, "tiles start on swizzle-atom boundaries");
+  static_assert(kSCol0 + 2 * kSStride <= 512, "tensor memory columns");
+  static_assert(kRegsLight + kRegsConvert + 2 * kRegsSoftmax <= 4 * kRegsLaunch, "setmaxnreg budget exceeds the CTA's register allocation");
+  // the producer is at most this many steps ahead of the softmax: raw tiles, converted K tiles, one step each being read
+  static_assert(kRawTiles / 2 + 1 + kKTiles + 4 <= kScaleSlots, "a step's scales are read before their slot is filled again");
+};
+
+// ------------------------------------------------------------------------------------ the line of units
+struct ChunkSeq {              // a sequence: its visible new tokens, the tokens in front of them, and what its tiles cost a head
+  int q0, n, ahead, tiles, units;
+  __device__ __forceinline__ ChunkSeq() : q0(0), n(0), ahead(0), tiles(0), units(0) {}
+  __device__ __forceinline__ ChunkSeq(const ChunkParams& p, int s, bool report) {
+    auto cu = [&](int i) { return min(max(p.cu[i], 0), p.n_rows); };
+    const int first = cu(s), given = max(cu(s + 1) - first, 0);
+    const long long most = static_cast<long long>(p.max_blocks) << p.c.bs_log2;
+    int len = max(p.seq_lens[s], 0);
+    if (len > most || given > p.max_new) {
+      if (report) raise_status(p.status, DEV_ERR_CACHE_RANGE);
+      len = given > p.max_new ? 0 : static_cast<int>(most);
+    }
+    n = min(given, len);
+    q0 = first + given - n;
+    ahead = len - n;
+    tiles = (n + p.tile_tokens - 1) / p.tile_tokens;
+    units = (tiles + 1) >> 1;
+  }
+  // units 0 .. j - 1 cost, j < units: two tiles each, seeing ahead + 2 tile_tokens (i + 1) tokens
+  __device__ __forceinline__ long long before(int j, int tile_tokens) const {
+    return static_cast<long long>(j) * (kChunkUnitCost + 2LL * ahead) + 2LL * tile_tokens * j * (j + 1);
+  }
+  __device__ __forceinline__ bool single(int j) const { return 2 * j + 1 == tiles; }      // a unit of one tile
+  __device__ __forceinline__ int seen(int j, int tile_tokens) const {                     // tokens that a unit's last row sees
+    return ahead + static_cast<int>(min(static_cast<long long>(n), 2LL * tile_tokens * (j + 1)));
+  }
+  __device__ __forceinline__ long long cost(int j, int tile_tokens) const {
+    return kChunkUnitCost + (single(j) ? 1LL : 2LL) * seen(j, tile_tokens);
+  }
+  __device__ __forceinline__ long long total(int tile_tokens) const {
+    return units == 0 ? 0 : before(units - 1, tile_tokens) + cost(units - 1, tile_tokens);
+  }
+};
+
+// Prefix sums over the sequences of what they cost, all heads, by a CTA of 512 threads: prefix[0 .. n_seqs]
+__device__ __forceinline__ void chunk_prefix(const ChunkParams& p, long long* prefix, long long* sums, bool report) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  long long cost = 0;
+  if (threadIdx.x < p.n_seqs) cost = ChunkSeq(p, threadIdx.x, report).total(p.tile_tokens) * p.c.n_kv;
+  long long incl = cost;
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const long long o = __shfl_up_sync(0xffffffffu, incl, d);
+    if (lane >= d) incl += o;
+  }
+  if (lane == 31) sums[warp] = incl;
+  __syncthreads();
+  for (int w = 0; w < warp; ++w) incl += sums[w];
+  if (threadIdx.x < p.n_seqs) prefix[threadIdx.x + 1] = incl;
+  if (threadIdx.x == 0) prefix[0] = 0;
+  __syncthreads();
+}
+
+struct ChunkLine {
+  long long total, whole;
+  int pieces, rest;
+  __device__ __forceinline__ ChunkLine(long long cost, int device_pieces)
+      : total(cost), pieces(static_cast<int>(min(static_cast<long long>(device_pieces), (cost + kChunkLeastCost - 1) / kChunkLeastCost))) {
+    whole = pieces == 0 ? 0 : total / pieces;
+    rest = static_cast<int>(total - whole * pieces);
+  }
+  __device__ __forceinline__ long long begin(int piece) const { return whole * piece + static_cast<uint32_t>(rest) * static_cast<uint32_t>(piece) / static_cast<uint32_t>(pieces); }
+};
+
+// A unit and its place on the line
+struct ChunkUnit {
+  ChunkSeq seq;
+  int s, head, j;
+  long long at;                // where it begins
+  int tiles, steps;            // its tiles; key steps up to its last row's end
+  __device__ __forceinline__ void settle(const ChunkParams& p) {
+    tiles = seq.single(j) ? 1 : 2;
+    steps = (seq.seen(j, p.tile_tokens) + kChunkKeys - 1) / kChunkKeys;
+  }
+  // the unit that holds position x < total
+  __device__ __forceinline__ void find(const ChunkParams& p, const long long* prefix, long long x) {
+    int lo = 0, hi = p.n_seqs - 1;
+    while (lo < hi) {                                              // the last sequence that begins at or before x (those without units are passed over)
+      const int mid = (lo + hi + 1) >> 1;
+      if (prefix[mid] <= x) lo = mid; else hi = mid - 1;
+    }
+    s = lo;
+    seq = ChunkSeq(p, s, false);
+    const long long a_head = (prefix[s + 1] - prefix[s]) / p.c.n_kv;
+    x -= prefix[s];
+    head = static_cast<int>(x / a_head);
+    x -= head * a_head;
+    lo = 0;
+    hi = seq.units - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (seq.before(mid, p.tile_tokens) <= x) lo = mid; else hi = mid - 1;
+    }
+    j = lo;
+    at = prefix[s] + head * a_head + seq.before(j, p.tile_tokens);
+    settle(p);
+  }
+  __device__ __forceinline__ long long end(const ChunkParams& p) const { return at + seq.cost(j, p.tile_tokens); }
+  __device__ __forceinline__ void next(const ChunkParams& p, const long long* prefix, long long line_end) {      // (past the last unit: at is the line's end)
+    at = end(p);
+    if (++j == seq.units) {
+      j = 0;
+      if (++head == p.c.n_kv) {
+        head = 0;
+        if (at >= line_end) return;
+        do ++s; while (prefix[s + 1] == prefix[s]);
+        seq = ChunkSeq(p, s, false);
+      }
+    }
+    settle(p);
+  }
+  // the first key step at or behind position x of the line: step k begins at `at` + unit cost + tiles * 80 k
+  __device__ __forceinline__ int step_at(long long x) const {
+    const long long in = x - at - kChunkUnitCost, width = static_cast<long long>(tiles) * kChunkKeys;
+    return in <= 0 ? 0 : static_cast<int>(min(static_cast<long long>(steps), (in + width - 1) / width));
+  }
+  __device__ __forceinline__ int steps_of_tile(const ChunkParams& p, int w) const {
+    const long long last = min(static_cast<long long>(seq.n), static_cast<long long>(2 * j + w + 1) * p.tile_tokens);
+    return (seq.ahead + static_cast<int>(last) + kChunkKeys - 1) / kChunkKeys;
+  }
+};
+// The items of a CTA in order: of each unit in its pieces, the steps [lo, hi), never none
+struct ChunkDeal {
+  const ChunkParams& p;
+  const long long* prefix;
+  ChunkLine line;
+  ChunkUnit u;
+  int piece, lo, hi;
+  long long end;
+  bool more;
+  __device__ __forceinline__ ChunkDeal(const ChunkParams& params, const long long* pre)
+      : p(params), prefix(pre), line(pre[params.n_seqs], params.n_ctas), piece(blockIdx.x), lo(0), hi(0), end(0), more(true) {
+    seek(true);
+  }
+  __device__ __forceinline__ void next() { seek(false); }
+  __device__ __forceinline__ void seek(bool fresh) {               // fresh: the first item of `piece`; else the one behind the present one
+    for (;;) {
+      if (fresh) {
+        more = piece < line.pieces;
+        if (!more) return;
+        const long long begin = line.begin(piece);
+        end = line.begin(piece + 1);
+        u.find(p, prefix, begin);
+        lo = u.step_at(begin);
+        fresh = false;
+      } else {
+        u.next(p, prefix, line.total);
+        if (u.at >= end) {
+          piece += gridDim.x;
+          fresh = true;
+          continue;
+        }
+        lo = 0;
+      }
+      hi = end >= u.end(p) ? u.steps : u.step_at(end);
+      if (lo < hi) return;
+    }
+  }
+};
+// What the other roles know of an item
+struct alignas(16) ChunkItem {
+  int lo, n;                   // its first key step and how many (0: there is no further item)
+  int tiles, mine[2];          // its tiles; of two, how many of the steps each has keys in
+  int q0, tok0, n_tok, ahead;  // the sequence's first visible row, the unit's first token of those, their number, the tokens in front
+  int head, s, seen;           // key/value head, sequence, tokens that the unit's last row sees
+  int slot;                    // of the workspace; -1: the item is the whole unit
+  int pad[3];
+};
+static_assert(sizeof(ChunkItem) == 64, "four loads");
+
+// ------------------------------------------------------------------------------------ small pieces
+__device__ __forceinline__ void bulk_load(void* smem_dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(smem_u32(smem_dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__host__ __device__ constexpr uint32_t make_idesc_f16(int m, int n, int a_mn, int b_mn) {
+  return make_idesc_bf16(m, n, a_mn, b_mn) & ~((1u << 7) | (1u << 10));
+}
+// 16 fp16 dimensions 16 c .. of row r of a tile whose rows are 128 bytes an atom of 64 dimensions, 128-byte swizzle.  Lanes with c >= 4 (the second atom) store
+// their second chunk first, so that the eight lanes of a row touch all banks.
+__device__ __forceinline__ void store_row_16(uint32_t tile, uint32_t atom_bytes, int r, int c, const uint32_t (&h)[8]) {
+  const uint32_t base = tile + (c >> 2) * atom_bytes + r * 128;
+  const int first = c >> 2, a = (2 * (c & 3) + first) ^ (r & 7), b = (2 * (c & 3) + 1 - first) ^ (r & 7);
+  if (first) {
+    sts128(base + a * 16, h[4], h[5], h[6], h[7]);
+    sts128(base + b * 16, h[0], h[1], h[2], h[3]);
+  } else {
+    sts128(base + a * 16, h[0], h[1], h[2], h[3]);
+    sts128(base + b * 16, h[4], h[5], h[6], h[7]);
+  }
+}
+
+// ------------------------------------------------------------------------------------ the kernel
+template <int HD>
+__global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_kernel(const __grid_constant__ ChunkParams p) {
+  using L = ChunkCfg<HD>;
+  constexpr int NR = L::kRawTiles, NK = L::kKTiles, NV = L::kVTiles, KEYS = kChunkKeys, PARTS = kChunkParts, NS = L::kScaleSlots;
+  extern __shared__ uint8_t smem_raw_chunk[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw_chunk) + 1023) & ~uintptr_t(1023));
+  long long* prefix = reinterpret_cast<long long*>(smem + L::kPrefixOff);
+  float* sc_ring = reinterpret_cast<float*>(smem + L::kScaleOff);
+  float* row_factor = reinterpret_cast<float*>(smem + L::kRowOff);
+  float2* ml_smem = reinterpret_cast<float2*>(smem + L::kMlOff);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBarOff);
+  uint64_t* raw_full = bars;                 // [NR] bytes of a tile landed
+  uint64_t* raw_empty = raw_full + NR;       // [NR] converted
+  uint64_t* k_full = raw_empty + NR;         // [NK] fp16 tile written
+  uint64_t* k_empty = k_full + NK;           // [NK] every issuer hands every tile back
+  uint64_t* v_full = k_empty + NK;           // [NV]
+  uint64_t* v_empty = v_full + NV;           // [NV]
+  uint64_t* sc_full = v_empty + NV;          // [NS] scales of a step written
+  uint64_t* q_full = sc_full + NS;           // [2] queries and their rows' factors
+  uint64_t* q_empty = q_full + 2;            // [2] by both issuers and all softmax warps
+  uint64_t* s_full = q_empty + 2;            // [2] scores of a step complete
+  uint64_t* p_ready = s_full + 2;            // [2] P stored, O rescaled if it had to be
+  uint64_t* s_free = p_ready + 2;            // [2] scores read out of tensor memory
+  uint64_t* pv_done = s_free + 2;            // [2] P V of a step complete
+  uint64_t* met = pv_done + 2;               // [2] alternate: both warpgroups' sums are there; both have read O
+  uint64_t* item_full = met + 2;             // [kChunkItems]
+  uint64_t* item_empty = item_full + kChunkItems;      // by the 15 other warps
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(item_empty + kChunkItems);
+  volatile uint32_t* abort_flag = tmem_slot + 1;
+  long long* scan_sums = reinterpret_cast<long long*>(tmem_slot + 2);                    // [16]
+
+  const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < NR; ++i) { mbar_init(&raw_full[i], 1); mbar_init(&raw_empty[i], 4); }
+    for (int i = 0; i < NK; ++i) { mbar_init(&k_full[i], 4); mbar_init(&k_empty[i], 2); }
+    for (int i = 0; i < NV; ++i) { mbar_init(&v_full[i], 4); mbar_init(&v_empty[i], 2); }
+    for (int i = 0; i < NS; ++i) mbar_init(&sc_full[i], 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&q_full[i], 4); mbar_init(&q_empty[i], 10); mbar_init(&s_full[i], 1); mbar_init(&p_ready[i], 4);
+      mbar_init(&s_free[i], 4); mbar_init(&pv_done[i], 1); mbar_init(&met[i], 8);
+    }
+    for (int i = 0; i < kChunkItems; ++i) { mbar_init(&item_full[i], 1); mbar_init(&item_empty[i], 15); }
+    *abort_flag = 0;
+    mbar_fence_init();
+  }
+  if (warp == 3) {
+    tmem_alloc(tmem_slot, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = *tmem_slot;
+  pdl_wait();
+  if (p.early_launch) pdl_launch_dependents();     // behind the wait: the joining kernel reads the lengths ahead of its own
+  chunk_prefix(p, prefix, scan_sums, blockIdx.x == 0);
+
+  const uint32_t smem_at = smem_u32(smem);
+  auto q_tile = [&](uint32_t slot) { return smem_at + slot * L::kQBytes; };
+  auto k_tile = [&](uint32_t g) { return smem_at + L::kKOff + g % NK * L::kTileBytes; };
+  auto v_tile = [&](uint32_t g) { return smem_at + L::kVOff + g % NV * L::kTileBytes; };
+
+  ChunkItem* const item_ring = reinterpret_cast<ChunkItem*>(smem + L::kItemOff);
+  uint32_t n_items = 0;                            // taken by this warp
+  auto take = [&](ChunkItem& it) {                 // the next item; false after an expired wait
+    const uint32_t at = n_items % kChunkItems;
+    if (!warp_mbar_wait(&item_full[at], (n_items / kChunkItems) & 1u, abort_flag)) return false;
+    const uint4* src = reinterpret_cast<const uint4*>(item_ring + at);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(&it)[i] = src[i];
+    __syncwarp();
+    mbar_arrive_if(&item_empty[at], lane == 0);
+    ++n_items;
+    return true;
+  };
+
+  if (warp < 4) {
+    setmaxnreg_dec<L::kRegsLight>();
+    if (warp == 3) {
+      // ------------------------------------------------------------------ the CTA's items
+      bool ok = true;
+      auto put = [&](const ChunkItem& it) {
+        const uint32_t at = n_items % kChunkItems;
+        if (!warp_mbar_wait(&item_empty[at], ((n_items / kChunkItems) & 1u) ^ 1u, abort_flag)) return false;
+        if (lane == 0) {
+          item_ring[at] = it;
+          mbar_arrive(&item_full[at]);
+        }
+        __syncwarp();
+        ++n_items;
+        return true;
+      };
+      for (ChunkDeal deal(p, prefix); deal.more && ok; deal.next()) {
+        const ChunkUnit& u = deal.u;
+        ChunkItem it;
+        it.lo = deal.lo;
+        it.n = deal.hi - deal.lo;
+        it.tiles = u.tiles;
+        it.mine[0] = min(deal.hi, u.steps_of_tile(p, 0)) - deal.lo;
+        it.mine[1] = min(deal.hi, u.steps_of_tile(p, 1)) - deal.lo;
+        it.q0 = u.seq.q0;
+        it.tok0 = 2 * u.j * p.tile_tokens;
+        it.n_tok = u.seq.n;
+        it.ahead = u.seq.ahead;
+        it.head = u.head;
+        it.s = u.s;
+        it.seen = u.seq.seen(u.j, p.tile_tokens);
+        it.slot = it.n == u.steps ? -1 : 2 * deal.piece + (deal.hi == u.steps ? 0 : 1);
+        ok = put(it);
+      }
+      if (ok) {
+        ChunkItem none{};
+        put(none);
+      }
+    } else if (warp == 0) {
+      // ------------------------------------------------------------------ bytes and scales
+      // The order of the tiles: K of step 0; then K of step j + 1 and V of step j (the scores of a step are wanted before the values of the one in front)
+      uint32_t r = 0, g = 0;                       // raw tiles, steps so far
+      bool ok = true;
+      for (;;) {
+        ChunkItem it;
+        ok = take(it);
+        if (!ok || it.n == 0) break;
+        const int lo = it.lo, n = it.n, seen = it.seen, head = it.head;
+        const int32_t* ids = p.table + it.s * p.ld_table;
+        auto load_id = [&](int j) {                // lane m < PARTS: the block of tokens 16 m .. of step j
+          int id = -1;
+          const int tok = (lo + j) * KEYS + lane * 16;
+          if (lane < PARTS && j < n && tok < seen) {
+            id = ids[tok >> p.c.bs_log2];
+            if (static_cast<uint32_t>(id) >= static_cast<uint32_t>(p.c.n_blocks)) {
+              raise_status(p.status, DEV_ERR_CACHE_RANGE);
+              id = -1;
+            }
+          }
+          return id;
+        };
+        auto copy = [&](const int8_t* from, int id, int j) {
+          const uint32_t st = r % NR, have = __ballot_sync(0xffffffffu, id >= 0);
+          if (!warp_mbar_wait(&raw_empty[st], ((r / NR) & 1u) ^ 1u, abort_flag)) return false;
+          if (lane == 0) mbar_expect_tx(&raw_full[st], __popc(have) * (16u * HD));
+          __syncwarp();
+          if (id >= 0) {
+            const int place = ((lo + j) * KEYS + lane * 16) & ((1 << p.c.bs_log2) - 1);
+            const long long row = ((static_cast<long long>(id) * p.c.n_kv + head) << p.c.bs_log2) + place;
+            bulk_load(smem + L::kRawOff + st * L::kRawBytes + lane * 16 * HD, from + row * HD, 16 * HD, &raw_full[st]);
+          }
+          ++r;
+          return true;
+        };
+        auto publish = [&](float2 sc, int id, uint32_t step) {
+          float* dst = sc_ring + (step % NS) * 16;
+          if (lane < PARTS) {
+            const float vs = sc.y < kCacheMinScale ? kCacheMinScale : sc.y, lg = fast_lg2(vs);      // (a NaN stays)
+            dst[lane] = id >= 0 ? sc.x : 0.f;
+            dst[PARTS + lane] = id >= 0 ? lg : -INFINITY;
+            dst[2 * PARTS + lane] = id >= 0 ? fast_ex2(-lg) * kWeightDown : 0.f;
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sc_full[step % NS]);
+        };
+        auto load_scales = [&](int id) {
+          float2 sc = make_float2(0.f, 0.f);
+          if (id >= 0) {
+            const long long at = static_cast<long long>(id) * p.c.n_kv + head;
+            sc = make_float2(p.c.k_scale[at], p.c.v_scale[at]);
+          }
+          return sc;
+        };
+        int id_v = load_id(0), id_k = load_id(1);  // of step j, whose V is next, and of the step behind it
+        ok = copy(p.c.k, id_v, 0);
+        float2 sc = load_scales(id_v);
+        for (int j = 0; j < n && ok; ++j, ++g) {
+          const int id_next = load_id(j + 2);
+          const float2 sc_next = load_scales(id_k);
+          publish(sc, id_v, g);
+          if (j + 1 < n) ok = copy(p.c.k, id_k, j + 1);
+          ok = ok && copy(p.c.v, id_v, j);
+          id_v = id_k;
+          id_k = id_next;
+          sc = sc_next;
+        }
+        if (!ok) break;
+      }
+      // every copy has landed before the CTA's shared memory passes to another one: converted, or (after an expired wait) by time
+      for (uint32_t e = r < NR ? 0 : r - NR; e < r && ok; ++e) ok = warp_mbar_wait(&raw_empty[e % NR], (e / NR) & 1u, abort_flag);
+      if (!ok) {
+        const long long t0 = clock64();
+        while (clock64() - t0 < 4000000) {}
+      }
+    } else if (warp <= 2) {
+      // ------------------------------------------------------------------ UMMA issuers
+      // Every issuer sees every K and V tile of the CTA, in order, and hands back those that it does not use, so that it never mistakes a barrier's phase for another.
+      const int w = warp - 1;
+      constexpr uint32_t idesc_s = make_idesc_f16(128, KEYS, 0, 0);        // S = Q K^T, both K-major
+      constexpr uint32_t idesc_o = make_idesc_f16(128, HD, 0, 1);          // O += P V, V is MN-major
+      const uint32_t tm_s = tmem_base + L::kSCol0 + w * L::kSStride, tm_p = tm_s + KEYS, tm_o = tmem_base + w * HD;
+      uint32_t base = 0, k_at = 0, v_at = 0, qn = 0, n_s = 0, n_p = 0;     // steps, tiles passed, query tiles, scores issued, P waited for
+      bool ok = true;
+      auto pass_k = [&](uint32_t to) {
+        for (; k_at < to; ++k_at) {
+          if (!warp_mbar_wait(&k_full[k_at % NK], (k_at / NK) & 1u, abort_flag)) return false;
+          mbar_arrive_if(&k_empty[k_at % NK], lane == 0);
+        }
+        return true;
+      };
+      auto pass_v = [&](uint32_t to) {
+        for (; v_at < to; ++v_at) {
+          if (!warp_mbar_wait(&v_full[v_at % NV], (v_at / NV) & 1u, abort_flag)) return false;
+          mbar_arrive_if(&v_empty[v_at % NV], lane == 0);
+        }
+        return true;
+      };
+      while (ok) {
+        ChunkItem it;
+        ok = take(it);
+        if (!ok || it.n == 0) break;
+        const int n = it.n, tiles = it.tiles;
+        const bool alternate = tiles == 1;
+        const int first = alternate ? w : 0, stride = alternate ? 2 : 1;
+        const int mine = alternate ? n : w == 0 ? it.mine[0] : it.mine[1];      // steps below this are the warpgroup's (every stride-th)
+        const int last = mine <= first ? -1 : first + (mine - 1 - first) / stride * stride;
+        const uint32_t slot = (qn + (alternate ? 0 : w)) & 1u;
+        // queries: wait for each tile of the item, hand back what is not used
+        for (int t = 0; t < tiles && ok; ++t) {
+          const uint32_t q = qn + t;
+          ok = warp_mbar_wait(&q_full[q & 1u], (q >> 1) & 1u, abort_flag);
+          if (ok && ((q & 1u) != slot || last < 0)) mbar_arrive_if(&q_empty[q & 1u], lane == 0);
+        }
+        qn += tiles;
+        if (!ok) break;
+        auto scores = [&](int j) {                 // of step j, into the warpgroup's columns once they are read
+          const uint32_t g = base + j;
+          if (!pass_k(g) || !warp_mbar_wait(&k_full[g % NK], (g / NK) & 1u, abort_flag)) return false;
+          if (n_s > 0 && !warp_mbar_wait(&s_free[w], (n_s - 1u) & 1u, abort_flag)) return false;
+          tc_fence_after_sync();
+          const uint64_t ad = make_smem_desc(q_tile(slot), 16, 1024, kSwizzle128B), bd = make_smem_desc(k_tile(g), 16, 1024, kSwizzle128B);
+          if (elect_one()) {
+#pragma unroll
+            for (int h = 0; h < L::kHalves; ++h)
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                umma_bf16_ss(tm_s, ad + h * (L::kQHalf >> 4) + 2 * k, bd + h * (L::kAtomBytes >> 4) + 2 * k, idesc_s, h != 0 || k != 0);
+            umma_commit(&s_full[w]);
+            umma_commit(&k_empty[g % NK]);
+            if (j == last) umma_commit(&q_empty[slot]);
+          }
+          __syncwarp();
+          k_at = g + 1;
+          ++n_s;
+          return true;
+        };
+        if (last >= 0) {
+          ok = scores(first);
+          for (int j = first; j <= last && ok; j += stride) {
+            const uint32_t g = base + j;
+            if (j < last && !scores(j + stride)) { ok = false; break; }
+            if (!pass_v(g) || !warp_mbar_wait(&v_full[g % NV], (g / NV) & 1u, abort_flag) || !warp_mbar_wait(&p_ready[w], n_p & 1u, abort_flag)) { ok = false; break; }
+            ++n_p;
+            tc_fence_after_sync();
+            const uint64_t bd = make_smem_desc(v_tile(g), L::kAtomBytes, 1024, kSwizzle128B);
+            if (elect_one()) {
+#pragma unroll
+              for (int ks = 0; ks < KEYS / 16; ++ks)             // 16 keys: 8 columns of P, 2 KB of V
+                umma_bf16_ts(tm_o, tm_p + ks * 8, bd + ks * (2048 >> 4), idesc_o, (j != first || ks != 0) ? 1u : 0u);
+              umma_commit(&pv_done[w]);
+              umma_commit(&v_empty[g % NV]);
+            }
+            __syncwarp();
+            v_at = g + 1;
+            if (alternate && j + 1 < n) ok = pass_v(g + 2);      // the other's values, as soon as they are there
+          }
+        }
+        ok = ok && pass_k(base + n) && pass_v(base + n);
+        base += n;
+      }
+      // the last hand-backs are asynchronous arrivals: in before the CTA ends
+      if (ok && w == 0) {
+        for (uint32_t e = base < NK ? 0 : base - NK; e < base && ok; ++e) ok = warp_mbar_wait(&k_empty[e % NK], (e / NK) & 1u, abort_flag);
+        for (uint32_t e = base < NV ? 0 : base - NV; e < base && ok; ++e) ok = warp_mbar_wait(&v_empty[e % NV], (e / NV) & 1u, abort_flag);
+        for (uint32_t e = qn < 2 ? 0 : qn - 2; e < qn && ok; ++e) ok = warp_mbar_wait(&q_empty[e & 1u], (e >> 1) & 1u, abort_flag);
+      }
+    }
+  } else if (warp < 8) {
+    // ------------------------------------------------------------------ converters
+    setmaxnreg_dec<L::kRegsConvert>();
+    const int cw = warp - 4;
+    constexpr int CHUNKS = HD / 16, ROWS = 32 / CHUNKS;                    // 16 dimensions a lane, rows a warp takes at once
+    const int chunk = lane % CHUNKS, sub = lane / CHUNKS;
+    uint32_t r = 0, k_at = 0, v_at = 0, qn = 0;
+    bool ok = true;
+    auto convert = [&](uint32_t tile, uint64_t* full, uint64_t* empty, uint32_t use) {      // the next raw tile
+      const uint32_t st = r % NR;
+      if (!warp_mbar_wait(&raw_full[st], (r / NR) & 1u, abort_flag) || !warp_mbar_wait(empty, (use & 1u) ^ 1u, abort_flag)) return false;
+      const uint32_t raw = smem_at + L::kRawOff + st * L::kRawBytes + chunk * 16;
+      constexpr int PASSES = (KEYS + 4 * ROWS - 1) / (4 * ROWS);
+#pragma unroll
+      for (int i = 0; i < PASSES; ++i) {
+        const int row = (i * 4 + cw) * ROWS + sub;
+        if (KEYS % (4 * ROWS) == 0 || row < KEYS) {
+          const uint4 x = lds128(raw + row * HD);
+          const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
+          uint32_t h[8];
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            h[2 * b] = bytes02_to_half2(xw[b]);
+            h[2 * b + 1] = bytes02_to_half2(xw[b] >> 8);
+          }
+          store_row_16(tile, L::kAtomBytes, row, chunk, h);
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      mbar_arrive_if(&raw_empty[st], lane == 0);
+      mbar_arrive_if(full, lane == 0);
+      ++r;
+      return true;
+    };
+    auto queries = [&](const ChunkItem& u, int t) {
+      const uint32_t slot = qn & 1u;
+      constexpr int PASSES = 128 / (4 * ROWS), BATCH = 4;
+#pragma unroll 1
+      for (int i0 = 0; i0 < PASSES; i0 += BATCH) {
+        uint4 x[BATCH][2];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+          const int row = ((i0 + i) * 4 + cw) * ROWS + sub, row_tok = row / p.group, tok = u.tok0 + t * p.tile_tokens + row_tok;
+          x[i][0] = x[i][1] = make_uint4(0u, 0u, 0u, 0u);
+          if (row_tok < p.tile_tokens && tok < u.n_tok) {
+            const uint4* src = reinterpret_cast<const uint4*>(p.q + static_cast<long long>(u.q0 + tok) * p.ld_q + (u.head * p.group + row - row_tok * p.group) * HD + chunk * 16);
+            x[i][0] = src[0];
+            x[i][1] = src[1];
+          }
+        }
+        if (i0 == 0 && !warp_mbar_wait(&q_empty[slot], ((qn >> 1) & 1u) ^ 1u, abort_flag)) return false;
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+          const int row = ((i0 + i) * 4 + cw) * ROWS + sub;
+          const uint32_t xw[8] = {x[i][0].x, x[i][0].y, x[i][0].z, x[i][0].w, x[i][1].x, x[i][1].y, x[i][1].z, x[i][1].w};
+          float y[16];
+#pragma unroll
+          for (int b = 0; b < 8; ++b) {
+            y[2 * b] = load16(static_cast<uint16_t>(xw[b] & 0xFFFFu), p.fp16);
+            y[2 * b + 1] = load16(static_cast<uint16_t>(xw[b] >> 16), p.fp16);
+          }
+          float mx = 0.f;
+#pragma unroll
+          for (int b = 0; b < 16; ++b) mx = fmaxf(mx, fabsf(y[b]));
+#pragma unroll
+          for (int d = 1; d < CHUNKS; d *= 2) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+          // the largest of the row to [1, 2), by an exponent of -126 to 126, so that both powers are normal numbers (see attention_cache.cuh)
+          const int e = mx > 0.f ? min(max(static_cast<int>(__float_as_uint(mx) >> 23) - 127, -126), 126) : 0;
+          const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23), up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+          uint32_t h[8];
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            h[2 * b] = Pair16<__half>::pack(y[4 * b] * down, y[4 * b + 2] * down);
+            h[2 * b + 1] = Pair16<__half>::pack(y[4 * b + 1] * down, y[4 * b + 3] * down);
+          }
+          store_row_16(q_tile(slot), L::kQHalf, row, chunk, h);
+          // (an infinite element makes the row NaN: of -Inf alone its scores would count as masked)
+          if (chunk == 0) row_factor[slot * 128 + row] = mx == INFINITY ? __uint_as_float(0x7FFFFFFFu) : p.scale_log2 * up;
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      mbar_arrive_if(&q_full[slot], lane == 0);
+      ++qn;
+      return true;
+    };
+    while (ok) {
+      ChunkItem it;
+      ok = take(it);
+      if (!ok || it.n == 0) break;
+      const int n = it.n;
+      for (int t = 0; t < it.tiles && ok; ++t) ok = queries(it, t);
+      for (int j = -1; j < n && ok; ++j) {
+        if (j + 1 < n) {
+          ok = convert(k_tile(k_at), &k_full[k_at % NK], &k_empty[k_at % NK], k_at / NK);
+          ++k_at;
+        }
+        if (j >= 0 && ok) {
+          ok = convert(v_tile(v_at), &v_full[v_at % NV], &v_empty[v_at % NV], v_at / NV);
+          ++v_at;
+        }
+      }
+    }
+  } else {
+    // ------------------------------------------------------------------ softmax warpgroups
+    setmaxnreg_inc<L::kRegsSoftmax>();
+    const int w = (warp - 8) >> 2, quarter = warp & 3;                     // (the quarter of the tensor memory's lanes that the warp reads)
+    const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
+    const uint32_t s_addr = lane_addr + L::kSCol0 + w * L::kSStride, p_addr = s_addr + KEYS, o_addr = lane_addr + w * HD;
+    const int row = quarter * 32 + lane, row_tok = row / p.group, row_head = row - row_tok * p.group;
+    uint32_t base = 0, qn = 0, n_s = 0, n_met = 0;                         // steps of the CTA, query tiles, the warpgroup's steps, meetings
+    bool ok = true;
+    while (ok) {
+      ChunkItem u;
+      ok = take(u);
+      if (!ok || u.n == 0) break;
+      const int n = u.n, tiles = u.tiles;
+      const bool alternate = tiles == 1;
+      const int first = alternate ? w : 0, stride = alternate ? 2 : 1;
+      const int mine = alternate ? n : w == 0 ? u.mine[0] : u.mine[1];
+      const uint32_t slot = (qn + (alternate ? 0 : w)) & 1u;
+      float factor = 0.f;
+      for (int t = 0; t < tiles && ok; ++t) {
+        const uint32_t q = qn + t;
+        ok = warp_mbar_wait(&q_full[q & 1u], (q >> 1) & 1u, abort_flag);
+        if (!ok) break;
+        if ((q & 1u) == slot) factor = row_factor[slot * 128 + row];
+        __syncwarp();
+        mbar_arrive_if(&q_empty[q & 1u], lane == 0);
+      }
+      qn += tiles;
+      if (!ok) break;
+      const int tok = u.tok0 + (alternate ? 0 : w) * p.tile_tokens + row_tok;
+      const bool stored = row_tok < p.tile_tokens && tok < u.n_tok;
+      const int limit = stored ? u.ahead + tok + 1 : 0x7fffffff;       // tokens that this row sees (rows that are not stored: all, for what they compute does not matter)
+      float m_ref = -INFINITY;
+      uint64_t l2 = 0;                             // row sum, two halves
+      bool any = false;                            // the warpgroup has a step of the item
+#pragma unroll 1
+      for (int j = first; j < mine; j += stride) {
+        const uint32_t g = base + j;
+        if (!warp_mbar_wait(&s_full[w], n_s & 1u, abort_flag)) { ok = false; break; }
+        ++n_s;
+        tc_fence_after_sync();
+        uint32_t s[KEYS];
+        tmem_ld_32x32_at<0>(s_addr, s);
+        tmem_ld_32x32_at<32>(s_addr, s);
+        tmem_ld_32x16_at<64>(s_addr, s);
+        if (!warp_mbar_wait(&sc_full[g % NS], (g / NS) & 1u, abort_flag)) { ok = false; break; }
+        float sc[16];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float4 x = reinterpret_cast<const float4*>(sc_ring + (g % NS) * 16)[i];
+          sc[4 * i] = x.x; sc[4 * i + 1] = x.y; sc[4 * i + 2] = x.z; sc[4 * i + 3] = x.w;
+        }
+        tmem_ld_wait_16<0>(s); tmem_ld_tie_16<16>(s); tmem_ld_tie_16<32>(s); tmem_ld_tie_16<48>(s); tmem_ld_tie_16<64>(s);
+        tc_fence_before_sync();
+        __syncwarp();
+        mbar_arrive_if(&s_free[w], lane == 0);
+        const int left = limit - (u.lo + j) * KEYS;           // keys of the step that the row sees
+        const bool masked = __any_sync(0xffffffffu, left < KEYS);
+        // largest t: of each 16 scores the largest, scaled
+        float mx = -INFINITY;
+#pragma unroll
+        for (int m = 0; m < PARTS; ++m) {
+          if (masked) {
+#pragma unroll
+            for (int i = 16 * m; i < 16 * m + 16; ++i) if (i >= left) s[i] = 0xff800000u;   // -inf
+          }
+          float c0 = -INFINITY, c1 = -INFINITY;
+#pragma unroll
+          for (int i = 16 * m; i < 16 * m + 16; i += 4) {
+            c0 = fmax3(c0, __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
+            c1 = fmax3(c1, __uint_as_float(s[i + 2]), __uint_as_float(s[i + 3]));
+          }
+          sc[m] *= factor;
+          const float t = fmaf(fmaxf(c0, c1), sc[m], sc[PARTS + m]);
+          if (masked && 16 * m >= left) {                        // (a hidden block's scale may be anything)
+            sc[m] = 1.f;
+            sc[PARTS + m] = 0.f;
+            sc[2 * PARTS + m] = 0.f;
+          } else {
+            mx = fmaxf(mx, t);
+          }
+        }
+        // the reference moves to 2^7 below the row's largest t when that comes more than 2^15 above it, and to the first one above -inf
+        const float m_old = m_ref;
+        const bool moved = mx > m_ref + kRefMoves;
+        m_ref = moved ? mx - kRefBelow : m_ref;
+        const uint32_t rescale = __ballot_sync(0xffffffffu, moved && any);
+        const float mb = m_ref == -INFINITY ? 0.f : m_ref;
+        const uint32_t pv_ok = any ? mbar_try_wait(&pv_done[w], n_s & 1u) : 1u;      // the previous step's, tested ahead
+        uint64_t sum2 = 0;
+        uint32_t pk[KEYS / 2];
+#pragma unroll
+        for (int m = 0; m < PARTS; ++m) {
+          const uint64_t c2 = pack2(sc[m], sc[m]), b2 = pack2(sc[PARTS + m] - mb, sc[PARTS + m] - mb);
+          uint64_t part2 = 0;
+#pragma unroll
+          for (int i = 8 * m; i < 8 * m + 8; ++i) {
+            float p0, p1;
+            unpack2(ffma2(pack2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c2, b2), p0, p1);
+            if (masked) {                                        // (-inf times a scale of 0 is NaN)
+              if (2 * i >= left) p0 = -INFINITY;
+              if (2 * i + 1 >= left) p1 = -INFINITY;
+            }
+            p0 = fast_ex2(p0);
+            p1 = fast_ex2(p1);
+            part2 = i == 8 * m ? pack2(p0, p1) : fadd2(part2, pack2(p0, p1));
+            pk[i] = Pair16<__half>::pack(p0, p1);
+          }
+          sum2 = ffma2(part2, pack2(sc[2 * PARTS + m], sc[2 * PARTS + m]), sum2);
+        }
+        // P goes where the previous step's was, and O may change: that step's P V has to be complete
+        if (any) {
+          if (!warp_mbar_wait_tested(pv_ok, &pv_done[w], n_s & 1u, abort_flag)) { ok = false; break; }
+          tc_fence_after_sync();
+        }
+        if (__builtin_expect(rescale != 0u, 0)) {
+          const float corr = moved ? fast_ex2(m_old - m_ref) : 1.0f;      // (from no reference: 0)
+          l2 = ffma2(l2, pack2(corr, corr), sum2);
+#pragma unroll 1
+          for (int c = 0; c < HD / 8; ++c) {
+            uint32_t o[8];
+            asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3]), "=r"(o[4]), "=r"(o[5]), "=r"(o[6]), "=r"(o[7]) : "r"(o_addr + c * 8) : "memory");
+            asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(o[0]), "+r"(o[1]), "+r"(o[2]), "+r"(o[3]), "+r"(o[4]), "+r"(o[5]), "+r"(o[6]), "+r"(o[7])::"memory");
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * corr);
+            tmem_st_32x8_from(o_addr + c * 8, o);
+          }
+        } else {
+          l2 = fadd2(l2, sum2);
+        }
+        __syncwarp();
+        tmem_st_32x32_from(p_addr, pk);
+        tmem_st_32x8_from(p_addr + 32, pk + 32);
+        tmem_st_wait();
+        tc_fence_before_sync();
+        __syncwarp();
+        mbar_arrive_if(&p_ready[w], lane == 0);
+        any = true;
+      }
+      base += n;
+      if (!ok) break;
+      // the item's end
+      if (any) {
+        if (!warp_mbar_wait(&pv_done[w], (n_s - 1u) & 1u, abort_flag)) { ok = false; break; }
+        tc_fence_after_sync();
+      }
+      float l, l_hi;
+      unpack2(l2, l, l_hi);
+      l += l_hi;
+      float m = m_ref, f_own = 1.f, f_other = 0.f;
+      bool both = false;
+      if (alternate) {
+        ml_smem[w * 128 + row] = make_float2(m, l);
+        tc_fence_before_sync();
+        __syncwarp();
+        mbar_arrive_if(&met[0], lane == 0);
+        if (!warp_mbar_wait(&met[0], n_met & 1u, abort_flag)) { ok = false; break; }
+        tc_fence_after_sync();
+        const float2 other = ml_smem[(1 - w) * 128 + row];
+        both = n > 1;                              // (of one step: the first warpgroup's alone)
+        const float top = fmaxf(m, other.x);
+        f_own = !any ? 0.f : m == -INFINITY && l == l ? 0.f : fast_ex2(m - top);           // (a row of NaN has no reference either)
+        f_other = !(both || !any) ? 0.f : other.x == -INFINITY && other.y == other.y ? 0.f : fast_ex2(other.x - top);
+        l = (any ? l * f_own : 0.f) + (both || !any ? other.y * f_other : 0.f);
+        m = top;
+      }
+      const bool whole = u.slot < 0;
+      const float inv = l == 0.f ? 0.f : kWeightDown / l;
+      const int col0 = alternate ? w * (HD / 2) : 0, cols = alternate ? HD / 2 : HD;
+      const long long part = static_cast<long long>(u.slot) * 2 + (alternate ? 0 : w);
+      uint16_t* dst = p.out + static_cast<long long>(u.q0 + (stored ? tok : 0)) * p.ld_out + (u.head * p.group + row_head) * HD;
+      const uint32_t o_other = lane_addr + (1 - w) * HD;
+      const bool use_own = any, use_other = alternate && (both || !any);
+#pragma unroll 1
+      for (int c = col0; c < col0 + cols; c += 32) {
+        uint32_t o[32], x[32];
+        __syncwarp();
+        if (use_own) tmem_ld_32x32(o_addr + c, o);
+        if (use_other) tmem_ld_32x32(o_other + c, x);
+        tmem_ld_wait_16<0>(o); tmem_ld_tie_16<16>(o);
+        tmem_ld_tie_16<0>(x); tmem_ld_tie_16<16>(x);
+        float y[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          const float a = use_own ? __uint_as_float(o[i]) * f_own : 0.f;
+          const float v = use_other ? fmaf(__uint_as_float(x[i]), f_other, a) : a;
+          y[(i & ~3) | ((i & 1) << 1) | ((i >> 1) & 1)] = v;     // four dimensions lie in the order 0, 2, 1, 3
+        }
+        if (stored && whole) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 8) {
+            uint32_t z[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              z[e] = p.fp16 ? Pair16<__half>::pack(y[i + 2 * e] * inv, y[i + 2 * e + 1] * inv) : Pair16<bf16>::pack(y[i + 2 * e] * inv, y[i + 2 * e + 1] * inv);
+            *reinterpret_cast<uint4*>(dst + c + i) = make_uint4(z[0], z[1], z[2], z[3]);
+          }
+        } else if (stored) {
+          float4* to = p.o_ws + (part * (HD / 4) + c / 4) * p.ws_rows + row;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) to[i * p.ws_rows] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+        }
+      }
+      if (stored && !whole && (!alternate || w == 0)) p.ml_ws[part * p.ws_rows + row] = make_float2(l == 0.f ? -INFINITY : m, l);
+      if (alternate) {
+        tc_fence_before_sync();
+        __syncwarp();
+        mbar_arrive_if(&met[1], lane == 0);
+        if (!warp_mbar_wait(&met[1], n_met & 1u, abort_flag)) { ok = false; break; }
+        tc_fence_after_sync();
+        ++n_met;
+      }
+    }
+  }
+
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 3) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem_base, 512);
+  }
+  if (threadIdx.x == 0 && *abort_flag) atomicCAS(p.status, DEV_OK, DEV_ERR_WAIT_TIMEOUT);
+}
+
+// The parts of cut units put together, in order: 128 threads, one a row, per (cut, tile, 8 columns), a unit being taken care of at the first cut in it.  Then the rows
+// that see nothing.
+template <int HD>
+__global__ void __launch_bounds__(512, 1) chunk_join_kernel(const __grid_constant__ ChunkParams p) {
+  constexpr int COLS = 8, CHUNKS = HD / COLS, BATCH = 8;
+  __shared__ long long prefix[kChunkMaxSeqs + 2], sums[16];
+  // On the whole device this kernel starts beside the one before it, which has let it go behind its own wait: the lengths are final
+  if (!p.early_launch) pdl_wait();
+  chunk_prefix(p, prefix, sums, false);
+  const ChunkLine line(prefix[p.n_seqs], p.n_ctas);
+  const int row = threadIdx.x & 127, row_tok = row / p.group, row_head = row - row_tok * p.group;
   pdl_wait();
   if (p.early_launch) pdl_launch_dependents();
-  const int heads = p.c.n_kv * p.group, t = threadIdx.x;
-  auto cu = [&](int i) { return min(max(p.cu[i], 0), p.n_rows); };
-  for (long long u = blockIdx.x; u < static_cast<long long>(p.n_rows) * heads; u += gridDim.x) {
-    const int row = static_cast<int>(u / heads), h = static_cast<int>(u - static_cast<long long>(row) * heads), kvh = h / p.group;
-    int s = 0, hi = p.n_seqs - 1;
-    while (s < hi) {
-      const int mid = (s + hi + 1) >> 1;
-      if (cu(mid) <= row) s = mid; else hi = mid - 1;
-    }
-    const int first = cu(s), n = cu(s + 1) - first;
-    if (row < first || row >= first + n) continue;
-    const long long most = static_cast<long long>(p.max_blocks) << p.c.bs_log2;
-    const int len = static_cast<int>(min(static_cast<long long>(max(p.seq_lens[s], 0)), most));
-    if (t == 0 && (n > p.max_new || p.seq_lens[s] > most)) raise_status(p.status, DEV_ERR_CACHE_RANGE);
-    if (n > p.max_new) continue;
-    const int limit = len - n + row - first + 1;
-    __syncthreads();
-    for (int i = t; i < HD; i += 128) q[i] = load16(p.q[row * p.ld_q + h * HD + i], p.fp16);
-    float m = -INFINITY, l = 0.f, o = 0.f;
-    for (int base = 0; base < limit; base += 128) {
-      float x = -INFINITY;
-      int id = -1;
-      float v_scale = 0.f;
-      if (base + t < limit) {
-        id = p.table[s * p.ld_table + ((base + t) >> p.c.bs_log2)];
-        if (static_cast<uint32_t>(id) >= static_cast<uint32_t>(p.c.n_blocks)) {
-          raise_status(p.status, DEV_ERR_CACHE_RANGE);
-          id = -1;
+  for (int it = blockIdx.x * 4 + (threadIdx.x >> 7); line.total > 0 && it < (line.pieces - 1) * 2 * CHUNKS; it += gridDim.x * 4) {
+    const int cut = it / (2 * CHUNKS) + 1, t = it / CHUNKS % 2, col0 = it % CHUNKS * COLS;      // (the tiles of a cut side by side)
+    ChunkUnit u;
+    const long long at = line.begin(cut);
+    u.find(p, prefix, at);
+    const int first_step = u.step_at(at);
+    if (t >= u.tiles || first_step == 0 || first_step == u.steps || u.step_at(line.begin(cut - 1)) != 0) continue;      // (not cut here, or not for the first time)
+    const int tok = (2 * u.j + t) * p.tile_tokens + row_tok;
+    if (row_tok >= p.tile_tokens || tok >= u.seq.n) continue;
+    int last = cut;                                                // the piece that has the unit's end
+    while (last + 1 < line.pieces && u.step_at(line.begin(last + 1)) < u.steps) ++last;
+    float m = -INFINITY, l = 0.f, acc[COLS];
+#pragma unroll
+    for (int i = 0; i < COLS; ++i) acc[i] = 0.f;
+    const int parts = last - cut + 2;                              // of pieces cut - 1 .. last
+    for (int b = 0; b < parts; b += BATCH) {
+      float ml[BATCH][2], x[BATCH][COLS];
+#pragma unroll
+      for (int e = 0; e < BATCH; ++e) {
+        ml[e][0] = -INFINITY;
+        ml[e][1] = 0.f;
+        const int piece = cut - 1 + b + e;
+        if (b + e < parts && u.step_at(line.begin(piece)) < u.step_at(line.begin(piece + 1)) ) {
+          const long long slot = (2LL * piece + (piece == last ? 0 : 1)) * 2 + t;
+          load_floats<2>(reinterpret_cast<const float*>(p.ml_ws + slot * p.ws_rows + row), ml[e]);
+          const float4* o = p.o_ws + (slot * (HD / 4) + col0 / 4) * p.ws_rows + row;
+          float y[4];
+          load_floats<4>(reinterpret_cast<const float*>(o), y);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[e][i] = y[i];
+          load_floats<4>(reinterpret_cast<const float*>(o + p.ws_rows), y);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[e][4 + i] = y[i];
         }
       }
-      __syncthreads();
-      if (id >= 0) {
-        const long long at = static_cast<long long>(id) * p.c.n_kv + kvh;
-        const int8_t* k = p.c.k + ((at << p.c.bs_log2) + ((base + t) & ((1 << p.c.bs_log2) - 1))) * HD;
-        float d = 0.f;
-        for (int i = 0; i < HD; ++i) d = fmaf(q[i], static_cast<float>(k[i]), d);
-        x = d * p.c.k_scale[at] * p.scale_log2;
-        v_scale = p.c.v_scale[at];
-      }
-      w[t] = x;
-      vs[t] = v_scale;
-      ids[t] = id;
-      __syncthreads();
       float top = m;
-      for (int i = 0; i < 128; ++i) top = fmaxf(top, w[i]);
-      const float corr = m == -INFINITY ? 0.f : fast_ex2(m - top);
+#pragma unroll
+      for (int e = 0; e < BATCH; ++e) top = fmaxf(top, ml[e][0]);
+      const float old = m == -INFINITY ? 0.f : fast_ex2(m - top);
+      if (l == l) l *= old;
+#pragma unroll
+      for (int i = 0; i < COLS; ++i) acc[i] *= old;
       m = top;
-      l *= corr;
-      o *= corr;
-      for (int i = 0; i < 128 && base + i < limit; ++i) {
-        if (ids[i] < 0) continue;
-        const float e = fast_ex2(w[i] - m);
-        l += e;
-        if (t < HD) {
-          const long long at = static_cast<long long>(ids[i]) * p.c.n_kv + kvh;
-          o = fmaf(e * vs[i], static_cast<float>(p.c.v[((at << p.c.bs_log2) + ((base + i) & ((1 << p.c.bs_log2) - 1))) * HD + t]), o);
-        }
+#pragma unroll
+      for (int e = 0; e < BATCH; ++e) {
+        const bool any = ml[e][1] != 0.f;                          // (NaN: yes)
+        const float f = !any ? 0.f : ml[e][1] == ml[e][1] ? fast_ex2(ml[e][0] - m) : ml[e][1];
+        if (any) l = fmaf(ml[e][1], f, l);
+#pragma unroll
+        for (int i = 0; i < COLS; ++i) acc[i] = any ? fmaf(x[e][i], f, acc[i]) : acc[i];
       }
-      __syncthreads();
     }
-    if (t < HD) {
-      const float y = l == 0.f ? 0.f : o / l;
-      p.out[row * p.ld_out + h * HD + t] = static_cast<uint16_t>((p.fp16 ? Pair16<__half>::pack(y, 0.f) : Pair16<bf16>::pack(y, 0.f)) & 0xFFFFu);
-    }
+    const float inv = l == 0.f ? 0.f : kWeightDown / l;
+    uint32_t y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      y[e] = p.fp16 ? Pair16<__half>::pack(acc[2 * e] * inv, acc[2 * e + 1] * inv) : Pair16<bf16>::pack(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+    *reinterpret_cast<uint4*>(p.out + static_cast<long long>(u.seq.q0 + tok) * p.ld_out + (u.head * p.group + row_head) * HD + col0) = make_uint4(y[0], y[1], y[2], y[3]);
+  }
+  // rows that see nothing: those in front of a sequence's visible tokens
+  const int lane = threadIdx.x & 31, chunks = p.c.n_kv * p.group * (HD / 8);
+  for (int s = blockIdx.x * 16 + (threadIdx.x >> 5); s < p.n_seqs; s += gridDim.x * 16) {
+    const ChunkSeq seq(p, s, false);
+    const int first = min(max(p.cu[s], 0), p.n_rows), given = min(max(p.cu[s + 1], 0), p.n_rows) - first;
+    if (given > p.max_new) continue;
+    for (int r = first; r < seq.q0; ++r)
+      for (int c = lane; c < chunks; c += 32) *reinterpret_cast<uint4*>(p.out + static_cast<long long>(r) * p.ld_out + c * 8) = make_uint4(0u, 0u, 0u, 0u);
   }
 }
 

@@ -110,22 +110,6 @@ struct AttnRrSmem {
   static_assert(kThreads * kRegsLaunch <= 65536, "registers");
 };
 
-// Wait for this thread's tensor-memory loads, tied to registers they fill so that no use can move ahead of it.
-template <int OFF, int N>
-__device__ __forceinline__ void tmem_ld_wait_16(uint32_t (&r)[N]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[OFF]), "+r"(r[OFF + 1]), "+r"(r[OFF + 2]), "+r"(r[OFF + 3]), "+r"(r[OFF + 4]), "+r"(r[OFF + 5]), "+r"(r[OFF + 6]), "+r"(r[OFF + 7]),
-                 "+r"(r[OFF + 8]), "+r"(r[OFF + 9]), "+r"(r[OFF + 10]), "+r"(r[OFF + 11]), "+r"(r[OFF + 12]), "+r"(r[OFF + 13]), "+r"(r[OFF + 14]), "+r"(r[OFF + 15])
-               ::"memory");
-}
-// ties 16 more registers behind the wait above (no instruction)
-template <int OFF, int N>
-__device__ __forceinline__ void tmem_ld_tie_16(uint32_t (&r)[N]) {
-  asm volatile("" : "+r"(r[OFF]), "+r"(r[OFF + 1]), "+r"(r[OFF + 2]), "+r"(r[OFF + 3]), "+r"(r[OFF + 4]), "+r"(r[OFF + 5]), "+r"(r[OFF + 6]), "+r"(r[OFF + 7]),
-                    "+r"(r[OFF + 8]), "+r"(r[OFF + 9]), "+r"(r[OFF + 10]), "+r"(r[OFF + 11]), "+r"(r[OFF + 12]), "+r"(r[OFF + 13]), "+r"(r[OFF + 14]), "+r"(r[OFF + 15])
-               ::"memory");
-}
-
 struct RrUnit {
   int r0, nt, n_q, head0, n_streams, S, n_kv, row0;
 };

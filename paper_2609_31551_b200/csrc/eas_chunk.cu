@@ -7,7 +7,28 @@
 
 using namespace eas;
 
-static size_t chunk_workspace(const eas_cache* c, int32_t n_seqs, int32_t n_rows, int32_t max_new, int32_t n_heads) { return 256; }
+static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+// scratch of a launch: two parts a piece of the line, two tiles each
+static size_t chunk_workspace(const eas_cache* c, int32_t max_new, int32_t n_heads, int* ws_rows, size_t* ml_off) {
+  const int group = n_heads / c->d.n_kv_heads;
+  *ws_rows = std::min(128 / group, std::max(max_new, 1)) * group;
+  const size_t rows = static_cast<size_t>(4) * c->sm_count * *ws_rows;
+  *ml_off = up256(rows * c->d.head_dim * 4);
+  return *ml_off + up256(rows * 8);
+}
+
+template <int HD>
+static eas_status launch_chunk(const ChunkParams& p, int budget, bool all, cudaStream_t stream) {
+  using L = ChunkCfg<HD>;
+  static OncePerDevice once;
+  if (once.first()) {
+    CUDA_TRY(cudaFuncSetAttribute(chunk_attention_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes));
+    CUDA_TRY(cudaFuncSetAttribute(chunk_join_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, kOnePerSmSmem));
+    once.settled();
+  }
+  EAS_TRY(launch_kernel(chunk_attention_kernel<HD>, std::min(budget, p.n_ctas), L::kThreads, L::kBytes, stream, p));
+  return launch_kernel(chunk_join_kernel<HD>, std::min(budget, p.n_ctas), 512, all ? 0 : kOnePerSmSmem, stream, p);
+}
 
 static eas_status chunk_attention(const eas_cache* c, const eas_cache_seqs* s, const void* q, int64_t ld_q, void* out, int64_t ld_out, int32_t n_rows,
                                   int32_t max_new, int32_t n_heads, int32_t dtype, float scale, void* workspace, size_t workspace_bytes, int32_t sm_budget,
@@ -19,27 +40,38 @@ static eas_status chunk_attention(const eas_cache* c, const eas_cache_seqs* s, c
   if (n_heads <= 0 || n_heads % G != 0) return fail(EAS_ERR_INVALID_ARG, "%d query heads for %d key/value heads", n_heads, G);
   if (n_rows < 0 || max_new < 0) return fail(EAS_ERR_INVALID_ARG, "n_rows %d, max_new %d", n_rows, max_new);
   if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(EAS_ERR_INVALID_ARG, "scale must be positive and finite");
+  if (n_heads / G > 128) return fail(EAS_ERR_UNSUPPORTED, "%d query heads per key/value head (at most 128)", n_heads / G);
   if (s->n_seqs == 0 || n_rows == 0) return EAS_OK;
   if (q == nullptr || out == nullptr || workspace == nullptr) return fail(EAS_ERR_INVALID_ARG, "a required pointer is null");
   if (!aligned16(q) || !aligned16(out)) return fail(EAS_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
   const int64_t w = static_cast<int64_t>(n_heads) * hd;
   if (ld_q < w || ld_out < w || ld_q % 8 != 0 || ld_out % 8 != 0)
     return fail(EAS_ERR_INVALID_ARG, "token distances must be multiples of 8 that hold a token's heads");
-  const size_t need = chunk_workspace(c, s->n_seqs, n_rows, max_new, n_heads);
+  ChunkParams p{};
+  size_t ml_off = 0;
+  const size_t need = chunk_workspace(c, std::min(max_new, n_rows), n_heads, &p.ws_rows, &ml_off);
   if (workspace_bytes < need) return fail(EAS_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, need);
   if ((reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return fail(EAS_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
   if (static_cast<int64_t>(s->max_blocks) * c->d.block_size > 0x7fffffffLL) return fail(EAS_ERR_UNSUPPORTED, "max_blocks %d is too large", s->max_blocks);
-  ChunkParams p{};
   p.c = view_of(c);
-  p.table = s->block_table; p.cu = s->cu_seqlens; p.seq_lens = s->seq_lens;
-  p.ld_table = s->ld_table; p.n_seqs = s->n_seqs; p.max_blocks = s->max_blocks; p.n_rows = n_rows; p.max_new = max_new;
+  p.ld_table = s->ld_table; p.max_blocks = s->max_blocks; p.n_rows = n_rows; p.max_new = max_new;
   p.q = static_cast<const uint16_t*>(q); p.out = static_cast<uint16_t*>(out);
-  p.ld_q = ld_q; p.ld_out = ld_out; p.fp16 = dtype == EAS_DTYPE_FP16; p.group = n_heads / G;
+  p.ld_q = ld_q; p.ld_out = ld_out; p.fp16 = dtype == EAS_DTYPE_FP16; p.group = n_heads / G; p.tile_tokens = 128 / p.group;
+  p.n_ctas = c->sm_count;
   p.scale_log2 = static_cast<float>(scale * kLog2e);
+  p.o_ws = static_cast<float4*>(workspace);
+  p.ml_ws = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + ml_off);
   p.status = status_dev;
-  const int grid = static_cast<int>(std::min<int64_t>(static_cast<int64_t>(n_rows) * n_heads, budget == c->sm_count ? 8 * budget : budget));
-  return hd == 64 ? launch_kernel(chunk_simple_kernel<64>, grid, 128, 0, static_cast<cudaStream_t>(stream), p)
-                  : launch_kernel(chunk_simple_kernel<128>, grid, 128, 0, static_cast<cudaStream_t>(stream), p);
+  const bool all = budget == c->sm_count;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  for (int first = 0; first < s->n_seqs; first += kChunkMaxSeqs) {
+    p.n_seqs = std::min(kChunkMaxSeqs, s->n_seqs - first);
+    p.table = s->block_table + first * s->ld_table;
+    p.cu = s->cu_seqlens + first;
+    p.seq_lens = s->seq_lens + first;
+    EAS_TRY(hd == 64 ? launch_chunk<64>(p, budget, all, st) : launch_chunk<128>(p, budget, all, st));
+  }
+  return EAS_OK;
 }
 
 extern "C" size_t eas_cache_chunk_workspace_bytes(const eas_cache* cache, int32_t n_seqs, int32_t n_rows, int32_t max_new, int32_t n_heads) {
@@ -47,7 +79,13 @@ extern "C" size_t eas_cache_chunk_workspace_bytes(const eas_cache* cache, int32_
     fail(EAS_ERR_INVALID_ARG, "bad arguments");
     return 0;
   }
-  return chunk_workspace(cache, n_seqs, n_rows, max_new, n_heads);
+  if (n_heads / cache->d.n_kv_heads > 128) {
+    fail(EAS_ERR_UNSUPPORTED, "%d query heads per key/value head (at most 128)", n_heads / cache->d.n_kv_heads);
+    return 0;
+  }
+  int ws_rows = 0;
+  size_t ml_off = 0;
+  return chunk_workspace(cache, std::min(max_new, n_rows), n_heads, &ws_rows, &ml_off);
 }
 
 extern "C" eas_status eas_cache_chunk_attention(const eas_cache* cache, const eas_cache_seqs* seqs, const void* q, int64_t ld_q, void* out, int64_t ld_out,

@@ -250,6 +250,21 @@ __device__ __forceinline__ void tmem_ld_32x32_at(uint32_t taddr, uint32_t (&r)[N
       : "r"(taddr + OFF)
       : "memory");
 }
+// Wait for this thread's tensor-memory loads, tied to registers they fill so that no use can move ahead of it.
+template <int OFF, int N>
+__device__ __forceinline__ void tmem_ld_wait_16(uint32_t (&r)[N]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[OFF]), "+r"(r[OFF + 1]), "+r"(r[OFF + 2]), "+r"(r[OFF + 3]), "+r"(r[OFF + 4]), "+r"(r[OFF + 5]), "+r"(r[OFF + 6]), "+r"(r[OFF + 7]),
+                 "+r"(r[OFF + 8]), "+r"(r[OFF + 9]), "+r"(r[OFF + 10]), "+r"(r[OFF + 11]), "+r"(r[OFF + 12]), "+r"(r[OFF + 13]), "+r"(r[OFF + 14]), "+r"(r[OFF + 15])
+               ::"memory");
+}
+// ties 16 more registers behind the wait above (no instruction)
+template <int OFF, int N>
+__device__ __forceinline__ void tmem_ld_tie_16(uint32_t (&r)[N]) {
+  asm volatile("" : "+r"(r[OFF]), "+r"(r[OFF + 1]), "+r"(r[OFF + 2]), "+r"(r[OFF + 3]), "+r"(r[OFF + 4]), "+r"(r[OFF + 5]), "+r"(r[OFF + 6]), "+r"(r[OFF + 7]),
+                    "+r"(r[OFF + 8]), "+r"(r[OFF + 9]), "+r"(r[OFF + 10]), "+r"(r[OFF + 11]), "+r"(r[OFF + 12]), "+r"(r[OFF + 13]), "+r"(r[OFF + 14]), "+r"(r[OFF + 15])
+               ::"memory");
+}
 __device__ __forceinline__ float fmax3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));

@@ -121,6 +121,45 @@ def bench_rows(a):
             "gbs": 6.0 * a.kv_heads * a.head_dim * T / ms / 1e6}
 
 
+def bench_chunk(a):
+    """--lens: cached tokens of each sequence, the new ones among them; --new: new tokens of each."""
+    lens, cache, table, dtype = _bench_cache(a)
+    new = [min(a.new, n) for n in lens]
+    q = torch.randn(sum(new), a.heads, a.head_dim, device="cuda").to(dtype)
+    held, out = torch.tensor(lens, dtype=torch.int32, device="cuda"), torch.empty_like(q)
+    cu = torch.tensor(np.concatenate([[0], np.cumsum(new)]), dtype=torch.int32, device="cuda")
+    ws = torch.empty(cache.chunk_workspace_bytes(len(lens), sum(new), max(new), a.heads), dtype=torch.uint8, device="cuda")
+    ms = _time(lambda: cache.chunk_attention(q, cu, held, table, max_new=max(new), out=out, workspace=ws, sm_budget=a.sm_budget), a.iters, a.warmup)
+    cache.check()
+    seen = sum(n * (h - n) + n * (n + 1) // 2 for n, h in zip(new, lens))
+    return {"kernel": "chunk", "lens": a.lens, "new": a.new, "heads": a.heads, "kv_heads": a.kv_heads, "head_dim": a.head_dim, "block": a.block,
+            "sm_budget": a.sm_budget, "ms": ms, "gbs": 2.0 * a.kv_heads * a.head_dim * sum(lens) / ms / 1e6, "tflops": 4.0 * a.heads * a.head_dim * seen / ms / 1e9}
+
+
+def bench_rotary(a):
+    """rotate: --lens tokens of queries and keys; append: the same into the cache behind --before tokens of each sequence."""
+    new = _lens(a.lens)
+    a.lens = ",".join(str(n + a.before) for n in new)
+    held, cache, table, dtype = _bench_cache(a)
+    T = sum(new)
+    qkv = torch.randn(T, a.heads + 2 * a.kv_heads, a.head_dim, device="cuda").to(dtype)
+    q, k, v = qkv[:, :a.heads], qkv[:, a.heads:a.heads + a.kv_heads], qkv[:, a.heads + a.kv_heads:]
+    quarter = a.head_dim // 8
+    rotary = L.Rotary(a.head_dim, base=1e6, sections=(2 * quarter, quarter, quarter))
+    positions = torch.randint(0, 30000, (3, T), dtype=torch.int32, device="cuda")
+    out = torch.empty_like(q, memory_format=torch.contiguous_format), torch.empty_like(k, memory_format=torch.contiguous_format)
+    if a.which == "rotate":
+        ms = _time(lambda: rotary.apply(q, k, positions, out=out, sm_budget=a.sm_budget), a.iters, a.warmup)
+    else:
+        cu = torch.tensor(np.concatenate([[0], np.cumsum(new)]), dtype=torch.int32, device="cuda")
+        start = torch.full((len(new),), a.before, dtype=torch.int32, device="cuda")
+        ms = _time(lambda: cache.append(q, k, v, cu, start, table, rotary, positions, out=out[0], sm_budget=a.sm_budget), a.iters, a.warmup)
+        cache.check()
+    width = 4.0 * (a.heads + a.kv_heads) if a.which == "rotate" else 4.0 * a.heads + 6.0 * a.kv_heads
+    return {"kernel": a.which, "tokens": T, "before": a.before, "heads": a.heads, "kv_heads": a.kv_heads, "head_dim": a.head_dim, "block": a.block,
+            "sm_budget": a.sm_budget, "ms": ms, "gbs": width * a.head_dim * T / ms / 1e6}
+
+
 def bench_attention(a):
     lens = _lens(a.lens)
     T, d = sum(lens), a.heads * a.head_dim
@@ -134,7 +173,7 @@ def bench_attention(a):
 def main():
     ap = argparse.ArgumentParser()
     sub = ap.add_subparsers(dest="which", required=True)
-    for name in ("gemm", "norm", "attention", "prompt", "token", "store", "load"):
+    for name in ("gemm", "norm", "attention", "prompt", "token", "store", "load", "chunk", "rotate", "append"):
         sp = sub.add_parser(name)
         sp.add_argument("--iters", type=int, default=20)
         sp.add_argument("--warmup", type=int, default=3)
@@ -147,15 +186,16 @@ def main():
             sp.add_argument("--rows", type=int, default=18464); sp.add_argument("--d", type=int, default=1024)
             sp.add_argument("--kind", type=int, default=0)
         elif name != "attention":
-            sp.add_argument("--lens", default="4096x64" if name == "token" else "2048x8"); sp.add_argument("--heads", type=int, default=32)
+            sp.add_argument("--lens", default="4096x64" if name in ("token", "chunk") else "2048x8"); sp.add_argument("--heads", type=int, default=32)
             sp.add_argument("--kv-heads", type=int, default=8); sp.add_argument("--head-dim", type=int, default=128)
             sp.add_argument("--block", type=int, default=64); sp.add_argument("--before", type=int, default=0); sp.add_argument("--fp16", action="store_true")
+            sp.add_argument("--new", type=int, default=4)
         else:
             sp.add_argument("--lens", default="577x32"); sp.add_argument("--heads", type=int, default=16)
             sp.add_argument("--head-dim", type=int, default=64); sp.add_argument("--impl", type=int, default=0)
     a = ap.parse_args()
     res = {"gemm": bench_gemm, "norm": bench_norm, "attention": bench_attention, "prompt": bench_prompt, "token": bench_token, "store": bench_rows,
-           "load": bench_rows}[a.which](a)
+           "load": bench_rows, "chunk": bench_chunk, "rotate": bench_rotary, "append": bench_rotary}[a.which](a)
     print(json.dumps(res))
 
 
