@@ -20,6 +20,8 @@
 // piece is the end of a unit, whole units, the beginning of one; cut units leave (m, l, O) in the workspace, and chunk_join_kernel puts them together in order.
 // Lengths are read on the device: each CTA sums them up itself.
 #pragma once
+#include <type_traits>
+
 #include "attention_cache.cuh"
 #include "kv_cache.cuh"
 #include "ptx.cuh"
@@ -61,7 +63,7 @@ struct ChunkCfg {
   static constexpr int kRawBytes = kChunkKeys * HD;
   static constexpr int kKOff = 2 * kQBytes, kVOff = kKOff + kKTiles * kTileBytes, kRawOff = kVOff + kVTiles * kTileBytes;
   static constexpr int kPrefixOff = kRawOff + kRawTiles * kRawBytes;
-  static constexpr int kScaleSlots = 16;
+  static constexpr int kScaleSlots = 32;
   static constexpr int kScaleOff = kPrefixOff + (kChunkMaxSeqs + 2) * 8;               // [slot][16]: key scales, log2 of value scales, their inverses
   static constexpr int kRowOff = kScaleOff + kScaleSlots * 64;                         // [2][128] factors of the rows' scores
   static constexpr int kMlOff = kRowOff + 2 * 128 * 4;                                 // [2][128] reference and sum of a warpgroup's rows
@@ -75,8 +77,8 @@ struct ChunkCfg {
   static_assert(kQBytes % 1024 == 0 && kAtomBytes % 1024 == 0, "tiles start on swizzle-atom boundaries");
   static_assert(kSCol0 + 2 * kSStride <= 512, "tensor memory columns");
   static_assert(kRegsLight + kRegsConvert + 2 * kRegsSoftmax <= 4 * kRegsLaunch, "setmaxnreg budget exceeds the CTA's register allocation");
-  // the producer is at most this many steps ahead of the softmax: raw tiles, converted K tiles, one step each being read
-  static_assert(kRawTiles / 2 + 1 + kKTiles + 4 <= kScaleSlots, "a step's scales are read before their slot is filled again");
+  // the producer is at most this many steps ahead of the softmax: a batch of scales, raw tiles, converted K tiles, one step each being read
+  static_assert(6 + kRawTiles / 2 + 1 + kKTiles + 4 <= kScaleSlots, "a step's scales are read before their slot is filled again");
 };
 
 // ------------------------------------------------------------------------------------ the line of units
@@ -261,18 +263,18 @@ __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint3
 __host__ __device__ constexpr uint32_t make_idesc_f16(int m, int n, int a_mn, int b_mn) {
   return make_idesc_bf16(m, n, a_mn, b_mn) & ~((1u << 7) | (1u << 10));
 }
-// 16 fp16 dimensions 16 c .. of row r of a tile whose rows are 128 bytes an atom of 64 dimensions, 128-byte swizzle.  Lanes with c >= 4 (the second atom) store
-// their second chunk first, so that the eight lanes of a row touch all banks.
+// Which row of ROWS and which 16 dimensions a lane takes, so that the eight lanes that go together read 128 bytes side by side, or two rows' different
+// halves, and store (below) to all banks
+template <int HD>
+__device__ __forceinline__ int2 lane_place(int lane) {             // (row, chunk)
+  if constexpr (HD == 64) return make_int2(lane >> 2, lane & 3);
+  else return make_int2(((lane >> 2) & 1) | ((lane >> 4) << 1), (lane & 3) | ((((lane >> 2) ^ (lane >> 3)) & 1) << 2));
+}
+// 16 fp16 dimensions 16 c .. of row r of a tile whose rows are 128 bytes an atom of 64 dimensions, 128-byte swizzle
 __device__ __forceinline__ void store_row_16(uint32_t tile, uint32_t atom_bytes, int r, int c, const uint32_t (&h)[8]) {
-  const uint32_t base = tile + (c >> 2) * atom_bytes + r * 128;
-  const int first = c >> 2, a = (2 * (c & 3) + first) ^ (r & 7), b = (2 * (c & 3) + 1 - first) ^ (r & 7);
-  if (first) {
-    sts128(base + a * 16, h[4], h[5], h[6], h[7]);
-    sts128(base + b * 16, h[0], h[1], h[2], h[3]);
-  } else {
-    sts128(base + a * 16, h[0], h[1], h[2], h[3]);
-    sts128(base + b * 16, h[4], h[5], h[6], h[7]);
-  }
+  const uint32_t at = tile + (c >> 2) * atom_bytes + r * 128 + (((2 * (c & 3)) ^ (r & 7)) << 4);
+  sts128(at, h[0], h[1], h[2], h[3]);
+  sts128(at ^ 16, h[4], h[5], h[6], h[7]);
 }
 
 // ------------------------------------------------------------------------------------ the kernel
@@ -401,41 +403,32 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
         if (!ok || it.n == 0) break;
         const int lo = it.lo, n = it.n, seen = it.seen, head = it.head;
         const int32_t* ids = p.table + it.s * p.ld_table;
-        auto load_id = [&](int j) {                // lane m < PARTS: the block of tokens 16 m .. of step j
-          int id = -1;
-          const int tok = (lo + j) * KEYS + lane * 16;
-          if (lane < PARTS && j < n && tok < seen) {
-            id = ids[tok >> p.c.bs_log2];
-            if (static_cast<uint32_t>(id) >= static_cast<uint32_t>(p.c.n_blocks)) {
-              raise_status(p.status, DEV_ERR_CACHE_RANGE);
-              id = -1;
-            }
-          }
-          return id;
+        // Block numbers and scales of kBatch steps at once, a part of 16 tokens a lane, asked for one or two batches ahead: they come from anywhere in memory
+        constexpr int kBatch = 6;
+        static_assert(kBatch * PARTS <= 32, "a lane has a part");
+        auto load_ids = [&](int j0) {              // lane m: the block of tokens 16 m .. of steps j0 ..
+          const int tok = (lo + j0) * KEYS + lane * 16;
+          return lane < kBatch * PARTS && j0 + lane / PARTS < n && tok < seen ? ids[tok >> p.c.bs_log2] : -1;
         };
-        auto copy = [&](const int8_t* from, int id, int j) {
-          const uint32_t st = r % NR, have = __ballot_sync(0xffffffffu, id >= 0);
+        auto checked = [&](int id, int j0) {       // (where the number is wanted, not where it is asked for)
+          if (static_cast<uint32_t>(id) < static_cast<uint32_t>(p.c.n_blocks)) return id;
+          if (lane < kBatch * PARTS && j0 + lane / PARTS < n && (lo + j0) * KEYS + lane * 16 < seen) raise_status(p.status, DEV_ERR_CACHE_RANGE);
+          return -1;
+        };
+        auto copy = [&](const int8_t* from, int batch_ids, int at, int j) {      // step j, the batch's step `at`
+          const int id = __shfl_sync(0xffffffffu, batch_ids, (at * PARTS + lane) & 31);
+          const bool there = lane < PARTS && id >= 0;
+          const uint32_t st = r % NR, have = __ballot_sync(0xffffffffu, there);
           if (!warp_mbar_wait(&raw_empty[st], ((r / NR) & 1u) ^ 1u, abort_flag)) return false;
           if (lane == 0) mbar_expect_tx(&raw_full[st], __popc(have) * (16u * HD));
           __syncwarp();
-          if (id >= 0) {
+          if (there) {
             const int place = ((lo + j) * KEYS + lane * 16) & ((1 << p.c.bs_log2) - 1);
             const long long row = ((static_cast<long long>(id) * p.c.n_kv + head) << p.c.bs_log2) + place;
             bulk_load(smem + L::kRawOff + st * L::kRawBytes + lane * 16 * HD, from + row * HD, 16 * HD, &raw_full[st]);
           }
           ++r;
           return true;
-        };
-        auto publish = [&](float2 sc, int id, uint32_t step) {
-          float* dst = sc_ring + (step % NS) * 16;
-          if (lane < PARTS) {
-            const float vs = sc.y < kCacheMinScale ? kCacheMinScale : sc.y, lg = fast_lg2(vs);      // (a NaN stays)
-            dst[lane] = id >= 0 ? sc.x : 0.f;
-            dst[PARTS + lane] = id >= 0 ? lg : -INFINITY;
-            dst[2 * PARTS + lane] = id >= 0 ? fast_ex2(-lg) * kWeightDown : 0.f;
-          }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&sc_full[step % NS]);
         };
         auto load_scales = [&](int id) {
           float2 sc = make_float2(0.f, 0.f);
@@ -445,17 +438,35 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
           }
           return sc;
         };
-        int id_v = load_id(0), id_k = load_id(1);  // of step j, whose V is next, and of the step behind it
-        ok = copy(p.c.k, id_v, 0);
-        float2 sc = load_scales(id_v);
-        for (int j = 0; j < n && ok; ++j, ++g) {
-          const int id_next = load_id(j + 2);
-          const float2 sc_next = load_scales(id_k);
-          publish(sc, id_v, g);
-          if (j + 1 < n) ok = copy(p.c.k, id_k, j + 1);
-          ok = ok && copy(p.c.v, id_v, j);
-          id_v = id_k;
-          id_k = id_next;
+        auto publish = [&](float2 sc, int id, uint32_t step, int steps) {
+          if (lane < steps * PARTS) {
+            float* dst = sc_ring + (step + lane / PARTS) % NS * 16 + lane % PARTS;
+            const float vs = sc.y < kCacheMinScale ? kCacheMinScale : sc.y, lg = fast_lg2(vs);      // (a NaN stays)
+            dst[0] = id >= 0 ? sc.x : 0.f;
+            dst[PARTS] = id >= 0 ? lg : -INFINITY;
+            dst[2 * PARTS] = id >= 0 ? fast_ex2(-lg) * kWeightDown : 0.f;
+          }
+          __syncwarp();
+          if (lane < steps) mbar_arrive(&sc_full[(step + lane) % NS]);
+        };
+        int now = load_ids(0), next = load_ids(kBatch);
+        now = checked(now, 0);
+        ok = copy(p.c.k, now, 0, 0);
+        float2 sc = load_scales(now);
+        for (int j0 = 0; j0 < n && ok; j0 += kBatch) {
+          const int behind = load_ids(j0 + 2 * kBatch);
+          next = checked(next, j0 + kBatch);
+          const float2 sc_next = load_scales(next);
+          const int steps = min(kBatch, n - j0);
+#pragma unroll 1
+          for (int i = 0; i < 2 * steps && ok; ++i) {              // K of step j + 1, V of step j
+            const int at = (i >> 1) + (i & 1 ? 0 : 1), j = j0 + at;
+            if (j < n) ok = copy(i & 1 ? p.c.v : p.c.k, at < kBatch ? now : next, at < kBatch ? at : 0, j);
+            if (i == 1) publish(sc, now, g, steps);
+          }
+          g += steps;
+          now = next;
+          next = behind;
           sc = sc_next;
         }
         if (!ok) break;
@@ -564,7 +575,8 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
     setmaxnreg_dec<L::kRegsConvert>();
     const int cw = warp - 4;
     constexpr int CHUNKS = HD / 16, ROWS = 32 / CHUNKS;                    // 16 dimensions a lane, rows a warp takes at once
-    const int chunk = lane % CHUNKS, sub = lane / CHUNKS;
+    const int2 place = lane_place<HD>(lane);
+    const int sub = place.x, chunk = place.y;
     uint32_t r = 0, k_at = 0, v_at = 0, qn = 0;
     bool ok = true;
     auto convert = [&](uint32_t tile, uint64_t* full, uint64_t* empty, uint32_t use) {      // the next raw tile
@@ -572,12 +584,14 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       if (!warp_mbar_wait(&raw_full[st], (r / NR) & 1u, abort_flag) || !warp_mbar_wait(empty, (use & 1u) ^ 1u, abort_flag)) return false;
       const uint32_t raw = smem_at + L::kRawOff + st * L::kRawBytes + chunk * 16;
       constexpr int PASSES = (KEYS + 4 * ROWS - 1) / (4 * ROWS);
+      uint4 x[PASSES];
+#pragma unroll
+      for (int i = 0; i < PASSES; ++i) x[i] = lds128(raw + min((i * 4 + cw) * ROWS + sub, KEYS - 1) * HD);
 #pragma unroll
       for (int i = 0; i < PASSES; ++i) {
         const int row = (i * 4 + cw) * ROWS + sub;
         if (KEYS % (4 * ROWS) == 0 || row < KEYS) {
-          const uint4 x = lds128(raw + row * HD);
-          const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
+          const uint32_t xw[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
           uint32_t h[8];
 #pragma unroll
           for (int b = 0; b < 4; ++b) {
@@ -625,7 +639,8 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
 #pragma unroll
           for (int b = 0; b < 16; ++b) mx = fmaxf(mx, fabsf(y[b]));
 #pragma unroll
-          for (int d = 1; d < CHUNKS; d *= 2) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+          for (int d = 1; d < 4; d *= 2) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+          if constexpr (HD == 128) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
           // the largest of the row to [1, 2), by an exponent of -126 to 126, so that both powers are normal numbers (see attention_cache.cuh)
           const int e = mx > 0.f ? min(max(static_cast<int>(__float_as_uint(mx) >> 23) - 127, -126), 126) : 0;
           const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23), up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
@@ -652,15 +667,11 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       if (!ok || it.n == 0) break;
       const int n = it.n;
       for (int t = 0; t < it.tiles && ok; ++t) ok = queries(it, t);
-      for (int j = -1; j < n && ok; ++j) {
-        if (j + 1 < n) {
-          ok = convert(k_tile(k_at), &k_full[k_at % NK], &k_empty[k_at % NK], k_at / NK);
-          ++k_at;
-        }
-        if (j >= 0 && ok) {
-          ok = convert(v_tile(v_at), &v_full[v_at % NV], &v_empty[v_at % NV], v_at / NV);
-          ++v_at;
-        }
+#pragma unroll 1
+      for (int t = 0; t < 2 * n && ok; ++t) {      // K of step 0, then K of step j + 1 and V of step j
+        const bool keys = t == 0 || (t & 1 && t + 1 < 2 * n);
+        const uint32_t g = keys ? k_at++ : v_at++, ring = keys ? g % NK : g % NV, use = keys ? g / NK : g / NV;
+        ok = convert(keys ? k_tile(g) : v_tile(g), (keys ? k_full : v_full) + ring, (keys ? k_empty : v_empty) + ring, use);
       }
     }
   } else {
@@ -719,60 +730,65 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
         tc_fence_before_sync();
         __syncwarp();
         mbar_arrive_if(&s_free[w], lane == 0);
-        const int left = limit - (u.lo + j) * KEYS;           // keys of the step that the row sees
-        const bool masked = __any_sync(0xffffffffu, left < KEYS);
-        // largest t: of each 16 scores the largest, scaled
-        float mx = -INFINITY;
-#pragma unroll
-        for (int m = 0; m < PARTS; ++m) {
-          if (masked) {
-#pragma unroll
-            for (int i = 16 * m; i < 16 * m + 16; ++i) if (i >= left) s[i] = 0xff800000u;   // -inf
-          }
-          float c0 = -INFINITY, c1 = -INFINITY;
-#pragma unroll
-          for (int i = 16 * m; i < 16 * m + 16; i += 4) {
-            c0 = fmax3(c0, __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
-            c1 = fmax3(c1, __uint_as_float(s[i + 2]), __uint_as_float(s[i + 3]));
-          }
-          sc[m] *= factor;
-          const float t = fmaf(fmaxf(c0, c1), sc[m], sc[PARTS + m]);
-          if (masked && 16 * m >= left) {                        // (a hidden block's scale may be anything)
-            sc[m] = 1.f;
-            sc[PARTS + m] = 0.f;
-            sc[2 * PARTS + m] = 0.f;
-          } else {
-            mx = fmaxf(mx, t);
-          }
-        }
-        // the reference moves to 2^7 below the row's largest t when that comes more than 2^15 above it, and to the first one above -inf
+        const int left = limit - (u.lo + j) * KEYS;              // keys of the step that the row sees
         const float m_old = m_ref;
-        const bool moved = mx > m_ref + kRefMoves;
-        m_ref = moved ? mx - kRefBelow : m_ref;
-        const uint32_t rescale = __ballot_sync(0xffffffffu, moved && any);
-        const float mb = m_ref == -INFINITY ? 0.f : m_ref;
-        const uint32_t pv_ok = any ? mbar_try_wait(&pv_done[w], n_s & 1u) : 1u;      // the previous step's, tested ahead
+        bool moved;
         uint64_t sum2 = 0;
         uint32_t pk[KEYS / 2];
+        const uint32_t pv_ok = any ? mbar_try_wait(&pv_done[w], n_s & 1u) : 1u;      // the previous step's, tested ahead
+        auto weigh = [&](auto cut) {                             // cut: some row of the warp does not see all keys of the step
+          constexpr bool CUT = decltype(cut)::value;
+          // largest t: of each 16 scores the largest, scaled
+          float mx = -INFINITY;
 #pragma unroll
-        for (int m = 0; m < PARTS; ++m) {
-          const uint64_t c2 = pack2(sc[m], sc[m]), b2 = pack2(sc[PARTS + m] - mb, sc[PARTS + m] - mb);
-          uint64_t part2 = 0;
+          for (int m = 0; m < PARTS; ++m) {
+            if constexpr (CUT) {
 #pragma unroll
-          for (int i = 8 * m; i < 8 * m + 8; ++i) {
-            float p0, p1;
-            unpack2(ffma2(pack2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c2, b2), p0, p1);
-            if (masked) {                                        // (-inf times a scale of 0 is NaN)
-              if (2 * i >= left) p0 = -INFINITY;
-              if (2 * i + 1 >= left) p1 = -INFINITY;
+              for (int i = 16 * m; i < 16 * m + 16; ++i) if (i >= left) s[i] = 0xff800000u;   // -inf
             }
-            p0 = fast_ex2(p0);
-            p1 = fast_ex2(p1);
-            part2 = i == 8 * m ? pack2(p0, p1) : fadd2(part2, pack2(p0, p1));
-            pk[i] = Pair16<__half>::pack(p0, p1);
+            float c0 = -INFINITY, c1 = -INFINITY;
+#pragma unroll
+            for (int i = 16 * m; i < 16 * m + 16; i += 4) {
+              c0 = fmax3(c0, __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
+              c1 = fmax3(c1, __uint_as_float(s[i + 2]), __uint_as_float(s[i + 3]));
+            }
+            sc[m] *= factor;
+            const float t = fmaf(fmaxf(c0, c1), sc[m], sc[PARTS + m]);
+            if (CUT && 16 * m >= left) {                         // (a hidden block's scale may be anything)
+              sc[m] = 1.f;
+              sc[PARTS + m] = 0.f;
+              sc[2 * PARTS + m] = 0.f;
+            } else {
+              mx = fmaxf(mx, t);
+            }
           }
-          sum2 = ffma2(part2, pack2(sc[2 * PARTS + m], sc[2 * PARTS + m]), sum2);
-        }
+          // the reference moves to 2^7 below the row's largest t when that comes more than 2^15 above it, and to the first one above -inf
+          moved = mx > m_ref + kRefMoves;
+          m_ref = moved ? mx - kRefBelow : m_ref;
+          const float mb = m_ref == -INFINITY ? 0.f : m_ref;
+#pragma unroll
+          for (int m = 0; m < PARTS; ++m) {
+            const uint64_t c2 = pack2(sc[m], sc[m]), b2 = pack2(sc[PARTS + m] - mb, sc[PARTS + m] - mb);
+            uint64_t part2 = 0;
+#pragma unroll
+            for (int i = 8 * m; i < 8 * m + 8; ++i) {
+              float p0, p1;
+              unpack2(ffma2(pack2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c2, b2), p0, p1);
+              if constexpr (CUT) {                               // (-inf times a scale of 0 is NaN)
+                if (2 * i >= left) p0 = -INFINITY;
+                if (2 * i + 1 >= left) p1 = -INFINITY;
+              }
+              p0 = fast_ex2(p0);
+              p1 = fast_ex2(p1);
+              part2 = i == 8 * m ? pack2(p0, p1) : fadd2(part2, pack2(p0, p1));
+              pk[i] = Pair16<__half>::pack(p0, p1);
+            }
+            sum2 = ffma2(part2, pack2(sc[2 * PARTS + m], sc[2 * PARTS + m]), sum2);
+          }
+        };
+        if (__builtin_expect(__any_sync(0xffffffffu, left < KEYS), 0)) weigh(std::true_type{});
+        else weigh(std::false_type{});
+        const uint32_t rescale = __ballot_sync(0xffffffffu, moved && any);
         // P goes where the previous step's was, and O may change: that step's P V has to be complete
         if (any) {
           if (!warp_mbar_wait_tested(pv_ok, &pv_done[w], n_s & 1u, abort_flag)) { ok = false; break; }
