@@ -8,7 +8,7 @@
 //   warp 3        walks the line of units (below) and tells the others the items of the CTA, through a ring
 //   warp 0        bytes of K and V, 16 tokens a bulk copy (they are contiguous), into a ring of 8-bit tiles; the scales of a step
 //   warps 1, 2    UMMA issuers, one per softmax warpgroup
-//   warps 4 ..    converters: a tile of queries, then of K and V, from bytes to fp16 in the tensor core's layout.  (0x6400 | (byte ^ 0x80)) - 1152: one logic operation and
+//   warps 4 ..    converters: tiles of queries, then two warps those of K and two those of V, from bytes to fp16 in the tensor core's layout.  (0x6400 | (byte ^ 0x80)) - 1152: one logic operation and
 //                 one subtraction for the bytes 0 and 2 of a word, a shift more for 1 and 3; so four dimensions lie in the order 0, 2, 1, 3, in the queries and the output too
 //   warps 8 ..    two softmax warpgroups, one thread a row
 //
@@ -55,21 +55,21 @@ struct ChunkParams {
 template <int HD>
 struct ChunkCfg {
   static constexpr int kHalves = HD / 64;
-  static constexpr int kRawTiles = HD == 128 ? 6 : 12, kKTiles = HD == 128 ? 2 : 3, kVTiles = HD == 128 ? 2 : 3;
+  static constexpr int kRawTiles = HD == 128 ? 3 : 6, kKTiles = HD == 128 ? 2 : 3, kVTiles = HD == 128 ? 2 : 3;
   static constexpr int kThreads = 512;
   static constexpr int kRegsLight = 64, kRegsConvert = 80, kRegsSoftmax = 184, kRegsLaunch = 128;
   static constexpr int kQHalf = 128 * 128, kQBytes = kQHalf * kHalves;                 // 128 rows x 64 elements
   static constexpr int kAtomBytes = kChunkKeys * 128, kTileBytes = kAtomBytes * kHalves;   // 80 keys x 64 elements
   static constexpr int kRawBytes = kChunkKeys * HD;
   static constexpr int kKOff = 2 * kQBytes, kVOff = kKOff + kKTiles * kTileBytes, kRawOff = kVOff + kVTiles * kTileBytes;
-  static constexpr int kPrefixOff = kRawOff + kRawTiles * kRawBytes;
+  static constexpr int kPrefixOff = kRawOff + 2 * kRawTiles * kRawBytes;                // (keys' tiles, then values')
   static constexpr int kScaleSlots = 32;
   static constexpr int kScaleOff = kPrefixOff + (kChunkMaxSeqs + 2) * 8;               // [slot][16]: key scales, log2 of value scales, their inverses
-  static constexpr int kRowOff = kScaleOff + kScaleSlots * 64;                         // [2][128] factors of the rows' scores
-  static constexpr int kMlOff = kRowOff + 2 * 128 * 4;                                 // [2][128] reference and sum of a warpgroup's rows
+  static constexpr int kRowOff = kScaleOff + kScaleSlots * 64;                         // [2][128] factors and offsets of the rows' scores
+  static constexpr int kMlOff = kRowOff + 2 * 128 * 8;                                 // [2][128] reference and sum of a warpgroup's rows
   static constexpr int kItemOff = kMlOff + 2 * 128 * 8;
   static constexpr int kBarOff = kItemOff + kChunkItems * 64;
-  static constexpr int kBars = 2 * kRawTiles + 2 * kKTiles + 2 * kVTiles + kScaleSlots + 2 + 2 + 4 * 2 + 2 + 2 * kChunkItems;
+  static constexpr int kBars = 4 * kRawTiles + 2 * kKTiles + 2 * kVTiles + kScaleSlots + 2 + 2 + 4 * 2 + 2 + 2 * kChunkItems;
   static constexpr int kBytes = kBarOff + kBars * 8 + 160 + 1024;                      // words, alignment slack
   static constexpr int kSCol0 = 2 * HD, kSStride = kChunkKeys + kChunkKeys / 2;        // tensor memory: O of both, then scores and P of each
   static_assert(kBytes <= 232448, "exceeds the shared memory of an SM");
@@ -78,7 +78,7 @@ struct ChunkCfg {
   static_assert(kSCol0 + 2 * kSStride <= 512, "tensor memory columns");
   static_assert(kRegsLight + kRegsConvert + 2 * kRegsSoftmax <= 4 * kRegsLaunch, "setmaxnreg budget exceeds the CTA's register allocation");
   // the producer is at most this many steps ahead of the softmax: a batch of scales, raw tiles, converted K tiles, one step each being read
-  static_assert(6 + kRawTiles / 2 + 1 + kKTiles + 4 <= kScaleSlots, "a step's scales are read before their slot is filled again");
+  static_assert(6 + kRawTiles + 1 + kKTiles + 4 <= kScaleSlots, "a step's scales are read before their slot is filled again");
 };
 
 // ------------------------------------------------------------------------------------ the line of units
@@ -253,6 +253,28 @@ struct alignas(16) ChunkItem {
 static_assert(sizeof(ChunkItem) == 64, "four loads");
 
 // ------------------------------------------------------------------------------------ small pieces
+// warp_mbar_wait in a few instructions: it stands in some twenty places, and the roles' loops share the instruction caches (see the measurements below).  The
+// bound is the same; a wait that ends by it raises the CTA's abort flag, and the others end by their own.
+__device__ __forceinline__ bool chunk_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* abort_flag) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .u32 t0, t1;\n\t"
+      "mov.u32 t0, %%clock;\n\t"
+      "LOOP%=:\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "@p bra DONE%=;\n\t"
+      "mov.u32 t1, %%clock;\n\t"
+      "sub.u32 t1, t1, t0;\n\t"
+      "setp.lt.u32 p, t1, 2000000000;\n\t"
+      "@p bra LOOP%=;\n\t"
+      "setp.ne.u32 p, t1, t1;\n\t"
+      "DONE%=:\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+  if (__builtin_expect(__all_sync(0xffffffffu, ok), 1)) return true;
+  *abort_flag = 1u;
+  return false;
+}
 __device__ __forceinline__ void bulk_load(void* smem_dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                ::"r"(smem_u32(smem_dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
@@ -286,12 +308,12 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw_chunk) + 1023) & ~uintptr_t(1023));
   long long* prefix = reinterpret_cast<long long*>(smem + L::kPrefixOff);
   float* sc_ring = reinterpret_cast<float*>(smem + L::kScaleOff);
-  float* row_factor = reinterpret_cast<float*>(smem + L::kRowOff);
+  float2* row_factor = reinterpret_cast<float2*>(smem + L::kRowOff);      // what a row's scores are multiplied by, and what is added to them before
   float2* ml_smem = reinterpret_cast<float2*>(smem + L::kMlOff);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBarOff);
-  uint64_t* raw_full = bars;                 // [NR] bytes of a tile landed
-  uint64_t* raw_empty = raw_full + NR;       // [NR] converted
-  uint64_t* k_full = raw_empty + NR;         // [NK] fp16 tile written
+  uint64_t* raw_full = bars;                 // [2 NR] bytes of a tile landed: keys, values
+  uint64_t* raw_empty = raw_full + 2 * NR;   // [2 NR] converted
+  uint64_t* k_full = raw_empty + 2 * NR;     // [NK] fp16 tile written
   uint64_t* k_empty = k_full + NK;           // [NK] every issuer hands every tile back
   uint64_t* v_full = k_empty + NK;           // [NV]
   uint64_t* v_empty = v_full + NV;           // [NV]
@@ -311,9 +333,9 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
 
   const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < NR; ++i) { mbar_init(&raw_full[i], 1); mbar_init(&raw_empty[i], 4); }
-    for (int i = 0; i < NK; ++i) { mbar_init(&k_full[i], 4); mbar_init(&k_empty[i], 2); }
-    for (int i = 0; i < NV; ++i) { mbar_init(&v_full[i], 4); mbar_init(&v_empty[i], 2); }
+    for (int i = 0; i < 2 * NR; ++i) { mbar_init(&raw_full[i], 1); mbar_init(&raw_empty[i], 2); }
+    for (int i = 0; i < NK; ++i) { mbar_init(&k_full[i], 2); mbar_init(&k_empty[i], 2); }
+    for (int i = 0; i < NV; ++i) { mbar_init(&v_full[i], 2); mbar_init(&v_empty[i], 2); }
     for (int i = 0; i < NS; ++i) mbar_init(&sc_full[i], 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(&q_full[i], 4); mbar_init(&q_empty[i], 10); mbar_init(&s_full[i], 1); mbar_init(&p_ready[i], 4);
@@ -344,7 +366,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
   uint32_t n_items = 0;                            // taken by this warp
   auto take = [&](ChunkItem& it) {                 // the next item; false after an expired wait
     const uint32_t at = n_items % kChunkItems;
-    if (!warp_mbar_wait(&item_full[at], (n_items / kChunkItems) & 1u, abort_flag)) return false;
+    if (!chunk_wait(&item_full[at], (n_items / kChunkItems) & 1u, abort_flag)) return false;
     const uint4* src = reinterpret_cast<const uint4*>(item_ring + at);
 #pragma unroll
     for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(&it)[i] = src[i];
@@ -361,7 +383,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       bool ok = true;
       auto put = [&](const ChunkItem& it) {
         const uint32_t at = n_items % kChunkItems;
-        if (!warp_mbar_wait(&item_empty[at], ((n_items / kChunkItems) & 1u) ^ 1u, abort_flag)) return false;
+        if (!chunk_wait(&item_empty[at], ((n_items / kChunkItems) & 1u) ^ 1u, abort_flag)) return false;
         if (lane == 0) {
           item_ring[at] = it;
           mbar_arrive(&item_full[at]);
@@ -395,7 +417,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
     } else if (warp == 0) {
       // ------------------------------------------------------------------ bytes and scales
       // The order of the tiles: K of step 0; then K of step j + 1 and V of step j (the scores of a step are wanted before the values of the one in front)
-      uint32_t r = 0, g = 0;                       // raw tiles, steps so far
+      uint32_t g = 0, at_k = 0, at_v = 0;          // steps, tiles of keys and of values so far
       bool ok = true;
       for (;;) {
         ChunkItem it;
@@ -415,19 +437,20 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
           if (lane < kBatch * PARTS && j0 + lane / PARTS < n && (lo + j0) * KEYS + lane * 16 < seen) raise_status(p.status, DEV_ERR_CACHE_RANGE);
           return -1;
         };
-        auto copy = [&](const int8_t* from, int batch_ids, int at, int j) {      // step j, the batch's step `at`
+        auto copy = [&](bool values, int batch_ids, int at, int j) {      // step j, the batch's step `at`
           const int id = __shfl_sync(0xffffffffu, batch_ids, (at * PARTS + lane) & 31);
-          const bool there = lane < PARTS && id >= 0;
-          const uint32_t st = r % NR, have = __ballot_sync(0xffffffffu, there);
-          if (!warp_mbar_wait(&raw_empty[st], ((r / NR) & 1u) ^ 1u, abort_flag)) return false;
+          const uint32_t have = __ballot_sync(0xffffffffu, lane < PARTS && id >= 0);
+          const int tok = (lo + j) * KEYS + lane * 16, place = tok & ((1 << p.c.bs_log2) - 1);
+          const bool there = (have >> lane & 1u) && (lane == 0 || place == 0);      // a lane copies from its part to the end of the block, or of what there is
+          const int parts = min(((1 << p.c.bs_log2) - place) >> 4, __popc(have >> lane));
+          const uint32_t tile = values ? at_v++ : at_k++, st = (values ? NR : 0) + tile % NR;
+          if (!chunk_wait(&raw_empty[st], ((tile / NR) & 1u) ^ 1u, abort_flag)) return false;
           if (lane == 0) mbar_expect_tx(&raw_full[st], __popc(have) * (16u * HD));
           __syncwarp();
           if (there) {
-            const int place = ((lo + j) * KEYS + lane * 16) & ((1 << p.c.bs_log2) - 1);
             const long long row = ((static_cast<long long>(id) * p.c.n_kv + head) << p.c.bs_log2) + place;
-            bulk_load(smem + L::kRawOff + st * L::kRawBytes + lane * 16 * HD, from + row * HD, 16 * HD, &raw_full[st]);
+            bulk_load(smem + L::kRawOff + st * L::kRawBytes + lane * 16 * HD, (values ? p.c.v : p.c.k) + row * HD, parts * 16 * HD, &raw_full[st]);
           }
-          ++r;
           return true;
         };
         auto load_scales = [&](int id) {
@@ -451,7 +474,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
         };
         int now = load_ids(0), next = load_ids(kBatch);
         now = checked(now, 0);
-        ok = copy(p.c.k, now, 0, 0);
+        ok = copy(false, now, 0, 0);
         float2 sc = load_scales(now);
         for (int j0 = 0; j0 < n && ok; j0 += kBatch) {
           const int behind = load_ids(j0 + 2 * kBatch);
@@ -461,7 +484,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
 #pragma unroll 1
           for (int i = 0; i < 2 * steps && ok; ++i) {              // K of step j + 1, V of step j
             const int at = (i >> 1) + (i & 1 ? 0 : 1), j = j0 + at;
-            if (j < n) ok = copy(i & 1 ? p.c.v : p.c.k, at < kBatch ? now : next, at < kBatch ? at : 0, j);
+            if (j < n) ok = copy(i & 1, at < kBatch ? now : next, at < kBatch ? at : 0, j);
             if (i == 1) publish(sc, now, g, steps);
           }
           g += steps;
@@ -472,7 +495,8 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
         if (!ok) break;
       }
       // every copy has landed before the CTA's shared memory passes to another one: converted, or (after an expired wait) by time
-      for (uint32_t e = r < NR ? 0 : r - NR; e < r && ok; ++e) ok = warp_mbar_wait(&raw_empty[e % NR], (e / NR) & 1u, abort_flag);
+      for (uint32_t e = g < NR ? 0 : g - NR; e < g && ok; ++e)
+        ok = chunk_wait(&raw_empty[e % NR], (e / NR) & 1u, abort_flag) && chunk_wait(&raw_empty[NR + e % NR], (e / NR) & 1u, abort_flag);
       if (!ok) {
         const long long t0 = clock64();
         while (clock64() - t0 < 4000000) {}
@@ -488,14 +512,14 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       bool ok = true;
       auto pass_k = [&](uint32_t to) {
         for (; k_at < to; ++k_at) {
-          if (!warp_mbar_wait(&k_full[k_at % NK], (k_at / NK) & 1u, abort_flag)) return false;
+          if (!chunk_wait(&k_full[k_at % NK], (k_at / NK) & 1u, abort_flag)) return false;
           mbar_arrive_if(&k_empty[k_at % NK], lane == 0);
         }
         return true;
       };
       auto pass_v = [&](uint32_t to) {
         for (; v_at < to; ++v_at) {
-          if (!warp_mbar_wait(&v_full[v_at % NV], (v_at / NV) & 1u, abort_flag)) return false;
+          if (!chunk_wait(&v_full[v_at % NV], (v_at / NV) & 1u, abort_flag)) return false;
           mbar_arrive_if(&v_empty[v_at % NV], lane == 0);
         }
         return true;
@@ -513,15 +537,15 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
         // queries: wait for each tile of the item, hand back what is not used
         for (int t = 0; t < tiles && ok; ++t) {
           const uint32_t q = qn + t;
-          ok = warp_mbar_wait(&q_full[q & 1u], (q >> 1) & 1u, abort_flag);
+          ok = chunk_wait(&q_full[q & 1u], (q >> 1) & 1u, abort_flag);
           if (ok && ((q & 1u) != slot || last < 0)) mbar_arrive_if(&q_empty[q & 1u], lane == 0);
         }
         qn += tiles;
         if (!ok) break;
         auto scores = [&](int j) {                 // of step j, into the warpgroup's columns once they are read
           const uint32_t g = base + j;
-          if (!pass_k(g) || !warp_mbar_wait(&k_full[g % NK], (g / NK) & 1u, abort_flag)) return false;
-          if (n_s > 0 && !warp_mbar_wait(&s_free[w], (n_s - 1u) & 1u, abort_flag)) return false;
+          if (!pass_k(g) || !chunk_wait(&k_full[g % NK], (g / NK) & 1u, abort_flag)) return false;
+          if (n_s > 0 && !chunk_wait(&s_free[w], (n_s - 1u) & 1u, abort_flag)) return false;
           tc_fence_after_sync();
           const uint64_t ad = make_smem_desc(q_tile(slot), 16, 1024, kSwizzle128B), bd = make_smem_desc(k_tile(g), 16, 1024, kSwizzle128B);
           if (elect_one()) {
@@ -539,35 +563,34 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
           ++n_s;
           return true;
         };
-        if (last >= 0) {
-          ok = scores(first);
-          for (int j = first; j <= last && ok; j += stride) {
-            const uint32_t g = base + j;
-            if (j < last && !scores(j + stride)) { ok = false; break; }
-            if (!pass_v(g) || !warp_mbar_wait(&v_full[g % NV], (g / NV) & 1u, abort_flag) || !warp_mbar_wait(&p_ready[w], n_p & 1u, abort_flag)) { ok = false; break; }
-            ++n_p;
-            tc_fence_after_sync();
-            const uint64_t bd = make_smem_desc(v_tile(g), L::kAtomBytes, 1024, kSwizzle128B);
-            if (elect_one()) {
+#pragma unroll 1
+        for (int j = first - stride; j <= last && ok && last >= 0; j += stride) {      // the scores of the step behind j, then P V of step j
+          if (j < last && !scores(j + stride)) { ok = false; break; }
+          if (j < first) continue;
+          const uint32_t g = base + j;
+          if (!pass_v(g) || !chunk_wait(&v_full[g % NV], (g / NV) & 1u, abort_flag) || !chunk_wait(&p_ready[w], n_p & 1u, abort_flag)) { ok = false; break; }
+          ++n_p;
+          tc_fence_after_sync();
+          const uint64_t bd = make_smem_desc(v_tile(g), L::kAtomBytes, 1024, kSwizzle128B);
+          if (elect_one()) {
 #pragma unroll
-              for (int ks = 0; ks < KEYS / 16; ++ks)             // 16 keys: 8 columns of P, 2 KB of V
-                umma_bf16_ts(tm_o, tm_p + ks * 8, bd + ks * (2048 >> 4), idesc_o, (j != first || ks != 0) ? 1u : 0u);
-              umma_commit(&pv_done[w]);
-              umma_commit(&v_empty[g % NV]);
-            }
-            __syncwarp();
-            v_at = g + 1;
-            if (alternate && j + 1 < n) ok = pass_v(g + 2);      // the other's values, as soon as they are there
+            for (int ks = 0; ks < KEYS / 16; ++ks)               // 16 keys: 8 columns of P, 2 KB of V
+              umma_bf16_ts(tm_o, tm_p + ks * 8, bd + ks * (2048 >> 4), idesc_o, (j != first || ks != 0) ? 1u : 0u);
+            umma_commit(&pv_done[w]);
+            umma_commit(&v_empty[g % NV]);
           }
+          __syncwarp();
+          v_at = g + 1;
+          if (alternate && j + 1 < n) ok = pass_v(g + 2);        // the other's values, as soon as they are there
         }
         ok = ok && pass_k(base + n) && pass_v(base + n);
         base += n;
       }
       // the last hand-backs are asynchronous arrivals: in before the CTA ends
       if (ok && w == 0) {
-        for (uint32_t e = base < NK ? 0 : base - NK; e < base && ok; ++e) ok = warp_mbar_wait(&k_empty[e % NK], (e / NK) & 1u, abort_flag);
-        for (uint32_t e = base < NV ? 0 : base - NV; e < base && ok; ++e) ok = warp_mbar_wait(&v_empty[e % NV], (e / NV) & 1u, abort_flag);
-        for (uint32_t e = qn < 2 ? 0 : qn - 2; e < qn && ok; ++e) ok = warp_mbar_wait(&q_empty[e & 1u], (e >> 1) & 1u, abort_flag);
+        for (uint32_t e = base < NK ? 0 : base - NK; e < base && ok; ++e) ok = chunk_wait(&k_empty[e % NK], (e / NK) & 1u, abort_flag);
+        for (uint32_t e = base < NV ? 0 : base - NV; e < base && ok; ++e) ok = chunk_wait(&v_empty[e % NV], (e / NV) & 1u, abort_flag);
+        for (uint32_t e = qn < 2 ? 0 : qn - 2; e < qn && ok; ++e) ok = chunk_wait(&q_empty[e & 1u], (e >> 1) & 1u, abort_flag);
       }
     }
   } else if (warp < 8) {
@@ -577,42 +600,61 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
     constexpr int CHUNKS = HD / 16, ROWS = 32 / CHUNKS;                    // 16 dimensions a lane, rows a warp takes at once
     const int2 place = lane_place<HD>(lane);
     const int sub = place.x, chunk = place.y;
-    uint32_t r = 0, k_at = 0, v_at = 0, qn = 0;
+    uint32_t qn = 0;
     bool ok = true;
-    auto convert = [&](uint32_t tile, uint64_t* full, uint64_t* empty, uint32_t use) {      // the next raw tile
-      const uint32_t st = r % NR;
-      if (!warp_mbar_wait(&raw_full[st], (r / NR) & 1u, abort_flag) || !warp_mbar_wait(empty, (use & 1u) ^ 1u, abort_flag)) return false;
-      const uint32_t raw = smem_at + L::kRawOff + st * L::kRawBytes + chunk * 16;
-      constexpr int PASSES = (KEYS + 4 * ROWS - 1) / (4 * ROWS);
-      uint4 x[PASSES];
+    // The next raw tile to fp16.  Keys: byte ^ 0x80 is a number + 128, and as the bits of an fp16 number (number + 128) 2^-24; the row's factor makes up
+    // for 2^-24, its offset for the 128 of every dimension.  Values are exact: (0x6400 | (byte ^ 0x80)) - 1152.  (One small loop body each: the code of all roles
+    // shares the instruction caches.)
+    // One pair of warps each.
+    const bool keys = cw < 2;
+    constexpr int STEP = 2 * ROWS, BATCH = 5, PASSES = KEYS / STEP;        // rows that a pair takes at once
+    static_assert(KEYS % STEP == 0 && PASSES % BATCH == 0 && STEP % 8 == 0, "whole passes; a row's place in its swizzle pattern stays");
+    const int row = (cw & 1) * ROWS + sub;
+    const uint32_t raw0 = smem_at + L::kRawOff + (keys ? 0 : NR) * L::kRawBytes + chunk * 16 + row * HD;
+    const uint32_t tile0 = smem_at + (keys ? L::kKOff : L::kVOff) + (chunk >> 2) * L::kAtomBytes + row * 128 + (((2 * (chunk & 3)) ^ (row & 7)) << 4);
+    uint64_t *const from_full = raw_full + (keys ? 0 : NR), *const from_empty = raw_empty + (keys ? 0 : NR);
+    uint64_t *const full = keys ? k_full : v_full, *const empty = keys ? k_empty : v_empty;
+    const uint32_t ring = keys ? NK : NV;
+    uint32_t st = 0, landed = 0, to = 0, gone = 1;                         // places in the two rings, and the phases to wait for
+    auto convert = [&]() {
+      if (!chunk_wait(&from_full[st], landed, abort_flag) || !chunk_wait(&empty[to], gone, abort_flag)) return false;
+      const uint32_t src = raw0 + st * L::kRawBytes, dst = tile0 + to * L::kTileBytes;
+#pragma unroll 1
+      for (int i0 = 0; i0 < PASSES; i0 += BATCH) {
+        uint4 x[BATCH];
 #pragma unroll
-      for (int i = 0; i < PASSES; ++i) x[i] = lds128(raw + min((i * 4 + cw) * ROWS + sub, KEYS - 1) * HD);
+        for (int i = 0; i < BATCH; ++i) x[i] = lds128(src + (i0 + i) * STEP * HD);
+        if (keys) {
 #pragma unroll
-      for (int i = 0; i < PASSES; ++i) {
-        const int row = (i * 4 + cw) * ROWS + sub;
-        if (KEYS % (4 * ROWS) == 0 || row < KEYS) {
-          const uint32_t xw[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-          uint32_t h[8];
-#pragma unroll
-          for (int b = 0; b < 4; ++b) {
-            h[2 * b] = bytes02_to_half2(xw[b]);
-            h[2 * b + 1] = bytes02_to_half2(xw[b] >> 8);
+          for (int i = 0; i < BATCH; ++i) {
+            const uint32_t at = dst + (i0 + i) * STEP * 128;
+            constexpr uint32_t M = 0x00FF00FFu, X = 0x00800080u;
+            sts128(at, (x[i].x & M) ^ X, ((x[i].x >> 8) & M) ^ X, (x[i].y & M) ^ X, ((x[i].y >> 8) & M) ^ X);
+            sts128(at ^ 16, (x[i].z & M) ^ X, ((x[i].z >> 8) & M) ^ X, (x[i].w & M) ^ X, ((x[i].w >> 8) & M) ^ X);
           }
-          store_row_16(tile, L::kAtomBytes, row, chunk, h);
+        } else {
+#pragma unroll
+          for (int i = 0; i < BATCH; ++i) {
+            const uint32_t at = dst + (i0 + i) * STEP * 128;
+            sts128(at, bytes02_to_half2(x[i].x), bytes02_to_half2(x[i].x >> 8), bytes02_to_half2(x[i].y), bytes02_to_half2(x[i].y >> 8));
+            sts128(at ^ 16, bytes02_to_half2(x[i].z), bytes02_to_half2(x[i].z >> 8), bytes02_to_half2(x[i].w), bytes02_to_half2(x[i].w >> 8));
+          }
         }
       }
       fence_proxy_async_smem();
       __syncwarp();
-      mbar_arrive_if(&raw_empty[st], lane == 0);
-      mbar_arrive_if(full, lane == 0);
-      ++r;
+      mbar_arrive_if(&from_empty[st], lane == 0);
+      mbar_arrive_if(&full[to], lane == 0);
+      if (++st == NR) { st = 0; landed ^= 1u; }
+      if (++to == ring) { to = 0; gone ^= 1u; }
       return true;
     };
     auto queries = [&](const ChunkItem& u, int t) {
       const uint32_t slot = qn & 1u;
-      constexpr int PASSES = 128 / (4 * ROWS), BATCH = 4;
+      constexpr int BATCH = 4;
+      const int rows = min(u.n_tok - u.tok0 - t * p.tile_tokens, p.tile_tokens) * p.group;      // (what the rows behind hold does not matter)
 #pragma unroll 1
-      for (int i0 = 0; i0 < PASSES; i0 += BATCH) {
+      for (int i0 = 0; i0 == 0 || i0 * 4 * ROWS < rows; i0 += BATCH) {
         uint4 x[BATCH][2];
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
@@ -624,7 +666,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
             x[i][1] = src[1];
           }
         }
-        if (i0 == 0 && !warp_mbar_wait(&q_empty[slot], ((qn >> 1) & 1u) ^ 1u, abort_flag)) return false;
+        if (i0 == 0 && !chunk_wait(&q_empty[slot], ((qn >> 1) & 1u) ^ 1u, abort_flag)) return false;
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
           const int row = ((i0 + i) * 4 + cw) * ROWS + sub;
@@ -641,18 +683,24 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
 #pragma unroll
           for (int d = 1; d < 4; d *= 2) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
           if constexpr (HD == 128) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-          // the largest of the row to [1, 2), by an exponent of -126 to 126, so that both powers are normal numbers (see attention_cache.cuh)
-          const int e = mx > 0.f ? min(max(static_cast<int>(__float_as_uint(mx) >> 23) - 127, -126), 126) : 0;
+          // the largest of the row to [2^14, 2^15) (fp16 ends at 65504), by an exponent of -126 to 126, so that both powers are normal numbers: what is
+          // below 2^-39 of the row's largest is lost
+          const int e = mx > 0.f ? min(max(static_cast<int>(__float_as_uint(mx) >> 23) - 127 - 14, -126), 126) : 0;
           const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23), up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
           uint32_t h[8];
+          float sum = 0.f;                         // of the numbers as fp16 has them
 #pragma unroll
           for (int b = 0; b < 4; ++b) {
             h[2 * b] = Pair16<__half>::pack(y[4 * b] * down, y[4 * b + 2] * down);
             h[2 * b + 1] = Pair16<__half>::pack(y[4 * b + 1] * down, y[4 * b + 3] * down);
+            sum += (Pair16<__half>::lo(h[2 * b]) + Pair16<__half>::hi(h[2 * b])) + (Pair16<__half>::lo(h[2 * b + 1]) + Pair16<__half>::hi(h[2 * b + 1]));
           }
+#pragma unroll
+          for (int d = 1; d < 4; d *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+          if constexpr (HD == 128) sum += __shfl_xor_sync(0xffffffffu, sum, 8);
           store_row_16(q_tile(slot), L::kQHalf, row, chunk, h);
           // (an infinite element makes the row NaN: of -Inf alone its scores would count as masked)
-          if (chunk == 0) row_factor[slot * 128 + row] = mx == INFINITY ? __uint_as_float(0x7FFFFFFFu) : p.scale_log2 * up;
+          if (chunk == 0) row_factor[slot * 128 + row] = make_float2(mx == INFINITY ? __uint_as_float(0x7FFFFFFFu) : p.scale_log2 * up * 16777216.f, sum * -7.62939453125e-06f);      // 2^24; -128 2^-24
         }
       }
       fence_proxy_async_smem();
@@ -668,11 +716,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       const int n = it.n;
       for (int t = 0; t < it.tiles && ok; ++t) ok = queries(it, t);
 #pragma unroll 1
-      for (int t = 0; t < 2 * n && ok; ++t) {      // K of step 0, then K of step j + 1 and V of step j
-        const bool keys = t == 0 || (t & 1 && t + 1 < 2 * n);
-        const uint32_t g = keys ? k_at++ : v_at++, ring = keys ? g % NK : g % NV, use = keys ? g / NK : g / NV;
-        ok = convert(keys ? k_tile(g) : v_tile(g), (keys ? k_full : v_full) + ring, (keys ? k_empty : v_empty) + ring, use);
-      }
+      for (int j = 0; j < n && ok; ++j) ok = convert();
     }
   } else {
     // ------------------------------------------------------------------ softmax warpgroups
@@ -692,10 +736,10 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       const int first = alternate ? w : 0, stride = alternate ? 2 : 1;
       const int mine = alternate ? n : w == 0 ? u.mine[0] : u.mine[1];
       const uint32_t slot = (qn + (alternate ? 0 : w)) & 1u;
-      float factor = 0.f;
+      float2 factor = make_float2(0.f, 0.f);
       for (int t = 0; t < tiles && ok; ++t) {
         const uint32_t q = qn + t;
-        ok = warp_mbar_wait(&q_full[q & 1u], (q >> 1) & 1u, abort_flag);
+        ok = chunk_wait(&q_full[q & 1u], (q >> 1) & 1u, abort_flag);
         if (!ok) break;
         if ((q & 1u) == slot) factor = row_factor[slot * 128 + row];
         __syncwarp();
@@ -705,6 +749,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       if (!ok) break;
       const int tok = u.tok0 + (alternate ? 0 : w) * p.tile_tokens + row_tok;
       const bool stored = row_tok < p.tile_tokens && tok < u.n_tok;
+      const bool active = __any_sync(0xffffffffu, stored);                 // a warp without a row that is stored only keeps the barriers going
       const int limit = stored ? u.ahead + tok + 1 : 0x7fffffff;       // tokens that this row sees (rows that are not stored: all, for what they compute does not matter)
       float m_ref = -INFINITY;
       uint64_t l2 = 0;                             // row sum, two halves
@@ -712,14 +757,21 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
 #pragma unroll 1
       for (int j = first; j < mine; j += stride) {
         const uint32_t g = base + j;
-        if (!warp_mbar_wait(&s_full[w], n_s & 1u, abort_flag)) { ok = false; break; }
+        if (!chunk_wait(&s_full[w], n_s & 1u, abort_flag)) { ok = false; break; }
         ++n_s;
+        if (!active) {
+          mbar_arrive_if(&s_free[w], lane == 0);
+          if (any && !chunk_wait(&pv_done[w], n_s & 1u, abort_flag)) { ok = false; break; }      // (in front of it, p_ready may still be in the phase before)
+          mbar_arrive_if(&p_ready[w], lane == 0);
+          any = true;
+          continue;
+        }
         tc_fence_after_sync();
         uint32_t s[KEYS];
         tmem_ld_32x32_at<0>(s_addr, s);
         tmem_ld_32x32_at<32>(s_addr, s);
         tmem_ld_32x16_at<64>(s_addr, s);
-        if (!warp_mbar_wait(&sc_full[g % NS], (g / NS) & 1u, abort_flag)) { ok = false; break; }
+        if (!chunk_wait(&sc_full[g % NS], (g / NS) & 1u, abort_flag)) { ok = false; break; }
         float sc[16];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -735,7 +787,6 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
         bool moved;
         uint64_t sum2 = 0;
         uint32_t pk[KEYS / 2];
-        const uint32_t pv_ok = any ? mbar_try_wait(&pv_done[w], n_s & 1u) : 1u;      // the previous step's, tested ahead
         auto weigh = [&](auto cut) {                             // cut: some row of the warp does not see all keys of the step
           constexpr bool CUT = decltype(cut)::value;
           // largest t: of each 16 scores the largest, scaled
@@ -752,7 +803,8 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
               c0 = fmax3(c0, __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
               c1 = fmax3(c1, __uint_as_float(s[i + 2]), __uint_as_float(s[i + 3]));
             }
-            sc[m] *= factor;
+            sc[m] *= factor.x;
+            sc[PARTS + m] = fmaf(factor.y, sc[m], sc[PARTS + m]);
             const float t = fmaf(fmaxf(c0, c1), sc[m], sc[PARTS + m]);
             if (CUT && 16 * m >= left) {                         // (a hidden block's scale may be anything)
               sc[m] = 1.f;
@@ -791,7 +843,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
         const uint32_t rescale = __ballot_sync(0xffffffffu, moved && any);
         // P goes where the previous step's was, and O may change: that step's P V has to be complete
         if (any) {
-          if (!warp_mbar_wait_tested(pv_ok, &pv_done[w], n_s & 1u, abort_flag)) { ok = false; break; }
+          if (!chunk_wait(&pv_done[w], n_s & 1u, abort_flag)) { ok = false; break; }
           tc_fence_after_sync();
         }
         if (__builtin_expect(rescale != 0u, 0)) {
@@ -823,7 +875,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       if (!ok) break;
       // the item's end
       if (any) {
-        if (!warp_mbar_wait(&pv_done[w], (n_s - 1u) & 1u, abort_flag)) { ok = false; break; }
+        if (!chunk_wait(&pv_done[w], (n_s - 1u) & 1u, abort_flag)) { ok = false; break; }
         tc_fence_after_sync();
       }
       float l, l_hi;
@@ -836,7 +888,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
         tc_fence_before_sync();
         __syncwarp();
         mbar_arrive_if(&met[0], lane == 0);
-        if (!warp_mbar_wait(&met[0], n_met & 1u, abort_flag)) { ok = false; break; }
+        if (!chunk_wait(&met[0], n_met & 1u, abort_flag)) { ok = false; break; }
         tc_fence_after_sync();
         const float2 other = ml_smem[(1 - w) * 128 + row];
         both = n > 1;                              // (of one step: the first warpgroup's alone)
@@ -854,7 +906,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       const uint32_t o_other = lane_addr + (1 - w) * HD;
       const bool use_own = any, use_other = alternate && (both || !any);
 #pragma unroll 1
-      for (int c = col0; c < col0 + cols; c += 32) {
+      for (int c = col0; c < col0 + cols && active; c += 32) {
         uint32_t o[32], x[32];
         __syncwarp();
         if (use_own) tmem_ld_32x32(o_addr + c, o);
@@ -888,7 +940,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
         tc_fence_before_sync();
         __syncwarp();
         mbar_arrive_if(&met[1], lane == 0);
-        if (!warp_mbar_wait(&met[1], n_met & 1u, abort_flag)) { ok = false; break; }
+        if (!chunk_wait(&met[1], n_met & 1u, abort_flag)) { ok = false; break; }
         tc_fence_after_sync();
         ++n_met;
       }
