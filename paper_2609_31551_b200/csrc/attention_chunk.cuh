@@ -34,6 +34,7 @@ constexpr int kChunkUnitCost = 160;      // of a unit's beginning and end, in to
 constexpr int kChunkLeastCost = 320;     // of a piece
 constexpr int kChunkItems = 4;           // items that the roles may be apart
 
+struct ChunkItem;
 struct ChunkParams {
   CacheView c;
   const int32_t *table, *cu, *seq_lens;
@@ -48,6 +49,7 @@ struct ChunkParams {
   float scale_log2;
   float4* o_ws;                // [2 pieces][2 tiles][HD / 4][ws_rows]: O, not divided by the sum
   float2* ml_ws;               // [2 pieces][2 tiles][ws_rows]: reference and sum (-inf, 0: no key)
+  ChunkItem* cut_ws;           // [pieces]: the item that a unit's first cut ends (n 0: none)
   uint32_t* status;
   int early_launch;
 };
@@ -142,6 +144,11 @@ struct ChunkLine {
       : total(cost), pieces(static_cast<int>(min(static_cast<long long>(device_pieces), (cost + kChunkLeastCost - 1) / kChunkLeastCost))) {
     whole = pieces == 0 ? 0 : total / pieces;
     rest = static_cast<int>(total - whole * pieces);
+  }
+  __device__ __forceinline__ int piece_of(long long x) const {      // the one that holds position x
+    int at = static_cast<int>(x / (whole + 1));                    // (the pieces are `whole` or one more long)
+    while (at + 1 < pieces && begin(at + 1) <= x) ++at;
+    return at;
   }
   __device__ __forceinline__ long long begin(int piece) const { return whole * piece + static_cast<uint32_t>(rest) * static_cast<uint32_t>(piece) / static_cast<uint32_t>(pieces); }
 };
@@ -248,7 +255,8 @@ struct alignas(16) ChunkItem {
   int q0, tok0, n_tok, ahead;  // the sequence's first visible row, the unit's first token of those, their number, the tokens in front
   int head, s, seen;           // key/value head, sequence, tokens that the unit's last row sees
   int slot;                    // of the workspace; -1: the item is the whole unit
-  int pad[3];
+  int parts;                   // of the unit's first item, if it is cut: in how many pieces the unit has steps
+  int pad[2];
 };
 static_assert(sizeof(ChunkItem) == 64, "four loads");
 
@@ -381,6 +389,8 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
     if (warp == 3) {
       // ------------------------------------------------------------------ the CTA's items
       bool ok = true;
+      if (lane == 0)
+        for (int piece = blockIdx.x; piece < p.n_ctas; piece += gridDim.x) p.cut_ws[piece].n = 0;
       auto put = [&](const ChunkItem& it) {
         const uint32_t at = n_items % kChunkItems;
         if (!chunk_wait(&item_empty[at], ((n_items / kChunkItems) & 1u) ^ 1u, abort_flag)) return false;
@@ -408,6 +418,11 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
         it.s = u.s;
         it.seen = u.seq.seen(u.j, p.tile_tokens);
         it.slot = it.n == u.steps ? -1 : 2 * deal.piece + (deal.hi == u.steps ? 0 : 1);
+        it.parts = 0;
+        if (deal.lo == 0 && deal.hi < u.steps) {
+          it.parts = deal.line.piece_of(u.at + kChunkUnitCost + static_cast<long long>(u.tiles) * KEYS * (u.steps - 1)) - deal.piece + 1;
+          if (lane == 0) p.cut_ws[deal.piece] = it;
+        }
         ok = put(it);
       }
       if (ok) {
@@ -651,7 +666,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
     };
     auto queries = [&](const ChunkItem& u, int t) {
       const uint32_t slot = qn & 1u;
-      constexpr int BATCH = 4;
+      constexpr int BATCH = 2;
       const int rows = min(u.n_tok - u.tok0 - t * p.tile_tokens, p.tile_tokens) * p.group;      // (what the rows behind hold does not matter)
 #pragma unroll 1
       for (int i0 = 0; i0 == 0 || i0 * 4 * ROWS < rows; i0 += BATCH) {
@@ -724,7 +739,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
     const int w = (warp - 8) >> 2, quarter = warp & 3;                     // (the quarter of the tensor memory's lanes that the warp reads)
     const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
     const uint32_t s_addr = lane_addr + L::kSCol0 + w * L::kSStride, p_addr = s_addr + KEYS, o_addr = lane_addr + w * HD;
-    const int row = quarter * 32 + lane, row_tok = row / p.group, row_head = row - row_tok * p.group;
+    const int row = quarter * 32 + lane, row_tok = row / p.group;
     uint32_t base = 0, qn = 0, n_s = 0, n_met = 0;                         // steps of the CTA, query tiles, the warpgroup's steps, meetings
     bool ok = true;
     while (ok) {
@@ -747,15 +762,18 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       }
       qn += tiles;
       if (!ok) break;
+      // (what the end needs is put together here: the item's fields would cost the steps their registers)
       const int tok = u.tok0 + (alternate ? 0 : w) * p.tile_tokens + row_tok;
       const bool stored = row_tok < p.tile_tokens && tok < u.n_tok;
       const bool active = __any_sync(0xffffffffu, stored);                 // a warp without a row that is stored only keeps the barriers going
-      const int limit = stored ? u.ahead + tok + 1 : 0x7fffffff;       // tokens that this row sees (rows that are not stored: all, for what they compute does not matter)
+      const int part = u.slot < 0 ? -1 : u.slot * 2 + (alternate ? 0 : w);  // of the workspace; -1: the item is the whole unit
+      uint16_t* const dst = p.out + static_cast<long long>(u.q0 + (stored ? tok : 0)) * p.ld_out + (u.head * p.group + row - row_tok * p.group) * HD;
+      int left = stored ? u.ahead + tok + 1 - (u.lo + first) * KEYS : 0x7fffffff;      // keys from the present step on that this row sees (rows that are not stored: all, for what they compute does not matter)
       float m_ref = -INFINITY;
       uint64_t l2 = 0;                             // row sum, two halves
       bool any = false;                            // the warpgroup has a step of the item
 #pragma unroll 1
-      for (int j = first; j < mine; j += stride) {
+      for (int j = first; j < mine; j += stride, left -= stored ? stride * KEYS : 0) {
         const uint32_t g = base + j;
         if (!chunk_wait(&s_full[w], n_s & 1u, abort_flag)) { ok = false; break; }
         ++n_s;
@@ -782,7 +800,6 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
         tc_fence_before_sync();
         __syncwarp();
         mbar_arrive_if(&s_free[w], lane == 0);
-        const int left = limit - (u.lo + j) * KEYS;              // keys of the step that the row sees
         const float m_old = m_ref;
         bool moved;
         uint64_t sum2 = 0;
@@ -863,8 +880,8 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
           l2 = fadd2(l2, sum2);
         }
         __syncwarp();
-        tmem_st_32x32_from(p_addr, pk);
-        tmem_st_32x8_from(p_addr + 32, pk + 32);
+#pragma unroll
+        for (int m = 0; m < PARTS; ++m) tmem_st_32x8_from(p_addr + 8 * m, pk + 8 * m);      // (eight registers at a time can be those that the scores had)
         tmem_st_wait();
         tc_fence_before_sync();
         __syncwarp();
@@ -898,11 +915,8 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
         l = (any ? l * f_own : 0.f) + (both || !any ? other.y * f_other : 0.f);
         m = top;
       }
-      const bool whole = u.slot < 0;
       const float inv = l == 0.f ? 0.f : kWeightDown / l;
       const int col0 = alternate ? w * (HD / 2) : 0, cols = alternate ? HD / 2 : HD;
-      const long long part = static_cast<long long>(u.slot) * 2 + (alternate ? 0 : w);
-      uint16_t* dst = p.out + static_cast<long long>(u.q0 + (stored ? tok : 0)) * p.ld_out + (u.head * p.group + row_head) * HD;
       const uint32_t o_other = lane_addr + (1 - w) * HD;
       const bool use_own = any, use_other = alternate && (both || !any);
 #pragma unroll 1
@@ -920,7 +934,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
           const float v = use_other ? fmaf(__uint_as_float(x[i]), f_other, a) : a;
           y[(i & ~3) | ((i & 1) << 1) | ((i >> 1) & 1)] = v;     // four dimensions lie in the order 0, 2, 1, 3
         }
-        if (stored && whole) {
+        if (stored && part < 0) {
 #pragma unroll
           for (int i = 0; i < 32; i += 8) {
             uint32_t z[4];
@@ -930,12 +944,12 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
             *reinterpret_cast<uint4*>(dst + c + i) = make_uint4(z[0], z[1], z[2], z[3]);
           }
         } else if (stored) {
-          float4* to = p.o_ws + (part * (HD / 4) + c / 4) * p.ws_rows + row;
+          float4* to = p.o_ws + (static_cast<long long>(part) * (HD / 4) + c / 4) * p.ws_rows + row;
 #pragma unroll
           for (int i = 0; i < 8; ++i) to[i * p.ws_rows] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
         }
       }
-      if (stored && !whole && (!alternate || w == 0)) p.ml_ws[part * p.ws_rows + row] = make_float2(l == 0.f ? -INFINITY : m, l);
+      if (stored && part >= 0 && (!alternate || w == 0)) p.ml_ws[static_cast<long long>(part) * p.ws_rows + row] = make_float2(l == 0.f ? -INFINITY : m, l);
       if (alternate) {
         tc_fence_before_sync();
         __syncwarp();
@@ -956,43 +970,41 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
   if (threadIdx.x == 0 && *abort_flag) atomicCAS(p.status, DEV_OK, DEV_ERR_WAIT_TIMEOUT);
 }
 
-// The parts of cut units put together, in order: 128 threads, one a row, per (cut, tile, 8 columns), a unit being taken care of at the first cut in it.  Then the rows
-// that see nothing.
+// The parts of cut units put together, in order: 128 threads, one a row, per (first cut of a unit, tile, 8 columns).  Before that, beside the end of the kernel
+// that leaves them, the rows that see nothing.
 template <int HD>
 __global__ void __launch_bounds__(512, 1) chunk_join_kernel(const __grid_constant__ ChunkParams p) {
   constexpr int COLS = 8, CHUNKS = HD / COLS, BATCH = 8;
-  __shared__ long long prefix[kChunkMaxSeqs + 2], sums[16];
   // On the whole device this kernel starts beside the one before it, which has let it go behind its own wait: the lengths are final
   if (!p.early_launch) pdl_wait();
-  chunk_prefix(p, prefix, sums, false);
-  const ChunkLine line(prefix[p.n_seqs], p.n_ctas);
-  const int row = threadIdx.x & 127, row_tok = row / p.group, row_head = row - row_tok * p.group;
+  const int lane = threadIdx.x & 31, chunks = p.c.n_kv * p.group * (HD / 8);
+  for (int s = blockIdx.x * 16 + (threadIdx.x >> 5); s < p.n_seqs; s += gridDim.x * 16) {
+    const ChunkSeq seq(p, s, false);                               // the rows in front of a sequence's visible tokens
+    const int first = min(max(p.cu[s], 0), p.n_rows), given = min(max(p.cu[s + 1], 0), p.n_rows) - first;
+    if (given > p.max_new) continue;
+    for (int r = first; r < seq.q0; ++r)
+      for (int c = lane; c < chunks; c += 32) *reinterpret_cast<uint4*>(p.out + static_cast<long long>(r) * p.ld_out + c * 8) = make_uint4(0u, 0u, 0u, 0u);
+  }
   pdl_wait();
   if (p.early_launch) pdl_launch_dependents();
-  for (int it = blockIdx.x * 4 + (threadIdx.x >> 7); line.total > 0 && it < (line.pieces - 1) * 2 * CHUNKS; it += gridDim.x * 4) {
-    const int cut = it / (2 * CHUNKS) + 1, t = it / CHUNKS % 2, col0 = it % CHUNKS * COLS;      // (the tiles of a cut side by side)
-    ChunkUnit u;
-    const long long at = line.begin(cut);
-    u.find(p, prefix, at);
-    const int first_step = u.step_at(at);
-    if (t >= u.tiles || first_step == 0 || first_step == u.steps || u.step_at(line.begin(cut - 1)) != 0) continue;      // (not cut here, or not for the first time)
-    const int tok = (2 * u.j + t) * p.tile_tokens + row_tok;
-    if (row_tok >= p.tile_tokens || tok >= u.seq.n) continue;
-    int last = cut;                                                // the piece that has the unit's end
-    while (last + 1 < line.pieces && u.step_at(line.begin(last + 1)) < u.steps) ++last;
+  const int row = threadIdx.x & 127, row_tok = row / p.group, row_head = row - row_tok * p.group;
+  for (int it = blockIdx.x * 4 + (threadIdx.x >> 7); it < p.n_ctas * 2 * CHUNKS; it += gridDim.x * 4) {
+    const int piece = it / (2 * CHUNKS), t = it / CHUNKS % 2, col0 = it % CHUNKS * COLS;
+    const ChunkItem& u = p.cut_ws[piece];
+    if (u.n == 0 || t >= u.tiles) continue;
+    const int tok = u.tok0 + t * p.tile_tokens + row_tok, parts = u.parts;
+    if (row_tok >= p.tile_tokens || tok >= u.n_tok) continue;
     float m = -INFINITY, l = 0.f, acc[COLS];
 #pragma unroll
     for (int i = 0; i < COLS; ++i) acc[i] = 0.f;
-    const int parts = last - cut + 2;                              // of pieces cut - 1 .. last
-    for (int b = 0; b < parts; b += BATCH) {
+    for (int b = 0; b < parts; b += BATCH) {                       // of pieces piece + b ..: the last one's is its first slot
       float ml[BATCH][2], x[BATCH][COLS];
 #pragma unroll
       for (int e = 0; e < BATCH; ++e) {
         ml[e][0] = -INFINITY;
         ml[e][1] = 0.f;
-        const int piece = cut - 1 + b + e;
-        if (b + e < parts && u.step_at(line.begin(piece)) < u.step_at(line.begin(piece + 1)) ) {
-          const long long slot = (2LL * piece + (piece == last ? 0 : 1)) * 2 + t;
+        if (b + e < parts) {
+          const long long slot = (2LL * (piece + b + e) + (b + e + 1 == parts ? 0 : 1)) * 2 + t;
           load_floats<2>(reinterpret_cast<const float*>(p.ml_ws + slot * p.ws_rows + row), ml[e]);
           const float4* o = p.o_ws + (slot * (HD / 4) + col0 / 4) * p.ws_rows + row;
           float y[4];
@@ -1026,16 +1038,7 @@ __global__ void __launch_bounds__(512, 1) chunk_join_kernel(const __grid_constan
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       y[e] = p.fp16 ? Pair16<__half>::pack(acc[2 * e] * inv, acc[2 * e + 1] * inv) : Pair16<bf16>::pack(acc[2 * e] * inv, acc[2 * e + 1] * inv);
-    *reinterpret_cast<uint4*>(p.out + static_cast<long long>(u.seq.q0 + tok) * p.ld_out + (u.head * p.group + row_head) * HD + col0) = make_uint4(y[0], y[1], y[2], y[3]);
-  }
-  // rows that see nothing: those in front of a sequence's visible tokens
-  const int lane = threadIdx.x & 31, chunks = p.c.n_kv * p.group * (HD / 8);
-  for (int s = blockIdx.x * 16 + (threadIdx.x >> 5); s < p.n_seqs; s += gridDim.x * 16) {
-    const ChunkSeq seq(p, s, false);
-    const int first = min(max(p.cu[s], 0), p.n_rows), given = min(max(p.cu[s + 1], 0), p.n_rows) - first;
-    if (given > p.max_new) continue;
-    for (int r = first; r < seq.q0; ++r)
-      for (int c = lane; c < chunks; c += 32) *reinterpret_cast<uint4*>(p.out + static_cast<long long>(r) * p.ld_out + c * 8) = make_uint4(0u, 0u, 0u, 0u);
+    *reinterpret_cast<uint4*>(p.out + static_cast<long long>(u.q0 + tok) * p.ld_out + (u.head * p.group + row_head) * HD + col0) = make_uint4(y[0], y[1], y[2], y[3]);
   }
 }
 

@@ -9,12 +9,13 @@ using namespace eas;
 
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 // scratch of a launch: two parts a piece of the line, two tiles each
-static size_t chunk_workspace(const eas_cache* c, int32_t max_new, int32_t n_heads, int* ws_rows, size_t* ml_off) {
+static size_t chunk_workspace(const eas_cache* c, int32_t max_new, int32_t n_heads, int* ws_rows, size_t* ml_off, size_t* cut_off) {
   const int group = n_heads / c->d.n_kv_heads;
   *ws_rows = std::min(128 / group, std::max(max_new, 1)) * group;
   const size_t rows = static_cast<size_t>(4) * c->sm_count * *ws_rows;
   *ml_off = up256(rows * c->d.head_dim * 4);
-  return *ml_off + up256(rows * 8);
+  *cut_off = *ml_off + up256(rows * 8);
+  return *cut_off + up256(c->sm_count * sizeof(ChunkItem));
 }
 
 template <int HD>
@@ -48,8 +49,8 @@ static eas_status chunk_attention(const eas_cache* c, const eas_cache_seqs* s, c
   if (ld_q < w || ld_out < w || ld_q % 8 != 0 || ld_out % 8 != 0)
     return fail(EAS_ERR_INVALID_ARG, "token distances must be multiples of 8 that hold a token's heads");
   ChunkParams p{};
-  size_t ml_off = 0;
-  const size_t need = chunk_workspace(c, std::min(max_new, n_rows), n_heads, &p.ws_rows, &ml_off);
+  size_t ml_off = 0, cut_off = 0;
+  const size_t need = chunk_workspace(c, std::min(max_new, n_rows), n_heads, &p.ws_rows, &ml_off, &cut_off);
   if (workspace_bytes < need) return fail(EAS_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, need);
   if ((reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return fail(EAS_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
   if (static_cast<int64_t>(s->max_blocks) * c->d.block_size > 0x7fffffffLL) return fail(EAS_ERR_UNSUPPORTED, "max_blocks %d is too large", s->max_blocks);
@@ -61,6 +62,7 @@ static eas_status chunk_attention(const eas_cache* c, const eas_cache_seqs* s, c
   p.scale_log2 = static_cast<float>(scale * kLog2e);
   p.o_ws = static_cast<float4*>(workspace);
   p.ml_ws = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + ml_off);
+  p.cut_ws = reinterpret_cast<ChunkItem*>(static_cast<uint8_t*>(workspace) + cut_off);
   p.status = status_dev;
   const bool all = budget == c->sm_count;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -84,8 +86,8 @@ extern "C" size_t eas_cache_chunk_workspace_bytes(const eas_cache* cache, int32_
     return 0;
   }
   int ws_rows = 0;
-  size_t ml_off = 0;
-  return chunk_workspace(cache, std::min(max_new, n_rows), n_heads, &ws_rows, &ml_off);
+  size_t ml_off = 0, cut_off = 0;
+  return chunk_workspace(cache, std::min(max_new, n_rows), n_heads, &ws_rows, &ml_off, &cut_off);
 }
 
 extern "C" eas_status eas_cache_chunk_attention(const eas_cache* cache, const eas_cache_seqs* seqs, const void* q, int64_t ld_q, void* out, int64_t ld_out,
