@@ -44,6 +44,7 @@ struct ChunkParams {
   uint16_t* out;
   long long ld_q, ld_out;
   int fp16, group, tile_tokens;
+  uint32_t by_group;           // ceil(2^32 / group), 0 for 1
   int n_ctas;                  // SMs of the device: pieces of the line, at most
   int ws_rows;                 // rows of a tile that the workspace holds
   float scale_log2;
@@ -82,6 +83,11 @@ struct ChunkCfg {
   // the producer is at most this many steps ahead of the softmax: a batch of scales, raw tiles, converted K tiles, one step each being read
   static_assert(6 + kRawTiles + 1 + kKTiles + 4 <= kScaleSlots, "a step's scales are read before their slot is filled again");
 };
+
+// row / group of a tile's row
+__device__ __forceinline__ int chunk_row_token(const ChunkParams& p, int row) {
+  return p.by_group == 0u ? row : static_cast<int>(__umulhi(static_cast<uint32_t>(row), p.by_group));      // (off by less than 128 / 2^32 < 1 / group)
+}
 
 // ------------------------------------------------------------------------------------ the line of units
 struct ChunkSeq {              // a sequence: its visible new tokens, the tokens in front of them, and what its tiles cost a head
@@ -172,9 +178,15 @@ struct ChunkUnit {
     }
     s = lo;
     seq = ChunkSeq(p, s, false);
-    const long long a_head = (prefix[s + 1] - prefix[s]) / p.c.n_kv;
+    const long long a_head = seq.total(p.tile_tokens);
     x -= prefix[s];
-    head = static_cast<int>(x / a_head);
+    lo = 0;
+    hi = p.c.n_kv - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (mid * a_head <= x) lo = mid; else hi = mid - 1;
+    }
+    head = lo;
     x -= head * a_head;
     lo = 0;
     hi = seq.units - 1;
@@ -203,7 +215,9 @@ struct ChunkUnit {
   // the first key step at or behind position x of the line: step k begins at `at` + unit cost + tiles * 80 k
   __device__ __forceinline__ int step_at(long long x) const {
     const long long in = x - at - kChunkUnitCost, width = static_cast<long long>(tiles) * kChunkKeys;
-    return in <= 0 ? 0 : static_cast<int>(min(static_cast<long long>(steps), (in + width - 1) / width));
+    if (in <= 0) return 0;
+    if (in >= steps * width) return steps;
+    return static_cast<int>((static_cast<uint32_t>(in) + static_cast<uint32_t>(width) - 1u) / static_cast<uint32_t>(width));      // (below 2^32: a sequence has at most 2^30 places)
   }
   __device__ __forceinline__ int steps_of_tile(const ChunkParams& p, int w) const {
     const long long last = min(static_cast<long long>(seq.n), static_cast<long long>(2 * j + w + 1) * p.tile_tokens);
@@ -264,6 +278,7 @@ static_assert(sizeof(ChunkItem) == 64, "four loads");
 // warp_mbar_wait in a few instructions: it stands in some twenty places, and the roles' loops share the instruction caches (see the measurements below).  The
 // bound is the same; a wait that ends by it raises the CTA's abort flag, and the others end by their own.
 __device__ __forceinline__ bool chunk_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* abort_flag) {
+  if (__builtin_expect(__all_sync(0xffffffffu, mbar_try_wait(bar, parity)), 1)) return true;
   uint32_t ok;
   asm volatile(
       "{\n\t.reg .pred p;\n\t.reg .u32 t0, t1;\n\t"
@@ -279,7 +294,7 @@ __device__ __forceinline__ bool chunk_wait(uint64_t* bar, uint32_t parity, volat
       "DONE%=:\n\t"
       "selp.u32 %0, 1, 0, p;\n\t}"
       : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
-  if (__builtin_expect(__all_sync(0xffffffffu, ok), 1)) return true;
+  if (__all_sync(0xffffffffu, ok)) return true;
   *abort_flag = 1u;
   return false;
 }
@@ -289,6 +304,13 @@ __device__ __forceinline__ void bulk_load(void* smem_dst, const void* src, uint3
 }
 __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+// f(integral constant i), one body for each i < N: a matrix instruction takes its descriptors from uniform registers, and what is not a constant to the compiler is moved
+// there for every one
+template <int N, typename F>
+__device__ __forceinline__ void for_constant(uint32_t i, F f) {
+  if (i == N - 1) f(std::integral_constant<int, N - 1>{});
+  else if constexpr (N > 1) for_constant<N - 1>(i, f);
 }
 __host__ __device__ constexpr uint32_t make_idesc_f16(int m, int n, int a_mn, int b_mn) {
   return make_idesc_bf16(m, n, a_mn, b_mn) & ~((1u << 7) | (1u << 10));
@@ -462,9 +484,13 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
           if (!chunk_wait(&raw_empty[st], ((tile / NR) & 1u) ^ 1u, abort_flag)) return false;
           if (lane == 0) mbar_expect_tx(&raw_full[st], __popc(have) * (16u * HD));
           __syncwarp();
-          if (there) {
-            const long long row = ((static_cast<long long>(id) * p.c.n_kv + head) << p.c.bs_log2) + place;
-            bulk_load(smem + L::kRawOff + st * L::kRawBytes + lane * 16 * HD, (values ? p.c.v : p.c.k) + row * HD, parts * 16 * HD, &raw_full[st]);
+          // one elected lane issues, with operands that are the same in all lanes
+          const int8_t* src = (values ? p.c.v : p.c.k) + (((static_cast<long long>(id) * p.c.n_kv + head) << p.c.bs_log2) + place) * HD;
+          for (uint32_t todo = __ballot_sync(0xffffffffu, there); todo != 0u; todo &= todo - 1u) {
+            const int l = __ffs(todo) - 1, n_parts = __shfl_sync(0xffffffffu, parts, l);
+            const int8_t* at_l = reinterpret_cast<const int8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), l));
+            if (elect_one()) bulk_load(smem + L::kRawOff + st * L::kRawBytes + l * 16 * HD, at_l, n_parts * 16 * HD, &raw_full[st]);
+            __syncwarp();
           }
           return true;
         };
@@ -562,16 +588,21 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
           if (!pass_k(g) || !chunk_wait(&k_full[g % NK], (g / NK) & 1u, abort_flag)) return false;
           if (n_s > 0 && !chunk_wait(&s_free[w], (n_s - 1u) & 1u, abort_flag)) return false;
           tc_fence_after_sync();
-          const uint64_t ad = make_smem_desc(q_tile(slot), 16, 1024, kSwizzle128B), bd = make_smem_desc(k_tile(g), 16, 1024, kSwizzle128B);
           if (elect_one()) {
+            const uint32_t ring = g % NK;
+            for_constant<2 * NK>(slot * NK + ring, [&](auto c) {
+              constexpr int Q = decltype(c)::value / NK, K = decltype(c)::value % NK;
+              const uint64_t ad = make_smem_desc(smem_at + Q * L::kQBytes, 16, 1024, kSwizzle128B);
+              const uint64_t bd = make_smem_desc(smem_at + L::kKOff + K * L::kTileBytes, 16, 1024, kSwizzle128B);
 #pragma unroll
-            for (int h = 0; h < L::kHalves; ++h)
+              for (int h = 0; h < L::kHalves; ++h)
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                umma_bf16_ss(tm_s, ad + h * (L::kQHalf >> 4) + 2 * k, bd + h * (L::kAtomBytes >> 4) + 2 * k, idesc_s, h != 0 || k != 0);
-            umma_commit(&s_full[w]);
-            umma_commit(&k_empty[g % NK]);
-            if (j == last) umma_commit(&q_empty[slot]);
+                for (int k = 0; k < 4; ++k)
+                  umma_bf16_ss(tm_s, ad + h * (L::kQHalf >> 4) + 2 * k, bd + h * (L::kAtomBytes >> 4) + 2 * k, idesc_s, h != 0 || k != 0);
+              umma_commit(&s_full[w]);
+              umma_commit(&k_empty[K]);
+              if (j == last) umma_commit(&q_empty[Q]);
+            });
           }
           __syncwarp();
           k_at = g + 1;
@@ -586,13 +617,16 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
           if (!pass_v(g) || !chunk_wait(&v_full[g % NV], (g / NV) & 1u, abort_flag) || !chunk_wait(&p_ready[w], n_p & 1u, abort_flag)) { ok = false; break; }
           ++n_p;
           tc_fence_after_sync();
-          const uint64_t bd = make_smem_desc(v_tile(g), L::kAtomBytes, 1024, kSwizzle128B);
           if (elect_one()) {
+            for_constant<NV>(g % NV, [&](auto c) {
+              constexpr int V = decltype(c)::value;
+              const uint64_t bd = make_smem_desc(smem_at + L::kVOff + V * L::kTileBytes, L::kAtomBytes, 1024, kSwizzle128B);
 #pragma unroll
-            for (int ks = 0; ks < KEYS / 16; ++ks)               // 16 keys: 8 columns of P, 2 KB of V
-              umma_bf16_ts(tm_o, tm_p + ks * 8, bd + ks * (2048 >> 4), idesc_o, (j != first || ks != 0) ? 1u : 0u);
-            umma_commit(&pv_done[w]);
-            umma_commit(&v_empty[g % NV]);
+              for (int ks = 0; ks < KEYS / 16; ++ks)             // 16 keys: 8 columns of P, 2 KB of V
+                umma_bf16_ts(tm_o, tm_p + ks * 8, bd + ks * (2048 >> 4), idesc_o, (j != first || ks != 0) ? 1u : 0u);
+              umma_commit(&pv_done[w]);
+              umma_commit(&v_empty[V]);
+            });
           }
           __syncwarp();
           v_at = g + 1;
@@ -666,56 +700,67 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
     };
     auto queries = [&](const ChunkItem& u, int t) {
       const uint32_t slot = qn & 1u;
-      constexpr int BATCH = 2;
+      constexpr int QBATCH = 4;
       const int rows = min(u.n_tok - u.tok0 - t * p.tile_tokens, p.tile_tokens) * p.group;      // (what the rows behind hold does not matter)
+      const uint16_t* const from = p.q + static_cast<long long>(u.q0 + u.tok0 + t * p.tile_tokens) * p.ld_q + u.head * p.group * HD + chunk * 16;
 #pragma unroll 1
-      for (int i0 = 0; i0 == 0 || i0 * 4 * ROWS < rows; i0 += BATCH) {
-        uint4 x[BATCH][2];
+      for (int row0 = cw * ROWS; row0 == cw * ROWS || row0 - cw * ROWS < rows; row0 += QBATCH * 4 * ROWS) {
+        uint4 x[QBATCH][2];
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
-          const int row = ((i0 + i) * 4 + cw) * ROWS + sub, row_tok = row / p.group, tok = u.tok0 + t * p.tile_tokens + row_tok;
+        for (int i = 0; i < QBATCH; ++i) {
+          const int row = row0 + i * 4 * ROWS + sub, row_tok = chunk_row_token(p, row);
           x[i][0] = x[i][1] = make_uint4(0u, 0u, 0u, 0u);
-          if (row_tok < p.tile_tokens && tok < u.n_tok) {
-            const uint4* src = reinterpret_cast<const uint4*>(p.q + static_cast<long long>(u.q0 + tok) * p.ld_q + (u.head * p.group + row - row_tok * p.group) * HD + chunk * 16);
+          if (row < rows) {
+            const uint4* src = reinterpret_cast<const uint4*>(from + row_tok * p.ld_q + (row - row_tok * p.group) * HD);
             x[i][0] = src[0];
             x[i][1] = src[1];
           }
         }
-        if (i0 == 0 && !chunk_wait(&q_empty[slot], ((qn >> 1) & 1u) ^ 1u, abort_flag)) return false;
+        if (row0 == cw * ROWS && !chunk_wait(&q_empty[slot], ((qn >> 1) & 1u) ^ 1u, abort_flag)) return false;
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
-          const int row = ((i0 + i) * 4 + cw) * ROWS + sub;
+        for (int i = 0; i < QBATCH; ++i) {
+          const int row = row0 + i * 4 * ROWS + sub;
           const uint32_t xw[8] = {x[i][0].x, x[i][0].y, x[i][0].z, x[i][0].w, x[i][1].x, x[i][1].y, x[i][1].z, x[i][1].w};
-          float y[16];
+          // the row's largest magnitude: as 16-bit integers, which order Inf above every number and NaN above Inf
+          uint32_t m2 = 0;
 #pragma unroll
-          for (int b = 0; b < 8; ++b) {
-            y[2 * b] = load16(static_cast<uint16_t>(xw[b] & 0xFFFFu), p.fp16);
-            y[2 * b + 1] = load16(static_cast<uint16_t>(xw[b] >> 16), p.fp16);
-          }
-          float mx = 0.f;
+          for (int b = 0; b < 8; ++b) m2 = __vmaxu2(m2, xw[b] & 0x7FFF7FFFu);
+          uint32_t m = max(m2 & 0xFFFFu, m2 >> 16);
 #pragma unroll
-          for (int b = 0; b < 16; ++b) mx = fmaxf(mx, fabsf(y[b]));
-#pragma unroll
-          for (int d = 1; d < 4; d *= 2) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-          if constexpr (HD == 128) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+          for (int d = 1; d < 4; d *= 2) m = max(m, __shfl_xor_sync(0xffffffffu, m, d));
+          if constexpr (HD == 128) m = max(m, __shfl_xor_sync(0xffffffffu, m, 8));
+          const float mx = load16(static_cast<uint16_t>(m), p.fp16);
           // the largest of the row to [2^14, 2^15) (fp16 ends at 65504), by an exponent of -126 to 126, so that both powers are normal numbers: what is
           // below 2^-39 of the row's largest is lost
-          const int e = mx > 0.f ? min(max(static_cast<int>(__float_as_uint(mx) >> 23) - 127 - 14, -126), 126) : 0;
+          const int e = m != 0u ? min(max(static_cast<int>(__float_as_uint(mx) >> 23) - 127 - 14, -126), 126) : 0;
           const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23), up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
-          uint32_t h[8];
-          float sum = 0.f;                         // of the numbers as fp16 has them
+          const uint64_t down2 = pack2(down, down);
+          uint64_t y[8], sum2 = 0;
 #pragma unroll
-          for (int b = 0; b < 4; ++b) {
-            h[2 * b] = Pair16<__half>::pack(y[4 * b] * down, y[4 * b + 2] * down);
-            h[2 * b + 1] = Pair16<__half>::pack(y[4 * b + 1] * down, y[4 * b + 3] * down);
-            sum += (Pair16<__half>::lo(h[2 * b]) + Pair16<__half>::hi(h[2 * b])) + (Pair16<__half>::lo(h[2 * b + 1]) + Pair16<__half>::hi(h[2 * b + 1]));
+          for (int b = 0; b < 8; ++b) {
+            y[b] = p.fp16 ? pack2(Pair16<__half>::lo(xw[b]), Pair16<__half>::hi(xw[b])) : pack2(Pair16<bf16>::lo(xw[b]), Pair16<bf16>::hi(xw[b]));
+            y[b] = fmul2(y[b], down2);             // (exact, and so is its rounding to fp16 but for what is lost)
+            sum2 = fadd2(sum2, y[b]);
           }
+          float sum, sum_hi;
+          unpack2(sum2, sum, sum_hi);
+          sum += sum_hi;
 #pragma unroll
           for (int d = 1; d < 4; d *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
           if constexpr (HD == 128) sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+          uint32_t h[8];
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            float y0, y1, y2, y3;
+            unpack2(y[2 * b], y0, y1);
+            unpack2(y[2 * b + 1], y2, y3);
+            h[2 * b] = Pair16<__half>::pack(y0, y2);
+            h[2 * b + 1] = Pair16<__half>::pack(y1, y3);
+          }
           store_row_16(q_tile(slot), L::kQHalf, row, chunk, h);
           // (an infinite element makes the row NaN: of -Inf alone its scores would count as masked)
-          if (chunk == 0) row_factor[slot * 128 + row] = make_float2(mx == INFINITY ? __uint_as_float(0x7FFFFFFFu) : p.scale_log2 * up * 16777216.f, sum * -7.62939453125e-06f);      // 2^24; -128 2^-24
+          if (chunk == 0)
+            row_factor[slot * 128 + row] = make_float2(mx * 0.f == 0.f ? p.scale_log2 * up * 16777216.f : __uint_as_float(0x7FFFFFFFu), sum * -7.62939453125e-06f);      // 2^24; -128 2^-24
         }
       }
       fence_proxy_async_smem();
@@ -739,7 +784,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
     const int w = (warp - 8) >> 2, quarter = warp & 3;                     // (the quarter of the tensor memory's lanes that the warp reads)
     const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
     const uint32_t s_addr = lane_addr + L::kSCol0 + w * L::kSStride, p_addr = s_addr + KEYS, o_addr = lane_addr + w * HD;
-    const int row = quarter * 32 + lane, row_tok = row / p.group;
+    const int row = quarter * 32 + lane, row_tok = chunk_row_token(p, row);
     uint32_t base = 0, qn = 0, n_s = 0, n_met = 0;                         // steps of the CTA, query tiles, the warpgroup's steps, meetings
     bool ok = true;
     while (ok) {
@@ -917,36 +962,36 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       }
       const float inv = l == 0.f ? 0.f : kWeightDown / l;
       const int col0 = alternate ? w * (HD / 2) : 0, cols = alternate ? HD / 2 : HD;
-      const uint32_t o_other = lane_addr + (1 - w) * HD;
-      const bool use_own = any, use_other = alternate && (both || !any);
+      // 16 columns of one O (without own steps: the other's), or of both, at a time
+      const bool two = alternate && both && any;
+      const uint32_t o_first = any || !alternate ? o_addr : lane_addr + (1 - w) * HD, o_second = lane_addr + (1 - w) * HD;
+      const float scale = part < 0 ? inv : 1.f, f_first = (any || !alternate ? f_own : f_other) * scale, f_second = f_other * scale;
 #pragma unroll 1
-      for (int c = col0; c < col0 + cols && active; c += 32) {
-        uint32_t o[32], x[32];
+      for (int c = col0; c < col0 + cols && active; c += 16) {
+        uint32_t o[16], x[16];
         __syncwarp();
-        if (use_own) tmem_ld_32x32(o_addr + c, o);
-        if (use_other) tmem_ld_32x32(o_other + c, x);
-        tmem_ld_wait_16<0>(o); tmem_ld_tie_16<16>(o);
-        tmem_ld_tie_16<0>(x); tmem_ld_tie_16<16>(x);
-        float y[32];
+        tmem_ld_32x16(o_first + c, o);
+        if (two) tmem_ld_32x16(o_second + c, x);
+        tmem_ld_wait_16<0>(o);
+        tmem_ld_tie_16<0>(x);
+        float y[16];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          const float a = use_own ? __uint_as_float(o[i]) * f_own : 0.f;
-          const float v = use_other ? fmaf(__uint_as_float(x[i]), f_other, a) : a;
-          y[(i & ~3) | ((i & 1) << 1) | ((i >> 1) & 1)] = v;     // four dimensions lie in the order 0, 2, 1, 3
+        for (int i = 0; i < 16; ++i) {
+          const float v = __uint_as_float(o[i]) * f_first;
+          y[(i & ~3) | ((i & 1) << 1) | ((i >> 1) & 1)] = two ? fmaf(__uint_as_float(x[i]), f_second, v) : v;      // four dimensions lie in the order 0, 2, 1, 3
         }
         if (stored && part < 0) {
 #pragma unroll
-          for (int i = 0; i < 32; i += 8) {
+          for (int i = 0; i < 16; i += 8) {
             uint32_t z[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              z[e] = p.fp16 ? Pair16<__half>::pack(y[i + 2 * e] * inv, y[i + 2 * e + 1] * inv) : Pair16<bf16>::pack(y[i + 2 * e] * inv, y[i + 2 * e + 1] * inv);
+            for (int e = 0; e < 4; ++e) z[e] = p.fp16 ? Pair16<__half>::pack(y[i + 2 * e], y[i + 2 * e + 1]) : Pair16<bf16>::pack(y[i + 2 * e], y[i + 2 * e + 1]);
             *reinterpret_cast<uint4*>(dst + c + i) = make_uint4(z[0], z[1], z[2], z[3]);
           }
         } else if (stored) {
           float4* to = p.o_ws + (static_cast<long long>(part) * (HD / 4) + c / 4) * p.ws_rows + row;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) to[i * p.ws_rows] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+          for (int i = 0; i < 4; ++i) to[i * p.ws_rows] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
         }
       }
       if (stored && part >= 0 && (!alternate || w == 0)) p.ml_ws[static_cast<long long>(part) * p.ws_rows + row] = make_float2(l == 0.f ? -INFINITY : m, l);
@@ -987,9 +1032,9 @@ __global__ void __launch_bounds__(512, 1) chunk_join_kernel(const __grid_constan
   }
   pdl_wait();
   if (p.early_launch) pdl_launch_dependents();
-  const int row = threadIdx.x & 127, row_tok = row / p.group, row_head = row - row_tok * p.group;
+  const int row = threadIdx.x & 127, row_tok = chunk_row_token(p, row), row_head = row - row_tok * p.group;
   for (int it = blockIdx.x * 4 + (threadIdx.x >> 7); it < p.n_ctas * 2 * CHUNKS; it += gridDim.x * 4) {
-    const int piece = it / (2 * CHUNKS), t = it / CHUNKS % 2, col0 = it % CHUNKS * COLS;
+    const int sub = it / p.n_ctas, piece = it - sub * p.n_ctas, t = sub / CHUNKS, col0 = sub % CHUNKS * COLS;      // (few pieces have a first cut: they are spread over the CTAs)
     const ChunkItem& u = p.cut_ws[piece];
     if (u.n == 0 || t >= u.tiles) continue;
     const int tok = u.tok0 + t * p.tile_tokens + row_tok, parts = u.parts;

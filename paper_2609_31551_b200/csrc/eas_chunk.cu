@@ -53,11 +53,12 @@ static eas_status chunk_attention(const eas_cache* c, const eas_cache_seqs* s, c
   const size_t need = chunk_workspace(c, std::min(max_new, n_rows), n_heads, &p.ws_rows, &ml_off, &cut_off);
   if (workspace_bytes < need) return fail(EAS_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, need);
   if ((reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return fail(EAS_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
-  if (static_cast<int64_t>(s->max_blocks) * c->d.block_size > 0x7fffffffLL) return fail(EAS_ERR_UNSUPPORTED, "max_blocks %d is too large", s->max_blocks);
+  if (static_cast<int64_t>(s->max_blocks) * c->d.block_size > (1LL << 30)) return fail(EAS_ERR_UNSUPPORTED, "max_blocks %d: more than 2^30 places a sequence", s->max_blocks);
   p.c = view_of(c);
   p.ld_table = s->ld_table; p.max_blocks = s->max_blocks; p.n_rows = n_rows; p.max_new = max_new;
   p.q = static_cast<const uint16_t*>(q); p.out = static_cast<uint16_t*>(out);
   p.ld_q = ld_q; p.ld_out = ld_out; p.fp16 = dtype == EAS_DTYPE_FP16; p.group = n_heads / G; p.tile_tokens = 128 / p.group;
+  p.by_group = p.group == 1 ? 0u : static_cast<uint32_t>(((1ull << 32) + p.group - 1) / p.group);
   p.n_ctas = c->sm_count;
   p.scale_log2 = static_cast<float>(scale * kLog2e);
   p.o_ws = static_cast<float4*>(workspace);
