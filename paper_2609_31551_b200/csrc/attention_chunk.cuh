@@ -60,7 +60,7 @@ struct ChunkCfg {
   static constexpr int kHalves = HD / 64;
   static constexpr int kRawTiles = HD == 128 ? 3 : 6, kKTiles = HD == 128 ? 2 : 3, kVTiles = HD == 128 ? 2 : 3;
   static constexpr int kThreads = 512;
-  static constexpr int kRegsLight = 64, kRegsConvert = 80, kRegsSoftmax = 184, kRegsLaunch = 128;
+  static constexpr int kRegsLight = 80, kRegsConvert = 96, kRegsSoftmax = 168, kRegsLaunch = 128;
   static constexpr int kQHalf = 128 * 128, kQBytes = kQHalf * kHalves;                 // 128 rows x 64 elements
   static constexpr int kAtomBytes = kChunkKeys * 128, kTileBytes = kAtomBytes * kHalves;   // 80 keys x 64 elements
   static constexpr int kRawBytes = kChunkKeys * HD;
@@ -845,63 +845,58 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
         tc_fence_before_sync();
         __syncwarp();
         mbar_arrive_if(&s_free[w], lane == 0);
+#pragma unroll
+        for (int m = 0; m < PARTS; ++m) {
+          sc[m] *= factor.x;
+          sc[PARTS + m] = fmaf(factor.y, sc[m], sc[PARTS + m]);
+        }
+        if (__builtin_expect(__any_sync(0xffffffffu, left < KEYS), 0)) {
+          // keys that the row does not see: -inf, against factors that are not 0; a part that it does not see at all has scales of its own (NaN, maybe)
+#pragma unroll
+          for (int i = 0; i < KEYS; ++i) if (i >= left) s[i] = 0xff800000u;
+#pragma unroll
+          for (int m = 0; m < PARTS; ++m) {
+            const bool hidden = 16 * m >= left;
+            sc[m] = hidden || sc[m] == 0.f ? 1e-37f : sc[m];
+            sc[PARTS + m] = hidden ? 0.f : sc[PARTS + m];
+            sc[2 * PARTS + m] = hidden ? 0.f : sc[2 * PARTS + m];
+          }
+        }
+        // largest t: of each 16 scores the largest, scaled
+        float mx = -INFINITY;
+#pragma unroll
+        for (int m = 0; m < PARTS; ++m) {
+          float c0 = __uint_as_float(s[16 * m]), c1 = __uint_as_float(s[16 * m + 1]);
+#pragma unroll
+          for (int i = 16 * m + 2; i < 16 * m + 14; i += 4) {
+            c0 = fmax3(c0, __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
+            c1 = fmax3(c1, __uint_as_float(s[i + 2]), __uint_as_float(s[i + 3]));
+          }
+          c0 = fmax3(c0, __uint_as_float(s[16 * m + 14]), __uint_as_float(s[16 * m + 15]));
+          mx = fmaxf(mx, fmaf(fmaxf(c0, c1), sc[m], sc[PARTS + m]));
+        }
+        // the reference moves to 2^7 below the row's largest t when that comes more than 2^15 above it, and to the first one above -inf
         const float m_old = m_ref;
-        bool moved;
+        const bool moved = mx > m_ref + kRefMoves;
+        m_ref = moved ? mx - kRefBelow : m_ref;
+        const float mb = m_ref == -INFINITY ? 0.f : m_ref;
         uint64_t sum2 = 0;
         uint32_t pk[KEYS / 2];
-        auto weigh = [&](auto cut) {                             // cut: some row of the warp does not see all keys of the step
-          constexpr bool CUT = decltype(cut)::value;
-          // largest t: of each 16 scores the largest, scaled
-          float mx = -INFINITY;
 #pragma unroll
-          for (int m = 0; m < PARTS; ++m) {
-            if constexpr (CUT) {
+        for (int m = 0; m < PARTS; ++m) {
+          const uint64_t c2 = pack2(sc[m], sc[m]), b2 = pack2(sc[PARTS + m] - mb, sc[PARTS + m] - mb);
+          uint64_t part2[2] = {0, 0};
 #pragma unroll
-              for (int i = 16 * m; i < 16 * m + 16; ++i) if (i >= left) s[i] = 0xff800000u;   // -inf
-            }
-            float c0 = -INFINITY, c1 = -INFINITY;
-#pragma unroll
-            for (int i = 16 * m; i < 16 * m + 16; i += 4) {
-              c0 = fmax3(c0, __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
-              c1 = fmax3(c1, __uint_as_float(s[i + 2]), __uint_as_float(s[i + 3]));
-            }
-            sc[m] *= factor.x;
-            sc[PARTS + m] = fmaf(factor.y, sc[m], sc[PARTS + m]);
-            const float t = fmaf(fmaxf(c0, c1), sc[m], sc[PARTS + m]);
-            if (CUT && 16 * m >= left) {                         // (a hidden block's scale may be anything)
-              sc[m] = 1.f;
-              sc[PARTS + m] = 0.f;
-              sc[2 * PARTS + m] = 0.f;
-            } else {
-              mx = fmaxf(mx, t);
-            }
+          for (int i = 0; i < 8; ++i) {
+            float p0, p1;
+            unpack2(ffma2(pack2(__uint_as_float(s[16 * m + 2 * i]), __uint_as_float(s[16 * m + 2 * i + 1])), c2, b2), p0, p1);
+            p0 = fast_ex2(p0);
+            p1 = fast_ex2(p1);
+            part2[i & 1] = i < 2 ? pack2(p0, p1) : fadd2(part2[i & 1], pack2(p0, p1));
+            pk[8 * m + i] = Pair16<__half>::pack(p0, p1);
           }
-          // the reference moves to 2^7 below the row's largest t when that comes more than 2^15 above it, and to the first one above -inf
-          moved = mx > m_ref + kRefMoves;
-          m_ref = moved ? mx - kRefBelow : m_ref;
-          const float mb = m_ref == -INFINITY ? 0.f : m_ref;
-#pragma unroll
-          for (int m = 0; m < PARTS; ++m) {
-            const uint64_t c2 = pack2(sc[m], sc[m]), b2 = pack2(sc[PARTS + m] - mb, sc[PARTS + m] - mb);
-            uint64_t part2 = 0;
-#pragma unroll
-            for (int i = 8 * m; i < 8 * m + 8; ++i) {
-              float p0, p1;
-              unpack2(ffma2(pack2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c2, b2), p0, p1);
-              if constexpr (CUT) {                               // (-inf times a scale of 0 is NaN)
-                if (2 * i >= left) p0 = -INFINITY;
-                if (2 * i + 1 >= left) p1 = -INFINITY;
-              }
-              p0 = fast_ex2(p0);
-              p1 = fast_ex2(p1);
-              part2 = i == 8 * m ? pack2(p0, p1) : fadd2(part2, pack2(p0, p1));
-              pk[i] = Pair16<__half>::pack(p0, p1);
-            }
-            sum2 = ffma2(part2, pack2(sc[2 * PARTS + m], sc[2 * PARTS + m]), sum2);
-          }
-        };
-        if (__builtin_expect(__any_sync(0xffffffffu, left < KEYS), 0)) weigh(std::true_type{});
-        else weigh(std::false_type{});
+          sum2 = ffma2(fadd2(part2[0], part2[1]), pack2(sc[2 * PARTS + m], sc[2 * PARTS + m]), sum2);
+        }
         const uint32_t rescale = __ballot_sync(0xffffffffu, moved && any);
         // P goes where the previous step's was, and O may change: that step's P V has to be complete
         if (any) {
