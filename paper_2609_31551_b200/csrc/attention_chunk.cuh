@@ -277,9 +277,14 @@ static_assert(sizeof(ChunkItem) == 64, "four loads");
 // ------------------------------------------------------------------------------------ small pieces
 // warp_mbar_wait in a few instructions: it stands in some twenty places, and the roles' loops share the instruction caches (see the measurements below).  The
 // bound is the same; a wait that ends by it raises the CTA's abort flag, and the others end by their own.
-__device__ __forceinline__ bool chunk_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* abort_flag) {
-  if (__builtin_expect(__all_sync(0xffffffffu, mbar_try_wait(bar, parity)), 1)) return true;
+__device__ __forceinline__ bool chunk_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag) {
   uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  if (__builtin_expect(__all_sync(0xffffffffu, ok), 1)) return true;
   asm volatile(
       "{\n\t.reg .pred p;\n\t.reg .u32 t0, t1;\n\t"
       "mov.u32 t0, %%clock;\n\t"
@@ -293,14 +298,26 @@ __device__ __forceinline__ bool chunk_wait(uint64_t* bar, uint32_t parity, volat
       "setp.ne.u32 p, t1, t1;\n\t"
       "DONE%=:\n\t"
       "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   if (__all_sync(0xffffffffu, ok)) return true;
   *abort_flag = 1u;
   return false;
 }
-__device__ __forceinline__ void bulk_load(void* smem_dst, const void* src, uint32_t bytes, uint64_t* bar) {
+// barriers by their address in shared memory
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void mbar_arrive_if(uint32_t bar, bool pred) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %1, 0;\n\t@p mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(bar), "r"(static_cast<uint32_t>(pred)) : "memory");
+}
+__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void umma_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void bulk_load(void* smem_dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-               ::"r"(smem_u32(smem_dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+               ::"r"(smem_u32(smem_dst)), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
@@ -340,38 +357,39 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
   float* sc_ring = reinterpret_cast<float*>(smem + L::kScaleOff);
   float2* row_factor = reinterpret_cast<float2*>(smem + L::kRowOff);      // what a row's scores are multiplied by, and what is added to them before
   float2* ml_smem = reinterpret_cast<float2*>(smem + L::kMlOff);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBarOff);
-  uint64_t* raw_full = bars;                 // [2 NR] bytes of a tile landed: keys, values
-  uint64_t* raw_empty = raw_full + 2 * NR;   // [2 NR] converted
-  uint64_t* k_full = raw_empty + 2 * NR;     // [NK] fp16 tile written
-  uint64_t* k_empty = k_full + NK;           // [NK] every issuer hands every tile back
-  uint64_t* v_full = k_empty + NK;           // [NV]
-  uint64_t* v_empty = v_full + NV;           // [NV]
-  uint64_t* sc_full = v_empty + NV;          // [NS] scales of a step written
-  uint64_t* q_full = sc_full + NS;           // [2] queries and their rows' factors
-  uint64_t* q_empty = q_full + 2;            // [2] by both issuers and all softmax warps
-  uint64_t* s_full = q_empty + 2;            // [2] scores of a step complete
-  uint64_t* p_ready = s_full + 2;            // [2] P stored, O rescaled if it had to be
-  uint64_t* s_free = p_ready + 2;            // [2] scores read out of tensor memory
-  uint64_t* pv_done = s_free + 2;            // [2] P V of a step complete
-  uint64_t* met = pv_done + 2;               // [2] alternate: both warpgroups' sums are there; both have read O
-  uint64_t* item_full = met + 2;             // [kChunkItems]
-  uint64_t* item_empty = item_full + kChunkItems;      // by the 15 other warps
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(item_empty + kChunkItems);
+  // barriers: addresses in shared memory, 8 bytes each
+  const uint32_t smem_at = smem_u32(smem);
+  const uint32_t raw_full = smem_at + L::kBarOff;         // [2 NR] bytes of a tile landed: keys, values
+  const uint32_t raw_empty = raw_full + 8 * 2 * NR;       // [2 NR] converted
+  const uint32_t k_full = raw_empty + 8 * 2 * NR;         // [NK] fp16 tile written
+  const uint32_t k_empty = k_full + 8 * NK;               // [NK] every issuer hands every tile back
+  const uint32_t v_full = k_empty + 8 * NK;               // [NV]
+  const uint32_t v_empty = v_full + 8 * NV;               // [NV]
+  const uint32_t sc_full = v_empty + 8 * NV;              // [NS] scales of a step written
+  const uint32_t q_full = sc_full + 8 * NS;               // [2] queries and their rows' factors
+  const uint32_t q_empty = q_full + 16;                   // [2] by both issuers and all softmax warps
+  const uint32_t s_full = q_empty + 16;                   // [2] scores of a step complete
+  const uint32_t p_ready = s_full + 16;                   // [2] P stored, O rescaled if it had to be
+  const uint32_t s_free = p_ready + 16;                   // [2] scores read out of tensor memory
+  const uint32_t pv_done = s_free + 16;                   // [2] P V of a step complete
+  const uint32_t met = pv_done + 16;                      // [2] alternate: both warpgroups' sums are there; both have read O
+  const uint32_t item_full = met + 16;                    // [kChunkItems]
+  const uint32_t item_empty = item_full + 8 * kChunkItems;      // by the 15 other warps
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::kBarOff + 8 * L::kBars);
   volatile uint32_t* abort_flag = tmem_slot + 1;
   long long* scan_sums = reinterpret_cast<long long*>(tmem_slot + 2);                    // [16]
 
   const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 2 * NR; ++i) { mbar_init(&raw_full[i], 1); mbar_init(&raw_empty[i], 2); }
-    for (int i = 0; i < NK; ++i) { mbar_init(&k_full[i], 2); mbar_init(&k_empty[i], 2); }
-    for (int i = 0; i < NV; ++i) { mbar_init(&v_full[i], 2); mbar_init(&v_empty[i], 2); }
-    for (int i = 0; i < NS; ++i) mbar_init(&sc_full[i], 1);
+    for (int i = 0; i < 2 * NR; ++i) { mbar_init(raw_full + 8 * i, 1); mbar_init(raw_empty + 8 * i, 2); }
+    for (int i = 0; i < NK; ++i) { mbar_init(k_full + 8 * i, 2); mbar_init(k_empty + 8 * i, 2); }
+    for (int i = 0; i < NV; ++i) { mbar_init(v_full + 8 * i, 2); mbar_init(v_empty + 8 * i, 2); }
+    for (int i = 0; i < NS; ++i) mbar_init(sc_full + 8 * i, 1);
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&q_full[i], 4); mbar_init(&q_empty[i], 10); mbar_init(&s_full[i], 1); mbar_init(&p_ready[i], 4);
-      mbar_init(&s_free[i], 4); mbar_init(&pv_done[i], 1); mbar_init(&met[i], 8);
+      mbar_init(q_full + 8 * i, 4); mbar_init(q_empty + 8 * i, 10); mbar_init(s_full + 8 * i, 1); mbar_init(p_ready + 8 * i, 4);
+      mbar_init(s_free + 8 * i, 4); mbar_init(pv_done + 8 * i, 1); mbar_init(met + 8 * i, 8);
     }
-    for (int i = 0; i < kChunkItems; ++i) { mbar_init(&item_full[i], 1); mbar_init(&item_empty[i], 15); }
+    for (int i = 0; i < kChunkItems; ++i) { mbar_init(item_full + 8 * i, 1); mbar_init(item_empty + 8 * i, 15); }
     *abort_flag = 0;
     mbar_fence_init();
   }
@@ -387,7 +405,6 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
   if (p.early_launch) pdl_launch_dependents();     // behind the wait: the joining kernel reads the lengths ahead of its own
   chunk_prefix(p, prefix, scan_sums, blockIdx.x == 0);
 
-  const uint32_t smem_at = smem_u32(smem);
   auto q_tile = [&](uint32_t slot) { return smem_at + slot * L::kQBytes; };
   auto k_tile = [&](uint32_t g) { return smem_at + L::kKOff + g % NK * L::kTileBytes; };
   auto v_tile = [&](uint32_t g) { return smem_at + L::kVOff + g % NV * L::kTileBytes; };
@@ -396,12 +413,12 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
   uint32_t n_items = 0;                            // taken by this warp
   auto take = [&](ChunkItem& it) {                 // the next item; false after an expired wait
     const uint32_t at = n_items % kChunkItems;
-    if (!chunk_wait(&item_full[at], (n_items / kChunkItems) & 1u, abort_flag)) return false;
+    if (!chunk_wait(item_full + 8 * at, (n_items / kChunkItems) & 1u, abort_flag)) return false;
     const uint4* src = reinterpret_cast<const uint4*>(item_ring + at);
 #pragma unroll
     for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(&it)[i] = src[i];
     __syncwarp();
-    mbar_arrive_if(&item_empty[at], lane == 0);
+    mbar_arrive_if(item_empty + 8 * at, lane == 0);
     ++n_items;
     return true;
   };
@@ -415,10 +432,10 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
         for (int piece = blockIdx.x; piece < p.n_ctas; piece += gridDim.x) p.cut_ws[piece].n = 0;
       auto put = [&](const ChunkItem& it) {
         const uint32_t at = n_items % kChunkItems;
-        if (!chunk_wait(&item_empty[at], ((n_items / kChunkItems) & 1u) ^ 1u, abort_flag)) return false;
+        if (!chunk_wait(item_empty + 8 * at, ((n_items / kChunkItems) & 1u) ^ 1u, abort_flag)) return false;
         if (lane == 0) {
           item_ring[at] = it;
-          mbar_arrive(&item_full[at]);
+          mbar_arrive(item_full + 8 * at);
         }
         __syncwarp();
         ++n_items;
@@ -481,15 +498,15 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
           const bool there = (have >> lane & 1u) && (lane == 0 || place == 0);      // a lane copies from its part to the end of the block, or of what there is
           const int parts = min(((1 << p.c.bs_log2) - place) >> 4, __popc(have >> lane));
           const uint32_t tile = values ? at_v++ : at_k++, st = (values ? NR : 0) + tile % NR;
-          if (!chunk_wait(&raw_empty[st], ((tile / NR) & 1u) ^ 1u, abort_flag)) return false;
-          if (lane == 0) mbar_expect_tx(&raw_full[st], __popc(have) * (16u * HD));
+          if (!chunk_wait(raw_empty + 8 * st, ((tile / NR) & 1u) ^ 1u, abort_flag)) return false;
+          if (lane == 0) mbar_expect_tx(raw_full + 8 * st, __popc(have) * (16u * HD));
           __syncwarp();
           // one elected lane issues, with operands that are the same in all lanes
           const int8_t* src = (values ? p.c.v : p.c.k) + (((static_cast<long long>(id) * p.c.n_kv + head) << p.c.bs_log2) + place) * HD;
           for (uint32_t todo = __ballot_sync(0xffffffffu, there); todo != 0u; todo &= todo - 1u) {
             const int l = __ffs(todo) - 1, n_parts = __shfl_sync(0xffffffffu, parts, l);
             const int8_t* at_l = reinterpret_cast<const int8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), l));
-            if (elect_one()) bulk_load(smem + L::kRawOff + st * L::kRawBytes + l * 16 * HD, at_l, n_parts * 16 * HD, &raw_full[st]);
+            if (elect_one()) bulk_load(smem + L::kRawOff + st * L::kRawBytes + l * 16 * HD, at_l, n_parts * 16 * HD, raw_full + 8 * st);
             __syncwarp();
           }
           return true;
@@ -511,7 +528,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
             dst[2 * PARTS] = id >= 0 ? fast_ex2(-lg) * kWeightDown : 0.f;
           }
           __syncwarp();
-          if (lane < steps) mbar_arrive(&sc_full[(step + lane) % NS]);
+          if (lane < steps) mbar_arrive(sc_full + 8 * ((step + lane) % NS));
         };
         int now = load_ids(0), next = load_ids(kBatch);
         now = checked(now, 0);
@@ -537,7 +554,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       }
       // every copy has landed before the CTA's shared memory passes to another one: converted, or (after an expired wait) by time
       for (uint32_t e = g < NR ? 0 : g - NR; e < g && ok; ++e)
-        ok = chunk_wait(&raw_empty[e % NR], (e / NR) & 1u, abort_flag) && chunk_wait(&raw_empty[NR + e % NR], (e / NR) & 1u, abort_flag);
+        ok = chunk_wait(raw_empty + 8 * (e % NR), (e / NR) & 1u, abort_flag) && chunk_wait(raw_empty + 8 * (NR + e % NR), (e / NR) & 1u, abort_flag);
       if (!ok) {
         const long long t0 = clock64();
         while (clock64() - t0 < 4000000) {}
@@ -553,15 +570,15 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       bool ok = true;
       auto pass_k = [&](uint32_t to) {
         for (; k_at < to; ++k_at) {
-          if (!chunk_wait(&k_full[k_at % NK], (k_at / NK) & 1u, abort_flag)) return false;
-          mbar_arrive_if(&k_empty[k_at % NK], lane == 0);
+          if (!chunk_wait(k_full + 8 * (k_at % NK), (k_at / NK) & 1u, abort_flag)) return false;
+          mbar_arrive_if(k_empty + 8 * (k_at % NK), lane == 0);
         }
         return true;
       };
       auto pass_v = [&](uint32_t to) {
         for (; v_at < to; ++v_at) {
-          if (!chunk_wait(&v_full[v_at % NV], (v_at / NV) & 1u, abort_flag)) return false;
-          mbar_arrive_if(&v_empty[v_at % NV], lane == 0);
+          if (!chunk_wait(v_full + 8 * (v_at % NV), (v_at / NV) & 1u, abort_flag)) return false;
+          mbar_arrive_if(v_empty + 8 * (v_at % NV), lane == 0);
         }
         return true;
       };
@@ -578,15 +595,15 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
         // queries: wait for each tile of the item, hand back what is not used
         for (int t = 0; t < tiles && ok; ++t) {
           const uint32_t q = qn + t;
-          ok = chunk_wait(&q_full[q & 1u], (q >> 1) & 1u, abort_flag);
-          if (ok && ((q & 1u) != slot || last < 0)) mbar_arrive_if(&q_empty[q & 1u], lane == 0);
+          ok = chunk_wait(q_full + 8 * (q & 1u), (q >> 1) & 1u, abort_flag);
+          if (ok && ((q & 1u) != slot || last < 0)) mbar_arrive_if(q_empty + 8 * (q & 1u), lane == 0);
         }
         qn += tiles;
         if (!ok) break;
         auto scores = [&](int j) {                 // of step j, into the warpgroup's columns once they are read
           const uint32_t g = base + j;
-          if (!pass_k(g) || !chunk_wait(&k_full[g % NK], (g / NK) & 1u, abort_flag)) return false;
-          if (n_s > 0 && !chunk_wait(&s_free[w], (n_s - 1u) & 1u, abort_flag)) return false;
+          if (!pass_k(g) || !chunk_wait(k_full + 8 * (g % NK), (g / NK) & 1u, abort_flag)) return false;
+          if (n_s > 0 && !chunk_wait(s_free + 8 * w, (n_s - 1u) & 1u, abort_flag)) return false;
           tc_fence_after_sync();
           if (elect_one()) {
             const uint32_t ring = g % NK;
@@ -599,9 +616,9 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
                   umma_bf16_ss(tm_s, ad + h * (L::kQHalf >> 4) + 2 * k, bd + h * (L::kAtomBytes >> 4) + 2 * k, idesc_s, h != 0 || k != 0);
-              umma_commit(&s_full[w]);
-              umma_commit(&k_empty[K]);
-              if (j == last) umma_commit(&q_empty[Q]);
+              umma_commit(s_full + 8 * w);
+              umma_commit(k_empty + 8 * K);
+              if (j == last) umma_commit(q_empty + 8 * Q);
             });
           }
           __syncwarp();
@@ -614,7 +631,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
           if (j < last && !scores(j + stride)) { ok = false; break; }
           if (j < first) continue;
           const uint32_t g = base + j;
-          if (!pass_v(g) || !chunk_wait(&v_full[g % NV], (g / NV) & 1u, abort_flag) || !chunk_wait(&p_ready[w], n_p & 1u, abort_flag)) { ok = false; break; }
+          if (!pass_v(g) || !chunk_wait(v_full + 8 * (g % NV), (g / NV) & 1u, abort_flag) || !chunk_wait(p_ready + 8 * w, n_p & 1u, abort_flag)) { ok = false; break; }
           ++n_p;
           tc_fence_after_sync();
           if (elect_one()) {
@@ -624,8 +641,8 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
 #pragma unroll
               for (int ks = 0; ks < KEYS / 16; ++ks)             // 16 keys: 8 columns of P, 2 KB of V
                 umma_bf16_ts(tm_o, tm_p + ks * 8, bd + ks * (2048 >> 4), idesc_o, (j != first || ks != 0) ? 1u : 0u);
-              umma_commit(&pv_done[w]);
-              umma_commit(&v_empty[V]);
+              umma_commit(pv_done + 8 * w);
+              umma_commit(v_empty + 8 * V);
             });
           }
           __syncwarp();
@@ -637,9 +654,9 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       }
       // the last hand-backs are asynchronous arrivals: in before the CTA ends
       if (ok && w == 0) {
-        for (uint32_t e = base < NK ? 0 : base - NK; e < base && ok; ++e) ok = chunk_wait(&k_empty[e % NK], (e / NK) & 1u, abort_flag);
-        for (uint32_t e = base < NV ? 0 : base - NV; e < base && ok; ++e) ok = chunk_wait(&v_empty[e % NV], (e / NV) & 1u, abort_flag);
-        for (uint32_t e = qn < 2 ? 0 : qn - 2; e < qn && ok; ++e) ok = chunk_wait(&q_empty[e & 1u], (e >> 1) & 1u, abort_flag);
+        for (uint32_t e = base < NK ? 0 : base - NK; e < base && ok; ++e) ok = chunk_wait(k_empty + 8 * (e % NK), (e / NK) & 1u, abort_flag);
+        for (uint32_t e = base < NV ? 0 : base - NV; e < base && ok; ++e) ok = chunk_wait(v_empty + 8 * (e % NV), (e / NV) & 1u, abort_flag);
+        for (uint32_t e = qn < 2 ? 0 : qn - 2; e < qn && ok; ++e) ok = chunk_wait(q_empty + 8 * (e & 1u), (e >> 1) & 1u, abort_flag);
       }
     }
   } else if (warp < 8) {
@@ -661,12 +678,12 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
     const int row = (cw & 1) * ROWS + sub;
     const uint32_t raw0 = smem_at + L::kRawOff + (keys ? 0 : NR) * L::kRawBytes + chunk * 16 + row * HD;
     const uint32_t tile0 = smem_at + (keys ? L::kKOff : L::kVOff) + (chunk >> 2) * L::kAtomBytes + row * 128 + (((2 * (chunk & 3)) ^ (row & 7)) << 4);
-    uint64_t *const from_full = raw_full + (keys ? 0 : NR), *const from_empty = raw_empty + (keys ? 0 : NR);
-    uint64_t *const full = keys ? k_full : v_full, *const empty = keys ? k_empty : v_empty;
+    const uint32_t from_full = raw_full + (keys ? 0 : 8 * NR), from_empty = raw_empty + (keys ? 0 : 8 * NR);
+    const uint32_t full = keys ? k_full : v_full, empty = keys ? k_empty : v_empty;
     const uint32_t ring = keys ? NK : NV;
     uint32_t st = 0, landed = 0, to = 0, gone = 1;                         // places in the two rings, and the phases to wait for
     auto convert = [&]() {
-      if (!chunk_wait(&from_full[st], landed, abort_flag) || !chunk_wait(&empty[to], gone, abort_flag)) return false;
+      if (!chunk_wait(from_full + 8 * st, landed, abort_flag) || !chunk_wait(empty + 8 * to, gone, abort_flag)) return false;
       const uint32_t src = raw0 + st * L::kRawBytes, dst = tile0 + to * L::kTileBytes;
 #pragma unroll 1
       for (int i0 = 0; i0 < PASSES; i0 += BATCH) {
@@ -692,8 +709,8 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       }
       fence_proxy_async_smem();
       __syncwarp();
-      mbar_arrive_if(&from_empty[st], lane == 0);
-      mbar_arrive_if(&full[to], lane == 0);
+      mbar_arrive_if(from_empty + 8 * st, lane == 0);
+      mbar_arrive_if(full + 8 * to, lane == 0);
       if (++st == NR) { st = 0; landed ^= 1u; }
       if (++to == ring) { to = 0; gone ^= 1u; }
       return true;
@@ -716,7 +733,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
             x[i][1] = src[1];
           }
         }
-        if (row0 == cw * ROWS && !chunk_wait(&q_empty[slot], ((qn >> 1) & 1u) ^ 1u, abort_flag)) return false;
+        if (row0 == cw * ROWS && !chunk_wait(q_empty + 8 * slot, ((qn >> 1) & 1u) ^ 1u, abort_flag)) return false;
 #pragma unroll
         for (int i = 0; i < QBATCH; ++i) {
           const int row = row0 + i * 4 * ROWS + sub;
@@ -765,7 +782,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       }
       fence_proxy_async_smem();
       __syncwarp();
-      mbar_arrive_if(&q_full[slot], lane == 0);
+      mbar_arrive_if(q_full + 8 * slot, lane == 0);
       ++qn;
       return true;
     };
@@ -799,11 +816,11 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       float2 factor = make_float2(0.f, 0.f);
       for (int t = 0; t < tiles && ok; ++t) {
         const uint32_t q = qn + t;
-        ok = chunk_wait(&q_full[q & 1u], (q >> 1) & 1u, abort_flag);
+        ok = chunk_wait(q_full + 8 * (q & 1u), (q >> 1) & 1u, abort_flag);
         if (!ok) break;
         if ((q & 1u) == slot) factor = row_factor[slot * 128 + row];
         __syncwarp();
-        mbar_arrive_if(&q_empty[q & 1u], lane == 0);
+        mbar_arrive_if(q_empty + 8 * (q & 1u), lane == 0);
       }
       qn += tiles;
       if (!ok) break;
@@ -816,40 +833,44 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       int left = stored ? u.ahead + tok + 1 - (u.lo + first) * KEYS : 0x7fffffff;      // keys from the present step on that this row sees (rows that are not stored: all, for what they compute does not matter)
       float m_ref = -INFINITY;
       uint64_t l2 = 0;                             // row sum, two halves
-      bool any = false;                            // the warpgroup has a step of the item
-#pragma unroll 1
-      for (int j = first; j < mine; j += stride, left -= stored ? stride * KEYS : 0) {
-        const uint32_t g = base + j;
-        if (!chunk_wait(&s_full[w], n_s & 1u, abort_flag)) { ok = false; break; }
-        ++n_s;
-        if (!active) {
-          mbar_arrive_if(&s_free[w], lane == 0);
-          if (any && !chunk_wait(&pv_done[w], n_s & 1u, abort_flag)) { ok = false; break; }      // (in front of it, p_ready may still be in the phase before)
-          mbar_arrive_if(&p_ready[w], lane == 0);
-          any = true;
-          continue;
+      bool any = false;                            // O holds a step of the item
+      if (!active) {
+        for (int j = first; j < mine && ok; j += stride) {
+          ok = chunk_wait(s_full + 8 * w, n_s & 1u, abort_flag);
+          ++n_s;
+          mbar_arrive_if(s_free + 8 * w, lane == 0);
+          ok = ok && chunk_wait(pv_done + 8 * w, n_s & 1u, abort_flag);    // (in front of it, p_ready may still be in the phase before)
+          mbar_arrive_if(p_ready + 8 * w, lane == 0);
         }
-        tc_fence_after_sync();
-        uint32_t s[KEYS];
-        tmem_ld_32x32_at<0>(s_addr, s);
-        tmem_ld_32x32_at<32>(s_addr, s);
-        tmem_ld_32x16_at<64>(s_addr, s);
-        if (!chunk_wait(&sc_full[g % NS], (g / NS) & 1u, abort_flag)) { ok = false; break; }
+      }
+      const int fewer = stored ? stride * KEYS : 0;
+#pragma unroll 1
+      for (int j = first; j < mine && active; j += stride, left -= fewer) {
+        const uint32_t g = base + j;
+        // factors and offsets of the step's parts, beside the product
+        if (!chunk_wait(sc_full + 8 * (g % NS), (g / NS) & 1u, abort_flag)) { ok = false; break; }
         float sc[16];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float4 x = reinterpret_cast<const float4*>(sc_ring + (g % NS) * 16)[i];
           sc[4 * i] = x.x; sc[4 * i + 1] = x.y; sc[4 * i + 2] = x.z; sc[4 * i + 3] = x.w;
         }
-        tmem_ld_wait_16<0>(s); tmem_ld_tie_16<16>(s); tmem_ld_tie_16<32>(s); tmem_ld_tie_16<48>(s); tmem_ld_tie_16<64>(s);
-        tc_fence_before_sync();
-        __syncwarp();
-        mbar_arrive_if(&s_free[w], lane == 0);
 #pragma unroll
         for (int m = 0; m < PARTS; ++m) {
           sc[m] *= factor.x;
           sc[PARTS + m] = fmaf(factor.y, sc[m], sc[PARTS + m]);
         }
+        if (!chunk_wait(s_full + 8 * w, n_s & 1u, abort_flag)) { ok = false; break; }
+        ++n_s;
+        tc_fence_after_sync();
+        uint32_t s[KEYS];
+        tmem_ld_32x32_at<0>(s_addr, s);
+        tmem_ld_32x32_at<32>(s_addr, s);
+        tmem_ld_32x16_at<64>(s_addr, s);
+        tmem_ld_wait_16<0>(s); tmem_ld_tie_16<16>(s); tmem_ld_tie_16<32>(s); tmem_ld_tie_16<48>(s); tmem_ld_tie_16<64>(s);
+        tc_fence_before_sync();
+        __syncwarp();
+        mbar_arrive_if(s_free + 8 * w, lane == 0);
         if (__builtin_expect(__any_sync(0xffffffffu, left < KEYS), 0)) {
           // keys that the row does not see: -inf, against factors that are not 0; a part that it does not see at all has scales of its own (NaN, maybe)
 #pragma unroll
@@ -899,10 +920,9 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
         }
         const uint32_t rescale = __ballot_sync(0xffffffffu, moved && any);
         // P goes where the previous step's was, and O may change: that step's P V has to be complete
-        if (any) {
-          if (!chunk_wait(&pv_done[w], n_s & 1u, abort_flag)) { ok = false; break; }
-          tc_fence_after_sync();
-        }
+        // (at an item's first step it is known to be: the same phase again)
+        if (!chunk_wait(pv_done + 8 * w, n_s & 1u, abort_flag)) { ok = false; break; }
+        tc_fence_after_sync();
         if (__builtin_expect(rescale != 0u, 0)) {
           const float corr = moved ? fast_ex2(m_old - m_ref) : 1.0f;      // (from no reference: 0)
           l2 = ffma2(l2, pack2(corr, corr), sum2);
@@ -925,14 +945,15 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
         tmem_st_wait();
         tc_fence_before_sync();
         __syncwarp();
-        mbar_arrive_if(&p_ready[w], lane == 0);
+        mbar_arrive_if(p_ready + 8 * w, lane == 0);
         any = true;
       }
       base += n;
       if (!ok) break;
+      any = first < mine;
       // the item's end
       if (any) {
-        if (!chunk_wait(&pv_done[w], (n_s - 1u) & 1u, abort_flag)) { ok = false; break; }
+        if (!chunk_wait(pv_done + 8 * w, (n_s - 1u) & 1u, abort_flag)) { ok = false; break; }
         tc_fence_after_sync();
       }
       float l, l_hi;
@@ -944,8 +965,8 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
         ml_smem[w * 128 + row] = make_float2(m, l);
         tc_fence_before_sync();
         __syncwarp();
-        mbar_arrive_if(&met[0], lane == 0);
-        if (!chunk_wait(&met[0], n_met & 1u, abort_flag)) { ok = false; break; }
+        mbar_arrive_if(met, lane == 0);
+        if (!chunk_wait(met, n_met & 1u, abort_flag)) { ok = false; break; }
         tc_fence_after_sync();
         const float2 other = ml_smem[(1 - w) * 128 + row];
         both = n > 1;                              // (of one step: the first warpgroup's alone)
@@ -993,8 +1014,8 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       if (alternate) {
         tc_fence_before_sync();
         __syncwarp();
-        mbar_arrive_if(&met[1], lane == 0);
-        if (!chunk_wait(&met[1], n_met & 1u, abort_flag)) { ok = false; break; }
+        mbar_arrive_if(met + 8, lane == 0);
+        if (!chunk_wait(met + 8, n_met & 1u, abort_flag)) { ok = false; break; }
         tc_fence_after_sync();
         ++n_met;
       }
