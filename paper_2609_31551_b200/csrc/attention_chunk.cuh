@@ -5,8 +5,8 @@
 // cache enter as they are, exact in fp16, as in attention_cache.cuh: queries are fp16 times a power of two per row, a block's key scale multiplies its scores in
 // fp32, its value scale v is an exponent: with t = score + log2 v and w = 2^(t - m),  out = sum w number / sum w / v, m being kept 2^7 to 2^15 below the largest t.
 //
-//   warp 3        walks the line of units (below) and tells the others the items of the CTA, through a ring
-//   warp 0        bytes of K and V, 16 tokens a bulk copy (they are contiguous), into a ring of 8-bit tiles; the scales of a step
+//   warps 0, 3    bytes of K and of V, a block's tokens of a head (they are contiguous) a bulk copy, into rings of 8-bit tiles; warp 0 the scales of the steps, too, and
+//                 warp 3 walks the line of units (below) and tells the others the items of the CTA, through a ring
 //   warps 1, 2    UMMA issuers, one per softmax warpgroup
 //   warps 4 ..    converters: tiles of queries, then two warps those of K and two those of V, from bytes to fp16 in the tensor core's layout.  (0x6400 | (byte ^ 0x80)) - 1152: one logic operation and
 //                 one subtraction for the bytes 0 and 2 of a word, a shift more for 1 and 3; so four dimensions lie in the order 0, 2, 1, 3, in the queries and the output too
@@ -237,7 +237,7 @@ struct ChunkDeal {
       : p(params), prefix(pre), line(pre[params.n_seqs], params.n_ctas), piece(blockIdx.x), lo(0), hi(0), end(0), more(true) {
     seek(true);
   }
-  __device__ __forceinline__ void next() { seek(false); }
+  __device__ __forceinline__ void next() { if (more) seek(false); }
   __device__ __forceinline__ void seek(bool fresh) {               // fresh: the first item of `piece`; else the one behind the present one
     for (;;) {
       if (fresh) {
@@ -425,136 +425,133 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
 
   if (warp < 4) {
     setmaxnreg_dec<L::kRegsLight>();
-    if (warp == 3) {
-      // ------------------------------------------------------------------ the CTA's items
-      bool ok = true;
-      if (lane == 0)
-        for (int piece = blockIdx.x; piece < p.n_ctas; piece += gridDim.x) p.cut_ws[piece].n = 0;
-      auto put = [&](const ChunkItem& it) {
-        const uint32_t at = n_items % kChunkItems;
-        if (!chunk_wait(item_empty + 8 * at, ((n_items / kChunkItems) & 1u) ^ 1u, abort_flag)) return false;
-        if (lane == 0) {
-          item_ring[at] = it;
-          mbar_arrive(item_full + 8 * at);
-        }
-        __syncwarp();
-        ++n_items;
-        return true;
-      };
-      for (ChunkDeal deal(p, prefix); deal.more && ok; deal.next()) {
-        const ChunkUnit& u = deal.u;
-        ChunkItem it;
-        it.lo = deal.lo;
-        it.n = deal.hi - deal.lo;
-        it.tiles = u.tiles;
-        it.mine[0] = min(deal.hi, u.steps_of_tile(p, 0)) - deal.lo;
-        it.mine[1] = min(deal.hi, u.steps_of_tile(p, 1)) - deal.lo;
-        it.q0 = u.seq.q0;
-        it.tok0 = 2 * u.j * p.tile_tokens;
-        it.n_tok = u.seq.n;
-        it.ahead = u.seq.ahead;
-        it.head = u.head;
-        it.s = u.s;
-        it.seen = u.seq.seen(u.j, p.tile_tokens);
-        it.slot = it.n == u.steps ? -1 : 2 * deal.piece + (deal.hi == u.steps ? 0 : 1);
-        it.parts = 0;
-        if (deal.lo == 0 && deal.hi < u.steps) {
-          it.parts = deal.line.piece_of(u.at + kChunkUnitCost + static_cast<long long>(u.tiles) * KEYS * (u.steps - 1)) - deal.piece + 1;
-          if (lane == 0) p.cut_ws[deal.piece] = it;
-        }
-        ok = put(it);
-      }
-      if (ok) {
-        ChunkItem none{};
-        put(none);
-      }
-    } else if (warp == 0) {
-      // ------------------------------------------------------------------ bytes and scales
-      // The order of the tiles: K of step 0; then K of step j + 1 and V of step j (the scores of a step are wanted before the values of the one in front)
-      uint32_t g = 0, at_k = 0, at_v = 0;          // steps, tiles of keys and of values so far
-      bool ok = true;
-      for (;;) {
-        ChunkItem it;
-        ok = take(it);
-        if (!ok || it.n == 0) break;
-        const int lo = it.lo, n = it.n, seen = it.seen, head = it.head;
+    if (warp == 0 || warp == 3) {
+      // ------------------------------------------------------------------ bytes: of keys (warp 0, which has the scales too) and of values (warp 3)
+      const bool values = warp == 3;
+      const int8_t* const cache = values ? p.c.v : p.c.k;
+      const uint32_t full = raw_full + (values ? 8 * NR : 0), empty = raw_empty + (values ? 8 * NR : 0);
+      const uint32_t raw = L::kRawOff + (values ? NR * L::kRawBytes : 0);
+      uint32_t g = 0;                              // steps so far
+      uint32_t st = 0, free = 1;                   // the ring's next place, and the phase in which it is empty
+      // A lane has a part of 16 tokens of the kBatch steps at hand.  Block numbers are asked for two batches ahead and scales one: they come from anywhere in memory.
+      constexpr int kBatch = 6;
+      static_assert(kBatch * PARTS <= 32, "a lane has a part");
+      auto stream = [&](const ChunkItem& it) {
         const int32_t* ids = p.table + it.s * p.ld_table;
-        // Block numbers and scales of kBatch steps at once, a part of 16 tokens a lane, asked for one or two batches ahead: they come from anywhere in memory
-        constexpr int kBatch = 6;
-        static_assert(kBatch * PARTS <= 32, "a lane has a part");
-        auto load_ids = [&](int j0) {              // lane m: the block of tokens 16 m .. of steps j0 ..
-          const int tok = (lo + j0) * KEYS + lane * 16;
-          return lane < kBatch * PARTS && j0 + lane / PARTS < n && tok < seen ? ids[tok >> p.c.bs_log2] : -1;
-        };
+        const int my_step = lane / PARTS, my_part = lane - my_step * PARTS, bs = 1 << p.c.bs_log2;
+        auto wanted = [&](int j0) { return my_step < kBatch && j0 + my_step < it.n && (it.lo + j0) * KEYS + lane * 16 < it.seen; };
+        auto load_id = [&](int j0) { return wanted(j0) ? ids[((it.lo + j0) * KEYS + lane * 16) >> p.c.bs_log2] : -1; };
         auto checked = [&](int id, int j0) {       // (where the number is wanted, not where it is asked for)
           if (static_cast<uint32_t>(id) < static_cast<uint32_t>(p.c.n_blocks)) return id;
-          if (lane < kBatch * PARTS && j0 + lane / PARTS < n && (lo + j0) * KEYS + lane * 16 < seen) raise_status(p.status, DEV_ERR_CACHE_RANGE);
+          if (wanted(j0)) raise_status(p.status, DEV_ERR_CACHE_RANGE);
           return -1;
-        };
-        auto copy = [&](bool values, int batch_ids, int at, int j) {      // step j, the batch's step `at`
-          const int id = __shfl_sync(0xffffffffu, batch_ids, (at * PARTS + lane) & 31);
-          const uint32_t have = __ballot_sync(0xffffffffu, lane < PARTS && id >= 0);
-          const int tok = (lo + j) * KEYS + lane * 16, place = tok & ((1 << p.c.bs_log2) - 1);
-          const bool there = (have >> lane & 1u) && (lane == 0 || place == 0);      // a lane copies from its part to the end of the block, or of what there is
-          const int parts = min(((1 << p.c.bs_log2) - place) >> 4, __popc(have >> lane));
-          const uint32_t tile = values ? at_v++ : at_k++, st = (values ? NR : 0) + tile % NR;
-          if (!chunk_wait(raw_empty + 8 * st, ((tile / NR) & 1u) ^ 1u, abort_flag)) return false;
-          if (lane == 0) mbar_expect_tx(raw_full + 8 * st, __popc(have) * (16u * HD));
-          __syncwarp();
-          // one elected lane issues, with operands that are the same in all lanes
-          const int8_t* src = (values ? p.c.v : p.c.k) + (((static_cast<long long>(id) * p.c.n_kv + head) << p.c.bs_log2) + place) * HD;
-          for (uint32_t todo = __ballot_sync(0xffffffffu, there); todo != 0u; todo &= todo - 1u) {
-            const int l = __ffs(todo) - 1, n_parts = __shfl_sync(0xffffffffu, parts, l);
-            const int8_t* at_l = reinterpret_cast<const int8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), l));
-            if (elect_one()) bulk_load(smem + L::kRawOff + st * L::kRawBytes + l * 16 * HD, at_l, n_parts * 16 * HD, raw_full + 8 * st);
-            __syncwarp();
-          }
-          return true;
         };
         auto load_scales = [&](int id) {
           float2 sc = make_float2(0.f, 0.f);
-          if (id >= 0) {
-            const long long at = static_cast<long long>(id) * p.c.n_kv + head;
+          if (!values && id >= 0) {
+            const long long at = static_cast<long long>(id) * p.c.n_kv + it.head;
             sc = make_float2(p.c.k_scale[at], p.c.v_scale[at]);
           }
           return sc;
         };
-        auto publish = [&](float2 sc, int id, uint32_t step, int steps) {
-          if (lane < steps * PARTS) {
-            float* dst = sc_ring + (step + lane / PARTS) % NS * 16 + lane % PARTS;
-            const float vs = sc.y < kCacheMinScale ? kCacheMinScale : sc.y, lg = fast_lg2(vs);      // (a NaN stays)
-            dst[0] = id >= 0 ? sc.x : 0.f;
-            dst[PARTS] = id >= 0 ? lg : -INFINITY;
-            dst[2 * PARTS] = id >= 0 ? fast_ex2(-lg) * kWeightDown : 0.f;
-          }
-          __syncwarp();
-          if (lane < steps) mbar_arrive(sc_full + 8 * ((step + lane) % NS));
-        };
-        int now = load_ids(0), next = load_ids(kBatch);
-        now = checked(now, 0);
-        ok = copy(false, now, 0, 0);
+        int now = checked(load_id(0), 0), next = load_id(kBatch);
         float2 sc = load_scales(now);
-        for (int j0 = 0; j0 < n && ok; j0 += kBatch) {
-          const int behind = load_ids(j0 + 2 * kBatch);
+        for (int j0 = 0; j0 < it.n; j0 += kBatch) {
+          const int behind = load_id(j0 + 2 * kBatch), steps = min(kBatch, it.n - j0);
+          // a lane copies from its part to the end of the block, of the step, or of what there is: the tokens of a head and block lie side by side
+          const int place = ((it.lo + j0) * KEYS + lane * 16) & (bs - 1);
+          const uint32_t have = __ballot_sync(0xffffffffu, now >= 0), lead = __ballot_sync(0xffffffffu, now >= 0 && (my_part == 0 || place == 0));
+          const int bytes = min((bs - place) >> 4, __popc(have >> lane & ((1u << (PARTS - my_part)) - 1u))) * (16 * HD);
+          const unsigned long long src = reinterpret_cast<unsigned long long>(cache + (((static_cast<long long>(now) * p.c.n_kv + it.head) << p.c.bs_log2) + place) * HD);
           next = checked(next, j0 + kBatch);
           const float2 sc_next = load_scales(next);
-          const int steps = min(kBatch, n - j0);
 #pragma unroll 1
-          for (int i = 0; i < 2 * steps && ok; ++i) {              // K of step j + 1, V of step j
-            const int at = (i >> 1) + (i & 1 ? 0 : 1), j = j0 + at;
-            if (j < n) ok = copy(i & 1, at < kBatch ? now : next, at < kBatch ? at : 0, j);
-            if (i == 1) publish(sc, now, g, steps);
+          for (int i = 0; i < steps; ++i) {
+            if (!chunk_wait(empty + 8 * st, free, abort_flag)) return false;
+            if (lane == 0) mbar_expect_tx(full + 8 * st, __popc(have >> (i * PARTS) & ((1u << PARTS) - 1u)) * (16u * HD));
+            __syncwarp();
+            // one elected lane issues, with operands that are the same in all lanes
+            for (uint32_t todo = lead & (((1u << PARTS) - 1u) << (i * PARTS)); todo != 0u; todo &= todo - 1u) {
+              const int l = __ffs(todo) - 1, n_bytes = __shfl_sync(0xffffffffu, bytes, l);
+              const unsigned long long from = __shfl_sync(0xffffffffu, src, l);
+              if (elect_one()) bulk_load(smem + raw + st * L::kRawBytes + (l - i * PARTS) * 16 * HD, reinterpret_cast<const void*>(from), n_bytes, full + 8 * st);
+              __syncwarp();
+            }
+            if (++st == NR) { st = 0; free ^= 1u; }
+            if (i == 0 && !values) {               // the batch's scales
+              if (lane < steps * PARTS) {
+                float* dst = sc_ring + (g + my_step) % NS * 16 + my_part;
+                const float vs = sc.y < kCacheMinScale ? kCacheMinScale : sc.y, lg = fast_lg2(vs);      // (a NaN stays)
+                dst[0] = now >= 0 ? sc.x : 0.f;
+                dst[PARTS] = now >= 0 ? lg : -INFINITY;
+                dst[2 * PARTS] = now >= 0 ? fast_ex2(-lg) * kWeightDown : 0.f;
+              }
+              __syncwarp();
+              if (lane < steps) mbar_arrive(sc_full + 8 * ((g + lane) % NS));
+            }
           }
           g += steps;
           now = next;
           next = behind;
           sc = sc_next;
         }
-        if (!ok) break;
+        return true;
+      };
+      bool ok = true;
+      if (!values) {
+        while (ok) {
+          ChunkItem it;
+          ok = take(it);
+          if (!ok || it.n == 0) break;
+          ok = stream(it);
+        }
+      } else {
+        // the items of the CTA, one ahead of their values
+        if (lane == 0)
+          for (int piece = blockIdx.x; piece < p.n_ctas; piece += gridDim.x) p.cut_ws[piece].n = 0;
+        ChunkDeal deal(p, prefix);
+        auto put = [&]() {
+          ChunkItem it{};
+          if (deal.more) {
+            const ChunkUnit& u = deal.u;
+            it.lo = deal.lo;
+            it.n = deal.hi - deal.lo;
+            it.tiles = u.tiles;
+            it.mine[0] = min(deal.hi, u.steps_of_tile(p, 0)) - deal.lo;
+            it.mine[1] = min(deal.hi, u.steps_of_tile(p, 1)) - deal.lo;
+            it.q0 = u.seq.q0;
+            it.tok0 = 2 * u.j * p.tile_tokens;
+            it.n_tok = u.seq.n;
+            it.ahead = u.seq.ahead;
+            it.head = u.head;
+            it.s = u.s;
+            it.seen = u.seq.seen(u.j, p.tile_tokens);
+            it.slot = it.n == u.steps ? -1 : 2 * deal.piece + (deal.hi == u.steps ? 0 : 1);
+            if (deal.lo == 0 && deal.hi < u.steps) {
+              it.parts = deal.line.piece_of(u.at + kChunkUnitCost + static_cast<long long>(u.tiles) * KEYS * (u.steps - 1)) - deal.piece + 1;
+              if (lane == 0) p.cut_ws[deal.piece] = it;
+            }
+          }
+          const uint32_t at = n_items % kChunkItems;
+          ok = ok && chunk_wait(item_empty + 8 * at, ((n_items / kChunkItems) & 1u) ^ 1u, abort_flag);
+          if (ok && lane == 0) {
+            item_ring[at] = it;
+            mbar_arrive(item_full + 8 * at);
+          }
+          __syncwarp();
+          ++n_items;
+          return it;
+        };
+        ChunkItem it = put();
+        while (ok && it.n != 0) {
+          deal.next();
+          const ChunkItem next = put();
+          ok = ok && stream(it);
+          it = next;
+        }
       }
       // every copy has landed before the CTA's shared memory passes to another one: converted, or (after an expired wait) by time
-      for (uint32_t e = g < NR ? 0 : g - NR; e < g && ok; ++e)
-        ok = chunk_wait(raw_empty + 8 * (e % NR), (e / NR) & 1u, abort_flag) && chunk_wait(raw_empty + 8 * (NR + e % NR), (e / NR) & 1u, abort_flag);
+      for (uint32_t e = g < NR ? 0 : g - NR; e < g && ok; ++e) ok = chunk_wait(empty + 8 * (e % NR), (e / NR) & 1u, abort_flag);
       if (!ok) {
         const long long t0 = clock64();
         while (clock64() - t0 < 4000000) {}
