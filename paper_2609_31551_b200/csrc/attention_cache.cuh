@@ -43,7 +43,9 @@ struct CacheAttnParams {
   uint16_t* out;
   long long ld_q, ld_out;
   int fp16;                    // type of q and out: 0 bf16, 1 fp16
-  int group, row_blocks;       // query heads per key/value head; blocks of 8 NT of them
+  int group, row_blocks;       // query heads per key/value head; blocks of 8 NT of them (CHUNK: of the most rows that a sequence has)
+  const int32_t* cu;           // CHUNK: rows of each sequence's new tokens, their number, the most of a sequence and the most that this kernel takes
+  int n_rows, max_new, most_rows;
   int n_ctas;                  // CTAs of the whole device: the line has kWarps pieces for each
   float scale_log2;            // scale * log2(e)
   float* ml_ws;                // [2 pieces][8 NT rows][2]
@@ -68,7 +70,8 @@ struct CacheAttnCfg {
   static constexpr int kRows = 8 * NT;
   static constexpr int kPrefixOff = kWarps * kDepth * kStageBytes;
   static constexpr int kLenOff = kPrefixOff + (kCacheMaxSeqs + 4) * 4;
-  static constexpr int kBarOff = kLenOff + kCacheMaxSeqs * 4;
+  static constexpr int kNewOff = kLenOff + kCacheMaxSeqs * 4;                  // CHUNK
+  static constexpr int kBarOff = kNewOff + kCacheMaxSeqs * 8;
   static constexpr int kBytes = kBarOff + kWarps * kDepth * 8 + 80 + 1024;     // barriers, words, alignment slack
   static_assert(kBytes <= 232448, "exceeds the shared memory of an SM");
   static_assert(kBytes > 116224, "a second CTA must not fit beside this one");
@@ -116,9 +119,23 @@ __device__ __forceinline__ float fast_lg2(float x) {
   return y;
 }
 
-// Prefix sums over the sequences of what a row of tiles costs, by a whole CTA of 256 or more threads (4 sequences a thread): prefix[0 .. n_seqs].
-template <int TILE>
-__device__ __forceinline__ void cache_prefix(const CacheAttnParams& p, int* prefix, int* lens, int* sums, bool report) {
+// CHUNK: several new tokens a sequence, its last ones.  Their query heads are the columns, in the order of the tokens, and a column sees the places up to its token's
+// own; 8 NT columns make a row of tiles.  Sequences of more columns than most_rows belong to another kernel (attention_chunk.cuh).
+struct CacheNew {
+  int q0, n;                   // the first row that sees something, and how many do
+  int given, first;
+  __device__ __forceinline__ CacheNew(const CacheAttnParams& p, int s, int len) {
+    first = min(max(p.cu[s], 0), p.n_rows);
+    given = max(min(max(p.cu[s + 1], 0), p.n_rows) - first, 0);
+    n = given > p.max_new || static_cast<long long>(given) * p.group > p.most_rows ? 0 : min(given, len);
+    q0 = first + given - n;
+  }
+};
+
+// Prefix sums over the sequences of what a row of tiles costs (CHUNK: of what all rows of tiles of the sequence do), by a whole CTA of 256 or more threads (4
+// sequences a thread): prefix[0 .. n_seqs].
+template <int TILE, int ROWS, bool CHUNK>
+__device__ __forceinline__ void cache_prefix(const CacheAttnParams& p, int* prefix, int* lens, int2* news, int* sums, bool report) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int t[4], sum = 0;
   if (threadIdx.x < 256) {
@@ -131,9 +148,19 @@ __device__ __forceinline__ void cache_prefix(const CacheAttnParams& p, int* pref
         n = static_cast<int>(most);
         if (report) raise_status(p.status, DEV_ERR_CACHE_RANGE);
       }
+      int rows = 1;
+      if constexpr (CHUNK) {
+        if (s < p.n_seqs) {
+          const CacheNew c(p, s, n);
+          if (report && c.given > p.max_new) raise_status(p.status, DEV_ERR_CACHE_RANGE);
+          rows = (c.n * p.group + ROWS - 1) / ROWS * p.c.n_kv;
+          if (rows == 0) n = 0;
+          if (news != nullptr) news[s] = make_int2(c.q0, c.n);
+        }
+      }
       if (lens != nullptr && s < p.n_seqs) lens[s] = n;
       t[i] = sum;
-      sum += n > 0 ? (n + TILE - 1) / TILE + kRowCost : 0;
+      sum += n > 0 ? ((n + TILE - 1) / TILE + kRowCost) * rows : 0;
     }
   }
   int incl = sum;
@@ -155,7 +182,7 @@ __device__ __forceinline__ void cache_prefix(const CacheAttnParams& p, int* pref
   __syncthreads();
 }
 
-template <int HD, int NT>
+template <int HD, int NT, bool CHUNK = false>
 __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_attention_kernel(const __grid_constant__ CacheAttnParams p) {
   using L = CacheAttnCfg<HD, NT>;
   constexpr int TILE = L::kTile, MT = L::kMt, ROWS = L::kRows, WARPS = L::kWarps, DEPTH = L::kDepth;
@@ -163,6 +190,7 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw_cache) + 1023) & ~uintptr_t(1023));
   int* sm_prefix = reinterpret_cast<int*>(smem + L::kPrefixOff);         // cost of a row of tiles, summed over the sequences before
   int* sm_len = reinterpret_cast<int*>(smem + L::kLenOff);
+  int2* sm_new = reinterpret_cast<int2*>(smem + L::kNewOff);             // CHUNK: first row, rows' tokens
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBarOff);       // [warp][stage] tile landed
   int* sm_sum = reinterpret_cast<int*>(bars + WARPS * DEPTH);            // [16] sums of the scan's warps; the rows that go on behind the warps
   volatile uint32_t* abort_flag = reinterpret_cast<uint32_t*>(sm_sum + 16);
@@ -177,9 +205,11 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
   }
   pdl_wait();
   if (p.early_launch) pdl_launch_dependents();     // behind the wait: the joining kernel reads the lengths ahead of its own
-  cache_prefix<TILE>(p, sm_prefix, sm_len, sm_sum, blockIdx.x == 0);
-  const int R = p.c.n_kv * p.row_blocks;                         // rows of tiles a sequence has
-  const CacheLine line(sm_prefix[p.n_seqs], R, p.n_ctas * WARPS);
+  cache_prefix<TILE, ROWS, CHUNK>(p, sm_prefix, sm_len, sm_new, sm_sum, blockIdx.x == 0);
+  const int R = p.c.n_kv * p.row_blocks;                         // rows of tiles a sequence has (CHUNK: at most)
+  const CacheLine line(sm_prefix[p.n_seqs], CHUNK ? 1 : R, p.n_ctas * WARPS);
+  auto blocks_of = [&](int s) { return CHUNK ? (sm_new[s].y * p.group + ROWS - 1) / ROWS : p.row_blocks; };
+  auto cost_of = [&](int s) { return CHUNK ? (sm_len[s] + TILE - 1) / TILE + kRowCost : sm_prefix[s + 1] - sm_prefix[s]; };      // of a row of tiles (that has some)
   const int qg = lane >> 2, qt = lane & 3;
   const int box_log2 = min(p.c.bs_log2, 5);
   uint8_t* const ring = smem + warp * DEPTH * L::kStageBytes;
@@ -195,7 +225,7 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
     int s0 = 0;
     {
       int hi = p.n_seqs - 1;
-      const int x = min(begin, line.total - 1) / R;
+      const int x = min(begin, line.total - 1) / (CHUNK ? 1 : R);
       while (s0 < hi) {                                          // the last sequence that begins at or before x (those without tiles are passed over)
         const int mid = (s0 + hi + 1) >> 1;
         if (sm_prefix[mid] <= x) s0 = mid; else hi = mid - 1;
@@ -204,22 +234,23 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
     // A walk along the line's rows from the piece's beginning.  One walker issues loads, DEPTH tiles ahead of the one that computes.
     struct Walk {
       int s, row, tile, n_tiles, left;      // sequence, row, next tile, tiles of the row; positions of the piece from the row's end on
-      int kvh, len;                         // the row's key/value head, the sequence's length
+      int kvh, len, blocks;                 // the row's key/value head, the sequence's length, its rows a key/value head
       const int32_t* ids;                   // and its line of the block table
     };
     auto at_row = [&](Walk& w) {
-      w.kvh = p.row_blocks == 1 ? w.row : w.row / p.row_blocks;
+      w.blocks = blocks_of(w.s);
+      w.kvh = w.blocks == 1 ? w.row : w.row / w.blocks;
       w.len = sm_len[w.s];
       w.ids = p.table + w.s * p.ld_table;
     };
     auto enter = [&](Walk& w) {             // at a row's first tile (or past it, at the piece's beginning)
       while (w.n_tiles <= w.tile && w.left > 0) {                // behind the row's last tile: the next row
-        if (++w.row == R) {
+        if (++w.row == (CHUNK ? p.c.n_kv * w.blocks : R)) {
           w.row = 0;
           do ++w.s; while (w.s < p.n_seqs && sm_prefix[w.s + 1] == sm_prefix[w.s]);
           if (w.s >= p.n_seqs) { w.left = 0; return; }
         }
-        const int cost = sm_prefix[w.s + 1] - sm_prefix[w.s];
+        const int cost = cost_of(w.s);
         w.n_tiles = min(cost, w.left) - kRowCost;                // tiles of it that belong to this piece
         w.left -= cost;
         w.tile = 0;
@@ -228,7 +259,7 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
     };
     Walk iw;
     {
-      const int cost = sm_prefix[s0 + 1] - sm_prefix[s0], in_seq = begin - sm_prefix[s0] * R, row = in_seq / cost, at = in_seq - row * cost;
+      const int cost = cost_of(s0), in_seq = begin - sm_prefix[s0] * (CHUNK ? 1 : R), row = in_seq / cost, at = in_seq - row * cost;
       iw.s = s0;
       iw.row = row;
       iw.tile = max(at - kRowCost, 0);
@@ -320,9 +351,22 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
     }
 
     while (more(cw) && ok) {
-      const int s = cw.s, kvh = cw.kvh, head0 = (cw.row - kvh * p.row_blocks) * ROWS;      // head0: within the group
-      const int n_rows = min(ROWS, p.group - head0);
-      const int first = cw.tile, last = cw.n_tiles, row_tiles = sm_prefix[s + 1] - sm_prefix[s] - kRowCost, len = cw.len;
+      const int s = cw.s, kvh = cw.kvh, head0 = (cw.row - kvh * cw.blocks) * ROWS;      // head0: within the group
+      const int q0 = CHUNK ? sm_new[s].x : s, n_new = CHUNK ? sm_new[s].y : 1;
+      const int n_rows = min(ROWS, n_new * p.group - head0);
+      const int first = cw.tile, last = cw.n_tiles, row_tiles = cost_of(s) - kRowCost, len = cw.len;
+      auto token_of = [&](int r) { return CHUNK ? (head0 + r) / p.group : 0; };                // of row r, and the place of its query or output
+      auto at_row_of = [&](int r, long long ld) {
+        const int tok = token_of(r);
+        return (q0 + tok) * ld + static_cast<long long>(kvh * p.group + head0 + r - tok * p.group) * HD;
+      };
+      int limit[NT][2];                                          // CHUNK: places that this lane's columns see
+      if constexpr (CHUNK) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) limit[j][b] = len - n_new + 1 + min(token_of(j * 8 + 2 * qt + b), n_new - 1);
+      }
       float m_ref[NT][2], l[NT][2], o[HD / 16][NT][4];
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
@@ -338,7 +382,7 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
       for (int j = 0; j < NT; ++j) {
         const int h = j * 8 + qg;
         float x[HD / 4];
-        const uint16_t* src = p.q + s * p.ld_q + static_cast<long long>(kvh * p.group + head0 + h) * HD + qt * (HD / 4);
+        const uint16_t* src = p.q + at_row_of(CHUNK ? min(h, n_rows - 1) : h, p.ld_q) + qt * (HD / 4);
 #pragma unroll
         for (int i = 0; i < HD / 32; ++i) {
           const uint4 v = h < n_rows ? *reinterpret_cast<const uint4*>(src + i * 8) : make_uint4(0u, 0u, 0u, 0u);
@@ -408,7 +452,7 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
         float mx[NT][2];
 #pragma unroll
         for (int j = 0; j < NT; ++j) mx[j][0] = mx[j][1] = -INFINITY;
-        const bool cut = tile * TILE + TILE > len || some[0] != (1u << MT) - 1u;
+        const bool cut = tile * TILE + TILE > (CHUNK ? len - n_new + 1 : len) || some[0] != (1u << MT) - 1u;
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
           const float ks = __shfl_sync(0xffffffffu, scales[0].x, m), lg = __shfl_sync(0xffffffffu, lane_lg, m);
@@ -424,10 +468,21 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
           if (cut) {                                             // tokens behind the sequence's end, or without a block
             const int left = some[0] & (1u << m) ? len - tile * TILE - m * 16 : 0;
             if (left <= 0) v_inv[m] = 0.f;
+            if constexpr (CHUNK) {
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-              if (qg >= left) sc[m][j][0] = sc[m][j][1] = -INFINITY;
-              if (qg + 8 >= left) sc[m][j][2] = sc[m][j][3] = -INFINITY;
+              for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                  const int seen = min(left, limit[j][b] - tile * TILE - m * 16);
+                  if (qg >= seen) sc[m][j][b] = -INFINITY;
+                  if (qg + 8 >= seen) sc[m][j][b + 2] = -INFINITY;
+                }
+            } else {
+#pragma unroll
+              for (int j = 0; j < NT; ++j) {
+                if (qg >= left) sc[m][j][0] = sc[m][j][1] = -INFINITY;
+                if (qg + 8 >= left) sc[m][j][2] = sc[m][j][3] = -INFINITY;
+              }
             }
           }
 #pragma unroll
@@ -471,8 +526,13 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
             const float r0 = ref[j][0], r1 = ref[j][1];
             const float w0 = fast_ex2(sc[m][j][0] - r0), w1 = fast_ex2(sc[m][j][1] - r1);
             const float w2 = fast_ex2(sc[m][j][2] - r0), w3 = fast_ex2(sc[m][j][3] - r1);
-            l[j][0] = fmaf(w0 + w2, v_inv[m], l[j][0]);
-            l[j][1] = fmaf(w1 + w3, v_inv[m], l[j][1]);
+            if (CHUNK && cut) {                                  // (the scale of a part that the column does not see may be NaN)
+              if (limit[j][0] > tile * TILE + m * 16) l[j][0] = fmaf(w0 + w2, v_inv[m], l[j][0]);
+              if (limit[j][1] > tile * TILE + m * 16) l[j][1] = fmaf(w1 + w3, v_inv[m], l[j][1]);
+            } else {
+              l[j][0] = fmaf(w0 + w2, v_inv[m], l[j][0]);
+              l[j][1] = fmaf(w1 + w3, v_inv[m], l[j][1]);
+            }
             pf[j][0] = transpose_8x8(Pair16<__half>::pack(w0, w1));         // tokens to columns 2 qt, 2 qt + 1, queries to rows
             pf[j][1] = transpose_8x8(Pair16<__half>::pack(w2, w3));
           }
@@ -538,7 +598,7 @@ __global__ void __launch_bounds__(CacheAttnCfg<HD, NT>::kThreads, 1) cache_atten
           if (r >= n_rows) continue;
           if (whole) {
             const float inv = x == 0.f ? 0.f : kWeightDown / x;
-            uint16_t* dst = p.out + s * p.ld_out + static_cast<long long>(kvh * p.group + head0 + r) * HD + qg * (HD / 8);
+            uint16_t* dst = p.out + at_row_of(r, p.ld_out) + qg * (HD / 8);
 #pragma unroll
             for (int i = 0; i < HD / 16; i += 4) {
               uint32_t y[4];
@@ -603,24 +663,36 @@ __device__ __forceinline__ void load_floats(const float* src, float (&x)[N]) {  
 
 // What the CTAs' and pieces' ends cut, put together: one warp per (sequence, query head), the parts in order.  Rows that one piece held are
 // there already; sequences without tokens get zeros.
-template <int HD, int NT>
+template <int HD, int NT, bool CHUNK = false>
 __global__ void __launch_bounds__(kCacheJoinThreads, 1) cache_join_kernel(const __grid_constant__ CacheAttnParams p) {
   constexpr int ROWS = 8 * NT, N = HD / 32, WARPS = CacheAttnCfg<HD, NT>::kWarps;
   __shared__ int prefix[kCacheMaxSeqs + 1], sums[kCacheJoinThreads / 32];
   // On the whole device this kernel starts beside the one before it, which has let it go behind its own wait: the lengths are final
   if (!p.early_launch) pdl_wait();
-  cache_prefix<CacheAttnCfg<HD, NT>::kTile>(p, prefix, nullptr, sums, false);
+  constexpr int TILE = CacheAttnCfg<HD, NT>::kTile;
+  cache_prefix<TILE, ROWS, CHUNK>(p, prefix, nullptr, nullptr, sums, false);
   const int lane = threadIdx.x & 31, heads = p.c.n_kv * p.group, R = p.c.n_kv * p.row_blocks;
-  const CacheLine line(prefix[p.n_seqs], R, p.n_ctas * WARPS);
+  const CacheLine line(prefix[p.n_seqs], CHUNK ? 1 : R, p.n_ctas * WARPS);
   bool waited = false;
   constexpr int kJoinWarps = kCacheJoinThreads / 32;
-  for (int u = blockIdx.x * kJoinWarps + (threadIdx.x >> 5); u < p.n_seqs * heads; u += gridDim.x * kJoinWarps) {
-    const int s = u / heads, h = u - s * heads, kvh = h / p.group, in_group = h - kvh * p.group;
-    const int row = kvh * p.row_blocks + in_group / ROWS, r = in_group % ROWS;
-    const int before = prefix[s], cost = prefix[s + 1] - before;
+  for (int u = blockIdx.x * kJoinWarps + (threadIdx.x >> 5); u < (CHUNK ? p.n_rows : p.n_seqs) * heads; u += gridDim.x * kJoinWarps) {
+    const int q_row = u / heads, h = u - q_row * heads, kvh = h / p.group;
+    int s = q_row, column = h - kvh * p.group, blocks = p.row_blocks, cost;
+    if constexpr (CHUNK) {
+      s = last_sequence(p.n_seqs, q_row, [&](int i) { return min(max(p.cu[i], 0), p.n_rows); });
+      const int len = min(static_cast<long long>(max(p.seq_lens[s], 0)), static_cast<long long>(p.max_blocks) << p.c.bs_log2);
+      const CacheNew c(p, s, len);
+      if (q_row < c.first || q_row >= c.first + c.given || c.given > p.max_new || static_cast<long long>(c.given) * p.group > p.most_rows) continue;
+      cost = q_row < c.q0 ? 0 : (len + TILE - 1) / TILE + kRowCost;      // 0: it sees nothing
+      column += (q_row - c.q0) * p.group;
+      blocks = (c.n * p.group + ROWS - 1) / ROWS;
+    } else {
+      cost = prefix[s + 1] - prefix[s];
+    }
+    const int row = kvh * blocks + column / ROWS, r = column % ROWS;
     int w0 = 0, w1 = 0;                                            // the row's first and last piece
     if (cost > 0) {
-      const int a = before * R + row * cost;
+      const int a = prefix[s] * (CHUNK ? 1 : R) + row * cost;
       w0 = line.piece_of(a + kRowCost);
       w1 = line.piece_of(a + cost - 1);
       if (w0 == w1) continue;
@@ -676,7 +748,7 @@ __global__ void __launch_bounds__(kCacheJoinThreads, 1) cache_join_kernel(const 
 #pragma unroll
       for (int i = 0; i < N; ++i) acc[i] *= inv;
     }
-    uint16_t* dst = p.out + s * p.ld_out + static_cast<long long>(h) * HD + lane * N;
+    uint16_t* dst = p.out + q_row * p.ld_out + static_cast<long long>(h) * HD + lane * N;
 #pragma unroll
     for (int i = 0; i < N; i += 2)
       *reinterpret_cast<uint32_t*>(dst + i) = p.fp16 ? Pair16<__half>::pack(acc[i], acc[i + 1]) : Pair16<bf16>::pack(acc[i], acc[i + 1]);

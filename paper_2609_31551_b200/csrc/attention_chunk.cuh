@@ -40,6 +40,7 @@ struct ChunkParams {
   const int32_t *table, *cu, *seq_lens;
   long long ld_table;
   int n_seqs, max_blocks, n_rows, max_new;
+  int few_rows;                // sequences of at most so many rows a key/value head belong to another kernel (attention_cache.cuh)
   const uint16_t* q;
   uint16_t* out;
   long long ld_q, ld_out;
@@ -92,7 +93,8 @@ __device__ __forceinline__ int chunk_row_token(const ChunkParams& p, int row) {
 // ------------------------------------------------------------------------------------ the line of units
 struct ChunkSeq {              // a sequence: its visible new tokens, the tokens in front of them, and what its tiles cost a head
   int q0, n, ahead, tiles, units;
-  __device__ __forceinline__ ChunkSeq() : q0(0), n(0), ahead(0), tiles(0), units(0) {}
+  bool mine;                   // this kernel's
+  __device__ __forceinline__ ChunkSeq() : q0(0), n(0), ahead(0), tiles(0), units(0), mine(false) {}
   __device__ __forceinline__ ChunkSeq(const ChunkParams& p, int s, bool report) {
     auto cu = [&](int i) { return min(max(p.cu[i], 0), p.n_rows); };
     const int first = cu(s), given = max(cu(s + 1) - first, 0);
@@ -102,6 +104,8 @@ struct ChunkSeq {              // a sequence: its visible new tokens, the tokens
       if (report) raise_status(p.status, DEV_ERR_CACHE_RANGE);
       len = given > p.max_new ? 0 : static_cast<int>(most);
     }
+    mine = given <= p.max_new && static_cast<long long>(given) * p.group > p.few_rows;
+    if (!mine) len = 0;
     n = min(given, len);
     q0 = first + given - n;
     ahead = len - n;
@@ -1038,9 +1042,8 @@ __global__ void __launch_bounds__(512, 1) chunk_join_kernel(const __grid_constan
   const int lane = threadIdx.x & 31, chunks = p.c.n_kv * p.group * (HD / 8);
   for (int s = blockIdx.x * 16 + (threadIdx.x >> 5); s < p.n_seqs; s += gridDim.x * 16) {
     const ChunkSeq seq(p, s, false);                               // the rows in front of a sequence's visible tokens
-    const int first = min(max(p.cu[s], 0), p.n_rows), given = min(max(p.cu[s + 1], 0), p.n_rows) - first;
-    if (given > p.max_new) continue;
-    for (int r = first; r < seq.q0; ++r)
+    if (!seq.mine) continue;
+    for (int r = min(max(p.cu[s], 0), p.n_rows); r < seq.q0; ++r)
       for (int c = lane; c < chunks; c += 32) *reinterpret_cast<uint4*>(p.out + static_cast<long long>(r) * p.ld_out + c * 8) = make_uint4(0u, 0u, 0u, 0u);
   }
   pdl_wait();

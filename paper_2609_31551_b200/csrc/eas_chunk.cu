@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "attention_cache.cuh"
 #include "attention_chunk.cuh"
 #include "cache_handle.cuh"
 
@@ -31,6 +32,58 @@ static eas_status launch_chunk(const ChunkParams& p, int budget, bool all, cudaS
   return launch_kernel(chunk_join_kernel<HD>, std::min(budget, p.n_ctas), 512, all ? 0 : kOnePerSmSmem, stream, p);
 }
 
+// ------------------------------------------------------------------------------------ few rows
+// Up to so many query rows a key/value head (new tokens times heads of the group) a sequence goes to the kernels of single tokens: of 402 MB of cache (48 sequences of
+// 4096 tokens, 8 key/value heads of 128) they take 76 us for 8 rows, 96 for 16 and 180 for 32, the tiles of 128 rows 183 for 16 and 195 for 36.
+constexpr int kFewRows = 32;
+
+static int few_columns(int rows) { return rows <= 8 ? 8 : 16; }
+static size_t few_workspace(const eas_cache* c, int rows, size_t* o_off) {
+  const int r = few_columns(rows), warps = r == 8 ? CacheAttnCfg<128, 1>::kWarps : CacheAttnCfg<128, 2>::kWarps;
+  const size_t n = static_cast<size_t>(2) * c->sm_count * warps * r;
+  *o_off = up256(n * 8);
+  return *o_off + up256(n * c->d.head_dim * 4);
+}
+template <int HD, int NT>
+static eas_status launch_few(const CacheAttnParams& p, int budget, bool all, cudaStream_t stream) {
+  using L = CacheAttnCfg<HD, NT>;
+  static OncePerDevice once;
+  if (once.first()) {
+    CUDA_TRY(cudaFuncSetAttribute(cache_attention_kernel<HD, NT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes));
+    CUDA_TRY(cudaFuncSetAttribute(cache_join_kernel<HD, NT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kOnePerSmSmem));
+    once.settled();
+  }
+  EAS_TRY(launch_kernel(cache_attention_kernel<HD, NT, true>, std::min(budget, p.n_ctas), L::kThreads, L::kBytes, stream, p));
+  const int64_t heads = static_cast<int64_t>(p.n_rows) * p.c.n_kv * p.group;
+  constexpr int kJoinWarps = kCacheJoinThreads / 32;
+  return launch_kernel(cache_join_kernel<HD, NT, true>, static_cast<int>(std::min<int64_t>(budget, (heads + kJoinWarps - 1) / kJoinWarps)), kCacheJoinThreads,
+                       all ? 0 : kOnePerSmSmem, stream, p);
+}
+
+// Which kernels a call needs: those for few rows alone, where no sequence has more; both, where most sequences have less than half of the most (a
+// prompt's chunk beside single tokens); else the tiles of 128 rows for all.
+struct ChunkPlan {
+  int few_rows = 0;            // most rows a key/value head of the sequences that the kernels for few rows take
+  bool tiles = false;
+};
+static ChunkPlan chunk_plan(int32_t n_seqs, int32_t n_rows, int32_t max_new, int group) {
+  ChunkPlan plan;
+  const int64_t most = static_cast<int64_t>(max_new) * group;
+  plan.tiles = most > kFewRows;
+  if (!plan.tiles) plan.few_rows = static_cast<int>(std::max<int64_t>(most, 1));
+  else if (group <= kFewRows && static_cast<int64_t>(n_rows) * 2 < static_cast<int64_t>(n_seqs) * max_new) plan.few_rows = kFewRows;
+  return plan;
+}
+
+// the kernels of a call run one behind the other: they share the scratch
+static size_t chunk_workspace_bytes(const eas_cache* c, const ChunkPlan& plan, int32_t n_rows, int32_t max_new, int32_t n_heads) {
+  int ws_rows = 0;
+  size_t a = 0, b = 0, bytes = 256;
+  if (plan.few_rows > 0) bytes = std::max(bytes, few_workspace(c, plan.few_rows, &a));
+  if (plan.tiles) bytes = std::max(bytes, chunk_workspace(c, std::min(max_new, n_rows), n_heads, &ws_rows, &a, &b));
+  return bytes;
+}
+
 static eas_status chunk_attention(const eas_cache* c, const eas_cache_seqs* s, const void* q, int64_t ld_q, void* out, int64_t ld_out, int32_t n_rows,
                                   int32_t max_new, int32_t n_heads, int32_t dtype, float scale, void* workspace, size_t workspace_bytes, int32_t sm_budget,
                                   void* stream, uint32_t* status_dev) {
@@ -41,32 +94,68 @@ static eas_status chunk_attention(const eas_cache* c, const eas_cache_seqs* s, c
   if (n_heads <= 0 || n_heads % G != 0) return fail(EAS_ERR_INVALID_ARG, "%d query heads for %d key/value heads", n_heads, G);
   if (n_rows < 0 || max_new < 0) return fail(EAS_ERR_INVALID_ARG, "n_rows %d, max_new %d", n_rows, max_new);
   if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(EAS_ERR_INVALID_ARG, "scale must be positive and finite");
-  if (n_heads / G > 128) return fail(EAS_ERR_UNSUPPORTED, "%d query heads per key/value head (at most 128)", n_heads / G);
+  const int group = n_heads / G;
+  if (group > 128) return fail(EAS_ERR_UNSUPPORTED, "%d query heads per key/value head (at most 128)", group);
   if (s->n_seqs == 0 || n_rows == 0) return EAS_OK;
   if (q == nullptr || out == nullptr || workspace == nullptr) return fail(EAS_ERR_INVALID_ARG, "a required pointer is null");
   if (!aligned16(q) || !aligned16(out)) return fail(EAS_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
   const int64_t w = static_cast<int64_t>(n_heads) * hd;
   if (ld_q < w || ld_out < w || ld_q % 8 != 0 || ld_out % 8 != 0)
     return fail(EAS_ERR_INVALID_ARG, "token distances must be multiples of 8 that hold a token's heads");
-  ChunkParams p{};
-  size_t ml_off = 0, cut_off = 0;
-  const size_t need = chunk_workspace(c, std::min(max_new, n_rows), n_heads, &p.ws_rows, &ml_off, &cut_off);
+  const ChunkPlan plan = chunk_plan(s->n_seqs, n_rows, max_new, group);
+  const size_t need = chunk_workspace_bytes(c, plan, n_rows, max_new, n_heads);
   if (workspace_bytes < need) return fail(EAS_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, need);
   if ((reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return fail(EAS_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
-  if (static_cast<int64_t>(s->max_blocks) * c->d.block_size > (1LL << 30)) return fail(EAS_ERR_UNSUPPORTED, "max_blocks %d: more than 2^30 places a sequence", s->max_blocks);
-  p.c = view_of(c);
-  p.ld_table = s->ld_table; p.max_blocks = s->max_blocks; p.n_rows = n_rows; p.max_new = max_new;
-  p.q = static_cast<const uint16_t*>(q); p.out = static_cast<uint16_t*>(out);
-  p.ld_q = ld_q; p.ld_out = ld_out; p.fp16 = dtype == EAS_DTYPE_FP16; p.group = n_heads / G; p.tile_tokens = 128 / p.group;
-  p.by_group = p.group == 1 ? 0u : static_cast<uint32_t>(((1ull << 32) + p.group - 1) / p.group);
-  p.n_ctas = c->sm_count;
-  p.scale_log2 = static_cast<float>(scale * kLog2e);
-  p.o_ws = static_cast<float4*>(workspace);
-  p.ml_ws = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + ml_off);
-  p.cut_ws = reinterpret_cast<ChunkItem*>(static_cast<uint8_t*>(workspace) + cut_off);
-  p.status = status_dev;
+  const int64_t places = static_cast<int64_t>(s->max_blocks) * c->d.block_size;
+  if (places > (1LL << 30)) return fail(EAS_ERR_UNSUPPORTED, "max_blocks %d: more than 2^30 places a sequence", s->max_blocks);
+  if (static_cast<int64_t>(n_rows) * n_heads > 0x7fffffffLL) return fail(EAS_ERR_UNSUPPORTED, "too many rows for one call");
   const bool all = budget == c->sm_count;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  uint8_t* const ws = static_cast<uint8_t*>(workspace);
+  if (plan.few_rows > 0) {
+    const int columns = few_columns(plan.few_rows);
+    CacheAttnParams p{};
+    p.map_k = c->map_k; p.map_v = c->map_v;
+    p.c = view_of(c);
+    p.group = group;
+    p.row_blocks = (plan.few_rows + columns - 1) / columns;
+    const int64_t tiles = (places + 31) / 32 + kRowCost;          // (no variant's tile is smaller)
+    if (tiles * G * p.row_blocks > 0x7fffffffLL / std::min(s->n_seqs, kCacheMaxSeqs))
+      return fail(EAS_ERR_UNSUPPORTED, "max_blocks %d is too large for %d sequences", s->max_blocks, s->n_seqs);
+    p.n_rows = n_rows; p.max_new = max_new; p.most_rows = plan.few_rows;
+    p.ld_table = s->ld_table; p.max_blocks = s->max_blocks;
+    p.q = static_cast<const uint16_t*>(q); p.out = static_cast<uint16_t*>(out);
+    p.ld_q = ld_q; p.ld_out = ld_out; p.fp16 = dtype == EAS_DTYPE_FP16;
+    p.n_ctas = c->sm_count;
+    p.scale_log2 = static_cast<float>(scale * kLog2e);
+    size_t o_off = 0;
+    few_workspace(c, plan.few_rows, &o_off);
+    p.ml_ws = reinterpret_cast<float*>(ws); p.o_ws = reinterpret_cast<float*>(ws + o_off);
+    p.status = status_dev;
+    for (int first = 0; first < s->n_seqs; first += kCacheMaxSeqs) {
+      p.n_seqs = std::min(kCacheMaxSeqs, s->n_seqs - first);
+      p.table = s->block_table + first * s->ld_table;
+      p.cu = s->cu_seqlens + first;
+      p.seq_lens = s->seq_lens + first;
+      EAS_TRY(hd == 64 ? (columns == 8 ? launch_few<64, 1>(p, budget, all, st) : launch_few<64, 2>(p, budget, all, st))
+                       : (columns == 8 ? launch_few<128, 1>(p, budget, all, st) : launch_few<128, 2>(p, budget, all, st)));
+    }
+  }
+  if (!plan.tiles) return EAS_OK;
+  ChunkParams p{};
+  size_t ml_off = 0, cut_off = 0;
+  chunk_workspace(c, std::min(max_new, n_rows), n_heads, &p.ws_rows, &ml_off, &cut_off);
+  p.c = view_of(c);
+  p.ld_table = s->ld_table; p.max_blocks = s->max_blocks; p.n_rows = n_rows; p.max_new = max_new; p.few_rows = plan.few_rows;
+  p.q = static_cast<const uint16_t*>(q); p.out = static_cast<uint16_t*>(out);
+  p.ld_q = ld_q; p.ld_out = ld_out; p.fp16 = dtype == EAS_DTYPE_FP16; p.group = group; p.tile_tokens = 128 / group;
+  p.by_group = group == 1 ? 0u : static_cast<uint32_t>(((1ull << 32) + group - 1) / group);
+  p.n_ctas = c->sm_count;
+  p.scale_log2 = static_cast<float>(scale * kLog2e);
+  p.o_ws = reinterpret_cast<float4*>(ws);
+  p.ml_ws = reinterpret_cast<float2*>(ws + ml_off);
+  p.cut_ws = reinterpret_cast<ChunkItem*>(ws + cut_off);
+  p.status = status_dev;
   for (int first = 0; first < s->n_seqs; first += kChunkMaxSeqs) {
     p.n_seqs = std::min(kChunkMaxSeqs, s->n_seqs - first);
     p.table = s->block_table + first * s->ld_table;
@@ -86,9 +175,7 @@ extern "C" size_t eas_cache_chunk_workspace_bytes(const eas_cache* cache, int32_
     fail(EAS_ERR_UNSUPPORTED, "%d query heads per key/value head (at most 128)", n_heads / cache->d.n_kv_heads);
     return 0;
   }
-  int ws_rows = 0;
-  size_t ml_off = 0, cut_off = 0;
-  return chunk_workspace(cache, std::min(max_new, n_rows), n_heads, &ws_rows, &ml_off, &cut_off);
+  return chunk_workspace_bytes(cache, chunk_plan(n_seqs, n_rows, max_new, n_heads / cache->d.n_kv_heads), n_rows, max_new, n_heads);
 }
 
 extern "C" eas_status eas_cache_chunk_attention(const eas_cache* cache, const eas_cache_seqs* seqs, const void* q, int64_t ld_q, void* out, int64_t ld_out,

@@ -28,6 +28,20 @@ struct CacheSeqs {
 
 __device__ __forceinline__ void raise_status(uint32_t* status, uint32_t code) { atomicCAS(status, DEV_OK, code); }
 
+// The last of the sequences 0 .. n - 1 whose key, which grows with the sequence, is at or below x (0 if none is): a whole warp looks at 32 of them at a time.
+template <typename Key>
+__device__ __forceinline__ int last_sequence(int n, int x, Key key) {
+  int lo = 0, hi = n - 1;
+  const int lane = threadIdx.x & 31;
+  while (lo < hi) {
+    const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step;
+    const int passed = __popc(__ballot_sync(0xffffffffu, at <= hi && key(at) <= x));
+    lo += passed * step;
+    hi = min(hi, lo + step - 1);
+  }
+  return lo;
+}
+
 template <typename T> struct Pair16;
 template <> struct Pair16<bf16> {
   static __device__ __forceinline__ float lo(uint32_t w) { return bf16_lo(w); }

@@ -176,20 +176,6 @@ struct AppendParams {
 
 constexpr int kAppendThreads = 256;
 
-// The last of the sequences 0 .. n - 1 whose key, which grows with the sequence, is at or below x (0 if none is): a whole warp looks at 32 of them at a time.
-template <typename Key>
-__device__ __forceinline__ int last_sequence(int n, int x, Key key) {
-  int lo = 0, hi = n - 1;
-  const int lane = threadIdx.x & 31;
-  while (lo < hi) {
-    const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step;
-    const int passed = __popc(__ballot_sync(0xffffffffu, at <= hi && key(at) <= x));
-    lo += passed * step;
-    hi = min(hi, lo + step - 1);
-  }
-  return lo;
-}
-
 // Eight fp32 values to eight numbers, as quantise8 does it
 __device__ __forceinline__ uint2 quantise8_fp32(const float* y, float s, float inv) {
   uint32_t q[8];
