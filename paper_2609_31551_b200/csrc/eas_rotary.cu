@@ -126,12 +126,14 @@ static eas_status launch_append(AppendParams& p, int budget, bool all, cudaStrea
     CUDA_TRY(cudaFuncSetAttribute(cache_append_kernel<HD, GT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kOnePerSmSmem));
     once.settled();
   }
-  // Key/value heads of an item: all of a block's, whose cosines then are worked out once, unless that leaves CTAs without work; at the least one pass of a CTA.
-  constexpr int kLeast = kAppendThreads / GT > 1 ? kAppendThreads / GT / 2 : 1;
+  // Key/value heads of an item: all of a block's, whose cosines then are worked out once, unless that leaves CTAs without work; at the least one pass of a CTA (a few
+  // rows a sequence: a warp for a head's keys or values).
+  const bool few = static_cast<int64_t>(p.r.n_rows) <= static_cast<int64_t>(p.s.n_seqs) * AppendUnits<HD, 32, T>::STEPS * AppendUnits<HD, 32, T>::ROWS;
+  const int least = kAppendThreads / (few ? 32 : GT) > 1 ? kAppendThreads / (few ? 32 : GT) / 2 : 1;
   const int64_t ctas = 2LL * g_device_sms;
   const int64_t blocks = std::max<int64_t>(p.pairs - p.s.n_seqs, 1);      // (about half of the sequences' spare numbers have a block)
   p.part_heads = p.c.n_kv;
-  while (p.part_heads > kLeast && blocks * ((p.c.n_kv + p.part_heads - 1) / p.part_heads) < 3 * ctas) p.part_heads = (p.part_heads + 1) / 2;
+  while (p.part_heads > least && blocks * ((p.c.n_kv + p.part_heads - 1) / p.part_heads) < 3 * ctas) p.part_heads = (p.part_heads + 1) / 2;
   p.head_parts = (p.c.n_kv + p.part_heads - 1) / p.part_heads;
   if (static_cast<int64_t>(p.pairs) * p.head_parts > 0x3fffffff) return fail(EAS_ERR_UNSUPPORTED, "too many rows for one call");
   split_heads(p.r.n_rows, std::max(p.r.n_heads, 1), 4 * 32 / (HD / 16), ctas * (kAppendThreads / 32), &p.q_parts, &p.q_part_heads);
@@ -174,6 +176,7 @@ static eas_status cache_append(const eas_cache* c, const eas_cache_seqs* s, cons
   const int64_t pairs = (in->n_rows >> c->bs_log2) + 2LL * s->n_seqs;
   if (pairs > 0x3fffffff) return fail(EAS_ERR_UNSUPPORTED, "too many rows for one call");
   p.pairs = static_cast<int>(pairs);
+  while ((1 << p.pairs_log2) < p.t.pairs) ++p.pairs_log2;
   p.status = status_dev;
   const bool all = budget == c->sm_count, h = in->dtype == EAS_DTYPE_FP16;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);

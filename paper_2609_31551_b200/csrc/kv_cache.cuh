@@ -177,19 +177,26 @@ __device__ __forceinline__ float cache_block_scale(float largest, float old, int
     if (!(s <= old) && old == old) {                             // the scale grows (or stops being a number)
       const float ratio = __fdiv_rn(old, s);
       constexpr int kLanes = HD / 16;
-      for (int t = tid / kLanes; t < lo; t += GT / kLanes) {
-        uint4* w = reinterpret_cast<uint4*>(dst + t * HD + (tid % kLanes) * 16);
-        const uint4 y = *w;
-        uint32_t yw[4] = {y.x, y.y, y.z, y.w};
+      constexpr int kTokens = GT / kLanes, kFlight = 4;          // tokens of all threads, of each thread in flight
+      for (int t0 = tid / kLanes; t0 < lo; t0 += kTokens * kFlight) {
+        uint4 y[kFlight];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t z = 0;
+        for (int i = 0; i < kFlight; ++i)
+          if (t0 + i * kTokens < lo) y[i] = *reinterpret_cast<const uint4*>(dst + (t0 + i * kTokens) * HD + (tid % kLanes) * 16);
 #pragma unroll
-          for (int b = 0; b < 4; ++b)
-            z |= (requantise(static_cast<int8_t>(yw[i] >> (8 * b)), old, s, ratio) & 0xFFu) << (8 * b);
-          yw[i] = z;
+        for (int i = 0; i < kFlight; ++i) {
+          if (t0 + i * kTokens >= lo) break;
+          uint32_t yw[4] = {y[i].x, y[i].y, y[i].z, y[i].w};
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            uint32_t z = 0;
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+              z |= (requantise(static_cast<int8_t>(yw[w] >> (8 * b)), old, s, ratio) & 0xFFu) << (8 * b);
+            yw[w] = z;
+          }
+          *reinterpret_cast<uint4*>(dst + (t0 + i * kTokens) * HD + (tid % kLanes) * 16) = make_uint4(yw[0], yw[1], yw[2], yw[3]);
         }
-        *w = make_uint4(yw[0], yw[1], yw[2], yw[3]);
       }
     } else {
       s = old;

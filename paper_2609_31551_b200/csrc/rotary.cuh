@@ -20,10 +20,26 @@ struct RotaryTable {                      // (kernel parameter)
   float scale;
 };
 
+// A thread's pair: which it works out cosines and sines of, for any number of rows.  (Taken from the parameters once: threads that read different ones go one after the
+// other, which for every row was two thirds of the time.)
+struct RotaryPair {
+  uint32_t f_lo, f_hi;
+  int axis;
+  int at;                                 // place in a row's table (below); -1: none
+  __device__ __forceinline__ RotaryPair(const RotaryTable& t, int pair) {
+    const int i = min(pair, t.pairs - 1);
+    f_lo = t.f_lo[i];
+    f_hi = t.f_hi[i];
+    axis = t.axis[i];
+    at = pair < t.pairs ? rotary_place(i, t.pairs) : -1;
+  }
+  // The table of a row: 8 pairs an item (16 dimensions), as four float4; those of all items side by side, so that threads of neighbouring items read side by side
+  static __device__ __forceinline__ int rotary_place(int pair, int pairs) { return ((pair >> 1) & 3) * (pairs >> 2) + (pair >> 3) * 2 + (pair & 1); }
+};
 // cosine and sine of a pair's angle at a position, times the scale (the sine's is negative where the rotation is taken back)
-__device__ __forceinline__ float2 rotary_turn(uint32_t f_lo, uint32_t f_hi, int position, float scale, float sin_scale) {
+__device__ __forceinline__ float2 rotary_turn(const RotaryPair& f, int position, float scale, float sin_scale) {
   const uint32_t p = static_cast<uint32_t>(position);
-  const uint32_t turn = p * f_hi + __umulhi(p, f_lo) - (position < 0 ? f_lo : 0u);      // bits 32 .. 63 of position * F
+  const uint32_t turn = p * f.f_hi + __umulhi(p, f.f_lo) - (position < 0 ? f.f_lo : 0u);      // bits 32 .. 63 of position * F
   float s, c;
   sincospif(static_cast<float>(static_cast<int32_t>(turn)) * 4.656612873077393e-10f, &s, &c);     // 2^-31
   return make_float2(c * scale, s * sin_scale);
@@ -45,13 +61,13 @@ struct RotaryRows {
 __device__ __forceinline__ int2 rotary_at(int c, int pairs, int neighbours) {
   return !neighbours && 8 * c < pairs ? make_int2(8 * c, pairs + 8 * c) : make_int2(16 * c, 16 * c + 8);
 }
-// the 16 values of a rotated item, turned by its 8 pairs' cosines and sines (8 float2 from shared memory)
+// the 16 values of a rotated item, turned by its 8 pairs' cosines and sines (cs: the item's first two in the row's table of `items` items)
 template <typename T>
-__device__ __forceinline__ void rotary_turn_16(const uint4& lo, const uint4& hi, const float4* cs, int neighbours, float (&y)[16]) {
+__device__ __forceinline__ void rotary_turn_16(const uint4& lo, const uint4& hi, const float4* cs, int items, int neighbours, float (&y)[16]) {
   const uint32_t a[4] = {lo.x, lo.y, lo.z, lo.w}, b[4] = {hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {           // two pairs
-    const float4 t = cs[i];
+    const float4 t = cs[i * items];
     if (neighbours) {
       const uint32_t w0 = i < 2 ? a[2 * i] : b[2 * i - 4], w1 = i < 2 ? a[2 * i + 1] : b[2 * i - 3];
       const float x0 = Pair16<T>::lo(w0), x1 = Pair16<T>::hi(w0), x2 = Pair16<T>::lo(w1), x3 = Pair16<T>::hi(w1);
@@ -71,7 +87,8 @@ __device__ __forceinline__ void rotary_turn_16(const uint4& lo, const uint4& hi,
 
 // One token's heads [head0, head1) of queries and keys side by side (keys behind the queries), by a warp.  cs: the warp's 64 cosines and sines.
 template <int HD, typename T>
-__device__ __forceinline__ void rotary_row(const RotaryTable& t, const RotaryRows& r, int row, int head0, int head1, const int (&position)[2], float2* cs) {
+__device__ __forceinline__ void rotary_row(const RotaryTable& t, const RotaryRows& r, const RotaryPair (&pair)[2], int row, int head0, int head1, const int (&position)[2],
+                                           float2* cs) {
   constexpr int ITEMS = HD / 16, LANES = 32 / ITEMS, BATCH = 4;          // items a head, heads a warp takes at once, loads in flight
   const int lane = threadIdx.x & 31, item = lane % ITEMS, sub = lane / ITEMS;
   const bool turned = 8 * item < t.pairs;
@@ -99,8 +116,7 @@ __device__ __forceinline__ void rotary_row(const RotaryTable& t, const RotaryRow
       __syncwarp();
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int pair = lane + 32 * i;
-        if (pair < t.pairs) cs[pair] = rotary_turn(t.f_lo[pair], t.f_hi[pair], position[i], t.scale, r.inverse ? -t.scale : t.scale);
+        if (pair[i].at >= 0) cs[pair[i].at] = rotary_turn(pair[i], position[i], t.scale, r.inverse ? -t.scale : t.scale);
       }
       __syncwarp();
       first = false;
@@ -112,7 +128,7 @@ __device__ __forceinline__ void rotary_row(const RotaryTable& t, const RotaryRow
       T* dst = to(h);
       if (turned) {
         float y[16];
-        rotary_turn_16<T>(lo[i], hi[i], reinterpret_cast<const float4*>(cs) + item * 4, t.neighbours, y);
+        rotary_turn_16<T>(lo[i], hi[i], reinterpret_cast<const float4*>(cs) + item, t.pairs >> 3, t.neighbours, y);
         lo[i] = make_uint4(Pair16<T>::pack(y[0], y[1]), Pair16<T>::pack(y[2], y[3]), Pair16<T>::pack(y[4], y[5]), Pair16<T>::pack(y[6], y[7]));
         hi[i] = make_uint4(Pair16<T>::pack(y[8], y[9]), Pair16<T>::pack(y[10], y[11]), Pair16<T>::pack(y[12], y[13]), Pair16<T>::pack(y[14], y[15]));
       }
@@ -134,16 +150,17 @@ constexpr int kRotaryThreads = 512;
 
 template <int HD, typename T>
 __global__ void __launch_bounds__(kRotaryThreads, 1) rotary_kernel(const __grid_constant__ RotaryParams p) {
-  __shared__ float2 table[kRotaryThreads / 32][kRotaryMaxPairs];
+  __shared__ __align__(16) float2 table[kRotaryThreads / 32][kRotaryMaxPairs];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const RotaryPair pair[2] = {{p.t, lane}, {p.t, lane + 32}};
   if (p.early_launch) pdl_launch_dependents();
   pdl_wait();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t units = static_cast<uint32_t>(p.r.n_rows) * p.parts, step = gridDim.x * (blockDim.x >> 5);      // (below 2^31)
   const int heads = p.r.n_heads + p.r.n_kv;
   auto position_of = [&](uint32_t u, int (&position)[2]) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-      position[i] = u < units && lane + 32 * i < p.t.pairs ? p.r.positions[p.t.axis[lane + 32 * i] * p.r.ld_positions + u / p.parts] : 0;
+      position[i] = u < units && pair[i].at >= 0 ? p.r.positions[pair[i].axis * p.r.ld_positions + u / p.parts] : 0;
   };
   int position[2];
   uint32_t u = blockIdx.x * (blockDim.x >> 5) + warp;
@@ -152,7 +169,7 @@ __global__ void __launch_bounds__(kRotaryThreads, 1) rotary_kernel(const __grid_
     int next[2];
     position_of(u + step, next);
     const int row = static_cast<int>(u / p.parts), head0 = static_cast<int>(u - row * p.parts) * p.part_heads;
-    rotary_row<HD, T>(p.t, p.r, row, head0, min(head0 + p.part_heads, heads), position, table[warp]);
+    rotary_row<HD, T>(p.t, p.r, pair, row, head0, min(head0 + p.part_heads, heads), position, table[warp]);
     position[0] = next[0];
     position[1] = next[1];
   }
@@ -167,6 +184,7 @@ struct AppendParams {
   const void* v;
   long long ld_v;
   int pairs;                              // numbers of (sequence, block) pairs (see cache_run)
+  int pairs_log2;                         // of the next power of two from the rotated pairs on
   int head_parts, part_heads;             // key/value heads of a pair in pieces
   uint32_t q_parts;                       // query heads of a token in pieces
   int q_part_heads;
@@ -194,70 +212,35 @@ __device__ __forceinline__ uint2 quantise8_fp32(const float* y, float s, float i
                     __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410));
 }
 
-// An item is the run of one sequence's new rows that lies in one block, and some of its key/value heads: the cosines and sines of the run's rows go to
-// shared memory once, then GT threads take a head's keys or values, as in cache_store_kernel (a thread has 4 rows of 16 dimensions, rotated in
-// fp32 and rounded once, to the number).  Behind those the queries: a warp takes a token's heads, or some of them.
+// GT threads take the keys or the values of one head of a run: 4 rows of 16 dimensions a thread, rotated in fp32 and rounded once, to the number; then the block's
+// scale and numbers as in cache_store_kernel.  `turns`: cosines and sines of the run's rows.
 template <int HD, int GT, typename T>
-__global__ void __launch_bounds__(kAppendThreads, 2) cache_append_kernel(const __grid_constant__ AppendParams p) {
-  extern __shared__ __align__(16) float2 append_turns[];
-  __shared__ uint32_t group_max[32];
-  if (p.early_launch) pdl_launch_dependents();
-  pdl_wait();
-  constexpr int ITEMS = HD / 16, ROWS = GT / ITEMS, STEPS = 4, GROUPS = kAppendThreads / GT;
-  const int tid = threadIdx.x % GT, group = threadIdx.x / GT, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int item = tid % ITEMS, sub = tid / ITEMS;
-  auto cu = [&](int i) { return min(max(p.s.cu[i], 0), p.r.n_rows); };
-  const int pair_items = p.pairs * p.head_parts;
-  const uint32_t q_units = static_cast<uint32_t>(p.r.n_heads > 0 ? p.r.n_rows : 0) * p.q_parts;
-  const uint32_t items = pair_items + (q_units + kAppendThreads / 32 - 1) / (kAppendThreads / 32);
-  for (uint32_t it = blockIdx.x; it < items; it += gridDim.x) {
-    if (it >= static_cast<uint32_t>(pair_items)) {
-      const uint32_t u = (it - pair_items) * (kAppendThreads / 32) + warp;
-      __syncthreads();                                             // (the table in shared memory is no longer read)
-      if (u >= q_units) continue;
-      const int row = static_cast<int>(u / p.q_parts), head0 = static_cast<int>(u - row * p.q_parts) * p.q_part_heads;
-      if (row < cu(0) || row >= cu(p.s.n_seqs)) continue;
-      int position[2] = {0, 0};
-      if (p.r.positions == nullptr) {
-        const int s = last_sequence(p.s.n_seqs, row, cu);
-        position[0] = position[1] = p.s.start[s] + (row - cu(s));
-      } else {
+struct AppendUnits {
+  static constexpr int ITEMS = HD / 16, ROWS = GT / ITEMS, STEPS = 4, GROUPS = kAppendThreads / GT;
+  const AppendParams& p;
+  const CacheRun& r;
+  const int part, n, units, tid, group, item, sub;
+  uint4 x[2 * STEPS];
+  __device__ __forceinline__ AppendUnits(const AppendParams& params, const CacheRun& run, int head_part)
+      : p(params), r(run), part(head_part), n(run.hi - run.lo), units(2 * min(params.part_heads, params.c.n_kv - head_part * params.part_heads)),
+        tid(threadIdx.x % GT), group(threadIdx.x / GT), item(tid % ITEMS), sub(tid / ITEMS) {}
+  __device__ __forceinline__ void fetch(int u) {                   // the rows of unit u: keys (even) or values (odd) of a head
+    const bool values = u & 1;
+    const int head = part * p.part_heads + (u >> 1);
+    const long long ld = values ? p.ld_v : p.r.ld_k;
+    const T* src = static_cast<const T*>(values ? p.v : p.r.k) + static_cast<long long>(r.row + sub) * ld + head * HD;
+    const int2 at = values ? make_int2(16 * item, 16 * item + 8) : rotary_at(item, p.t.pairs, p.t.neighbours);
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-          if (lane + 32 * i < p.t.pairs) position[i] = p.r.positions[p.t.axis[lane + 32 * i] * p.r.ld_positions + row];
+    for (int i = 0; i < STEPS; ++i) {
+      x[2 * i] = x[2 * i + 1] = make_uint4(0u, 0u, 0u, 0u);
+      if (u < units && sub + i * ROWS < n) {
+        x[2 * i] = *reinterpret_cast<const uint4*>(src + i * ROWS * ld + at.x);
+        x[2 * i + 1] = *reinterpret_cast<const uint4*>(src + i * ROWS * ld + at.y);
       }
-      rotary_row<HD, T>(p.t, p.r, row, head0, min(head0 + p.q_part_heads, p.r.n_heads), position, append_turns + warp * kRotaryMaxPairs);
-      continue;
     }
-    const int pair = static_cast<int>(it) / p.head_parts, part = static_cast<int>(it) - pair * p.head_parts;
-    const CacheRun r = cache_run_of(p.c, p.s, last_sequence(p.s.n_seqs, pair, [&](int i) { return (cu(i) >> p.c.bs_log2) + 2 * i; }), p.r.n_rows, pair, p.status,
-                                    threadIdx.x == 0 && part == 0);
-    if (r.block < 0) continue;
-    const int n = r.hi - r.lo, units = 2 * min(p.part_heads, p.c.n_kv - part * p.part_heads);
-    uint4 x[2 * STEPS];
-    auto fetch = [&](int u) {                                      // the rows of unit u: keys (even) or values (odd) of a head
-      const bool values = u & 1;
-      const int head = part * p.part_heads + (u >> 1);
-      const long long ld = values ? p.ld_v : p.r.ld_k;
-      const T* src = static_cast<const T*>(values ? p.v : p.r.k) + static_cast<long long>(r.row + sub) * ld + head * HD;
-      const int2 at = values ? make_int2(16 * item, 16 * item + 8) : rotary_at(item, p.t.pairs, p.t.neighbours);
-#pragma unroll
-      for (int i = 0; i < STEPS; ++i) {
-        x[2 * i] = x[2 * i + 1] = make_uint4(0u, 0u, 0u, 0u);
-        if (u < units && sub + i * ROWS < n) {
-          x[2 * i] = *reinterpret_cast<const uint4*>(src + i * ROWS * ld + at.x);
-          x[2 * i + 1] = *reinterpret_cast<const uint4*>(src + i * ROWS * ld + at.y);
-        }
-      }
-    };
-    fetch(group);
-    __syncthreads();                                               // (the last item's table is no longer read)
-    for (int e = threadIdx.x; e < n * p.t.pairs; e += kAppendThreads) {
-      const int j = e / p.t.pairs, i = e - j * p.t.pairs;
-      const int position = p.r.positions == nullptr ? r.place + j : p.r.positions[p.t.axis[i] * p.r.ld_positions + r.row + j];
-      append_turns[e] = rotary_turn(p.t.f_lo[i], p.t.f_hi[i], position, p.t.scale, p.t.scale);
-    }
-    __syncthreads();
+  }
+  __device__ __forceinline__ void all(const float2* turns, uint32_t* group_max) {      // (fetch(group) came before)
+    const int lane = threadIdx.x & 31;
 #pragma unroll 1
     for (int u = group; u < units; u += GROUPS) {
       const bool values = u & 1, turned = !values && 8 * item < p.t.pairs;
@@ -270,7 +253,7 @@ __global__ void __launch_bounds__(kAppendThreads, 2) cache_append_kernel(const _
 #pragma unroll
       for (int i = 0; i < STEPS; ++i) {
         if (turned && sub + i * ROWS < n) {
-          rotary_turn_16<T>(x[2 * i], x[2 * i + 1], reinterpret_cast<const float4*>(append_turns + (sub + i * ROWS) * p.t.pairs) + item * 4, p.t.neighbours, y[i]);
+          rotary_turn_16<T>(x[2 * i], x[2 * i + 1], reinterpret_cast<const float4*>(turns + (sub + i * ROWS) * p.t.pairs) + item, p.t.pairs >> 3, p.t.neighbours, y[i]);
         } else {
           const uint32_t w[8] = {x[2 * i].x, x[2 * i].y, x[2 * i].z, x[2 * i].w, x[2 * i + 1].x, x[2 * i + 1].y, x[2 * i + 1].z, x[2 * i + 1].w};
 #pragma unroll
@@ -285,7 +268,7 @@ __global__ void __launch_bounds__(kAppendThreads, 2) cache_append_kernel(const _
       fetch(u + GROUPS);
       m = __reduce_max_sync(0xffffffffu, m);
       if constexpr (GT > 32) {
-        if (lane == 0) group_max[warp] = m;
+        if (lane == 0) group_max[threadIdx.x >> 5] = m;
         asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(GT) : "memory");
         m = group_max[(group * GT >> 5) + (lane & (GT / 32 - 1))];
         m = __reduce_max_sync(0xffffffffu, m);
@@ -305,6 +288,70 @@ __global__ void __launch_bounds__(kAppendThreads, 2) cache_append_kernel(const _
         }
       }
       if (tid == 0) *scale = s;
+    }
+  }
+};
+
+// An item is the run of one sequence's new rows that lies in one block, and some of its key/value heads: the cosines and sines of the run's rows go to
+// shared memory once for all of them.  A run of a few rows (a decoding step, a draft) has a warp for a head's keys or values, a longer one GT threads, one for 64
+// values of a full block.  Behind those items the queries: a warp takes a token's heads, or some of them.
+template <int HD, int GT, typename T>
+__global__ void __launch_bounds__(kAppendThreads, 2) cache_append_kernel(const __grid_constant__ AppendParams p) {
+  extern __shared__ __align__(16) float2 append_turns[];
+  __shared__ uint32_t group_max[32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const RotaryPair q_pair[2] = {{p.t, lane}, {p.t, lane + 32}};
+  const int pairs_log2 = p.pairs_log2, my_row = threadIdx.x >> pairs_log2;
+  const RotaryPair k_pair(p.t, threadIdx.x & ((1 << pairs_log2) - 1));
+  if (p.early_launch) pdl_launch_dependents();
+  pdl_wait();
+  auto cu = [&](int i) { return min(max(p.s.cu[i], 0), p.r.n_rows); };
+  const int pair_items = p.pairs * p.head_parts;
+  const uint32_t q_units = static_cast<uint32_t>(p.r.n_heads > 0 ? p.r.n_rows : 0) * p.q_parts;
+  const uint32_t items = pair_items + (q_units + kAppendThreads / 32 - 1) / (kAppendThreads / 32);
+  for (uint32_t it = blockIdx.x; it < items; it += gridDim.x) {
+    if (it >= static_cast<uint32_t>(pair_items)) {
+      const uint32_t u = (it - pair_items) * (kAppendThreads / 32) + warp;
+      __syncthreads();                                             // (the table in shared memory is no longer read)
+      if (u >= q_units) continue;
+      const int row = static_cast<int>(u / p.q_parts), head0 = static_cast<int>(u - row * p.q_parts) * p.q_part_heads;
+      if (row < cu(0) || row >= cu(p.s.n_seqs)) continue;
+      int position[2] = {0, 0};
+      if (p.r.positions == nullptr) {
+        const int s = last_sequence(p.s.n_seqs, row, cu);
+        position[0] = position[1] = static_cast<int>(static_cast<uint32_t>(p.s.start[s]) + static_cast<uint32_t>(row - cu(s)));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (q_pair[i].at >= 0) position[i] = p.r.positions[q_pair[i].axis * p.r.ld_positions + row];
+      }
+      rotary_row<HD, T>(p.t, p.r, q_pair, row, head0, min(head0 + p.q_part_heads, p.r.n_heads), position, append_turns + warp * kRotaryMaxPairs);
+      continue;
+    }
+    const int pair = static_cast<int>(it) / p.head_parts, part = static_cast<int>(it) - pair * p.head_parts;
+    const CacheRun r = cache_run_of(p.c, p.s, last_sequence(p.s.n_seqs, pair, [&](int i) { return (cu(i) >> p.c.bs_log2) + 2 * i; }), p.r.n_rows, pair, p.status,
+                                    threadIdx.x == 0 && part == 0);
+    if (r.block < 0) continue;
+    const int n = r.hi - r.lo;
+    auto turns = [&]() {
+      __syncthreads();                                             // (the last item's table is no longer read)
+      if (k_pair.at >= 0)
+        for (int j = my_row; j < n; j += kAppendThreads >> pairs_log2) {
+          const int position = p.r.positions == nullptr ? r.place + j : p.r.positions[k_pair.axis * p.r.ld_positions + r.row + j];
+          append_turns[j * p.t.pairs + k_pair.at] = rotary_turn(k_pair, position, p.t.scale, p.t.scale);
+        }
+      __syncthreads();
+    };
+    if (GT > 32 && n <= AppendUnits<HD, 32, T>::STEPS * AppendUnits<HD, 32, T>::ROWS) {
+      AppendUnits<HD, 32, T> units(p, r, part);
+      units.fetch(units.group);
+      turns();
+      units.all(append_turns, group_max);
+    } else {
+      AppendUnits<HD, GT, T> units(p, r, part);
+      units.fetch(units.group);
+      turns();
+      units.all(append_turns, group_max);
     }
   }
 }
