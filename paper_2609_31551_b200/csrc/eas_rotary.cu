@@ -126,29 +126,27 @@ static eas_status launch_append(AppendParams& p, int budget, bool all, cudaStrea
     CUDA_TRY(cudaFuncSetAttribute(cache_append_kernel<HD, GT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kOnePerSmSmem));
     once.settled();
   }
-  // Key/value heads of an item: all of a block's, whose cosines then are worked out once, unless that leaves CTAs without work; at the least one pass of a CTA (a few
-  // rows a sequence: a warp for a head's keys or values).
-  const bool few = static_cast<int64_t>(p.r.n_rows) <= static_cast<int64_t>(p.s.n_seqs) * AppendUnits<HD, 32, T>::STEPS * AppendUnits<HD, 32, T>::ROWS;
-  const int least = kAppendThreads / (few ? 32 : GT) > 1 ? kAppendThreads / (few ? 32 : GT) / 2 : 1;
-  const int64_t ctas = 2LL * g_device_sms;
+  // Key/value heads of an item: all of a block's, whose cosines then are worked out once, unless that leaves CTAs without work; at the least one pass of a CTA.
+  constexpr int kLeast = kAppendThreads / GT > 1 ? kAppendThreads / GT / 2 : 1;
+  const int64_t ctas = static_cast<int64_t>(kAppendCtas) * g_device_sms;
   const int64_t blocks = std::max<int64_t>(p.pairs - p.s.n_seqs, 1);      // (about half of the sequences' spare numbers have a block)
   p.part_heads = p.c.n_kv;
-  while (p.part_heads > least && blocks * ((p.c.n_kv + p.part_heads - 1) / p.part_heads) < 3 * ctas) p.part_heads = (p.part_heads + 1) / 2;
+  while (p.part_heads > kLeast && blocks * ((p.c.n_kv + p.part_heads - 1) / p.part_heads) < 2 * ctas) p.part_heads = (p.part_heads + 1) / 2;
   p.head_parts = (p.c.n_kv + p.part_heads - 1) / p.part_heads;
   if (static_cast<int64_t>(p.pairs) * p.head_parts > 0x3fffffff) return fail(EAS_ERR_UNSUPPORTED, "too many rows for one call");
-  split_heads(p.r.n_rows, std::max(p.r.n_heads, 1), 4 * 32 / (HD / 16), ctas * (kAppendThreads / 32), &p.q_parts, &p.q_part_heads);
+  split_heads(p.r.n_rows, std::max(p.r.n_heads, 1), kAppendBatch * 32 / (HD / 16), ctas * (kAppendThreads / 32), &p.q_parts, &p.q_part_heads);
   const int64_t items = static_cast<int64_t>(p.pairs) * p.head_parts + (static_cast<int64_t>(p.r.n_heads > 0 ? p.r.n_rows : 0) * p.q_parts + kAppendThreads / 32 - 1) / (kAppendThreads / 32);
   return launch_kernel(cache_append_kernel<HD, GT, T>, static_cast<int>(std::min<int64_t>(all ? ctas : budget, items)), kAppendThreads, all ? table : kOnePerSmSmem,
                        stream, p);
 }
+// threads of a head's keys or values: 32 values each of what a sequence has on average in a block
 template <int HD, typename T>
 static eas_status launch_append(AppendParams& p, int budget, bool all, cudaStream_t stream) {
-  switch (HD << p.c.bs_log2) {                                     // values of a block and head: 64 a thread
-    case 16384: return launch_append<HD, 256, T>(p, budget, all, stream);
-    case 8192: return launch_append<HD, 128, T>(p, budget, all, stream);
-    case 4096: return launch_append<HD, 64, T>(p, budget, all, stream);
-    default: return launch_append<HD, 32, T>(p, budget, all, stream);
-  }
+  const int64_t rows = std::min<int64_t>((p.r.n_rows + p.s.n_seqs - 1) / p.s.n_seqs, 1 << p.c.bs_log2), values = rows * HD;
+  if (values > 4096) return launch_append<HD, 256, T>(p, budget, all, stream);
+  if (values > 2048) return launch_append<HD, 128, T>(p, budget, all, stream);
+  if (values > 1024) return launch_append<HD, 64, T>(p, budget, all, stream);
+  return launch_append<HD, 32, T>(p, budget, all, stream);
 }
 
 static eas_status cache_append(const eas_cache* c, const eas_cache_seqs* s, const eas_rotary* rotary, const eas_rotary_inputs* in, const void* v, int64_t ld_v,

@@ -166,44 +166,44 @@ __device__ __forceinline__ uint32_t requantise(int q, float old, float s, float 
   return __float_as_uint(n + 12582912.0f);
 }
 
-// The scale of a block and head whose new values are at most `largest` in magnitude, the lo tokens that it has already having the scale `old`; where it
-// grows, GT threads round those again.  (NaN: Inf or NaN among the values, the block and head reads as NaN.)
-template <int HD, int GT>
-__device__ __forceinline__ float cache_block_scale(float largest, float old, int lo, int8_t* dst, int tid) {
+// The scale of a block and head whose new values are at most `largest` in magnitude, the lo tokens that it has already having the scale `old`.
+// (NaN: Inf or NaN among the values, the block and head reads as NaN.)
+__device__ __forceinline__ float cache_new_scale(float largest, float old, int lo, bool& grows) {
   float s = __fdiv_rn(largest, 127.0f);
   if (s < kCacheMinScale) s = kCacheMinScale;
   if (!(s * 0.0f == 0.0f)) s = __uint_as_float(0x7FFFFFFFu);
-  if (lo > 0) {
-    if (!(s <= old) && old == old) {                             // the scale grows (or stops being a number)
-      const float ratio = __fdiv_rn(old, s);
-      constexpr int kLanes = HD / 16;
-      constexpr int kTokens = GT / kLanes, kFlight = 4;          // tokens of all threads, of each thread in flight
-      for (int t0 = tid / kLanes; t0 < lo; t0 += kTokens * kFlight) {
-        uint4 y[kFlight];
+  grows = lo > 0 && !(s <= old) && old == old;                   // (or stops being a number)
+  return lo > 0 && !grows ? old : s;
+}
+// Where it grows, GT threads round the tokens that are there again.
+template <int HD, int GT>
+__device__ __forceinline__ void cache_requantise(float old, float s, int lo, int8_t* dst, int tid) {
+  const float ratio = __fdiv_rn(old, s);
+  constexpr int kLanes = HD / 16, kTokens = GT / kLanes, kFlight = 4;      // threads a token, tokens of all threads, of each thread in flight
+  for (int t0 = tid / kLanes; t0 < lo; t0 += kTokens * kFlight) {
+    uint4 y[kFlight];
 #pragma unroll
-        for (int i = 0; i < kFlight; ++i)
-          if (t0 + i * kTokens < lo) y[i] = *reinterpret_cast<const uint4*>(dst + (t0 + i * kTokens) * HD + (tid % kLanes) * 16);
+    for (int i = 0; i < kFlight; ++i)
+      if (t0 + i * kTokens < lo) y[i] = *reinterpret_cast<const uint4*>(dst + (t0 + i * kTokens) * HD + (tid % kLanes) * 16);
 #pragma unroll
-        for (int i = 0; i < kFlight; ++i) {
-          if (t0 + i * kTokens >= lo) break;
-          uint32_t yw[4] = {y[i].x, y[i].y, y[i].z, y[i].w};
+    for (int i = 0; i < kFlight; ++i) {
+      if (t0 + i * kTokens >= lo) break;
+      uint32_t yw[4] = {y[i].x, y[i].y, y[i].z, y[i].w};
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            uint32_t z = 0;
+      for (int w = 0; w < 4; ++w) {
+        uint32_t z = 0;
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
-              z |= (requantise(static_cast<int8_t>(yw[w] >> (8 * b)), old, s, ratio) & 0xFFu) << (8 * b);
-            yw[w] = z;
-          }
-          *reinterpret_cast<uint4*>(dst + (t0 + i * kTokens) * HD + (tid % kLanes) * 16) = make_uint4(yw[0], yw[1], yw[2], yw[3]);
-        }
+        for (int b = 0; b < 4; ++b)
+          z |= (requantise(static_cast<int8_t>(yw[w] >> (8 * b)), old, s, ratio) & 0xFFu) << (8 * b);
+        yw[w] = z;
       }
-    } else {
-      s = old;
+      *reinterpret_cast<uint4*>(dst + (t0 + i * kTokens) * HD + (tid % kLanes) * 16) = make_uint4(yw[0], yw[1], yw[2], yw[3]);
     }
   }
-  return s;
 }
+// (called, where its registers would cost the way that most calls take)
+template <int HD, int GT>
+__device__ __noinline__ void cache_requantise_apart(float old, float s, int lo, int8_t* dst, int tid) { cache_requantise<HD, GT>(old, s, lo, dst, tid); }
 
 // GT threads per (sequence, block, head, keys or values): the largest magnitude of the new rows, the scale, the numbers.  Memory-bound: 2 bytes
 // read and 1 written per value.  A thread holds all of its values, at most 8 loads of 16 bytes (GT = block_size * head_dim / 64): they are all
@@ -251,7 +251,9 @@ __global__ void __launch_bounds__(512, 1) cache_store_kernel(const __grid_consta
     } else {
       __syncwarp();
     }
-    const float s = cache_block_scale<HD, GT>(Pair16<T>::lo(m), old, r.lo, dst, tid);
+    bool grows;
+    const float s = cache_new_scale(Pair16<T>::lo(m), old, r.lo, grows);
+    if (grows) cache_requantise<HD, GT>(old, s, r.lo, dst, tid);
     const float inv = __fdiv_rn(1.0f, s);
     int8_t* out = dst + (r.lo + sub) * HD + chunk * 8;
 #pragma unroll
