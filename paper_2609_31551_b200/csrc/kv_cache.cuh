@@ -201,10 +201,6 @@ __device__ __forceinline__ void cache_requantise(float old, float s, int lo, int
     }
   }
 }
-// (called, where its registers would cost the way that most calls take)
-template <int HD, int GT>
-__device__ __noinline__ void cache_requantise_apart(float old, float s, int lo, int8_t* dst, int tid) { cache_requantise<HD, GT>(old, s, lo, dst, tid); }
-
 // GT threads per (sequence, block, head, keys or values): the largest magnitude of the new rows, the scale, the numbers.  Memory-bound: 2 bytes
 // read and 1 written per value.  A thread holds all of its values, at most 8 loads of 16 bytes (GT = block_size * head_dim / 64): they are all
 // in flight at once, 64 KB an SM, and are read once.  6227 tokens of 8 heads of 128 into blocks of 64 take 12 us, 16384 32 (half the copy rate: a group

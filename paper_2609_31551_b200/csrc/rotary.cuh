@@ -33,15 +33,18 @@ struct RotaryPair {
     f_lo = t.f_lo[i];
     f_hi = t.f_hi[i];
     axis = t.axis[i];
-    at = pair < t.pairs ? rotary_place(i, t.pairs) : -1;
+    at = pair < t.pairs ? rotary_place(i, t.pairs, t.neighbours) : -1;
   }
   __device__ __forceinline__ void put(float* row, float2 turn) const {
     row[at] = turn.x;
     row[at + 2] = turn.y;
   }
-  // The table of a row: 8 pairs an item (16 dimensions), as four float4, cosines and sines of two pairs; those of all items side by side, so that threads of
-  // neighbouring items read side by side
-  static __device__ __forceinline__ int rotary_place(int pair, int pairs) { return ((pair >> 1) & 3) * (pairs >> 1) + (pair >> 3) * 4 + (pair & 1); }
+  // The table of a row: 8 pairs an item (16 dimensions, as two chunks of 8), as four float4, cosines and sines of the two pairs that word i of the chunks belongs to; those
+  // of all items side by side, so that threads of neighbouring items read side by side
+  static __device__ __forceinline__ int rotary_place(int pair, int pairs, int neighbours) {
+    const int k = pair & 7, word = neighbours ? k & 3 : k >> 1, which = neighbours ? k >> 2 : k & 1;
+    return word * (pairs >> 1) + (pair >> 3) * 4 + which;
+  }
 };
 // cosine and sine of a pair's angle at a position, times the scale (the sine's is negative where the rotation is taken back).  The turn's upper bits are the nearest
 // quarter, the rest an angle within pi / 4, for which the Taylor sums up to x^9 and x^8 are off by less than 2^-29 and 2^-25.
@@ -75,32 +78,22 @@ struct RotaryRows {
 __device__ __forceinline__ int2 rotary_at(int c, int pairs, int neighbours) {
   return !neighbours && 8 * c < pairs ? make_int2(8 * c, pairs + 8 * c) : make_int2(16 * c, 16 * c + 8);
 }
-// the 16 values of a rotated item, turned by its 8 pairs' cosines and sines (cs: the item's first two in the row's table of `items` items)
+// Words of two pairs: of halves, a word of the first chunk has the pairs' first values and one of the second chunk their second ones; of neighbours, a word has a pair.
+// (lo, hi), the way there and back: bytes of a word of each chunk to (first values, second values), the same for both, by two permutations.
+struct RotaryWords {
+  uint32_t lo, hi;
+  __device__ __forceinline__ explicit RotaryWords(int neighbours) : lo(neighbours ? 0x5410u : 0x3210u), hi(neighbours ? 0x7632u : 0x7654u) {}
+};
+// Word i of the item's chunks (a: first, b: second) turned: the two pairs' first values and their second ones, fp32.  cs: the item's first float4 in the row's table of
+// `items` items.
 template <typename T>
-__device__ __forceinline__ void rotary_turn_16(const uint4& lo, const uint4& hi, const float4* cs, int items, int neighbours, float (&y)[16]) {
-  const uint32_t a[4] = {lo.x, lo.y, lo.z, lo.w}, b[4] = {hi.x, hi.y, hi.z, hi.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {           // two pairs
-    const float4 t = cs[i * items];
-    const uint64_t cos2 = pack2(t.x, t.y), sin2 = pack2(t.z, t.w), minus2 = pack2(-t.z, -t.w);
-    uint64_t u, v;                        // the pairs' first and second values
-    if (neighbours) {
-      const uint32_t w0 = i < 2 ? a[2 * i] : b[2 * i - 4], w1 = i < 2 ? a[2 * i + 1] : b[2 * i - 3];
-      u = pack2(Pair16<T>::lo(w0), Pair16<T>::lo(w1));
-      v = pack2(Pair16<T>::hi(w0), Pair16<T>::hi(w1));
-    } else {
-      u = pack2(Pair16<T>::lo(a[i]), Pair16<T>::hi(a[i]));
-      v = pack2(Pair16<T>::lo(b[i]), Pair16<T>::hi(b[i]));
-    }
-    const uint64_t u_new = ffma2(u, cos2, fmul2(v, minus2)), v_new = ffma2(v, cos2, fmul2(u, sin2));
-    if (neighbours) {
-      unpack2(u_new, y[4 * i], y[4 * i + 2]);
-      unpack2(v_new, y[4 * i + 1], y[4 * i + 3]);
-    } else {
-      unpack2(u_new, y[2 * i], y[2 * i + 1]);
-      unpack2(v_new, y[8 + 2 * i], y[9 + 2 * i]);
-    }
-  }
+__device__ __forceinline__ void rotary_turn_word(const RotaryWords& w, uint32_t a, uint32_t b, const float4* cs, uint64_t& first, uint64_t& second) {
+  const uint32_t u = __byte_perm(a, b, w.lo), v = __byte_perm(a, b, w.hi);
+  const uint64_t u2 = pack2(Pair16<T>::lo(u), Pair16<T>::hi(u)), v2 = pack2(Pair16<T>::lo(v), Pair16<T>::hi(v));
+  const float4 t = *cs;
+  const uint64_t cos2 = pack2(t.x, t.y);
+  first = ffma2(v2, pack2(-t.z, -t.w), fmul2(u2, cos2));
+  second = ffma2(u2, pack2(t.z, t.w), fmul2(v2, cos2));
 }
 
 // One token's heads [head0, head1) of queries and keys side by side (keys behind the queries), by a warp.  cs: the warp's 64 cosines and sines.
@@ -110,6 +103,7 @@ __device__ __forceinline__ void rotary_row(const RotaryTable& t, const RotaryRow
   constexpr int ITEMS = HD / 16, LANES = 32 / ITEMS;                     // items a head, heads a warp takes at once (BATCH times that are in flight)
   const int lane = threadIdx.x & 31, item = lane % ITEMS, sub = lane / ITEMS;
   const bool turned = 8 * item < t.pairs;
+  const RotaryWords words(t.neighbours);
   const int2 at = rotary_at(item, t.pairs, t.neighbours);
   auto from = [&](int h) {
     return h < r.n_heads ? static_cast<const T*>(r.q) + row * r.ld_q + h * HD : static_cast<const T*>(r.k) + row * r.ld_k + (h - r.n_heads) * HD;
@@ -145,10 +139,20 @@ __device__ __forceinline__ void rotary_row(const RotaryTable& t, const RotaryRow
       if (h >= head1 || (!turned && r.in_place)) continue;
       T* dst = to(h);
       if (turned) {
-        float y[16];
-        rotary_turn_16<T>(lo[i], hi[i], reinterpret_cast<const float4*>(cs) + item, t.pairs >> 3, t.neighbours, y);
-        lo[i] = make_uint4(Pair16<T>::pack(y[0], y[1]), Pair16<T>::pack(y[2], y[3]), Pair16<T>::pack(y[4], y[5]), Pair16<T>::pack(y[6], y[7]));
-        hi[i] = make_uint4(Pair16<T>::pack(y[8], y[9]), Pair16<T>::pack(y[10], y[11]), Pair16<T>::pack(y[12], y[13]), Pair16<T>::pack(y[14], y[15]));
+        uint32_t a[4] = {lo[i].x, lo[i].y, lo[i].z, lo[i].w}, b[4] = {hi[i].x, hi[i].y, hi[i].z, hi[i].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          uint64_t first, second;
+          rotary_turn_word<T>(words, a[e], b[e], reinterpret_cast<const float4*>(cs) + e * (t.pairs >> 3) + item, first, second);
+          float f0, f1, s0, s1;
+          unpack2(first, f0, f1);
+          unpack2(second, s0, s1);
+          const uint32_t f = Pair16<T>::pack(f0, f1), s = Pair16<T>::pack(s0, s1);
+          a[e] = __byte_perm(f, s, words.lo);
+          b[e] = __byte_perm(f, s, words.hi);
+        }
+        lo[i] = make_uint4(a[0], a[1], a[2], a[3]);
+        hi[i] = make_uint4(b[0], b[1], b[2], b[3]);
       }
       *reinterpret_cast<uint4*>(dst + at.x) = lo[i];
       *reinterpret_cast<uint4*>(dst + at.y) = hi[i];
@@ -210,30 +214,40 @@ struct AppendParams {
   int early_launch;
 };
 
-constexpr int kAppendThreads = 256, kAppendCtas = 3, kAppendSteps = 2, kAppendBatch = 2;      // CTAs an SM: one's loads beside the others' arithmetic
+constexpr int kAppendThreads = 256, kAppendCtas = 2, kAppendSteps = 2, kAppendBatch = 2;      // CTAs an SM (three spill registers)
 
-// Eight fp32 values to eight numbers, as quantise8 does it
-__device__ __forceinline__ uint2 quantise8_fp32(const float* y, float s, float inv) {
+// An item's 16 values, word by word as rotary_turn_word leaves them, to its two chunks of eight numbers, as quantise8 does it.  order: of a word's four bytes, first
+// values before second ones or pair by pair
+__device__ __forceinline__ void quantise16(const uint64_t (&first)[4], const uint64_t (&second)[4], float s, float inv, uint32_t order, uint2& lo, uint2& hi) {
   const uint64_t inv2 = pack2(inv, inv), magic = pack2(12582912.0f, 12582912.0f), less = pack2(-12582912.0f, -12582912.0f), minus = pack2(-1.0f, -1.0f);
-  uint32_t q[8];
+  uint32_t q[16];
   float off = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 8; i += 2) {
-    const uint64_t r = fmul2(pack2(y[i], y[i + 1]), inv2);
+  for (int i = 0; i < 8; ++i) {
+    const uint64_t r = fmul2(i & 1 ? second[i >> 1] : first[i >> 1], inv2);
     const uint64_t t = fadd2(r, magic);                            // the nearest integer in the low bits
     float a, b, d0, d1;
     unpack2(t, a, b);
     unpack2(ffma2(fadd2(t, less), minus, r), d0, d1);
     off = fmax3(off, fabsf(d0), fabsf(d1));
-    q[i] = __float_as_uint(a);
-    q[i + 1] = __float_as_uint(b);
+    q[2 * i] = __float_as_uint(a);
+    q[2 * i + 1] = __float_as_uint(b);
   }
   if (__builtin_expect(off > 0.5f - 3.0517578125e-05f, 0)) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) q[i] = quantise(y[i], s, inv);
+    for (int i = 0; i < 8; ++i) {
+      float a, b;
+      unpack2(i & 1 ? second[i >> 1] : first[i >> 1], a, b);
+      q[2 * i] = quantise(a, s, inv);
+      q[2 * i + 1] = quantise(b, s, inv);
+    }
   }
-  return make_uint2(__byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410),
-                    __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410));
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    w[i] = __byte_perm(__byte_perm(__byte_perm(q[4 * i], q[4 * i + 1], 0x0040), __byte_perm(q[4 * i + 2], q[4 * i + 3], 0x0040), 0x5410), 0u, order);
+  lo = make_uint2(__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410));
+  hi = make_uint2(__byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632));
 }
 
 // An item is the run of one sequence's new rows that lies in one block, and some of its key/value heads: the cosines and sines of the run's rows go to
@@ -248,6 +262,7 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendCtas) cache_append_kern
   const RotaryPair q_pair[2] = {{p.t, lane}, {p.t, lane + 32}};
   const int pairs_log2 = p.pairs_log2, my_row = threadIdx.x >> pairs_log2;
   const RotaryPair k_pair(p.t, threadIdx.x & ((1 << pairs_log2) - 1));
+  const RotaryWords words(p.t.neighbours);
   if (p.early_launch) pdl_launch_dependents();
   pdl_wait();
   auto cu = [&](int i) { return min(max(p.s.cu[i], 0), p.r.n_rows); };
@@ -284,7 +299,7 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendCtas) cache_append_kern
     {
       const int units = 2 * min(p.part_heads, p.c.n_kv - part * p.part_heads), rounds = (n + CAP - 1) / CAP;
 #pragma unroll 1
-      for (int u = group, first = 1; u < units || first; u += kAppendThreads / GT, first = 0) {
+      for (int u = group; u < units || u == group; u += kAppendThreads / GT) {
         const bool values = u & 1, turned = !values && 8 * item < p.t.pairs;
         const int head = part * p.part_heads + (u >> 1);
         const long long ld = values ? p.ld_v : p.r.ld_k, at = static_cast<long long>(r.block) * p.c.n_kv + head;
@@ -293,7 +308,7 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendCtas) cache_append_kern
         float* scale = (values ? p.c.v_scale : p.c.k_scale) + at;
         int8_t* dst = (values ? p.c.v : p.c.k) + ((at << p.c.bs_log2) * HD);
         uint4 x[2 * STEPS];
-        float y[STEPS][16];
+        uint64_t first[STEPS][4], second[STEPS][4];
         auto load = [&](int row0) {                                // rows row0 + sub, ...
 #pragma unroll
           for (int i = 0; i < STEPS; ++i) {
@@ -307,27 +322,40 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendCtas) cache_append_kern
         auto turn = [&](int row0) {
 #pragma unroll
           for (int i = 0; i < STEPS; ++i) {
+            const uint32_t a[4] = {x[2 * i].x, x[2 * i].y, x[2 * i].z, x[2 * i].w}, b[4] = {x[2 * i + 1].x, x[2 * i + 1].y, x[2 * i + 1].z, x[2 * i + 1].w};
             if (turned && row0 + sub + i * ROWS < n) {
-              rotary_turn_16<T>(x[2 * i], x[2 * i + 1], reinterpret_cast<const float4*>(append_turns + (row0 + sub + i * ROWS) * p.t.pairs) + item, p.t.pairs >> 3, p.t.neighbours, y[i]);
-            } else {
-              const uint32_t w[8] = {x[2 * i].x, x[2 * i].y, x[2 * i].z, x[2 * i].w, x[2 * i + 1].x, x[2 * i + 1].y, x[2 * i + 1].z, x[2 * i + 1].w};
+              const float4* cs = reinterpret_cast<const float4*>(append_turns + (row0 + sub + i * ROWS) * p.t.pairs) + item;
 #pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                y[i][2 * e] = Pair16<T>::lo(w[e]);
-                y[i][2 * e + 1] = Pair16<T>::hi(w[e]);
+              for (int e = 0; e < 4; ++e) rotary_turn_word<T>(words, a[e], b[e], cs + e * (p.t.pairs >> 3), first[i][e], second[i][e]);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                first[i][e] = pack2(Pair16<T>::lo(a[e]), Pair16<T>::hi(a[e]));
+                second[i][e] = pack2(Pair16<T>::lo(b[e]), Pair16<T>::hi(b[e]));
               }
             }
           }
         };
         load(0);
         const float old = r.lo > 0 && u < units ? *scale : 0.0f;
-        if (first) {                                               // (beside the first loads)
+        if (u == group) {                                          // (beside the first loads)
           __syncthreads();                                         // (the last item's table is no longer read)
-          if (k_pair.at >= 0)
-            for (int j = my_row; j < n; j += kAppendThreads >> pairs_log2) {
-              const int position = p.r.positions == nullptr ? r.place + j : p.r.positions[k_pair.axis * p.r.ld_positions + r.row + j];
-              k_pair.put(reinterpret_cast<float*>(append_turns + j * p.t.pairs), rotary_turn(k_pair, position, p.t.scale, p.t.scale));
+          if (k_pair.at >= 0) {
+            const int apart = kAppendThreads >> pairs_log2;
+            const int32_t* from = p.r.positions == nullptr ? nullptr : p.r.positions + k_pair.axis * p.r.ld_positions + r.row;
+            for (int j0 = my_row; j0 < n; j0 += 8 * apart) {       // 8 positions in flight
+              int position[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const int j = min(j0 + e * apart, n - 1);
+                position[e] = from == nullptr ? r.place + j : from[j];
+              }
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (j0 + e * apart < n)
+                  k_pair.put(reinterpret_cast<float*>(append_turns + (j0 + e * apart) * p.t.pairs), rotary_turn(k_pair, position[e], p.t.scale, p.t.scale));
             }
+          }
           __syncthreads();
           if (u >= units) break;
         }
@@ -344,7 +372,13 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendCtas) cache_append_kern
 #pragma unroll
           for (int i = 0; i < STEPS; ++i)
 #pragma unroll
-            for (int e = 0; e < 16; e += 2) largest = fmax3(largest, fabsf(y[i][e]), fabsf(y[i][e + 1]));
+            for (int e = 0; e < 4; ++e) {
+              float a, b;
+              unpack2(first[i][e], a, b);
+              largest = fmax3(largest, fabsf(a), fabsf(b));
+              unpack2(second[i][e], a, b);
+              largest = fmax3(largest, fabsf(a), fabsf(b));
+            }
         }
         const float whole = Pair16<T>::lo(max(m2 & 0xFFFFu, m2 >> 16));
         uint32_t m = __float_as_uint(whole * 0.f == 0.f ? largest : whole);
@@ -360,7 +394,6 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendCtas) cache_append_kern
         }
         bool grows;
         const float s = cache_new_scale(__uint_as_float(m), old, r.lo, grows);
-        if (grows) cache_requantise_apart<HD, GT>(old, s, r.lo, dst, tid);
         const float inv = __fdiv_rn(1.0f, s);
         int8_t* out = dst + (r.lo + sub) * HD;
 #pragma unroll 1
@@ -373,11 +406,14 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendCtas) cache_append_kern
           for (int i = 0; i < STEPS; ++i) {
             const int j = round * CAP + i * ROWS;
             if (sub + j < n) {
-              *reinterpret_cast<uint2*>(out + j * HD + dims.x) = quantise8_fp32(y[i], s, inv);
-              *reinterpret_cast<uint2*>(out + j * HD + dims.y) = quantise8_fp32(y[i] + 8, s, inv);
+              uint2 lo, hi;
+              quantise16(first[i], second[i], s, inv, turned && p.t.neighbours ? 0x3120u : 0x3210u, lo, hi);
+              *reinterpret_cast<uint2*>(out + j * HD + dims.x) = lo;
+              *reinterpret_cast<uint2*>(out + j * HD + dims.y) = hi;
             }
           }
         }
+        if (grows) cache_requantise<HD, GT>(old, s, r.lo, dst, tid);      // (last: the new values' registers are free)
         if (tid == 0) *scale = s;
       }
     }
