@@ -131,7 +131,7 @@ static eas_status launch_append(AppendParams& p, int budget, bool all, cudaStrea
   const int64_t ctas = static_cast<int64_t>(kAppendCtas) * g_device_sms;
   const int64_t blocks = std::max<int64_t>(p.pairs - p.s.n_seqs, 1);      // (about half of the sequences' spare numbers have a block)
   p.part_heads = p.c.n_kv;
-  while (p.part_heads > kLeast && blocks * ((p.c.n_kv + p.part_heads - 1) / p.part_heads) < 2 * ctas) p.part_heads = (p.part_heads + 1) / 2;
+  while (p.part_heads > kLeast && blocks * ((p.c.n_kv + p.part_heads - 1) / p.part_heads) < ctas) p.part_heads = (p.part_heads + 1) / 2;
   p.head_parts = (p.c.n_kv + p.part_heads - 1) / p.part_heads;
   if (static_cast<int64_t>(p.pairs) * p.head_parts > 0x3fffffff) return fail(EAS_ERR_UNSUPPORTED, "too many rows for one call");
   split_heads(p.r.n_rows, std::max(p.r.n_heads, 1), kAppendBatch * 32 / (HD / 16), ctas * (kAppendThreads / 32), &p.q_parts, &p.q_part_heads);
