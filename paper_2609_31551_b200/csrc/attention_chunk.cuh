@@ -59,21 +59,21 @@ struct ChunkParams {
 template <int HD>
 struct ChunkCfg {
   static constexpr int kHalves = HD / 64;
-  static constexpr int kRawTiles = HD == 128 ? 3 : 6, kKTiles = HD == 128 ? 2 : 3, kVTiles = HD == 128 ? 2 : 3;
+  static constexpr int kRawK = HD == 128 ? 3 : 6, kRawV = HD == 128 ? 2 : 6, kKTiles = HD == 128 ? 2 : 3, kVTiles = 3;
   static constexpr int kThreads = 512;
   static constexpr int kRegsLight = 80, kRegsConvert = 96, kRegsSoftmax = 168, kRegsLaunch = 128;
   static constexpr int kQHalf = 128 * 128, kQBytes = kQHalf * kHalves;                 // 128 rows x 64 elements
   static constexpr int kAtomBytes = kChunkKeys * 128, kTileBytes = kAtomBytes * kHalves;   // 80 keys x 64 elements
   static constexpr int kRawBytes = kChunkKeys * HD;
   static constexpr int kKOff = 2 * kQBytes, kVOff = kKOff + kKTiles * kTileBytes, kRawOff = kVOff + kVTiles * kTileBytes;
-  static constexpr int kPrefixOff = kRawOff + 2 * kRawTiles * kRawBytes;                // (keys' tiles, then values')
+  static constexpr int kPrefixOff = kRawOff + (kRawK + kRawV) * kRawBytes;              // (keys' tiles, then values')
   static constexpr int kScaleSlots = 32;
   static constexpr int kScaleOff = kPrefixOff + (kChunkMaxSeqs + 2) * 8;               // [slot][16]: key scales, log2 of value scales, their inverses
   static constexpr int kRowOff = kScaleOff + kScaleSlots * 64;                         // [2][128] factors and offsets of the rows' scores
   static constexpr int kMlOff = kRowOff + 2 * 128 * 8;                                 // [2][128] reference and sum of a warpgroup's rows
   static constexpr int kItemOff = kMlOff + 2 * 128 * 8;
   static constexpr int kBarOff = kItemOff + kChunkItems * 64;
-  static constexpr int kBars = 4 * kRawTiles + 2 * kKTiles + 2 * kVTiles + kScaleSlots + 2 + 2 + 4 * 2 + 2 + 2 * kChunkItems;
+  static constexpr int kBars = 2 * (kRawK + kRawV) + 2 * kKTiles + 2 * kVTiles + kScaleSlots + 2 + 2 + 4 * 2 + 2 + 2 * kChunkItems;
   static constexpr int kBytes = kBarOff + kBars * 8 + 160 + 1024;                      // words, alignment slack
   static constexpr int kSCol0 = 2 * HD, kSStride = kChunkKeys + kChunkKeys / 2;        // tensor memory: O of both, then scores and P of each
   static_assert(kBytes <= 232448, "exceeds the shared memory of an SM");
@@ -82,7 +82,7 @@ struct ChunkCfg {
   static_assert(kSCol0 + 2 * kSStride <= 512, "tensor memory columns");
   static_assert(kRegsLight + kRegsConvert + 2 * kRegsSoftmax <= 4 * kRegsLaunch, "setmaxnreg budget exceeds the CTA's register allocation");
   // the producer is at most this many steps ahead of the softmax: a batch of scales, raw tiles, converted K tiles, one step each being read
-  static_assert(6 + kRawTiles + 1 + kKTiles + 4 <= kScaleSlots, "a step's scales are read before their slot is filled again");
+  static_assert(6 + kRawK + 1 + kKTiles + 4 <= kScaleSlots, "a step's scales are read before their slot is filled again");
 };
 
 // row / group of a tile's row
@@ -354,7 +354,7 @@ __device__ __forceinline__ void store_row_16(uint32_t tile, uint32_t atom_bytes,
 template <int HD>
 __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_kernel(const __grid_constant__ ChunkParams p) {
   using L = ChunkCfg<HD>;
-  constexpr int NR = L::kRawTiles, NK = L::kKTiles, NV = L::kVTiles, KEYS = kChunkKeys, PARTS = kChunkParts, NS = L::kScaleSlots;
+  constexpr int NRK = L::kRawK, NR = NRK + L::kRawV, NK = L::kKTiles, NV = L::kVTiles, KEYS = kChunkKeys, PARTS = kChunkParts, NS = L::kScaleSlots;
   extern __shared__ uint8_t smem_raw_chunk[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw_chunk) + 1023) & ~uintptr_t(1023));
   long long* prefix = reinterpret_cast<long long*>(smem + L::kPrefixOff);
@@ -363,9 +363,9 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
   float2* ml_smem = reinterpret_cast<float2*>(smem + L::kMlOff);
   // barriers: addresses in shared memory, 8 bytes each
   const uint32_t smem_at = smem_u32(smem);
-  const uint32_t raw_full = smem_at + L::kBarOff;         // [2 NR] bytes of a tile landed: keys, values
-  const uint32_t raw_empty = raw_full + 8 * 2 * NR;       // [2 NR] converted
-  const uint32_t k_full = raw_empty + 8 * 2 * NR;         // [NK] fp16 tile written
+  const uint32_t raw_full = smem_at + L::kBarOff;         // [NR] bytes of a tile landed: NRK of keys, the others of values
+  const uint32_t raw_empty = raw_full + 8 * NR;           // [NR] converted
+  const uint32_t k_full = raw_empty + 8 * NR;             // [NK] fp16 tile written
   const uint32_t k_empty = k_full + 8 * NK;               // [NK] every issuer hands every tile back
   const uint32_t v_full = k_empty + 8 * NK;               // [NV]
   const uint32_t v_empty = v_full + 8 * NV;               // [NV]
@@ -385,7 +385,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
 
   const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 2 * NR; ++i) { mbar_init(raw_full + 8 * i, 1); mbar_init(raw_empty + 8 * i, 2); }
+    for (int i = 0; i < NR; ++i) { mbar_init(raw_full + 8 * i, 1); mbar_init(raw_empty + 8 * i, 2); }
     for (int i = 0; i < NK; ++i) { mbar_init(k_full + 8 * i, 2); mbar_init(k_empty + 8 * i, 2); }
     for (int i = 0; i < NV; ++i) { mbar_init(v_full + 8 * i, 2); mbar_init(v_empty + 8 * i, 2); }
     for (int i = 0; i < NS; ++i) mbar_init(sc_full + 8 * i, 1);
@@ -433,8 +433,8 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       // ------------------------------------------------------------------ bytes: of keys (warp 0, which has the scales too) and of values (warp 3)
       const bool values = warp == 3;
       const int8_t* const cache = values ? p.c.v : p.c.k;
-      const uint32_t full = raw_full + (values ? 8 * NR : 0), empty = raw_empty + (values ? 8 * NR : 0);
-      const uint32_t raw = L::kRawOff + (values ? NR * L::kRawBytes : 0);
+      const uint32_t full = raw_full + (values ? 8 * NRK : 0), empty = raw_empty + (values ? 8 * NRK : 0), ring = values ? NR - NRK : NRK;
+      const uint32_t raw = L::kRawOff + (values ? NRK * L::kRawBytes : 0);
       uint32_t g = 0;                              // steps so far
       uint32_t st = 0, free = 1;                   // the ring's next place, and the phase in which it is empty
       // A lane has a part of 16 tokens of the kBatch steps at hand.  Block numbers are asked for two batches ahead and scales one: they come from anywhere in memory.
@@ -481,7 +481,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
               if (elect_one()) bulk_load(smem + raw + st * L::kRawBytes + (l - i * PARTS) * 16 * HD, reinterpret_cast<const void*>(from), n_bytes, full + 8 * st);
               __syncwarp();
             }
-            if (++st == NR) { st = 0; free ^= 1u; }
+            if (++st == ring) { st = 0; free ^= 1u; }
             if (i == 0 && !values) {               // the batch's scales
               if (lane < steps * PARTS) {
                 float* dst = sc_ring + (g + my_step) % NS * 16 + my_part;
@@ -555,7 +555,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
         }
       }
       // every copy has landed before the CTA's shared memory passes to another one: converted, or (after an expired wait) by time
-      for (uint32_t e = g < NR ? 0 : g - NR; e < g && ok; ++e) ok = chunk_wait(empty + 8 * (e % NR), (e / NR) & 1u, abort_flag);
+      for (uint32_t e = g < ring ? 0 : g - ring; e < g && ok; ++e) ok = chunk_wait(empty + 8 * (e % ring), (e / ring) & 1u, abort_flag);
       if (!ok) {
         const long long t0 = clock64();
         while (clock64() - t0 < 4000000) {}
@@ -677,11 +677,11 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
     constexpr int STEP = 2 * ROWS, BATCH = 5, PASSES = KEYS / STEP;        // rows that a pair takes at once
     static_assert(KEYS % STEP == 0 && PASSES % BATCH == 0 && STEP % 8 == 0, "whole passes; a row's place in its swizzle pattern stays");
     const int row = (cw & 1) * ROWS + sub;
-    const uint32_t raw0 = smem_at + L::kRawOff + (keys ? 0 : NR) * L::kRawBytes + chunk * 16 + row * HD;
+    const uint32_t raw0 = smem_at + L::kRawOff + (keys ? 0 : NRK) * L::kRawBytes + chunk * 16 + row * HD;
     const uint32_t tile0 = smem_at + (keys ? L::kKOff : L::kVOff) + (chunk >> 2) * L::kAtomBytes + row * 128 + (((2 * (chunk & 3)) ^ (row & 7)) << 4);
-    const uint32_t from_full = raw_full + (keys ? 0 : 8 * NR), from_empty = raw_empty + (keys ? 0 : 8 * NR);
+    const uint32_t from_full = raw_full + (keys ? 0 : 8 * NRK), from_empty = raw_empty + (keys ? 0 : 8 * NRK);
     const uint32_t full = keys ? k_full : v_full, empty = keys ? k_empty : v_empty;
-    const uint32_t ring = keys ? NK : NV;
+    const uint32_t raws = keys ? NRK : NR - NRK, ring = keys ? NK : NV;
     uint32_t st = 0, landed = 0, to = 0, gone = 1;                         // places in the two rings, and the phases to wait for
     auto convert = [&]() {
       if (!chunk_wait(from_full + 8 * st, landed, abort_flag) || !chunk_wait(empty + 8 * to, gone, abort_flag)) return false;
@@ -712,7 +712,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       __syncwarp();
       mbar_arrive_if(from_empty + 8 * st, lane == 0);
       mbar_arrive_if(full + 8 * to, lane == 0);
-      if (++st == NR) { st = 0; landed ^= 1u; }
+      if (++st == raws) { st = 0; landed ^= 1u; }
       if (++to == ring) { to = 0; gone ^= 1u; }
       return true;
     };
