@@ -56,6 +56,8 @@ struct ChunkParams {
   int early_launch;
 };
 
+constexpr int kChunkDealBytes = 160;
+
 template <int HD>
 struct ChunkCfg {
   static constexpr int kHalves = HD / 64;
@@ -72,7 +74,8 @@ struct ChunkCfg {
   static constexpr int kRowOff = kScaleOff + kScaleSlots * 64;                         // [2][128] factors and offsets of the rows' scores
   static constexpr int kMlOff = kRowOff + 2 * 128 * 8;                                 // [2][128] reference and sum of a warpgroup's rows
   static constexpr int kItemOff = kMlOff + 2 * 128 * 8;
-  static constexpr int kBarOff = kItemOff + kChunkItems * 64;
+  static constexpr int kDealOff = kItemOff + kChunkItems * 64;                         // where warp 3 is on the line
+  static constexpr int kBarOff = kDealOff + kChunkDealBytes;
   static constexpr int kBars = 2 * (kRawK + kRawV) + 2 * kKTiles + 2 * kVTiles + kScaleSlots + 2 + 2 + 4 * 2 + 2 + 2 * kChunkItems;
   static constexpr int kBytes = kBarOff + kBars * 8 + 160 + 1024;                      // words, alignment slack
   static constexpr int kSCol0 = 2 * HD, kSStride = kChunkKeys + kChunkKeys / 2;        // tensor memory: O of both, then scores and P of each
@@ -160,7 +163,7 @@ struct ChunkLine {
     while (at + 1 < pieces && begin(at + 1) <= x) ++at;
     return at;
   }
-  __device__ __forceinline__ long long begin(int piece) const { return whole * piece + static_cast<uint32_t>(rest) * static_cast<uint32_t>(piece) / static_cast<uint32_t>(pieces); }
+  __device__ __forceinline__ long long begin(int piece) const { return whole * piece + min(piece, rest); }      // (the first `rest` pieces are one more long)
 };
 
 // A unit and its place on the line
@@ -230,20 +233,14 @@ struct ChunkUnit {
 };
 // The items of a CTA in order: of each unit in its pieces, the steps [lo, hi), never none
 struct ChunkDeal {
-  const ChunkParams& p;
-  const long long* prefix;
   ChunkLine line;
   ChunkUnit u;
   int piece, lo, hi;
   long long end;
-  bool more;
-  __device__ __forceinline__ ChunkDeal(const ChunkParams& params, const long long* pre)
-      : p(params), prefix(pre), line(pre[params.n_seqs], params.n_ctas), piece(blockIdx.x), lo(0), hi(0), end(0), more(true) {
-    seek(true);
-  }
-  __device__ __forceinline__ void next() { if (more) seek(false); }
-  __device__ __forceinline__ void seek(bool fresh) {               // fresh: the first item of `piece`; else the one behind the present one
-    for (;;) {
+  bool fresh, more;            // the next item is the first one of `piece`; there is a present one
+  __device__ __forceinline__ ChunkDeal(long long cost, int n_ctas) : line(cost, n_ctas), piece(blockIdx.x), lo(0), hi(0), end(0), fresh(true), more(true) {}
+  __device__ __forceinline__ void next(const ChunkParams& p, const long long* prefix) {
+    do {
       if (fresh) {
         more = piece < line.pieces;
         if (!more) return;
@@ -254,18 +251,19 @@ struct ChunkDeal {
         fresh = false;
       } else {
         u.next(p, prefix, line.total);
-        if (u.at >= end) {
-          piece += gridDim.x;
-          fresh = true;
-          continue;
-        }
         lo = 0;
       }
-      hi = end >= u.end(p) ? u.steps : u.step_at(end);
-      if (lo < hi) return;
-    }
+      if (u.at >= end) {
+        piece += gridDim.x;
+        fresh = true;
+        hi = 0;
+      } else {
+        hi = u.step_at(min(end, u.end(p)));
+      }
+    } while (lo >= hi);
   }
 };
+static_assert(sizeof(ChunkDeal) <= kChunkDealBytes, "its place in shared memory");
 // What the other roles know of an item
 struct alignas(16) ChunkItem {
   int lo, n;                   // its first key step and how many (0: there is no further item)
@@ -351,7 +349,7 @@ __device__ __forceinline__ void store_row_16(uint32_t tile, uint32_t atom_bytes,
 }
 
 // ------------------------------------------------------------------------------------ the kernel
-template <int HD>
+template <int HD, typename T>
 __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_kernel(const __grid_constant__ ChunkParams p) {
   using L = ChunkCfg<HD>;
   constexpr int NRK = L::kRawK, NR = NRK + L::kRawV, NK = L::kKTiles, NV = L::kVTiles, KEYS = kChunkKeys, PARTS = kChunkParts, NS = L::kScaleSlots;
@@ -501,58 +499,58 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
         }
         return true;
       };
+      // Warp 3 walks the line, one item ahead of its values
+      if (values && lane == 0)
+        for (int piece = blockIdx.x; piece < p.n_ctas; piece += gridDim.x) p.cut_ws[piece].n = 0;
+      // (its place on the line lies in shared memory while the warp copies: in registers it costs the loop of the copies its own)
+      ChunkDeal* const place = reinterpret_cast<ChunkDeal*>(smem + L::kDealOff);
+      if (values && lane == 0) *place = ChunkDeal(prefix[p.n_seqs], p.n_ctas);
+      __syncwarp();
+      auto put = [&](ChunkItem& it) {
+        ChunkDeal deal = *place;
+        deal.next(p, prefix);
+        __syncwarp();
+        if (lane == 0) *place = deal;
+        it = ChunkItem{};
+        if (deal.more) {
+          const ChunkUnit& u = deal.u;
+          it.lo = deal.lo;
+          it.n = deal.hi - deal.lo;
+          it.tiles = u.tiles;
+          it.mine[0] = min(deal.hi, u.steps_of_tile(p, 0)) - deal.lo;
+          it.mine[1] = min(deal.hi, u.steps_of_tile(p, 1)) - deal.lo;
+          it.q0 = u.seq.q0;
+          it.tok0 = 2 * u.j * p.tile_tokens;
+          it.n_tok = u.seq.n;
+          it.ahead = u.seq.ahead;
+          it.head = u.head;
+          it.s = u.s;
+          it.seen = u.seq.seen(u.j, p.tile_tokens);
+          it.slot = it.n == u.steps ? -1 : 2 * deal.piece + (deal.hi == u.steps ? 0 : 1);
+          if (deal.lo == 0 && deal.hi < u.steps) {
+            it.parts = deal.line.piece_of(u.at + kChunkUnitCost + static_cast<long long>(u.tiles) * KEYS * (u.steps - 1)) - deal.piece + 1;
+            if (lane == 0) p.cut_ws[deal.piece] = it;
+          }
+        }
+        const uint32_t at = n_items % kChunkItems;
+        if (!chunk_wait(item_empty + 8 * at, ((n_items / kChunkItems) & 1u) ^ 1u, abort_flag)) return false;
+        if (lane == 0) {
+          item_ring[at] = it;
+          mbar_arrive(item_full + 8 * at);
+        }
+        __syncwarp();
+        ++n_items;
+        return true;
+      };
       bool ok = true;
-      if (!values) {
-        while (ok) {
-          ChunkItem it;
-          ok = take(it);
-          if (!ok || it.n == 0) break;
-          ok = stream(it);
-        }
-      } else {
-        // the items of the CTA, one ahead of their values
-        if (lane == 0)
-          for (int piece = blockIdx.x; piece < p.n_ctas; piece += gridDim.x) p.cut_ws[piece].n = 0;
-        ChunkDeal deal(p, prefix);
-        auto put = [&]() {
-          ChunkItem it{};
-          if (deal.more) {
-            const ChunkUnit& u = deal.u;
-            it.lo = deal.lo;
-            it.n = deal.hi - deal.lo;
-            it.tiles = u.tiles;
-            it.mine[0] = min(deal.hi, u.steps_of_tile(p, 0)) - deal.lo;
-            it.mine[1] = min(deal.hi, u.steps_of_tile(p, 1)) - deal.lo;
-            it.q0 = u.seq.q0;
-            it.tok0 = 2 * u.j * p.tile_tokens;
-            it.n_tok = u.seq.n;
-            it.ahead = u.seq.ahead;
-            it.head = u.head;
-            it.s = u.s;
-            it.seen = u.seq.seen(u.j, p.tile_tokens);
-            it.slot = it.n == u.steps ? -1 : 2 * deal.piece + (deal.hi == u.steps ? 0 : 1);
-            if (deal.lo == 0 && deal.hi < u.steps) {
-              it.parts = deal.line.piece_of(u.at + kChunkUnitCost + static_cast<long long>(u.tiles) * KEYS * (u.steps - 1)) - deal.piece + 1;
-              if (lane == 0) p.cut_ws[deal.piece] = it;
-            }
-          }
-          const uint32_t at = n_items % kChunkItems;
-          ok = ok && chunk_wait(item_empty + 8 * at, ((n_items / kChunkItems) & 1u) ^ 1u, abort_flag);
-          if (ok && lane == 0) {
-            item_ring[at] = it;
-            mbar_arrive(item_full + 8 * at);
-          }
-          __syncwarp();
-          ++n_items;
-          return it;
-        };
-        ChunkItem it = put();
-        while (ok && it.n != 0) {
-          deal.next();
-          const ChunkItem next = put();
-          ok = ok && stream(it);
-          it = next;
-        }
+      ChunkItem it;
+      it.n = -1;                                   // values: there is none yet
+      while (ok && it.n != 0) {
+        ChunkItem next;
+        ok = values ? put(next) : take(next);
+        if (!values) it = next;
+        if (ok && it.n > 0) ok = stream(it);
+        it = next;
       }
       // every copy has landed before the CTA's shared memory passes to another one: converted, or (after an expired wait) by time
       for (uint32_t e = g < ring ? 0 : g - ring; e < g && ok; ++e) ok = chunk_wait(empty + 8 * (e % ring), (e / ring) & 1u, abort_flag);
@@ -567,22 +565,11 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       constexpr uint32_t idesc_s = make_idesc_f16(128, KEYS, 0, 0);        // S = Q K^T, both K-major
       constexpr uint32_t idesc_o = make_idesc_f16(128, HD, 0, 1);          // O += P V, V is MN-major
       const uint32_t tm_s = tmem_base + L::kSCol0 + w * L::kSStride, tm_p = tm_s + KEYS, tm_o = tmem_base + w * HD;
-      uint32_t base = 0, k_at = 0, v_at = 0, qn = 0, n_s = 0, n_p = 0;     // steps, tiles passed, query tiles, scores issued, P waited for
+      uint32_t qn = 0, n_s = 0, n_p = 0;           // query tiles, scores issued, P waited for
+      uint32_t k_st = 0, k_ph = 0, v_st = 0, v_ph = 0;                     // places in the rings, and the phases in which they are filled
       bool ok = true;
-      auto pass_k = [&](uint32_t to) {
-        for (; k_at < to; ++k_at) {
-          if (!chunk_wait(k_full + 8 * (k_at % NK), (k_at / NK) & 1u, abort_flag)) return false;
-          mbar_arrive_if(k_empty + 8 * (k_at % NK), lane == 0);
-        }
-        return true;
-      };
-      auto pass_v = [&](uint32_t to) {
-        for (; v_at < to; ++v_at) {
-          if (!chunk_wait(v_full + 8 * (v_at % NV), (v_at / NV) & 1u, abort_flag)) return false;
-          mbar_arrive_if(v_empty + 8 * (v_at % NV), lane == 0);
-        }
-        return true;
-      };
+      auto next_k = [&]() { if (++k_st == NK) { k_st = 0; k_ph ^= 1u; } };
+      auto next_v = [&]() { if (++v_st == NV) { v_st = 0; v_ph ^= 1u; } };
       while (ok) {
         ChunkItem it;
         ok = take(it);
@@ -594,70 +581,77 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
         const int last = mine <= first ? -1 : first + (mine - 1 - first) / stride * stride;
         const uint32_t slot = (qn + (alternate ? 0 : w)) & 1u;
         // queries: wait for each tile of the item, hand back what is not used
-        for (int t = 0; t < tiles && ok; ++t) {
-          const uint32_t q = qn + t;
-          ok = chunk_wait(q_full + 8 * (q & 1u), (q >> 1) & 1u, abort_flag);
-          if (ok && ((q & 1u) != slot || last < 0)) mbar_arrive_if(q_empty + 8 * (q & 1u), lane == 0);
+        for (int t = 0; t < tiles && ok; ++t, ++qn) {
+          ok = chunk_wait(q_full + 8 * (qn & 1u), (qn >> 1) & 1u, abort_flag);
+          if (ok && ((qn & 1u) != slot || last < 0)) mbar_arrive_if(q_empty + 8 * (qn & 1u), lane == 0);
         }
-        qn += tiles;
-        if (!ok) break;
-        auto scores = [&](int j) {                 // of step j, into the warpgroup's columns once they are read
-          const uint32_t g = base + j;
-          if (!pass_k(g) || !chunk_wait(k_full + 8 * (g % NK), (g / NK) & 1u, abort_flag)) return false;
-          if (n_s > 0 && !chunk_wait(s_free + 8 * w, (n_s - 1u) & 1u, abort_flag)) return false;
-          tc_fence_after_sync();
-          if (elect_one()) {
-            const uint32_t ring = g % NK;
-            for_constant<2 * NK>(slot * NK + ring, [&](auto c) {
-              constexpr int Q = decltype(c)::value / NK, K = decltype(c)::value % NK;
-              const uint64_t ad = make_smem_desc(smem_at + Q * L::kQBytes, 16, 1024, kSwizzle128B);
-              const uint64_t bd = make_smem_desc(smem_at + L::kKOff + K * L::kTileBytes, 16, 1024, kSwizzle128B);
-#pragma unroll
-              for (int h = 0; h < L::kHalves; ++h)
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                  umma_bf16_ss(tm_s, ad + h * (L::kQHalf >> 4) + 2 * k, bd + h * (L::kAtomBytes >> 4) + 2 * k, idesc_s, h != 0 || k != 0);
-              umma_commit(s_full + 8 * w);
-              umma_commit(k_empty + 8 * K);
-              if (j == last) umma_commit(q_empty + 8 * Q);
-            });
+        int k_at = 0, v_at = 0;                    // the item's tiles that are dealt with
+        // tiles up to `to`, which another warpgroup uses, as soon as they are there
+        auto pass_k = [&](int to) {
+          for (; k_at < to && ok; ++k_at, next_k()) {
+            ok = chunk_wait(k_full + 8 * k_st, k_ph, abort_flag);
+            mbar_arrive_if(k_empty + 8 * k_st, lane == 0);
           }
-          __syncwarp();
-          k_at = g + 1;
-          ++n_s;
-          return true;
         };
+        auto pass_v = [&](int to) {
+          for (; v_at < to && ok; ++v_at, next_v()) {
+            ok = chunk_wait(v_full + 8 * v_st, v_ph, abort_flag);
+            mbar_arrive_if(v_empty + 8 * v_st, lane == 0);
+          }
+        };
+        // the scores of the step behind j, into the warpgroup's columns once they are read, then P V of step j
 #pragma unroll 1
-        for (int j = first - stride; j <= last && ok && last >= 0; j += stride) {      // the scores of the step behind j, then P V of step j
-          if (j < last && !scores(j + stride)) { ok = false; break; }
+        for (int j = first - stride; j <= last && ok; j += stride) {
+          if (j < last) {
+            pass_k(j + stride);
+            if (!ok || !chunk_wait(k_full + 8 * k_st, k_ph, abort_flag) || !chunk_wait(s_free + 8 * w, (n_s & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+            tc_fence_after_sync();
+            if (elect_one()) {
+              for_constant<2 * NK>(slot * NK + k_st, [&](auto c) {
+                constexpr int Q = decltype(c)::value / NK, K = decltype(c)::value % NK;
+                const uint64_t ad = make_smem_desc(smem_at + Q * L::kQBytes, 16, 1024, kSwizzle128B);
+                const uint64_t bd = make_smem_desc(smem_at + L::kKOff + K * L::kTileBytes, 16, 1024, kSwizzle128B);
+#pragma unroll
+                for (int h = 0; h < L::kHalves; ++h)
+#pragma unroll
+                  for (int k = 0; k < 4; ++k)
+                    umma_bf16_ss(tm_s, ad + h * (L::kQHalf >> 4) + 2 * k, bd + h * (L::kAtomBytes >> 4) + 2 * k, idesc_s, h != 0 || k != 0);
+              });
+              umma_commit(s_full + 8 * w);
+              umma_commit(k_empty + 8 * k_st);
+              if (j + stride == last) umma_commit(q_empty + 8 * slot);
+            }
+            __syncwarp();
+            ++k_at; next_k();
+            ++n_s;
+          }
           if (j < first) continue;
-          const uint32_t g = base + j;
-          if (!pass_v(g) || !chunk_wait(v_full + 8 * (g % NV), (g / NV) & 1u, abort_flag) || !chunk_wait(p_ready + 8 * w, n_p & 1u, abort_flag)) { ok = false; break; }
+          pass_v(j);
+          if (!ok || !chunk_wait(v_full + 8 * v_st, v_ph, abort_flag) || !chunk_wait(p_ready + 8 * w, n_p & 1u, abort_flag)) { ok = false; break; }
           ++n_p;
           tc_fence_after_sync();
           if (elect_one()) {
-            for_constant<NV>(g % NV, [&](auto c) {
+            for_constant<NV>(v_st, [&](auto c) {
               constexpr int V = decltype(c)::value;
               const uint64_t bd = make_smem_desc(smem_at + L::kVOff + V * L::kTileBytes, L::kAtomBytes, 1024, kSwizzle128B);
 #pragma unroll
               for (int ks = 0; ks < KEYS / 16; ++ks)             // 16 keys: 8 columns of P, 2 KB of V
                 umma_bf16_ts(tm_o, tm_p + ks * 8, bd + ks * (2048 >> 4), idesc_o, (j != first || ks != 0) ? 1u : 0u);
-              umma_commit(pv_done + 8 * w);
-              umma_commit(v_empty + 8 * V);
             });
+            umma_commit(pv_done + 8 * w);
+            umma_commit(v_empty + 8 * v_st);
           }
           __syncwarp();
-          v_at = g + 1;
-          if (alternate && j + 1 < n) ok = pass_v(g + 2);        // the other's values, as soon as they are there
+          ++v_at; next_v();
         }
-        ok = ok && pass_k(base + n) && pass_v(base + n);
-        base += n;
+        pass_k(n);
+        pass_v(n);
       }
       // the last hand-backs are asynchronous arrivals: in before the CTA ends
-      if (ok && w == 0) {
-        for (uint32_t e = base < NK ? 0 : base - NK; e < base && ok; ++e) ok = chunk_wait(k_empty + 8 * (e % NK), (e / NK) & 1u, abort_flag);
-        for (uint32_t e = base < NV ? 0 : base - NV; e < base && ok; ++e) ok = chunk_wait(v_empty + 8 * (e % NV), (e / NV) & 1u, abort_flag);
-        for (uint32_t e = qn < 2 ? 0 : qn - 2; e < qn && ok; ++e) ok = chunk_wait(q_empty + 8 * (e & 1u), (e >> 1) & 1u, abort_flag);
+      if (w == 0) {
+        for (int i = 0; i < NK && ok; ++i, next_k()) ok = chunk_wait(k_empty + 8 * k_st, k_ph ^ 1u, abort_flag);
+        for (int i = 0; i < NV && ok; ++i, next_v()) ok = chunk_wait(v_empty + 8 * v_st, v_ph ^ 1u, abort_flag);
+        for (int i = 0; i < 2 && ok; ++i, ++qn) ok = chunk_wait(q_empty + 8 * (qn & 1u), ((qn >> 1) & 1u) ^ 1u, abort_flag);
       }
     }
   } else if (warp < 8) {
@@ -718,7 +712,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
     };
     auto queries = [&](const ChunkItem& u, int t) {
       const uint32_t slot = qn & 1u;
-      constexpr int QBATCH = 4;
+      constexpr int QBATCH = 2;
       const int rows = min(u.n_tok - u.tok0 - t * p.tile_tokens, p.tile_tokens) * p.group;      // (what the rows behind hold does not matter)
       const uint16_t* const from = p.q + static_cast<long long>(u.q0 + u.tok0 + t * p.tile_tokens) * p.ld_q + u.head * p.group * HD + chunk * 16;
 #pragma unroll 1
@@ -747,7 +741,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
 #pragma unroll
           for (int d = 1; d < 4; d *= 2) m = max(m, __shfl_xor_sync(0xffffffffu, m, d));
           if constexpr (HD == 128) m = max(m, __shfl_xor_sync(0xffffffffu, m, 8));
-          const float mx = load16(static_cast<uint16_t>(m), p.fp16);
+          const float mx = load16(static_cast<uint16_t>(m), std::is_same_v<T, __half>);
           // the largest of the row to [2^14, 2^15) (fp16 ends at 65504), by an exponent of -126 to 126, so that both powers are normal numbers: what is
           // below 2^-39 of the row's largest is lost
           const int e = m != 0u ? min(max(static_cast<int>(__float_as_uint(mx) >> 23) - 127 - 14, -126), 126) : 0;
@@ -756,7 +750,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
           uint64_t y[8], sum2 = 0;
 #pragma unroll
           for (int b = 0; b < 8; ++b) {
-            y[b] = p.fp16 ? pack2(Pair16<__half>::lo(xw[b]), Pair16<__half>::hi(xw[b])) : pack2(Pair16<bf16>::lo(xw[b]), Pair16<bf16>::hi(xw[b]));
+            y[b] = pack2(Pair16<T>::lo(xw[b]), Pair16<T>::hi(xw[b]));
             y[b] = fmul2(y[b], down2);             // (exact, and so is its rounding to fp16 but for what is lost)
             sum2 = fadd2(sum2, y[b]);
           }
@@ -1002,7 +996,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
           for (int i = 0; i < 16; i += 8) {
             uint32_t z[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) z[e] = p.fp16 ? Pair16<__half>::pack(y[i + 2 * e], y[i + 2 * e + 1]) : Pair16<bf16>::pack(y[i + 2 * e], y[i + 2 * e + 1]);
+            for (int e = 0; e < 4; ++e) z[e] = Pair16<T>::pack(y[i + 2 * e], y[i + 2 * e + 1]);
             *reinterpret_cast<uint4*>(dst + c + i) = make_uint4(z[0], z[1], z[2], z[3]);
           }
         } else if (stored) {

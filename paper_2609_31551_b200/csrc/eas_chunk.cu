@@ -19,16 +19,16 @@ static size_t chunk_workspace(const eas_cache* c, int32_t max_new, int32_t n_hea
   return *cut_off + up256(c->sm_count * sizeof(ChunkItem));
 }
 
-template <int HD>
+template <int HD, typename T>
 static eas_status launch_chunk(const ChunkParams& p, int budget, bool all, cudaStream_t stream) {
   using L = ChunkCfg<HD>;
   static OncePerDevice once;
   if (once.first()) {
-    CUDA_TRY(cudaFuncSetAttribute(chunk_attention_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes));
+    CUDA_TRY(cudaFuncSetAttribute(chunk_attention_kernel<HD, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes));
     CUDA_TRY(cudaFuncSetAttribute(chunk_join_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, kOnePerSmSmem));
     once.settled();
   }
-  EAS_TRY(launch_kernel(chunk_attention_kernel<HD>, std::min(budget, p.n_ctas), L::kThreads, L::kBytes, stream, p));
+  EAS_TRY(launch_kernel(chunk_attention_kernel<HD, T>, std::min(budget, p.n_ctas), L::kThreads, L::kBytes, stream, p));
   return launch_kernel(chunk_join_kernel<HD>, std::min(budget, p.n_ctas), 512, all ? 0 : kOnePerSmSmem, stream, p);
 }
 
@@ -161,7 +161,8 @@ static eas_status chunk_attention(const eas_cache* c, const eas_cache_seqs* s, c
     p.table = s->block_table + first * s->ld_table;
     p.cu = s->cu_seqlens + first;
     p.seq_lens = s->seq_lens + first;
-    EAS_TRY(hd == 64 ? launch_chunk<64>(p, budget, all, st) : launch_chunk<128>(p, budget, all, st));
+    EAS_TRY(hd == 64 ? (p.fp16 ? launch_chunk<64, __half>(p, budget, all, st) : launch_chunk<64, bf16>(p, budget, all, st))
+                     : (p.fp16 ? launch_chunk<128, __half>(p, budget, all, st) : launch_chunk<128, bf16>(p, budget, all, st)));
   }
   return EAS_OK;
 }
