@@ -12,8 +12,8 @@ SMs, and the neighbour's own slow-down.
     python -m paper_2609_31551_b200.coresidency --config c1 --micro-batch 8
 
 `--neighbour` chooses what else a language model's workers would run there: `prompt`, the causal attention of a prefill batch (compute-bound
-like the matrix products, with bursts of K and V from L2), or `token`, the attention of a decoding step over 8-bit caches (bound by HBM, which no
-partition of the SMs divides).
+like the matrix products, with bursts of K and V from L2), `token`, the attention of a decoding step over 8-bit caches (bound by HBM, which no
+partition of the SMs divides), or `chunk`, the attention of a worker that does both: chunks of prompts and drafts of a few tokens over the same caches.
 
 The neighbour's kernels never wait for the encoder's or the reverse: they are independent launches on two streams."""
 from __future__ import annotations
@@ -87,6 +87,14 @@ class TokenNeighbour:
     """Decode attention: one token of each of `n` sequences (32 query heads, 8 key/value heads of 128) over its 8-bit cache."""
 
     def __init__(self, n: int = 64, tokens: int = 4096, block: int = 64):
+        self._fill(n, tokens, block)
+        self.q = torch.randn(n, 32, 128, device="cuda").bfloat16()
+        self.out = torch.empty_like(self.q)
+        self.workspace = torch.empty(self.cache.attention_workspace_bytes(n, 32), dtype=torch.uint8, device="cuda")
+        self.flops = 4.0 * 32 * 128 * n * tokens
+        torch.cuda.synchronize()
+
+    def _fill(self, n, tokens, block):
         from . import language as L
         blocks = tokens // block
         self.cache = L.KvCache(n * blocks, block, 8, 128)
@@ -94,14 +102,9 @@ class TokenNeighbour:
         self.cache.v.random_(-127, 128)
         self.cache.k_scale.fill_(0.03)
         self.cache.v_scale.fill_(0.03)
-        self.q = torch.randn(n, 32, 128, device="cuda").bfloat16()
-        self.out = torch.empty_like(self.q)
         self.lens = torch.full((n,), tokens, dtype=torch.int32, device="cuda")
         self.table = torch.randperm(n * blocks, device="cuda").to(torch.int32).view(n, blocks)
-        self.workspace = torch.empty(self.cache.attention_workspace_bytes(n, 32), dtype=torch.uint8, device="cuda")
-        self.flops = 4.0 * 32 * 128 * n * tokens
         self.stream = torch.cuda.Stream()
-        torch.cuda.synchronize()
 
     def enqueue(self, count: int, sm_budget: int):
         for _ in range(count):
@@ -111,7 +114,27 @@ class TokenNeighbour:
         self.cache.check()
 
 
-NEIGHBOURS = {"gemm": PrefillNeighbour, "prompt": PromptNeighbour, "token": TokenNeighbour}
+class ChunkNeighbour(TokenNeighbour):
+    """Chunk attention: `chunk` new tokens of the first sequence and four of each other one, over the same caches."""
+
+    def __init__(self, n: int = 32, tokens: int = 4096, block: int = 64, chunk: int = 1024):
+        self._fill(n, tokens, block)
+        new = [chunk] + [4] * (n - 1)
+        self.cu = torch.tensor(np.concatenate([[0], np.cumsum(new)]), dtype=torch.int32, device="cuda")
+        self.max_new = chunk
+        self.q = torch.randn(sum(new), 32, 128, device="cuda").bfloat16()
+        self.out = torch.empty_like(self.q)
+        self.workspace = torch.empty(self.cache.chunk_workspace_bytes(n, sum(new), chunk, 32), dtype=torch.uint8, device="cuda")
+        self.flops = 4.0 * 32 * 128 * sum(m * (tokens - m) + m * (m + 1) / 2 for m in new)
+        torch.cuda.synchronize()
+
+    def enqueue(self, count: int, sm_budget: int):
+        for _ in range(count):
+            self.cache.chunk_attention(self.q, self.cu, self.lens, self.table, max_new=self.max_new, out=self.out, workspace=self.workspace, sm_budget=sm_budget,
+                                       stream=self.stream)
+
+
+NEIGHBOURS = {"gemm": PrefillNeighbour, "prompt": PromptNeighbour, "token": TokenNeighbour, "chunk": ChunkNeighbour}
 
 
 def _encode_ms(enc, batch, sm_budget, reps, stream):

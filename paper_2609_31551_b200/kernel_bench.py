@@ -6,8 +6,10 @@
     python -m paper_2609_31551_b200.kernel_bench prompt --lens 2048x8 --heads 32 --kv-heads 8 --head-dim 128 --before 0
     python -m paper_2609_31551_b200.kernel_bench token --lens 4096x64 --heads 32 --kv-heads 8 --head-dim 128 --block 64
     python -m paper_2609_31551_b200.kernel_bench store --lens 2048x8 --kv-heads 8 --head-dim 128 --block 64      (or load)
+    python -m paper_2609_31551_b200.kernel_bench chunk --lens 4096x64 --new 4 --heads 32 --kv-heads 8 --head-dim 128 --block 64
+    python -m paper_2609_31551_b200.kernel_bench append --lens 2048x8 --before 0 --heads 32 --kv-heads 8 --head-dim 128 --block 64      (or rotate)
 
-Prints one JSON line per run: milliseconds per launch and TFLOP/s (GEMM, attention, prompt) or GB/s (norm, token, store, load)."""
+Prints one JSON line per run: milliseconds per launch and TFLOP/s (GEMM, attention, prompt, chunk) or GB/s (norm, token, chunk, store, load, append, rotate)."""
 from __future__ import annotations
 import argparse
 import json
