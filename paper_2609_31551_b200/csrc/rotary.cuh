@@ -214,7 +214,7 @@ struct AppendParams {
   int early_launch;
 };
 
-constexpr int kAppendThreads = 256, kAppendCtas = 2, kAppendSteps = 2, kAppendBatch = 2;      // CTAs an SM (three spill registers)
+constexpr int kAppendThreads = 256, kAppendCtas = 2, kAppendSteps = 2, kAppendBatch = 4;      // CTAs an SM (three spill registers)
 
 // An item's 16 values, word by word as rotary_turn_word leaves them, to its two chunks of eight numbers, as quantise8 does it.  order: of a word's four bytes, first
 // values before second ones or pair by pair
@@ -268,26 +268,8 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendCtas) cache_append_kern
   auto cu = [&](int i) { return min(max(p.s.cu[i], 0), p.r.n_rows); };
   const int pair_items = p.pairs * p.head_parts;
   const uint32_t q_units = static_cast<uint32_t>(p.r.n_heads > 0 ? p.r.n_rows : 0) * p.q_parts;
-  const uint32_t items = pair_items + (q_units + kAppendThreads / 32 - 1) / (kAppendThreads / 32);
-  for (uint32_t it = blockIdx.x; it < items; it += gridDim.x) {
-    if (it >= static_cast<uint32_t>(pair_items)) {
-      const uint32_t u = (it - pair_items) * (kAppendThreads / 32) + warp;
-      __syncthreads();                                             // (the table in shared memory is no longer read)
-      if (u >= q_units) continue;
-      const int row = static_cast<int>(u / p.q_parts), head0 = static_cast<int>(u - row * p.q_parts) * p.q_part_heads;
-      if (row < cu(0) || row >= cu(p.s.n_seqs)) continue;
-      int position[2] = {0, 0};
-      if (p.r.positions == nullptr) {
-        const int s = last_sequence(p.s.n_seqs, row, cu);
-        position[0] = position[1] = static_cast<int>(static_cast<uint32_t>(p.s.start[s]) + static_cast<uint32_t>(row - cu(s)));
-      } else {
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          if (q_pair[i].at >= 0) position[i] = p.r.positions[q_pair[i].axis * p.r.ld_positions + row];
-      }
-      rotary_row<HD, kAppendBatch, T>(p.t, p.r, q_pair, row, head0, min(head0 + p.q_part_heads, p.r.n_heads), position, append_turns + warp * kRotaryMaxPairs);
-      continue;
-    }
+  uint32_t it = blockIdx.x;
+  for (; it < static_cast<uint32_t>(pair_items); it += gridDim.x) {
     const int pair = static_cast<int>(it) / p.head_parts, part = static_cast<int>(it) - pair * p.head_parts;
     const CacheRun r = cache_run_of(p.c, p.s, last_sequence(p.s.n_seqs, pair, [&](int i) { return (cu(i) >> p.c.bs_log2) + 2 * i; }), p.r.n_rows, pair, p.status,
                                     threadIdx.x == 0 && part == 0);
@@ -417,6 +399,36 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendCtas) cache_append_kern
         if (tid == 0) *scale = s;
       }
     }
+  }
+  if (q_units == 0) return;
+  __syncthreads();                                                 // (the table in shared memory is no longer read)
+  // Queries.  Positions are read one unit ahead, as in rotary_kernel
+  const int row_first = cu(0), row_end = cu(p.s.n_seqs);
+  constexpr uint32_t kWarps = kAppendThreads / 32;
+  auto position_of = [&](uint32_t u, int (&position)[2]) {
+    position[0] = position[1] = 0;
+    if (u >= q_units) return;
+    const int row = static_cast<int>(u / p.q_parts);
+    if (p.r.positions != nullptr) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (q_pair[i].at >= 0) position[i] = p.r.positions[q_pair[i].axis * p.r.ld_positions + row];
+    } else {
+      const int s = last_sequence(p.s.n_seqs, row, cu);
+      position[0] = position[1] = static_cast<int>(static_cast<uint32_t>(p.s.start[s]) + static_cast<uint32_t>(row - cu(s)));
+    }
+  };
+  uint32_t u = (it - pair_items) * kWarps + warp;
+  int position[2];
+  position_of(u, position);
+  for (; u < q_units; u += gridDim.x * kWarps) {
+    int next[2];
+    position_of(u + gridDim.x * kWarps, next);
+    const int row = static_cast<int>(u / p.q_parts), head0 = static_cast<int>(u - row * p.q_parts) * p.q_part_heads;
+    if (row >= row_first && row < row_end)
+      rotary_row<HD, kAppendBatch, T>(p.t, p.r, q_pair, row, head0, min(head0 + p.q_part_heads, p.r.n_heads), position, append_turns + warp * kRotaryMaxPairs);
+    position[0] = next[0];
+    position[1] = next[1];
   }
 }
 
