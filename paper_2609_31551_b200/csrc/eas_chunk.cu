@@ -33,9 +33,15 @@ static eas_status launch_chunk(const ChunkParams& p, int budget, bool all, cudaS
 }
 
 // ------------------------------------------------------------------------------------ few rows
-// Up to so many query rows a key/value head (new tokens times heads of the group) a sequence goes to the kernels of single tokens: of 402 MB of cache (48 sequences of
-// 4096 tokens, 8 key/value heads of 128) they take 76 us for 8 rows, 96 for 16 and 180 for 32, the tiles of 128 rows 183 for 16 and 195 for 36.
+// Up to so many query rows a key/value head (new tokens times heads of the group) a sequence goes to the kernels of single tokens, which read the cache once for every 16 of
+// them, rather than to the tiles of 128 rows.  In us, these kernels and the tiles, back to back, 8 key/value heads of 128: 48 sequences of 4096 tokens with 8
+// rows 77 and 133, with 16 rows 96 and 133; of 32 rows, 64 sequences of 500 57 and 70, 4 of 4096 25 and 31, one of 700 12.5 and 18.7; 48 of 2048 (16 heads of 64) 125 and 141.
 constexpr int kFewRows = 32;
+// But with more than 16 rows and heads of 128 the second reading is dear where the cache does not fit L2 (126 MB): 32 rows of 48 sequences of 4096 tokens take 180 and 134,
+// of 2 of 65536 112 and 91.  How long the sequences are is known on the device alone; the width of the table stands for it.  And most of them must have more than 16 rows: 1
+// to 8 tokens of 4 heads (18 rows on average) behind 8192 134 and 165.
+constexpr int64_t kFewBytes = 128 << 20;
+constexpr int kFewAverage = 20;
 
 static int few_columns(int rows) { return rows <= 8 ? 8 : 16; }
 static size_t few_workspace(const eas_cache* c, int rows, size_t* o_off) {
@@ -66,17 +72,18 @@ struct ChunkPlan {
   int few_rows = 0;            // most rows a key/value head of the sequences that the kernels for few rows take
   bool tiles = false;
 };
-static ChunkPlan chunk_plan(int32_t n_seqs, int32_t n_rows, int32_t max_new, int group) {
+static ChunkPlan chunk_plan(const eas_cache* c, int32_t n_seqs, int32_t n_rows, int32_t max_new, int group, int64_t places) {
   ChunkPlan plan;
-  const int64_t most = static_cast<int64_t>(max_new) * group;
-  plan.tiles = most > kFewRows;
+  const int64_t most = static_cast<int64_t>(max_new) * group, token_bytes = 2LL * c->d.n_kv_heads * c->d.head_dim;
+  plan.tiles = most > kFewRows || (most > 16 && c->d.head_dim == 128 && static_cast<int64_t>(n_rows) * group >= static_cast<int64_t>(n_seqs) * kFewAverage &&
+                                   n_seqs * places >= kFewBytes / token_bytes);
   if (!plan.tiles) plan.few_rows = static_cast<int>(std::max<int64_t>(most, 1));
   else if (group <= kFewRows && static_cast<int64_t>(n_rows) * 2 < static_cast<int64_t>(n_seqs) * max_new) plan.few_rows = kFewRows;
   return plan;
 }
 
-// the kernels of a call run one behind the other: they share the scratch
-static size_t chunk_workspace_bytes(const eas_cache* c, const ChunkPlan& plan, int32_t n_rows, int32_t max_new, int32_t n_heads) {
+// The kernels of a call run one behind the other: they share the scratch.
+static size_t plan_workspace(const eas_cache* c, const ChunkPlan& plan, int32_t n_rows, int32_t max_new, int32_t n_heads) {
   int ws_rows = 0;
   size_t a = 0, b = 0, bytes = 256;
   if (plan.few_rows > 0) bytes = std::max(bytes, few_workspace(c, plan.few_rows, &a));
@@ -102,12 +109,12 @@ static eas_status chunk_attention(const eas_cache* c, const eas_cache_seqs* s, c
   const int64_t w = static_cast<int64_t>(n_heads) * hd;
   if (ld_q < w || ld_out < w || ld_q % 8 != 0 || ld_out % 8 != 0)
     return fail(EAS_ERR_INVALID_ARG, "token distances must be multiples of 8 that hold a token's heads");
-  const ChunkPlan plan = chunk_plan(s->n_seqs, n_rows, max_new, group);
-  const size_t need = chunk_workspace_bytes(c, plan, n_rows, max_new, n_heads);
-  if (workspace_bytes < need) return fail(EAS_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, need);
-  if ((reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return fail(EAS_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
   const int64_t places = static_cast<int64_t>(s->max_blocks) * c->d.block_size;
   if (places > (1LL << 30)) return fail(EAS_ERR_UNSUPPORTED, "max_blocks %d: more than 2^30 places a sequence", s->max_blocks);
+  const ChunkPlan plan = chunk_plan(c, s->n_seqs, n_rows, max_new, group, places);
+  const size_t need = plan_workspace(c, plan, n_rows, max_new, n_heads);
+  if (workspace_bytes < need) return fail(EAS_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, need);
+  if ((reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return fail(EAS_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
   if (static_cast<int64_t>(n_rows) * n_heads > 0x7fffffffLL) return fail(EAS_ERR_UNSUPPORTED, "too many rows for one call");
   const bool all = budget == c->sm_count;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -176,7 +183,11 @@ extern "C" size_t eas_cache_chunk_workspace_bytes(const eas_cache* cache, int32_
     fail(EAS_ERR_UNSUPPORTED, "%d query heads per key/value head (at most 128)", n_heads / cache->d.n_kv_heads);
     return 0;
   }
-  return chunk_workspace_bytes(cache, chunk_plan(n_seqs, n_rows, max_new, n_heads / cache->d.n_kv_heads), n_rows, max_new, n_heads);
+  // for a table of any width
+  size_t bytes = 0;
+  for (const int64_t places : {int64_t{0}, int64_t{1} << 30})
+    bytes = std::max(bytes, plan_workspace(cache, chunk_plan(cache, n_seqs, n_rows, max_new, n_heads / cache->d.n_kv_heads, places), n_rows, max_new, n_heads));
+  return bytes;
 }
 
 extern "C" eas_status eas_cache_chunk_attention(const eas_cache* cache, const eas_cache_seqs* seqs, const void* q, int64_t ld_q, void* out, int64_t ld_out,

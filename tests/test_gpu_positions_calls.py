@@ -161,6 +161,23 @@ def test_shapes_as_they_come():
         _check_chunk(_cache(numbers, scales), numbers, scales, q, _cu(lens), held, table, max_new=(high, None, high + 5)[i % 3])
 
 
+@pytest.mark.parametrize("hd,dtype", [(128, BF), (128, FP), (64, BF)])
+@pytest.mark.parametrize("lens", [[5] * 6, [8, 8, 7, 8, 0, 8], [6, 1, 5, 5, 8, 5]])
+def test_drafts_behind_a_table_of_any_width(hd, dtype, lens):
+    """The width of the table, of which most is not used, may choose other kernels; a workspace of the stated size does for all."""
+    H, G, bs = 8, 2, 16
+    held = [n + b for n, b in zip(lens, (700, 0, 90, 33, 5, 1500))]
+    narrow, n_blocks = _table(91, held, bs)
+    numbers, scales = _filled(n_blocks, G, bs, hd, 92)
+    q = _rand((sum(lens), H, hd), dtype, 93, 2.0)
+    c = _cache(numbers, scales)
+    workspace = torch.empty(c.chunk_workspace_bytes(len(lens), sum(lens), max(lens), H), dtype=torch.uint8, device="cuda")
+    for width in (narrow.shape[1], 4096, 40000):
+        table = torch.full((len(lens), width), -7, dtype=torch.int32)
+        table[:, :narrow.shape[1]] = narrow
+        _check_chunk(c, numbers, scales, q, _cu(lens), held, table, max_new=max(lens), workspace=workspace)
+
+
 def test_coresidency_with_chunks_beside_the_encoder():
     from paper_2609_31551_b200 import coresidency
     rows = coresidency.measure("c0", 2, levels=(0.5,), reps=2, neighbour="chunk")
