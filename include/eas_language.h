@@ -121,7 +121,8 @@ eas_status eas_cache_attention(const eas_cache* cache, const eas_cache_seqs* seq
  * n_rows: rows of q that exist (a bound on cu_seqlens).  max_new: the most new tokens that a sequence has (n_rows does, too; a smaller number chooses
  * kernels for few rows): a sequence with more is not computed and raises the status word to EAS_DEVICE_CACHE_RANGE.
  * workspace: device scratch of eas_cache_chunk_workspace_bytes() (0 on bad arguments), 256-byte aligned; its contents do not matter and nothing of it is used
- * by a later call, but calls that may run at the same time need one each. */
+ * by a later call, but calls that may run at the same time need one each.
+ * Limits (UNSUPPORTED): 128 query heads a key/value head, 2^30 places a sequence (max_blocks * block_size), n_rows * n_heads below 2^31. */
 size_t eas_cache_chunk_workspace_bytes(const eas_cache* cache, int32_t n_seqs, int32_t n_rows, int32_t max_new, int32_t n_heads);
 eas_status eas_cache_chunk_attention(const eas_cache* cache, const eas_cache_seqs* seqs, const void* q, int64_t ld_q, void* out, int64_t ld_out,
                                      int32_t n_rows, int32_t max_new, int32_t n_heads, int32_t dtype, float scale, void* workspace, size_t workspace_bytes,

@@ -24,6 +24,9 @@
 // More than 16 query heads a key/value head are rows of tiles of their own, so the cache is read once for every 16 of them, from L2 where it fits:
 // 8 caches of 16384 tokens with 2 key/value heads of 128 take 20 us for 8 query heads each, 24 for 12 or 16, 36 for 32, 60 for 64.
 //
+// Several new tokens a sequence (CHUNK): their heads are the columns, up to 32 of them here; a column sees the places up to its own token's.  48 sequences of 4096 tokens, 32 and 8
+// heads of 128: 75 us with one token, 77 with 2 (8 columns), 96 with 4 (16: two thirds more instructions a tile, 8 warps an SM instead of 12; with 10 to 12 registers spill, 101 to 109).
+//
 // Measured, back to back in a graph, both launches: 8 caches of 24000 to 65536 tokens (64 heads, 8 of keys and values, of 128) 109 us, 93 % of the copy rate (113
 // to 121 among other calls); 48 of up to 8192 (32 and 8 heads of 128) 19.5, of them 9 for the bytes and the rest the chain from the lengths to the first
 // tile; 128 of 500 to 3500 (16 heads of 64, one query head each) 90, 69 %: 900 instructions a tile of 64 tokens, three warps a scheduler.  The join is 2 us of it.

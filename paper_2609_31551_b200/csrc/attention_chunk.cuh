@@ -1,24 +1,38 @@
 // Attention of several new tokens a sequence over the 8-bit cache, on tcgen05 tensor cores: out = softmax(scale q K^T) V, the new tokens being the
 // last of their sequence.
 //
-// The query heads that share a key/value head are rows of one matrix, 128 / group tokens a tile of 128 rows, as in attention_prompt.cuh; the numbers of the
-// cache enter as they are, exact in fp16, as in attention_cache.cuh: queries are fp16 times a power of two per row, a block's key scale multiplies its scores in
-// fp32, its value scale v is an exponent: with t = score + log2 v and w = 2^(t - m),  out = sum w number / sum w / v, m being kept 2^7 to 2^15 below the largest t.
+// The query heads that share a key/value head are rows of one matrix, 128 / group tokens a tile of 128 rows, as in attention_prompt.cuh; the numbers of the cache
+// enter exact in fp16 as in attention_cache.cuh: queries are fp16 times a power of two per row, a block's key scale multiplies its scores in fp32, its value scale v
+// is an exponent: with t = score + log2 v and w = 2^(t - m),  out = sum w number / sum w / v, m being kept 2^7 to 2^15 below the largest t.
 //
 //   warps 0, 3    bytes of K and of V, a block's tokens of a head (they are contiguous) a bulk copy, into rings of 8-bit tiles; warp 0 the scales of the steps, too, and
-//                 warp 3 walks the line of units (below) and tells the others the items of the CTA, through a ring
+//                 warp 3 walks the line of units (below) and tells the others the items of the CTA, through a ring.  (One warp for both took 1100 cycles a copy and was what
+//                 long caches of few rows waited for.)
 //   warps 1, 2    UMMA issuers, one per softmax warpgroup
-//   warps 4 ..    converters: tiles of queries, then two warps those of K and two those of V, from bytes to fp16 in the tensor core's layout.  (0x6400 | (byte ^ 0x80)) - 1152: one logic operation and
-//                 one subtraction for the bytes 0 and 2 of a word, a shift more for 1 and 3; so four dimensions lie in the order 0, 2, 1, 3, in the queries and the output too
+//   warps 4 ..    converters: tiles of queries, then two warps those of K and two those of V, from bytes to fp16 in the tensor core's layout.  Keys: byte ^ 0x80 as the bits of an
+//                 fp16 number is (number + 128) 2^-24, two bytes by one and-xor; the row's factor makes up for 2^-24 and its offset for the 128 (exact: products and sums are
+//                 fp32).  Values: (0x6400 | (byte ^ 0x80)) - 1152, a subtraction more.  Bytes 0 and 2 of a word, then 1 and 3: four dimensions lie in the order 0, 2, 1,
+//                 3, in the queries and the output too
 //   warps 8 ..    two softmax warpgroups, one thread a row
 //
-// A step is 80 keys.  A unit of two tiles of one key/value head (shared) brings each K and V tile to both warpgroups; a unit of one tile gives its steps to the
-// warpgroups in turn (alternate), which put their results together at its end: O lies in tensor memory, where the lanes of both can read it.  So two steps are in
-// flight whether there are many rows (bound by the pipes) or few (bound by the bytes).
+// A step is 80 keys: 5 parts of 16, the smallest block, and as many scores as a thread's registers hold beside their weights.  A unit of two tiles of one key/value head
+// (shared) brings each K and V tile to both warpgroups; a unit of one tile gives its steps to the warpgroups in turn (alternate), which put their results together at its
+// end: O lies in tensor memory, where the lanes of both can read it.  So two steps are in flight whether there are many rows (bound by the pipes) or few (bound by the
+// conversion of the bytes).
 //
 // The units of all sequences and heads form a line, in tokens seen times tiles, cut into one equal piece an SM (a function of the shapes and the device, not of sm_budget).  A
 // piece is the end of a unit, whole units, the beginning of one; cut units leave (m, l, O) in the workspace, and chunk_join_kernel puts them together in order.
 // Lengths are read on the device: each CTA sums them up itself.
+//
+// Measured, back to back in a graph, both launches, 32 and 8 heads of 128 unless stated: two chunks of 2048 tokens behind 14336 1.00 to 1.06 ms, 970 to 1020 TFLOP/s (the kernel for
+// prompts, whose keys and values are 16-bit, 0.89; behind 30720 2.05 to 2.2); 512 of 40 and 8 heads behind 11801 166 (prompts: 155); 12 sequences of 16384 with 16
+// new tokens 128, 3.1 TB/s; 12 prompts of 600 tokens, 16 heads of 64, 91 to 100.
+// Many rows: a step of both tiles takes 2900 cycles, of which the tensor pipe is busy 49 %, the special functions 50 %, the ALUs 43 %, the issue slots 52 %: the chain of a
+// step (scores read 190, weighed 1700, P stored 200, waits the rest) with two warps a scheduler.  Few rows: 1700 cycles a step, a pair of warps converting keys (1200 and
+// its waits).  Short sequences: 16 cycles an instruction, 4.9 of them for instructions (7.2 when the code of all roles was 124 KB and not 97) and 5.7 for memory and
+// tensor memory: a CTA begins and ends units all the time, and its first scores come 13 us after its start (lengths 1.5, the first item 2, block numbers 1, bytes 1.5, two tiles of
+// queries 2 to 4 each).
+// Rings of converted tiles: three of values, since the warpgroups are up to two steps apart (with two, 1.09 ms for the chunks of 2048 and 166 us for the 12 sequences).
 #pragma once
 #include <type_traits>
 

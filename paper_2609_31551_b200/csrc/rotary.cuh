@@ -5,6 +5,14 @@
 // fp32 loses the angles of far positions (a position of 700000 is known to 0.03 rad), fp64 costs 64 times as much.  So angles are whole numbers: with
 // F = round(inv_freq / 2 pi * 2^64), position * F mod 2^64 is the angle in turns of 2^-64, exactly but for the rounding of F, which a position below 2^31
 // makes 2^-34 turns.  Of those the upper 32 bits count.
+//
+// Alone, the rotation is a copy: a warp takes a token's heads, 32 bytes a lane and head, 16 heads of 128 (32 of 64) in flight; cosines and sines are worked out once a
+// token (64 pairs, two a lane) into 512 bytes of shared memory.  16384 tokens of 32 and 8 heads of 128 54.6 us, 6.14 TB/s, 94 % of the copy rate; 6 prompts of 6227 tokens
+// 23.7; 40 tokens 2.3 (one launch).
+// On the way into the cache (append), a block's run of new rows has its cosines worked out once for all heads (8 bytes a pair and row of shared memory, 32 KB for 64 rows of
+// 64 pairs), is read once, rotated in fp32 and rounded once, to its number; queries go warp by warp behind.  16384 tokens 88 us, 4.2 TB/s (a launch of its own for the queries: 93; rotation and
+// storing as two operators, with the rotated keys through memory: 86, less exact), 6 prompts of 6227 tokens 43, 64 single tokens 7.8.  Of the 88, 50 are keys and
+// values: a group of threads goes from head to head in series, 16 warps an SM (registers), and waits for loads 3 of 9 cycles an instruction.
 #pragma once
 #include <type_traits>
 
@@ -214,7 +222,7 @@ struct AppendParams {
   int early_launch;
 };
 
-constexpr int kAppendThreads = 256, kAppendCtas = 2, kAppendSteps = 2, kAppendBatch = 4;      // CTAs an SM (three spill registers)
+constexpr int kAppendThreads = 256, kAppendCtas = 2, kAppendSteps = 2, kAppendBatch = 4;      // CTAs an SM (three spill registers); rows a thread, of keys or values; heads a lane has in flight, of queries
 
 // An item's 16 values, word by word as rotary_turn_word leaves them, to its two chunks of eight numbers, as quantise8 does it.  order: of a word's four bytes, first
 // values before second ones or pair by pair

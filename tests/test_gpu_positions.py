@@ -2,8 +2,9 @@
 
 Bounds.  u = eps / 2 of the data type is the largest relative error of one rounding to it (bf16 2^-8, fp16 2^-11).
 Rotation, y = s (a cos - b sin):
-  - the angle: cut to 2^-32 turns and rounded to fp32 (2^-25 of a half turn), so below pi (2^-25 + 2^-31) + 2^-33 < 2^-23.3; sincospif: 2 ulp, 2^-23 of a value
-    up to 1.  Together below 2^-22 for a cosine or sine, twice that with its product by s, the two products and the difference (2^-24 of a term each):
+  - the angle: cut to 2^-32 turns and rounded to fp32 (2^-25 of a half turn), so below pi (2^-25 + 2^-31) + 2^-33 < 2^-23.3; its cosine or sine: cut off below
+    2^-25, 2^-25 for the last rounding (of a value up to 1) and less for those before it, 2^-23.  Together below 2^-22 for a cosine or sine, twice that with its
+    product by s, the two products and the difference (2^-24 of a term each):
                                                                                                  2^-21 s (|a| + |b|)
   - the output is rounded once: u |y|, and half of 2^-24 where fp16 has no more bits.
 Numbers of the cache: half a step of the scale, and the rotation's error; the scale: that error and 2^-23 of itself.  Kept numbers, rounded again: half a step of the new one.
