@@ -29,7 +29,7 @@
 // new tokens 128, 3.1 TB/s; 12 prompts of 600 tokens, 16 heads of 64, 91 to 100.
 // Many rows: a step of both tiles takes 2900 cycles, of which the tensor pipe is busy 49 %, the special functions 50 %, the ALUs 43 %, the issue slots 52 %: the chain of a
 // step (scores read 190, weighed 1700, P stored 200, waits the rest) with two warps a scheduler.  Few rows: 1700 cycles a step, a pair of warps converting keys (1200 and
-// its waits).  Short sequences: 16 cycles an instruction, 4.9 of them for instructions (7.2 when the code of all roles was 124 KB and not 97) and 5.7 for memory and
+// its waits), with shared memory busy for some 1200 of them (bytes in 160, read and written as fp16 480, operands of the two products 580).  Short sequences: 16 cycles an instruction, 4.9 of them for instructions (7.2 when the code of all roles was 124 KB and not 97) and 5.7 for memory and
 // tensor memory: a CTA begins and ends units all the time, and its first scores come 13 us after its start (lengths 1.5, the first item 2, block numbers 1, bytes 1.5, two tiles of
 // queries 2 to 4 each).
 // Rings of converted tiles: three of values, since the warpgroups are up to two steps apart (with two, 1.09 ms for the chunks of 2048 and 166 us for the 12 sequences).

@@ -178,6 +178,30 @@ def test_drafts_behind_a_table_of_any_width(hd, dtype, lens):
         _check_chunk(c, numbers, scales, q, _cu(lens), held, table, max_new=max(lens), workspace=workspace)
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("H,G,lens,before", [(128, 1, [3, 1, 9], [40, 700, 0]), (100, 1, [2, 5], [333, 80]), (130, 2, [70], [100]), (64, 64, [1, 129, 2], [500, 31, 0]),
+                                             (24, 24, [33, 300], [0, 1000])])
+def test_groups_of_all_sizes(hd, H, G, lens, before):
+    held = [a + b for a, b in zip(lens, before)]
+    table, n_blocks = _table(101, held, 32)
+    numbers, scales = _filled(n_blocks, G, 32, hd, 102)
+    q = _rand((sum(lens), H, hd), BF, 103, 2.0)
+    c = _cache(numbers, scales)
+    _check_chunk(c, numbers, scales, q, _cu(lens), held, table, max_new=max(lens))
+    _check_chunk(c, numbers, scales, q, _cu(lens), held, table)
+
+
+@pytest.mark.parametrize("lens,before", [([4], [700]), ([40, 3], [900, 0])])
+def test_a_step_with_queries_turned_in_place(lens, before):
+    j = Job(111, lens, before)
+    ref = j.result(j.run())
+    j.reset()
+    q = j.q.clone()
+    assert j.cache.append(q, j.k, j.v, j.cu, j.before, j.table, j.rotary, j.positions, out=q) is q
+    out = j.cache.chunk_attention(q, j.cu, j.held, j.table, max_new=j.max_new)
+    assert all(torch.equal(a, b) for a, b in zip(j.result(out), ref))
+
+
 def test_coresidency_with_chunks_beside_the_encoder():
     from paper_2609_31551_b200 import coresidency
     rows = coresidency.measure("c0", 2, levels=(0.5,), reps=2, neighbour="chunk")
