@@ -178,6 +178,19 @@ def test_drafts_behind_a_table_of_any_width(hd, dtype, lens):
         _check_chunk(c, numbers, scales, q, _cu(lens), held, table, max_new=max(lens), workspace=workspace)
 
 
+@pytest.mark.parametrize("H,G", [(8, 2), (16, 2), (9, 1), (2, 2)])
+@pytest.mark.parametrize("lens", [[70, 1, 1, 1, 1], [70, 1, 1, 0, 1, 1], [70, 3, 0, 0, 1], [70, 2, 1, 1, 1], [70]])
+def test_a_chunk_beside_single_tokens_and_drafts(H, G, lens):
+    before = [300, 900, 0, 31, 64, 1000][:len(lens)]
+    held = [a + b for a, b in zip(lens, before)]
+    table, n_blocks = _table(121, held, 16)
+    numbers, scales = _filled(n_blocks, G, 16, 128, 122)
+    q = _rand((sum(lens), H, 128), BF, 123, 2.0)
+    c = _cache(numbers, scales)
+    _check_chunk(c, numbers, scales, q, _cu(lens), held, table, max_new=70)
+    _check_chunk(c, numbers, scales, q, _cu(lens), held, table)
+
+
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("H,G,lens,before", [(128, 1, [3, 1, 9], [40, 700, 0]), (100, 1, [2, 5], [333, 80]), (130, 2, [70], [100]), (64, 64, [1, 129, 2], [500, 31, 0]),
                                              (24, 24, [33, 300], [0, 1000])])
