@@ -47,6 +47,7 @@ constexpr int kChunkKeys = 80, kChunkParts = kChunkKeys / 16;
 constexpr int kChunkUnitCost = 160;      // of a unit's beginning and end, in tokens of one tile
 constexpr int kChunkLeastCost = 320;     // of a piece
 constexpr int kChunkItems = 4;           // items that the roles may be apart
+constexpr int kChunkMaxPieces = 1024;    // SMs of a device, at most
 
 struct ChunkItem;
 struct ChunkParams {
@@ -1056,11 +1057,29 @@ __global__ void __launch_bounds__(512, 1) chunk_join_kernel(const __grid_constan
   }
   pdl_wait();
   if (p.early_launch) pdl_launch_dependents();
+  // the pieces that a unit's first cut ends, listed by each CTA
+  __shared__ int cuts[kChunkMaxPieces], counts[16];
+  const int warp = threadIdx.x >> 5;
+  int n_cuts = 0;
+  for (int piece0 = 0; piece0 < p.n_ctas; piece0 += 512) {
+    const int piece = piece0 + static_cast<int>(threadIdx.x);
+    const bool has = piece < p.n_ctas && p.cut_ws[piece].n != 0;
+    const uint32_t with = __ballot_sync(0xffffffffu, has);
+    if (lane == 0) counts[warp] = __popc(with);
+    __syncthreads();
+    int at = n_cuts;
+    for (int w = 0; w < 16; ++w) {
+      if (w < warp) at += counts[w];
+      n_cuts += counts[w];
+    }
+    if (has) cuts[at + __popc(with & ((1u << lane) - 1u))] = piece;
+    __syncthreads();
+  }
   const int row = threadIdx.x & 127, row_tok = chunk_row_token(p, row), row_head = row - row_tok * p.group;
-  for (int it = blockIdx.x * 4 + (threadIdx.x >> 7); it < p.n_ctas * 2 * CHUNKS; it += gridDim.x * 4) {
-    const int sub = it / p.n_ctas, piece = it - sub * p.n_ctas, t = sub / CHUNKS, col0 = sub % CHUNKS * COLS;      // (few pieces have a first cut: they are spread over the CTAs)
+  for (int it = blockIdx.x + (threadIdx.x >> 7) * gridDim.x; it < n_cuts * 2 * CHUNKS; it += gridDim.x * 4) {      // (few of them: spread over the CTAs)
+    const int piece = cuts[it / (2 * CHUNKS)], t = it / CHUNKS & 1, col0 = it % CHUNKS * COLS;
     const ChunkItem& u = p.cut_ws[piece];
-    if (u.n == 0 || t >= u.tiles) continue;
+    if (t >= u.tiles) continue;
     const int tok = u.tok0 + t * p.tile_tokens + row_tok, parts = u.parts;
     if (row_tok >= p.tile_tokens || tok >= u.n_tok) continue;
     float m = -INFINITY, l = 0.f, acc[COLS];

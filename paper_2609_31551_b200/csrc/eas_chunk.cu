@@ -152,6 +152,7 @@ static eas_status chunk_attention(const eas_cache* c, const eas_cache_seqs* s, c
     }
   }
   if (!plan.tiles) return EAS_OK;
+  if (c->sm_count > kChunkMaxPieces) return fail(EAS_ERR_ARCH, "%d SMs (at most %d)", c->sm_count, kChunkMaxPieces);
   ChunkParams p{};
   size_t ml_off = 0, cut_off = 0;
   chunk_workspace(c, std::min(max_new, n_rows), n_heads, &p.ws_rows, &ml_off, &cut_off);
