@@ -25,7 +25,7 @@
 // Lengths are read on the device: each CTA sums them up itself.
 //
 // Measured, back to back in a graph, both launches, 32 and 8 heads of 128 unless stated: two chunks of 2048 tokens behind 14336 1.00 to 1.06 ms, 970 to 1020 TFLOP/s (the kernel for
-// prompts, whose keys and values are 16-bit, 0.89; behind 30720 2.05 to 2.2); 512 of 40 and 8 heads behind 11801 166 (prompts: 155); 12 sequences of 16384 with 16
+// prompts, whose keys and values are 16-bit, 0.89; behind 30720 2.05 to 2.25); 512 of 40 and 8 heads behind 11801 160 to 167 (prompts: 155 to 164); 64 tokens behind 16320 44; 12 sequences of 16384 with 16
 // new tokens 128, 3.1 TB/s; 12 prompts of 600 tokens, 16 heads of 64, 91 to 100.
 // Many rows: a step of both tiles takes 2900 cycles, of which the tensor pipe is busy 49 %, the special functions 50 %, the ALUs 43 %, the issue slots 52 %: the chain of a
 // step (scores read 190, weighed 1700, P stored 200, waits the rest) with two warps a scheduler.  Few rows: 1700 cycles a step, a pair of warps converting keys (1200 and
@@ -1042,7 +1042,8 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
 }
 
 // The parts of cut units put together, in order: 128 threads, one a row, per (first cut of a unit, tile, 8 columns).  Before that, beside the end of the kernel
-// that leaves them, the rows that see nothing.
+// that leaves them, the rows that see nothing.  Bound by the latency of three rounds of loads, eight parts at once, and by the parts' bytes where all SMs leave some: with 8 units in 18 pieces
+// each, 64 tokens behind 16320, the call takes 44 us (68 when a group of threads met the same piece in every round, and all its columns were its own).  (Four parts at once, or two CTAs an SM: 37 -> 42 to 45 for one unit of 148 pieces, the others within 2 %.)
 template <int HD>
 __global__ void __launch_bounds__(512, 1) chunk_join_kernel(const __grid_constant__ ChunkParams p) {
   constexpr int COLS = 8, CHUNKS = HD / COLS, BATCH = 8;

@@ -35,10 +35,10 @@ static eas_status launch_chunk(const ChunkParams& p, int budget, bool all, cudaS
 // ------------------------------------------------------------------------------------ few rows
 // Up to so many query rows a key/value head (new tokens times heads of the group) a sequence goes to the kernels of single tokens, which read the cache once for every 16 of
 // them, rather than to the tiles of 128 rows.  In us, these kernels and the tiles, back to back, 8 key/value heads of 128: 48 sequences of 4096 tokens with 8
-// rows 77 and 133, with 16 rows 96 and 133; of 32 rows, 64 sequences of 500 57 and 70, 4 of 4096 25 and 31, one of 700 12.5 and 18.7; 48 of 2048 (16 heads of 64) 125 and 141.
+// rows 77 and 132, with 16 rows 96 and 133; of 32 rows, 64 sequences of 500 57 and 69, 4 of 4096 25 and 27, one of 700 12.3 and 14.7; 48 of 2048 (16 heads of 64) 125 and 144.
 constexpr int kFewRows = 32;
-// But with more than 16 rows and heads of 128 the second reading is dear where the cache does not fit L2 (126 MB): 32 rows of 48 sequences of 4096 tokens take 180 and 134,
-// of 2 of 65536 112 and 91.  How long the sequences are is known on the device alone; the width of the table stands for it.  And most of them must have more than 16 rows: 48 of up
+// But with more than 16 rows and heads of 128 the second reading is dear where the cache does not fit L2 (126 MB): 32 rows of 48 sequences of 4096 tokens take 180 and 133,
+// of 2 of 65536 112 and 83, of 16 of 4096 68 and 58.  How long the sequences are is known on the device alone; the width of the table stands for it.  And most of them must have more than 16 rows: 48 of up
 // to 8192 with 1 to 8 tokens of 4 heads, 11 rows on average, take 133 and 140.
 constexpr int64_t kFewBytes = 128 << 20;
 constexpr int kFewAverage = 20;
