@@ -423,8 +423,6 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
   chunk_prefix(p, prefix, scan_sums, blockIdx.x == 0);
 
   auto q_tile = [&](uint32_t slot) { return smem_at + slot * L::kQBytes; };
-  auto k_tile = [&](uint32_t g) { return smem_at + L::kKOff + g % NK * L::kTileBytes; };
-  auto v_tile = [&](uint32_t g) { return smem_at + L::kVOff + g % NV * L::kTileBytes; };
 
   ChunkItem* const item_ring = reinterpret_cast<ChunkItem*>(smem + L::kItemOff);
   uint32_t n_items = 0;                            // taken by this warp

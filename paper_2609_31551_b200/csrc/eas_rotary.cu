@@ -112,7 +112,7 @@ static eas_status rotary_apply(const eas_rotary* rotary, const eas_rotary_inputs
   p.r = rows_of(in);
   p.r.in_place = (in->n_heads == 0 || (in->q == in->out_q && in->ld_q == in->ld_out_q)) && (in->n_kv_heads == 0 || (in->k == in->out_k && in->ld_k == in->ld_out_k));
   const bool all = budget == g_device_sms, h = in->dtype == EAS_DTYPE_FP16;
-  split_heads(in->n_rows, heads, 4 * 32 / (hd / 16), static_cast<int64_t>(g_device_sms) * (kRotaryThreads / 32), &p.parts, &p.part_heads);
+  split_heads(in->n_rows, heads, kRotaryBatch * 32 / (hd / 16), static_cast<int64_t>(g_device_sms) * (kRotaryThreads / 32), &p.parts, &p.part_heads);
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (hd == 64) return h ? launch_rotary<64, __half>(p, budget, all, st) : launch_rotary<64, bf16>(p, budget, all, st);
   return h ? launch_rotary<128, __half>(p, budget, all, st) : launch_rotary<128, bf16>(p, budget, all, st);
