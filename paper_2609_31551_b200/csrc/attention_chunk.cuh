@@ -9,10 +9,10 @@
 //                 warp 3 walks the line of units (below) and tells the others the items of the CTA, through a ring.  (One warp for both took 1100 cycles a copy and was what
 //                 long caches of few rows waited for.)
 //   warps 1, 2    UMMA issuers, one per softmax warpgroup
-//   warps 4 ..    converters: tiles of queries, then two warps those of K and two those of V, from bytes to fp16 in the tensor core's layout.  Keys: byte ^ 0x80 as the bits of an
-//                 fp16 number is (number + 128) 2^-24, two bytes by one and-xor; the row's factor makes up for 2^-24 and its offset for the 128 (exact: products and sums are
-//                 fp32).  Values: (0x6400 | (byte ^ 0x80)) - 1152, a subtraction more.  Bytes 0 and 2 of a word, then 1 and 3: four dimensions lie in the order 0, 2, 1,
-//                 3, in the queries and the output too
+//   warps 4 ..    converters: tiles of queries, then two warps those of K and two those of V, from bytes to fp16 in the tensor core's layout: (0x6400 | (byte ^ 0x80)) - 1152,
+//                 exact.  Bytes 0 and 2 of a word, then 1 and 3: four dimensions lie in the order 0, 2, 1, 3, in the queries and the output too.  (Keys as number + 128, the
+//                 128 taken off the score by the row's sum, would save the subtraction, but the fp32 sums of the product round at the size of 128 sum |q|: 5e-3 of a weight
+//                 for quiet keys under a loud scale.)
 //   warps 8 ..    two softmax warpgroups, one thread a row
 //
 // A step is 80 keys: 5 parts of 16, the smallest block, and as many scores as a thread's registers hold beside their weights.  A unit of two tiles of one key/value head
@@ -86,8 +86,8 @@ struct ChunkCfg {
   static constexpr int kPrefixOff = kRawOff + (kRawK + kRawV) * kRawBytes;              // (keys' tiles, then values')
   static constexpr int kScaleSlots = 32;
   static constexpr int kScaleOff = kPrefixOff + (kChunkMaxSeqs + 2) * 8;               // [slot][16]: key scales, log2 of value scales, their inverses
-  static constexpr int kRowOff = kScaleOff + kScaleSlots * 64;                         // [2][128] factors and offsets of the rows' scores
-  static constexpr int kMlOff = kRowOff + 2 * 128 * 8;                                 // [2][128] reference and sum of a warpgroup's rows
+  static constexpr int kRowOff = kScaleOff + kScaleSlots * 64;                         // [2][128] factors of the rows' scores
+  static constexpr int kMlOff = kRowOff + 2 * 128 * 4;                                 // [2][128] reference and sum of a warpgroup's rows
   static constexpr int kItemOff = kMlOff + 2 * 128 * 8;
   static constexpr int kDealOff = kItemOff + kChunkItems * 64;                         // where warp 3 is on the line
   static constexpr int kBarOff = kDealOff + kChunkDealBytes;
@@ -372,7 +372,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw_chunk) + 1023) & ~uintptr_t(1023));
   long long* prefix = reinterpret_cast<long long*>(smem + L::kPrefixOff);
   float* sc_ring = reinterpret_cast<float*>(smem + L::kScaleOff);
-  float2* row_factor = reinterpret_cast<float2*>(smem + L::kRowOff);      // what a row's scores are multiplied by, and what is added to them before
+  float* row_factor = reinterpret_cast<float*>(smem + L::kRowOff);        // what a row's scores are multiplied by
   float2* ml_smem = reinterpret_cast<float2*>(smem + L::kMlOff);
   // barriers: addresses in shared memory, 8 bytes each
   const uint32_t smem_at = smem_u32(smem);
@@ -676,10 +676,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
     const int sub = place.x, chunk = place.y;
     uint32_t qn = 0;
     bool ok = true;
-    // The next raw tile to fp16.  Keys: byte ^ 0x80 is a number + 128, and as the bits of an fp16 number (number + 128) 2^-24; the row's factor makes up
-    // for 2^-24, its offset for the 128 of every dimension.  Values are exact: (0x6400 | (byte ^ 0x80)) - 1152.  (One small loop body each: the code of all roles
-    // shares the instruction caches.)
-    // One pair of warps each.
+    // The next raw tile to fp16: keys by one pair of warps, values by the other.  (One small loop body: the code of all roles shares the instruction caches.)
     const bool keys = cw < 2;
     constexpr int STEP = 2 * ROWS, BATCH = 5, PASSES = KEYS / STEP;        // rows that a pair takes at once
     static_assert(KEYS % STEP == 0 && PASSES % BATCH == 0 && STEP % 8 == 0, "whole passes; a row's place in its swizzle pattern stays");
@@ -698,21 +695,11 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
         uint4 x[BATCH];
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) x[i] = lds128(src + (i0 + i) * STEP * HD);
-        if (keys) {
 #pragma unroll
-          for (int i = 0; i < BATCH; ++i) {
-            const uint32_t at = dst + (i0 + i) * STEP * 128;
-            constexpr uint32_t M = 0x00FF00FFu, X = 0x00800080u;
-            sts128(at, (x[i].x & M) ^ X, ((x[i].x >> 8) & M) ^ X, (x[i].y & M) ^ X, ((x[i].y >> 8) & M) ^ X);
-            sts128(at ^ 16, (x[i].z & M) ^ X, ((x[i].z >> 8) & M) ^ X, (x[i].w & M) ^ X, ((x[i].w >> 8) & M) ^ X);
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < BATCH; ++i) {
-            const uint32_t at = dst + (i0 + i) * STEP * 128;
-            sts128(at, bytes02_to_half2(x[i].x), bytes02_to_half2(x[i].x >> 8), bytes02_to_half2(x[i].y), bytes02_to_half2(x[i].y >> 8));
-            sts128(at ^ 16, bytes02_to_half2(x[i].z), bytes02_to_half2(x[i].z >> 8), bytes02_to_half2(x[i].w), bytes02_to_half2(x[i].w >> 8));
-          }
+        for (int i = 0; i < BATCH; ++i) {
+          const uint32_t at = dst + (i0 + i) * STEP * 128;
+          sts128(at, bytes02_to_half2(x[i].x), bytes02_to_half2(x[i].x >> 8), bytes02_to_half2(x[i].y), bytes02_to_half2(x[i].y >> 8));
+          sts128(at ^ 16, bytes02_to_half2(x[i].z), bytes02_to_half2(x[i].z >> 8), bytes02_to_half2(x[i].w), bytes02_to_half2(x[i].w >> 8));
         }
       }
       fence_proxy_async_smem();
@@ -760,32 +747,18 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
           const int e = m != 0u ? min(max(static_cast<int>(__float_as_uint(mx) >> 23) - 127 - 14, -126), 126) : 0;
           const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23), up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
           const uint64_t down2 = pack2(down, down);
-          uint64_t y[8], sum2 = 0;
-#pragma unroll
-          for (int b = 0; b < 8; ++b) {
-            y[b] = pack2(Pair16<T>::lo(xw[b]), Pair16<T>::hi(xw[b]));
-            y[b] = fmul2(y[b], down2);             // (exact, and so is its rounding to fp16 but for what is lost)
-            sum2 = fadd2(sum2, y[b]);
-          }
-          float sum, sum_hi;
-          unpack2(sum2, sum, sum_hi);
-          sum += sum_hi;
-#pragma unroll
-          for (int d = 1; d < 4; d *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-          if constexpr (HD == 128) sum += __shfl_xor_sync(0xffffffffu, sum, 8);
           uint32_t h[8];
 #pragma unroll
           for (int b = 0; b < 4; ++b) {
             float y0, y1, y2, y3;
-            unpack2(y[2 * b], y0, y1);
-            unpack2(y[2 * b + 1], y2, y3);
+            unpack2(fmul2(pack2(Pair16<T>::lo(xw[2 * b]), Pair16<T>::hi(xw[2 * b])), down2), y0, y1);          // (exact, and so is its rounding to fp16 but for what is lost)
+            unpack2(fmul2(pack2(Pair16<T>::lo(xw[2 * b + 1]), Pair16<T>::hi(xw[2 * b + 1])), down2), y2, y3);
             h[2 * b] = Pair16<__half>::pack(y0, y2);
             h[2 * b + 1] = Pair16<__half>::pack(y1, y3);
           }
           store_row_16(q_tile(slot), L::kQHalf, row, chunk, h);
           // (an infinite element makes the row NaN: of -Inf alone its scores would count as masked)
-          if (chunk == 0)
-            row_factor[slot * 128 + row] = make_float2(mx * 0.f == 0.f ? p.scale_log2 * up * 16777216.f : __uint_as_float(0x7FFFFFFFu), sum * -7.62939453125e-06f);      // 2^24; -128 2^-24
+          if (chunk == 0) row_factor[slot * 128 + row] = mx * 0.f == 0.f ? p.scale_log2 * up : __uint_as_float(0x7FFFFFFFu);
         }
       }
       fence_proxy_async_smem();
@@ -821,7 +794,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       const int first = alternate ? w : 0, stride = alternate ? 2 : 1;
       const int mine = alternate ? n : w == 0 ? u.mine[0] : u.mine[1];
       const uint32_t slot = (qn + (alternate ? 0 : w)) & 1u;
-      float2 factor = make_float2(0.f, 0.f);
+      float factor = 0.f;
       for (int t = 0; t < tiles && ok; ++t) {
         const uint32_t q = qn + t;
         ok = chunk_wait(q_full + 8 * (q & 1u), (q >> 1) & 1u, abort_flag);
@@ -855,7 +828,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
 #pragma unroll 1
       for (int j = first; j < mine && active; j += stride, left -= fewer) {
         const uint32_t g = base + j;
-        // factors and offsets of the step's parts, beside the product
+        // factors of the step's parts, beside the product
         if (!chunk_wait(sc_full + 8 * (g % NS), (g / NS) & 1u, abort_flag)) { ok = false; break; }
         float sc[16];
 #pragma unroll
@@ -864,10 +837,7 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
           sc[4 * i] = x.x; sc[4 * i + 1] = x.y; sc[4 * i + 2] = x.z; sc[4 * i + 3] = x.w;
         }
 #pragma unroll
-        for (int m = 0; m < PARTS; ++m) {
-          sc[m] *= factor.x;
-          sc[PARTS + m] = fmaf(factor.y, sc[m], sc[PARTS + m]);
-        }
+        for (int m = 0; m < PARTS; ++m) sc[m] *= factor;
         if (!chunk_wait(s_full + 8 * w, n_s & 1u, abort_flag)) { ok = false; break; }
         ++n_s;
         tc_fence_after_sync();

@@ -1,0 +1,45 @@
+"""Calls of rotary positions, appending and chunk attention that lie off the beaten track: axes that share memory, keys alone, bounds that are not met, tables as wide as
+they may be, quiet keys under loud scales, queries and scales at the ends of their ranges.  The bounds are those of test_gpu_positions.py."""
+import pytest
+import torch
+
+from tests.test_gpu_positions import _cache, _check_append, _check_chunk, _check_rotated, _cu, _dev, _filled, _rand, _rotary, _table
+
+pytestmark = pytest.mark.gpu
+BF, FP = torch.bfloat16, torch.float16
+
+
+# ------------------------------------------------------------------------------------------------ ranges
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("max_new", [3, 60])
+def test_quiet_keys_under_a_loud_scale(dtype, hd, max_new):
+    """Numbers of -1, 0 and 1, most of them 0, in blocks whose scale another token has set, and queries of one sign: the sum over |q| times 127 steps of the scale is some
+    thousand times a score, and must not stand in its error.  Scores are within a few units of each other, so every key counts."""
+    bs, G, H = 16, 2, 8
+    lens, before = [max_new, 1], [5, 40]
+    held = [a + b for a, b in zip(lens, before)]
+    table, n_blocks = _table(17, held, bs)
+    gen = torch.Generator().manual_seed(18)
+    numbers, scales = _filled(n_blocks, G, bs, hd, 19)
+    keys = (torch.rand(numbers[0].shape, generator=gen) < 4.0 / hd).to(torch.int8) * (torch.randint(0, 2, numbers[0].shape, generator=gen, dtype=torch.int8) * 2 - 1)
+    q = ((torch.rand((sum(lens), H, hd), generator=gen) * 0.5 + 0.5) * 8.0).to(dtype)
+    numbers, scales = [keys, numbers[1]], [torch.full_like(scales[0], 6.0), scales[1]]
+    _check_chunk(_cache(numbers, scales), numbers, scales, q, _cu(lens), held, table, max_new=max_new)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("max_new", [3, 60])
+@pytest.mark.parametrize("power", [100, 117, 120, 125])
+def test_queries_at_the_upper_end_of_bf16(hd, max_new, power):
+    """Queries of up to 2^127 over keys whose scale takes it back: the scores are those of ordinary ones."""
+    bs, G, H = 16, 2, 4
+    lens, before = [max_new, 1], [50, 40]
+    held = [a + b for a, b in zip(lens, before)]
+    table, n_blocks = _table(20, held, bs)
+    numbers, scales = _filled(n_blocks, G, bs, hd, 21)
+    q = (_rand((sum(lens), H, hd), BF, 22).float().clamp(-3.9, 3.9) * 2.0 ** power).to(BF)
+    assert torch.isfinite(q).all()
+    for split in (0, 30):                                                  # the scale of the scores may take part of it
+        sc = [scales[0] * 2.0 ** (split - power), scales[1]]
+        _check_chunk(_cache(numbers, sc), numbers, sc, q, _cu(lens), held, table, scale=hd ** -0.5 * 2.0 ** -split, max_new=max_new)
