@@ -118,8 +118,8 @@ eas_status eas_cache_attention(const eas_cache* cache, const eas_cache_seqs* seq
  * next chunk of a prompt, a draft to be verified, single tokens between them.  Row i of n sees places 0 .. i + seq_lens[s] - n; a row that sees nothing (a sequence
  * shorter than its chunk, or of length 0 or less) gets 0, and rows that cu_seqlens does not name are left alone.  out = softmax(scale * q k^T) v with the types of
  * eas_cache_attention.  Of `seqs` it takes cu_seqlens and seq_lens; they are read when the call's work runs.
- * n_rows: rows of q that exist (a bound on cu_seqlens).  max_new: the most new tokens that a sequence has (n_rows does, too; a smaller number chooses
- * kernels for few rows): a sequence with more is not computed and raises the status word to EAS_DEVICE_CACHE_RANGE.
+ * n_rows: rows of q that exist (a bound on cu_seqlens).  max_new: the most new tokens that a sequence has: a sequence with more is not computed and raises the
+ * status word to EAS_DEVICE_CACHE_RANGE.  Any bound is right (n_rows, if nothing is known); the kernels are chosen by it, so the exact number is the fastest.
  * workspace: device scratch of eas_cache_chunk_workspace_bytes() (0 on bad arguments), 256-byte aligned; its contents do not matter and nothing of it is used
  * by a later call, but calls that may run at the same time need one each.
  * Limits (UNSUPPORTED): 128 query heads a key/value head, 2^30 places a sequence (max_blocks * block_size), n_rows * n_heads below 2^31. */

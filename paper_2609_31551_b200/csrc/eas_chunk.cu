@@ -68,8 +68,11 @@ static eas_status launch_few(const CacheAttnParams& p, int budget, bool all, cud
 
 // Which kernels a call needs: those for few rows alone, where no sequence has more; both, where most sequences have less than half of the most (a
 // prompt's chunk beside single tokens); else the tiles of 128 rows for all.
-// A chunk beside which there is at most a token a sequence has the others' rows in 8 columns: 512 tokens and 63 single ones behind 4096, 32 and 8 heads of 128, 178 us
-// instead of 194.  (With a few drafts among them it has not: 1187 tokens, 19 single ones and drafts of 2, 3 and 4 would take 174 instead of 170, the last two by tiles.)
+// A chunk beside which there is at most a token a sequence, as far as max_new and n_rows tell, has the others' rows in 8 columns: 512 tokens and 63 single ones behind 4096, 32
+// and 8 heads of 128, 176 us instead of 188.  (With a few drafts among them it has not: 1187 tokens, 19 single ones and drafts of 2, 3 and 4 would take 174 instead of 170,
+// the last two by tiles.)
+// A max_new of n_rows or more, the default of the binding, tells nothing of how the rows are spread; their average does.  With it, 64 single tokens behind 4096 take 103 us (124 in 16
+// columns), 48 drafts of 4 104 (143 by tiles), of 8 147 (189 in 16 columns).
 struct ChunkPlan {
   int few_rows = 0;            // most rows a key/value head of the sequences that the kernels for few rows take
   bool tiles = false;
@@ -77,11 +80,15 @@ struct ChunkPlan {
 static ChunkPlan chunk_plan(const eas_cache* c, int32_t n_seqs, int32_t n_rows, int32_t max_new, int group, int64_t places) {
   ChunkPlan plan;
   const int64_t most = static_cast<int64_t>(max_new) * group, token_bytes = 2LL * c->d.n_kv_heads * c->d.head_dim;
-  plan.tiles = most > kFewRows || (most > 16 && c->d.head_dim == 128 && static_cast<int64_t>(n_rows) * group >= static_cast<int64_t>(n_seqs) * kFewAverage &&
-                                   n_seqs * places >= kFewBytes / token_bytes);
-  if (!plan.tiles) plan.few_rows = static_cast<int>(std::max<int64_t>(most, 1));
-  else if (group <= kFewRows && static_cast<int64_t>(n_rows) * 2 < static_cast<int64_t>(n_seqs) * max_new)
-    plan.few_rows = group <= 8 && n_rows - max_new <= n_seqs - 1 ? 8 : kFewRows;
+  const bool twice_dear = c->d.head_dim == 128 && static_cast<int64_t>(n_rows) * group >= static_cast<int64_t>(n_seqs) * kFewAverage && n_seqs * places >= kFewBytes / token_bytes;
+  plan.tiles = most > kFewRows || (most > 16 && twice_dear);
+  if (!plan.tiles) {
+    plan.few_rows = static_cast<int>(std::max<int64_t>(most, 1));
+  } else if (group <= kFewRows && static_cast<int64_t>(n_rows) * 2 < static_cast<int64_t>(n_seqs) * max_new) {
+    const bool known = max_new < n_rows;
+    const bool single = known ? n_rows - max_new <= n_seqs - 1 : n_rows <= n_seqs;
+    plan.few_rows = group <= 8 && single ? 8 : !known && twice_dear ? 16 : kFewRows;
+  }
   return plan;
 }
 

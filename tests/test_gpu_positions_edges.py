@@ -9,6 +9,22 @@ pytestmark = pytest.mark.gpu
 BF, FP = torch.bfloat16, torch.float16
 
 
+# ------------------------------------------------------------------------------------------------ which kernel
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("lens", [[4] * 12, [3, 4, 8, 1, 5], [4, 2, 1], [1] * 9])
+def test_drafts_without_a_bound_go_to_the_kernels_for_few_rows(hd, lens):
+    """max_new left out says nothing of how the rows are spread: single tokens, and drafts of 9 to 32 rows a key/value head, are computed by the same kernels as with their bound, to the same bits."""
+    H, G, bs = 8, 2, 16
+    held = [n + b for n, b in zip(lens, range(300, 1500, 100))]
+    table, n_blocks = _table(hd, held, bs)
+    numbers, scales = _filled(n_blocks, G, bs, hd, 11)
+    q = _rand((sum(lens), H, hd), BF, 12, 2.0)
+    c = _cache(numbers, scales)
+    exact = _check_chunk(c, numbers, scales, q, _cu(lens), held, table, max_new=max(lens))
+    for loose in (None, sum(lens) + 7):
+        assert torch.equal(_check_chunk(c, numbers, scales, q, _cu(lens), held, table, max_new=loose), exact)
+
+
 # ------------------------------------------------------------------------------------------------ ranges
 @pytest.mark.parametrize("dtype", [BF, FP])
 @pytest.mark.parametrize("hd", [64, 128])
