@@ -44,6 +44,7 @@ constexpr int64_t kFewBytes = 128 << 20;
 constexpr int kFewAverage = 20;
 
 static int few_columns(int rows) { return rows <= 8 ? 8 : 16; }
+static int64_t few_blocks(int rows) { return (rows + few_columns(rows) - 1) / few_columns(rows); }
 static size_t few_workspace(const eas_cache* c, int rows, size_t* o_off) {
   const int r = few_columns(rows), warps = r == 8 ? CacheAttnCfg<128, 1>::kWarps : CacheAttnCfg<128, 2>::kWarps;
   const size_t n = static_cast<size_t>(2) * c->sm_count * warps * r;
@@ -73,6 +74,8 @@ static eas_status launch_few(const CacheAttnParams& p, int budget, bool all, cud
 // the last two by tiles.)
 // A max_new of n_rows or more, the default of the binding, tells nothing of how the rows are spread; their average does.  With it, 64 single tokens behind 4096 take 103 us (124 in 16
 // columns), 48 drafts of 4 104 (143 by tiles), of 8 147 (189 in 16 columns).
+// The kernels for few rows add up what all sequences may cost in 32 bits; behind a table so wide that the sum could pass them (8 sequences of 8 key/value heads and 2^30 places each), the tiles,
+// whose line has 64, take all.
 struct ChunkPlan {
   int few_rows = 0;            // most rows a key/value head of the sequences that the kernels for few rows take
   bool tiles = false;
@@ -88,6 +91,10 @@ static ChunkPlan chunk_plan(const eas_cache* c, int32_t n_seqs, int32_t n_rows, 
     const bool known = max_new < n_rows;
     const bool single = known ? n_rows - max_new <= n_seqs - 1 : n_rows <= n_seqs;
     plan.few_rows = group <= 8 && single ? 8 : !known && twice_dear ? 16 : kFewRows;
+  }
+  if (plan.few_rows > 0) {
+    const int64_t tiles = (places + 31) / 32 + kRowCost, row_tiles = few_blocks(plan.few_rows) * c->d.n_kv_heads;      // (no variant's tile is smaller than 32 places)
+    if (tiles * row_tiles > 0x7fffffffLL / std::clamp(n_seqs, 1, kCacheMaxSeqs)) return ChunkPlan{0, true};
   }
   return plan;
 }
@@ -135,10 +142,7 @@ static eas_status chunk_attention(const eas_cache* c, const eas_cache_seqs* s, c
     p.map_k = c->map_k; p.map_v = c->map_v;
     p.c = view_of(c);
     p.group = group;
-    p.row_blocks = (plan.few_rows + columns - 1) / columns;
-    const int64_t tiles = (places + 31) / 32 + kRowCost;          // (no variant's tile is smaller)
-    if (tiles * G * p.row_blocks > 0x7fffffffLL / std::min(s->n_seqs, kCacheMaxSeqs))
-      return fail(EAS_ERR_UNSUPPORTED, "max_blocks %d is too large for %d sequences", s->max_blocks, s->n_seqs);
+    p.row_blocks = static_cast<int>(few_blocks(plan.few_rows));
     p.n_rows = n_rows; p.max_new = max_new; p.most_rows = plan.few_rows;
     p.ld_table = s->ld_table; p.max_blocks = s->max_blocks;
     p.q = static_cast<const uint16_t*>(q); p.out = static_cast<uint16_t*>(out);
@@ -194,7 +198,7 @@ extern "C" size_t eas_cache_chunk_workspace_bytes(const eas_cache* cache, int32_
     fail(EAS_ERR_UNSUPPORTED, "%d query heads per key/value head (at most 128)", n_heads / cache->d.n_kv_heads);
     return 0;
   }
-  // for a table of any width
+  // for a table of any width: a wider one brings the tiles in, or has them take all
   size_t bytes = 0;
   for (const int64_t places : {int64_t{0}, int64_t{1} << 30})
     bytes = std::max(bytes, plan_workspace(cache, chunk_plan(cache, n_seqs, n_rows, max_new, n_heads / cache->d.n_kv_heads, places), n_rows, max_new, n_heads));

@@ -25,6 +25,23 @@ def test_drafts_without_a_bound_go_to_the_kernels_for_few_rows(hd, lens):
         assert torch.equal(_check_chunk(c, numbers, scales, q, _cu(lens), held, table, max_new=loose), exact)
 
 
+@pytest.mark.parametrize("hd,H,G", [(128, 8, 8), (64, 16, 8)])
+@pytest.mark.parametrize("lens", [[1] * 8, [2, 1, 4, 1, 1, 0, 3, 1], [40, 1, 1, 1, 1, 1, 1, 1], [33, 40, 38, 1, 2, 40, 12, 39]])
+def test_tables_as_wide_as_they_may_be(hd, H, G, lens):
+    """2^30 places a sequence, of which a few hundred are used."""
+    bs, width = 128, 1 << 23
+    held = [n + b for n, b in zip(lens, (700, 0, 90, 33, 5, 260, 128, 127))]
+    narrow, n_blocks = _table(13, held, bs)
+    numbers, scales = _filled(n_blocks, G, bs, hd, 14)
+    table = torch.full((len(lens), width), -7, dtype=torch.int32)
+    table[:, :narrow.shape[1]] = narrow
+    q = _rand((sum(lens), H, hd), BF, 15, 2.0)
+    c = _cache(numbers, scales)
+    for max_new in (max(lens), None):
+        workspace = torch.empty(c.chunk_workspace_bytes(len(lens), sum(lens), sum(lens) if max_new is None else max_new, H), dtype=torch.uint8, device="cuda")
+        _check_chunk(c, numbers, scales, q, _cu(lens), held, table, max_new=max_new, workspace=workspace)
+
+
 # ------------------------------------------------------------------------------------------------ ranges
 @pytest.mark.parametrize("dtype", [BF, FP])
 @pytest.mark.parametrize("hd", [64, 128])
