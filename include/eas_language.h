@@ -154,7 +154,7 @@ typedef struct {
   void* out_q;            /* as q, as k: the same address and distance (in place), or memory that overlaps no input */
   void* out_k;
   int64_t ld_q, ld_k, ld_out_q, ld_out_k;
-  const int32_t* positions; /* device [n_axes][n_rows], distance ld_positions */
+  const int32_t* positions; /* device [n_axes][n_rows], distance ld_positions (0: one row for all axes) */
   int64_t ld_positions;
   int32_t n_rows, n_heads, n_kv_heads, dtype;
   int32_t inverse;        /* 1: by -angle, which takes the rotation back; times scale, the gradient's way through it */

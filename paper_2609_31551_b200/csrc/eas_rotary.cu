@@ -53,6 +53,12 @@ static eas_status check_rows(const char* name, const void* in, const void* out, 
     return fail(EAS_ERR_INVALID_ARG, "%s: token distances must be multiples of 8 that hold a token's heads", name);
   return EAS_OK;
 }
+// The axes lie n_rows apart or more, or are one and the same (kernels only read them)
+static eas_status check_positions(const eas_rotary* r, const eas_rotary_inputs* in) {
+  if (in->positions == nullptr || (in->ld_positions != 0 && in->ld_positions < in->n_rows))
+    return fail(EAS_ERR_INVALID_ARG, "positions: [%d][%d] wanted", r->n_axes, in->n_rows);
+  return EAS_OK;
+}
 static eas_status check_inputs(const eas_rotary* r, const eas_rotary_inputs* in) {
   if (r == nullptr || in == nullptr) return fail(EAS_ERR_INVALID_ARG, "a required pointer is null");
   if (in->dtype != EAS_DTYPE_BF16 && in->dtype != EAS_DTYPE_FP16) return fail(EAS_ERR_UNSUPPORTED, "dtype %d", in->dtype);
@@ -101,7 +107,7 @@ static eas_status rotary_apply(const eas_rotary* rotary, const eas_rotary_inputs
   if (in->n_rows > 0) {
     if (in->n_heads > 0) EAS_TRY(check_rows("q", in->q, in->out_q, in->ld_q, in->ld_out_q, static_cast<int64_t>(in->n_heads) * hd));
     if (in->n_kv_heads > 0) EAS_TRY(check_rows("k", in->k, in->out_k, in->ld_k, in->ld_out_k, static_cast<int64_t>(in->n_kv_heads) * hd));
-    if (in->positions == nullptr || in->ld_positions < in->n_rows) return fail(EAS_ERR_INVALID_ARG, "positions: [%d][%d] wanted", rotary->n_axes, in->n_rows);
+    EAS_TRY(check_positions(rotary, in));
   }
   int budget = 0;
   EAS_TRY(resolve_budget(sm_budget, &budget));
@@ -162,7 +168,7 @@ static eas_status cache_append(const eas_cache* c, const eas_cache_seqs* s, cons
   if (in->n_heads > 0) EAS_TRY(check_rows("q", in->q, in->out_q, in->ld_q, in->ld_out_q, static_cast<int64_t>(in->n_heads) * hd));
   EAS_TRY(check_rows("k", in->k, in->k, in->ld_k, in->ld_k, static_cast<int64_t>(G) * hd));
   EAS_TRY(check_rows("v", v, v, ld_v, ld_v, static_cast<int64_t>(G) * hd));
-  if (in->positions != nullptr && in->ld_positions < in->n_rows) return fail(EAS_ERR_INVALID_ARG, "positions: [%d][%d] wanted", rotary->n_axes, in->n_rows);
+  if (in->positions != nullptr) EAS_TRY(check_positions(rotary, in));
   AppendParams p{};
   p.c = view_of(c);
   p.s = CacheSeqs{s->block_table, s->cu_seqlens, s->start, s->ld_table, s->n_seqs, s->max_blocks};

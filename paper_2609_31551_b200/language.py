@@ -276,8 +276,8 @@ class Rotary:
         return positions.data_ptr(), positions.stride(0) if self.n_axes > 1 else rows
 
     def apply(self, q, k, positions, out=None, inverse=False, sm_budget=0, stream=None):
-        """eas_rotary_apply: q [T, n_heads, head_dim] and k [T, n_kv_heads, head_dim] (or None) at positions (int32 [n_axes, T], or [T] with one axis, on
-        the device) -> rotated (q, k).  out: a pair of tensors for them, (q, k) themselves to rotate in place.  inverse takes a rotation back; a
+        """eas_rotary_apply: q [T, n_heads, head_dim] and k [T, n_kv_heads, head_dim] (or None) at positions (int32 [n_axes, T], which may be one row expanded, or
+        [T] with one axis, on the device) -> rotated (q, k).  out: a pair of tensors for them, (q, k) themselves to rotate in place.  inverse takes a rotation back; a
         gradient goes through apply by inverse=True."""
         dtype, index = q.dtype, q.get_device()
         if self.handle is None:

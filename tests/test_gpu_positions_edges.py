@@ -9,6 +9,32 @@ pytestmark = pytest.mark.gpu
 BF, FP = torch.bfloat16, torch.float16
 
 
+# ------------------------------------------------------------------------------------------------ positions
+@pytest.mark.parametrize("T", [1, 2, 37])
+def test_axes_may_share_their_positions(T):
+    """Text tokens on three axes: one row of positions, seen three times."""
+    import paper_2609_31551_b200 as P
+    hd, G, bs = 64, 2, 16
+    r, rot = _rotary(hd, hd, (16, 8, 8))
+    q, k = _rand((T, 4, hd), BF, 1), _rand((T, G, hd), BF, 2)
+    pos = torch.randint(0, 5000, (T,), generator=torch.Generator().manual_seed(3), dtype=torch.int32).cuda()
+    shared, apart = pos.expand(3, -1), pos.repeat(3, 1)
+    assert shared.stride(0) == 0
+    out = r.apply(q.cuda(), k.cuda(), shared)
+    _check_rotated(q, out[0], rot, apart.cpu().numpy())
+    _check_rotated(k, out[1], rot, apart.cpu().numpy())
+    table, n_blocks = _table(1, [T + 5], bs)
+    was = _filled(n_blocks, G, bs, hd, 4)
+    c = _cache(*was)
+    turned = c.append(q.cuda(), k.cuda(), k.cuda(), _dev([0, T]), _dev([5]), table.cuda(), r, shared)
+    c.check()
+    _check_append(c, was, *was, rot, q, k, k, [0, T], [5], table, apart.cpu().numpy(), turned)
+    if T > 2:                                                              # axes that overlap otherwise are a mistake
+        for call in (lambda p: r.apply(q.cuda(), k.cuda(), p), lambda p: c.append(q.cuda(), k.cuda(), k.cuda(), _dev([0, T]), _dev([5]), table.cuda(), r, p)):
+            with pytest.raises(P.EasError):
+                call(torch.zeros(3 * T, dtype=torch.int32, device="cuda").as_strided((3, T), (1, 1)))
+
+
 # ------------------------------------------------------------------------------------------------ which kernel
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("lens", [[4] * 12, [3, 4, 8, 1, 5], [4, 2, 1], [1] * 9])
