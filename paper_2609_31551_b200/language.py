@@ -276,26 +276,38 @@ class Rotary:
         return positions.data_ptr(), positions.stride(0) if self.n_axes > 1 else rows
 
     def apply(self, q, k, positions, out=None, inverse=False, sm_budget=0, stream=None):
-        """eas_rotary_apply: q [T, n_heads, head_dim] and k [T, n_kv_heads, head_dim] (or None) at positions (int32 [n_axes, T], which may be one row expanded, or
-        [T] with one axis, on the device) -> rotated (q, k).  out: a pair of tensors for them, (q, k) themselves to rotate in place.  inverse takes a rotation back; a
-        gradient goes through apply by inverse=True."""
-        dtype, index = q.dtype, q.get_device()
+        """eas_rotary_apply: q [T, n_heads, head_dim] and k [T, n_kv_heads, head_dim] (one of them may be None) at positions (int32 [n_axes, T], which may be one
+        row expanded, or [T] with one axis, on the device) -> rotated (q, k).  out: a pair of tensors for them, (q, k) themselves to rotate in place.  inverse takes a
+        rotation back; a gradient goes through apply by inverse=True."""
+        x = k if q is None else q
+        if x is None:
+            raise B.EasError(1, "queries, keys or both")
+        dtype, index = x.dtype, x.get_device()
         if self.handle is None:
             raise B.EasError(1, "the rotary positions are closed")
-        if index < 0 or dtype not in _DTYPES or q.dim() != 3 or (k is not None and k.dim() != 3):
-            raise B.EasError(1, f"q and k must be bf16 or fp16 tensors [tokens, heads, head_dim] on a GPU, q is {dtype} {tuple(q.shape)} on {q.device}")
+        if index < 0 or dtype not in _DTYPES or x.dim() != 3 or (k is not None and k.dim() != 3):
+            raise B.EasError(1, f"q and k must be bf16 or fp16 tensors [tokens, heads, head_dim] on a GPU, not {dtype} {tuple(x.shape)} on {x.device}")
         if _elsewhere(index, stream):
             with _on(index, stream):
                 return self.apply(q, k, positions, out, inverse, sm_budget)
-        T, H, hd = q.shape
-        ld_q = _rows(q, "q", H, self.head_dim, dtype, index)
-        G, ld_k, at_k, at_out_k, ld_out_k, out_k = 0, 0, None, None, 0, None
-        if out is None:
-            out_q = torch.empty_like(q, memory_format=torch.contiguous_format)
-            ld_out_q = H * hd
-        else:
+        T, hd = x.shape[0], self.head_dim
+        H, ld_q, at_q, at_out_q, ld_out_q, out_q = 0, 0, 0, 0, 0, None
+        G, ld_k, at_k, at_out_k, ld_out_k, out_k = 0, 0, 0, 0, 0, None
+        if out is not None:
+            if len(out) != 2 or (q is not None and out[0] is None) or (k is not None and out[1] is None):
+                raise B.EasError(1, "out must be a pair of tensors, for q and for k")
             out_q, out_k = out
-            ld_out_q = _rows(out_q, "out of q", H, hd, dtype, index)
+        if q is not None:
+            H = q.shape[1]
+            ld_q = _rows(q, "q", H, hd, dtype, index)
+            if out is None:
+                out_q = torch.empty_like(q, memory_format=torch.contiguous_format)
+                ld_out_q = H * hd
+            else:
+                ld_out_q = _rows(out_q, "out of q", H, hd, dtype, index)
+            at_q, at_out_q = q.data_ptr(), out_q.data_ptr()
+            if out_q.shape[0] != T:
+                raise B.EasError(1, "the output of q must have as many tokens as q")
         if k is not None:
             G = k.shape[1]
             ld_k = _rows(k, "k", G, hd, dtype, index)
@@ -307,11 +319,8 @@ class Rotary:
             at_k, at_out_k = k.data_ptr(), out_k.data_ptr()
             if k.shape[0] != T or out_k.shape[0] != T:
                 raise B.EasError(1, "k and its output must have as many tokens as q")
-        if out_q.shape[0] != T:
-            raise B.EasError(1, "the output of q must have as many tokens as q")
         at, ld_pos = self._positions(positions, T, index)
-        rec = _pack_rotary(q.data_ptr(), at_k or 0, out_q.data_ptr(), at_out_k or 0, ld_q, ld_k, ld_out_q, ld_out_k, at, ld_pos, T, H, G, _DTYPES[dtype],
-                           1 if inverse else 0)
+        rec = _pack_rotary(at_q, at_k, at_out_q, at_out_k, ld_q, ld_k, ld_out_q, ld_out_k, at, ld_pos, T, H, G, _DTYPES[dtype], 1 if inverse else 0)
         rc = self.lib.eas_rotary_apply(self.handle, rec, sm_budget, torch._C._cuda_getCurrentRawStream(index))
         if rc:
             B._check(rc)

@@ -35,6 +35,29 @@ def test_axes_may_share_their_positions(T):
                 call(torch.zeros(3 * T, dtype=torch.int32, device="cuda").as_strided((3, T), (1, 1)))
 
 
+def test_rotation_of_keys_alone():
+    import paper_2609_31551_b200 as P
+    r, rot = _rotary(128, 64, (16, 8, 8))
+    k = _rand((21, 3, 128), FP, 5)
+    pos = torch.randint(0, 900, (3, 21), generator=torch.Generator().manual_seed(6), dtype=torch.int32)
+    kd = k.cuda()
+    none, out = r.apply(None, kd, pos.cuda())
+    assert none is None
+    _check_rotated(k, out, rot, pos.numpy())
+    assert torch.equal(r.apply(kd, None, pos.cuda())[0], out)
+    buf = torch.empty_like(kd)
+    assert r.apply(None, kd, pos.cuda(), out=(None, buf))[1] is buf and torch.equal(buf, out)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    again = r.apply(None, kd, pos.cuda(), stream=side)[1]
+    side.synchronize()
+    assert torch.equal(again, out)
+    for call in (lambda: r.apply(None, None, pos.cuda()), lambda: r.apply(kd, kd, pos.cuda(), out=(buf, None)), lambda: r.apply(kd, kd, pos.cuda(), out=(None, buf)),
+                 lambda: r.apply(kd, kd, pos.cuda(), out=buf[:2]), lambda: r.apply(kd, None, pos.cuda(), out=(buf,)), lambda: r.apply(None, kd.float(), pos.cuda())):
+        with pytest.raises(P.EasError):
+            call()
+
+
 # ------------------------------------------------------------------------------------------------ which kernel
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("lens", [[4] * 12, [3, 4, 8, 1, 5], [4, 2, 1], [1] * 9])
