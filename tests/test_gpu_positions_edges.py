@@ -125,3 +125,19 @@ def test_queries_at_the_upper_end_of_bf16(hd, max_new, power):
     for split in (0, 30):                                                  # the scale of the scores may take part of it
         sc = [scales[0] * 2.0 ** (split - power), scales[1]]
         _check_chunk(_cache(numbers, sc), numbers, sc, q, _cu(lens), held, table, scale=hd ** -0.5 * 2.0 ** -split, max_new=max_new)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("max_new", [4, 60])
+@pytest.mark.parametrize("power", [-92, -60, 100])
+def test_value_scales_at_both_ends(hd, max_new, power):
+    """Values of 2^-97 and 2^107 and their sums in bf16, against the oracle."""
+    lens, before, bs, G = [max_new, 1], [200, 90], 16, 2
+    held = [a + b for a, b in zip(lens, before)]
+    table, n_blocks = _table(23, held, bs)
+    numbers, scales = _filled(n_blocks, G, bs, hd, 24)
+    q = _rand((sum(lens), 4, hd), BF, 25)
+    sc = [scales[0], scales[1] * 2.0 ** power]
+    assert float(sc[1].min()) >= 2.0 ** -100
+    out = _check_chunk(_cache(numbers, sc), numbers, sc, q, _cu(lens), held, table, max_new=max_new)
+    assert (out != 0).any(dim=-1).all()
