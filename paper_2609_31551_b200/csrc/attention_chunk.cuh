@@ -742,8 +742,8 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
           for (int d = 1; d < 4; d *= 2) m = max(m, __shfl_xor_sync(0xffffffffu, m, d));
           if constexpr (HD == 128) m = max(m, __shfl_xor_sync(0xffffffffu, m, 8));
           const float mx = load16(static_cast<uint16_t>(m), std::is_same_v<T, __half>);
-          // the largest of the row to [2^14, 2^15) (fp16 ends at 65504), by an exponent of -126 to 126, so that both powers are normal numbers: what is
-          // below 2^-39 of the row's largest is lost
+          // the largest of the row to [2^14, 2^15) (fp16 ends at 65504), by an exponent of -126 to 126, so that both powers are normal numbers: an
+          // element is off by at most 2^-25 of these, 2^-39 of the row's largest (bf16 above 2^-31 of the largest and fp16 above 2^-28 are exact)
           const int e = m != 0u ? min(max(static_cast<int>(__float_as_uint(mx) >> 23) - 127 - 14, -126), 126) : 0;
           const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23), up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
           const uint64_t down2 = pack2(down, down);
