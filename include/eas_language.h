@@ -116,8 +116,10 @@ eas_status eas_cache_attention(const eas_cache* cache, const eas_cache_seqs* seq
 /* ---- attention of several new tokens a sequence over the cache ----
  * Rows cu_seqlens[s] .. cu_seqlens[s+1] - 1 of q are the LAST tokens among places 0 .. seq_lens[s] - 1 of sequence s (their keys and values stored before): the
  * next chunk of a prompt, a draft to be verified, single tokens between them.  Row i of n sees places 0 .. i + seq_lens[s] - n; a row that sees nothing (a sequence
- * shorter than its chunk, or of length 0 or less) gets 0, and rows that cu_seqlens does not name are left alone.  out = softmax(scale * q k^T) v with the types of
- * eas_cache_attention.  Of `seqs` it takes cu_seqlens and seq_lens; they are read when the call's work runs.
+ * shorter than its chunk, or of length 0 or less) gets 0, and rows that cu_seqlens does not name are left alone.  out = softmax(scale * q k^T) v with the types and
+ * the precision of eas_cache_attention; it overlaps no input.  Of `seqs` it takes cu_seqlens and seq_lens; they are read when the call's work runs.
+ * Which kernels run is decided by n_seqs, n_rows, max_new, the heads and max_blocks: the same inputs give the same bits for any sm_budget and in every replay, but
+ * with another max_new, another width of the table or other sequences beside it a sequence's last bits may differ.
  * n_rows: rows of q that exist (a bound on cu_seqlens).  max_new: the most new tokens that a sequence has: a sequence with more is not computed and raises the
  * status word to EAS_DEVICE_CACHE_RANGE.  Any bound is right (n_rows, if nothing is known); the kernels are chosen by it, so the exact number is the fastest.
  * workspace: device scratch of eas_cache_chunk_workspace_bytes() (0 on bad arguments), 256-byte aligned; its contents do not matter and nothing of it is used

@@ -509,8 +509,8 @@ class KvCache:
         """eas_cache_chunk_attention: rows cu_seqlens[s] .. cu_seqlens[s + 1] - 1 of q [rows, n_heads, head_dim] are the last tokens among places
         0 .. seq_lens[s] - 1 of sequence s (stored before); each sees the places up to its own.  max_new: the most new tokens of a sequence, which
         chooses the kernels: the exact number is the fastest (default: any number); a captured call can be replayed for other cu_seqlens and seq_lens within it.  Rows that cu_seqlens does not name are
-        left as they were (`out`) or are not set.  workspace: a uint8 tensor of chunk_workspace_bytes(), on a 256-byte boundary; calls that
-        may run at the same time need one each (default: allocated by the call)."""
+        left as they were (`out`, which overlaps no input) or are not set.  A sequence's last bits may depend on max_new, on the table's width and on the other sequences.
+        workspace: a uint8 tensor of chunk_workspace_bytes(), on a 256-byte boundary; calls that may run at the same time need one each (default: allocated by the call)."""
         index, dtype = self._index, q.dtype
         if _elsewhere(index, stream):
             with _on(index, stream):
