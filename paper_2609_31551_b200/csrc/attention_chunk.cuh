@@ -4,6 +4,9 @@
 // The query heads that share a key/value head are rows of one matrix, 128 / group tokens a tile of 128 rows, as in attention_prompt.cuh; the numbers of the cache
 // enter exact in fp16 as in attention_cache.cuh: queries are fp16 times a power of two per row, a block's key scale multiplies its scores in fp32, its value scale v
 // is an exponent: with t = score + log2 v and w = 2^(t - m),  out = sum w number / sum w / v, m being kept 2^7 to 2^15 below the largest t.
+// The weights are rounded to fp16 for their product with the numbers, the only operands that the tensor core has beside numbers exact in 16 bits, with 11 bits
+// where bf16 has 8; the sum below the line takes them unrounded, and it, the references and O are fp32.  Against 64 bits the outputs are off by 0.00025 in fp16
+// (0.00021 with weights of 32 bits) and by 0.0017 in bf16 either way.
 //
 //   warps 0, 3    bytes of K and of V, a block's tokens of a head (they are contiguous) a bulk copy, into rings of 8-bit tiles; warp 0 the scales of the steps, too, and
 //                 warp 3 walks the line of units (below) and tells the others the items of the CTA, through a ring.  (One warp for both took 1100 cycles a copy and was what
@@ -15,24 +18,28 @@
 //                 for quiet keys under a loud scale.)
 //   warps 8 ..    two softmax warpgroups, one thread a row
 //
-// A step is 80 keys: 5 parts of 16, the smallest block, and as many scores as a thread's registers hold beside their weights.  A unit of two tiles of one key/value head
-// (shared) brings each K and V tile to both warpgroups; a unit of one tile gives its steps to the warpgroups in turn (alternate), which put their results together at its
-// end: O lies in tensor memory, where the lanes of both can read it.  So two steps are in flight whether there are many rows (bound by the pipes) or few (bound by the
-// conversion of the bytes).
+// A step is 80 keys: 5 parts of 16, the smallest block, and as many scores as a thread's registers hold beside their weights.  A unit of two tiles of one
+// key/value head (shared) brings each K and V tile to both warpgroups; a unit of one tile gives its steps to the warpgroups in turn (alternate), which put
+// their results together at its end: O lies in tensor memory, where the lanes of both can read it.  So two steps are in flight whether there are many rows
+// (bound by the pipes) or few (bound by the conversion of the bytes).
 //
-// The units of all sequences and heads form a line, in tokens seen times tiles, cut into one equal piece an SM (a function of the shapes and the device, not of sm_budget).  A
-// piece is the end of a unit, whole units, the beginning of one; cut units leave (m, l, O) in the workspace, and chunk_join_kernel puts them together in order.
-// Lengths are read on the device: each CTA sums them up itself.
+// The units of all sequences and heads form a line, in tokens seen times tiles, cut into one equal piece an SM (a function of the shapes and the device, not of
+// sm_budget).  A piece is the end of a unit, whole units, the beginning of one; cut units leave (m, l, O) in the workspace, and chunk_join_kernel puts them
+// together in order.  Lengths are read on the device: each CTA sums them up itself.
 //
-// Measured, back to back in a graph, both launches, 32 and 8 heads of 128 unless stated: two chunks of 2048 tokens behind 14336 1.00 to 1.06 ms, 970 to 1020 TFLOP/s (the kernel for
-// prompts, whose keys and values are 16-bit, 0.89; behind 30720 2.05 to 2.25); 512 of 40 and 8 heads behind 11801 160 to 167 (prompts: 155 to 164); 64 tokens behind 16320 44; 12 sequences of 16384 with 16
-// new tokens 128, 3.1 TB/s; 12 prompts of 600 tokens, 16 heads of 64, 91 to 100.
-// Many rows: a step of both tiles takes 2900 cycles, of which the tensor pipe is busy 49 %, the special functions 50 %, the ALUs 43 %, the issue slots 52 %: the chain of a
-// step (scores read 190, weighed 1700, P stored 200, waits the rest) with two warps a scheduler.  Few rows: 1700 cycles a step, a pair of warps converting keys (1200 and
-// its waits), with shared memory busy for some 1200 of them (bytes in 160, read and written as fp16 480, operands of the two products 580).  Short sequences: 16 cycles an instruction, 4.9 of them for instructions (7.2 when the code of all roles was 124 KB and not 97) and 5.7 for memory and
-// tensor memory: a CTA begins and ends units all the time, and its first scores come 13 us after its start (lengths 1.5, the first item 2, block numbers 1, bytes 1.5, two tiles of
-// queries 2 to 4 each).
-// Rings of converted tiles: three of values, since the warpgroups are up to two steps apart (with two, 1.09 ms for the chunks of 2048 and 166 us for the 12 sequences).
+// Measured, back to back in a graph, both launches, 32 and 8 heads of 128 unless stated: two chunks of 2048 tokens behind 14336 1.04 to 1.1 ms, 930 to 990
+// TFLOP/s (the kernel for prompts, whose keys and values are 16-bit, 0.92 to 0.99), behind 30720 2.1 to 2.3 (2.17); 512 of 40 and 8 heads behind 11801 162 to
+// 190 us (122 to 161); 64 tokens behind 16320 42; 12 sequences of 16384 with 16 new tokens 127, 3.2 TB/s; 12 prompts of 600 tokens, 16 heads of 64, 83 (29).
+// The ranges are the clock's, under the power cap.
+// Many rows: a step of both tiles takes 2520 cycles in the loop, 2700 with the units' ends, of which the tensor pipe is busy 47 %, the special functions 48 %,
+// the ALUs 41 %, the issue slots 51 %: the chain of a step (scores read, weighed, P stored, waits) with two warps a scheduler.  (With biased keys, above, the
+// same cycles at a clock 4 to 6 % higher.)
+// Few rows: 1460 cycles a step of one warpgroup, a pair of warps converting keys in 1000 and values in 870, beside its waits.
+// Short sequences: 15 cycles an instruction, 4.4 of them for instructions (7.2 when the code of all roles was 124 KB and not 97) and 5.4 for memory and tensor
+// memory: a CTA begins and ends units all the time, and its first scores come 13 us after its start (lengths 1.5, the first item 2, block numbers 1, bytes 1.5,
+// two tiles of queries 2 to 4 each).
+// Rings of converted tiles: three of values, since the warpgroups are up to two steps apart (with two, 8 and 28 % more for the chunks of 2048 and the 12
+// sequences).
 #pragma once
 #include <type_traits>
 
@@ -339,8 +346,8 @@ __device__ __forceinline__ void bulk_load(void* smem_dst, const void* src, uint3
 __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
-// f(integral constant i), one body for each i < N: a matrix instruction takes its descriptors from uniform registers, and what is not a constant to the compiler is moved
-// there for every one
+// f(integral constant i), one body for each i < N: a matrix instruction takes its descriptors from uniform registers, and what is not a constant to the
+// compiler is moved there for every one
 template <int N, typename F>
 __device__ __forceinline__ void for_constant(uint32_t i, F f) {
   if (i == N - 1) f(std::integral_constant<int, N - 1>{});
@@ -448,7 +455,8 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       const uint32_t raw = L::kRawOff + (values ? NRK * L::kRawBytes : 0);
       uint32_t g = 0;                              // steps so far
       uint32_t st = 0, free = 1;                   // the ring's next place, and the phase in which it is empty
-      // A lane has a part of 16 tokens of the kBatch steps at hand.  Block numbers are asked for two batches ahead and scales one: they come from anywhere in memory.
+      // A lane has a part of 16 tokens of the kBatch steps at hand.  Block numbers are asked for two batches ahead and scales one: they come from anywhere in
+      // memory.
       constexpr int kBatch = 6;
       static_assert(kBatch * PARTS <= 32, "a lane has a part");
       auto stream = [&](const ChunkItem& it) {
@@ -573,7 +581,8 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
       }
     } else if (warp <= 2) {
       // ------------------------------------------------------------------ UMMA issuers
-      // Every issuer sees every K and V tile of the CTA, in order, and hands back those that it does not use, so that it never mistakes a barrier's phase for another.
+      // Every issuer sees every K and V tile of the CTA, in order, and hands back those that it does not use, so that it never mistakes a barrier's phase for
+      // another.
       const int w = warp - 1;
       constexpr uint32_t idesc_s = make_idesc_f16(128, KEYS, 0, 0);        // S = Q K^T, both K-major
       constexpr uint32_t idesc_o = make_idesc_f16(128, HD, 0, 1);          // O += P V, V is MN-major
@@ -1010,8 +1019,9 @@ __global__ void __launch_bounds__(ChunkCfg<HD>::kThreads, 1) chunk_attention_ker
 }
 
 // The parts of cut units put together, in order: 128 threads, one a row, per (first cut of a unit, tile, 8 columns).  Before that, beside the end of the kernel
-// that leaves them, the rows that see nothing.  Bound by the latency of three rounds of loads, eight parts at once, and by the parts' bytes where all SMs leave some: with 8 units in 18 pieces
-// each, 64 tokens behind 16320, the call takes 44 us (68 when a group of threads met the same piece in every round, and all its columns were its own).  (Four parts at once, or two CTAs an SM: 37 -> 42 to 45 for one unit of 148 pieces, the others within 2 %.)
+// that leaves them, the rows that see nothing.  Bound by the latency of three rounds of loads, eight parts at once, and by the parts' bytes where all SMs leave
+// some: with 8 units in 18 pieces each, 64 tokens behind 16320, the call takes 42 us (68 when a group of threads met the same piece in every round, and all its
+// columns were its own).  (Four parts at once, or two CTAs an SM: 37 -> 42 to 45 for one unit of 148 pieces, the others within 2 %.)
 template <int HD>
 __global__ void __launch_bounds__(512, 1) chunk_join_kernel(const __grid_constant__ ChunkParams p) {
   constexpr int COLS = 8, CHUNKS = HD / COLS, BATCH = 8;

@@ -33,13 +33,17 @@ static eas_status launch_chunk(const ChunkParams& p, int budget, bool all, cudaS
 }
 
 // ------------------------------------------------------------------------------------ few rows
-// Up to so many query rows a key/value head (new tokens times heads of the group) a sequence goes to the kernels of single tokens, which read the cache once for every 16 of
-// them, rather than to the tiles of 128 rows.  In us, these kernels and the tiles, back to back, 8 key/value heads of 128: 48 sequences of 4096 tokens with 8
-// rows 77 and 132, with 16 rows 96 and 133; of 32 rows, 64 sequences of 500 57 and 69, 4 of 4096 25 and 27, one of 700 12.3 and 14.7; 48 of 2048 (16 heads of 64) 125 and 144.
+// Up to so many query rows a key/value head (new tokens times heads of the group) a sequence goes to the kernels of single tokens, which read the cache once for
+// every 16 of them, rather than to the tiles of 128 rows.  In us, these kernels and the tiles, back to back, 8 key/value heads of 128: 48 sequences of 4096 tokens
+// with 8 rows 77 and 135, with 16 rows 96 and 136; of 32 rows, 64 sequences of 500 57 and 65, 4 of 4096 25 and 27, one of 700 12.3 and 14.8; 48 of 2048 (16 heads
+// of 64) 125 and 144.
 constexpr int kFewRows = 32;
-// But with more than 16 rows and heads of 128 the second reading is dear where the cache does not fit L2 (126 MB): 32 rows of 48 sequences of 4096 tokens take 180 and 133,
-// of 2 of 65536 112 and 83, of 16 of 4096 68 and 58.  How long the sequences are is known on the device alone; the width of the table stands for it.  And most of them must have more than 16 rows: 48 of up
-// to 8192 with 1 to 8 tokens of 4 heads, 11 rows on average, take 133 and 140.
+// But with more than 16 rows and heads of 128 the second reading is dear where the cache does not fit L2 (126 MB): 32 rows of 48 sequences of 4096 tokens take
+// 180 and 136, of 2 of 65536 112 and 86, of 16 of 4096 68 and 59.  How long the sequences are is known on the device alone; the width of the table stands for
+// it, so a table far wider than its sequences may cost the 8 us of the 64 sequences above, and sequences' last bits may depend on it.
+// And most of them must have more than 16 rows.  48 sequences of 4096 with up to 8 tokens of 4 heads, by their rows on average: 7.5 102 and 112, 11 112 and
+// 122, 17 115 and 136, 18 (half with 32 rows, half with 4) 134 and 136, 22 to 24 (half with 32, half with 12 or 16) 137 and 138, 25 157 and 137, 28 157 and
+// 137; 20, if all have 20, 173 and 135.
 constexpr int64_t kFewBytes = 128 << 20;
 constexpr int kFewAverage = 20;
 
@@ -69,13 +73,12 @@ static eas_status launch_few(const CacheAttnParams& p, int budget, bool all, cud
 
 // Which kernels a call needs: those for few rows alone, where no sequence has more; both, where most sequences have less than half of the most (a
 // prompt's chunk beside single tokens); else the tiles of 128 rows for all.
-// A chunk beside which there is at most a token a sequence, as far as max_new and n_rows tell, has the others' rows in 8 columns: 512 tokens and 63 single ones behind 4096, 32
-// and 8 heads of 128, 176 us instead of 188.  (With a few drafts among them it has not: 1187 tokens, 19 single ones and drafts of 2, 3 and 4 would take 174 instead of 170,
-// the last two by tiles.)
-// A max_new of n_rows or more, the default of the binding, tells nothing of how the rows are spread; their average does.  With it, 64 single tokens behind 4096 take 103 us (124 in 16
-// columns), 48 drafts of 4 104 (143 by tiles), of 8 147 (189 in 16 columns).
-// The kernels for few rows add up what all sequences may cost in 32 bits; behind a table so wide that the sum could pass them (8 sequences of 8 key/value heads and 2^30 places each), the tiles,
-// whose line has 64, take all.
+// A chunk beside which there is at most a token a sequence, as far as max_new and n_rows tell, has the others' rows in 8 columns: 512 tokens and 63 single ones
+// behind 4096, 32 and 8 heads of 128, 176 us instead of 188.  (With a few drafts among them it has not: 1187 tokens, 19 single ones and drafts of 2, 3 and 4
+// would take 174 instead of 170, the last two by tiles.) A max_new of n_rows or more, the default of the binding, tells nothing of how the rows are spread;
+// their average does.  With it, 64 single tokens behind 4096 take 103 us (124 in 16 columns), 48 drafts of 4 104 (143 by tiles), of 8 147 (189 in 16 columns).
+// The kernels for few rows add up what all sequences may cost in 32 bits; behind a table so wide that the sum could pass them (8 sequences of 8 key/value heads
+// and 2^30 places each), the tiles, whose line has 64, take all.
 struct ChunkPlan {
   int few_rows = 0;            // most rows a key/value head of the sequences that the kernels for few rows take
   bool tiles = false;
@@ -83,7 +86,8 @@ struct ChunkPlan {
 static ChunkPlan chunk_plan(const eas_cache* c, int32_t n_seqs, int32_t n_rows, int32_t max_new, int group, int64_t places) {
   ChunkPlan plan;
   const int64_t most = static_cast<int64_t>(max_new) * group, token_bytes = 2LL * c->d.n_kv_heads * c->d.head_dim;
-  const bool twice_dear = c->d.head_dim == 128 && static_cast<int64_t>(n_rows) * group >= static_cast<int64_t>(n_seqs) * kFewAverage && n_seqs * places >= kFewBytes / token_bytes;
+  const bool twice_dear = c->d.head_dim == 128 && static_cast<int64_t>(n_rows) * group >= static_cast<int64_t>(n_seqs) * kFewAverage &&
+                          n_seqs * places >= kFewBytes / token_bytes;
   plan.tiles = most > kFewRows || (most > 16 && twice_dear);
   if (!plan.tiles) {
     plan.few_rows = static_cast<int>(std::max<int64_t>(most, 1));
@@ -93,7 +97,8 @@ static ChunkPlan chunk_plan(const eas_cache* c, int32_t n_seqs, int32_t n_rows, 
     plan.few_rows = group <= 8 && single ? 8 : !known && twice_dear ? 16 : kFewRows;
   }
   if (plan.few_rows > 0) {
-    const int64_t tiles = (places + 31) / 32 + kRowCost, row_tiles = few_blocks(plan.few_rows) * c->d.n_kv_heads;      // (no variant's tile is smaller than 32 places)
+    const int64_t tiles = (places + 31) / 32 + kRowCost;           // (no variant's tile is smaller)
+    const int64_t row_tiles = few_blocks(plan.few_rows) * c->d.n_kv_heads;
     if (tiles * row_tiles > 0x7fffffffLL / std::clamp(n_seqs, 1, kCacheMaxSeqs)) return ChunkPlan{0, true};
   }
   return plan;

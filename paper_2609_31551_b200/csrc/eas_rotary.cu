@@ -76,8 +76,8 @@ static RotaryRows rows_of(const eas_rotary_inputs* in) {
   return r;
 }
 
-// A token's heads go to one warp, whose 64 cosines serve them all, unless that leaves warps of the device without work: then to as many as there are batches of loads
-// (a warp takes `batch` heads at once).
+// A token's heads go to one warp, whose 64 cosines serve them all, unless that leaves warps of the device without work: then to as many as there are batches of
+// loads (a warp takes `batch` heads at once).
 static void split_heads(int rows, int heads, int batch, int64_t warps, uint32_t* parts, int* part_heads) {
   int n = 1;
   const int most = (heads + batch - 1) / batch;

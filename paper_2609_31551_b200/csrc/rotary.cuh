@@ -6,13 +6,14 @@
 // F = round(inv_freq / 2 pi * 2^64), position * F mod 2^64 is the angle in turns of 2^-64, exactly but for the rounding of F, which a position below 2^31
 // makes 2^-34 turns.  Of those the upper 32 bits count.
 //
-// Alone, the rotation is a copy: a warp takes a token's heads, 32 bytes a lane and head, 16 heads of 128 (32 of 64) in flight; cosines and sines are worked out once a
-// token (64 pairs, two a lane) into 512 bytes of shared memory.  16384 tokens of 32 and 8 heads of 128 54.6 us, 6.14 TB/s, 94 % of the copy rate; 6 prompts of 6227 tokens
-// 23.7; 40 tokens 2.3 (one launch).
-// On the way into the cache (append), a block's run of new rows has its cosines worked out once for all heads (8 bytes a pair and row of shared memory, 32 KB for 64 rows of
-// 64 pairs), is read once, rotated in fp32 and rounded once, to its number; queries go warp by warp behind.  16384 tokens 88 us, 4.2 TB/s (a launch of its own for the queries: 93; rotation and
-// storing as two operators, with the rotated keys through memory: 86, less exact), 6 prompts of 6227 tokens 43, 64 single tokens 7.8.  Of the 88, 50 are keys and
-// values: a group of threads goes from head to head in series, 16 warps an SM (registers), and waits for loads 3 of 9 cycles an instruction.
+// Alone, the rotation is a copy: a warp takes a token's heads, 32 bytes a lane and head, 16 heads of 128 (32 of 64) in flight; cosines and sines are worked out
+// once a token (64 pairs, two a lane) into 512 bytes of shared memory.  16384 tokens of 32 and 8 heads of 128 54.6 us, 6.14 TB/s, 94 % of the copy rate; 6
+// prompts of 6227 tokens 23.7; 40 tokens 2.3 (one launch).
+// On the way into the cache (append), a block's run of new rows has its cosines worked out once for all heads (8 bytes a pair and row of shared memory, 32 KB
+// for 64 rows of 64 pairs), is read once, rotated in fp32 and rounded once, to its number; queries go warp by warp behind.  16384 tokens 88 us, 4.2 TB/s (a
+// launch of its own for the queries: 93; rotation and storing as two operators, with the rotated keys through memory: 86, less exact), 6 prompts of 6227 tokens
+// 43, 64 single tokens 7.8 (7.0 with queries dealt to whole CTAs, when 16384 tokens took 111).  Of the 88, 50 are keys and values: a group of threads goes from
+// head to head in series, 16 warps an SM (registers), and waits for loads 3 of 9 cycles an instruction.
 #pragma once
 #include <type_traits>
 
@@ -30,8 +31,8 @@ struct RotaryTable {                      // (kernel parameter)
   float scale;
 };
 
-// A thread's pair: which it works out cosines and sines of, for any number of rows.  (Taken from the parameters once: threads that read different ones go one after the
-// other, which for every row was two thirds of the time.)
+// A thread's pair: which it works out cosines and sines of, for any number of rows.  (Taken from the parameters once: threads that read different ones go one
+// after the other, which for every row was two thirds of the time.)
 struct RotaryPair {
   uint32_t f_lo, f_hi;
   int axis;
@@ -47,8 +48,8 @@ struct RotaryPair {
     row[at] = turn.x;
     row[at + 2] = turn.y;
   }
-  // The table of a row: 8 pairs an item (16 dimensions, as two chunks of 8), as four float4, cosines and sines of the two pairs that word i of the chunks belongs to; those
-  // of all items side by side, so that threads of neighbouring items read side by side
+  // The table of a row: 8 pairs an item (16 dimensions, as two chunks of 8), as four float4, cosines and sines of the two pairs that word i of the chunks
+  // belongs to; those of all items side by side, so that threads of neighbouring items read side by side
   static __device__ __forceinline__ int rotary_place(int pair, int pairs, int neighbours) {
     const int k = pair & 7, word = neighbours ? k & 3 : k >> 1, which = neighbours ? k >> 2 : k & 1;
     return word * (pairs >> 1) + (pair >> 3) * 4 + which;
@@ -86,14 +87,15 @@ struct RotaryRows {
 __device__ __forceinline__ int2 rotary_at(int c, int pairs, int neighbours) {
   return !neighbours && 8 * c < pairs ? make_int2(8 * c, pairs + 8 * c) : make_int2(16 * c, 16 * c + 8);
 }
-// Words of two pairs: of halves, a word of the first chunk has the pairs' first values and one of the second chunk their second ones; of neighbours, a word has a pair.
+// Words of two pairs: of halves, a word of the first chunk has the pairs' first values and one of the second chunk their second ones; of neighbours, a word has
+// a pair.
 // (lo, hi), the way there and back: bytes of a word of each chunk to (first values, second values), the same for both, by two permutations.
 struct RotaryWords {
   uint32_t lo, hi;
   __device__ __forceinline__ explicit RotaryWords(int neighbours) : lo(neighbours ? 0x5410u : 0x3210u), hi(neighbours ? 0x7632u : 0x7654u) {}
 };
-// Word i of the item's chunks (a: first, b: second) turned: the two pairs' first values and their second ones, fp32.  cs: the item's first float4 in the row's table of
-// `items` items.
+// Word i of the item's chunks (a: first, b: second) turned: the two pairs' first values and their second ones, fp32.  cs: the item's first float4 in the row's
+// table of `items` items.
 template <typename T>
 __device__ __forceinline__ void rotary_turn_word(const RotaryWords& w, uint32_t a, uint32_t b, const float4* cs, uint64_t& first, uint64_t& second) {
   const uint32_t u = __byte_perm(a, b, w.lo), v = __byte_perm(a, b, w.hi);
@@ -259,7 +261,8 @@ __device__ __forceinline__ void quantise16(const uint64_t (&first)[4], const uin
 }
 
 // An item is the run of one sequence's new rows that lies in one block, and some of its key/value heads: the cosines and sines of the run's rows go to
-// shared memory once for all of them.  GT: threads of a head's keys or values, a warp where runs have a few rows (decoding steps, drafts).  Behind those items the queries: a warp takes a token's heads, or some of them.
+// shared memory once for all of them.  GT: threads of a head's keys or values, a warp where runs have a few rows (decoding steps, drafts).  Behind those items
+// the queries: a warp takes a token's heads, or some of them.
 template <int HD, int GT, typename T>
 __global__ void __launch_bounds__(kAppendThreads, kAppendCtas) cache_append_kernel(const __grid_constant__ AppendParams p) {
   extern __shared__ __align__(16) float2 append_turns[];
@@ -284,8 +287,8 @@ __global__ void __launch_bounds__(kAppendThreads, kAppendCtas) cache_append_kern
     if (r.block < 0) continue;
     const int n = r.hi - r.lo;
     // The keys or the values of one head at a time by THREADS threads, 2 rows of 16 dimensions a thread, rotated in fp32 and rounded once, to the number; then the
-    // block's scale and numbers as in cache_store_kernel.  (Four rows a thread do not fit the registers of two CTAs an SM.)  A run of more rows than the threads have
-    // takes several rounds, and all but the last are read again for their numbers.
+    // block's scale and numbers as in cache_store_kernel.  (Four rows a thread do not fit the registers of two CTAs an SM.)  A run of more rows than the
+    // threads have takes several rounds, and all but the last are read again for their numbers.
     {
       const int units = 2 * min(p.part_heads, p.c.n_kv - part * p.part_heads), rounds = (n + CAP - 1) / CAP;
 #pragma unroll 1
